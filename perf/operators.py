@@ -98,7 +98,8 @@ def draw(rng):
                          y=rng.choice(["bf16", "fp32"]), train=rng.random() < 0.5)
             else:
                 c["weight"] = rng.choice(["bf16", "bf16", "int8"])
-                c["hidden"] = 512 * rng.randint(1, 8) if c["weight"] == "bf16" else 1024 * rng.randint(1, 4)
+                # (the widths that blobs have)
+                c["hidden"] = rng.choice([512, 1024, 2048, 4096] if c["weight"] == "bf16" else [1024, 2048, 4096])
                 c["inter"] = _spread(rng, 24, 14336 if c["weight"] == "int8" else 4096)
                 c["inter"] += -c["inter"] % 8 if c["weight"] == "int8" else 0
                 if kind == "experts":
