@@ -52,6 +52,8 @@ typedef struct moe_cache moe_cache_t; /* opaque, owned by the library */
 enum moe_status { MOE_OK = 0, MOE_EINVAL = -1, MOE_ENOMEM = -2, MOE_EHIP = -3, MOE_ESTATE = -4 };
 enum moe_weight_fmt { MOE_W_FP32 = 0, MOE_W_BF16 = 1, MOE_W_INT8_PC = 2, MOE_W_INT4_G128 = 3 };
 enum moe_act_fmt { MOE_A_FP32 = 0, MOE_A_BF16 = 1 };
+/* elements of rows (the row operators below); 8-bit codes stand for code * scale of their row */
+enum moe_row_fmt { MOE_R_FP32 = 0, MOE_R_BF16 = 1, MOE_R_INT8 = 2 };
 /* The logit range Delta that scales the prior (Eq. 9-10; App. D on the choice of the estimate): the running mean
  * over the tokens seen since the last reset (the paper's method), a fixed value given by the caller (e.g. from a
  * calibration set), or the current token's own range max z - min z. */
@@ -317,6 +319,80 @@ int moe_cache_fill_form(moe_cache_t *ctx, int32_t *out_host);
  * timed between two resets, later ones run untimed.  Each timed launch is preceded by a 50 us hold of the stream,
  * so that the kernel is already queued behind its start marker when the device reaches the marker. */
 int moe_cache_profile(moe_cache_t *ctx, int32_t enable, int32_t reset, double *avg_us, int64_t *launches);
+
+/* ---- Many rows at once: a layer of a long prompt or of a training batch whose experts are all in device memory ----
+ *
+ * The calls below need no context, allocate nothing and wait for nothing: they check their arguments (MOE_EINVAL), enqueue
+ * their kernels on `stream` (whose device must be current) and return; all pointers are device memory.  They may be captured
+ * into a graph.  Rows are dense (row i at i * hidden elements) where no stride is given; strides count elements.
+ * hidden <= 8192, n_rows and n_tokens * top_k < 2^26, experts <= 512, top_k <= 8.  Elements are aligned to their type; rows
+ * whose addresses and width allow 16-byte accesses are faster.  n_rows or n_tokens 0 is no error.
+ * Sums and statistics are held in 32 bits; results are the same bit for bit from call to call.
+ *
+ * moe_norm_rows: h_out = h + y (rounded to h_fmt), x = h_out * rstd * gain, rstd = 1 / sqrt(mean(h_out^2) + eps).
+ *   y_dev NULL: h_out = h, h_out_dev may then be NULL.  gain_dev (fp32 [hidden]) NULL: ones.  h_fmt, y_fmt: fp32 or bf16.
+ *   h_out_dev may be h_dev itself where h_stride is hidden.  rstd_dev (fp32 [n_rows]) may be NULL; the backward needs it.
+ *   x_fmt MOE_R_INT8: with v = h_out * gain and top the largest |v| of the row, code = round(v * (127 * (1 / top))) (32-bit steps, to even) and
+ *   scale_dev[row] = top / 127 * rstd, so that code * scale stands for x.  A row with top < 1e-30 has codes and scale 0, one
+ *   that holds an infinity or NaN codes 0 and scale NaN.  Other formats: scale_dev is NULL.
+ * moe_norm_rows_backward: gradients of h (and of y) and of gain, from those of x and of h_out:
+ *   n = h_out * rstd, dh = dh_out + rstd (dx gain - n mean(dx gain n)), dgain = sum over the rows of dx n (fp32 [hidden]).
+ *   h_out_dev, rstd_dev: as moe_norm_rows left them.  dx_dev: x_fmt fp32 or bf16.  dh_in_dev (h_fmt, the gradient of h_out) may
+ *   be NULL, and so may dgain_dev.  dh_dev: h_fmt, may be dh_in_dev.  With dgain_dev a workspace of
+ *   moe_norm_rows_backward_bytes(n_rows, hidden) bytes, 16-byte aligned, is needed. */
+int moe_norm_rows(const void *h_dev, int32_t h_fmt, int64_t h_stride, const void *y_dev, int32_t y_fmt, int64_t y_stride,
+                  const float *gain_dev, float eps, int32_t n_rows, int32_t hidden, void *h_out_dev, void *x_dev, int32_t x_fmt,
+                  float *scale_dev, float *rstd_dev, void *stream);
+size_t moe_norm_rows_backward_bytes(int32_t n_rows, int32_t hidden);
+int moe_norm_rows_backward(const void *h_out_dev, int32_t h_fmt, const float *gain_dev, const float *rstd_dev, const void *dx_dev,
+                           int32_t x_fmt, const void *dh_in_dev, int32_t n_rows, int32_t hidden, void *dh_dev, float *dgain_dev,
+                           void *workspace_dev, size_t workspace_bytes, void *stream);
+
+/* Tokens sorted by expert.  ids_dev [n_tokens, top_k]: the expert of each place (token, k); an id outside 0..n_experts-1 (-1)
+ * is a place without an expert.  An expert's rows are its places in the order of the tokens:
+ *   offsets_dev [n_experts + 1]       expert e has rows offsets[e] .. offsets[e + 1] - 1
+ *   row_of_dev  [n_tokens, top_k]     row of each place, -1: none
+ *   entry_of_dev [n_tokens * top_k]   place (token * top_k + k) of each row, -1: a row of nobody (those come last)
+ * The workspace: moe_sort_tokens_bytes bytes, 4-byte aligned (0: none needed).
+ * moe_gather_rows: xs[row_of[t, k]] = x[t] for elements of any moe_row_fmt, scale_dev [n_tokens] -> xs_scale_dev likewise
+ *   (both NULL: none); rows of nobody are zeros.  xs_dev: [n_tokens * top_k, hidden].  Its gradient is moe_combine_rows of the
+ *   gradients of xs with weight_dev NULL.
+ * moe_combine_rows: y[t] = base[t] + sum over k of weight[t, k] * ys[row_of[t, k]], the places without a row left out whatever
+ *   their weight is.  weight_dev (fp32) NULL: ones; base_dev (y_fmt, may be y_dev) NULL: zeros.  Formats: fp32 or bf16.
+ * moe_combine_rows_backward: dys[row_of[t, k]] = weight[t, k] * dy[t] (rows of nobody: zeros) and
+ *   dweight[t, k] = <dy[t], ys[row_of[t, k]]> (places without a row: 0; dweight_dev and ys_dev NULL: not wanted).  The gradient
+ *   of base is dy itself. */
+size_t moe_sort_tokens_bytes(int32_t n_tokens, int32_t top_k, int32_t n_experts);
+int moe_sort_tokens(const int32_t *ids_dev, int32_t n_tokens, int32_t top_k, int32_t n_experts, int32_t *offsets_dev,
+                    int32_t *row_of_dev, int32_t *entry_of_dev, void *workspace_dev, size_t workspace_bytes, void *stream);
+int moe_gather_rows(const void *x_dev, int32_t fmt, int64_t x_stride, const float *scale_dev, const int32_t *row_of_dev,
+                    const int32_t *offsets_dev, int32_t n_tokens, int32_t top_k, int32_t n_experts, int32_t hidden, void *xs_dev,
+                    float *xs_scale_dev, void *stream);
+int moe_combine_rows(const void *ys_dev, int32_t ys_fmt, const int32_t *row_of_dev, const float *weight_dev, const void *base_dev,
+                     int32_t n_tokens, int32_t top_k, int32_t hidden, void *y_dev, int32_t y_fmt, void *stream);
+int moe_combine_rows_backward(const void *dy_dev, int32_t dy_fmt, const void *ys_dev, int32_t ys_fmt, const int32_t *row_of_dev,
+                              const int32_t *offsets_dev, const float *weight_dev, int32_t n_tokens, int32_t top_k,
+                              int32_t n_experts, int32_t hidden, void *dys_dev, float *dweight_dev, void *stream);
+
+/* The SwiGLU experts on sorted rows (Eq. 1 without the weighted sum): ys[r] = E_e(xs[r]) for offsets[e] <= r < offsets[e + 1],
+ * zeros for the rows of nobody.  blobs_dev: packed experts (moe_pack_expert), expert e at e * blob_stride bytes, 16-byte aligned;
+ * e.g. a slot pool that holds all experts.  hidden and inter as moe_blob_bytes takes them, one blob smaller than 4 GB.
+ *   MOE_W_BF16     xs_dev bf16, scale_dev NULL
+ *   MOE_W_INT8_PC  xs_dev 8-bit codes with a scale for each row (moe_norm_rows, moe_gather_rows).  The sums of the first product
+ *                  are whole numbers and exact; h is bf16.
+ * Other formats are refused.  ys_dev: bf16.  xs_dev and ys_dev 16-byte aligned.
+ * h_dev: bf16 [n_rows, pitch], pitch = inter rounded up to a multiple of 64: the products silu(g) * u as the down projection reads
+ * them.  gu_dev: bf16 [n_rows, 2, pitch]: g and u, for the backward, or NULL.  Both 16-byte aligned; the caller keeps them for the
+ * backward or throws them away.
+ * moe_experts_rows_backward (MOE_W_BF16): from dys the gradients of xs and, in the layout of the blobs, of the weights (zeros
+ * for an expert without rows).  h_dev, gu_dev: as the forward left them; dgu_dev: workspace like gu_dev (may be gu_dev itself,
+ * which is then overwritten).  dxs_dev or dblobs_dev NULL: not wanted.  Rows of nobody: dxs is zero. */
+int moe_experts_rows(int32_t weight_fmt, int32_t hidden, int32_t inter, int32_t n_experts, const void *blobs_dev, int64_t blob_stride,
+                     const void *xs_dev, const float *scale_dev, const int32_t *offsets_dev, int32_t n_rows, void *h_dev, void *gu_dev,
+                     void *ys_dev, void *stream);
+int moe_experts_rows_backward(int32_t weight_fmt, int32_t hidden, int32_t inter, int32_t n_experts, const void *blobs_dev,
+                              int64_t blob_stride, const void *xs_dev, const int32_t *offsets_dev, int32_t n_rows, const void *h_dev,
+                              const void *gu_dev, const void *dys_dev, void *dgu_dev, void *dxs_dev, void *dblobs_dev, void *stream);
 
 const char *moe_last_error(void);
 

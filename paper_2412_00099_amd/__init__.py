@@ -6,3 +6,7 @@ built the import raises, naming the build command.
 from .binding import *  # noqa: F401,F403
 from .binding import LIB_PATH, lib  # noqa: F401
 from .runtime import ExpertStore, MoEDecoder  # noqa: F401
+from .rows import (  # noqa: F401
+    KeptExperts, NormedRows, TokenOrder, combine_rows, combine_rows_backward, experts_rows, experts_rows_backward, gather_rows,
+    norm_rows, norm_rows_backward, sort_tokens,
+)

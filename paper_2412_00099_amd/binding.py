@@ -17,6 +17,7 @@ MOE_MAX_TOPK = 8
 MOE_OK, MOE_EINVAL, MOE_ENOMEM, MOE_EHIP, MOE_ESTATE = 0, -1, -2, -3, -4
 MOE_W_FP32, MOE_W_BF16, MOE_W_INT8_PC, MOE_W_INT4_G128 = 0, 1, 2, 3
 MOE_A_FP32, MOE_A_BF16 = 0, 1
+MOE_R_FP32, MOE_R_BF16, MOE_R_INT8 = 0, 1, 2
 MOE_DELTA_RUNNING_MEAN, MOE_DELTA_FIXED, MOE_DELTA_TOKEN = 0, 1, 2
 MOE_ROUTE_CACHE_PRIOR, MOE_ROUTE_MAX_RANK, MOE_ROUTE_CUMSUM = 0, 1, 2
 MOE_POLICY_LRU, MOE_POLICY_FARTHEST = 0, 1
@@ -154,6 +155,27 @@ lib.moe_residual_rmsnorm.restype = C.c_int
 lib.moe_residual_rmsnorm.argtypes = [_vp, _vp, _vp, C.c_float, C.c_int32, _vp, C.c_int32, C.c_int32, _vp]
 lib.moe_cache_profile.restype = C.c_int
 lib.moe_cache_profile.argtypes = [_vp, C.c_int32, C.c_int32, C.POINTER(C.c_double), C.POINTER(C.c_int64)]
+_i32, _i64, _sz = C.c_int32, C.c_int64, C.c_size_t
+lib.moe_norm_rows.restype = C.c_int
+lib.moe_norm_rows.argtypes = [_vp, _i32, _i64, _vp, _i32, _i64, _vp, C.c_float, _i32, _i32, _vp, _vp, _i32, _vp, _vp, _vp]
+lib.moe_norm_rows_backward_bytes.restype = _sz
+lib.moe_norm_rows_backward_bytes.argtypes = [_i32, _i32]
+lib.moe_norm_rows_backward.restype = C.c_int
+lib.moe_norm_rows_backward.argtypes = [_vp, _i32, _vp, _vp, _vp, _i32, _vp, _i32, _i32, _vp, _vp, _vp, _sz, _vp]
+lib.moe_sort_tokens_bytes.restype = _sz
+lib.moe_sort_tokens_bytes.argtypes = [_i32, _i32, _i32]
+lib.moe_sort_tokens.restype = C.c_int
+lib.moe_sort_tokens.argtypes = [_vp, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _sz, _vp]
+lib.moe_gather_rows.restype = C.c_int
+lib.moe_gather_rows.argtypes = [_vp, _i32, _i64, _vp, _vp, _vp, _i32, _i32, _i32, _i32, _vp, _vp, _vp]
+lib.moe_combine_rows.restype = C.c_int
+lib.moe_combine_rows.argtypes = [_vp, _i32, _vp, _vp, _vp, _i32, _i32, _i32, _vp, _i32, _vp]
+lib.moe_combine_rows_backward.restype = C.c_int
+lib.moe_combine_rows_backward.argtypes = [_vp, _i32, _vp, _i32, _vp, _vp, _vp, _i32, _i32, _i32, _i32, _vp, _vp, _vp]
+lib.moe_experts_rows.restype = C.c_int
+lib.moe_experts_rows.argtypes = [_i32, _i32, _i32, _i32, _vp, _i64, _vp, _vp, _vp, _i32, _vp, _vp, _vp, _vp]
+lib.moe_experts_rows_backward.restype = C.c_int
+lib.moe_experts_rows_backward.argtypes = [_i32, _i32, _i32, _i32, _vp, _i64, _vp, _vp, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp]
 lib.moe_last_error.restype = C.c_char_p
 lib.moe_last_error.argtypes = []
 
@@ -162,6 +184,8 @@ EXPORTS = [
     "moe_expert_forward", "moe_route_batch", "moe_expert_forward_batch", "moe_expert_forward_static", "moe_cache_last_route", "moe_cache_stats", "moe_cache_tables", "moe_cache_snapshot",
     "moe_cache_restore", "moe_trace_misses", "moe_cache_plan", "moe_cache_boundary_form", "moe_cache_fill_form", "moe_cache_set_lambda",
     "moe_cache_set_baseline", "moe_cache_reset", "moe_residual_rmsnorm", "moe_cache_profile", "moe_last_error",
+    "moe_norm_rows", "moe_norm_rows_backward_bytes", "moe_norm_rows_backward", "moe_sort_tokens_bytes", "moe_sort_tokens",
+    "moe_gather_rows", "moe_combine_rows", "moe_combine_rows_backward", "moe_experts_rows", "moe_experts_rows_backward",
 ]
 
 
@@ -334,3 +358,59 @@ def moe_cache_profile(ctx, enable: int, reset: bool = True):
     avg, n = C.c_double(), C.c_int64()
     _check(lib.moe_cache_profile(ctx, int(enable), int(reset), C.byref(avg), C.byref(n)), "moe_cache_profile")
     return avg.value, n.value
+
+
+def moe_norm_rows(h_dev, h_fmt, h_stride, y_dev, y_fmt, y_stride, gain_dev, eps, n_rows, hidden, h_out_dev, x_dev, x_fmt,
+                  scale_dev, rstd_dev, stream) -> None:
+    _check(lib.moe_norm_rows(h_dev, h_fmt, h_stride, y_dev, y_fmt, y_stride, gain_dev, eps, n_rows, hidden, h_out_dev, x_dev,
+                             x_fmt, scale_dev, rstd_dev, stream), "moe_norm_rows")
+
+
+def moe_norm_rows_backward_bytes(n_rows: int, hidden: int) -> int:
+    return int(lib.moe_norm_rows_backward_bytes(n_rows, hidden))
+
+
+def moe_norm_rows_backward(h_out_dev, h_fmt, gain_dev, rstd_dev, dx_dev, x_fmt, dh_in_dev, n_rows, hidden, dh_dev, dgain_dev,
+                           workspace_dev, workspace_bytes, stream) -> None:
+    _check(lib.moe_norm_rows_backward(h_out_dev, h_fmt, gain_dev, rstd_dev, dx_dev, x_fmt, dh_in_dev, n_rows, hidden, dh_dev,
+                                      dgain_dev, workspace_dev, workspace_bytes, stream), "moe_norm_rows_backward")
+
+
+def moe_sort_tokens_bytes(n_tokens: int, top_k: int, n_experts: int) -> int:
+    return int(lib.moe_sort_tokens_bytes(n_tokens, top_k, n_experts))
+
+
+def moe_sort_tokens(ids_dev, n_tokens, top_k, n_experts, offsets_dev, row_of_dev, entry_of_dev, workspace_dev, workspace_bytes,
+                    stream) -> None:
+    _check(lib.moe_sort_tokens(ids_dev, n_tokens, top_k, n_experts, offsets_dev, row_of_dev, entry_of_dev, workspace_dev,
+                               workspace_bytes, stream), "moe_sort_tokens")
+
+
+def moe_gather_rows(x_dev, fmt, x_stride, scale_dev, row_of_dev, offsets_dev, n_tokens, top_k, n_experts, hidden, xs_dev,
+                    xs_scale_dev, stream) -> None:
+    _check(lib.moe_gather_rows(x_dev, fmt, x_stride, scale_dev, row_of_dev, offsets_dev, n_tokens, top_k, n_experts, hidden,
+                               xs_dev, xs_scale_dev, stream), "moe_gather_rows")
+
+
+def moe_combine_rows(ys_dev, ys_fmt, row_of_dev, weight_dev, base_dev, n_tokens, top_k, hidden, y_dev, y_fmt, stream) -> None:
+    _check(lib.moe_combine_rows(ys_dev, ys_fmt, row_of_dev, weight_dev, base_dev, n_tokens, top_k, hidden, y_dev, y_fmt, stream),
+           "moe_combine_rows")
+
+
+def moe_combine_rows_backward(dy_dev, dy_fmt, ys_dev, ys_fmt, row_of_dev, offsets_dev, weight_dev, n_tokens, top_k, n_experts,
+                              hidden, dys_dev, dweight_dev, stream) -> None:
+    _check(lib.moe_combine_rows_backward(dy_dev, dy_fmt, ys_dev, ys_fmt, row_of_dev, offsets_dev, weight_dev, n_tokens, top_k,
+                                         n_experts, hidden, dys_dev, dweight_dev, stream), "moe_combine_rows_backward")
+
+
+def moe_experts_rows(weight_fmt, hidden, inter, n_experts, blobs_dev, blob_stride, xs_dev, scale_dev, offsets_dev, n_rows, h_dev,
+                     gu_dev, ys_dev, stream) -> None:
+    _check(lib.moe_experts_rows(weight_fmt, hidden, inter, n_experts, blobs_dev, blob_stride, xs_dev, scale_dev, offsets_dev,
+                                n_rows, h_dev, gu_dev, ys_dev, stream), "moe_experts_rows")
+
+
+def moe_experts_rows_backward(weight_fmt, hidden, inter, n_experts, blobs_dev, blob_stride, xs_dev, offsets_dev, n_rows, h_dev,
+                              gu_dev, dys_dev, dgu_dev, dxs_dev, dblobs_dev, stream) -> None:
+    _check(lib.moe_experts_rows_backward(weight_fmt, hidden, inter, n_experts, blobs_dev, blob_stride, xs_dev, offsets_dev, n_rows,
+                                         h_dev, gu_dev, dys_dev, dgu_dev, dxs_dev, dblobs_dev, stream),
+           "moe_experts_rows_backward")

@@ -9,6 +9,14 @@
 
 namespace moe {
 
+// sets the calling thread's message (moe_last_error) and returns code
+int fail(int code, const char *fmt, ...);
+#define HIP_TRY(expr)                                                                        \
+  do {                                                                                       \
+    hipError_t e_ = (expr);                                                                  \
+    if (e_ != hipSuccess) return fail(MOE_EHIP, "%s: %s", #expr, hipGetErrorString(e_));     \
+  } while (0)
+
 constexpr int kWave = 64;
 
 // Per-layer cache state, device resident.  One wavefront owns it during a routing step:

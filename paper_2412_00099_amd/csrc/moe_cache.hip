@@ -22,6 +22,9 @@ namespace {
 
 thread_local std::string g_err;
 
+}  // namespace
+
+namespace moe {
 int fail(int code, const char *fmt, ...) {
   char buf[512];
   va_list ap;
@@ -31,12 +34,9 @@ int fail(int code, const char *fmt, ...) {
   g_err = buf;
   return code;
 }
+}  // namespace moe
 
-#define HIP_TRY(expr)                                                                        \
-  do {                                                                                       \
-    hipError_t e_ = (expr);                                                                  \
-    if (e_ != hipSuccess) return fail(MOE_EHIP, "%s: %s", #expr, hipGetErrorString(e_));     \
-  } while (0)
+namespace {
 
 // Keeps the compute stream busy for about `ticks` periods of the 100 MHz wall clock (bounded by the iteration
 // count whatever the clock does).  Enqueued ahead of a launch that is timed with events: the start event of such

@@ -1,0 +1,395 @@
+// Tokens sorted by the expert that takes them, their rows brought into that order and the results brought back.
+//
+// A place is a token's k-th choice, place = token * top_k + k.  The sort is a stable counting sort: an expert's rows come in
+// the order of the tokens, so the result does not depend on timing (no atomics).  Places without an expert (an id outside
+// 0..n_experts-1) have no row; as many rows at the end of the order belong to nobody and are filled with zeros.
+#include "rows.h"
+
+namespace moe {
+namespace {
+
+constexpr int kSortWaves = 16, kSortThreads = kSortWaves * 64;
+constexpr int kSortBlocks = 256;      // workgroups of the two-launch form at most
+constexpr int kSortSingle = 16384;    // places that one workgroup sorts by itself
+constexpr int kSortChunk = 4096;      // places a workgroup takes at least in the two-launch form
+
+// Lanes of the wavefront that hold the same key as this one.  BITS: bits of a key.
+template <int BITS>
+__device__ __forceinline__ uint64_t same_key(int key) {
+  uint64_t m = ~0ull;
+#pragma unroll
+  for (int b = 0; b < BITS; ++b) {
+    const bool one = (key >> b) & 1;
+    const uint64_t v = __ballot(one);
+    m &= one ? v : ~v;
+  }
+  return m;
+}
+__device__ __forceinline__ int key_of(const int32_t *ids, int64_t at, int64_t end, int n_experts) {
+  const int id = at < end ? ids[at] : -1;
+  return (uint32_t)id < (uint32_t)n_experts ? id : n_experts;  // n_experts: no row
+}
+
+// counts[wave][expert] of the places begin..end, a contiguous part for each wavefront
+template <int BITS>
+__device__ __forceinline__ void count_places(const int32_t *ids, int64_t begin, int64_t end, int64_t per_wave, int n_experts, int *counts,
+                                             int pitch) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t w0 = begin + wave * per_wave, w1 = min(end, w0 + per_wave);
+  for (int64_t at = w0; at < w1; at += 64) {
+    const int key = key_of(ids, at + lane, w1, n_experts);
+    const uint64_t m = same_key<BITS>(key);
+    if (key < n_experts && (m & ((1ull << lane) - 1)) == 0) counts[wave * pitch + key] += __popcll(m);
+  }
+}
+// the same walk with counts turned into the first free row of each (wavefront, expert)
+template <int BITS>
+__device__ __forceinline__ void place_rows(const int32_t *ids, int64_t begin, int64_t end, int64_t per_wave, int n_experts, int *next, int pitch,
+                                           int32_t *row_of, int32_t *entry_of) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t w0 = begin + wave * per_wave, w1 = min(end, w0 + per_wave);
+  for (int64_t at = w0; at < w1; at += 64) {
+    const int key = key_of(ids, at + lane, w1, n_experts);
+    const uint64_t m = same_key<BITS>(key);
+    const uint64_t before = m & ((1ull << lane) - 1);
+    int row = -1;
+    if (key < n_experts) {
+      row = next[wave * pitch + key] + __popcll(before);
+      entry_of[row] = (int32_t)(at + lane);
+    }
+    if (at + lane < w1) row_of[at + lane] = row;
+    __builtin_amdgcn_wave_barrier();
+    if (key < n_experts && before == 0) next[wave * pitch + key] += __popcll(m);
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+// exclusive sum over the threads of the workgroup (1024); `s` holds 16 words
+__device__ __forceinline__ int block_scan(int v, int *s, int &total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int x = v;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int y = __shfl_up(x, o);
+    if (lane >= o) x += y;
+  }
+  if (lane == 63) s[wave] = x;
+  __syncthreads();
+  int before = 0, all = 0;
+  for (int w = 0; w < kSortWaves; ++w) {
+    const int c = s[w];
+    if (w < wave) before += c;
+    all += c;
+  }
+  total = all;
+  return before + x - v;
+}
+
+// BLOCKS = false: one workgroup sorts everything.  BLOCKS = true: workgroup b takes places b * chunk ..; hist [workgroups]
+// [n_experts] holds what each counts.
+template <int BITS, bool BLOCKS>
+__global__ __launch_bounds__(kSortThreads) void sort_kernel(const int32_t *ids, int64_t n, int n_experts, int64_t chunk, const int32_t *hist,
+                                                            int32_t *offsets, int32_t *row_of, int32_t *entry_of) {
+  extern __shared__ int counts[];  // [kSortWaves][n_experts], then 16 words
+  int *scratch = counts + kSortWaves * n_experts;
+  const int e = threadIdx.x;
+  const int64_t begin = BLOCKS ? blockIdx.x * chunk : 0, end = BLOCKS ? min(n, begin + chunk) : n;
+  const int64_t per_wave = ((end - begin + kSortWaves - 1) / kSortWaves + 63) / 64 * 64;
+  for (int i = threadIdx.x; i < kSortWaves * n_experts; i += kSortThreads) counts[i] = 0;
+  __syncthreads();
+  count_places<BITS>(ids, begin, end, per_wave, n_experts, counts, n_experts);
+  __syncthreads();
+  // this expert's places in all of the input and in the workgroups before this one
+  int all = 0, earlier = 0;
+  if (e < n_experts) {
+    if constexpr (BLOCKS) {
+      for (int b = 0; b < (int)gridDim.x; ++b) {
+        const int c = hist[b * n_experts + e];
+        all += c;
+        if (b < (int)blockIdx.x) earlier += c;
+      }
+    } else {
+      for (int w = 0; w < kSortWaves; ++w) all += counts[w * n_experts + e];
+    }
+  }
+  int total;
+  const int first = block_scan(all, scratch, total);
+  if (e < n_experts) {
+    if (blockIdx.x == 0) offsets[e] = first;
+    int at = first + earlier;
+    for (int w = 0; w < kSortWaves; ++w) {
+      const int c = counts[w * n_experts + e];
+      counts[w * n_experts + e] = at;
+      at += c;
+    }
+  }
+  if (blockIdx.x == 0 && e == 0) offsets[n_experts] = total;
+  __syncthreads();
+  place_rows<BITS>(ids, begin, end, per_wave, n_experts, counts, n_experts, row_of, entry_of);
+  // rows of nobody
+  for (int64_t r = total + (int64_t)blockIdx.x * kSortThreads + threadIdx.x; r < n; r += (int64_t)gridDim.x * kSortThreads) entry_of[r] = -1;
+}
+
+template <int BITS>
+__global__ __launch_bounds__(kSortThreads) void histogram_kernel(const int32_t *ids, int64_t n, int n_experts, int64_t chunk, int32_t *hist) {
+  extern __shared__ int counts[];
+  const int64_t begin = blockIdx.x * chunk, end = min(n, begin + chunk);
+  const int64_t per_wave = ((end - begin + kSortWaves - 1) / kSortWaves + 63) / 64 * 64;
+  for (int i = threadIdx.x; i < kSortWaves * n_experts; i += kSortThreads) counts[i] = 0;
+  __syncthreads();
+  count_places<BITS>(ids, begin, end, per_wave, n_experts, counts, n_experts);
+  __syncthreads();
+  if ((int)threadIdx.x < n_experts) {
+    int c = 0;
+    for (int w = 0; w < kSortWaves; ++w) c += counts[w * n_experts + threadIdx.x];
+    hist[blockIdx.x * n_experts + threadIdx.x] = c;
+  }
+}
+
+int64_t sort_chunk(int64_t n) {
+  const int64_t even = (n + kSortBlocks - 1) / kSortBlocks;
+  return even > kSortChunk ? (even + 1023) / 1024 * 1024 : kSortChunk;
+}
+
+// the row of place (t, k), -1: none (whatever lies outside the order counts as none)
+__device__ __forceinline__ int row_at(const OrderParams &o, int64_t t, int k) {
+  const int r = __builtin_amdgcn_readfirstlane(o.row_of[t * o.top_k + k]);
+  return (uint32_t)r < (uint32_t)o.n_tokens * (uint32_t)o.top_k ? r : -1;
+}
+// how many rows belong to somebody
+__device__ __forceinline__ int64_t rows_used(const OrderParams &o) { return max(0, o.offsets[o.n_experts]); }
+
+// ---- rows into the order ----
+// V: the widest unit that rows, strides and addresses allow (16, 4, 2 or 1 bytes).  A wavefront takes a token: it reads the row
+// once and writes it to each of its places.
+template <typename V>
+__global__ __launch_bounds__(256) void gather_kernel(const OrderParams o, const uint8_t *x, int64_t x_stride, int row_units, const float *scale,
+                                                     uint8_t *xs, float *xs_scale) {
+  const int lane = threadIdx.x & 63;
+  const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (t >= o.n_tokens) return;
+  int row[MOE_MAX_TOPK];
+#pragma unroll
+  for (int k = 0; k < MOE_MAX_TOPK; ++k) row[k] = k < o.top_k ? row_at(o, t, k) : -1;
+  const V *in = reinterpret_cast<const V *>(x + t * x_stride);
+  V *out = reinterpret_cast<V *>(xs);
+  constexpr int U = 4;  // units in flight per lane
+  for (int c = lane; c < row_units; c += 64 * U) {
+    V v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) v[u] = in[min(c + u * 64, row_units - 1)];
+#pragma unroll
+    for (int k = 0; k < MOE_MAX_TOPK; ++k) {
+      if (row[k] < 0) continue;
+      V *to = out + (int64_t)row[k] * row_units + c;
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (c + u * 64 < row_units) to[u * 64] = v[u];
+    }
+  }
+  if (scale && lane < o.top_k) {
+    const int r = o.row_of[t * o.top_k + lane];
+    if ((uint32_t)r < (uint32_t)o.n_tokens * (uint32_t)o.top_k) xs_scale[r] = scale[t];
+  }
+  // rows of nobody: as many as there are places without a row, one token's wavefront after the other
+  const int64_t n = (int64_t)o.n_tokens * o.top_k;
+  for (int64_t r = rows_used(o) + t; r < n; r += o.n_tokens) {
+    for (int c = lane; c < row_units; c += 64) out[r * row_units + c] = V{};
+    if (scale && lane == 0) xs_scale[r] = 0.f;
+  }
+}
+
+// ---- results back ----
+// y = base + sum over k of weight * row, in the order of k.  KC: top_k rounded up to a power of two.  Places without a row read
+// one that is there (or nothing at all if there is none) and are left out by a selection, not by a weight of 0.
+template <int YS, int Y, int VEC, int KC>
+__global__ __launch_bounds__(256) void combine_kernel(const OrderParams o, const void *ys, const float *weight, const void *base, void *y) {
+  const int lane = threadIdx.x & 63;
+  const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (t >= o.n_tokens) return;
+  const int d = o.hidden;
+  int row[KC];
+  float w[KC];
+  int some = -1;
+#pragma unroll
+  for (int k = 0; k < KC; ++k) {
+    row[k] = k < o.top_k ? row_at(o, t, k) : -1;
+    w[k] = weight && k < o.top_k ? weight[t * o.top_k + k] : 1.f;
+    if (row[k] >= 0) some = row[k];
+  }
+  for (int c = lane * VEC; c < d; c += 64 * VEC) {
+    float acc[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) acc[i] = 0.f;
+    if (some >= 0) {
+      float v[KC][VEC];
+#pragma unroll
+      for (int k = 0; k < KC; ++k) load_row<YS>(ys, (int64_t)(row[k] >= 0 ? row[k] : some) * d + c, v[k]);
+#pragma unroll
+      for (int k = 0; k < KC; ++k)
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) acc[i] = row[k] >= 0 ? __builtin_fmaf(w[k], v[k][i], acc[i]) : acc[i];
+    }
+    if (base) {
+      float b[VEC];
+      load_row<Y>(base, t * d + c, b);
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) acc[i] += b[i];
+    }
+    store_row<Y>(y, t * d + c, acc);
+  }
+}
+
+// dys[row] = weight * dy[token], dweight = <dy[token], ys[row]>
+template <int DY, int YS, int VEC>
+__global__ __launch_bounds__(256) void combine_backward_kernel(const OrderParams o, const void *dy, const void *ys, const float *weight, void *dys,
+                                                               float *dweight) {
+  const int lane = threadIdx.x & 63;
+  const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (t >= o.n_tokens) return;
+  const int d = o.hidden;
+  int row[MOE_MAX_TOPK];
+  float w[MOE_MAX_TOPK], dot[MOE_MAX_TOPK];
+#pragma unroll
+  for (int k = 0; k < MOE_MAX_TOPK; ++k) {
+    row[k] = k < o.top_k ? row_at(o, t, k) : -1;
+    w[k] = weight && k < o.top_k ? weight[t * o.top_k + k] : 1.f;
+    dot[k] = 0.f;
+  }
+  for (int c = lane * VEC; c < d; c += 64 * VEC) {
+    float g[VEC];
+    load_row<DY>(dy, t * d + c, g);
+#pragma unroll
+    for (int k = 0; k < MOE_MAX_TOPK; ++k) {
+      if (row[k] < 0) continue;
+      const int64_t at = (int64_t)row[k] * d + c;
+      float v[VEC];
+      if (dweight) {
+        load_row<YS>(ys, at, v);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) dot[k] = __builtin_fmaf(g[i], v[i], dot[k]);
+      }
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) v[i] = w[k] * g[i];
+      store_row<YS>(dys, at, v);
+    }
+  }
+  if (dweight) {
+#pragma unroll
+    for (int k = 0; k < MOE_MAX_TOPK; ++k) {
+      if (k >= o.top_k) continue;
+      const float s = wave_sum(dot[k]);
+      if (lane == 0) dweight[t * o.top_k + k] = row[k] >= 0 ? s : 0.f;
+    }
+  }
+  const int64_t n = (int64_t)o.n_tokens * o.top_k;
+  for (int64_t r = rows_used(o) + t; r < n; r += o.n_tokens) {
+    float zero[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) zero[i] = 0.f;
+    for (int c = lane * VEC; c < d; c += 64 * VEC) store_row<YS>(dys, r * d + c, zero);
+  }
+}
+
+bool aligned(const void *p, int by) { return reinterpret_cast<uintptr_t>(p) % by == 0; }
+
+template <int N>
+struct Const {
+  static constexpr int value = N;
+};
+
+}  // namespace
+
+size_t sort_tokens_bytes(int64_t n, int n_experts) {
+  if (n <= kSortSingle) return 0;
+  return (size_t)((n + sort_chunk(n) - 1) / sort_chunk(n)) * n_experts * sizeof(int32_t);
+}
+
+hipError_t launch_sort_tokens(const int32_t *ids, int64_t n, int n_experts, int32_t *offsets, int32_t *row_of, int32_t *entry_of,
+                              void *workspace, hipStream_t s) {
+  int32_t *hist = static_cast<int32_t *>(workspace);
+  const size_t lds = ((size_t)kSortWaves * n_experts + 16) * sizeof(int);
+  const auto go = [&](auto BITS) {
+    constexpr int B = decltype(BITS)::value;
+    if (n <= kSortSingle) {
+      hipLaunchKernelGGL((sort_kernel<B, false>), dim3(1), dim3(kSortThreads), lds, s, ids, n, n_experts, (int64_t)0, hist, offsets, row_of, entry_of);
+      return;
+    }
+    const int64_t chunk = sort_chunk(n);
+    const dim3 grid((uint32_t)((n + chunk - 1) / chunk));
+    hipLaunchKernelGGL((histogram_kernel<B>), grid, dim3(kSortThreads), lds, s, ids, n, n_experts, chunk, hist);
+    hipLaunchKernelGGL((sort_kernel<B, true>), grid, dim3(kSortThreads), lds, s, ids, n, n_experts, chunk, hist, offsets, row_of, entry_of);
+  };
+  // (keys 0..n_experts)
+  if (n_experts < 64) go(Const<6>{});
+  else if (n_experts < 128) go(Const<7>{});
+  else go(Const<10>{});
+  return hipGetLastError();
+}
+
+hipError_t launch_gather_rows(const OrderParams &o, const void *x, int fmt, int64_t x_stride, const float *scale, void *xs, float *xs_scale,
+                              hipStream_t s) {
+  const int64_t row = (int64_t)o.hidden * row_elem(fmt), stride = x_stride * row_elem(fmt);
+  const dim3 grid((uint32_t)((o.n_tokens + 3) / 4)), block(256);
+  const auto go = [&](auto v) {
+    using V = decltype(v);
+    hipLaunchKernelGGL((gather_kernel<V>), grid, block, 0, s, o, static_cast<const uint8_t *>(x), stride, (int)(row / sizeof(V)), scale,
+                       static_cast<uint8_t *>(xs), xs_scale);
+  };
+  const auto fits = [&](int by) { return row % by == 0 && stride % by == 0 && aligned(x, by) && aligned(xs, by); };
+  if (fits(16)) go(rows_u32x4{});
+  else if (fits(4)) go(uint32_t{});
+  else if (fits(2)) go(uint16_t{});
+  else go(uint8_t{});
+  return hipGetLastError();
+}
+
+hipError_t launch_combine_rows(const OrderParams &o, const void *ys, int ys_fmt, const float *weight, const void *base, void *y, int y_fmt,
+                               hipStream_t s) {
+  const bool wide = o.hidden % 8 == 0 && aligned(ys, 16) && aligned(y, 16) && (!base || aligned(base, 16));
+  const dim3 grid((uint32_t)((o.n_tokens + 3) / 4)), block(256);
+  const auto go = [&](auto YS, auto Y) {
+    const auto with = [&](auto VEC, auto KC) {
+      hipLaunchKernelGGL((combine_kernel<decltype(YS)::value, decltype(Y)::value, decltype(VEC)::value, decltype(KC)::value>), grid, block, 0, s, o,
+                         ys, weight, base, y);
+    };
+    const auto k = [&](auto VEC) {
+      if (o.top_k == 1) with(VEC, Const<1>{});
+      else if (o.top_k == 2) with(VEC, Const<2>{});
+      else if (o.top_k <= 4) with(VEC, Const<4>{});
+      else with(VEC, Const<8>{});
+    };
+    if (wide) k(Const<8>{});
+    else k(Const<1>{});
+  };
+  const auto y_of = [&](auto YS) {
+    if (y_fmt == MOE_R_FP32) go(YS, Const<MOE_R_FP32>{});
+    else go(YS, Const<MOE_R_BF16>{});
+  };
+  if (ys_fmt == MOE_R_FP32) y_of(Const<MOE_R_FP32>{});
+  else y_of(Const<MOE_R_BF16>{});
+  return hipGetLastError();
+}
+
+hipError_t launch_combine_rows_backward(const OrderParams &o, const void *dy, int dy_fmt, const void *ys, int ys_fmt, const float *weight,
+                                        void *dys, float *dweight, hipStream_t s) {
+  const bool wide = o.hidden % 8 == 0 && aligned(dy, 16) && (!ys || aligned(ys, 16)) && aligned(dys, 16);
+  const dim3 grid((uint32_t)((o.n_tokens + 3) / 4)), block(256);
+  const auto go = [&](auto DY, auto YS) {
+    const auto with = [&](auto VEC) {
+      hipLaunchKernelGGL((combine_backward_kernel<decltype(DY)::value, decltype(YS)::value, decltype(VEC)::value>), grid, block, 0, s, o, dy, ys,
+                         weight, dys, dweight);
+    };
+    if (wide) with(Const<8>{});
+    else with(Const<1>{});
+  };
+  const auto ys_of = [&](auto DY) {
+    if (ys_fmt == MOE_R_FP32) go(DY, Const<MOE_R_FP32>{});
+    else go(DY, Const<MOE_R_BF16>{});
+  };
+  if (dy_fmt == MOE_R_FP32) ys_of(Const<MOE_R_FP32>{});
+  else ys_of(Const<MOE_R_BF16>{});
+  return hipGetLastError();
+}
+
+}  // namespace moe
