@@ -63,18 +63,20 @@ struct ExpertRowsParams {
 };
 // row length of the arrays over the records: a whole number of the kernels' tiles
 __host__ __device__ constexpr int expert_rows_pitch(int inter) { return (inter + 63) / 64 * 64; }
-// h [n_rows][pitch] = silu(x Wg^T) * (x Wu^T); gu (may be NULL) [n_rows][2][pitch]: the two products
-hipError_t launch_experts_up(const ExpertRowsParams &p, int weight_fmt, const void *xs, const float *scale, uint16_t *h, uint16_t *gu,
+// h [n_rows][pitch] = silu(x Wg^T) * (x Wu^T); gu (may be NULL) fp32 [n_rows][2][pitch]: the two products
+hipError_t launch_experts_up(const ExpertRowsParams &p, int weight_fmt, const void *xs, const float *scale, uint16_t *h, float *gu, int n_cus,
                              hipStream_t s);
-hipError_t launch_experts_down(const ExpertRowsParams &p, int weight_fmt, const uint16_t *h, uint16_t *ys, hipStream_t s);
+hipError_t launch_experts_down(const ExpertRowsParams &p, int weight_fmt, const uint16_t *h, uint16_t *ys, int n_cus, hipStream_t s);
 // dgu [n_rows][2][pitch]: the gradients of the two products
-hipError_t launch_experts_dgu(const ExpertRowsParams &p, const uint16_t *dys, const uint16_t *gu, uint16_t *dgu, hipStream_t s);
-hipError_t launch_experts_dx(const ExpertRowsParams &p, const uint16_t *dgu, uint16_t *dxs, hipStream_t s);
+hipError_t launch_experts_dgu(const ExpertRowsParams &p, const uint16_t *dys, const float *gu, uint16_t *dgu, int n_cus, hipStream_t s);
+hipError_t launch_experts_dx(const ExpertRowsParams &p, const uint16_t *dgu, uint16_t *dxs, int n_cus, hipStream_t s);
 hipError_t launch_experts_dw(const ExpertRowsParams &p, const uint16_t *xs, const uint16_t *dys, const uint16_t *h, const uint16_t *dgu,
-                             uint8_t *dblobs, hipStream_t s);
+                             uint8_t *dblobs, int n_cus, hipStream_t s);
 
 // ---- device helpers ----
 #if defined(__HIPCC__)
+// for lambdas that are called in several places: as calls they would keep their captures in memory
+#define MOE_ROWS_INLINE __attribute__((always_inline))
 typedef uint32_t rows_u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t rows_u32x2 __attribute__((ext_vector_type(2)));
 

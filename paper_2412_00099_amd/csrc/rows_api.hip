@@ -155,7 +155,7 @@ int moe_combine_rows_backward(const void *dy, int32_t dy_fmt, const void *ys, in
 }
 
 int moe_experts_rows(int32_t weight_fmt, int32_t hidden, int32_t inter, int32_t n_experts, const void *blobs, int64_t blob_stride,
-                     const void *xs, const float *scale, const int32_t *offsets, int32_t n_rows, void *h, void *gu, void *ys, void *stream) {
+                     const void *xs, const float *scale, const int32_t *offsets, int32_t n_rows, void *h, float *gu, void *ys, void *stream) {
   if (const int bad = check_experts(weight_fmt, hidden, inter, n_experts, blobs, blob_stride, offsets, n_rows)) return bad;
   if (n_rows == 0) return MOE_OK;
   if (!xs || !h || !ys) return fail(MOE_EINVAL, "xs_dev, h_dev or ys_dev is NULL");
@@ -164,13 +164,15 @@ int moe_experts_rows(int32_t weight_fmt, int32_t hidden, int32_t inter, int32_t 
     return fail(MOE_EINVAL, "xs_dev, h_dev, gu_dev and ys_dev have to be 16-byte aligned");
   const ExpertRowsParams p{static_cast<const uint8_t *>(blobs), blob_stride, offsets, n_experts, n_rows, hidden, inter};
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  HIP_TRY(launch_experts_up(p, weight_fmt, xs, scale, static_cast<uint16_t *>(h), static_cast<uint16_t *>(gu), s));
-  HIP_TRY(launch_experts_down(p, weight_fmt, static_cast<const uint16_t *>(h), static_cast<uint16_t *>(ys), s));
+  int cus = 0;
+  HIP_TRY(compute_units(&cus));
+  HIP_TRY(launch_experts_up(p, weight_fmt, xs, scale, static_cast<uint16_t *>(h), gu, cus, s));
+  HIP_TRY(launch_experts_down(p, weight_fmt, static_cast<const uint16_t *>(h), static_cast<uint16_t *>(ys), cus, s));
   return MOE_OK;
 }
 
 int moe_experts_rows_backward(int32_t weight_fmt, int32_t hidden, int32_t inter, int32_t n_experts, const void *blobs, int64_t blob_stride,
-                              const void *xs, const int32_t *offsets, int32_t n_rows, const void *h, const void *gu, const void *dys, void *dgu,
+                              const void *xs, const int32_t *offsets, int32_t n_rows, const void *h, const float *gu, const void *dys, void *dgu,
                               void *dxs, void *dblobs, void *stream) {
   if (weight_fmt != MOE_W_BF16) return fail(MOE_EINVAL, "gradients are of bf16 blobs, not of weight format %d", weight_fmt);
   if (const int bad = check_experts(weight_fmt, hidden, inter, n_experts, blobs, blob_stride, offsets, n_rows)) return bad;
@@ -181,9 +183,11 @@ int moe_experts_rows_backward(int32_t weight_fmt, int32_t hidden, int32_t inter,
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const uint16_t *x16 = static_cast<const uint16_t *>(xs), *d16 = static_cast<const uint16_t *>(dys), *h16 = static_cast<const uint16_t *>(h);
   uint16_t *dgu16 = static_cast<uint16_t *>(dgu);
-  if (n_rows > 0 && (dxs || dblobs)) HIP_TRY(launch_experts_dgu(p, d16, static_cast<const uint16_t *>(gu), dgu16, s));
-  if (n_rows > 0 && dxs) HIP_TRY(launch_experts_dx(p, dgu16, static_cast<uint16_t *>(dxs), s));
-  if (dblobs) HIP_TRY(launch_experts_dw(p, x16, d16, h16, dgu16, static_cast<uint8_t *>(dblobs), s));
+  int cus = 0;
+  HIP_TRY(compute_units(&cus));
+  if (n_rows > 0 && (dxs || dblobs)) HIP_TRY(launch_experts_dgu(p, d16, gu, dgu16, cus, s));
+  if (n_rows > 0 && dxs) HIP_TRY(launch_experts_dx(p, dgu16, static_cast<uint16_t *>(dxs), cus, s));
+  if (dblobs) HIP_TRY(launch_experts_dw(p, x16, d16, h16, dgu16, static_cast<uint8_t *>(dblobs), cus, s));
   return MOE_OK;
 }
 

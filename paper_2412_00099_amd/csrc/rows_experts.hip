@@ -6,16 +6,23 @@
 //   dWg = dG^T X, dWu = dU^T X, dWd^T = H^T dY
 //
 // Three forms of product, all on the matrix cores with sums in 32 bits:
-//   rows_kernel     both operands have the summed index side by side (X with gate / up rows, dY with down columns)
-//   columns_kernel  the summed index are the records, so the weights' side is transposed on its way out of LDS
-//   weights_kernel  the summed index are the rows: both sides are transposed
-// H, G, U and their gradients pass through memory rounded to bf16, as the rows do.  With 8-bit weights the rows of the first
-// product are 8-bit codes too (whole-number sums, exact), H stays bf16 and the weights of down are widened to bf16, which holds
-// every code exactly.
+//   kUp, kDgu   both operands have the summed index side by side (X with gate / up rows, dY with down columns)
+//   kColumns    the summed index are the records (H with down, dG and dU with gate and up): the weights' side is transposed on
+//               its way out of LDS
+//   kWeights    the summed index are the rows: both sides are transposed
+// H and the gradients of G and U pass through memory rounded to bf16, as the rows do; G and U themselves are kept for the
+// backward in 32 bits (rounded to bf16 they were the largest part of the gradients' error).  With 8-bit weights the rows of the
+// first product are 8-bit codes too (whole-number sums, exact), H stays bf16 and the weights of down are widened to bf16, which
+// holds every code exactly.
 //
-// Which expert and which of its rows a workgroup has is worked out from `offsets` on the device; the grid is the most that
-// n_rows rows can need and workgroups without a tile leave.  All loads go through buffer resources that end where the expert's
-// rows or records end: what lies beyond arrives as zeros.
+// A workgroup of eight wavefronts has a compute unit to itself and walks over tiles of up to 256 x 256, a wavefront 128 x 64 of
+// it.  Steps of 32 (8-bit: 64) summed values go through a ring of five 32 KB stages in LDS, filled by loads that bypass the
+// registers, two stages at a time: up to four, 128 KB a compute unit, are on their way while one is used.  The fragments of the next step are read
+// while the matrix cores work on this one's, so a step costs one barrier.  The next tile's first stages are requested ahead of
+// the results' stores.
+//
+// Which expert and which of its rows a tile has is worked out from `offsets` on the device.  All loads go through buffer
+// resources that end where the expert's rows or records end: what lies beyond arrives as zeros.
 #include "rows.h"
 
 namespace moe {
@@ -25,16 +32,33 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __amdgpu_buffer_rsrc_t Buffer;
 #define LDS_PTR(T, p) ((__attribute__((address_space(3))) T *)(p))
 
-constexpr int kTile = 128;              // rows and columns of a workgroup's tile
-constexpr int kStepBytes = 128;         // bytes of a row that a step takes: 64 bf16 or 128 8-bit values
-constexpr int kBlock = 256;
-constexpr int kTileBytes = kTile * kStepBytes;  // 16 KB, one operand's part of a step
+constexpr int kCols = 256;        // columns of a tile (128 records where each has two products)
+constexpr int kMaxBlocks = 8;     // 32-row blocks of a tile at most
+constexpr int kWavesWg = 8, kBlock = kWavesWg * 64;
+constexpr int kStageBytes = 32768, kHalf = 16384;  // a stage: 16 KB of the rows' side, 16 KB of the weights' side
+constexpr int kStages = 5;                         // 160 KB, all of a compute unit's LDS
 
+enum { kUp = 0, kDgu = 1, kColumns = 2, kWeights = 3 };
+
+struct ProductArgs {
+  ExpertRowsParams p;
+  const uint8_t *a;    // rows' side: xs, dys, h or dgu
+  const uint8_t *b;    // kWeights: xs
+  const uint8_t *a2, *b2;  // kWeights: h and dys
+  const float *scale;  // 8-bit rows
+  const float *gu_in;  // kDgu
+  uint16_t *out;       // kUp: h; kDgu: dgu; kColumns: ys or dxs
+  float *gu_out;       // kUp: or nullptr
+  uint8_t *dblobs;     // kWeights
+  int32_t a_pitch;     // kColumns: elements of a row of a
+  int32_t sections, first;  // kColumns: out = sum over s < sections of columns s * pitch .. of a times part first + s of the records
+};
+
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 __device__ __forceinline__ Buffer buffer_of(const void *base, uint32_t bytes) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(base), 0, (int)bytes, 0x00020000);
 }
@@ -42,8 +66,16 @@ __device__ __forceinline__ Buffer buffer_of(const void *base, uint32_t bytes) {
 __device__ __forceinline__ void to_lds(Buffer b, uint32_t off, uint32_t at, uint8_t *lds) {
   __builtin_amdgcn_raw_ptr_buffer_load_lds(b, LDS_PTR(void, lds), 16, off, at, 0, 0);
 }
-__device__ __forceinline__ void wait_loads_and_meet() {
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+// all but the last N loads of the workgroup's wavefronts have landed
+template <int N>
+__device__ __forceinline__ void landed_but() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+// the reads of LDS that the workgroup has issued are done
+__device__ __forceinline__ void everybody_has_read() {
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 }
@@ -53,46 +85,60 @@ __device__ __forceinline__ f32x4 mma(i32x4 a, i32x4 b, f32x4 c) {
 }
 __device__ __forceinline__ i32x4 mma(i32x4 a, i32x4 b, i32x4 c) { return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0); }
 
-// The tile of a workgroup.
+// ---- tiles ------------------------------------------------------------------------------------------------
 struct Tile {
-  int expert;    // n_experts: the rows of nobody; -1: no tile
+  int expert;  // -1: no tile
   int row0, rows;
   int col;
 };
+__device__ __forceinline__ int first_row(const ExpertRowsParams &p, int e) { return min(max(p.offsets[e], 0), p.n_rows); }
+__device__ __forceinline__ int row_count(const ExpertRowsParams &p, int e) { return max(min(p.offsets[e + 1], p.n_rows) - first_row(p, e), 0); }
+__device__ __forceinline__ int wave_total(int v) {
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o);
+  return uniform(v);
+}
+
+// An expert's rows are cut into the fewest parts of at most `blocks` 32-row blocks, all of nearly the same size.  `blocks` is
+// the size from 4 to 8 for which the launch's rounds of one tile a workgroup take the least time: a tile costs its rows and, for
+// the weights that have to come in whatever its rows are, about 64 more.
+struct TilePlan {
+  int blocks, total;
+};
+__device__ __forceinline__ TilePlan plan_tiles(const ExpertRowsParams &p, int n_cols, int workgroups) {
+  const int lane = threadIdx.x & 63;
+  int n[5] = {};
+  for (int e = lane; e < p.n_experts; e += 64) {
+    const int c = row_count(p, e);
+#pragma unroll
+    for (int i = 0; i < 5; ++i) n[i] += (c + (4 + i) * 32 - 1) / ((4 + i) * 32);
+  }
+  TilePlan best{8, 0};
+  int64_t least = INT64_MAX;
+#pragma unroll
+  for (int i = 4; i >= 0; --i) {
+    const int total = wave_total(n[i]) * n_cols;
+    const int64_t cost = (int64_t)((total + workgroups - 1) / workgroups) * ((4 + i) * 32 + 64);
+    if (cost < least) {
+      least = cost;
+      best.blocks = 4 + i;
+      best.total = total;
+    }
+  }
+  return best;
+}
 // Tiles in the order expert, column, row, so that the workgroups that share weights are neighbours; the list is dealt to the
 // eight XCDs in eight parts, since workgroups go to them in turn and each has an L2 of its own.
-__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
-__device__ __forceinline__ Tile search_tile(const ExpertRowsParams &p, int n_cols, bool nobody, int block) {
-  const int lane = threadIdx.x & 63, groups = p.n_experts + (nobody ? 1 : 0);
-  int total = 0;
-  for (int e0 = 0; e0 < groups; e0 += 64) {
-    const int e = e0 + lane;
-    int c = 0;
-    if (e < groups) {
-      const int a = min(max(p.offsets[e], 0), p.n_rows), b = e < p.n_experts ? min(p.offsets[e + 1], p.n_rows) : p.n_rows;
-      c = max(b - a, 0);
-    }
-    int t = (c + kTile - 1) / kTile;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) t += __shfl_xor(t, o);
-    total += t;
-  }
-  total = uniform(total) * n_cols;
-  Tile r;
-  r.expert = -1;
-  r.row0 = r.rows = r.col = 0;
-  const int part = (total + 7) / 8, in_part = block >> 3, want = (block & 7) * part + in_part;
-  if (in_part >= part || want >= total) return r;
+__device__ __forceinline__ Tile find_tile(const ExpertRowsParams &p, const TilePlan &plan, int n_cols, int in_part, int xcd) {
+  const int lane = threadIdx.x & 63;
+  Tile r{-1, 0, 0, 0};
+  const int part = (plan.total + 7) / 8, want = xcd * part + in_part;
+  if (in_part >= part || want >= plan.total) return r;
   int before = 0;
-  for (int e0 = 0; e0 < groups; e0 += 64) {
-    const int e = e0 + lane;
-    int a = 0, c = 0;
-    if (e < groups) {
-      a = min(max(p.offsets[e], 0), p.n_rows);
-      const int b = e < p.n_experts ? min(p.offsets[e + 1], p.n_rows) : p.n_rows;
-      c = max(b - a, 0);
-    }
-    const int t = (c + kTile - 1) / kTile * n_cols;
+  const int most = plan.blocks * 32;
+  for (int e0 = 0; e0 < p.n_experts; e0 += 64) {
+    const int e = e0 + lane, c = e < p.n_experts ? row_count(p, e) : 0;
+    const int parts = (c + most - 1) / most, t = parts * n_cols;
     int upto = t;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
@@ -101,398 +147,559 @@ __device__ __forceinline__ Tile search_tile(const ExpertRowsParams &p, int n_col
     }
     const uint64_t past = __ballot(before + upto > want);
     if (past != 0) {
-      const int l = __ffsll((unsigned long long)past) - 1;
-      const int left = want - before - __shfl(upto - t, l), count = __shfl(c, l), row_tiles = (count + kTile - 1) / kTile;
+      const int l = uniform(__ffsll((unsigned long long)past) - 1);
+      const int left = want - before - uniform(__shfl(upto - t, l)), count = uniform(__shfl(c, l)), of = uniform(__shfl(parts, l));
       r.expert = e0 + l;
-      r.col = left / row_tiles;
-      const int rt = left - r.col * row_tiles;
-      r.row0 = __shfl(a, l) + rt * kTile;
-      r.rows = min(kTile, count - rt * kTile);
+      r.col = left / of;
+      const int each = ((count + of - 1) / of + 15) / 16 * 16, at = (left - r.col * of) * each;
+      r.row0 = first_row(p, r.expert) + at;
+      r.rows = max(min(each, count - at), 0);
       return r;
     }
     before += uniform(__shfl(upto, 63));
   }
   return r;
 }
-// (in scalar registers: it makes the buffer resources)
-__device__ __forceinline__ Tile find_tile(const ExpertRowsParams &p, int n_cols, bool nobody, int block) {
-  Tile t = search_tile(p, n_cols, nobody, block);
-  t.expert = uniform(t.expert);
-  t.row0 = uniform(t.row0);
-  t.rows = uniform(t.rows);
-  t.col = uniform(t.col);
-  return t;
-}
-int tile_grid(const ExpertRowsParams &p, int n_cols, bool nobody) {
-  const int64_t groups = p.n_experts + (nobody ? 1 : 0);
-  const int64_t tiles = (p.n_rows / kTile + (groups < p.n_rows ? groups : p.n_rows)) * n_cols;
-  return (int)((tiles + 7) / 8 * 8);
-}
+
+// (in scalar registers: a tile makes buffer resources and decides what is done)
+__device__ __forceinline__ Tile uniform_tile(const Tile &t) { return Tile{uniform(t.expert), uniform(t.row0), uniform(t.rows), uniform(t.col)}; }
 
 // ---- LDS images -------------------------------------------------------------------------------------------
-// Side by side: 128 rows of 128 bytes.  16-byte chunk c of row r lies at c ^ (r / 2 % 8): the 16 rows that a fragment reads at
-// one chunk then cover all banks.
-__device__ __forceinline__ int chunk_at(int r, int c) { return c ^ ((r >> 1) & 7); }
-__device__ __forceinline__ i32x4 fragment(const uint8_t *tile, int r, int chunk) {
-  return *reinterpret_cast<const i32x4 *>(tile + r * kStepBytes + chunk_at(r, chunk) * 16);
-}
-// Transposed, 16-bit: 64 rows (the summed index) of 128 columns, 256 bytes.  The 32 bytes of 16 columns move as one: group g of
-// row k lies at g ^ f(k), so that the 8 rows that are read together lie in different banks.
+// Side by side: 256 rows of 64 bytes, four 16-byte chunks.  Chunk c of row r lies at c ^ f(r).  A fragment's lanes read 16 bytes
+// of 16 rows each, in four turns; a turn takes four lanes each of four groups: rows 0-3 and 12-15 at one chunk and rows 4-11 at
+// its neighbour, or the other way round.  f, by the row's group of four, spreads both kinds over all banks.  The groups are 4
+// rows in a row where a fragment has 16 rows in a row, and 4 of each 8 where it has those.
+__device__ __forceinline__ int spread(int four) { return (((four ^ (four >> 1)) & 1) << 1) | ((four >> 1) & 1); }
+__device__ __forceinline__ int swap_rows(int r) { return spread(r >> 2); }
+__device__ __forceinline__ int swap_fours(int r) { return spread(r >> 3); }
+// Transposed, 16-bit: 32 rows (the summed index) of 256 columns, 512 bytes.  Where a fragment has 16 columns in a row, their 32
+// bytes (group g) lie at g ^ swap16(k); where it has 4 of each 8, 64 bytes (group g) lie at g ^ k % 4.
 __device__ __forceinline__ int swap16(int k) { return (k & 3) | ((k >> 1) & 4); }
-// the fragment of 16 columns (group g) and 32 rows from k0 on: the lane's column, 8 rows
-__device__ __forceinline__ i32x4 fragment_t16(const uint8_t *tile, int g, int k0, int lane) {
-  const int j = lane & 15, k = k0 + (lane >> 4) * 8 + (j >> 2);
-  const uint8_t *at = tile + k * 256 + ((g ^ swap16(k)) * 32) + (j & 3) * 8;
+// Results: register i of a lane is column (lane / 16) * 4 + i of a fragment.  With PAIRED fragments j and j + 1 have 4 columns
+// of each 8 in turn, so that a lane has 8 columns in a row and stores 16 bytes.
+__device__ __forceinline__ i32x4 transposed(const uint8_t *at) {  // 8 summed values of the lane's column: rows of `at` and + 4
   const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, at));
-  const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, at + 4 * 256));
+  const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, at + 4 * 512));
   return __builtin_bit_cast(i32x4, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
-// Transposed, 8-bit: 64 rows of 128 columns, 128 bytes; 16 columns are 16 bytes, group g of row k at g ^ (k % 8).  The codes
-// q + 128 are widened to bf16 (exact).
-__device__ __forceinline__ i32x4 fragment_t8(const uint8_t *tile, int g, int k0, int lane) {
-  const int j = lane & 15, k = k0 + (lane >> 4) * 8 + (j >> 1);
-  const uint8_t *at = tile + k * 128 + ((g ^ (k & 7)) * 16) + (j & 1) * 8;
-  const i32x2 q = __builtin_amdgcn_ds_read_tr8_b64_v2i32(LDS_PTR(i32x2, at));
+// 8 codes q + 128 as bf16 (whole numbers up to 128: the lower halves of the floats are zero)
+__device__ __forceinline__ i32x4 widen(i32x2 q) {
   i32x4 v;
 #pragma unroll
   for (int w = 0; w < 2; ++w) {
-    const uint32_t u = (uint32_t)q[w];
-    const float f0 = (float)(u & 0xff) - 128.f, f1 = (float)((u >> 8) & 0xff) - 128.f, f2 = (float)((u >> 16) & 0xff) - 128.f,
-                f3 = (float)(u >> 24) - 128.f;
-    // (whole numbers up to 128: the lower halves of the floats are zero)
+    const int u = q[w] ^ (int)0x80808080;
+    const float f0 = (float)(int8_t)u, f1 = (float)(int8_t)(u >> 8), f2 = (float)(int8_t)(u >> 16), f3 = (float)(u >> 24);
     v[2 * w] = (int)__builtin_amdgcn_perm(__float_as_uint(f1), __float_as_uint(f0), 0x07060302);
     v[2 * w + 1] = (int)__builtin_amdgcn_perm(__float_as_uint(f3), __float_as_uint(f2), 0x07060302);
   }
   return v;
 }
 
-// offsets of the lane's loads for 128 rows of 128 bytes: load i of wavefront w covers rows (w * 4 + i) * 8 ..
-__device__ __forceinline__ int side_row(int i) { return ((threadIdx.x >> 6) * 4 + i) * 8 + (threadIdx.x & 63) / 8; }
-__device__ __forceinline__ uint32_t side_chunk(int r) { return (uint32_t)chunk_at(r, threadIdx.x & 7) * 16; }
-
-__device__ __forceinline__ void store4(uint16_t *p, const float (&v)[4]) {
+// Results go through buffer resources too: rows that the tile does not have lie behind their end and are dropped, so that no
+// lane branches (a branch that differs between lanes would take the loops around it out of scalar control).
+constexpr uint32_t kNowhere = 0xf8000000u;
+__device__ __forceinline__ void store8(Buffer p, uint32_t off, const float (&v)[8]) {
+  rows_u32x4 w;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
+  __builtin_amdgcn_raw_buffer_store_b128(w, p, off, 0, 0);
+}
+__device__ __forceinline__ void store8_f32(Buffer p, uint32_t off, const float (&v)[8]) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    rows_u32x4 w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(v[4 * h + i]);
+    __builtin_amdgcn_raw_buffer_store_b128(w, p, off + 16 * h, 0, 0);
+  }
+}
+__device__ __forceinline__ void load8_f32(Buffer p, uint32_t off, float (&v)[8]) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const rows_u32x4 w = __builtin_amdgcn_raw_buffer_load_b128(p, off + 16 * h, 0, 0);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[4 * h + i] = __uint_as_float(w[i]);
+  }
+}
+__device__ __forceinline__ void store4(Buffer p, uint32_t off, const float (&v)[4]) {
   rows_u32x2 w;
   w[0] = pack_bf16(v[0], v[1]);
   w[1] = pack_bf16(v[2], v[3]);
-  *reinterpret_cast<rows_u32x2 *>(p) = w;
+  __builtin_amdgcn_raw_buffer_store_b64(w, p, off, 0, 0);
 }
+__device__ __forceinline__ float half_lo(uint32_t v) { return (float)__builtin_bit_cast(_Float16, (uint16_t)v); }
+__device__ __forceinline__ float half_hi(uint32_t v) { return (float)__builtin_bit_cast(_Float16, (uint16_t)(v >> 16)); }
 __device__ __forceinline__ float sigmoid(float g) { return __builtin_amdgcn_rcpf(1.f + __expf(-g)); }
-__device__ __forceinline__ float half_at(const uint8_t *p, int64_t at) { return (float)reinterpret_cast<const _Float16 *>(p)[at]; }
 
-// ---- rows x rows ----------------------------------------------------------------------------------------------
-enum { kUp = 0, kDgu = 1 };
-// kUp: 64 records a tile; its LDS rows are 16 gate rows, 16 up rows, 16 gate rows, .., so that a wavefront has both products of
-// a record in the same lane and register.  kDgu: 128 records a tile (their down columns).
-template <bool INT8, int MODE>
-__global__ __launch_bounds__(kBlock) void rows_kernel(const ExpertRowsParams p, const uint8_t *xs, const float *scale, const uint16_t *gu_in,
-                                                      uint16_t *h, uint16_t *gu) {
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[2][2][kTileBytes];
-  constexpr int REC = MODE == kUp ? 64 : 128;
-  constexpr int EL = INT8 ? 1 : 2;
-  const int pitch = expert_rows_pitch(p.inter);
-  const Tile t = find_tile(p, (pitch + REC - 1) / REC, false, blockIdx.x);
-  if (t.expert < 0) return;
-  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), wm = wave >> 1, wn = wave & 1;
-  const uint32_t row_bytes = (uint32_t)p.hidden * EL;
-  const uint8_t *blob = p.blobs + t.expert * p.blob_stride;
-  const Buffer a = buffer_of(xs + (int64_t)t.row0 * row_bytes, t.rows * row_bytes), b = buffer_of(blob, (uint32_t)p.inter * 3 * row_bytes);
-  const int rec0 = t.col * REC;
-  uint32_t a_off[4], b_off[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int r = side_row(i);
-    a_off[i] = (uint32_t)r * row_bytes + side_chunk(r);
-    const int rec = rec0 + (MODE == kUp ? (r >> 5) * 16 + (r & 15) : r), which = MODE == kUp ? (r >> 4) & 1 : 2;
-    b_off[i] = rec < p.inter ? (uint32_t)(rec * 3 + which) * row_bytes + side_chunk(r) : 0xffffff00u;
+// ---- one tile ---------------------------------------------------------------------------------------------
+template <int FORM, bool INT8>
+struct Product {
+  static constexpr int EL = INT8 ? 1 : 2;
+  static constexpr int B_LOADS = FORM == kColumns && INT8 ? 1 : 2, LOADS = 2 + B_LOADS;
+  using Acc = std::conditional_t<INT8 && FORM == kUp, i32x4, f32x4>;
+
+  const ProductArgs g;  // (a copy: through a reference the arguments would not be known to be the same in every lane)
+  uint8_t *lds;
+  int lane, wave, wm, wn, pitch;
+  uint32_t row_bytes;
+  // the tile whose loads are being issued
+  Buffer a, b;
+  uint32_t a_off[2], b_off[2];
+  int steps;  // even
+  // the stage that is requested next: its place in the ring and where its operands are
+  uint32_t put, a_at, b_at;
+  int section_left;                              // kColumns: stages of the first section to come
+  const uint8_t *a_base, *b_base;                // kWeights: of the stage
+  uint32_t a_row, b_row, a_skip, b_skip;
+  int rows_left;
+
+  __device__ __forceinline__ Product(const ProductArgs &args, uint8_t *l) : g(args), lds(l) {
+    lane = threadIdx.x & 63;
+    wave = uniform(threadIdx.x >> 6);
+    wm = wave >> 2;
+    wn = wave & 3;
+    pitch = expert_rows_pitch(g.p.inter);
+    row_bytes = (uint32_t)g.p.hidden * EL;
   }
-  const auto stage = [&](int buf, int k) {
+
+  // offsets of the lane's loads of a side-by-side image
+  __device__ __forceinline__ int side_row(int i) const { return (wave * 2 + i) * 16 + lane / 4; }
+
+  __device__ __forceinline__ void open(const Tile &t) {
+    const ExpertRowsParams &p = g.p;
+    put = a_at = b_at = 0;
+    if constexpr (FORM == kWeights) {
+      // t.col: columns of the gradient; t.row0, t.rows: its rows, 2 * pitch of gate and up, then pitch of down
+      const bool down = t.row0 >= 2 * pitch;
+      const int m0 = down ? t.row0 - 2 * pitch : t.row0, row0 = uniform(first_row(p, t.expert));
+      rows_left = uniform(row_count(p, t.expert));
+      steps = (rows_left + 63) / 64 * 2;  // (an even number, as the other forms have; rows that are not there are zeros)
+      a_row = (down ? pitch : 2 * pitch) * 2;
+      b_row = row_bytes;
+      a_skip = m0 * 2;
+      b_skip = t.col * kCols * 2;
+      a_base = (down ? g.a2 : g.a) + (int64_t)row0 * a_row + a_skip;
+      b_base = (down ? g.b2 : g.b) + (int64_t)row0 * b_row + b_skip;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      to_lds(a, a_off[i], k * kStepBytes, &lds[buf][0][(wave * 4 + i) * 1024]);
-      to_lds(b, b_off[i], k * kStepBytes, &lds[buf][1][(wave * 4 + i) * 1024]);
-    }
-  };
-  using Acc = std::conditional_t<INT8, i32x4, f32x4>;
-  Acc acc[4][4];
-#pragma unroll
-  for (int m = 0; m < 4; ++m)
-#pragma unroll
-    for (int n = 0; n < 4; ++n) acc[m][n] = Acc{};
-  const int steps = row_bytes / kStepBytes;
-  stage(0, 0);
-  for (int k = 0; k < steps; ++k) {
-    wait_loads_and_meet();
-    if (k + 1 < steps) stage((k + 1) & 1, k + 1);
-    const uint8_t *ta = lds[k & 1][0], *tb = lds[k & 1][1];
-#pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
-      i32x4 x[4], w[4];
-#pragma unroll
-      for (int m = 0; m < 4; ++m) x[m] = fragment(ta, wm * 64 + m * 16 + (lane & 15), kk * 4 + (lane >> 4));
-#pragma unroll
-      for (int n = 0; n < 4; ++n) {
-        w[n] = fragment(tb, wn * 64 + n * 16 + (lane & 15), kk * 4 + (lane >> 4));
-        if constexpr (INT8) w[n] ^= (int)0x80808080;
+      for (int i = 0; i < 2; ++i) {
+        const int k = (wave * 2 + i) * 2 + lane / 32, pos = lane & 31;
+        a_off[i] = k * a_row + (pos ^ (swap16(k) << 1)) * 16;
+        b_off[i] = k * b_row + (pos ^ ((k & 3) << 2)) * 16;
       }
+    } else {
+      const uint32_t rec_bytes = 3 * row_bytes, a_bytes = FORM == kColumns ? (uint32_t)g.a_pitch * 2 : row_bytes;
+      a = buffer_of(g.a + (int64_t)t.row0 * a_bytes, t.rows * a_bytes);
+      b = buffer_of(p.blobs + t.expert * p.blob_stride, (uint32_t)p.inter * rec_bytes);
 #pragma unroll
-      for (int m = 0; m < 4; ++m)
-#pragma unroll
-        for (int n = 0; n < 4; ++n) acc[m][n] = mma(w[n], x[m], acc[m][n]);
-    }
-  }
-  // lane: row lane % 16 of each 16 rows, records (lane / 16) * 4 .. + 3 of each 16 records
-#pragma unroll
-  for (int m = 0; m < 4; ++m) {
-    const int r = wm * 64 + m * 16 + (lane & 15);
-    if (r >= t.rows) continue;
-    const int64_t row = t.row0 + r;
-    if constexpr (MODE == kUp) {
-      const float sx = INT8 ? scale[row] : 1.f;
-#pragma unroll
-      for (int n = 0; n < 2; ++n) {
-        const int rec = rec0 + wn * 32 + n * 16 + (lane >> 4) * 4;
-        float g[4], u[4], v[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          g[i] = (float)acc[m][2 * n][i];
-          u[i] = (float)acc[m][2 * n + 1][i];
+      for (int i = 0; i < 2; ++i) {
+        const int r = side_row(i);
+        a_off[i] = (uint32_t)r * a_bytes + ((lane & 3) ^ swap_rows(r)) * 16;
+        if constexpr (FORM == kColumns) {
           if constexpr (INT8) {
-            const uint8_t *tail = blob + (int64_t)p.inter * 3 * row_bytes;
-            const bool in = rec + i < p.inter;
-            g[i] = in ? g[i] * (sx * half_at(tail, rec + i)) : 0.f;
-            u[i] = in ? u[i] * (sx * half_at(tail, p.inter + rec + i)) : 0.f;
+            const int k = wave * 4 + lane / 16;
+            b_off[i] = (uint32_t)k * rec_bytes + t.col * kCols + ((lane & 15) ^ (k & 15)) * 16;
+          } else {
+            const int k = (wave * 2 + i) * 2 + lane / 32;
+            b_off[i] = (uint32_t)k * rec_bytes + t.col * kCols * 2 + ((lane & 31) ^ (swap16(k) << 1)) * 16;
           }
-          v[i] = g[i] * sigmoid(g[i]) * u[i];
+        } else {
+          const int rec = FORM == kUp ? t.col * 128 + (r >> 6) * 32 + (r & 31) : t.col * kCols + r, which = FORM == kUp ? (r >> 5) & 1 : 2;
+          // (a record that is not there: outside of the resource)
+          b_off[i] = rec < p.inter ? (uint32_t)(rec * 3 + which) * row_bytes + ((lane & 3) ^ swap_fours(r)) * 16 : kNowhere;
         }
-        store4(h + row * pitch + rec, v);
-        if (gu) {
-          store4(gu + row * 2 * pitch + rec, g);
-          store4(gu + (row * 2 + 1) * pitch + rec, u);
-        }
+      }
+      if constexpr (FORM == kColumns) b_at = g.first * row_bytes;
+      section_left = pitch / 32;
+      steps = FORM == kColumns ? section_left * g.sections : row_bytes / 64;
+    }
+  }
+
+  // Requests the next two stages (behind a tile's last one: what comes next in memory, or zeros), load by load in turn: where
+  // the summed index lies side by side, the two stages have the two halves of each 128-byte line.
+  __device__ __forceinline__ void stage_pair() {
+    const uint32_t second = ring_next(put);
+    uint8_t *at0 = lds + put + wave * 2048, *at1 = lds + second + wave * 2048;
+    if constexpr (FORM == kWeights) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        uint8_t *at = h ? at1 : at0;
+        const int n = max(min(32, rows_left), 0);
+        const Buffer as = buffer_of(a_base, n > 0 ? n * a_row - a_skip : 0), bs = buffer_of(b_base, n > 0 ? n * b_row - b_skip : 0);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) to_lds(as, a_off[i], 0, at + i * 1024);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) to_lds(bs, b_off[i], 0, at + kHalf + i * 1024);
+        advance();
       }
     } else {
 #pragma unroll
-      for (int n = 0; n < 4; ++n) {
-        const int rec = rec0 + wn * 64 + n * 16 + (lane >> 4) * 4;
-        if (rec >= pitch) continue;
-        const rows_u32x2 gw = *reinterpret_cast<const rows_u32x2 *>(gu_in + row * 2 * pitch + rec),
-                         uw = *reinterpret_cast<const rows_u32x2 *>(gu_in + (row * 2 + 1) * pitch + rec);
-        float dg[4], du[4];
+      for (int i = 0; i < 2; ++i) {
+        to_lds(a, a_off[i], a_at, at0 + i * 1024);
+        to_lds(a, a_off[i], a_at + 64, at1 + i * 1024);
+      }
+      const uint32_t b0 = b_at;
+      advance();
+      const uint32_t b1 = b_at;
+      advance();
+#pragma unroll
+      for (int i = 0; i < B_LOADS; ++i) {
+        to_lds(b, b_off[i], b0, FORM == kColumns && INT8 ? lds + put + kHalf + wave * 1024 : at0 + kHalf + i * 1024);
+        to_lds(b, b_off[i], b1, FORM == kColumns && INT8 ? lds + second + kHalf + wave * 1024 : at1 + kHalf + i * 1024);
+      }
+    }
+    put = ring_next(second);
+  }
+  // to the operands of the next stage
+  __device__ __forceinline__ void advance() {
+    if constexpr (FORM == kWeights) {
+      rows_left -= 32;
+      a_base += 32 * a_row;
+      b_base += 32 * b_row;
+    } else {
+      a_at += 64;
+      if constexpr (FORM == kColumns) {
+        // (behind the last record: outside of the resource)
+        b_at += 32 * 3 * row_bytes;
+        if (--section_left == 0) b_at = (g.first + 1) * row_bytes;
+      } else {
+        b_at += 64;
+      }
+    }
+  }
+  static __device__ __forceinline__ uint32_t ring_next(uint32_t at) { return at == (kStages - 1) * kStageBytes ? 0 : at + kStageBytes; }
+  // the first stages of a tile; nobody reads LDS any more
+  __device__ __forceinline__ void stage_first() {
+    stage_pair();
+    stage_pair();
+  }
+  // as stage_first leaves it, for the tile that it was called for
+  __device__ __forceinline__ void skip_first() {
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      advance();
+      put = ring_next(put);
+    }
+  }
+
+  // Where the lane's fragments lie in a stage: of the weights for each j, of the rows for block 0.
+  __device__ __forceinline__ void fragment_offsets(uint32_t (&w_at)[4], uint32_t &x_at) const {
+    const int l = lane & 15, q = lane >> 4;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if constexpr (FORM == kWeights) {
+        const int k = q * 8 + (l >> 2), chunk = wn * 8 + (j >> 1) * 4 + (l & 3);
+        w_at[j] = kHalf + k * 512 + ((chunk ^ ((k & 3) << 2)) * 16) + (j & 1) * 8;
+      } else if constexpr (FORM == kColumns && INT8) {
+        const int k = q * 8 + (l >> 1);
+        w_at[j] = kHalf + k * 256 + (((wn * 4 + j) ^ (k & 15)) * 16) + (l & 1) * 8;
+      } else if constexpr (FORM == kColumns) {
+        const int k = q * 8 + (l >> 2);
+        w_at[j] = kHalf + k * 512 + (((wn * 4 + j) ^ swap16(k)) * 32) + (l & 3) * 8;
+      } else {
+        // kUp: fragments 0, 2 are gate rows, 1, 3 up rows
+        const int four = FORM == kUp ? j >> 1 : j & 1, half = FORM == kUp ? j & 1 : j >> 1;
+        const int r = wn * 64 + half * 32 + (l >> 2) * 8 + four * 4 + (l & 3);
+        w_at[j] = kHalf + r * 64 + ((q ^ swap_fours(r)) * 16);
+      }
+    }
+    if constexpr (FORM == kWeights) {
+      const int k = q * 8 + (l >> 2);
+      x_at = k * 512 + ((wm ^ swap16(k)) * 32) + (l & 3) * 8;
+    } else {
+      const int r = wm * 16 + l;
+      x_at = r * 64 + ((q ^ swap_rows(r)) * 16);
+    }
+  }
+  __device__ __forceinline__ i32x4 read_w(uint32_t at) const {
+    if constexpr (FORM == kWeights || (FORM == kColumns && !INT8)) return transposed(lds + at);
+    else if constexpr (FORM == kColumns) return widen(__builtin_amdgcn_ds_read_tr8_b64_v2i32(LDS_PTR(i32x2, lds + at)));
+    else {
+      i32x4 w = *reinterpret_cast<const i32x4 *>(lds + at);
+      if constexpr (INT8) w ^= (int)0x80808080;
+      return w;
+    }
+  }
+  // block m; at: of block 0 (transposed, the block is part of what was exchanged: see swap16)
+  __device__ __forceinline__ i32x4 read_x(uint32_t x_at, uint32_t ring, int m) const {
+    if constexpr (FORM == kWeights) return transposed(lds + ring + (x_at ^ (m * 64)));
+    else return *reinterpret_cast<const i32x4 *>(lds + ring + x_at + m * 2048);
+  }
+
+  // the product of the tile that is open; then `next` opens the next one, and the results are stored
+  template <typename Next>
+  __device__ __forceinline__ void run(const Tile &t, Next next) {
+    const int blocks = (t.rows + 31) / 32;  // of 32 rows; a wavefront has half of each
+    Acc acc[kMaxBlocks][4];
+#pragma unroll
+    for (int m = 0; m < kMaxBlocks; ++m)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[m][j] = Acc{};
+    i32x4 x[kMaxBlocks], w0[4], w1[4];
+    uint32_t w_at[4], x_at, ring = 0;  // ring: place of the stage whose fragments are read
+    fragment_offsets(w_at, x_at);
+    // Step s works on stage s and reads the fragments of stage s + 1, a block's once the block of this step has gone to the matrix
+    // cores.  At an even step everybody has read stage s: with stage s - 1 it leaves room for stages s + 4 and s + 5.  At an odd
+    // one stages s + 1 and s + 2 have landed, the two behind them may be on their way.  Blocks that the tile does not have are
+    // jumped over.  (Behind the last step stages are requested and read that nobody uses.)
+    const auto step = [&](i32x4 (&now)[4], i32x4 (&then)[4], bool even) MOE_ROWS_INLINE {
+      if (even) {
+        everybody_has_read();
+        stage_pair();
+      } else {
+        landed_but<2 * LOADS>();
+      }
+      ring = ring_next(ring);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) then[j] = read_w(ring + w_at[j]);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int m = 0; m < kMaxBlocks; ++m) {
+        if (m > 0 && m >= blocks) break;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[m][j] = mma(now[j], x[m], acc[m][j]);
+        x[m] = read_x(x_at, ring, m);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    if (steps > 0) {
+      landed_but<0>();
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w0[j] = read_w(w_at[j]);
+#pragma unroll
+      for (int m = 0; m < kMaxBlocks; ++m) x[m] = read_x(x_at, 0, m);
+      for (int left = steps; left > 0; left -= 2) {
+        step(w0, w1, true);
+        step(w1, w0, false);
+      }
+    }
+    everybody_has_read();
+    next();
+    store(t, acc, blocks);
+  }
+
+  // lane: row lane % 16 of each block of 16 rows; columns as said at the LDS images
+  __device__ __forceinline__ void store(const Tile &t, const Acc (&acc)[kMaxBlocks][4], int blocks) const {
+    const ExpertRowsParams &p = g.p;
+    const int q = lane >> 4, r0 = wm * 16 + (lane & 15);
+    const uint8_t *blob = p.blobs + t.expert * p.blob_stride;
+    const int64_t tail = (int64_t)p.inter * 3 * row_bytes;
+    if constexpr (FORM == kUp) {
+      const int rec = t.col * 128 + wn * 32 + q * 8;
+      const Buffer h = buffer_of(g.out + (int64_t)t.row0 * pitch, t.rows * pitch * 2);
+      const Buffer both = buffer_of(g.gu_out + (int64_t)t.row0 * 2 * pitch, g.gu_out ? t.rows * 2 * pitch * 4 : 0);
+      float sg[8], su[8];
+      if constexpr (INT8) {
+        const Buffer scales = buffer_of(blob + tail, p.inter * 4);
+        const rows_u32x4 vg = __builtin_amdgcn_raw_buffer_load_b128(scales, rec < p.inter ? rec * 2 : kNowhere, 0, 0),
+                         vu = __builtin_amdgcn_raw_buffer_load_b128(scales, rec < p.inter ? (p.inter + rec) * 2 : kNowhere, 0, 0);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float g = i & 1 ? bf16_hi(gw[i >> 1]) : bf16_lo(gw[i >> 1]), u = i & 1 ? bf16_hi(uw[i >> 1]) : bf16_lo(uw[i >> 1]);
-          const float s = sigmoid(g), dh = acc[m][n][i];
-          dg[i] = dh * u * (s * (1.f + g * (1.f - s)));
-          du[i] = dh * (g * s);
+          sg[2 * i] = half_lo(vg[i]);
+          sg[2 * i + 1] = half_hi(vg[i]);
+          su[2 * i] = half_lo(vu[i]);
+          su[2 * i + 1] = half_hi(vu[i]);
         }
-        store4(gu + row * 2 * pitch + rec, dg);
-        store4(gu + (row * 2 + 1) * pitch + rec, du);
+      }
+      const Buffer row_scale = buffer_of(g.scale + t.row0, INT8 ? t.rows * 4 : 0);
+#pragma unroll
+      for (int m = 0; m < kMaxBlocks; ++m) {
+        if (m > 0 && m >= blocks) break;
+        const uint32_t r = r0 + m * 32;
+        const float sx = INT8 ? __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(row_scale, r * 4, 0, 0)) : 1.f;
+        float v[8], gate[8], up[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          gate[i] = (float)acc[m][(i >> 2) * 2][i & 3];
+          up[i] = (float)acc[m][(i >> 2) * 2 + 1][i & 3];
+          if constexpr (INT8) {
+            gate[i] *= sx * sg[i];
+            up[i] *= sx * su[i];
+          }
+          v[i] = gate[i] * sigmoid(gate[i]) * up[i];
+        }
+        store8(h, rec < pitch ? (r * pitch + rec) * 2 : kNowhere, v);
+        if (g.gu_out) {
+          const uint32_t at = rec < pitch ? (r * 2 * pitch + rec) * 4 : kNowhere;
+          store8_f32(both, at, gate);
+          store8_f32(both, at + pitch * 4, up);
+        }
+      }
+    } else if constexpr (FORM == kDgu) {
+      const Buffer in = buffer_of(g.gu_in + (int64_t)t.row0 * 2 * pitch, t.rows * 2 * pitch * 4),
+                   out = buffer_of(g.out + (int64_t)t.row0 * 2 * pitch, t.rows * 2 * pitch * 2);
+#pragma unroll
+      for (int m = 0; m < kMaxBlocks; ++m) {
+        if (m > 0 && m >= blocks) break;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int rec = t.col * kCols + wn * 64 + h * 32 + q * 8;
+          const uint32_t at = rec < pitch ? (r0 + m * 32) * 2 * pitch + rec : kNowhere / 4;
+          float gate[8], up[8];
+          load8_f32(in, at * 4, gate);
+          load8_f32(in, (at + pitch) * 4, up);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const float s = sigmoid(gate[i]), dh = acc[m][h * 2 + (i >> 2)][i & 3], x = gate[i];
+            gate[i] = dh * up[i] * (s * (1.f + x * (1.f - s)));
+            up[i] = dh * (x * s);
+          }
+          // (behind the last record: both resources end before kNowhere / 2)
+          store8(out, at * 2, gate);
+          store8(out, (at + pitch) * 2, up);
+        }
+      }
+    } else if constexpr (FORM == kColumns) {
+      const Buffer out = buffer_of(g.out + (int64_t)t.row0 * p.hidden, t.rows * p.hidden * 2);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int col = t.col * kCols + wn * 64 + j * 16 + q * 4;
+        float sd[4];
+        if constexpr (INT8) {
+          const rows_u32x2 w = *reinterpret_cast<const rows_u32x2 *>(blob + tail + (int64_t)p.inter * 4 + col * 2);
+          sd[0] = half_lo(w[0]);
+          sd[1] = half_hi(w[0]);
+          sd[2] = half_lo(w[1]);
+          sd[3] = half_hi(w[1]);
+        }
+#pragma unroll
+        for (int m = 0; m < kMaxBlocks; ++m) {
+          if (m > 0 && m >= blocks) break;
+          float v[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v[i] = INT8 ? acc[m][j][i] * sd[i] : acc[m][j][i];
+          store4(out, ((r0 + m * 32) * p.hidden + col) * 2, v);
+        }
+      }
+    } else {
+      const Buffer out = buffer_of(g.dblobs + t.expert * p.blob_stride, (uint32_t)tail);
+#pragma unroll
+      for (int m = 0; m < kMaxBlocks; ++m) {
+        if (m > 0 && m >= blocks) break;
+        const int r = r0 + m * 32, at = t.row0 + r, which = at >= 2 * pitch ? 2 : at >= pitch ? 1 : 0, rec = at - which * pitch;
+        // (a record that is not there lies behind the end)
+        const uint32_t to = r < t.rows ? ((rec * 3 + which) * p.hidden + t.col * kCols + wn * 64 + q * 8) * 2 : kNowhere;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          float v[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) v[i] = acc[m][h * 2 + (i >> 2)][i & 3];
+          store8(out, to + h * 64, v);
+        }
       }
     }
   }
-}
+};
 
-// ---- rows x columns -------------------------------------------------------------------------------------------
-// out = sum over `sections` of A_s W_s: A_s = columns s * pitch .. of a (a_pitch elements a row), W_s = part first + s of the
-// records.  Down: H with the columns; the gradient of the rows: dG with the gate rows, dU with the up rows.
-template <bool INT8>
-__global__ __launch_bounds__(kBlock) void columns_kernel(const ExpertRowsParams p, const uint16_t *a_in, int a_pitch, int sections, int first,
-                                                         uint16_t *out) {
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[2][2][kTileBytes];
-  constexpr int EL = INT8 ? 1 : 2;
-  constexpr int W_LOADS = INT8 ? 2 : 4;
-  const int pitch = expert_rows_pitch(p.inter);
-  const Tile t = find_tile(p, p.hidden / kTile, true, blockIdx.x);
-  if (t.expert < 0) return;
-  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), wm = wave >> 1, wn = wave & 1;
-  const int n0 = t.col * kTile;
-  if (t.expert == p.n_experts) {  // rows of nobody
-    for (int r = threadIdx.x >> 4; r < t.rows; r += kBlock / 16)
-      *reinterpret_cast<rows_u32x4 *>(out + (int64_t)(t.row0 + r) * p.hidden + n0 + (threadIdx.x & 15) * 8) = rows_u32x4{};
-    return;
-  }
-  const uint32_t row_bytes = (uint32_t)p.hidden * EL, rec_bytes = 3 * row_bytes, a_bytes = (uint32_t)a_pitch * 2;
-  const uint8_t *blob = p.blobs + t.expert * p.blob_stride;
-  const Buffer a = buffer_of(a_in + (int64_t)t.row0 * a_pitch, t.rows * a_bytes), b = buffer_of(blob, (uint32_t)p.inter * rec_bytes);
-  uint32_t a_off[4], b_off[W_LOADS];
-  int b_row[W_LOADS];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int r = side_row(i);
-    a_off[i] = (uint32_t)r * a_bytes + side_chunk(r);
-  }
-#pragma unroll
-  for (int i = 0; i < W_LOADS; ++i) {
-    int k, col;
-    if constexpr (INT8) {
-      k = (wave * W_LOADS + i) * 8 + lane / 8;
-      col = ((lane & 7) ^ (k & 7)) * 16;
+template <int FORM, bool INT8>
+__global__ __launch_bounds__(kBlock, 2) void product_kernel(const ProductArgs g) {
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[kStages * kStageBytes];
+  Product<FORM, INT8> f(g, lds);
+  const ExpertRowsParams &p = g.p;
+  const int workgroups = gridDim.x, per_xcd = workgroups / 8, xcd = blockIdx.x & 7;
+  const int n_cols = FORM == kUp ? (f.pitch + 127) / 128 : FORM == kDgu ? (f.pitch + kCols - 1) / kCols : p.hidden / kCols;
+  // kWeights: 2 * pitch rows of gate and up gradients, then pitch of down
+  const int m_both = (2 * f.pitch + 255) / 256, m_tiles = m_both + (f.pitch + 255) / 256;
+  TilePlan plan{8, p.n_experts * m_tiles * n_cols};
+  if constexpr (FORM != kWeights) plan = plan_tiles(p, n_cols, workgroups);
+  const auto tile = [&](int i) MOE_ROWS_INLINE {
+    if constexpr (FORM == kWeights) {
+      Tile r{-1, 0, 0, 0};
+      const int part = (plan.total + 7) / 8, want = xcd * part + i;
+      if (i >= part || want >= plan.total) return r;
+      r.col = want % n_cols;
+      const int m = want / n_cols, at = m % m_tiles;
+      r.expert = m / m_tiles;
+      r.row0 = at < m_both ? at * 256 : 2 * f.pitch + (at - m_both) * 256;
+      r.rows = min(256, (at < m_both ? 2 : 3) * f.pitch - r.row0);
+      return r;
     } else {
-      k = (wave * W_LOADS + i) * 4 + lane / 16;
-      col = ((((lane & 15) >> 1) ^ swap16(k)) * 2 + (lane & 1)) * 16;
-    }
-    b_row[i] = k;
-    b_off[i] = (uint32_t)k * rec_bytes + first * row_bytes + n0 * EL + col;
-  }
-  const int per_section = pitch / 64, steps = per_section * sections;
-  const auto stage = [&](int buf, int s) {
-    const int sec = s >= per_section ? 1 : 0, k = s - sec * per_section;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) to_lds(a, a_off[i], s * kStepBytes, &lds[buf][0][(wave * 4 + i) * 1024]);
-#pragma unroll
-    for (int i = 0; i < W_LOADS; ++i) {
-      const uint32_t off = b_row[i] + k * 64 < p.inter ? b_off[i] + (uint32_t)k * 64 * rec_bytes + sec * row_bytes : 0xffffff00u;
-      to_lds(b, off, 0, &lds[buf][1][(wave * W_LOADS + i) * 1024]);
+      return find_tile(p, plan, n_cols, i, xcd);
     }
   };
-  f32x4 acc[4][4];
-#pragma unroll
-  for (int m = 0; m < 4; ++m)
-#pragma unroll
-    for (int n = 0; n < 4; ++n) acc[m][n] = f32x4{};
-  stage(0, 0);
-  for (int s = 0; s < steps; ++s) {
-    wait_loads_and_meet();
-    if (s + 1 < steps) stage((s + 1) & 1, s + 1);
-    const uint8_t *ta = lds[s & 1][0], *tb = lds[s & 1][1];
-#pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
-      i32x4 x[4], w[4];
-#pragma unroll
-      for (int m = 0; m < 4; ++m) x[m] = fragment(ta, wm * 64 + m * 16 + (lane & 15), kk * 4 + (lane >> 4));
-#pragma unroll
-      for (int n = 0; n < 4; ++n) w[n] = INT8 ? fragment_t8(tb, wn * 4 + n, kk * 32, lane) : fragment_t16(tb, wn * 4 + n, kk * 32, lane);
-#pragma unroll
-      for (int m = 0; m < 4; ++m)
-#pragma unroll
-        for (int n = 0; n < 4; ++n) acc[m][n] = mma(w[n], x[m], acc[m][n]);
-    }
+  int i = blockIdx.x >> 3;
+  Tile now = uniform_tile(tile(i));
+  if (now.expert >= 0) {
+    f.open(now);
+    f.stage_first();
   }
-  const uint8_t *down_scale = blob + (int64_t)p.inter * rec_bytes + (int64_t)p.inter * 4;
-#pragma unroll
-  for (int m = 0; m < 4; ++m) {
-    const int r = wm * 64 + m * 16 + (lane & 15);
-    if (r >= t.rows) continue;
-#pragma unroll
-    for (int n = 0; n < 4; ++n) {
-      const int col = n0 + wn * 64 + n * 16 + (lane >> 4) * 4;
-      float v[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = INT8 ? acc[m][n][i] * half_at(down_scale, col + i) : acc[m][n][i];
-      store4(out + (int64_t)(t.row0 + r) * p.hidden + col, v);
-    }
+  if constexpr (FORM == kColumns) {  // rows of nobody
+    const int used = uniform(min(max(p.offsets[p.n_experts], 0), p.n_rows));
+    for (int64_t r = used + blockIdx.x; r < p.n_rows; r += workgroups)
+      for (int c = threadIdx.x * 8; c < p.hidden; c += kBlock * 8) *reinterpret_cast<rows_u32x4 *>(g.out + r * p.hidden + c) = rows_u32x4{};
+  }
+  while (now.expert >= 0) {
+    // (once more: carried over from the end of the last turn, the buffers would not be known to be the same in every lane)
+    f.open(now);
+    f.skip_first();
+    i += per_xcd;
+    const Tile next = uniform_tile(tile(i));
+    const auto open_next = [&]() MOE_ROWS_INLINE {
+      if (next.expert < 0) return;
+      f.open(next);
+      f.stage_first();
+    };
+    f.run(now, open_next);
+    now = uniform_tile(next);
   }
 }
 
-// ---- columns x columns: gradients of the weights --------------------------------------------------------------
-__global__ __launch_bounds__(kBlock) void weights_kernel(const ExpertRowsParams p, const uint16_t *xs, const uint16_t *dys, const uint16_t *h,
-                                                         const uint16_t *dgu, uint8_t *dblobs) {
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[2][2][kTileBytes];
-  const int pitch = expert_rows_pitch(p.inter), n_n = p.hidden / kTile, n_m = (p.inter + kTile - 1) / kTile;
-  int i0 = blockIdx.x;
-  const int n0 = i0 % n_n * kTile;
-  i0 /= n_n;
-  const int m0 = i0 % n_m * kTile;
-  i0 /= n_m;
-  const int which = i0 % 3, e = i0 / 3;
-  const int row0 = uniform(min(max(p.offsets[e], 0), p.n_rows)), rows = uniform(max(min(p.offsets[e + 1], p.n_rows) - row0, 0));
-  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), wm = wave >> 1, wn = wave & 1;
-  const uint16_t *a_in = which == 2 ? h : dgu + which * pitch, *b_in = which == 2 ? dys : xs;
-  const int a_pitch = which == 2 ? pitch : 2 * pitch;
-  uint32_t a_off[4], b_off[4];
-  const uint32_t a_bytes = (uint32_t)a_pitch * 2, b_bytes = (uint32_t)p.hidden * 2;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int k = (wave * 4 + i) * 4 + lane / 16, col = ((((lane & 15) >> 1) ^ swap16(k)) * 2 + (lane & 1)) * 16;
-    a_off[i] = (uint32_t)k * a_bytes + col;
-    b_off[i] = (uint32_t)k * b_bytes + col;
-  }
-  const int steps = (rows + 63) / 64;
-  const auto stage = [&](int buf, int s) {
-    const int64_t r = row0 + s * 64;
-    const int n = min(64, rows - s * 64);
-    // (the rest of a row behind the tile's columns belongs to the resource; rows behind the expert's do not)
-    const Buffer a = buffer_of(a_in + r * a_pitch + m0, n * a_bytes - (m0 + (which == 1 ? pitch : 0)) * 2),
-                 b = buffer_of(b_in + r * p.hidden + n0, n * b_bytes - n0 * 2);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      to_lds(a, a_off[i], 0, &lds[buf][0][(wave * 4 + i) * 1024]);
-      to_lds(b, b_off[i], 0, &lds[buf][1][(wave * 4 + i) * 1024]);
-    }
-  };
-  f32x4 acc[4][4];
-#pragma unroll
-  for (int m = 0; m < 4; ++m)
-#pragma unroll
-    for (int n = 0; n < 4; ++n) acc[m][n] = f32x4{};
-  if (steps > 0) stage(0, 0);
-  for (int s = 0; s < steps; ++s) {
-    wait_loads_and_meet();
-    if (s + 1 < steps) stage((s + 1) & 1, s + 1);
-    const uint8_t *ta = lds[s & 1][0], *tb = lds[s & 1][1];
-#pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
-      i32x4 x[4], w[4];
-#pragma unroll
-      for (int m = 0; m < 4; ++m) x[m] = fragment_t16(ta, wm * 4 + m, kk * 32, lane);
-#pragma unroll
-      for (int n = 0; n < 4; ++n) w[n] = fragment_t16(tb, wn * 4 + n, kk * 32, lane);
-#pragma unroll
-      for (int m = 0; m < 4; ++m)
-#pragma unroll
-        for (int n = 0; n < 4; ++n) acc[m][n] = mma(w[n], x[m], acc[m][n]);
-    }
-  }
-  uint16_t *out = reinterpret_cast<uint16_t *>(dblobs + e * p.blob_stride);
-#pragma unroll
-  for (int m = 0; m < 4; ++m) {
-    const int rec = m0 + wm * 64 + m * 16 + (lane & 15);
-    if (rec >= p.inter) continue;
-#pragma unroll
-    for (int n = 0; n < 4; ++n) {
-      const float v[4] = {acc[m][n][0], acc[m][n][1], acc[m][n][2], acc[m][n][3]};
-      store4(out + ((int64_t)rec * 3 + which) * p.hidden + n0 + wn * 64 + n * 16 + (lane >> 4) * 4, v);
-    }
-  }
+template <int FORM, bool INT8>
+hipError_t launch_product(const ProductArgs &g, int n_cus, hipStream_t s) {
+  // one workgroup a compute unit, in whole eights
+  hipLaunchKernelGGL((product_kernel<FORM, INT8>), dim3(n_cus / 8 * 8), dim3(kBlock), 0, s, g);
+  return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_experts_up(const ExpertRowsParams &p, int weight_fmt, const void *xs, const float *scale, uint16_t *h, uint16_t *gu,
+hipError_t launch_experts_up(const ExpertRowsParams &p, int weight_fmt, const void *xs, const float *scale, uint16_t *h, float *gu, int n_cus,
                              hipStream_t s) {
-  const dim3 grid(tile_grid(p, expert_rows_pitch(p.inter) / 64, false));
-  const uint8_t *x = static_cast<const uint8_t *>(xs);
-  if (weight_fmt == MOE_W_INT8_PC)
-    hipLaunchKernelGGL((rows_kernel<true, kUp>), grid, dim3(kBlock), 0, s, p, x, scale, (const uint16_t *)nullptr, h, gu);
-  else
-    hipLaunchKernelGGL((rows_kernel<false, kUp>), grid, dim3(kBlock), 0, s, p, x, scale, (const uint16_t *)nullptr, h, gu);
-  return hipGetLastError();
+  ProductArgs g{};
+  g.p = p;
+  g.a = static_cast<const uint8_t *>(xs);
+  g.scale = scale;
+  g.out = h;
+  g.gu_out = gu;
+  return weight_fmt == MOE_W_INT8_PC ? launch_product<kUp, true>(g, n_cus, s) : launch_product<kUp, false>(g, n_cus, s);
 }
-hipError_t launch_experts_down(const ExpertRowsParams &p, int weight_fmt, const uint16_t *h, uint16_t *ys, hipStream_t s) {
-  const dim3 grid(tile_grid(p, p.hidden / kTile, true));
-  const int pitch = expert_rows_pitch(p.inter);
-  if (weight_fmt == MOE_W_INT8_PC)
-    hipLaunchKernelGGL((columns_kernel<true>), grid, dim3(kBlock), 0, s, p, h, pitch, 1, 2, ys);
-  else
-    hipLaunchKernelGGL((columns_kernel<false>), grid, dim3(kBlock), 0, s, p, h, pitch, 1, 2, ys);
-  return hipGetLastError();
+hipError_t launch_experts_down(const ExpertRowsParams &p, int weight_fmt, const uint16_t *h, uint16_t *ys, int n_cus, hipStream_t s) {
+  ProductArgs g{};
+  g.p = p;
+  g.a = reinterpret_cast<const uint8_t *>(h);
+  g.a_pitch = expert_rows_pitch(p.inter);
+  g.sections = 1;
+  g.first = 2;
+  g.out = ys;
+  return weight_fmt == MOE_W_INT8_PC ? launch_product<kColumns, true>(g, n_cus, s) : launch_product<kColumns, false>(g, n_cus, s);
 }
-hipError_t launch_experts_dgu(const ExpertRowsParams &p, const uint16_t *dys, const uint16_t *gu, uint16_t *dgu, hipStream_t s) {
-  const dim3 grid(tile_grid(p, (expert_rows_pitch(p.inter) + 127) / 128, false));
-  hipLaunchKernelGGL((rows_kernel<false, kDgu>), grid, dim3(kBlock), 0, s, p, reinterpret_cast<const uint8_t *>(dys), (const float *)nullptr, gu,
-                     (uint16_t *)nullptr, dgu);
-  return hipGetLastError();
+hipError_t launch_experts_dgu(const ExpertRowsParams &p, const uint16_t *dys, const float *gu, uint16_t *dgu, int n_cus, hipStream_t s) {
+  ProductArgs g{};
+  g.p = p;
+  g.a = reinterpret_cast<const uint8_t *>(dys);
+  g.gu_in = gu;
+  g.out = dgu;
+  return launch_product<kDgu, false>(g, n_cus, s);
 }
-hipError_t launch_experts_dx(const ExpertRowsParams &p, const uint16_t *dgu, uint16_t *dxs, hipStream_t s) {
-  const dim3 grid(tile_grid(p, p.hidden / kTile, true));
-  hipLaunchKernelGGL((columns_kernel<false>), grid, dim3(kBlock), 0, s, p, dgu, 2 * expert_rows_pitch(p.inter), 2, 0, dxs);
-  return hipGetLastError();
+hipError_t launch_experts_dx(const ExpertRowsParams &p, const uint16_t *dgu, uint16_t *dxs, int n_cus, hipStream_t s) {
+  ProductArgs g{};
+  g.p = p;
+  g.a = reinterpret_cast<const uint8_t *>(dgu);
+  g.a_pitch = 2 * expert_rows_pitch(p.inter);
+  g.sections = 2;
+  g.first = 0;
+  g.out = dxs;
+  return launch_product<kColumns, false>(g, n_cus, s);
 }
 hipError_t launch_experts_dw(const ExpertRowsParams &p, const uint16_t *xs, const uint16_t *dys, const uint16_t *h, const uint16_t *dgu,
-                             uint8_t *dblobs, hipStream_t s) {
-  const dim3 grid(p.n_experts * 3 * ((p.inter + kTile - 1) / kTile) * (p.hidden / kTile));
-  hipLaunchKernelGGL(weights_kernel, grid, dim3(kBlock), 0, s, p, xs, dys, h, dgu, dblobs);
-  return hipGetLastError();
+                             uint8_t *dblobs, int n_cus, hipStream_t s) {
+  ProductArgs g{};
+  g.p = p;
+  g.a = reinterpret_cast<const uint8_t *>(dgu);
+  g.b = reinterpret_cast<const uint8_t *>(xs);
+  g.a2 = reinterpret_cast<const uint8_t *>(h);
+  g.b2 = reinterpret_cast<const uint8_t *>(dys);
+  g.dblobs = dblobs;
+  return launch_product<kWeights, false>(g, n_cus, s);
 }
 
 }  // namespace moe

@@ -202,7 +202,7 @@ def experts_rows(weight_fmt, blobs, inter, xs, offsets, *, scale=None, keep=Fals
     s = _stream(dev, blobs, offsets, scale)
     pitch = (inter + 63) // 64 * 64
     h = torch.empty((n, pitch), dtype=torch.bfloat16, device=dev)
-    gu = torch.empty((n, 2, pitch), dtype=torch.bfloat16, device=dev) if keep else None
+    gu = torch.empty((n, 2, pitch), dtype=torch.float32, device=dev) if keep else None
     ys = torch.empty((n, d), dtype=torch.bfloat16, device=dev)
     with torch.cuda.device(dev):
         B.moe_experts_rows(wfmt, d, inter, e, _ptr(blobs), stride, _ptr(xs), _ptr(scale), _ptr(offsets), n, _ptr(h), _ptr(gu), _ptr(ys), s)
@@ -214,10 +214,10 @@ def experts_rows_backward(weight_fmt, blobs, inter, xs, offsets, kept, dys, *, r
     wfmt, e, stride, n, d = _experts(weight_fmt, blobs, inter, xs, offsets)
     pitch = (inter + 63) // 64 * 64
     _dense(dys, (n, d), torch.bfloat16, "dys"), _dense(kept.h, (n, pitch), torch.bfloat16, "kept.h")
-    _dense(kept.gu, (n, 2, pitch), torch.bfloat16, "kept.gu")
+    _dense(kept.gu, (n, 2, pitch), torch.float32, "kept.gu")
     dev = xs.device
     s = _stream(dev, blobs, offsets, dys, kept.h, kept.gu)
-    dgu = torch.empty_like(kept.gu)
+    dgu = torch.empty((n, 2, pitch), dtype=torch.bfloat16, device=dev)
     dxs = torch.empty_like(xs) if rows else None
     dblobs = torch.empty_like(blobs) if weights else None
     with torch.cuda.device(dev):
