@@ -16,10 +16,10 @@
 // holds every code exactly.
 //
 // A workgroup of eight wavefronts has a compute unit to itself and walks over tiles of up to 256 x 256, a wavefront 128 x 64 of
-// it.  Steps of 32 (8-bit: 64) summed values go through a ring of five 32 KB stages in LDS, filled by loads that bypass the
-// registers, two stages at a time: up to four, 128 KB a compute unit, are on their way while one is used.  The fragments of the next step are read
-// while the matrix cores work on this one's, so a step costs one barrier.  The next tile's first stages are requested ahead of
-// the results' stores.
+// it.  The summed index goes through LDS in stages of 64 (8-bit: 128) values, whole 128-byte lines, filled by loads that bypass
+// the registers: two stages of the rows' side, which other workgroups of the XCD read too, and three of the weights' side, which
+// comes from memory.  A stage is two steps of the matrix cores; the fragments of the next step are read while they work on this
+// one's, and there is one barrier a stage.  The next tile's first stages are requested ahead of the results' stores.
 //
 // Which expert and which of its rows a tile has is worked out from `offsets` on the device.  All loads go through buffer
 // resources that end where the expert's rows or records end: what lies beyond arrives as zeros.
@@ -39,8 +39,9 @@ typedef __amdgpu_buffer_rsrc_t Buffer;
 constexpr int kCols = 256;        // columns of a tile (128 records where each has two products)
 constexpr int kMaxBlocks = 8;     // 32-row blocks of a tile at most
 constexpr int kWavesWg = 8, kBlock = kWavesWg * 64;
-constexpr int kStageBytes = 32768, kHalf = 16384;  // a stage: 16 KB of the rows' side, 16 KB of the weights' side
-constexpr int kStages = 5;                         // 160 KB, all of a compute unit's LDS
+constexpr int kStageBytes = 32768;                 // of one side
+constexpr int kRowStages = 2, kWeightStages = 3;   // 160 KB, all of a compute unit's LDS
+constexpr uint32_t kWeightBase = kRowStages * kStageBytes, kLdsBytes = (kRowStages + kWeightStages) * kStageBytes;
 
 enum { kUp = 0, kDgu = 1, kColumns = 2, kWeights = 3 };
 
@@ -66,10 +67,10 @@ __device__ __forceinline__ Buffer buffer_of(const void *base, uint32_t bytes) {
 __device__ __forceinline__ void to_lds(Buffer b, uint32_t off, uint32_t at, uint8_t *lds) {
   __builtin_amdgcn_raw_ptr_buffer_load_lds(b, LDS_PTR(void, lds), 16, off, at, 0, 0);
 }
-// all but the last N loads of the workgroup's wavefronts have landed
+// all but the last N loads of each wavefront of the workgroup have landed, and the reads of LDS that they have issued are done
 template <int N>
 __device__ __forceinline__ void landed_but() {
-  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 }
@@ -165,14 +166,13 @@ __device__ __forceinline__ Tile find_tile(const ExpertRowsParams &p, const TileP
 __device__ __forceinline__ Tile uniform_tile(const Tile &t) { return Tile{uniform(t.expert), uniform(t.row0), uniform(t.rows), uniform(t.col)}; }
 
 // ---- LDS images -------------------------------------------------------------------------------------------
-// Side by side: 256 rows of 64 bytes, four 16-byte chunks.  Chunk c of row r lies at c ^ f(r).  A fragment's lanes read 16 bytes
-// of 16 rows each, in four turns; a turn takes four lanes each of four groups: rows 0-3 and 12-15 at one chunk and rows 4-11 at
-// its neighbour, or the other way round.  f, by the row's group of four, spreads both kinds over all banks.  The groups are 4
-// rows in a row where a fragment has 16 rows in a row, and 4 of each 8 where it has those.
-__device__ __forceinline__ int spread(int four) { return (((four ^ (four >> 1)) & 1) << 1) | ((four >> 1) & 1); }
-__device__ __forceinline__ int swap_rows(int r) { return spread(r >> 2); }
-__device__ __forceinline__ int swap_fours(int r) { return spread(r >> 3); }
-// Transposed, 16-bit: 32 rows (the summed index) of 256 columns, 512 bytes.  Where a fragment has 16 columns in a row, their 32
+// Side by side: 256 rows of 128 bytes, eight 16-byte chunks, the first four for the stage's first step.  Chunk c of row r lies at
+// c ^ f(r).  A fragment's lanes read 16 bytes of 16 rows each, in four turns; a turn takes four lanes each of four groups: rows
+// 0-3 and 12-15 at one chunk and rows 4-11 at its neighbour, or the other way round.  f spreads both kinds over all banks, where a
+// fragment has 16 rows in a row and where it has 4 of each 8.
+__device__ __forceinline__ int swap_rows(int r) { return (r >> 1) & 7; }
+__device__ __forceinline__ int swap_fours(int r) { return ((r >> 1) & 1) | ((r >> 2) & 6); }
+// Transposed, 16-bit: 64 rows (the summed index) of 256 columns, 512 bytes.  Where a fragment has 16 columns in a row, their 32
 // bytes (group g) lie at g ^ swap16(k); where it has 4 of each 8, 64 bytes (group g) lie at g ^ k % 4.
 __device__ __forceinline__ int swap16(int k) { return (k & 3) | ((k >> 1) & 4); }
 // Results: register i of a lane is column (lane / 16) * 4 + i of a fragment.  With PAIRED fragments j and j + 1 have 4 columns
@@ -235,7 +235,8 @@ __device__ __forceinline__ float sigmoid(float g) { return __builtin_amdgcn_rcpf
 template <int FORM, bool INT8>
 struct Product {
   static constexpr int EL = INT8 ? 1 : 2;
-  static constexpr int B_LOADS = FORM == kColumns && INT8 ? 1 : 2, LOADS = 2 + B_LOADS;
+  static constexpr bool NARROW = FORM == kColumns && INT8;       // the weights' stage is of bytes: half as long
+  static constexpr int A_LOADS = 4, B_LOADS = NARROW ? 2 : 4;  // of a wavefront for a stage
   using Acc = std::conditional_t<INT8 && FORM == kUp, i32x4, f32x4>;
 
   const ProductArgs g;  // (a copy: through a reference the arguments would not be known to be the same in every lane)
@@ -244,14 +245,17 @@ struct Product {
   uint32_t row_bytes;
   // the tile whose loads are being issued
   Buffer a, b;
-  uint32_t a_off[2], b_off[2];
-  int steps;  // even
-  // the stage that is requested next: its place in the ring and where its operands are
-  uint32_t put, a_at, b_at;
+  // the lane's place in loads 0 and 1; 2 and 3 are a_more, b_more behind them (side by side the weights' are exchanged otherwise)
+  static constexpr bool SIDE = FORM == kUp || FORM == kDgu;
+  uint32_t a_off[2], b_off[SIDE ? 4 : 2];
+  uint32_t a_more, b_more;
+  int stages;
+  // the stages that are requested next: their places and where their operands are
+  uint32_t a_put, b_put, a_at, b_at;
   int section_left;                              // kColumns: stages of the first section to come
-  const uint8_t *a_base, *b_base;                // kWeights: of the stage
+  const uint8_t *a_base, *b_base;                // kWeights
   uint32_t a_row, b_row, a_skip, b_skip;
-  int rows_left;
+  int a_rows_left, b_rows_left;
 
   __device__ __forceinline__ Product(const ProductArgs &args, uint8_t *l) : g(args), lds(l) {
     lane = threadIdx.x & 63;
@@ -262,27 +266,27 @@ struct Product {
     row_bytes = (uint32_t)g.p.hidden * EL;
   }
 
-  // offsets of the lane's loads of a side-by-side image
-  __device__ __forceinline__ int side_row(int i) const { return (wave * 2 + i) * 16 + lane / 4; }
-
   __device__ __forceinline__ void open(const Tile &t) {
     const ExpertRowsParams &p = g.p;
-    put = a_at = b_at = 0;
+    a_put = a_at = b_at = 0;
+    b_put = kWeightBase;
     if constexpr (FORM == kWeights) {
       // t.col: columns of the gradient; t.row0, t.rows: its rows, 2 * pitch of gate and up, then pitch of down
       const bool down = t.row0 >= 2 * pitch;
       const int m0 = down ? t.row0 - 2 * pitch : t.row0, row0 = uniform(first_row(p, t.expert));
-      rows_left = uniform(row_count(p, t.expert));
-      steps = (rows_left + 63) / 64 * 2;  // (an even number, as the other forms have; rows that are not there are zeros)
+      a_rows_left = b_rows_left = uniform(row_count(p, t.expert));
+      stages = (a_rows_left + 63) / 64;
       a_row = (down ? pitch : 2 * pitch) * 2;
       b_row = row_bytes;
       a_skip = m0 * 2;
       b_skip = t.col * kCols * 2;
       a_base = (down ? g.a2 : g.a) + (int64_t)row0 * a_row + a_skip;
       b_base = (down ? g.b2 : g.b) + (int64_t)row0 * b_row + b_skip;
+      a_more = 4 * a_row;
+      b_more = 4 * b_row;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const int k = (wave * 2 + i) * 2 + lane / 32, pos = lane & 31;
+        const int k = (wave * 4 + i) * 2 + lane / 32, pos = lane & 31;
         a_off[i] = k * a_row + (pos ^ (swap16(k) << 1)) * 16;
         b_off[i] = k * b_row + (pos ^ ((k & 3) << 2)) * 16;
       }
@@ -290,116 +294,117 @@ struct Product {
       const uint32_t rec_bytes = 3 * row_bytes, a_bytes = FORM == kColumns ? (uint32_t)g.a_pitch * 2 : row_bytes;
       a = buffer_of(g.a + (int64_t)t.row0 * a_bytes, t.rows * a_bytes);
       b = buffer_of(p.blobs + t.expert * p.blob_stride, (uint32_t)p.inter * rec_bytes);
+      a_more = 16 * a_bytes;
+      b_more = 4 * rec_bytes;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const int r = side_row(i);
-        a_off[i] = (uint32_t)r * a_bytes + ((lane & 3) ^ swap_rows(r)) * 16;
-        if constexpr (FORM == kColumns) {
-          if constexpr (INT8) {
-            const int k = wave * 4 + lane / 16;
-            b_off[i] = (uint32_t)k * rec_bytes + t.col * kCols + ((lane & 15) ^ (k & 15)) * 16;
-          } else {
-            const int k = (wave * 2 + i) * 2 + lane / 32;
-            b_off[i] = (uint32_t)k * rec_bytes + t.col * kCols * 2 + ((lane & 31) ^ (swap16(k) << 1)) * 16;
-          }
-        } else {
+        const int r = (wave * 4 + i) * 8 + lane / 8;
+        a_off[i] = (uint32_t)r * a_bytes + ((lane & 7) ^ swap_rows(r)) * 16;
+        if constexpr (NARROW) {
+          const int k = (wave * 2 + i) * 4 + lane / 16;
+          b_off[i] = (uint32_t)k * rec_bytes + t.col * kCols + ((lane & 15) ^ (k & 15)) * 16;
+        } else if constexpr (FORM == kColumns) {
+          const int k = (wave * 4 + i) * 2 + lane / 32;
+          b_off[i] = (uint32_t)k * rec_bytes + t.col * kCols * 2 + ((lane & 31) ^ (swap16(k) << 1)) * 16;
+        }
+      }
+      if constexpr (SIDE) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          // kUp: of each 64 rows the first 32 are gate rows, the others the same records' up rows.  (A record that is not there
+          // lies behind the end of the resource.)
+          const int r = (wave * 4 + i) * 8 + lane / 8;
           const int rec = FORM == kUp ? t.col * 128 + (r >> 6) * 32 + (r & 31) : t.col * kCols + r, which = FORM == kUp ? (r >> 5) & 1 : 2;
-          // (a record that is not there: outside of the resource)
-          b_off[i] = rec < p.inter ? (uint32_t)(rec * 3 + which) * row_bytes + ((lane & 3) ^ swap_fours(r)) * 16 : kNowhere;
+          b_off[i] = (uint32_t)(rec * 3 + which) * row_bytes + ((lane & 7) ^ swap_fours(r)) * 16;
         }
       }
       if constexpr (FORM == kColumns) b_at = g.first * row_bytes;
-      section_left = pitch / 32;
-      steps = FORM == kColumns ? section_left * g.sections : row_bytes / 64;
+      section_left = pitch / 64;
+      stages = FORM == kColumns ? section_left * g.sections : row_bytes / 128;
     }
   }
 
-  // Requests the next two stages (behind a tile's last one: what comes next in memory, or zeros), load by load in turn: where
-  // the summed index lies side by side, the two stages have the two halves of each 128-byte line.
-  __device__ __forceinline__ void stage_pair() {
-    const uint32_t second = ring_next(put);
-    uint8_t *at0 = lds + put + wave * 2048, *at1 = lds + second + wave * 2048;
+  // Requests the next stage of a side (behind a tile's last one: what comes next in memory, or zeros).
+  __device__ __forceinline__ void request_rows() {
+    uint8_t *at = lds + a_put + wave * 4096;
     if constexpr (FORM == kWeights) {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        uint8_t *at = h ? at1 : at0;
-        const int n = max(min(32, rows_left), 0);
-        const Buffer as = buffer_of(a_base, n > 0 ? n * a_row - a_skip : 0), bs = buffer_of(b_base, n > 0 ? n * b_row - b_skip : 0);
-#pragma unroll
-        for (int i = 0; i < 2; ++i) to_lds(as, a_off[i], 0, at + i * 1024);
-#pragma unroll
-        for (int i = 0; i < 2; ++i) to_lds(bs, b_off[i], 0, at + kHalf + i * 1024);
-        advance();
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        to_lds(a, a_off[i], a_at, at0 + i * 1024);
-        to_lds(a, a_off[i], a_at + 64, at1 + i * 1024);
-      }
-      const uint32_t b0 = b_at;
-      advance();
-      const uint32_t b1 = b_at;
-      advance();
-#pragma unroll
-      for (int i = 0; i < B_LOADS; ++i) {
-        to_lds(b, b_off[i], b0, FORM == kColumns && INT8 ? lds + put + kHalf + wave * 1024 : at0 + kHalf + i * 1024);
-        to_lds(b, b_off[i], b1, FORM == kColumns && INT8 ? lds + second + kHalf + wave * 1024 : at1 + kHalf + i * 1024);
-      }
+      const int n = max(min(64, a_rows_left), 0);
+      a = buffer_of(a_base, n > 0 ? n * a_row - a_skip : 0);
     }
-    put = ring_next(second);
+#pragma unroll
+    for (int i = 0; i < A_LOADS; ++i) to_lds(a, a_off[i & 1], (FORM == kWeights ? 0 : a_at) + (i >> 1) * a_more, at + i * 1024);
+    next_rows();
   }
-  // to the operands of the next stage
-  __device__ __forceinline__ void advance() {
+  __device__ __forceinline__ void request_weights() {
+    uint8_t *at = lds + b_put + wave * (NARROW ? 2048 : 4096);
     if constexpr (FORM == kWeights) {
-      rows_left -= 32;
-      a_base += 32 * a_row;
-      b_base += 32 * b_row;
+      const int n = max(min(64, b_rows_left), 0);
+      b = buffer_of(b_base, n > 0 ? n * b_row - b_skip : 0);
+    }
+#pragma unroll
+    for (int i = 0; i < B_LOADS; ++i) to_lds(b, b_off[SIDE ? i : i & 1], (FORM == kWeights ? 0 : b_at) + (SIDE ? 0 : (i >> 1) * b_more), at + i * 1024);
+    next_weights();
+  }
+  __device__ __forceinline__ void next_rows() {
+    a_put = next_row_stage(a_put);
+    if constexpr (FORM == kWeights) {
+      a_rows_left -= 64;
+      a_base += 64 * a_row;
     } else {
-      a_at += 64;
-      if constexpr (FORM == kColumns) {
-        // (behind the last record: outside of the resource)
-        b_at += 32 * 3 * row_bytes;
-        if (--section_left == 0) b_at = (g.first + 1) * row_bytes;
-      } else {
-        b_at += 64;
-      }
+      a_at += 128;
     }
   }
-  static __device__ __forceinline__ uint32_t ring_next(uint32_t at) { return at == (kStages - 1) * kStageBytes ? 0 : at + kStageBytes; }
+  __device__ __forceinline__ void next_weights() {
+    b_put = next_weight_stage(b_put);
+    if constexpr (FORM == kWeights) {
+      b_rows_left -= 64;
+      b_base += 64 * b_row;
+    } else if constexpr (FORM == kColumns) {
+      // (behind the last record: outside of the resource)
+      b_at += 64 * 3 * row_bytes;
+      if (--section_left == 0) b_at = (g.first + 1) * row_bytes;
+    } else {
+      b_at += 128;
+    }
+  }
+  static __device__ __forceinline__ uint32_t next_row_stage(uint32_t at) { return kStageBytes - at; }
+  static __device__ __forceinline__ uint32_t next_weight_stage(uint32_t at) { return at == kLdsBytes - kStageBytes ? kWeightBase : at + kStageBytes; }
   // the first stages of a tile; nobody reads LDS any more
-  __device__ __forceinline__ void stage_first() {
-    stage_pair();
-    stage_pair();
+  __device__ __forceinline__ void request_first() {
+    request_rows();
+    request_weights();
+    request_rows();
+    request_weights();
+    request_weights();
   }
-  // as stage_first leaves it, for the tile that it was called for
+  // as request_first leaves it, for the tile that it was called for
   __device__ __forceinline__ void skip_first() {
-#pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      advance();
-      put = ring_next(put);
-    }
+    next_rows();
+    next_rows();
+    next_weights();
+    next_weights();
+    next_weights();
   }
 
-  // Where the lane's fragments lie in a stage: of the weights for each j, of the rows for block 0.
+  // Where the lane's fragments lie in a stage: of the weights for each j, of the rows for block 0; of the stage's first step.
   __device__ __forceinline__ void fragment_offsets(uint32_t (&w_at)[4], uint32_t &x_at) const {
     const int l = lane & 15, q = lane >> 4;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       if constexpr (FORM == kWeights) {
         const int k = q * 8 + (l >> 2), chunk = wn * 8 + (j >> 1) * 4 + (l & 3);
-        w_at[j] = kHalf + k * 512 + ((chunk ^ ((k & 3) << 2)) * 16) + (j & 1) * 8;
-      } else if constexpr (FORM == kColumns && INT8) {
+        w_at[j] = k * 512 + ((chunk ^ ((k & 3) << 2)) * 16) + (j & 1) * 8;
+      } else if constexpr (NARROW) {
         const int k = q * 8 + (l >> 1);
-        w_at[j] = kHalf + k * 256 + (((wn * 4 + j) ^ (k & 15)) * 16) + (l & 1) * 8;
+        w_at[j] = k * 256 + (((wn * 4 + j) ^ (k & 15)) * 16) + (l & 1) * 8;
       } else if constexpr (FORM == kColumns) {
         const int k = q * 8 + (l >> 2);
-        w_at[j] = kHalf + k * 512 + (((wn * 4 + j) ^ swap16(k)) * 32) + (l & 3) * 8;
+        w_at[j] = k * 512 + (((wn * 4 + j) ^ swap16(k)) * 32) + (l & 3) * 8;
       } else {
         // kUp: fragments 0, 2 are gate rows, 1, 3 up rows
         const int four = FORM == kUp ? j >> 1 : j & 1, half = FORM == kUp ? j & 1 : j >> 1;
         const int r = wn * 64 + half * 32 + (l >> 2) * 8 + four * 4 + (l & 3);
-        w_at[j] = kHalf + r * 64 + ((q ^ swap_fours(r)) * 16);
+        w_at[j] = r * 128 + ((q ^ swap_fours(r)) * 16);
       }
     }
     if constexpr (FORM == kWeights) {
@@ -407,22 +412,25 @@ struct Product {
       x_at = k * 512 + ((wm ^ swap16(k)) * 32) + (l & 3) * 8;
     } else {
       const int r = wm * 16 + l;
-      x_at = r * 64 + ((q ^ swap_rows(r)) * 16);
+      x_at = r * 128 + ((q ^ swap_rows(r)) * 16);
     }
   }
-  __device__ __forceinline__ i32x4 read_w(uint32_t at) const {
-    if constexpr (FORM == kWeights || (FORM == kColumns && !INT8)) return transposed(lds + at);
-    else if constexpr (FORM == kColumns) return widen(__builtin_amdgcn_ds_read_tr8_b64_v2i32(LDS_PTR(i32x2, lds + at)));
-    else {
-      i32x4 w = *reinterpret_cast<const i32x4 *>(lds + at);
+  // second: of the stage's second step
+  __device__ __forceinline__ i32x4 read_w(uint32_t w_at, uint32_t stage, bool second) const {
+    if constexpr (NARROW) {
+      return widen(__builtin_amdgcn_ds_read_tr8_b64_v2i32(LDS_PTR(i32x2, lds + stage + w_at + (second ? 32 * 256 : 0))));
+    } else if constexpr (FORM == kWeights || FORM == kColumns) {
+      return transposed(lds + stage + w_at + (second ? 32 * 512 : 0));
+    } else {
+      i32x4 w = *reinterpret_cast<const i32x4 *>(lds + stage + (w_at ^ (second ? 64 : 0)));
       if constexpr (INT8) w ^= (int)0x80808080;
       return w;
     }
   }
-  // block m; at: of block 0 (transposed, the block is part of what was exchanged: see swap16)
-  __device__ __forceinline__ i32x4 read_x(uint32_t x_at, uint32_t ring, int m) const {
-    if constexpr (FORM == kWeights) return transposed(lds + ring + (x_at ^ (m * 64)));
-    else return *reinterpret_cast<const i32x4 *>(lds + ring + x_at + m * 2048);
+  // block m (transposed, the block is part of what was exchanged: see swap16)
+  __device__ __forceinline__ i32x4 read_x(uint32_t x_at, uint32_t stage, bool second, int m) const {
+    if constexpr (FORM == kWeights) return transposed(lds + stage + (x_at ^ (m * 64)) + (second ? 32 * 512 : 0));
+    else return *reinterpret_cast<const i32x4 *>(lds + stage + (x_at ^ (second ? 64 : 0)) + m * 4096);
   }
 
   // the product of the tile that is open; then `next` opens the next one, and the results are stored
@@ -435,40 +443,38 @@ struct Product {
 #pragma unroll
       for (int j = 0; j < 4; ++j) acc[m][j] = Acc{};
     i32x4 x[kMaxBlocks], w0[4], w1[4];
-    uint32_t w_at[4], x_at, ring = 0;  // ring: place of the stage whose fragments are read
+    uint32_t w_at[4], x_at, rows_stage = 0, weights_stage = kWeightBase;  // the stages whose fragments are read
     fragment_offsets(w_at, x_at);
-    // Step s works on stage s and reads the fragments of stage s + 1, a block's once the block of this step has gone to the matrix
-    // cores.  At an even step everybody has read stage s: with stage s - 1 it leaves room for stages s + 4 and s + 5.  At an odd
-    // one stages s + 1 and s + 2 have landed, the two behind them may be on their way.  Blocks that the tile does not have are
-    // jumped over.  (Behind the last step stages are requested and read that nobody uses.)
-    const auto step = [&](i32x4 (&now)[4], i32x4 (&then)[4], bool even) MOE_ROWS_INLINE {
-      if (even) {
-        everybody_has_read();
-        stage_pair();
-      } else {
-        landed_but<2 * LOADS>();
-      }
-      ring = ring_next(ring);
+    // A step reads the fragments of the next one, a block's once the block of this step has gone to the matrix cores.  Blocks that
+    // the tile does not have are jumped over.
+    const auto step = [&](i32x4 (&now)[4], i32x4 (&then)[4], bool second) MOE_ROWS_INLINE {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) then[j] = read_w(ring + w_at[j]);
+      for (int j = 0; j < 4; ++j) then[j] = read_w(w_at[j], weights_stage, second);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int m = 0; m < kMaxBlocks; ++m) {
         if (m > 0 && m >= blocks) break;
 #pragma unroll
         for (int j = 0; j < 4; ++j) acc[m][j] = mma(now[j], x[m], acc[m][j]);
-        x[m] = read_x(x_at, ring, m);
+        x[m] = read_x(x_at, rows_stage, second, m);
         __builtin_amdgcn_sched_barrier(0);
       }
     };
-    if (steps > 0) {
-      landed_but<0>();
+    if (stages > 0) {
+      landed_but<A_LOADS + 2 * B_LOADS>();
 #pragma unroll
-      for (int j = 0; j < 4; ++j) w0[j] = read_w(w_at[j]);
+      for (int j = 0; j < 4; ++j) w0[j] = read_w(w_at[j], weights_stage, false);
 #pragma unroll
-      for (int m = 0; m < kMaxBlocks; ++m) x[m] = read_x(x_at, 0, m);
-      for (int left = steps; left > 0; left -= 2) {
+      for (int m = 0; m < kMaxBlocks; ++m) x[m] = read_x(x_at, rows_stage, false, m);
+      for (int left = stages; left > 0; --left) {
         step(w0, w1, true);
+        // Everybody has read all of this stage: its places are free.  The next one has landed when no more than the weights of
+        // the one behind it are outstanding.  (Behind the last stage what is requested and read is not used.)
+        landed_but<B_LOADS>();
+        request_rows();
+        request_weights();
+        rows_stage = next_row_stage(rows_stage);
+        weights_stage = next_weight_stage(weights_stage);
         step(w1, w0, false);
       }
     }
@@ -592,7 +598,7 @@ struct Product {
 
 template <int FORM, bool INT8>
 __global__ __launch_bounds__(kBlock, 2) void product_kernel(const ProductArgs g) {
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[kStages * kStageBytes];
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[kLdsBytes];
   Product<FORM, INT8> f(g, lds);
   const ExpertRowsParams &p = g.p;
   const int workgroups = gridDim.x, per_xcd = workgroups / 8, xcd = blockIdx.x & 7;
@@ -620,7 +626,7 @@ __global__ __launch_bounds__(kBlock, 2) void product_kernel(const ProductArgs g)
   Tile now = uniform_tile(tile(i));
   if (now.expert >= 0) {
     f.open(now);
-    f.stage_first();
+    f.request_first();
   }
   if constexpr (FORM == kColumns) {  // rows of nobody
     const int used = uniform(min(max(p.offsets[p.n_experts], 0), p.n_rows));
@@ -636,7 +642,7 @@ __global__ __launch_bounds__(kBlock, 2) void product_kernel(const ProductArgs g)
     const auto open_next = [&]() MOE_ROWS_INLINE {
       if (next.expert < 0) return;
       f.open(next);
-      f.stage_first();
+      f.request_first();
     };
     f.run(now, open_next);
     now = uniform_tile(next);
