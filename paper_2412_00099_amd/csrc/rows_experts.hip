@@ -19,7 +19,7 @@
 // it.  The summed index goes through LDS in stages of 64 (8-bit: 128) values, whole 128-byte lines, filled by loads that bypass
 // the registers: two stages of the rows' side, which other workgroups of the XCD read too, and three of the weights' side, which
 // comes from memory.  A stage is two steps of the matrix cores; the fragments of the next step are read while they work on this
-// one's, and there is one barrier a stage.  The next tile's first stages are requested ahead of the results' stores.
+// one's, and there is one barrier a stage.  Both rings run on from tile to tile.
 //
 // Which expert and which of its rows a tile has is worked out from `offsets` on the device.  All loads go through buffer
 // resources that end where the expert's rows or records end: what lies beyond arrives as zeros.
@@ -74,96 +74,127 @@ __device__ __forceinline__ void landed_but() {
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 }
-// the reads of LDS that the workgroup has issued are done
-__device__ __forceinline__ void everybody_has_read() {
-  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-  __builtin_amdgcn_s_barrier();
-  asm volatile("" ::: "memory");
-}
-
 __device__ __forceinline__ f32x4 mma(i32x4 a, i32x4 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 __device__ __forceinline__ i32x4 mma(i32x4 a, i32x4 b, i32x4 c) { return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0); }
 
 // ---- tiles ------------------------------------------------------------------------------------------------
+// kWeights: row0, rows are the expert's, col = tile of the gradient's rows * n_cols + tile of its columns
 struct Tile {
   int expert;  // -1: no tile
-  int row0, rows;
-  int col;
+  int row0, rows, col;
 };
 __device__ __forceinline__ int first_row(const ExpertRowsParams &p, int e) { return min(max(p.offsets[e], 0), p.n_rows); }
 __device__ __forceinline__ int row_count(const ExpertRowsParams &p, int e) { return max(min(p.offsets[e + 1], p.n_rows) - first_row(p, e), 0); }
-__device__ __forceinline__ int wave_total(int v) {
+template <typename T>
+__device__ __forceinline__ T wave_total(T v) {
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o);
-  return uniform(v);
+  return v;
+}
+template <typename T>
+__device__ __forceinline__ T sum_upto(T v, int lane) {  // of lanes 0 .. lane
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const T y = __shfl_up(v, o);
+    if (lane >= o) v += y;
+  }
+  return v;
 }
 
-// An expert's rows are cut into the fewest parts of at most `blocks` 32-row blocks, all of nearly the same size.  `blocks` is
-// the size from 4 to 8 for which the launch's rounds of one tile a workgroup take the least time: a tile costs its rows and, for
-// the weights that have to come in whatever its rows are, about 64 more.
-struct TilePlan {
-  int blocks, total;
+// What an expert's tiles are.  Its rows are cut into the fewest parts of at most 256, all of nearly the same size.  cost: of a
+// tile, in rows; that the weights have to come in costs about as much as 128 rows do (kWeights: 256 columns times the rows, and the
+// stores).
+struct ExpertTiles {
+  int parts, each, n, cost;
 };
-__device__ __forceinline__ TilePlan plan_tiles(const ExpertRowsParams &p, int n_cols, int workgroups) {
-  const int lane = threadIdx.x & 63;
-  int n[5] = {};
-  for (int e = lane; e < p.n_experts; e += 64) {
-    const int c = row_count(p, e);
-#pragma unroll
-    for (int i = 0; i < 5; ++i) n[i] += (c + (4 + i) * 32 - 1) / ((4 + i) * 32);
-  }
-  TilePlan best{8, 0};
-  int64_t least = INT64_MAX;
-#pragma unroll
-  for (int i = 4; i >= 0; --i) {
-    const int total = wave_total(n[i]) * n_cols;
-    const int64_t cost = (int64_t)((total + workgroups - 1) / workgroups) * ((4 + i) * 32 + 64);
-    if (cost < least) {
-      least = cost;
-      best.blocks = 4 + i;
-      best.total = total;
-    }
-  }
-  return best;
+template <int FORM>
+__device__ __forceinline__ ExpertTiles expert_tiles(int count, int n_cols, int m_tiles) {
+  ExpertTiles t;
+  t.parts = (count + 255) / 256;
+  t.each = t.parts > 0 ? ((count + t.parts - 1) / t.parts + 15) / 16 * 16 : 0;
+  t.n = FORM == kWeights ? m_tiles * n_cols : t.parts * n_cols;
+  t.cost = FORM == kWeights ? count + 384 : t.each + 128;
+  return t;
 }
-// Tiles in the order expert, column, row, so that the workgroups that share weights are neighbours; the list is dealt to the
-// eight XCDs in eight parts, since workgroups go to them in turn and each has an L2 of its own.
-__device__ __forceinline__ Tile find_tile(const ExpertRowsParams &p, const TilePlan &plan, int n_cols, int in_part, int xcd) {
-  const int lane = threadIdx.x & 63;
-  Tile r{-1, 0, 0, 0};
-  const int part = (plan.total + 7) / 8, want = xcd * part + in_part;
-  if (in_part >= part || want >= plan.total) return r;
-  int before = 0;
-  const int most = plan.blocks * 32;
+// Tiles in the order expert, column, row, so that the workgroups that share weights are neighbours.  The list is cut into eight
+// parts of the same cost, one for each XCD: workgroups go to the XCDs in turn and each XCD has an L2 of its own.  Within a part the
+// XCD's workgroups take tiles in turn.
+struct TileList {
+  int next, end, step;  // the workgroup's tiles: next, next + step, .. below end
+};
+template <int FORM>
+__device__ __forceinline__ TileList deal_tiles(const ExpertRowsParams &p, int n_cols, int m_tiles) {
+  const int lane = threadIdx.x & 63, xcd = blockIdx.x & 7;
+  int64_t cost = 0;
+  for (int e = lane; e < p.n_experts; e += 64) {
+    const ExpertTiles t = expert_tiles<FORM>(row_count(p, e), n_cols, m_tiles);
+    cost += (int64_t)t.n * t.cost;
+  }
+  cost = wave_total(cost);
+  const int64_t from = cost * xcd / 8, to = cost * (xcd + 1) / 8;
+  int begin = -1, end = -1, tiles = 0;
+  int64_t before = 0;
   for (int e0 = 0; e0 < p.n_experts; e0 += 64) {
-    const int e = e0 + lane, c = e < p.n_experts ? row_count(p, e) : 0;
-    const int parts = (c + most - 1) / most, t = parts * n_cols;
-    int upto = t;
+    const int e = e0 + lane;
+    const ExpertTiles t = e < p.n_experts ? expert_tiles<FORM>(row_count(p, e), n_cols, m_tiles) : ExpertTiles{0, 0, 0, 1};
+    const int64_t own = (int64_t)t.n * t.cost, past = before + sum_upto(own, lane), first = past - own;
+    const int first_tile = tiles + sum_upto(t.n, lane) - t.n;
+    const int b = first <= from && from < past ? first_tile + (int)((from - first + t.cost - 1) / t.cost) : -1;
+    const int l = first <= to && to < past ? first_tile + (int)((to - first + t.cost - 1) / t.cost) : -1;
+    begin = max(begin, b);
+    end = max(end, l);
+    before = __shfl(past, 63);
+    tiles = __shfl(first_tile + t.n, 63);
+  }
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int y = __shfl_up(upto, o);
-      if (lane >= o) upto += y;
-    }
-    const uint64_t past = __ballot(before + upto > want);
-    if (past != 0) {
-      const int l = uniform(__ffsll((unsigned long long)past) - 1);
-      const int left = want - before - uniform(__shfl(upto - t, l)), count = uniform(__shfl(c, l)), of = uniform(__shfl(parts, l));
+  for (int o = 1; o < 64; o <<= 1) {
+    begin = max(begin, __shfl_xor(begin, o));
+    end = max(end, __shfl_xor(end, o));
+  }
+  TileList r;
+  r.step = gridDim.x / 8;
+  r.next = uniform(begin < 0 ? tiles : begin) + (blockIdx.x >> 3);
+  r.end = uniform(end < 0 ? tiles : end);
+  return r;
+}
+// Lane i: tile list.next + i * list.step
+template <int FORM>
+__device__ __forceinline__ Tile lane_tile(const ExpertRowsParams &p, const TileList &list, int n_cols, int m_tiles) {
+  const int lane = threadIdx.x & 63;
+  const int64_t at = list.next + (int64_t)lane * list.step;
+  const int want = at < list.end ? (int)at : -1;
+  Tile r{-1, 0, 0, 0};
+  int before = 0;
+  for (int e0 = 0; e0 < p.n_experts; e0 += 64) {
+    const int e = e0 + lane, row0 = e < p.n_experts ? first_row(p, e) : 0, count = e < p.n_experts ? row_count(p, e) : 0;
+    const ExpertTiles t = e < p.n_experts ? expert_tiles<FORM>(count, n_cols, m_tiles) : ExpertTiles{0, 0, 0, 0};
+    const int past = before + sum_upto(t.n, lane);
+    // the first expert whose tiles end behind `want`
+    int l = 0;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) l += __shfl(past, l + o - 1) <= want ? o : 0;
+    const int of = __shfl(t.parts, l), each = __shfl(t.each, l), rows = __shfl(count, l), from = __shfl(row0, l);
+    const int left = want - __shfl(past - t.n, l);
+    const int all = __shfl(past, 63);
+    if (want >= before && want < all) {
       r.expert = e0 + l;
-      r.col = left / of;
-      const int each = ((count + of - 1) / of + 15) / 16 * 16, at = (left - r.col * of) * each;
-      r.row0 = first_row(p, r.expert) + at;
-      r.rows = max(min(each, count - at), 0);
-      return r;
+      if constexpr (FORM == kWeights) {
+        r.row0 = from;
+        r.rows = rows;
+        r.col = left;
+      } else {
+        r.col = left / of;
+        const int at_row = (left - r.col * of) * each;
+        r.row0 = from + at_row;
+        r.rows = min(each, rows - at_row);
+      }
     }
-    before += uniform(__shfl(upto, 63));
+    before = all;
   }
   return r;
 }
-
-// (in scalar registers: a tile makes buffer resources and decides what is done)
-__device__ __forceinline__ Tile uniform_tile(const Tile &t) { return Tile{uniform(t.expert), uniform(t.row0), uniform(t.rows), uniform(t.col)}; }
 
 // ---- LDS images -------------------------------------------------------------------------------------------
 // Side by side: 256 rows of 128 bytes, eight 16-byte chunks, the first four for the stage's first step.  Chunk c of row r lies at
@@ -243,18 +274,21 @@ struct Product {
   uint8_t *lds;
   int lane, wave, wm, wn, pitch;
   uint32_t row_bytes;
-  // the tile whose loads are being issued
-  Buffer a, b;
-  // the lane's place in loads 0 and 1; 2 and 3 are a_more, b_more behind them (side by side the weights' are exchanged otherwise)
+  int n_cols, m_both, m_tiles;  // tiles over the columns; kWeights: over 2 * pitch rows of gate and up gradients, then pitch of down
+  // The workgroup's tiles, 64 at a time: lane i of `list` has tile listed + i, of `list_after` listed + 64 + i.
+  TileList deal;
+  Tile list, list_after;
+  int listed;
+  // What is requested next, of the rows and of the weights: the tile, how many of its stages are left, the place in the ring and
+  // where the operand is; the lane's place in loads 0 and 1 (2 and 3 are a_more, b_more behind; side by side see b_xor)
   static constexpr bool SIDE = FORM == kUp || FORM == kDgu;
-  uint32_t a_off[2], b_off[SIDE ? 4 : 2];
-  uint32_t a_more, b_more;
-  int stages;
-  // the stages that are requested next: their places and where their operands are
-  uint32_t a_put, b_put, a_at, b_at;
+  Buffer a, b;
+  int a_tile, b_tile, a_left, b_left;
+  uint32_t a_put, b_put, a_at, b_at, a_more, b_more;
+  uint32_t a_off[2], b_off[SIDE ? 1 : 2];
   int section_left;                              // kColumns: stages of the first section to come
   const uint8_t *a_base, *b_base;                // kWeights
-  uint32_t a_row, b_row, a_skip, b_skip;
+  uint32_t a_row, a_skip, b_skip;
   int a_rows_left, b_rows_left;
 
   __device__ __forceinline__ Product(const ProductArgs &args, uint8_t *l) : g(args), lds(l) {
@@ -264,127 +298,166 @@ struct Product {
     wn = wave & 3;
     pitch = expert_rows_pitch(g.p.inter);
     row_bytes = (uint32_t)g.p.hidden * EL;
+    n_cols = FORM == kUp ? (pitch + 127) / 128 : FORM == kDgu ? (pitch + kCols - 1) / kCols : g.p.hidden / kCols;
+    m_both = (2 * pitch + 255) / 256;
+    m_tiles = m_both + (pitch + 255) / 256;
+    deal = deal_tiles<FORM>(g.p, n_cols, m_tiles);
+    listed = 0;
+    list = lane_tile<FORM>(g.p, deal, n_cols, m_tiles);
+    list_more();
+    a_put = 0;
+    b_put = kWeightBase;
+    a_tile = b_tile = 0;
+    open_rows();
+    open_weights();
+  }
+  __device__ __forceinline__ void list_more() {
+    deal.next += 64 * deal.step;
+    list_after = Tile{-1, 0, 0, 0};
+    if (deal.next < deal.end) list_after = lane_tile<FORM>(g.p, deal, n_cols, m_tiles);
+  }
+  // tile i of the workgroup, the same in every lane
+  __device__ __forceinline__ Tile tile(int i) const {
+    const bool after = i - listed >= 64;
+    const int l = (i - listed) & 63;
+    const auto of = [&](int x, int y) MOE_ROWS_INLINE { return after ? __builtin_amdgcn_readlane(y, l) : __builtin_amdgcn_readlane(x, l); };
+    return Tile{of(list.expert, list_after.expert), of(list.row0, list_after.row0), of(list.rows, list_after.rows), of(list.col, list_after.col)};
+  }
+  // kWeights: the tile's rows of the gradient: first of the 3 * pitch, how many
+  __device__ __forceinline__ int gradient_row(const Tile &t) const {
+    const int m = t.col / n_cols;
+    return m < m_both ? m * 256 : 2 * pitch + (m - m_both) * 256;
+  }
+  __device__ __forceinline__ int gradient_rows(int first) const { return min(256, (first < 2 * pitch ? 2 : 3) * pitch - first); }
+  __device__ __forceinline__ int stages_of(const Tile &t) const {
+    // (an expert without rows has a stage of zeros: its gradients)
+    return FORM == kWeights ? max((t.rows + 63) / 64, 1) : FORM == kColumns ? pitch / 64 * g.sections : row_bytes / 128;
   }
 
-  __device__ __forceinline__ void open(const Tile &t) {
-    const ExpertRowsParams &p = g.p;
-    a_put = a_at = b_at = 0;
-    b_put = kWeightBase;
+  // a_tile, b_tile: from its first stage on.  Behind the last tile nothing is loaded (a resource without bytes).
+  __device__ __forceinline__ void open_rows() {
+    const Tile t = tile(a_tile);
+    const bool any = t.expert >= 0;
+    a_left = any ? stages_of(t) : INT32_MAX;
+    a_at = 0;
     if constexpr (FORM == kWeights) {
-      // t.col: columns of the gradient; t.row0, t.rows: its rows, 2 * pitch of gate and up, then pitch of down
-      const bool down = t.row0 >= 2 * pitch;
-      const int m0 = down ? t.row0 - 2 * pitch : t.row0, row0 = uniform(first_row(p, t.expert));
-      a_rows_left = b_rows_left = uniform(row_count(p, t.expert));
-      stages = (a_rows_left + 63) / 64;
+      const int m = gradient_row(t);
+      const bool down = m >= 2 * pitch;
+      a_rows_left = any ? t.rows : 0;
       a_row = (down ? pitch : 2 * pitch) * 2;
-      b_row = row_bytes;
-      a_skip = m0 * 2;
-      b_skip = t.col * kCols * 2;
-      a_base = (down ? g.a2 : g.a) + (int64_t)row0 * a_row + a_skip;
-      b_base = (down ? g.b2 : g.b) + (int64_t)row0 * b_row + b_skip;
+      a_skip = (down ? m - 2 * pitch : m) * 2;
+      a_base = (down ? g.a2 : g.a) + (int64_t)t.row0 * a_row + a_skip;
       a_more = 4 * a_row;
-      b_more = 4 * b_row;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const int k = (wave * 4 + i) * 2 + lane / 32, pos = lane & 31;
-        a_off[i] = k * a_row + (pos ^ (swap16(k) << 1)) * 16;
-        b_off[i] = k * b_row + (pos ^ ((k & 3) << 2)) * 16;
+        const int k = (wave * 4 + i) * 2 + lane / 32;
+        a_off[i] = k * a_row + ((lane & 31) ^ (swap16(k) << 1)) * 16;
       }
     } else {
-      const uint32_t rec_bytes = 3 * row_bytes, a_bytes = FORM == kColumns ? (uint32_t)g.a_pitch * 2 : row_bytes;
-      a = buffer_of(g.a + (int64_t)t.row0 * a_bytes, t.rows * a_bytes);
-      b = buffer_of(p.blobs + t.expert * p.blob_stride, (uint32_t)p.inter * rec_bytes);
+      const uint32_t a_bytes = FORM == kColumns ? (uint32_t)g.a_pitch * 2 : row_bytes;
+      a = buffer_of(g.a + (int64_t)t.row0 * a_bytes, any ? t.rows * a_bytes : 0);
       a_more = 16 * a_bytes;
-      b_more = 4 * rec_bytes;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int r = (wave * 4 + i) * 8 + lane / 8;
         a_off[i] = (uint32_t)r * a_bytes + ((lane & 7) ^ swap_rows(r)) * 16;
-        if constexpr (NARROW) {
-          const int k = (wave * 2 + i) * 4 + lane / 16;
-          b_off[i] = (uint32_t)k * rec_bytes + t.col * kCols + ((lane & 15) ^ (k & 15)) * 16;
-        } else if constexpr (FORM == kColumns) {
-          const int k = (wave * 4 + i) * 2 + lane / 32;
-          b_off[i] = (uint32_t)k * rec_bytes + t.col * kCols * 2 + ((lane & 31) ^ (swap16(k) << 1)) * 16;
-        }
       }
-      if constexpr (SIDE) {
+    }
+  }
+  __device__ __forceinline__ void open_weights() {
+    const Tile t = tile(b_tile);
+    const bool any = t.expert >= 0;
+    b_left = any ? stages_of(t) : INT32_MAX;
+    if constexpr (FORM == kWeights) {
+      const bool down = gradient_row(t) >= 2 * pitch;
+      b_at = 0;
+      b_rows_left = any ? t.rows : 0;
+      b_skip = t.col % n_cols * kCols * 2;
+      b_base = (down ? g.b2 : g.b) + (int64_t)t.row0 * row_bytes + b_skip;
+      b_more = 4 * row_bytes;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          // kUp: of each 64 rows the first 32 are gate rows, the others the same records' up rows.  (A record that is not there
-          // lies behind the end of the resource.)
-          const int r = (wave * 4 + i) * 8 + lane / 8;
-          const int rec = FORM == kUp ? t.col * 128 + (r >> 6) * 32 + (r & 31) : t.col * kCols + r, which = FORM == kUp ? (r >> 5) & 1 : 2;
-          b_off[i] = (uint32_t)(rec * 3 + which) * row_bytes + ((lane & 7) ^ swap_fours(r)) * 16;
+      for (int i = 0; i < 2; ++i) {
+        const int k = (wave * 4 + i) * 2 + lane / 32;
+        b_off[i] = k * row_bytes + ((lane & 31) ^ ((k & 3) << 2)) * 16;
+      }
+    } else {
+      const uint32_t rec_bytes = 3 * row_bytes;
+      b = buffer_of(g.p.blobs + (int64_t)max(t.expert, 0) * g.p.blob_stride, any ? (uint32_t)g.p.inter * rec_bytes : 0);
+      section_left = pitch / 64;
+      if constexpr (SIDE) {
+        // kUp: of each 64 rows of the image the first 32 are gate rows, the others the same records' up rows.  (A record that is not
+        // there lies behind the end of the resource.)  Load i has the records 8 * i further on, and its chunks are exchanged with
+        // 2 * i: see swap_fours.
+        const int r = wave * 32 + lane / 8;
+        const int rec = FORM == kUp ? t.col * 128 + (r >> 6) * 32 + (r & 31) : t.col * kCols + r, which = FORM == kUp ? (r >> 5) & 1 : 2;
+        b_off[0] = (uint32_t)(rec * 3 + which) * row_bytes + ((lane & 7) ^ ((lane >> 4) & 1)) * 16;
+        b_more = 8 * rec_bytes;
+        b_at = 0;
+      } else {
+        b_at = g.first * row_bytes;
+        b_more = 4 * rec_bytes;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          if constexpr (NARROW) {
+            const int k = (wave * 2 + i) * 4 + lane / 16;
+            b_off[i] = (uint32_t)k * rec_bytes + t.col * kCols + ((lane & 15) ^ (k & 15)) * 16;
+          } else {
+            const int k = (wave * 4 + i) * 2 + lane / 32;
+            b_off[i] = (uint32_t)k * rec_bytes + t.col * kCols * 2 + ((lane & 31) ^ (swap16(k) << 1)) * 16;
+          }
         }
       }
-      if constexpr (FORM == kColumns) b_at = g.first * row_bytes;
-      section_left = pitch / 64;
-      stages = FORM == kColumns ? section_left * g.sections : row_bytes / 128;
     }
   }
 
-  // Requests the next stage of a side (behind a tile's last one: what comes next in memory, or zeros).
+  // requests the next stage of a side, of the next tile if this one has no more
   __device__ __forceinline__ void request_rows() {
+    if (a_left == 0) {
+      ++a_tile;
+      open_rows();
+    }
+    --a_left;
     uint8_t *at = lds + a_put + wave * 4096;
     if constexpr (FORM == kWeights) {
       const int n = max(min(64, a_rows_left), 0);
       a = buffer_of(a_base, n > 0 ? n * a_row - a_skip : 0);
+      a_rows_left -= 64;
+      a_base += 64 * a_row;
     }
 #pragma unroll
-    for (int i = 0; i < A_LOADS; ++i) to_lds(a, a_off[i & 1], (FORM == kWeights ? 0 : a_at) + (i >> 1) * a_more, at + i * 1024);
-    next_rows();
+    for (int i = 0; i < A_LOADS; ++i) to_lds(a, a_off[i & 1], a_at + (i >> 1) * a_more, at + i * 1024);
+    if constexpr (FORM != kWeights) a_at += 128;
+    a_put = next_row_stage(a_put);
   }
   __device__ __forceinline__ void request_weights() {
+    if (b_left == 0) {
+      ++b_tile;
+      open_weights();
+    }
+    --b_left;
     uint8_t *at = lds + b_put + wave * (NARROW ? 2048 : 4096);
     if constexpr (FORM == kWeights) {
       const int n = max(min(64, b_rows_left), 0);
-      b = buffer_of(b_base, n > 0 ? n * b_row - b_skip : 0);
+      b = buffer_of(b_base, n > 0 ? n * row_bytes - b_skip : 0);
+      b_rows_left -= 64;
+      b_base += 64 * row_bytes;
     }
 #pragma unroll
-    for (int i = 0; i < B_LOADS; ++i) to_lds(b, b_off[SIDE ? i : i & 1], (FORM == kWeights ? 0 : b_at) + (SIDE ? 0 : (i >> 1) * b_more), at + i * 1024);
-    next_weights();
-  }
-  __device__ __forceinline__ void next_rows() {
-    a_put = next_row_stage(a_put);
-    if constexpr (FORM == kWeights) {
-      a_rows_left -= 64;
-      a_base += 64 * a_row;
-    } else {
-      a_at += 128;
+    for (int i = 0; i < B_LOADS; ++i) {
+      if constexpr (SIDE) to_lds(b, b_off[0] ^ (i * 32), b_at + i * b_more, at + i * 1024);
+      else to_lds(b, b_off[i & 1], b_at + (i >> 1) * b_more, at + i * 1024);
     }
-  }
-  __device__ __forceinline__ void next_weights() {
-    b_put = next_weight_stage(b_put);
-    if constexpr (FORM == kWeights) {
-      b_rows_left -= 64;
-      b_base += 64 * b_row;
+    if constexpr (SIDE) {
+      b_at += 128;
     } else if constexpr (FORM == kColumns) {
       // (behind the last record: outside of the resource)
       b_at += 64 * 3 * row_bytes;
       if (--section_left == 0) b_at = (g.first + 1) * row_bytes;
-    } else {
-      b_at += 128;
     }
+    b_put = next_weight_stage(b_put);
   }
   static __device__ __forceinline__ uint32_t next_row_stage(uint32_t at) { return kStageBytes - at; }
   static __device__ __forceinline__ uint32_t next_weight_stage(uint32_t at) { return at == kLdsBytes - kStageBytes ? kWeightBase : at + kStageBytes; }
-  // the first stages of a tile; nobody reads LDS any more
-  __device__ __forceinline__ void request_first() {
-    request_rows();
-    request_weights();
-    request_rows();
-    request_weights();
-    request_weights();
-  }
-  // as request_first leaves it, for the tile that it was called for
-  __device__ __forceinline__ void skip_first() {
-    next_rows();
-    next_rows();
-    next_weights();
-    next_weights();
-    next_weights();
-  }
 
   // Where the lane's fragments lie in a stage: of the weights for each j, of the rows for block 0; of the stage's first step.
   __device__ __forceinline__ void fragment_offsets(uint32_t (&w_at)[4], uint32_t &x_at) const {
@@ -433,58 +506,80 @@ struct Product {
     else return *reinterpret_cast<const i32x4 *>(lds + stage + (x_at ^ (second ? 64 : 0)) + m * 4096);
   }
 
-  // the product of the tile that is open; then `next` opens the next one, and the results are stored
-  template <typename Next>
-  __device__ __forceinline__ void run(const Tile &t, Next next) {
-    const int blocks = (t.rows + 31) / 32;  // of 32 rows; a wavefront has half of each
-    Acc acc[kMaxBlocks][4];
-#pragma unroll
-    for (int m = 0; m < kMaxBlocks; ++m)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) acc[m][j] = Acc{};
+  __device__ __forceinline__ void run() {
+    Tile t = tile(0);
+    if (t.expert < 0) return;
     i32x4 x[kMaxBlocks], w0[4], w1[4];
     uint32_t w_at[4], x_at, rows_stage = 0, weights_stage = kWeightBase;  // the stages whose fragments are read
     fragment_offsets(w_at, x_at);
-    // A step reads the fragments of the next one, a block's once the block of this step has gone to the matrix cores.  Blocks that
-    // the tile does not have are jumped over.
-    const auto step = [&](i32x4 (&now)[4], i32x4 (&then)[4], bool second) MOE_ROWS_INLINE {
+    request_rows();
+    request_weights();
+    request_rows();
+    request_weights();
+    request_weights();
+    landed_but<A_LOADS + 2 * B_LOADS>();
 #pragma unroll
-      for (int j = 0; j < 4; ++j) then[j] = read_w(w_at[j], weights_stage, second);
-      __builtin_amdgcn_sched_barrier(0);
+    for (int j = 0; j < 4; ++j) w0[j] = read_w(w_at[j], weights_stage, false);
 #pragma unroll
-      for (int m = 0; m < kMaxBlocks; ++m) {
-        if (m > 0 && m >= blocks) break;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[m][j] = mma(now[j], x[m], acc[m][j]);
-        x[m] = read_x(x_at, rows_stage, second, m);
-        __builtin_amdgcn_sched_barrier(0);
+    for (int m = 0; m < kMaxBlocks; ++m) x[m] = read_x(x_at, rows_stage, false, m);
+    int stores = 0;  // that this wavefront has issued behind its last request, at least
+    for (int i = 0; t.expert >= 0;) {
+      const int m0 = FORM == kWeights ? gradient_row(t) : 0;
+      const int blocks = ((FORM == kWeights ? gradient_rows(m0) : t.rows) + 31) / 32;  // of 32 rows; a wavefront has half of each
+      ++i;
+      if (i - listed == 64) {
+        list = list_after;
+        listed += 64;
+        list_more();
       }
-    };
-    if (stages > 0) {
-      landed_but<A_LOADS + 2 * B_LOADS>();
+      const Tile next = tile(i);
+      Acc acc[kMaxBlocks][4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) w0[j] = read_w(w_at[j], weights_stage, false);
+      for (int m = 0; m < kMaxBlocks; ++m)
 #pragma unroll
-      for (int m = 0; m < kMaxBlocks; ++m) x[m] = read_x(x_at, rows_stage, false, m);
-      for (int left = stages; left > 0; --left) {
+        for (int j = 0; j < 4; ++j) acc[m][j] = Acc{};
+      // A step reads the fragments of the next one, a block's once the block of this step has gone to the matrix cores.  Blocks that
+      // the tile does not have are jumped over.
+      const auto step = [&](i32x4 (&now)[4], i32x4 (&then)[4], bool second) MOE_ROWS_INLINE {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) then[j] = read_w(w_at[j], weights_stage, second);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int m = 0; m < kMaxBlocks; ++m) {
+          if (m > 0 && m >= blocks) break;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) acc[m][j] = mma(now[j], x[m], acc[m][j]);
+          x[m] = read_x(x_at, rows_stage, second, m);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      };
+      for (int left = stages_of(t); left > 0; --left) {
         step(w0, w1, true);
-        // Everybody has read all of this stage: its places are free.  The next one has landed when no more than the weights of
-        // the one behind it are outstanding.  (Behind the last stage what is requested and read is not used.)
-        landed_but<B_LOADS>();
+        // Everybody has read all of this stage: its places are free.  The next one has landed when no more than the weights of the
+        // one behind it are outstanding, and the stores of the tile before, which came behind those.
+        if (stores >= 24) landed_but<B_LOADS + 24>();
+        else if (stores >= 12) landed_but<B_LOADS + 12>();
+        else landed_but<B_LOADS>();
+        stores = 0;
         request_rows();
         request_weights();
         rows_stage = next_row_stage(rows_stage);
         weights_stage = next_weight_stage(weights_stage);
         step(w1, w0, false);
       }
+      // the next tile's blocks that this one did not have
+#pragma unroll
+      for (int m = 1; m < kMaxBlocks; ++m)
+        if (m >= blocks) x[m] = read_x(x_at, rows_stage, false, m);
+      store(t, m0, acc, blocks);
+      stores = blocks * (FORM == kUp ? 1 : FORM == kColumns ? 4 : FORM == kWeights ? 2 : 0);
+      t = next;
     }
-    everybody_has_read();
-    next();
-    store(t, acc, blocks);
   }
 
   // lane: row lane % 16 of each block of 16 rows; columns as said at the LDS images
-  __device__ __forceinline__ void store(const Tile &t, const Acc (&acc)[kMaxBlocks][4], int blocks) const {
+  // m0: kWeights, the tile's first row of the gradient's 3 * pitch
+  __device__ __forceinline__ void store(const Tile &t, int m0, const Acc (&acc)[kMaxBlocks][4], int blocks) const {
     const ExpertRowsParams &p = g.p;
     const int q = lane >> 4, r0 = wm * 16 + (lane & 15);
     const uint8_t *blob = p.blobs + t.expert * p.blob_stride;
@@ -578,12 +673,13 @@ struct Product {
       }
     } else {
       const Buffer out = buffer_of(g.dblobs + t.expert * p.blob_stride, (uint32_t)tail);
+      const int m_rows = gradient_rows(m0), col0 = t.col % n_cols * kCols;
 #pragma unroll
       for (int m = 0; m < kMaxBlocks; ++m) {
         if (m > 0 && m >= blocks) break;
-        const int r = r0 + m * 32, at = t.row0 + r, which = at >= 2 * pitch ? 2 : at >= pitch ? 1 : 0, rec = at - which * pitch;
+        const int r = r0 + m * 32, at = m0 + r, which = at >= 2 * pitch ? 2 : at >= pitch ? 1 : 0, rec = at - which * pitch;
         // (a record that is not there lies behind the end)
-        const uint32_t to = r < t.rows ? ((rec * 3 + which) * p.hidden + t.col * kCols + wn * 64 + q * 8) * 2 : kNowhere;
+        const uint32_t to = r < m_rows ? ((rec * 3 + which) * p.hidden + col0 + wn * 64 + q * 8) * 2 : kNowhere;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           float v[8];
@@ -599,54 +695,14 @@ struct Product {
 template <int FORM, bool INT8>
 __global__ __launch_bounds__(kBlock, 2) void product_kernel(const ProductArgs g) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds[kLdsBytes];
-  Product<FORM, INT8> f(g, lds);
-  const ExpertRowsParams &p = g.p;
-  const int workgroups = gridDim.x, per_xcd = workgroups / 8, xcd = blockIdx.x & 7;
-  const int n_cols = FORM == kUp ? (f.pitch + 127) / 128 : FORM == kDgu ? (f.pitch + kCols - 1) / kCols : p.hidden / kCols;
-  // kWeights: 2 * pitch rows of gate and up gradients, then pitch of down
-  const int m_both = (2 * f.pitch + 255) / 256, m_tiles = m_both + (f.pitch + 255) / 256;
-  TilePlan plan{8, p.n_experts * m_tiles * n_cols};
-  if constexpr (FORM != kWeights) plan = plan_tiles(p, n_cols, workgroups);
-  const auto tile = [&](int i) MOE_ROWS_INLINE {
-    if constexpr (FORM == kWeights) {
-      Tile r{-1, 0, 0, 0};
-      const int part = (plan.total + 7) / 8, want = xcd * part + i;
-      if (i >= part || want >= plan.total) return r;
-      r.col = want % n_cols;
-      const int m = want / n_cols, at = m % m_tiles;
-      r.expert = m / m_tiles;
-      r.row0 = at < m_both ? at * 256 : 2 * f.pitch + (at - m_both) * 256;
-      r.rows = min(256, (at < m_both ? 2 : 3) * f.pitch - r.row0);
-      return r;
-    } else {
-      return find_tile(p, plan, n_cols, i, xcd);
-    }
-  };
-  int i = blockIdx.x >> 3;
-  Tile now = uniform_tile(tile(i));
-  if (now.expert >= 0) {
-    f.open(now);
-    f.request_first();
-  }
   if constexpr (FORM == kColumns) {  // rows of nobody
+    const ExpertRowsParams &p = g.p;
     const int used = uniform(min(max(p.offsets[p.n_experts], 0), p.n_rows));
-    for (int64_t r = used + blockIdx.x; r < p.n_rows; r += workgroups)
+    for (int64_t r = used + blockIdx.x; r < p.n_rows; r += gridDim.x)
       for (int c = threadIdx.x * 8; c < p.hidden; c += kBlock * 8) *reinterpret_cast<rows_u32x4 *>(g.out + r * p.hidden + c) = rows_u32x4{};
   }
-  while (now.expert >= 0) {
-    // (once more: carried over from the end of the last turn, the buffers would not be known to be the same in every lane)
-    f.open(now);
-    f.skip_first();
-    i += per_xcd;
-    const Tile next = uniform_tile(tile(i));
-    const auto open_next = [&]() MOE_ROWS_INLINE {
-      if (next.expert < 0) return;
-      f.open(next);
-      f.request_first();
-    };
-    f.run(now, open_next);
-    now = uniform_tile(next);
-  }
+  Product<FORM, INT8> f(g, lds);
+  f.run();
 }
 
 template <int FORM, bool INT8>
