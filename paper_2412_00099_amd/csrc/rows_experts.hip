@@ -127,6 +127,7 @@ struct TileList {
 template <int FORM>
 __device__ __forceinline__ TileList deal_tiles(const ExpertRowsParams &p, int n_cols, int m_tiles) {
   const int lane = threadIdx.x & 63, xcd = blockIdx.x & 7;
+  TileList r;
   int64_t cost = 0;
   for (int e = lane; e < p.n_experts; e += 64) {
     const ExpertTiles t = expert_tiles<FORM>(row_count(p, e), n_cols, m_tiles);
@@ -153,7 +154,6 @@ __device__ __forceinline__ TileList deal_tiles(const ExpertRowsParams &p, int n_
     begin = max(begin, __shfl_xor(begin, o));
     end = max(end, __shfl_xor(end, o));
   }
-  TileList r;
   r.step = gridDim.x / 8;
   r.next = uniform(begin < 0 ? tiles : begin) + (blockIdx.x >> 3);
   r.end = uniform(end < 0 ? tiles : end);
@@ -410,44 +410,41 @@ struct Product {
     }
   }
 
-  // requests the next stage of a side, of the next tile if this one has no more
-  __device__ __forceinline__ void request_rows() {
-    if (a_left == 0) {
-      ++a_tile;
-      open_rows();
-    }
-    --a_left;
+  // Requests load i of the next stage of a side; behind the last load the side is at the stage after it, of the next tile if this
+  // one has no more.
+  __device__ __forceinline__ void request_rows(int i) {
     uint8_t *at = lds + a_put + wave * 4096;
     if constexpr (FORM == kWeights) {
       const int n = max(min(64, a_rows_left), 0);
       a = buffer_of(a_base, n > 0 ? n * a_row - a_skip : 0);
+    }
+    to_lds(a, a_off[i & 1], a_at + (i >> 1) * a_more, at + i * 1024);
+    if (i + 1 < A_LOADS) return;
+    if constexpr (FORM == kWeights) {
       a_rows_left -= 64;
       a_base += 64 * a_row;
+    } else {
+      a_at += 128;
     }
-#pragma unroll
-    for (int i = 0; i < A_LOADS; ++i) to_lds(a, a_off[i & 1], a_at + (i >> 1) * a_more, at + i * 1024);
-    if constexpr (FORM != kWeights) a_at += 128;
     a_put = next_row_stage(a_put);
-  }
-  __device__ __forceinline__ void request_weights() {
-    if (b_left == 0) {
-      ++b_tile;
-      open_weights();
+    if (--a_left == 0) {
+      ++a_tile;
+      open_rows();
     }
-    --b_left;
+  }
+  __device__ __forceinline__ void request_weights(int i) {
     uint8_t *at = lds + b_put + wave * (NARROW ? 2048 : 4096);
     if constexpr (FORM == kWeights) {
       const int n = max(min(64, b_rows_left), 0);
       b = buffer_of(b_base, n > 0 ? n * row_bytes - b_skip : 0);
+    }
+    if constexpr (SIDE) to_lds(b, b_off[0] ^ (i * 32), b_at + i * b_more, at + i * 1024);
+    else to_lds(b, b_off[i & 1], b_at + (i >> 1) * b_more, at + i * 1024);
+    if (i + 1 < B_LOADS) return;
+    if constexpr (FORM == kWeights) {
       b_rows_left -= 64;
       b_base += 64 * row_bytes;
-    }
-#pragma unroll
-    for (int i = 0; i < B_LOADS; ++i) {
-      if constexpr (SIDE) to_lds(b, b_off[0] ^ (i * 32), b_at + i * b_more, at + i * 1024);
-      else to_lds(b, b_off[i & 1], b_at + (i >> 1) * b_more, at + i * 1024);
-    }
-    if constexpr (SIDE) {
+    } else if constexpr (SIDE) {
       b_at += 128;
     } else if constexpr (FORM == kColumns) {
       // (behind the last record: outside of the resource)
@@ -455,6 +452,18 @@ struct Product {
       if (--section_left == 0) b_at = (g.first + 1) * row_bytes;
     }
     b_put = next_weight_stage(b_put);
+    if (--b_left == 0) {
+      ++b_tile;
+      open_weights();
+    }
+  }
+  __device__ __forceinline__ void request_rows() {
+#pragma unroll
+    for (int i = 0; i < A_LOADS; ++i) request_rows(i);
+  }
+  __device__ __forceinline__ void request_weights() {
+#pragma unroll
+    for (int i = 0; i < B_LOADS; ++i) request_weights(i);
   }
   static __device__ __forceinline__ uint32_t next_row_stage(uint32_t at) { return kStageBytes - at; }
   static __device__ __forceinline__ uint32_t next_weight_stage(uint32_t at) { return at == kLdsBytes - kStageBytes ? kWeightBase : at + kStageBytes; }
@@ -546,10 +555,17 @@ struct Product {
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int m = 0; m < kMaxBlocks; ++m) {
-          if (m > 0 && m >= blocks) break;
+          if (m == 0 || m < blocks) {
 #pragma unroll
-          for (int j = 0; j < 4; ++j) acc[m][j] = mma(now[j], x[m], acc[m][j]);
-          x[m] = read_x(x_at, rows_stage, second, m);
+            for (int j = 0; j < 4; ++j) acc[m][j] = mma(now[j], x[m], acc[m][j]);
+            x[m] = read_x(x_at, rows_stage, second, m);
+          }
+          // (load by load in between: all at once they would hold up the matrix cores; kWeights, whose tiles are short, is slower
+          // that way)
+          if (!second && FORM != kWeights) {
+            if (m < A_LOADS) request_rows(m);
+            else if (m < A_LOADS + B_LOADS) request_weights(m - A_LOADS);
+          }
           __builtin_amdgcn_sched_barrier(0);
         }
       };
@@ -561,8 +577,10 @@ struct Product {
         else if (stores >= 12) landed_but<B_LOADS + 12>();
         else landed_but<B_LOADS>();
         stores = 0;
-        request_rows();
-        request_weights();
+        if constexpr (FORM == kWeights) {
+          request_rows();
+          request_weights();
+        }
         rows_stage = next_row_stage(rows_stage);
         weights_stage = next_weight_stage(weights_stage);
         step(w1, w0, false);
