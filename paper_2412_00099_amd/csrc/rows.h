@@ -88,24 +88,30 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, v);
 }
 
-// VEC elements of type FMT (VEC 8: 16-byte accesses; 1: one element)
-template <int FMT, int VEC>
+template <bool ONCE, typename T>
+__device__ __forceinline__ T load_one(const T *p) {
+  if constexpr (ONCE) return __builtin_nontemporal_load(p);
+  else return *p;
+}
+// VEC elements of type FMT (VEC 8: 16-byte accesses; 1: one element).  ONCE: read by nobody else in the launch, so it need not
+// push anything out of the caches
+template <int FMT, int VEC, bool ONCE = false>
 __device__ __forceinline__ void load_row(const void *p, int64_t at, float (&v)[VEC]) {
   if constexpr (VEC == 1) {
     if constexpr (FMT == MOE_R_FP32)
-      v[0] = static_cast<const float *>(p)[at];
+      v[0] = load_one<ONCE>(static_cast<const float *>(p) + at);
     else
-      v[0] = __uint_as_float((uint32_t) static_cast<const uint16_t *>(p)[at] << 16);
+      v[0] = __uint_as_float((uint32_t)load_one<ONCE>(static_cast<const uint16_t *>(p) + at) << 16);
   } else if constexpr (FMT == MOE_R_FP32) {
     const rows_u32x4 *q = reinterpret_cast<const rows_u32x4 *>(static_cast<const float *>(p) + at);
-    const rows_u32x4 a = q[0], b = q[1];
+    const rows_u32x4 a = load_one<ONCE>(q), b = load_one<ONCE>(q + 1);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       v[i] = __uint_as_float(a[i]);
       v[4 + i] = __uint_as_float(b[i]);
     }
   } else {
-    const rows_u32x4 a = *reinterpret_cast<const rows_u32x4 *>(static_cast<const uint16_t *>(p) + at);
+    const rows_u32x4 a = load_one<ONCE>(reinterpret_cast<const rows_u32x4 *>(static_cast<const uint16_t *>(p) + at));
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       v[2 * i] = bf16_lo(a[i]);

@@ -5,6 +5,8 @@
 //   same however the sum of squares is split over lanes, and both reductions of a row run together.
 //   backward, n = h' r: dh = dh' + r (dx gain - n mean(dx gain n)), dgain = sum over the rows of dx n
 // Bound by memory: every row is read once into registers and written once.  All sums are in 32 bits.
+#include <algorithm>
+
 #include "rows.h"
 
 namespace moe {
@@ -12,19 +14,6 @@ namespace {
 
 constexpr int kMaxWaves = 16;
 
-// A row belongs to a wavefront or to a whole workgroup; `part` holds one value per wavefront.
-struct RowLanes {
-  int lane, wave, waves;  // waves of the row
-};
-__device__ __forceinline__ float row_sum(float v, const RowLanes &l, float *part) {
-  v = wave_sum(v);
-  if (l.waves == 1) return v;
-  if (l.lane == 0) part[l.wave] = v;
-  __syncthreads();
-  float s = 0.f;
-  for (int w = 0; w < l.waves; ++w) s += part[w];
-  return s;
-}
 __device__ __forceinline__ uint32_t wave_max_bits(uint32_t v) {
 #pragma unroll
   for (int m = 1; m < 64; m <<= 1) v = max(v, (uint32_t)__shfl_xor((int)v, m));
@@ -36,19 +25,14 @@ template <int H, int Y, int X, int VEC, int NV>
 __global__ __launch_bounds__(1024) void norm_rows_kernel(const NormRowsParams p, const int waves) {
   __shared__ float part_ss[kMaxWaves];
   __shared__ uint32_t part_top[kMaxWaves];
-  RowLanes l;
-  l.lane = threadIdx.x & 63;
-  l.waves = waves;
-  int64_t row;
+  // a row belongs to a wavefront or to the whole workgroup
+  const int lane = threadIdx.x & 63, wave = waves == 1 ? 0 : threadIdx.x >> 6;
+  int64_t row = blockIdx.x;
   if (waves == 1) {
-    l.wave = 0;
-    row = (int64_t)blockIdx.x * (blockDim.x >> 6) + (threadIdx.x >> 6);
+    row = row * (blockDim.x >> 6) + (threadIdx.x >> 6);
     if (row >= p.n_rows) return;  // (no barrier in this form)
-  } else {
-    l.wave = threadIdx.x >> 6;
-    row = blockIdx.x;
   }
-  const int t = l.wave * 64 + l.lane, step = waves * 64 * VEC, d = p.hidden;
+  const int t = wave * 64 + lane, step = waves * 64 * VEC, d = p.hidden;
   float h[NV][VEC], y[NV][VEC];
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
@@ -96,9 +80,9 @@ __global__ __launch_bounds__(1024) void norm_rows_kernel(const NormRowsParams p,
   ss = wave_sum(ss);
   if constexpr (X == MOE_R_INT8) top = wave_max_bits(top);
   if (waves > 1) {
-    if (l.lane == 0) {
-      part_ss[l.wave] = ss;
-      part_top[l.wave] = top;
+    if (lane == 0) {
+      part_ss[wave] = ss;
+      part_top[wave] = top;
     }
     __syncthreads();
     ss = 0.f;
@@ -144,15 +128,16 @@ __global__ __launch_bounds__(1024) void norm_rows_kernel(const NormRowsParams p,
 }
 
 constexpr int kBackParts = 512;  // workgroups of the backward launch at most: two per compute unit
+constexpr int kBackWaves = 8;    // of a workgroup; a row has some of them, the others take other rows
 
+// (with the rows of the workgroup one after the other on all its wavefronts a compute unit had 4 of them, too few for the memory:
+// 4096 x 2048, h fp32, x bf16 took 31 us)
 template <int H, int X, int VEC, int NV>
-__global__ __launch_bounds__(1024) void norm_rows_backward_kernel(const NormRowsBackwardParams p, const int waves) {
-  __shared__ float part[2][kMaxWaves];
-  RowLanes l;
-  l.lane = threadIdx.x & 63;
-  l.wave = threadIdx.x >> 6;
-  l.waves = waves;
-  const int t = threadIdx.x, step = waves * 64 * VEC, d = p.hidden;
+__global__ __launch_bounds__(kBackWaves * 64) void norm_rows_backward_kernel(const NormRowsBackwardParams p, const int waves) {
+  __shared__ float part[2][kBackWaves];
+  extern __shared__ float sums[];  // [groups - 1][hidden]
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, group = wave / waves, groups = kBackWaves / waves;
+  const int t = threadIdx.x - group * waves * 64, step = waves * 64 * VEC, d = p.hidden;
   float gain[NV][VEC], dgain[NV][VEC];
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
@@ -165,15 +150,18 @@ __global__ __launch_bounds__(1024) void norm_rows_backward_kernel(const NormRows
     if (p.gain && at < d) load_row<MOE_R_FP32>(p.gain, at, gain[j]);
   }
   int turn = 0;
-  for (int64_t row = blockIdx.x; row < p.n_rows; row += gridDim.x, turn ^= 1) {
-    float n[NV][VEC], g[NV][VEC];
-    const float r = p.rstd[row];
+  for (int64_t row0 = (int64_t)blockIdx.x * groups; row0 < p.n_rows; row0 += (int64_t)gridDim.x * groups, turn ^= 1) {
+    const int64_t row = row0 + group;
+    const bool there = row < p.n_rows;  // (a group without a row goes along for the barrier)
+    float n[NV][VEC], g[NV][VEC], up[NV][VEC];
+    const float r = there ? p.rstd[row] : 0.f;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       const int at = j * step + t * VEC;
-      if (at < d) {
+      if (there && at < d) {
         load_row<H>(p.h, row * d + at, n[j]);
         load_row<X>(p.dx, row * d + at, g[j]);
+        if (p.dh) load_row<H>(p.dh, row * d + at, up[j]);
       } else {
 #pragma unroll
         for (int i = 0; i < VEC; ++i) n[j][i] = g[j][i] = 0.f;
@@ -189,42 +177,67 @@ __global__ __launch_bounds__(1024) void norm_rows_backward_kernel(const NormRows
         g[j][i] *= gain[j][i];
         dot = __builtin_fmaf(g[j][i], n[j][i], dot);
       }
-    // (two sets of words in turn: the next row's first is written only behind this row's barrier)
-    dot = row_sum(dot, l, part[turn]) / (float)d;
+    dot = wave_sum(dot);
+    if (waves > 1) {
+      // (two sets of words in turn: the next row's first is written only behind this row's barrier)
+      if (lane == 0) part[turn][wave] = dot;
+      __syncthreads();
+      dot = 0.f;
+      for (int w = 0; w < waves; ++w) dot += part[turn][group * waves + w];
+    }
+    dot /= (float)d;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       const int at = j * step + t * VEC;
-      if (at >= d) continue;
-      float up[VEC];
+      if (!there || at >= d) continue;
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) up[i] = 0.f;
-      if (p.dh) load_row<H>(p.dh, row * d + at, up);
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) up[i] = __builtin_fmaf(r, g[j][i] - n[j][i] * dot, up[i]);
-      store_row<H>(p.dh_out, row * d + at, up);
+      for (int i = 0; i < VEC; ++i) up[j][i] = __builtin_fmaf(r, g[j][i] - n[j][i] * dot, p.dh ? up[j][i] : 0.f);
+      store_row<H>(p.dh_out, row * d + at, up[j]);
     }
   }
-  if (p.dgain) {
+  if (!p.dgain) return;
+  // the groups' sums, always in the same order
+  if (group > 0) {
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       const int at = j * step + t * VEC;
-      if (at < d) store_row<MOE_R_FP32>(p.partial, (int64_t)blockIdx.x * d + at, dgain[j]);
+      if (at < d)
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) sums[(group - 1) * d + at + i] = dgain[j][i];
     }
+  }
+  __syncthreads();
+  if (group > 0) return;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int at = j * step + t * VEC;
+    if (at >= d) continue;
+    for (int k = 0; k < groups - 1; ++k)
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) dgain[j][i] += sums[k * d + at + i];
+    store_row<MOE_R_FP32>(p.partial, (int64_t)blockIdx.x * d + at, dgain[j]);
   }
 }
 
-// dgain: 64 columns a workgroup, its wavefronts share the rows of `partial`; always in the same order
+// dgain: 32 columns a workgroup, 32 threads a column share the rows of `partial`; always in the same order
 __global__ __launch_bounds__(1024) void sum_parts_kernel(const float *partial, int parts, int d, float *out) {
-  __shared__ float s[16][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
-  float v = 0.f;
-  if (c < d)
-    for (int i = wave; i < parts; i += 16) v += partial[(int64_t)i * d + c];
-  s[wave][lane] = v;
+  __shared__ float s[32][33];
+  const int col = threadIdx.x & 31, of = threadIdx.x >> 5, c = blockIdx.x * 32 + col;
+  float v[kBackParts / 32];
+#pragma unroll
+  for (int i = 0; i < kBackParts / 32; ++i) {
+    const int k = of + i * 32;
+    v[i] = c < d && k < parts ? partial[(int64_t)k * d + c] : 0.f;
+  }
+#pragma unroll
+  for (int i = 1; i < kBackParts / 32; ++i) v[0] += v[i];
+  s[of][col] = v[0];
   __syncthreads();
-  if (wave == 0 && c < d) {
-    for (int w = 1; w < 16; ++w) v += s[w][lane];
-    out[c] = v;
+  if (of == 0 && c < d) {
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) sum += s[i][col];
+    out[c] = sum;
   }
 }
 
@@ -280,28 +293,46 @@ hipError_t launch_norm_rows(const NormRowsParams &p, int n_cus, hipStream_t s) {
   return hipGetLastError();
 }
 
-int norm_rows_backward_parts(int n_rows, int hidden) { return n_rows < kBackParts ? n_rows : kBackParts; }
+namespace {
+struct BackShape {
+  int vec, waves, nv, groups, parts;
+};
+// wavefronts of a row, so that a lane has at most 16 of its columns
+BackShape back_shape(int n_rows, int hidden, bool wide) {
+  BackShape b;
+  b.vec = wide ? 8 : 1;
+  const int most = wide ? 2 : 16;
+  b.waves = 1;
+  while (b.waves * 64 * b.vec * most < hidden) b.waves *= 2;
+  b.nv = (hidden + b.waves * 64 * b.vec - 1) / (b.waves * 64 * b.vec);
+  b.groups = kBackWaves / b.waves;
+  b.parts = std::min((n_rows + b.groups - 1) / b.groups, kBackParts);
+  return b;
+}
+}  // namespace
+
+int norm_rows_backward_parts(int n_rows, int hidden) { return std::min(n_rows, kBackParts); }
 
 hipError_t launch_norm_rows_backward(const NormRowsBackwardParams &p, hipStream_t s) {
   const int d = p.hidden;
   const bool wide = d % 8 == 0 && aligned16(p.h) && aligned16(p.dx) && (!p.dh || aligned16(p.dh)) && aligned16(p.dh_out) &&
                     (!p.gain || aligned16(p.gain)) && (!p.dgain || aligned16(p.partial));
-  const int vec = wide ? 8 : 1, most = wide ? 2 : 8;
-  int waves = 1;
-  while ((int64_t)waves * 64 * vec * most < d) waves *= 2;
-  const int nv = (d + waves * 64 * vec - 1) / (waves * 64 * vec), parts = norm_rows_backward_parts(p.n_rows, d);
+  const BackShape b = back_shape(p.n_rows, d, wide);
+  const int nv = b.nv, parts = b.parts;
+  const size_t lds = p.dgain ? (size_t)(b.groups - 1) * d * sizeof(float) : 0;
   const auto go = [&](auto H, auto X) {
     const auto with = [&](auto VEC, auto NV) {
       if (parts == 0) return;  // (no rows: dgain is zero)
       hipLaunchKernelGGL((norm_rows_backward_kernel<decltype(H)::value, decltype(X)::value, decltype(VEC)::value, decltype(NV)::value>),
-                         dim3(parts), dim3(waves * 64), 0, s, p, waves);
+                         dim3(parts), dim3(kBackWaves * 64), lds, s, p, b.waves);
     };
     if (wide) {
       if (nv == 1) with(Const<8>{}, Const<1>{});
       else with(Const<8>{}, Const<2>{});
     } else {
       if (nv <= 2) with(Const<1>{}, Const<2>{});
-      else with(Const<1>{}, Const<8>{});
+      else if (nv <= 8) with(Const<1>{}, Const<8>{});
+      else with(Const<1>{}, Const<16>{});
     }
   };
   const auto x = [&](auto H) {
@@ -312,7 +343,7 @@ hipError_t launch_norm_rows_backward(const NormRowsBackwardParams &p, hipStream_
   else x(Const<MOE_R_BF16>{});
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !p.dgain) return e;
-  hipLaunchKernelGGL(sum_parts_kernel, dim3((d + 63) / 64), dim3(1024), 0, s, p.partial, parts, d, p.dgain);
+  hipLaunchKernelGGL(sum_parts_kernel, dim3((d + 31) / 32), dim3(1024), 0, s, p.partial, parts, d, p.dgain);
   return hipGetLastError();
 }
 

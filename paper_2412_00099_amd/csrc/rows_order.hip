@@ -10,8 +10,8 @@ namespace {
 
 constexpr int kSortWaves = 16, kSortThreads = kSortWaves * 64;
 constexpr int kSortBlocks = 256;      // workgroups of the two-launch form at most
-constexpr int kSortSingle = 16384;    // places that one workgroup sorts by itself
-constexpr int kSortChunk = 4096;      // places a workgroup takes at least in the two-launch form
+constexpr int kSortSingle = 4096;     // places that one workgroup sorts by itself (16384 take 25 us, in two launches 12)
+constexpr int kSortChunk = 1024;      // places a workgroup takes at least in the two-launch form: one for each thread
 
 // Lanes of the wavefront that hold the same key as this one.  BITS: bits of a key.
 template <int BITS>
@@ -90,24 +90,36 @@ __device__ __forceinline__ int block_scan(int v, int *s, int &total) {
 template <int BITS, bool BLOCKS>
 __global__ __launch_bounds__(kSortThreads) void sort_kernel(const int32_t *ids, int64_t n, int n_experts, int64_t chunk, const int32_t *hist,
                                                             int32_t *offsets, int32_t *row_of, int32_t *entry_of) {
-  extern __shared__ int counts[];  // [kSortWaves][n_experts], then 16 words
-  int *scratch = counts + kSortWaves * n_experts;
+  extern __shared__ int counts[];  // [kSortWaves][n_experts], two words per expert, 16 words
+  int *sum_all = counts + kSortWaves * n_experts, *sum_earlier = sum_all + n_experts, *scratch = sum_earlier + n_experts;
   const int e = threadIdx.x;
   const int64_t begin = BLOCKS ? blockIdx.x * chunk : 0, end = BLOCKS ? min(n, begin + chunk) : n;
   const int64_t per_wave = ((end - begin + kSortWaves - 1) / kSortWaves + 63) / 64 * 64;
-  for (int i = threadIdx.x; i < kSortWaves * n_experts; i += kSortThreads) counts[i] = 0;
+  for (int i = threadIdx.x; i < (kSortWaves + 2) * n_experts; i += kSortThreads) counts[i] = 0;
   __syncthreads();
+  if constexpr (BLOCKS) {
+    // what all workgroups and those before this one have counted: whole numbers, the order of the additions is of no matter
+    const int parts = kSortThreads / n_experts, k = threadIdx.x / n_experts, x = threadIdx.x - k * n_experts;
+    if (k < parts) {
+      int all = 0, earlier = 0;
+#pragma unroll 8
+      for (int b = k; b < (int)gridDim.x; b += parts) {
+        const int c = hist[b * n_experts + x];
+        all += c;
+        earlier += b < (int)blockIdx.x ? c : 0;
+      }
+      atomicAdd(&sum_all[x], all);
+      atomicAdd(&sum_earlier[x], earlier);
+    }
+  }
   count_places<BITS>(ids, begin, end, per_wave, n_experts, counts, n_experts);
   __syncthreads();
   // this expert's places in all of the input and in the workgroups before this one
   int all = 0, earlier = 0;
   if (e < n_experts) {
     if constexpr (BLOCKS) {
-      for (int b = 0; b < (int)gridDim.x; ++b) {
-        const int c = hist[b * n_experts + e];
-        all += c;
-        if (b < (int)blockIdx.x) earlier += c;
-      }
+      all = sum_all[e];
+      earlier = sum_earlier[e];
     } else {
       for (int w = 0; w < kSortWaves; ++w) all += counts[w * n_experts + e];
     }
@@ -151,11 +163,20 @@ int64_t sort_chunk(int64_t n) {
   return even > kSortChunk ? (even + 1023) / 1024 * 1024 : kSortChunk;
 }
 
-// the row of place (t, k), -1: none (whatever lies outside the order counts as none)
-__device__ __forceinline__ int row_at(const OrderParams &o, int64_t t, int k) {
-  const int r = __builtin_amdgcn_readfirstlane(o.row_of[t * o.top_k + k]);
-  return (uint32_t)r < (uint32_t)o.n_tokens * (uint32_t)o.top_k ? r : -1;
-}
+// The rows (and weights) of token t: lane k loads place k, all of them in one request.  -1: none (whatever lies outside the order
+// counts as none).
+struct Places {
+  int row_v;
+  float weight_v;
+  __device__ __forceinline__ Places(const OrderParams &o, int64_t t, const float *weight, int lane) {
+    const int64_t at = t * o.top_k + min(lane, o.top_k - 1);
+    row_v = o.row_of[at];
+    if ((uint32_t)row_v >= (uint32_t)o.n_tokens * (uint32_t)o.top_k || lane >= o.top_k) row_v = -1;
+    weight_v = weight ? weight[at] : 1.f;
+  }
+  __device__ __forceinline__ int row(int k) const { return __builtin_amdgcn_readlane(row_v, k); }
+  __device__ __forceinline__ float weight(int k) const { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(weight_v), k)); }
+};
 // how many rows belong to somebody
 __device__ __forceinline__ int64_t rows_used(const OrderParams &o) { return max(0, o.offsets[o.n_experts]); }
 
@@ -168,9 +189,10 @@ __global__ __launch_bounds__(256) void gather_kernel(const OrderParams o, const 
   const int lane = threadIdx.x & 63;
   const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (t >= o.n_tokens) return;
+  const Places places(o, t, nullptr, lane);
   int row[MOE_MAX_TOPK];
 #pragma unroll
-  for (int k = 0; k < MOE_MAX_TOPK; ++k) row[k] = k < o.top_k ? row_at(o, t, k) : -1;
+  for (int k = 0; k < MOE_MAX_TOPK; ++k) row[k] = places.row(k);
   const V *in = reinterpret_cast<const V *>(x + t * x_stride);
   V *out = reinterpret_cast<V *>(xs);
   constexpr int U = 4;  // units in flight per lane
@@ -188,8 +210,7 @@ __global__ __launch_bounds__(256) void gather_kernel(const OrderParams o, const 
     }
   }
   if (scale && lane < o.top_k) {
-    const int r = o.row_of[t * o.top_k + lane];
-    if ((uint32_t)r < (uint32_t)o.n_tokens * (uint32_t)o.top_k) xs_scale[r] = scale[t];
+    if (places.row_v >= 0) xs_scale[places.row_v] = scale[t];
   }
   // rows of nobody: as many as there are places without a row, one token's wavefront after the other
   const int64_t n = (int64_t)o.n_tokens * o.top_k;
@@ -201,42 +222,58 @@ __global__ __launch_bounds__(256) void gather_kernel(const OrderParams o, const 
 
 // ---- results back ----
 // y = base + sum over k of weight * row, in the order of k.  KC: top_k rounded up to a power of two.  Places without a row read
-// one that is there (or nothing at all if there is none) and are left out by a selection, not by a weight of 0.
-template <int YS, int Y, int VEC, int KC>
+// one that is there (or nothing at all if there is none) and are left out by a selection, not by a weight of 0.  A wavefront takes
+// a token, CH units of a row at a time, so that it reads a row's bytes one after the other (8191 x 8 rows of 2048 bf16 onto fp32:
+// 117 us by single units, 110 so, 92 with loads that leave the caches alone: 4.4 TB/s).
+template <int YS, int Y, int VEC, int KC, int CH>
 __global__ __launch_bounds__(256) void combine_kernel(const OrderParams o, const void *ys, const float *weight, const void *base, void *y) {
   const int lane = threadIdx.x & 63;
   const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (t >= o.n_tokens) return;
   const int d = o.hidden;
+  const Places places(o, t, weight, lane);
   int row[KC];
   float w[KC];
   int some = -1;
 #pragma unroll
   for (int k = 0; k < KC; ++k) {
-    row[k] = k < o.top_k ? row_at(o, t, k) : -1;
-    w[k] = weight && k < o.top_k ? weight[t * o.top_k + k] : 1.f;
+    row[k] = places.row(k);
+    w[k] = places.weight(k);
     if (row[k] >= 0) some = row[k];
   }
-  for (int c = lane * VEC; c < d; c += 64 * VEC) {
-    float acc[VEC];
+  for (int c = lane * VEC; c < d; c += 64 * VEC * CH) {
+    int at[CH];
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) acc[i] = 0.f;
+    for (int u = 0; u < CH; ++u) at[u] = min(c + u * 64 * VEC, d - VEC);
+    float acc[CH][VEC], b[CH][VEC];
+    if (base)
+#pragma unroll
+      for (int u = 0; u < CH; ++u) load_row<Y>(base, t * d + at[u], b[u]);
+#pragma unroll
+    for (int u = 0; u < CH; ++u)
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) acc[u][i] = 0.f;
     if (some >= 0) {
-      float v[KC][VEC];
 #pragma unroll
-      for (int k = 0; k < KC; ++k) load_row<YS>(ys, (int64_t)(row[k] >= 0 ? row[k] : some) * d + c, v[k]);
+      for (int k = 0; k < KC; ++k) {
+        const int64_t from = (int64_t)(row[k] >= 0 ? row[k] : some) * d;
 #pragma unroll
-      for (int k = 0; k < KC; ++k)
+        for (int u = 0; u < CH; ++u) {
+          float v[VEC];
+          load_row<YS, VEC, true>(ys, from + at[u], v);
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) acc[i] = row[k] >= 0 ? __builtin_fmaf(w[k], v[k][i], acc[i]) : acc[i];
+          for (int i = 0; i < VEC; ++i) acc[u][i] = row[k] >= 0 ? __builtin_fmaf(w[k], v[i], acc[u][i]) : acc[u][i];
+        }
+      }
     }
-    if (base) {
-      float b[VEC];
-      load_row<Y>(base, t * d + c, b);
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) acc[i] += b[i];
+    for (int u = 0; u < CH; ++u) {
+      if (c + u * 64 * VEC >= d) continue;
+      if (base)
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) acc[u][i] += b[u][i];
+      store_row<Y>(y, t * d + at[u], acc[u]);
     }
-    store_row<Y>(y, t * d + c, acc);
   }
 }
 
@@ -248,12 +285,13 @@ __global__ __launch_bounds__(256) void combine_backward_kernel(const OrderParams
   const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (t >= o.n_tokens) return;
   const int d = o.hidden;
+  const Places places(o, t, weight, lane);
   int row[MOE_MAX_TOPK];
   float w[MOE_MAX_TOPK], dot[MOE_MAX_TOPK];
 #pragma unroll
   for (int k = 0; k < MOE_MAX_TOPK; ++k) {
-    row[k] = k < o.top_k ? row_at(o, t, k) : -1;
-    w[k] = weight && k < o.top_k ? weight[t * o.top_k + k] : 1.f;
+    row[k] = places.row(k);
+    w[k] = places.weight(k);
     dot[k] = 0.f;
   }
   for (int c = lane * VEC; c < d; c += 64 * VEC) {
@@ -265,7 +303,7 @@ __global__ __launch_bounds__(256) void combine_backward_kernel(const OrderParams
       const int64_t at = (int64_t)row[k] * d + c;
       float v[VEC];
       if (dweight) {
-        load_row<YS>(ys, at, v);
+        load_row<YS, VEC, true>(ys, at, v);
 #pragma unroll
         for (int i = 0; i < VEC; ++i) dot[k] = __builtin_fmaf(g[i], v[i], dot[k]);
       }
@@ -308,7 +346,7 @@ size_t sort_tokens_bytes(int64_t n, int n_experts) {
 hipError_t launch_sort_tokens(const int32_t *ids, int64_t n, int n_experts, int32_t *offsets, int32_t *row_of, int32_t *entry_of,
                               void *workspace, hipStream_t s) {
   int32_t *hist = static_cast<int32_t *>(workspace);
-  const size_t lds = ((size_t)kSortWaves * n_experts + 16) * sizeof(int);
+  const size_t lds = ((size_t)(kSortWaves + 2) * n_experts + 16) * sizeof(int);
   const auto go = [&](auto BITS) {
     constexpr int B = decltype(BITS)::value;
     if (n <= kSortSingle) {
@@ -350,8 +388,12 @@ hipError_t launch_combine_rows(const OrderParams &o, const void *ys, int ys_fmt,
   const dim3 grid((uint32_t)((o.n_tokens + 3) / 4)), block(256);
   const auto go = [&](auto YS, auto Y) {
     const auto with = [&](auto VEC, auto KC) {
-      hipLaunchKernelGGL((combine_kernel<decltype(YS)::value, decltype(Y)::value, decltype(VEC)::value, decltype(KC)::value>), grid, block, 0, s, o,
-                         ys, weight, base, y);
+      const auto go_on = [&](auto CH) {
+        hipLaunchKernelGGL((combine_kernel<decltype(YS)::value, decltype(Y)::value, decltype(VEC)::value, decltype(KC)::value, decltype(CH)::value>),
+                           grid, block, 0, s, o, ys, weight, base, y);
+      };
+      if (o.hidden <= 64 * decltype(VEC)::value * 2) go_on(Const<1>{});
+      else go_on(Const<4>{});
     };
     const auto k = [&](auto VEC) {
       if (o.top_k == 1) with(VEC, Const<1>{});
