@@ -36,12 +36,8 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __amdgpu_buffer_rsrc_t Buffer;
 #define LDS_PTR(T, p) ((__attribute__((address_space(3))) T *)(p))
 
-constexpr int kCols = 256;        // columns of a tile (128 records where each has two products)
-constexpr int kMaxBlocks = 8;     // 32-row blocks of a tile at most
 constexpr int kWavesWg = 8, kBlock = kWavesWg * 64;
-constexpr int kStageBytes = 32768;                 // of one side
-constexpr int kRowStages = 2, kWeightStages = 3;   // 160 KB, all of a compute unit's LDS
-constexpr uint32_t kWeightBase = kRowStages * kStageBytes, kLdsBytes = (kRowStages + kWeightStages) * kStageBytes;
+constexpr int kRowStages = 2, kWeightStages = 3;
 
 enum { kUp = 0, kDgu = 1, kColumns = 2, kWeights = 3 };
 
@@ -103,16 +99,16 @@ __device__ __forceinline__ T sum_upto(T v, int lane) {  // of lanes 0 .. lane
   return v;
 }
 
-// What an expert's tiles are.  Its rows are cut into the fewest parts of at most 256, all of nearly the same size.  cost: of a
+// What an expert's tiles are.  Its rows are cut into the fewest parts of at most MOST, all of nearly the same size.  cost: of a
 // tile, in rows; that the weights have to come in costs about as much as 128 rows do (kWeights: 256 columns times the rows, and the
 // stores).
 struct ExpertTiles {
   int parts, each, n, cost;
 };
-template <int FORM>
+template <int FORM, int MOST>
 __device__ __forceinline__ ExpertTiles expert_tiles(int count, int n_cols, int m_tiles) {
   ExpertTiles t;
-  t.parts = (count + 255) / 256;
+  t.parts = (count + MOST - 1) / MOST;
   t.each = t.parts > 0 ? ((count + t.parts - 1) / t.parts + 15) / 16 * 16 : 0;
   t.n = FORM == kWeights ? m_tiles * n_cols : t.parts * n_cols;
   t.cost = FORM == kWeights ? count + 384 : t.each + 128;
@@ -124,13 +120,13 @@ __device__ __forceinline__ ExpertTiles expert_tiles(int count, int n_cols, int m
 struct TileList {
   int next, end, step;  // the workgroup's tiles: next, next + step, .. below end
 };
-template <int FORM>
+template <int FORM, int MOST>
 __device__ __forceinline__ TileList deal_tiles(const ExpertRowsParams &p, int n_cols, int m_tiles) {
   const int lane = threadIdx.x & 63, xcd = blockIdx.x & 7;
   TileList r;
   int64_t cost = 0;
   for (int e = lane; e < p.n_experts; e += 64) {
-    const ExpertTiles t = expert_tiles<FORM>(row_count(p, e), n_cols, m_tiles);
+    const ExpertTiles t = expert_tiles<FORM, MOST>(row_count(p, e), n_cols, m_tiles);
     cost += (int64_t)t.n * t.cost;
   }
   cost = wave_total(cost);
@@ -139,7 +135,7 @@ __device__ __forceinline__ TileList deal_tiles(const ExpertRowsParams &p, int n_
   int64_t before = 0;
   for (int e0 = 0; e0 < p.n_experts; e0 += 64) {
     const int e = e0 + lane;
-    const ExpertTiles t = e < p.n_experts ? expert_tiles<FORM>(row_count(p, e), n_cols, m_tiles) : ExpertTiles{0, 0, 0, 1};
+    const ExpertTiles t = e < p.n_experts ? expert_tiles<FORM, MOST>(row_count(p, e), n_cols, m_tiles) : ExpertTiles{0, 0, 0, 1};
     const int64_t own = (int64_t)t.n * t.cost, past = before + sum_upto(own, lane), first = past - own;
     const int first_tile = tiles + sum_upto(t.n, lane) - t.n;
     const int b = first <= from && from < past ? first_tile + (int)((from - first + t.cost - 1) / t.cost) : -1;
@@ -160,7 +156,7 @@ __device__ __forceinline__ TileList deal_tiles(const ExpertRowsParams &p, int n_
   return r;
 }
 // Lane i: tile list.next + i * list.step
-template <int FORM>
+template <int FORM, int MOST>
 __device__ __forceinline__ Tile lane_tile(const ExpertRowsParams &p, const TileList &list, int n_cols, int m_tiles) {
   const int lane = threadIdx.x & 63;
   const int64_t at = list.next + (int64_t)lane * list.step;
@@ -169,7 +165,7 @@ __device__ __forceinline__ Tile lane_tile(const ExpertRowsParams &p, const TileL
   int before = 0;
   for (int e0 = 0; e0 < p.n_experts; e0 += 64) {
     const int e = e0 + lane, row0 = e < p.n_experts ? first_row(p, e) : 0, count = e < p.n_experts ? row_count(p, e) : 0;
-    const ExpertTiles t = e < p.n_experts ? expert_tiles<FORM>(count, n_cols, m_tiles) : ExpertTiles{0, 0, 0, 0};
+    const ExpertTiles t = e < p.n_experts ? expert_tiles<FORM, MOST>(count, n_cols, m_tiles) : ExpertTiles{0, 0, 0, 0};
     const int past = before + sum_upto(t.n, lane);
     // the first expert whose tiles end behind `want`
     int l = 0;
@@ -208,9 +204,10 @@ __device__ __forceinline__ int swap_fours(int r) { return ((r >> 1) & 1) | ((r >
 __device__ __forceinline__ int swap16(int k) { return (k & 3) | ((k >> 1) & 4); }
 // Results: register i of a lane is column (lane / 16) * 4 + i of a fragment.  With PAIRED fragments j and j + 1 have 4 columns
 // of each 8 in turn, so that a lane has 8 columns in a row and stores 16 bytes.
+template <int ROW_BYTES>
 __device__ __forceinline__ i32x4 transposed(const uint8_t *at) {  // 8 summed values of the lane's column: rows of `at` and + 4
   const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, at));
-  const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, at + 4 * 512));
+  const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, at + 4 * ROW_BYTES));
   return __builtin_bit_cast(i32x4, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 // 8 codes q + 128 as bf16 (whole numbers up to 128: the lower halves of the floats are zero)
@@ -229,19 +226,28 @@ __device__ __forceinline__ i32x4 widen(i32x2 q) {
 // Results go through buffer resources too: rows that the tile does not have lie behind their end and are dropped, so that no
 // lane branches (a branch that differs between lanes would take the loops around it out of scalar control).
 constexpr uint32_t kNowhere = 0xf8000000u;
-__device__ __forceinline__ void store8(Buffer p, uint32_t off, const float (&v)[8]) {
-  rows_u32x4 w;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) w[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
-  __builtin_amdgcn_raw_buffer_store_b128(w, p, off, 0, 0);
-}
-__device__ __forceinline__ void store8_f32(Buffer p, uint32_t off, const float (&v)[8]) {
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
+template <int N>
+__device__ __forceinline__ void store_bf16(Buffer p, uint32_t off, const float (&v)[N]) {
+  if constexpr (N == 8) {
     rows_u32x4 w;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(v[4 * h + i]);
-    __builtin_amdgcn_raw_buffer_store_b128(w, p, off + 16 * h, 0, 0);
+    for (int i = 0; i < 4; ++i) w[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
+    __builtin_amdgcn_raw_buffer_store_b128(w, p, off, 0, 0);
+  } else {
+    rows_u32x2 w;
+    w[0] = pack_bf16(v[0], v[1]);
+    w[1] = pack_bf16(v[2], v[3]);
+    __builtin_amdgcn_raw_buffer_store_b64(w, p, off, 0, 0);
+  }
+}
+template <int N>
+__device__ __forceinline__ void store_f32(Buffer p, uint32_t off, const float (&v)[N]) {
+#pragma unroll
+  for (int h = 0; h < N; h += 4) {
+    rows_u32x4 w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(v[h + i]);
+    __builtin_amdgcn_raw_buffer_store_b128(w, p, off + 4 * h, 0, 0);
   }
 }
 __device__ __forceinline__ void load8_f32(Buffer p, uint32_t off, float (&v)[8]) {
@@ -252,22 +258,23 @@ __device__ __forceinline__ void load8_f32(Buffer p, uint32_t off, float (&v)[8])
     for (int i = 0; i < 4; ++i) v[4 * h + i] = __uint_as_float(w[i]);
   }
 }
-__device__ __forceinline__ void store4(Buffer p, uint32_t off, const float (&v)[4]) {
-  rows_u32x2 w;
-  w[0] = pack_bf16(v[0], v[1]);
-  w[1] = pack_bf16(v[2], v[3]);
-  __builtin_amdgcn_raw_buffer_store_b64(w, p, off, 0, 0);
-}
 __device__ __forceinline__ float half_lo(uint32_t v) { return (float)__builtin_bit_cast(_Float16, (uint16_t)v); }
 __device__ __forceinline__ float half_hi(uint32_t v) { return (float)__builtin_bit_cast(_Float16, (uint16_t)(v >> 16)); }
 __device__ __forceinline__ float sigmoid(float g) { return __builtin_amdgcn_rcpf(1.f + __expf(-g)); }
 
 // ---- one tile ---------------------------------------------------------------------------------------------
-template <int FORM, bool INT8>
+// NJ: fragments of 16 weight rows or columns a wavefront has.  MB: 32-row blocks of a tile at most.
+template <int FORM, bool INT8, int NJ, int MB>
 struct Product {
   static constexpr int EL = INT8 ? 1 : 2;
+  static constexpr int ROWS = MB * 32, COLS = NJ * 64, OF_WAVE = NJ * 16;  // of a tile; of a wavefront
+  static constexpr int RECS = COLS / 2;                                   // kUp: records of a tile, each has two products
+  static constexpr uint32_t ROW_STAGE = ROWS * 128, WEIGHT_STAGE = COLS * 128, WEIGHT_BASE = kRowStages * ROW_STAGE;
+  static constexpr uint32_t LDS_BYTES = WEIGHT_BASE + kWeightStages * WEIGHT_STAGE;
   static constexpr bool NARROW = FORM == kColumns && INT8;       // the weights' stage is of bytes: half as long
-  static constexpr int A_LOADS = 4, B_LOADS = NARROW ? 2 : 4;  // of a wavefront for a stage
+  static constexpr int A_LOADS = MB / 2, B_LOADS = NARROW ? NJ / 2 : NJ;  // of a wavefront for a stage
+  static constexpr bool FOURS = FORM == kDgu || (FORM == kUp && NJ == 4);  // side by side: fragments of 4 rows of each 8
+  static constexpr int T_BYTES = NARROW ? COLS : COLS * 2, T_LANES = T_BYTES / 16, T_ROWS = 64 / T_LANES;  // transposed: a row, its lanes in a load, rows of a load
   using Acc = std::conditional_t<INT8 && FORM == kUp, i32x4, f32x4>;
 
   const ProductArgs g;  // (a copy: through a reference the arguments would not be known to be the same in every lane)
@@ -298,15 +305,15 @@ struct Product {
     wn = wave & 3;
     pitch = expert_rows_pitch(g.p.inter);
     row_bytes = (uint32_t)g.p.hidden * EL;
-    n_cols = FORM == kUp ? (pitch + 127) / 128 : FORM == kDgu ? (pitch + kCols - 1) / kCols : g.p.hidden / kCols;
+    n_cols = FORM == kUp ? (pitch + RECS - 1) / RECS : FORM == kDgu ? (pitch + COLS - 1) / COLS : g.p.hidden / COLS;
     m_both = (2 * pitch + 255) / 256;
     m_tiles = m_both + (pitch + 255) / 256;
-    deal = deal_tiles<FORM>(g.p, n_cols, m_tiles);
+    deal = deal_tiles<FORM, ROWS>(g.p, n_cols, m_tiles);
     listed = 0;
-    list = lane_tile<FORM>(g.p, deal, n_cols, m_tiles);
+    list = lane_tile<FORM, ROWS>(g.p, deal, n_cols, m_tiles);
     list_more();
     a_put = 0;
-    b_put = kWeightBase;
+    b_put = WEIGHT_BASE;
     a_tile = b_tile = 0;
     open_rows();
     open_weights();
@@ -314,7 +321,7 @@ struct Product {
   __device__ __forceinline__ void list_more() {
     deal.next += 64 * deal.step;
     list_after = Tile{-1, 0, 0, 0};
-    if (deal.next < deal.end) list_after = lane_tile<FORM>(g.p, deal, n_cols, m_tiles);
+    if (deal.next < deal.end) list_after = lane_tile<FORM, ROWS>(g.p, deal, n_cols, m_tiles);
   }
   // tile i of the workgroup, the same in every lane
   __device__ __forceinline__ Tile tile(int i) const {
@@ -359,7 +366,7 @@ struct Product {
       a_more = 16 * a_bytes;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const int r = (wave * 4 + i) * 8 + lane / 8;
+        const int r = (wave * A_LOADS + i) * 8 + lane / 8;
         a_off[i] = (uint32_t)r * a_bytes + ((lane & 7) ^ swap_rows(r)) * 16;
       }
     }
@@ -372,7 +379,7 @@ struct Product {
       const bool down = gradient_row(t) >= 2 * pitch;
       b_at = 0;
       b_rows_left = any ? t.rows : 0;
-      b_skip = t.col % n_cols * kCols * 2;
+      b_skip = t.col % n_cols * COLS * 2;
       b_base = (down ? g.b2 : g.b) + (int64_t)t.row0 * row_bytes + b_skip;
       b_more = 4 * row_bytes;
 #pragma unroll
@@ -385,12 +392,12 @@ struct Product {
       b = buffer_of(g.p.blobs + (int64_t)max(t.expert, 0) * g.p.blob_stride, any ? (uint32_t)g.p.inter * rec_bytes : 0);
       section_left = pitch / 64;
       if constexpr (SIDE) {
-        // kUp: of each 64 rows of the image the first 32 are gate rows, the others the same records' up rows.  (A record that is not
-        // there lies behind the end of the resource.)  Load i has the records 8 * i further on, and its chunks are exchanged with
-        // 2 * i: see swap_fours.
-        const int r = wave * 32 + lane / 8;
-        const int rec = FORM == kUp ? t.col * 128 + (r >> 6) * 32 + (r & 31) : t.col * kCols + r, which = FORM == kUp ? (r >> 5) & 1 : 2;
-        b_off[0] = (uint32_t)(rec * 3 + which) * row_bytes + ((lane & 7) ^ ((lane >> 4) & 1)) * 16;
+        // kUp: of a wavefront's rows of the image the first half are gate rows, the others the same records' up rows.  (A record
+        // that is not there lies behind the end of the resource.)  Load i has the records 8 * i further on, its chunks are
+        // exchanged with another number: see swap_rows, swap_fours.
+        const int r = wave * (B_LOADS * 8) + lane / 8, half = OF_WAVE / 2;
+        const int rec = FORM == kUp ? t.col * RECS + r / OF_WAVE * half + r % half : t.col * COLS + r, which = FORM == kUp ? r / half & 1 : 2;
+        b_off[0] = (uint32_t)(rec * 3 + which) * row_bytes + ((lane & 7) ^ (FOURS ? swap_fours(r) : swap_rows(r))) * 16;
         b_more = 8 * rec_bytes;
         b_at = 0;
       } else {
@@ -398,13 +405,9 @@ struct Product {
         b_more = 4 * rec_bytes;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          if constexpr (NARROW) {
-            const int k = (wave * 2 + i) * 4 + lane / 16;
-            b_off[i] = (uint32_t)k * rec_bytes + t.col * kCols + ((lane & 15) ^ (k & 15)) * 16;
-          } else {
-            const int k = (wave * 4 + i) * 2 + lane / 32;
-            b_off[i] = (uint32_t)k * rec_bytes + t.col * kCols * 2 + ((lane & 31) ^ (swap16(k) << 1)) * 16;
-          }
+          const int k = (wave * B_LOADS + i) * T_ROWS + lane / T_LANES, pos = lane % T_LANES;
+          const int chunk = NARROW ? pos ^ (k & (T_LANES - 1)) : pos ^ (swap16(k) << 1);
+          b_off[i] = (uint32_t)k * rec_bytes + t.col * COLS * EL + chunk * 16;
         }
       }
     }
@@ -413,7 +416,7 @@ struct Product {
   // Requests load i of the next stage of a side; behind the last load the side is at the stage after it, of the next tile if this
   // one has no more.
   __device__ __forceinline__ void request_rows(int i) {
-    uint8_t *at = lds + a_put + wave * 4096;
+    uint8_t *at = lds + a_put + wave * (A_LOADS * 1024);
     if constexpr (FORM == kWeights) {
       const int n = max(min(64, a_rows_left), 0);
       a = buffer_of(a_base, n > 0 ? n * a_row - a_skip : 0);
@@ -433,12 +436,12 @@ struct Product {
     }
   }
   __device__ __forceinline__ void request_weights(int i) {
-    uint8_t *at = lds + b_put + wave * (NARROW ? 2048 : 4096);
+    uint8_t *at = lds + b_put + wave * (B_LOADS * 1024);
     if constexpr (FORM == kWeights) {
       const int n = max(min(64, b_rows_left), 0);
       b = buffer_of(b_base, n > 0 ? n * row_bytes - b_skip : 0);
     }
-    if constexpr (SIDE) to_lds(b, b_off[0] ^ (i * 32), b_at + i * b_more, at + i * 1024);
+    if constexpr (SIDE) to_lds(b, b_off[0] ^ (i * (FOURS ? 32 : 64)), b_at + i * b_more, at + i * 1024);
     else to_lds(b, b_off[i & 1], b_at + (i >> 1) * b_more, at + i * 1024);
     if (i + 1 < B_LOADS) return;
     if constexpr (FORM == kWeights) {
@@ -465,28 +468,31 @@ struct Product {
 #pragma unroll
     for (int i = 0; i < B_LOADS; ++i) request_weights(i);
   }
-  static __device__ __forceinline__ uint32_t next_row_stage(uint32_t at) { return kStageBytes - at; }
-  static __device__ __forceinline__ uint32_t next_weight_stage(uint32_t at) { return at == kLdsBytes - kStageBytes ? kWeightBase : at + kStageBytes; }
+  static __device__ __forceinline__ uint32_t next_row_stage(uint32_t at) { return ROW_STAGE - at; }
+  static __device__ __forceinline__ uint32_t next_weight_stage(uint32_t at) { return at == LDS_BYTES - WEIGHT_STAGE ? WEIGHT_BASE : at + WEIGHT_STAGE; }
 
   // Where the lane's fragments lie in a stage: of the weights for each j, of the rows for block 0; of the stage's first step.
-  __device__ __forceinline__ void fragment_offsets(uint32_t (&w_at)[4], uint32_t &x_at) const {
+  __device__ __forceinline__ void fragment_offsets(uint32_t (&w_at)[NJ], uint32_t &x_at) const {
     const int l = lane & 15, q = lane >> 4;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < NJ; ++j) {
       if constexpr (FORM == kWeights) {
         const int k = q * 8 + (l >> 2), chunk = wn * 8 + (j >> 1) * 4 + (l & 3);
         w_at[j] = k * 512 + ((chunk ^ ((k & 3) << 2)) * 16) + (j & 1) * 8;
       } else if constexpr (NARROW) {
         const int k = q * 8 + (l >> 1);
-        w_at[j] = k * 256 + (((wn * 4 + j) ^ (k & 15)) * 16) + (l & 1) * 8;
+        w_at[j] = k * T_BYTES + (((wn * NJ + j) ^ (k & (T_LANES - 1))) * 16) + (l & 1) * 8;
       } else if constexpr (FORM == kColumns) {
         const int k = q * 8 + (l >> 2);
-        w_at[j] = k * 512 + (((wn * 4 + j) ^ swap16(k)) * 32) + (l & 3) * 8;
-      } else {
+        w_at[j] = k * T_BYTES + (((wn * NJ + j) ^ swap16(k)) * 32) + (l & 3) * 8;
+      } else if constexpr (FOURS) {
         // kUp: fragments 0, 2 are gate rows, 1, 3 up rows
         const int four = FORM == kUp ? j >> 1 : j & 1, half = FORM == kUp ? j & 1 : j >> 1;
-        const int r = wn * 64 + half * 32 + (l >> 2) * 8 + four * 4 + (l & 3);
+        const int r = wn * OF_WAVE + half * 32 + (l >> 2) * 8 + four * 4 + (l & 3);
         w_at[j] = r * 128 + ((q ^ swap_fours(r)) * 16);
+      } else {
+        const int r = wn * OF_WAVE + j * 16 + l;  // gate rows, up rows
+        w_at[j] = r * 128 + ((q ^ swap_rows(r)) * 16);
       }
     }
     if constexpr (FORM == kWeights) {
@@ -500,9 +506,9 @@ struct Product {
   // second: of the stage's second step
   __device__ __forceinline__ i32x4 read_w(uint32_t w_at, uint32_t stage, bool second) const {
     if constexpr (NARROW) {
-      return widen(__builtin_amdgcn_ds_read_tr8_b64_v2i32(LDS_PTR(i32x2, lds + stage + w_at + (second ? 32 * 256 : 0))));
+      return widen(__builtin_amdgcn_ds_read_tr8_b64_v2i32(LDS_PTR(i32x2, lds + stage + w_at + (second ? 32 * T_BYTES : 0))));
     } else if constexpr (FORM == kWeights || FORM == kColumns) {
-      return transposed(lds + stage + w_at + (second ? 32 * 512 : 0));
+      return transposed<T_BYTES>(lds + stage + w_at + (second ? 32 * T_BYTES : 0));
     } else {
       i32x4 w = *reinterpret_cast<const i32x4 *>(lds + stage + (w_at ^ (second ? 64 : 0)));
       if constexpr (INT8) w ^= (int)0x80808080;
@@ -511,15 +517,15 @@ struct Product {
   }
   // block m (transposed, the block is part of what was exchanged: see swap16)
   __device__ __forceinline__ i32x4 read_x(uint32_t x_at, uint32_t stage, bool second, int m) const {
-    if constexpr (FORM == kWeights) return transposed(lds + stage + (x_at ^ (m * 64)) + (second ? 32 * 512 : 0));
+    if constexpr (FORM == kWeights) return transposed<512>(lds + stage + (x_at ^ (m * 64)) + (second ? 32 * 512 : 0));
     else return *reinterpret_cast<const i32x4 *>(lds + stage + (x_at ^ (second ? 64 : 0)) + m * 4096);
   }
 
   __device__ __forceinline__ void run() {
     Tile t = tile(0);
     if (t.expert < 0) return;
-    i32x4 x[kMaxBlocks], w0[4], w1[4];
-    uint32_t w_at[4], x_at, rows_stage = 0, weights_stage = kWeightBase;  // the stages whose fragments are read
+    i32x4 x[MB], w0[NJ], w1[NJ];
+    uint32_t w_at[NJ], x_at, rows_stage = 0, weights_stage = WEIGHT_BASE;  // the stages whose fragments are read
     fragment_offsets(w_at, x_at);
     request_rows();
     request_weights();
@@ -528,9 +534,9 @@ struct Product {
     request_weights();
     landed_but<A_LOADS + 2 * B_LOADS>();
 #pragma unroll
-    for (int j = 0; j < 4; ++j) w0[j] = read_w(w_at[j], weights_stage, false);
+    for (int j = 0; j < NJ; ++j) w0[j] = read_w(w_at[j], weights_stage, false);
 #pragma unroll
-    for (int m = 0; m < kMaxBlocks; ++m) x[m] = read_x(x_at, rows_stage, false, m);
+    for (int m = 0; m < MB; ++m) x[m] = read_x(x_at, rows_stage, false, m);
     int stores = 0;  // that this wavefront has issued behind its last request, at least
     for (int i = 0; t.expert >= 0;) {
       const int m0 = FORM == kWeights ? gradient_row(t) : 0;
@@ -542,22 +548,22 @@ struct Product {
         list_more();
       }
       const Tile next = tile(i);
-      Acc acc[kMaxBlocks][4];
+      Acc acc[MB][NJ];
 #pragma unroll
-      for (int m = 0; m < kMaxBlocks; ++m)
+      for (int m = 0; m < MB; ++m)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[m][j] = Acc{};
+        for (int j = 0; j < NJ; ++j) acc[m][j] = Acc{};
       // A step reads the fragments of the next one, a block's once the block of this step has gone to the matrix cores.  Blocks that
       // the tile does not have are jumped over.
-      const auto step = [&](i32x4 (&now)[4], i32x4 (&then)[4], bool second) MOE_ROWS_INLINE {
+      const auto step = [&](i32x4 (&now)[NJ], i32x4 (&then)[NJ], bool second) MOE_ROWS_INLINE {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) then[j] = read_w(w_at[j], weights_stage, second);
+        for (int j = 0; j < NJ; ++j) then[j] = read_w(w_at[j], weights_stage, second);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int m = 0; m < kMaxBlocks; ++m) {
+        for (int m = 0; m < MB; ++m) {
           if (m == 0 || m < blocks) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) acc[m][j] = mma(now[j], x[m], acc[m][j]);
+            for (int j = 0; j < NJ; ++j) acc[m][j] = mma(now[j], x[m], acc[m][j]);
             x[m] = read_x(x_at, rows_stage, second, m);
           }
           // (load by load in between: all at once they would hold up the matrix cores; kWeights, whose tiles are short, is slower
@@ -567,6 +573,13 @@ struct Product {
             else if (m < A_LOADS + B_LOADS) request_weights(m - A_LOADS);
           }
           __builtin_amdgcn_sched_barrier(0);
+        }
+        if (!second && FORM != kWeights) {
+#pragma unroll
+          for (int m = MB; m < A_LOADS + B_LOADS; ++m) {
+            if (m < A_LOADS) request_rows(m);
+            else request_weights(m - A_LOADS);
+          }
         }
       };
       for (int left = stages_of(t); left > 0; --left) {
@@ -587,47 +600,51 @@ struct Product {
       }
       // the next tile's blocks that this one did not have
 #pragma unroll
-      for (int m = 1; m < kMaxBlocks; ++m)
+      for (int m = 1; m < MB; ++m)
         if (m >= blocks) x[m] = read_x(x_at, rows_stage, false, m);
       store(t, m0, acc, blocks);
-      stores = blocks * (FORM == kUp ? 1 : FORM == kColumns ? 4 : FORM == kWeights ? 2 : 0);
+      stores = blocks * (FORM == kUp ? 1 : FORM == kColumns ? NJ : FORM == kWeights ? 2 : 0);
       t = next;
     }
   }
 
   // lane: row lane % 16 of each block of 16 rows; columns as said at the LDS images
   // m0: kWeights, the tile's first row of the gradient's 3 * pitch
-  __device__ __forceinline__ void store(const Tile &t, int m0, const Acc (&acc)[kMaxBlocks][4], int blocks) const {
+  __device__ __forceinline__ void store(const Tile &t, int m0, const Acc (&acc)[MB][NJ], int blocks) const {
     const ExpertRowsParams &p = g.p;
     const int q = lane >> 4, r0 = wm * 16 + (lane & 15);
     const uint8_t *blob = p.blobs + t.expert * p.blob_stride;
     const int64_t tail = (int64_t)p.inter * 3 * row_bytes;
     if constexpr (FORM == kUp) {
-      const int rec = t.col * 128 + wn * 32 + q * 8;
+      constexpr int N = NJ * 2;  // records of a lane
+      const int rec = t.col * RECS + wn * (OF_WAVE / 2) + q * N;
       const Buffer h = buffer_of(g.out + (int64_t)t.row0 * pitch, t.rows * pitch * 2);
       const Buffer both = buffer_of(g.gu_out + (int64_t)t.row0 * 2 * pitch, g.gu_out ? t.rows * 2 * pitch * 4 : 0);
-      float sg[8], su[8];
+      float sg[N], su[N];
       if constexpr (INT8) {
         const Buffer scales = buffer_of(blob + tail, p.inter * 4);
-        const rows_u32x4 vg = __builtin_amdgcn_raw_buffer_load_b128(scales, rec < p.inter ? rec * 2 : kNowhere, 0, 0),
-                         vu = __builtin_amdgcn_raw_buffer_load_b128(scales, rec < p.inter ? (p.inter + rec) * 2 : kNowhere, 0, 0);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          sg[2 * i] = half_lo(vg[i]);
-          sg[2 * i + 1] = half_hi(vg[i]);
-          su[2 * i] = half_lo(vu[i]);
-          su[2 * i + 1] = half_hi(vu[i]);
+        for (int i = 0; i < N; i += 4) {
+          const rows_u32x2 vg = __builtin_amdgcn_raw_buffer_load_b64(scales, rec < p.inter ? (rec + i) * 2 : kNowhere, 0, 0),
+                           vu = __builtin_amdgcn_raw_buffer_load_b64(scales, rec < p.inter ? (p.inter + rec + i) * 2 : kNowhere, 0, 0);
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            sg[i + 2 * k] = half_lo(vg[k]);
+            sg[i + 2 * k + 1] = half_hi(vg[k]);
+            su[i + 2 * k] = half_lo(vu[k]);
+            su[i + 2 * k + 1] = half_hi(vu[k]);
+          }
         }
       }
       const Buffer row_scale = buffer_of(g.scale + t.row0, INT8 ? t.rows * 4 : 0);
 #pragma unroll
-      for (int m = 0; m < kMaxBlocks; ++m) {
+      for (int m = 0; m < MB; ++m) {
         if (m > 0 && m >= blocks) break;
         const uint32_t r = r0 + m * 32;
         const float sx = INT8 ? __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(row_scale, r * 4, 0, 0)) : 1.f;
-        float v[8], gate[8], up[8];
+        float v[N], gate[N], up[N];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < N; ++i) {
           gate[i] = (float)acc[m][(i >> 2) * 2][i & 3];
           up[i] = (float)acc[m][(i >> 2) * 2 + 1][i & 3];
           if constexpr (INT8) {
@@ -636,22 +653,22 @@ struct Product {
           }
           v[i] = gate[i] * sigmoid(gate[i]) * up[i];
         }
-        store8(h, rec < pitch ? (r * pitch + rec) * 2 : kNowhere, v);
+        store_bf16(h, rec < pitch ? (r * pitch + rec) * 2 : kNowhere, v);
         if (g.gu_out) {
           const uint32_t at = rec < pitch ? (r * 2 * pitch + rec) * 4 : kNowhere;
-          store8_f32(both, at, gate);
-          store8_f32(both, at + pitch * 4, up);
+          store_f32(both, at, gate);
+          store_f32(both, at + pitch * 4, up);
         }
       }
     } else if constexpr (FORM == kDgu) {
       const Buffer in = buffer_of(g.gu_in + (int64_t)t.row0 * 2 * pitch, t.rows * 2 * pitch * 4),
                    out = buffer_of(g.out + (int64_t)t.row0 * 2 * pitch, t.rows * 2 * pitch * 2);
 #pragma unroll
-      for (int m = 0; m < kMaxBlocks; ++m) {
+      for (int m = 0; m < MB; ++m) {
         if (m > 0 && m >= blocks) break;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int rec = t.col * kCols + wn * 64 + h * 32 + q * 8;
+        for (int h = 0; h < NJ / 2; ++h) {
+          const int rec = t.col * COLS + wn * OF_WAVE + h * 32 + q * 8;
           const uint32_t at = rec < pitch ? (r0 + m * 32) * 2 * pitch + rec : kNowhere / 4;
           float gate[8], up[8];
           load8_f32(in, at * 4, gate);
@@ -663,15 +680,15 @@ struct Product {
             up[i] = dh * (x * s);
           }
           // (behind the last record: both resources end before kNowhere / 2)
-          store8(out, at * 2, gate);
-          store8(out, (at + pitch) * 2, up);
+          store_bf16(out, at * 2, gate);
+          store_bf16(out, (at + pitch) * 2, up);
         }
       }
     } else if constexpr (FORM == kColumns) {
       const Buffer out = buffer_of(g.out + (int64_t)t.row0 * p.hidden, t.rows * p.hidden * 2);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int col = t.col * kCols + wn * 64 + j * 16 + q * 4;
+      for (int j = 0; j < NJ; ++j) {
+        const int col = t.col * COLS + wn * OF_WAVE + j * 16 + q * 4;
         float sd[4];
         if constexpr (INT8) {
           const rows_u32x2 w = *reinterpret_cast<const rows_u32x2 *>(blob + tail + (int64_t)p.inter * 4 + col * 2);
@@ -681,19 +698,19 @@ struct Product {
           sd[3] = half_hi(w[1]);
         }
 #pragma unroll
-        for (int m = 0; m < kMaxBlocks; ++m) {
+        for (int m = 0; m < MB; ++m) {
           if (m > 0 && m >= blocks) break;
           float v[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i) v[i] = INT8 ? acc[m][j][i] * sd[i] : acc[m][j][i];
-          store4(out, ((r0 + m * 32) * p.hidden + col) * 2, v);
+          store_bf16(out, ((r0 + m * 32) * p.hidden + col) * 2, v);
         }
       }
     } else {
       const Buffer out = buffer_of(g.dblobs + t.expert * p.blob_stride, (uint32_t)tail);
-      const int m_rows = gradient_rows(m0), col0 = t.col % n_cols * kCols;
+      const int m_rows = gradient_rows(m0), col0 = t.col % n_cols * COLS;
 #pragma unroll
-      for (int m = 0; m < kMaxBlocks; ++m) {
+      for (int m = 0; m < MB; ++m) {
         if (m > 0 && m >= blocks) break;
         const int r = r0 + m * 32, at = m0 + r, which = at >= 2 * pitch ? 2 : at >= pitch ? 1 : 0, rec = at - which * pitch;
         // (a record that is not there lies behind the end)
@@ -703,30 +720,40 @@ struct Product {
           float v[8];
 #pragma unroll
           for (int i = 0; i < 8; ++i) v[i] = acc[m][h * 2 + (i >> 2)][i & 3];
-          store8(out, to + h * 64, v);
+          store_bf16(out, to + h * 64, v);
         }
       }
     }
   }
 };
 
-template <int FORM, bool INT8>
-__global__ __launch_bounds__(kBlock, 2) void product_kernel(const ProductArgs g) {
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[kLdsBytes];
+template <int FORM, bool INT8, int NJ, int MB>
+__global__ __launch_bounds__(kBlock, NJ == 4 ? 2 : 4) void product_kernel(const ProductArgs g) {
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[Product<FORM, INT8, NJ, MB>::LDS_BYTES];
   if constexpr (FORM == kColumns) {  // rows of nobody
     const ExpertRowsParams &p = g.p;
     const int used = uniform(min(max(p.offsets[p.n_experts], 0), p.n_rows));
     for (int64_t r = used + blockIdx.x; r < p.n_rows; r += gridDim.x)
       for (int c = threadIdx.x * 8; c < p.hidden; c += kBlock * 8) *reinterpret_cast<rows_u32x4 *>(g.out + r * p.hidden + c) = rows_u32x4{};
   }
-  Product<FORM, INT8> f(g, lds);
+  Product<FORM, INT8, NJ, MB> f(g, lds);
   f.run();
 }
 
+// Tiles of 256 x 256 where they are as many as the compute units, which then have one workgroup each; otherwise tiles of 64 rows
+// and 128 columns, and two workgroups a compute unit.  (SMALL_FIGURES)
 template <int FORM, bool INT8>
 hipError_t launch_product(const ProductArgs &g, int n_cus, hipStream_t s) {
-  // one workgroup a compute unit, in whole eights
-  hipLaunchKernelGGL((product_kernel<FORM, INT8>), dim3(n_cus / 8 * 8), dim3(kBlock), 0, s, g);
+  const int grid = n_cus / 8 * 8;  // (the XCDs are eight)
+  if constexpr (FORM != kWeights) {
+    const int pitch = expert_rows_pitch(g.p.inter), n_cols = FORM == kUp ? (pitch + 127) / 128 : FORM == kDgu ? (pitch + 255) / 256 : g.p.hidden / 256;
+    const int64_t tiles = (int64_t)(g.p.n_rows / 256 + (g.p.n_experts < g.p.n_rows ? g.p.n_experts : g.p.n_rows)) * n_cols;
+    if (tiles < grid) {
+      hipLaunchKernelGGL((product_kernel<FORM, INT8, 2, 2>), dim3(2 * grid), dim3(kBlock), 0, s, g);
+      return hipGetLastError();
+    }
+  }
+  hipLaunchKernelGGL((product_kernel<FORM, INT8, 4, 8>), dim3(grid), dim3(kBlock), 0, s, g);
   return hipGetLastError();
 }
 

@@ -355,6 +355,69 @@ def test_experts(lib, counts, fmt, hidden, inter):
     assert torch.equal(ys, again)
 
 
+MANY = [300, 0, 1, 31, 257, 512, 96, 700, 33, 16] * 4  # (with these and a wide layer there are more tiles than compute units)
+
+
+@pytest.mark.parametrize("fmt,hidden,inter", [("bf16", 1024, 1000), ("int8", 1024, 904), ("bf16", 2048, 897)])
+def test_experts_many_tiles(lib, fmt, hidden, inter):
+    g = gen(inter)
+    blobs, dense = make_blobs(lib, g, fmt, len(MANY), hidden, inter)
+    n = sum(MANY)
+    xs, scale, x = make_rows(g, fmt, n + 5, hidden)
+    ys = lib.experts_rows(fmt, blobs, inter, xs, offsets_of(MANY), scale=scale)
+    assert not ys[n:].any()
+    at = 0
+    for e, (c, (wg, wu, wd)) in enumerate(zip(MANY, dense)):
+        r = x[at:at + c]
+        a, b = r @ wg.t(), r @ wu.t()
+        s = torch.sigmoid(a)
+        h = a * s * b
+        ref = h @ wd.t()
+        sums = 64 * U32
+        dh = U16 * h.abs() + sums * (1.1 * b.abs() * (r.abs() @ wg.abs().t()) + (a * s).abs() * (r.abs() @ wu.abs().t())) + 8 * U32 * h.abs()
+        within(ys[at:at + c], ref, 1.01 * (dh @ wd.abs().t()) + 64 * U32 * (h.abs() @ wd.abs().t()) + 1.01 * U16 * ref.abs() + 1e-12, f"ys {e}")
+        at += c
+    assert torch.equal(ys, lib.experts_rows(fmt, blobs, inter, xs, offsets_of(MANY), scale=scale))
+    if fmt == "int8":
+        return
+    dys = normal(g, n + 5, hidden, dtype=BF16)
+    again, kept = lib.experts_rows(fmt, blobs, inter, xs, offsets_of(MANY), keep=True)
+    dxs, dblobs = lib.experts_rows_backward(fmt, blobs, inter, xs, offsets_of(MANY), kept, dys)
+    assert torch.equal(again, ys) and not dxs[n:].any()
+    dw = dblobs.view(BF16).view(len(MANY), inter, 3, hidden)
+    at = 0
+    for e, c in enumerate(MANY):
+        if c == 0:
+            assert not dw[e].any()
+            continue
+        leaves = [t.clone().requires_grad_() for t in (x[at:at + c], *dense[e])]
+        grads = torch.autograd.grad(plain_expert(*leaves), leaves, dys[at:at + c].double())
+        for got, ref, what in zip((dxs[at:at + c], dw[e, :, 0], dw[e, :, 1], dw[e, :, 2].t()), grads, ("dx", "dgate", "dup", "ddown")):
+            off_ = float((got.double() - ref).norm() / ref.norm())
+            assert off_ <= 6 * U16, (what, e, off_)
+        at += c
+
+
+def test_experts_more_tiles_than_a_list_holds(lib):
+    """A workgroup lists 64 of its tiles at a time: gradients of many wide experts without rows but the last ones."""
+    hidden, inter, experts = 4096, 64, 512
+    g = gen(61)
+    blobs = (torch.randn(experts, inter * 3 * hidden, generator=g, device=DEV) * 0.02).to(BF16).view(torch.uint8)
+    counts = [0] * (experts - 3) + [5, 0, 70]
+    xs, dys = normal(g, 75, hidden, dtype=BF16), normal(g, 75, hidden, dtype=BF16)
+    ys, kept = lib.experts_rows("bf16", blobs, inter, xs, offsets_of(counts), keep=True)
+    dxs, dblobs = lib.experts_rows_backward("bf16", blobs, inter, xs, offsets_of(counts), kept, dys)
+    dw = dblobs.view(BF16).view(experts, inter, 3, hidden)
+    assert not dw[:experts - 3].any() and not dw[experts - 2].any()
+    for e, rows in ((experts - 3, slice(0, 5)), (experts - 1, slice(5, 75))):
+        wg, wu, wd = blobs[e].view(BF16).view(inter, 3, hidden).double().unbind(1)
+        leaves = [t.clone().requires_grad_() for t in (xs[rows].double(), wg, wu, wd.t())]
+        y = plain_expert(*leaves)
+        grads = torch.autograd.grad(y, leaves, dys[rows].double())
+        for got, ref in ((ys[rows], y.detach()), (dxs[rows], grads[0]), (dw[e, :, 0], grads[1]), (dw[e, :, 1], grads[2]), (dw[e, :, 2].t(), grads[3])):
+            assert float((got.double() - ref).norm() / ref.norm()) <= 6 * U16
+
+
 def plain_expert(x, wg, wu, wd):
     a, b = x @ wg.t(), x @ wu.t()
     return (torch.nn.functional.silu(a) * b) @ wd.t()
