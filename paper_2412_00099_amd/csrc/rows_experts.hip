@@ -16,7 +16,7 @@
 // holds every code exactly.
 //
 // A workgroup of eight wavefronts has a compute unit to itself and walks over tiles of up to 256 x 256, a wavefront 128 x 64 of
-// it.  The summed index goes through LDS in stages of 64 (8-bit: 128) values, whole 128-byte lines, filled by loads that bypass
+// it; where experts have few rows two workgroups share a compute unit and tiles are 64 x 128.  The summed index goes through LDS in stages of 64 (8-bit: 128) values, whole 128-byte lines, filled by loads that bypass
 // the registers: two stages of the rows' side, which other workgroups of the XCD read too, and three of the weights' side, which
 // comes from memory.  A stage is two steps of the matrix cores; the fragments of the next step are read while they work on this
 // one's, and there is one barrier a stage.  Both rings run on from tile to tile.
@@ -740,15 +740,19 @@ __global__ __launch_bounds__(kBlock, NJ == 4 ? 2 : 4) void product_kernel(const 
   f.run();
 }
 
-// Tiles of 256 x 256 where they are as many as the compute units, which then have one workgroup each; otherwise tiles of 64 rows
-// and 128 columns, and two workgroups a compute unit.  (SMALL_FIGURES)
+// Tiles of 256 x 256 where they are as many as the compute units, which then have one workgroup each, and an expert has more than 96
+// rows on average; otherwise tiles of 64 rows and 128 columns, and two workgroups a compute unit.  Measured with 60 experts of
+// 2048 x 1408 and four a token, kUp + kColumns in us, small tiles against large ones: 16 tokens 122 and 161, 512 tokens 223 and
+// 253 (8 bits: 147 and 180), 1024 tokens (68 rows an expert) 273 and 318 (182 and 207), 1280 tokens 280 and 316, 2048 tokens (137
+// rows) 348 and 338 (235 and 242), 4096 tokens 578 and 458 (398 and 323).  Where large tiles are too few: 8 experts of 1024 x 704
+// and two a token, 512 tokens 26 and 55, 2048 tokens 46 and 59.
 template <int FORM, bool INT8>
 hipError_t launch_product(const ProductArgs &g, int n_cus, hipStream_t s) {
   const int grid = n_cus / 8 * 8;  // (the XCDs are eight)
   if constexpr (FORM != kWeights) {
     const int pitch = expert_rows_pitch(g.p.inter), n_cols = FORM == kUp ? (pitch + 127) / 128 : FORM == kDgu ? (pitch + 255) / 256 : g.p.hidden / 256;
     const int64_t tiles = (int64_t)(g.p.n_rows / 256 + (g.p.n_experts < g.p.n_rows ? g.p.n_experts : g.p.n_rows)) * n_cols;
-    if (tiles < grid) {
+    if (tiles < grid || g.p.n_rows <= 96 * (int64_t)g.p.n_experts) {
       hipLaunchKernelGGL((product_kernel<FORM, INT8, 2, 2>), dim3(2 * grid), dim3(kBlock), 0, s, g);
       return hipGetLastError();
     }
