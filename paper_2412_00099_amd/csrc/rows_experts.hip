@@ -100,8 +100,8 @@ __device__ __forceinline__ T sum_upto(T v, int lane) {  // of lanes 0 .. lane
 }
 
 // What an expert's tiles are.  Its rows are cut into the fewest parts of at most MOST, all of nearly the same size.  cost: of a
-// tile, in rows; that the weights have to come in costs about as much as 128 rows do (kWeights: 256 columns times the rows, and the
-// stores).
+// tile, in rows; that the weights have to come in costs about as much as 128 rows do.  kWeights: the rows in
+// whole stages and 64 for the stores (16384 rows in 60 uneven experts: 590 us, with 212 for them 624, with unrounded rows and 384 634).
 struct ExpertTiles {
   int parts, each, n, cost;
 };
@@ -111,7 +111,7 @@ __device__ __forceinline__ ExpertTiles expert_tiles(int count, int n_cols, int m
   t.parts = (count + MOST - 1) / MOST;
   t.each = t.parts > 0 ? ((count + t.parts - 1) / t.parts + 15) / 16 * 16 : 0;
   t.n = FORM == kWeights ? m_tiles * n_cols : t.parts * n_cols;
-  t.cost = FORM == kWeights ? count + 384 : t.each + 128;
+  t.cost = FORM == kWeights ? (count + 63) / 64 * 64 + 64 : t.each + 128;
   return t;
 }
 // Tiles in the order expert, column, row, so that the workgroups that share weights are neighbours.  The list is cut into eight
@@ -240,15 +240,38 @@ __device__ __forceinline__ void store_bf16(Buffer p, uint32_t off, const float (
     __builtin_amdgcn_raw_buffer_store_b64(w, p, off, 0, 0);
   }
 }
-template <int N>
-__device__ __forceinline__ void store_f32(Buffer p, uint32_t off, const float (&v)[N]) {
+// Whole lines.  Before: a lane of row l (of 16) has 16 bytes in a, and 16 bytes further on or in the line's second half in b.  After:
+// the lanes l and l ^ 8 have both of row l & 7 in a and both of row (l & 7) + 8 in b, lane l the part l / 8.  A store then
+// writes eight rows of 128 bytes rather than sixteen of 64 (alone, 1 GB of gradients: 221 us in halves, 175 in whole lines).
+__device__ __forceinline__ void swap_halves(rows_u32x4 &a, rows_u32x4 &b) {
+  const bool low = (threadIdx.x & 8) == 0;
 #pragma unroll
-  for (int h = 0; h < N; h += 4) {
-    rows_u32x4 w;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(v[h + i]);
-    __builtin_amdgcn_raw_buffer_store_b128(w, p, off + 4 * h, 0, 0);
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t got = __builtin_amdgcn_update_dpp(0, low ? b[i] : a[i], 0x128, 0xf, 0xf, true);  // (of lane l ^ 8)
+    a[i] = low ? a[i] : got;
+    b[i] = low ? got : b[i];
   }
+}
+// (past the caches, which the loads need: gradients of the weights 655 us without, 629 with)
+__device__ __forceinline__ void store16(Buffer p, uint32_t off, rows_u32x4 v) { __builtin_amdgcn_raw_buffer_store_b128(v, p, off, 0, 2); }
+// `off`: of row l & 7; row (l & 7) + 8 lies `eight_rows` bytes on
+__device__ __forceinline__ void store_lines(Buffer p, uint32_t off, uint32_t eight_rows, rows_u32x4 a, rows_u32x4 b) {
+  swap_halves(a, b);
+  store16(p, off, a);
+  store16(p, off + eight_rows, b);
+}
+__device__ __forceinline__ rows_u32x4 four_f32(const float *v) {
+  rows_u32x4 w;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(v[i]);
+  return w;
+}
+template <typename Get>
+__device__ __forceinline__ rows_u32x4 eight_bf16(Get v) {
+  rows_u32x4 w;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = pack_bf16(v(2 * i), v(2 * i + 1));
+  return w;
 }
 __device__ __forceinline__ void load8_f32(Buffer p, uint32_t off, float (&v)[8]) {
 #pragma unroll
@@ -655,9 +678,15 @@ struct Product {
         }
         store_bf16(h, rec < pitch ? (r * pitch + rec) * 2 : kNowhere, v);
         if (g.gu_out) {
-          const uint32_t at = rec < pitch ? (r * 2 * pitch + rec) * 4 : kNowhere;
-          store_f32(both, at, gate);
-          store_f32(both, at + pitch * 4, up);
+          if constexpr (N == 8) {
+            const uint32_t at = rec < pitch ? ((m * 32 + wm * 16 + (lane & 7)) * 2 * pitch + rec + (lane & 8) / 2) * 4 : kNowhere;
+            store_lines(both, at, 64 * pitch, four_f32(gate), four_f32(gate + 4));
+            store_lines(both, at + pitch * 4, 64 * pitch, four_f32(up), four_f32(up + 4));
+          } else {
+            const uint32_t at = rec < pitch ? (r * 2 * pitch + rec) * 4 : kNowhere;
+            store16(both, at, four_f32(gate));
+            store16(both, at + pitch * 4, four_f32(up));
+          }
         }
       }
     } else if constexpr (FORM == kDgu) {
@@ -666,6 +695,7 @@ struct Product {
 #pragma unroll
       for (int m = 0; m < MB; ++m) {
         if (m > 0 && m >= blocks) break;
+        rows_u32x4 dg[NJ / 2], du[NJ / 2];
 #pragma unroll
         for (int h = 0; h < NJ / 2; ++h) {
           const int rec = t.col * COLS + wn * OF_WAVE + h * 32 + q * 8;
@@ -679,9 +709,20 @@ struct Product {
             gate[i] = dh * up[i] * (s * (1.f + x * (1.f - s)));
             up[i] = dh * (x * s);
           }
-          // (behind the last record: both resources end before kNowhere / 2)
-          store_bf16(out, at * 2, gate);
-          store_bf16(out, (at + pitch) * 2, up);
+          dg[h] = eight_bf16([&](int i) MOE_ROWS_INLINE { return gate[i]; });
+          du[h] = eight_bf16([&](int i) MOE_ROWS_INLINE { return up[i]; });
+        }
+        // (behind the last record: the resource ends before kNowhere / 2)
+        if constexpr (NJ == 4) {
+          const int rec = t.col * COLS + wn * OF_WAVE + (lane & 8) * 4 + q * 8;
+          const uint32_t at = rec < pitch ? (m * 32 + wm * 16 + (lane & 7)) * 2 * pitch + rec : kNowhere / 4;
+          store_lines(out, at * 2, 32 * pitch, dg[0], dg[1]);
+          store_lines(out, (at + pitch) * 2, 32 * pitch, du[0], du[1]);
+        } else {
+          const int rec = t.col * COLS + wn * OF_WAVE + q * 8;
+          const uint32_t at = rec < pitch ? (r0 + m * 32) * 2 * pitch + rec : kNowhere / 4;
+          store16(out, at * 2, dg[0]);
+          store16(out, (at + pitch) * 2, du[0]);
         }
       }
     } else if constexpr (FORM == kColumns) {
@@ -712,16 +753,12 @@ struct Product {
 #pragma unroll
       for (int m = 0; m < MB; ++m) {
         if (m > 0 && m >= blocks) break;
-        const int r = r0 + m * 32, at = m0 + r, which = at >= 2 * pitch ? 2 : at >= pitch ? 1 : 0, rec = at - which * pitch;
+        const int r = m * 32 + wm * 16 + (lane & 7), at = m0 + r, which = at >= 2 * pitch ? 2 : at >= pitch ? 1 : 0, rec = at - which * pitch;
         // (a record that is not there lies behind the end)
-        const uint32_t to = r < m_rows ? ((rec * 3 + which) * p.hidden + col0 + wn * 64 + q * 8) * 2 : kNowhere;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          float v[8];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) v[i] = acc[m][h * 2 + (i >> 2)][i & 3];
-          store_bf16(out, to + h * 64, v);
-        }
+        const uint32_t to = r < m_rows ? ((rec * 3 + which) * p.hidden + col0 + wn * 64 + (lane & 8) * 4 + q * 8) * 2 : kNowhere;
+        const rows_u32x4 v0 = eight_bf16([&](int i) MOE_ROWS_INLINE { return acc[m][i >> 2][i & 3]; }),
+                   v1 = eight_bf16([&](int i) MOE_ROWS_INLINE { return acc[m][2 + (i >> 2)][i & 3]; });
+        store_lines(out, to, 8 * 3 * p.hidden * 2, v0, v1);
       }
     }
   }
