@@ -321,9 +321,9 @@ struct Product {
   static constexpr int EL = INT8 ? 1 : 2;
   static constexpr int ROWS = MB * 32, COLS = NJ * 64, OF_WAVE = NJ * 16;  // of a tile; of a wavefront
   static constexpr int RECS = COLS / 2;                                   // kUp: records of a tile, each has two products
-  static constexpr uint32_t ROW_STAGE = ROWS * 128, WEIGHT_STAGE = COLS * 128, WEIGHT_BASE = kRowStages * ROW_STAGE;
-  static constexpr uint32_t LDS_BYTES = WEIGHT_BASE + kWeightStages * WEIGHT_STAGE;
   static constexpr bool NARROW = FORM == kColumns && INT8;       // the weights' stage is of bytes: half as long
+  static constexpr uint32_t ROW_STAGE = ROWS * 128, WEIGHT_STAGE = COLS * (NARROW ? 64 : 128), WEIGHT_BASE = kRowStages * ROW_STAGE;
+  static constexpr uint32_t LDS_BYTES = WEIGHT_BASE + kWeightStages * WEIGHT_STAGE;
   static constexpr int A_LOADS = MB / 2, B_LOADS = NARROW ? NJ / 2 : NJ;  // of a wavefront for a stage
   static constexpr bool FOURS = FORM == kDgu || (FORM == kUp && NJ == 4);  // side by side: fragments of 4 rows of each 8
   static constexpr int T_BYTES = NARROW ? COLS : COLS * 2, T_LANES = T_BYTES / 16, T_ROWS = 64 / T_LANES;  // transposed: a row, its lanes in a load, rows of a load
@@ -794,7 +794,7 @@ struct Product {
 };
 
 template <int FORM, bool INT8, int NJ, int MB>
-__global__ __launch_bounds__(kBlock, NJ == 4 ? 2 : 4) void product_kernel(const ProductArgs g) {
+__global__ __launch_bounds__(kBlock, MB == 8 ? 2 : 4) void product_kernel(const ProductArgs g) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds[Product<FORM, INT8, NJ, MB>::LDS_BYTES];
   if constexpr (FORM == kColumns) {  // rows of nobody
     const ExpertRowsParams &p = g.p;
@@ -812,14 +812,24 @@ __global__ __launch_bounds__(kBlock, NJ == 4 ? 2 : 4) void product_kernel(const 
 // 253 (8 bits: 147 and 180), 1024 tokens (68 rows an expert) 273 and 318 (182 and 207), 1280 tokens 280 and 316, 2048 tokens (137
 // rows) 348 and 338 (235 and 242), 4096 tokens 578 and 458 (398 and 323).  Where large tiles are too few: 8 experts of 1024 x 704
 // and two a token, 512 tokens 26 and 55, 2048 tokens 46 and 59.
+//
+// Columns of bytes: small tiles have 256 of them where tiles of 128 would be three or more for a compute unit.  In us against 128:
+// 16 tokens 38 and 45, 64 tokens 41 and 51, 512 tokens 62 and 68; where there are fewer tiles, 2 tokens 24 and 19, 8 experts and
+// 2048 tokens 26 and 23.
 template <int FORM, bool INT8>
 hipError_t launch_product(const ProductArgs &g, int n_cus, hipStream_t s) {
   const int grid = n_cus / 8 * 8;  // (the XCDs are eight)
   if constexpr (FORM != kWeights) {
-    const int pitch = expert_rows_pitch(g.p.inter), n_cols = FORM == kUp ? (pitch + 127) / 128 : FORM == kDgu ? (pitch + 255) / 256 : g.p.hidden / 256;
-    const int64_t tiles = (int64_t)(g.p.n_rows / 256 + (g.p.n_experts < g.p.n_rows ? g.p.n_experts : g.p.n_rows)) * n_cols;
-    if (tiles < grid || g.p.n_rows <= 96 * (int64_t)g.p.n_experts) {
-      hipLaunchKernelGGL((product_kernel<FORM, INT8, 2, 2>), dim3(2 * grid), dim3(kBlock), 0, s, g);
+    // at most, from what the host knows
+    const int64_t n_rows = g.p.n_rows, n_experts = g.p.n_experts, with_rows = n_rows < n_experts ? n_rows : n_experts;
+    const int pitch = expert_rows_pitch(g.p.inter), wide = FORM == kUp ? 2 * pitch : FORM == kDgu ? pitch : g.p.hidden;
+    const auto tiles = [&](int rows, int cols) { return (n_rows / rows + with_rows) * ((wide + cols - 1) / cols); };
+    if (tiles(256, 256) < grid || n_rows <= 96 * n_experts) {
+      constexpr bool BYTES = FORM == kColumns && INT8;
+      if (BYTES && tiles(64, 128) >= 3 * grid)
+        hipLaunchKernelGGL((product_kernel<FORM, INT8, BYTES ? 4 : 2, 2>), dim3(2 * grid), dim3(kBlock), 0, s, g);
+      else
+        hipLaunchKernelGGL((product_kernel<FORM, INT8, 2, 2>), dim3(2 * grid), dim3(kBlock), 0, s, g);
       return hipGetLastError();
     }
   }
