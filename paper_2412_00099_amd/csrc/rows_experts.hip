@@ -228,8 +228,8 @@ __device__ __forceinline__ Tile lane_tile(const ExpertRowsParams &p, const TileL
 // fragment has 16 rows in a row and where it has 4 of each 8.
 __device__ __forceinline__ int swap_rows(int r) { return (r >> 1) & 7; }
 __device__ __forceinline__ int swap_fours(int r) { return ((r >> 1) & 1) | ((r >> 2) & 6); }
-// Transposed, 16-bit: 64 rows (the summed index) of 256 columns, 512 bytes.  Where a fragment has 16 columns in a row, their 32
-// bytes (group g) lie at g ^ swap16(k); where it has 4 of each 8, 64 bytes (group g) lie at g ^ k % 4.
+// Transposed, 16-bit: 64 rows (the summed index) of 256 columns, 512 bytes.  kWeights' rows: a fragment has 16 columns in a row,
+// their 32 bytes (group g) lie at g ^ swap16(k).  Weights: it has 4 of each 8, 64 bytes (group g) lie at g ^ k % 4.
 __device__ __forceinline__ int swap16(int k) { return (k & 3) | ((k >> 1) & 4); }
 // Results: register i of a lane is column (lane / 16) * 4 + i of a fragment.  With PAIRED fragments j and j + 1 have 4 columns
 // of each 8 in turn, so that a lane has 8 columns in a row and stores 16 bytes.
@@ -458,7 +458,7 @@ struct Product {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           const int k = (wave * B_LOADS + i) * T_ROWS + lane / T_LANES, pos = lane % T_LANES;
-          const int chunk = NARROW ? pos ^ (k & (T_LANES - 1)) : pos ^ (swap16(k) << 1);
+          const int chunk = NARROW ? pos ^ (k & (T_LANES - 1)) : pos ^ ((k & 3) << 2);
           b_off[i] = (uint32_t)k * rec_bytes + t.col * COLS * EL + chunk * 16;
         }
       }
@@ -528,15 +528,12 @@ struct Product {
     const int l = lane & 15, q = lane >> 4;
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
-      if constexpr (FORM == kWeights) {
-        const int k = q * 8 + (l >> 2), chunk = wn * 8 + (j >> 1) * 4 + (l & 3);
-        w_at[j] = k * 512 + ((chunk ^ ((k & 3) << 2)) * 16) + (j & 1) * 8;
-      } else if constexpr (NARROW) {
+      if constexpr (NARROW) {
         const int k = q * 8 + (l >> 1);
         w_at[j] = k * T_BYTES + (((wn * NJ + j) ^ (k & (T_LANES - 1))) * 16) + (l & 1) * 8;
-      } else if constexpr (FORM == kColumns) {
-        const int k = q * 8 + (l >> 2);
-        w_at[j] = k * T_BYTES + (((wn * NJ + j) ^ swap16(k)) * 32) + (l & 3) * 8;
+      } else if constexpr (!SIDE) {
+        const int k = q * 8 + (l >> 2), chunk = wn * NJ * 2 + (j >> 1) * 4 + (l & 3);
+        w_at[j] = k * T_BYTES + ((chunk ^ ((k & 3) << 2)) * 16) + (j & 1) * 8;
       } else if constexpr (FOURS) {
         // kUp: fragments 0, 2 are gate rows, 1, 3 up rows
         const int four = FORM == kUp ? j >> 1 : j & 1, half = FORM == kUp ? j & 1 : j >> 1;
@@ -655,7 +652,7 @@ struct Product {
       for (int m = 1; m < MB; ++m)
         if (m >= blocks) x[m] = read_x(x_at, rows_stage, false, m);
       store(t, m0, acc, blocks);
-      stores = blocks * (FORM == kUp ? 1 : FORM == kColumns ? NJ : FORM == kWeights ? 2 : 0);
+      stores = blocks * (FORM == kUp ? 1 : FORM == kColumns && INT8 ? NJ : FORM == kColumns || FORM == kWeights ? NJ / 2 : 0);
       t = next;
     }
   }
@@ -756,24 +753,31 @@ struct Product {
       }
     } else if constexpr (FORM == kColumns) {
       const Buffer out = buffer_of(g.out + (int64_t)t.row0 * p.hidden, t.rows * p.hidden * 2);
+      if constexpr (INT8) {
 #pragma unroll
-      for (int j = 0; j < NJ; ++j) {
-        const int col = t.col * COLS + wn * OF_WAVE + j * 16 + q * 4;
-        float sd[4];
-        if constexpr (INT8) {
+        for (int j = 0; j < NJ; ++j) {
+          const int col = t.col * COLS + wn * OF_WAVE + j * 16 + q * 4;
           const rows_u32x2 w = *reinterpret_cast<const rows_u32x2 *>(blob + tail + (int64_t)p.inter * 4 + col * 2);
-          sd[0] = half_lo(w[0]);
-          sd[1] = half_hi(w[0]);
-          sd[2] = half_lo(w[1]);
-          sd[3] = half_hi(w[1]);
+          const float sd[4] = {half_lo(w[0]), half_hi(w[0]), half_lo(w[1]), half_hi(w[1])};
+#pragma unroll
+          for (int m = 0; m < MB; ++m) {
+            if (m > 0 && m >= blocks) break;
+            const float v[4] = {acc[m][j][0] * sd[0], acc[m][j][1] * sd[1], acc[m][j][2] * sd[2], acc[m][j][3] * sd[3]};
+            store_bf16(out, ((r0 + m * 32) * p.hidden + col) * 2, v);
+          }
         }
+      } else {
 #pragma unroll
         for (int m = 0; m < MB; ++m) {
           if (m > 0 && m >= blocks) break;
-          float v[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) v[i] = INT8 ? acc[m][j][i] * sd[i] : acc[m][j][i];
-          store_bf16(out, ((r0 + m * 32) * p.hidden + col) * 2, v);
+          const auto half = [&](int h) MOE_ROWS_INLINE {
+            return eight_bf16([&](int i) MOE_ROWS_INLINE { return acc[m][h * 2 + (i >> 2)][i & 3]; });
+          };
+          const int col = t.col * COLS + wn * OF_WAVE + q * 8;
+          if constexpr (NJ == 4)
+            store_lines(out, ((m * 32 + wm * 16 + (lane & 7)) * p.hidden + col + (lane & 8) * 4) * 2, 8 * p.hidden * 2, half(0), half(1));
+          else
+            __builtin_amdgcn_raw_buffer_store_b128(half(0), out, ((r0 + m * 32) * p.hidden + col) * 2, 0, 0);
         }
       }
     } else {
