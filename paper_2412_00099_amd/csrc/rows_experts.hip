@@ -83,20 +83,29 @@ struct Tile {
 };
 __device__ __forceinline__ int first_row(const ExpertRowsParams &p, int e) { return min(max(p.offsets[e], 0), p.n_rows); }
 __device__ __forceinline__ int row_count(const ExpertRowsParams &p, int e) { return max(min(p.offsets[e + 1], p.n_rows) - first_row(p, e), 0); }
-template <typename T>
-__device__ __forceinline__ T wave_total(T v) {
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o);
-  return v;
+// of lanes 0 .. lane: within rows of 16 lanes, then over the rows
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int from_lane(int v) {
+  return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, true);
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int64_t from_lane(int64_t v) {
+  const uint32_t lo = from_lane<CTRL, ROWS>((int)v), hi = from_lane<CTRL, ROWS>((int)(v >> 32));
+  return (int64_t)((uint64_t)hi << 32 | lo);
 }
 template <typename T>
-__device__ __forceinline__ T sum_upto(T v, int lane) {  // of lanes 0 .. lane
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const T y = __shfl_up(v, o);
-    if (lane >= o) v += y;
-  }
+__device__ __forceinline__ T sum_upto(T v) {
+  v += from_lane<0x111, 0xf>(v);
+  v += from_lane<0x112, 0xf>(v);
+  v += from_lane<0x114, 0xf>(v);
+  v += from_lane<0x118, 0xf>(v);
+  v += from_lane<0x142, 0xa>(v);
+  v += from_lane<0x143, 0xc>(v);
   return v;
+}
+__device__ __forceinline__ int of_lane(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
+__device__ __forceinline__ int64_t of_lane(int64_t v, int lane) {
+  return (int64_t)((uint64_t)(uint32_t)of_lane((int)(v >> 32), lane) << 32 | (uint32_t)of_lane((int)v, lane));
 }
 
 // What an expert's tiles are.  Its rows are cut into the fewest parts of at most MOST, all of nearly the same size.  cost: of a
@@ -127,39 +136,47 @@ struct TileList {
   int next, end, step;  // the workgroup's tiles: next, next + step, .. below end
   int whole, pieces;    // from `whole` on a tile counts as so many, of a part of its rows each
 };
+// lane i: of expert e0 + i (behind the last one: no tiles)
+template <int FORM, int MOST>
+__device__ __forceinline__ ExpertTiles lane_expert(const ExpertRowsParams &p, int e0, int n_cols, int m_tiles) {
+  const int e = e0 + (threadIdx.x & 63);
+  ExpertTiles t = expert_tiles<FORM, MOST>(e < p.n_experts ? row_count(p, e) : 0, n_cols, m_tiles);
+  if (e >= p.n_experts) t.n = 0;  // (kWeights has tiles for experts without rows)
+  return t;
+}
 template <int FORM, int MOST>
 __device__ __forceinline__ TileList deal_tiles(const ExpertRowsParams &p, int n_cols, int m_tiles) {
-  const int lane = threadIdx.x & 63, xcd = blockIdx.x & 7;
-  TileList r;
-  int64_t cost = 0;
-  for (int e = lane; e < p.n_experts; e += 64) {
-    const ExpertTiles t = expert_tiles<FORM, MOST>(row_count(p, e), n_cols, m_tiles);
-    cost += (int64_t)t.n * t.cost;
+  const int xcd = blockIdx.x & 7;
+  ExpertTiles t = lane_expert<FORM, MOST>(p, 0, n_cols, m_tiles);
+  int64_t upto = sum_upto((int64_t)t.n * t.cost), total = of_lane(upto, 63);  // the cost, up to the lane's expert and of all
+  for (int e0 = 64; e0 < p.n_experts; e0 += 64) {
+    const ExpertTiles more = lane_expert<FORM, MOST>(p, e0, n_cols, m_tiles);
+    total += of_lane(sum_upto((int64_t)more.n * more.cost), 63);
   }
-  cost = wave_total(cost);
-  const int64_t from = cost * xcd / 8, to = cost * (xcd + 1) / 8;
   int begin = -1, end = -1, tiles = 0;
   int64_t before = 0;
-  for (int e0 = 0; e0 < p.n_experts; e0 += 64) {
-    const int e = e0 + lane;
-    const ExpertTiles t = e < p.n_experts ? expert_tiles<FORM, MOST>(row_count(p, e), n_cols, m_tiles) : ExpertTiles{0, 0, 0, 1};
-    const int64_t own = (int64_t)t.n * t.cost, past = before + sum_upto(own, lane), first = past - own;
-    const int first_tile = tiles + sum_upto(t.n, lane) - t.n;
-    const int b = first <= from && from < past ? first_tile + (int)((from - first + t.cost - 1) / t.cost) : -1;
-    const int l = first <= to && to < past ? first_tile + (int)((to - first + t.cost - 1) / t.cost) : -1;
-    begin = max(begin, b);
-    end = max(end, l);
-    before = __shfl(past, 63);
-    tiles = __shfl(first_tile + t.n, 63);
+  for (int e0 = 0;;) {
+    const int past = tiles + sum_upto(t.n);
+    // the tile before which a share of the cost is spent, if one of these experts has it
+    const auto cut = [&](int64_t share, int &tile) MOE_ROWS_INLINE {
+      const uint64_t there = __ballot(share < upto);
+      if (share < before || there == 0) return;
+      const int l = __builtin_ctzll(there), cost = of_lane(t.cost, l), n = of_lane(t.n, l);
+      tile = of_lane(past, l) - n + (int)ceil((double)(share - (of_lane(upto, l) - (int64_t)n * cost)) / (double)cost);
+    };
+    cut(total * xcd / 8, begin);
+    cut(total * (xcd + 1) / 8, end);
+    tiles = of_lane(past, 63);
+    before = of_lane(upto, 63);
+    e0 += 64;
+    if (e0 >= p.n_experts) break;
+    t = lane_expert<FORM, MOST>(p, e0, n_cols, m_tiles);
+    upto = before + sum_upto((int64_t)t.n * t.cost);
   }
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    begin = max(begin, __shfl_xor(begin, o));
-    end = max(end, __shfl_xor(end, o));
-  }
-  r.step = gridDim.x / 8;
+  TileList r;
   begin = uniform(begin < 0 ? tiles : begin);
   r.end = uniform(end < 0 ? tiles : end);
+  r.step = gridDim.x / 8;
   r.next = begin + (blockIdx.x >> 3);
   r.whole = r.end;
   r.pieces = 1;
@@ -187,14 +204,14 @@ __device__ __forceinline__ Tile lane_tile(const ExpertRowsParams &p, const TileL
   for (int e0 = 0; e0 < p.n_experts; e0 += 64) {
     const int e = e0 + lane, row0 = e < p.n_experts ? first_row(p, e) : 0, count = e < p.n_experts ? row_count(p, e) : 0;
     const ExpertTiles t = e < p.n_experts ? expert_tiles<FORM, MOST>(count, n_cols, m_tiles) : ExpertTiles{0, 0, 0, 0};
-    const int past = before + sum_upto(t.n, lane);
+    const int past = before + sum_upto(t.n);
     // the first expert whose tiles end behind `want`
     int l = 0;
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) l += __shfl(past, l + o - 1) <= want ? o : 0;
     const int of = __shfl(t.parts, l), each = __shfl(t.each, l), rows = __shfl(count, l), from = __shfl(row0, l);
     const int left = want - __shfl(past - t.n, l);
-    const int all = __shfl(past, 63);
+    const int all = of_lane(past, 63);
     if (want >= before && want < all) {
       r.expert = e0 + l;
       if constexpr (FORM == kWeights) {
@@ -334,9 +351,10 @@ struct Product {
   int lane, wave, wm, wn, pitch;
   uint32_t row_bytes;
   int n_cols, m_both, m_tiles;  // tiles over the columns; kWeights: over 2 * pitch rows of gate and up gradients, then pitch of down
-  // The workgroup's tiles, 64 at a time: lane i of `list` has tile listed + i, of `list_after` listed + 64 + i.
+  // Of the workgroup's tiles: lane i has tile listed + i.  (Requests are at most as many tiles ahead as there are stages.)
+  static constexpr int LIST = 64 - 2 * kWeightStages;
   TileList deal;
-  Tile list, list_after;
+  Tile list;
   int listed;
   // What is requested next, of the rows and of the weights: the tile, how many of its stages are left, the place in the ring and
   // where the operand is; the lane's place in loads 0 and 1 (2 and 3 are a_more, b_more behind; side by side see b_xor)
@@ -363,24 +381,16 @@ struct Product {
     deal = deal_tiles<FORM, ROWS>(g.p, n_cols, m_tiles);
     listed = 0;
     list = lane_tile<FORM, ROWS>(g.p, deal, n_cols, m_tiles);
-    list_more();
     a_put = 0;
     b_put = WEIGHT_BASE;
     a_tile = b_tile = 0;
     open_rows();
     open_weights();
   }
-  __device__ __forceinline__ void list_more() {
-    deal.next += 64 * deal.step;
-    list_after = Tile{-1, 0, 0, 0};
-    if (deal.next < deal.end) list_after = lane_tile<FORM, ROWS>(g.p, deal, n_cols, m_tiles);
-  }
   // tile i of the workgroup, the same in every lane
   __device__ __forceinline__ Tile tile(int i) const {
-    const bool after = i - listed >= 64;
-    const int l = (i - listed) & 63;
-    const auto of = [&](int x, int y) MOE_ROWS_INLINE { return after ? __builtin_amdgcn_readlane(y, l) : __builtin_amdgcn_readlane(x, l); };
-    return Tile{of(list.expert, list_after.expert), of(list.row0, list_after.row0), of(list.rows, list_after.rows), of(list.col, list_after.col)};
+    const int l = i - listed;
+    return Tile{of_lane(list.expert, l), of_lane(list.row0, l), of_lane(list.rows, l), of_lane(list.col, l)};
   }
   // kWeights: the tile's rows of the gradient: first of the 3 * pitch, how many
   __device__ __forceinline__ int gradient_row(const Tile &t) const {
@@ -590,13 +600,6 @@ struct Product {
     for (int i = 0; t.expert >= 0;) {
       const int m0 = FORM == kWeights ? gradient_row(t) : 0;
       const int blocks = ((FORM == kWeights ? gradient_rows(m0) : t.rows) + 31) / 32;  // of 32 rows; a wavefront has half of each
-      ++i;
-      if (i - listed == 64) {
-        list = list_after;
-        listed += 64;
-        list_more();
-      }
-      const Tile next = tile(i);
       Acc acc[MB][NJ];
 #pragma unroll
       for (int m = 0; m < MB; ++m)
@@ -653,7 +656,12 @@ struct Product {
         if (m >= blocks) x[m] = read_x(x_at, rows_stage, false, m);
       store(t, m0, acc, blocks);
       stores = blocks * (FORM == kUp ? 1 : FORM == kColumns && INT8 ? NJ : FORM == kColumns || FORM == kWeights ? NJ / 2 : 0);
-      t = next;
+      if (++i - listed == LIST) {
+        listed += LIST;
+        deal.next += LIST * deal.step;
+        list = lane_tile<FORM, ROWS>(g.p, deal, n_cols, m_tiles);
+      }
+      t = tile(i);
     }
   }
 
