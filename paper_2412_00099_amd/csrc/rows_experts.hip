@@ -108,7 +108,8 @@ __device__ __forceinline__ int64_t of_lane(int64_t v, int lane) {
   return (int64_t)((uint64_t)(uint32_t)of_lane((int)(v >> 32), lane) << 32 | (uint32_t)of_lane((int)v, lane));
 }
 
-// What an expert's tiles are.  Its rows are cut into the fewest parts of at most MOST, all of nearly the same size.  cost: of a
+// What an expert's tiles are.  Its rows are cut into the fewest parts of at most MOST, all but the last of the same size,
+// which is whole blocks: they are computed whole.  cost: of a
 // tile, in rows; that the weights have to come in costs about as much as 128 rows do.  kWeights: the rows in
 // whole stages and 64 for the stores (16384 rows in 60 uneven experts: 590 us, with 212 for them 624, with unrounded rows and 384 634).
 struct ExpertTiles {
@@ -118,7 +119,7 @@ template <int FORM, int MOST>
 __device__ __forceinline__ ExpertTiles expert_tiles(int count, int n_cols, int m_tiles) {
   ExpertTiles t;
   t.parts = (count + MOST - 1) / MOST;
-  t.each = t.parts > 0 ? ((count + t.parts - 1) / t.parts + 15) / 16 * 16 : 0;
+  t.each = t.parts > 0 ? ((count + t.parts - 1) / t.parts + 31) / 32 * 32 : 0;
   t.n = FORM == kWeights ? m_tiles * n_cols : t.parts * n_cols;
   t.cost = FORM == kWeights ? (count + 63) / 64 * 64 + 64 : t.each + 128;
   return t;
