@@ -6,6 +6,7 @@ library (MoEError).
 """
 from __future__ import annotations
 
+from functools import lru_cache
 from typing import NamedTuple
 
 import torch
@@ -35,8 +36,10 @@ class KeptExperts(NamedTuple):
     gu: torch.Tensor
 
 
-_FLOATS = (torch.float32, torch.bfloat16)
-_empty = torch.empty
+_FLOATS = {torch.float32: B.MOE_R_FP32, torch.bfloat16: B.MOE_R_BF16}
+_empty, _empty_like = torch.empty, torch.empty_like
+# (the numbers themselves: making Stream and device objects of them takes longer than some of the kernels)
+_current_device, _stream_of = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
 
 
 def _ptr(t):
@@ -44,16 +47,19 @@ def _ptr(t):
 
 
 def _fmt(t, allowed):
-    if t.dtype not in allowed:
-        raise ValueError(f"{t.dtype} is not among {allowed}")
-    return _ROW_FMT[t.dtype]
+    fmt = allowed.get(t.dtype)
+    if fmt is None:
+        raise ValueError(f"{t.dtype} is not among {tuple(allowed)}")
+    return fmt
 
 
 def _rows(t, name):
-    """A matrix whose rows are dense (they may lie apart); returns its stride."""
-    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+    """(rows, columns, stride) of a matrix whose rows are dense (they may lie apart)."""
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 2 or (stride[1] != 1 and shape[1] > 1):
         raise ValueError(f"{name} has to be a matrix with dense rows")
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    n, d = shape
+    return n, d, stride[0] if n > 1 else d
 
 
 def _dense(t, shape, dtype, name):
@@ -61,51 +67,48 @@ def _dense(t, shape, dtype, name):
         raise ValueError(f"{name} has to be contiguous, {tuple(shape)}" + (f", {dtype}" if dtype else ""))
 
 
-class _Call:
-    """The GPU that all tensors are on, made current for the call, and its current stream."""
+def _on(t, *others):
+    """The GPU that all of the tensors are on."""
+    at = t.get_device()
+    if at < 0:
+        raise ValueError("the tensors have to be on a GPU")
+    for o in others:
+        if o is not None and o.get_device() != at:
+            raise ValueError("all tensors have to be on one GPU")
+    return at
 
-    __slots__ = ("at", "back")
 
-    def __init__(self, t, *others):
-        self.at = at = t.get_device()
-        if at < 0:
-            raise ValueError("the tensors have to be on a GPU")
-        for o in others:
-            if o is not None and o.get_device() != at:
-                raise ValueError("all tensors have to be on one GPU")
+def _elsewhere(at, f, *args, **kw):
+    """f with GPU `at` as the current one"""
+    with torch.cuda.device(at):
+        return f(*args, **kw)
 
-    def __enter__(self):
-        self.back = torch.cuda.current_device()
-        if self.back != self.at:
-            torch.cuda.set_device(self.at)
-        # (the number itself: making a Stream object of it takes longer than some of the kernels)
-        return torch._C._cuda_getCurrentRawStream(self.at)
 
-    def __exit__(self, *_):
-        if self.back != self.at:
-            torch.cuda.set_device(self.back)
+_backward_bytes = lru_cache(maxsize=256)(B.moe_norm_rows_backward_bytes)
+_sort_bytes = lru_cache(maxsize=256)(B.moe_sort_tokens_bytes)
 
 
 def norm_rows(h, y=None, gain=None, *, eps=1e-6, out=torch.bfloat16) -> NormedRows:
     """h + y and its root-mean-square norm times gain, as `out`: float32, bfloat16, or int8 codes with a scale per row."""
-    h_fmt, h_stride = _fmt(h, _FLOATS), _rows(h, "h")
-    n, d = h.shape
+    h_fmt, (n, d, h_stride) = _fmt(h, _FLOATS), _rows(h, "h")
     y_fmt, y_stride = h_fmt, d
     if y is not None:
-        y_fmt, y_stride = _fmt(y, _FLOATS), _rows(y, "y")
-        if y.shape != h.shape:
+        y_fmt, (yn, yd, y_stride) = _fmt(y, _FLOATS), _rows(y, "y")
+        if yn != n or yd != d:
             raise ValueError("y has to have the shape of h")
     _dense(gain, (d,), torch.float32, "gain")
-    if out not in _ROW_FMT:
+    x_fmt = _ROW_FMT.get(out)
+    if x_fmt is None:
         raise ValueError(f"{out} is not among {tuple(_ROW_FMT)}")
-    with _Call(h, y, gain) as s:
-        dev = h.device
-        h_out = h if y is None else _empty((n, d), dtype=h.dtype, device=dev)
-        x = _empty((n, d), dtype=out, device=dev)
-        rstd = _empty(n, dtype=torch.float32, device=dev)
-        scale = _empty(n, dtype=torch.float32, device=dev) if out is torch.int8 else None
-        B.moe_norm_rows(h.data_ptr(), h_fmt, h_stride, _ptr(y), y_fmt, y_stride, _ptr(gain), eps, n, d,
-                        None if y is None else h_out.data_ptr(), x.data_ptr(), _ROW_FMT[out], _ptr(scale), rstd.data_ptr(), s)
+    at = _on(h, y, gain)
+    if at != _current_device():
+        return _elsewhere(at, norm_rows, h, y, gain, eps=eps, out=out)
+    h_out = h if y is None else _empty_like(h) if h_stride == d else h.new_empty((n, d))
+    x = _empty((n, d), dtype=out, device=h.device)
+    rstd = _empty(n, dtype=torch.float32, device=h.device)
+    scale = _empty_like(rstd) if out is torch.int8 else None
+    B.moe_norm_rows(h.data_ptr(), h_fmt, h_stride, _ptr(y), y_fmt, y_stride, _ptr(gain), eps, n, d,
+                    None if y is None else h_out.data_ptr(), x.data_ptr(), x_fmt, _ptr(scale), rstd.data_ptr(), _stream_of(at))
     return NormedRows(h_out, x, scale, rstd)
 
 
@@ -119,13 +122,15 @@ def norm_rows_backward(h, gain, rstd, dx, dh=None):
     _dense(dh, (n, d), h.dtype, "dh")
     _dense(gain, (d,), torch.float32, "gain")
     _dense(rstd, (n,), torch.float32, "rstd")
-    with _Call(h, gain, rstd, dx, dh) as s:
-        out = _empty((n, d), dtype=h.dtype, device=h.device)
-        dgain = torch.empty_like(gain) if gain is not None else None
-        need = B.moe_norm_rows_backward_bytes(n, d) if gain is not None else 0
-        work = _empty(need, dtype=torch.uint8, device=h.device) if need else None
-        B.moe_norm_rows_backward(h.data_ptr(), h_fmt, _ptr(gain), rstd.data_ptr(), dx.data_ptr(), x_fmt, _ptr(dh), n, d,
-                                 out.data_ptr(), _ptr(dgain), _ptr(work), need, s)
+    at = _on(h, gain, rstd, dx, dh)
+    if at != _current_device():
+        return _elsewhere(at, norm_rows_backward, h, gain, rstd, dx, dh)
+    out = _empty_like(h)
+    dgain = _empty_like(gain) if gain is not None else None
+    need = _backward_bytes(n, d) if gain is not None else 0
+    work = _empty(need, dtype=torch.uint8, device=h.device) if need else None
+    B.moe_norm_rows_backward(h.data_ptr(), h_fmt, _ptr(gain), rstd.data_ptr(), dx.data_ptr(), x_fmt, _ptr(dh), n, d,
+                             out.data_ptr(), _ptr(dgain), _ptr(work), need, _stream_of(at))
     return out, dgain
 
 
@@ -135,14 +140,14 @@ def sort_tokens(ids, n_experts) -> TokenOrder:
         raise ValueError("ids has to be [tokens, top_k]")
     t, k = ids.shape
     _dense(ids, (t, k), torch.int32, "ids")
-    with _Call(ids) as s:
-        dev = ids.device
-        offsets = _empty(n_experts + 1, dtype=torch.int32, device=dev)
-        row_of, entry_of = _empty((t, k), dtype=torch.int32, device=dev), _empty(t * k, dtype=torch.int32, device=dev)
-        need = B.moe_sort_tokens_bytes(t, k, n_experts)
-        work = _empty(need, dtype=torch.uint8, device=dev) if need else None
-        B.moe_sort_tokens(ids.data_ptr(), t, k, n_experts, offsets.data_ptr(), row_of.data_ptr(), entry_of.data_ptr(), _ptr(work),
-                          need, s)
+    at = _on(ids)
+    if at != _current_device():
+        return _elsewhere(at, sort_tokens, ids, n_experts)
+    offsets, row_of, entry_of = ids.new_empty(n_experts + 1), _empty_like(ids), ids.new_empty(t * k)
+    need = _sort_bytes(t, k, n_experts)
+    work = _empty(need, dtype=torch.uint8, device=ids.device) if need else None
+    B.moe_sort_tokens(ids.data_ptr(), t, k, n_experts, offsets.data_ptr(), row_of.data_ptr(), entry_of.data_ptr(), _ptr(work), need,
+                      _stream_of(at))
     return TokenOrder(offsets, row_of, entry_of)
 
 
@@ -157,45 +162,55 @@ def _order(order):
 def gather_rows(x, order, scale=None):
     """(xs, its scales or None): the rows of x, and of scale if there is one, in the order of the experts."""
     t, k, e = _order(order)
-    fmt, stride = _fmt(x, _ROW_FMT), _rows(x, "x")
-    d = x.shape[1]
-    if x.shape[0] != t:
+    fmt, (n, d, stride) = _fmt(x, _ROW_FMT), _rows(x, "x")
+    if n != t:
         raise ValueError("x has to have a row for each token")
     _dense(scale, (t,), torch.float32, "scale")
-    with _Call(x, scale, order.row_of, order.offsets) as s:
-        xs = _empty((t * k, d), dtype=x.dtype, device=x.device)
-        xs_scale = _empty(t * k, dtype=torch.float32, device=x.device) if scale is not None else None
-        B.moe_gather_rows(x.data_ptr(), fmt, stride, _ptr(scale), order.row_of.data_ptr(), order.offsets.data_ptr(), t, k, e, d,
-                          xs.data_ptr(), _ptr(xs_scale), s)
+    at = _on(x, scale, order.row_of, order.offsets)
+    if at != _current_device():
+        return _elsewhere(at, gather_rows, x, order, scale)
+    xs = x.new_empty((t * k, d))
+    xs_scale = scale.new_empty(t * k) if scale is not None else None
+    B.moe_gather_rows(x.data_ptr(), fmt, stride, _ptr(scale), order.row_of.data_ptr(), order.offsets.data_ptr(), t, k, e, d,
+                      xs.data_ptr(), _ptr(xs_scale), _stream_of(at))
     return xs, xs_scale
 
 
 def combine_rows(ys, order, weight=None, base=None, out=None):
     """base + the weighted sum of each token's rows, as base's type (without base: `out`, or the type of ys)."""
     t, k, _ = _order(order)
-    d = ys.shape[1]
+    ys_fmt, d = _fmt(ys, _FLOATS), ys.shape[-1]
     _dense(ys, (t * k, d), None, "ys")
     _dense(weight, (t, k), torch.float32, "weight")
     _dense(base, (t, d), out, "base")
-    with _Call(ys, weight, base, order.row_of) as s:
-        y = _empty((t, d), dtype=base.dtype if base is not None else out or ys.dtype, device=ys.device)
-        B.moe_combine_rows(ys.data_ptr(), _fmt(ys, _FLOATS), order.row_of.data_ptr(), _ptr(weight), _ptr(base), t, k, d,
-                           y.data_ptr(), _fmt(y, _FLOATS), s)
+    at = _on(ys, weight, base, order.row_of)
+    if at != _current_device():
+        return _elsewhere(at, combine_rows, ys, order, weight, base, out)
+    if base is not None:
+        y = _empty_like(base)
+    elif out is None or out is ys.dtype:
+        y = ys.new_empty((t, d))
+    else:
+        y = _empty((t, d), dtype=out, device=ys.device)
+    B.moe_combine_rows(ys.data_ptr(), ys_fmt, order.row_of.data_ptr(), _ptr(weight), _ptr(base), t, k, d, y.data_ptr(),
+                       _fmt(y, _FLOATS), _stream_of(at))
     return y
 
 
 def combine_rows_backward(dy, ys, order, weight=None):
     """(gradient of ys, gradient of weight or None without one)"""
     t, k, e = _order(order)
-    d = dy.shape[1]
+    d = dy.shape[-1]
     _dense(dy, (t, d), None, "dy")
     _dense(ys, (t * k, d), None, "ys")
     _dense(weight, (t, k), torch.float32, "weight")
-    with _Call(dy, ys, weight, order.row_of, order.offsets) as s:
-        dys = torch.empty_like(ys)
-        dweight = torch.empty_like(weight) if weight is not None else None
-        B.moe_combine_rows_backward(dy.data_ptr(), _fmt(dy, _FLOATS), ys.data_ptr(), _fmt(ys, _FLOATS), order.row_of.data_ptr(),
-                                    order.offsets.data_ptr(), _ptr(weight), t, k, e, d, dys.data_ptr(), _ptr(dweight), s)
+    at = _on(dy, ys, weight, order.row_of, order.offsets)
+    if at != _current_device():
+        return _elsewhere(at, combine_rows_backward, dy, ys, order, weight)
+    dys = _empty_like(ys)
+    dweight = _empty_like(weight) if weight is not None else None
+    B.moe_combine_rows_backward(dy.data_ptr(), _fmt(dy, _FLOATS), ys.data_ptr(), _fmt(ys, _FLOATS), order.row_of.data_ptr(),
+                                order.offsets.data_ptr(), _ptr(weight), t, k, e, d, dys.data_ptr(), _ptr(dweight), _stream_of(at))
     return dys, dweight
 
 
@@ -216,13 +231,15 @@ def experts_rows(weight_fmt, blobs, inter, xs, offsets, *, scale=None, keep=Fals
     keep: returns (ys, KeptExperts) for the backward, else ys."""
     wfmt, e, stride, n, d = _experts(weight_fmt, blobs, xs, offsets)
     _dense(scale, (n,), torch.float32, "scale")
-    with _Call(xs, blobs, offsets, scale) as s:
-        dev, pitch = xs.device, (inter + 63) // 64 * 64
-        h = _empty((n, pitch), dtype=torch.bfloat16, device=dev)
-        gu = _empty((n, 2, pitch), dtype=torch.float32, device=dev) if keep else None
-        ys = _empty((n, d), dtype=torch.bfloat16, device=dev)
-        B.moe_experts_rows(wfmt, d, inter, e, blobs.data_ptr(), stride, xs.data_ptr(), _ptr(scale), offsets.data_ptr(), n,
-                           h.data_ptr(), _ptr(gu), ys.data_ptr(), s)
+    at = _on(xs, blobs, offsets, scale)
+    if at != _current_device():
+        return _elsewhere(at, experts_rows, weight_fmt, blobs, inter, xs, offsets, scale=scale, keep=keep)
+    dev, pitch = xs.device, (inter + 63) // 64 * 64
+    h = _empty((n, pitch), dtype=torch.bfloat16, device=dev)
+    gu = _empty((n, 2, pitch), dtype=torch.float32, device=dev) if keep else None
+    ys = _empty((n, d), dtype=torch.bfloat16, device=dev)
+    B.moe_experts_rows(wfmt, d, inter, e, blobs.data_ptr(), stride, xs.data_ptr(), _ptr(scale), offsets.data_ptr(), n,
+                       h.data_ptr(), _ptr(gu), ys.data_ptr(), _stream_of(at))
     return (ys, KeptExperts(h, gu)) if keep else ys
 
 
@@ -233,10 +250,12 @@ def experts_rows_backward(weight_fmt, blobs, inter, xs, offsets, kept, dys, *, r
     _dense(dys, (n, d), torch.bfloat16, "dys")
     _dense(kept.h, (n, pitch), torch.bfloat16, "kept.h")
     _dense(kept.gu, (n, 2, pitch), torch.float32, "kept.gu")
-    with _Call(xs, blobs, offsets, dys, kept.h, kept.gu) as s:
-        dgu = _empty((n, 2, pitch), dtype=torch.bfloat16, device=xs.device)
-        dxs = torch.empty_like(xs) if rows else None
-        dblobs = torch.empty_like(blobs) if weights else None
-        B.moe_experts_rows_backward(wfmt, d, inter, e, blobs.data_ptr(), stride, xs.data_ptr(), offsets.data_ptr(), n,
-                                    kept.h.data_ptr(), kept.gu.data_ptr(), dys.data_ptr(), dgu.data_ptr(), _ptr(dxs), _ptr(dblobs), s)
+    at = _on(xs, blobs, offsets, dys, kept.h, kept.gu)
+    if at != _current_device():
+        return _elsewhere(at, experts_rows_backward, weight_fmt, blobs, inter, xs, offsets, kept, dys, rows=rows, weights=weights)
+    dgu = _empty((n, 2, pitch), dtype=torch.bfloat16, device=xs.device)
+    dxs = _empty_like(xs) if rows else None
+    dblobs = _empty_like(blobs) if weights else None
+    B.moe_experts_rows_backward(wfmt, d, inter, e, blobs.data_ptr(), stride, xs.data_ptr(), offsets.data_ptr(), n, kept.h.data_ptr(),
+                                kept.gu.data_ptr(), dys.data_ptr(), dgu.data_ptr(), _ptr(dxs), _ptr(dblobs), _stream_of(at))
     return dxs, dblobs
