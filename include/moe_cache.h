@@ -325,8 +325,8 @@ int moe_cache_profile(moe_cache_t *ctx, int32_t enable, int32_t reset, double *a
  * The calls below need no context, allocate nothing and wait for nothing: they check their arguments (MOE_EINVAL), enqueue
  * their kernels on `stream` (whose device must be current) and return; all pointers are device memory.  They may be captured
  * into a graph.  Rows are dense (row i at i * hidden elements) where no stride is given; strides count elements.
- * hidden <= 8192, n_rows and n_tokens * top_k < 2^26, experts <= 512, top_k <= 8.  Elements are aligned to their type; rows
- * whose addresses and width allow 16-byte accesses are faster.  n_rows or n_tokens 0 is no error.
+ * hidden <= 8192, n_rows and n_tokens * top_k < 2^26, experts <= 512, top_k <= 8.  Elements are aligned to their type (the
+ * experts' rows to 16 bytes).  n_rows or n_tokens 0 is no error.
  * Sums and statistics are held in 32 bits; results are the same bit for bit from call to call.
  *
  * moe_norm_rows: h_out = h + y (rounded to h_fmt), x = h_out * rstd * gain, rstd = 1 / sqrt(mean(h_out^2) + eps).

@@ -88,10 +88,28 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, v);
 }
 
+// (16 bytes may begin at any element of their type: the same instructions)
+typedef uint32_t rows_u32x4_f32 __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t rows_u32x4_bf16 __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t rows_u32x4_codes __attribute__((ext_vector_type(4), aligned(1)));
+typedef uint32_t rows_u32x2_codes __attribute__((ext_vector_type(2), aligned(1)));
+
 template <bool ONCE, typename T>
 __device__ __forceinline__ T load_one(const T *p) {
   if constexpr (ONCE) return __builtin_nontemporal_load(p);
   else return *p;
+}
+// VEC columns from c on, of a row of d >= VEC: the last unit begins where it has VEC, and its first `skip` columns belong to the
+// unit before it.
+struct RowUnit {
+  int at, skip;
+};
+template <int VEC>
+__device__ __forceinline__ RowUnit row_unit(int c, int d) {
+  RowUnit u;
+  u.at = min(c, d - VEC);
+  u.skip = c - u.at;
+  return u;
 }
 // VEC elements of type FMT (VEC 8: 16-byte accesses; 1: one element).  ONCE: read by nobody else in the launch, so it need not
 // push anything out of the caches
@@ -103,15 +121,15 @@ __device__ __forceinline__ void load_row(const void *p, int64_t at, float (&v)[V
     else
       v[0] = __uint_as_float((uint32_t)load_one<ONCE>(static_cast<const uint16_t *>(p) + at) << 16);
   } else if constexpr (FMT == MOE_R_FP32) {
-    const rows_u32x4 *q = reinterpret_cast<const rows_u32x4 *>(static_cast<const float *>(p) + at);
-    const rows_u32x4 a = load_one<ONCE>(q), b = load_one<ONCE>(q + 1);
+    const rows_u32x4_f32 *q = reinterpret_cast<const rows_u32x4_f32 *>(static_cast<const float *>(p) + at);
+    const rows_u32x4_f32 a = load_one<ONCE>(q), b = load_one<ONCE>(q + 1);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       v[i] = __uint_as_float(a[i]);
       v[4 + i] = __uint_as_float(b[i]);
     }
   } else {
-    const rows_u32x4 a = load_one<ONCE>(reinterpret_cast<const rows_u32x4 *>(static_cast<const uint16_t *>(p) + at));
+    const rows_u32x4_bf16 a = load_one<ONCE>(reinterpret_cast<const rows_u32x4_bf16 *>(static_cast<const uint16_t *>(p) + at));
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       v[2 * i] = bf16_lo(a[i]);
@@ -133,14 +151,27 @@ __device__ __forceinline__ void store_row(void *p, int64_t at, const float (&v)[
       a[i] = __float_as_uint(v[i]);
       b[i] = __float_as_uint(v[4 + i]);
     }
-    rows_u32x4 *q = reinterpret_cast<rows_u32x4 *>(static_cast<float *>(p) + at);
+    rows_u32x4_f32 *q = reinterpret_cast<rows_u32x4_f32 *>(static_cast<float *>(p) + at);
     q[0] = a;
     q[1] = b;
   } else {
     rows_u32x4 a;
 #pragma unroll
     for (int i = 0; i < 4; ++i) a[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
-    *reinterpret_cast<rows_u32x4 *>(static_cast<uint16_t *>(p) + at) = a;
+    *reinterpret_cast<rows_u32x4_bf16 *>(static_cast<uint16_t *>(p) + at) = a;
+  }
+}
+// those of the unit that belong to it; at: of the row's first element
+template <int FMT, int VEC>
+__device__ __forceinline__ void store_unit(void *p, int64_t at, const RowUnit &u, const float (&v)[VEC]) {
+  if (u.skip == 0) {
+    store_row<FMT>(p, at + u.at, v);
+  } else {
+#pragma unroll
+    for (int i = 1; i < VEC; ++i) {
+      const float one[1] = {v[i]};
+      if (i >= u.skip) store_row<FMT>(p, at + u.at + i, one);
+    }
   }
 }
 // v as the type keeps it

@@ -10,7 +10,7 @@ namespace {
 
 constexpr int kSortWaves = 16, kSortThreads = kSortWaves * 64;
 constexpr int kSortBlocks = 256;      // workgroups of the two-launch form at most
-constexpr int kSortSingle = 4096;     // places that one workgroup sorts by itself (16384 take 25 us, in two launches 12)
+constexpr int kSortSingle = 4096;     // places that one workgroup sorts by itself (2044 take 4.8 us, in two launches 6.6; 4000 7.1 and 6.8; 8000 11.8 and 8.1; 16384 25 and 9)
 constexpr int kSortChunk = 1024;      // places a workgroup takes at least in the two-launch form: one for each thread
 
 // Lanes of the wavefront that hold the same key as this one.  BITS: bits of a key.
@@ -181,10 +181,12 @@ struct Places {
 __device__ __forceinline__ int64_t rows_used(const OrderParams &o) { return max(0, o.offsets[o.n_experts]); }
 
 // ---- rows into the order ----
-// V: the widest unit that rows, strides and addresses allow (16, 4, 2 or 1 bytes).  A wavefront takes a token: it reads the row
-// once and writes it to each of its places.
+// A wavefront takes a token: it reads the row once and writes it to each of its places.  V: 16 bytes wherever the row begins (the
+// last unit begins where it has 16 and writes again what the one before has written), or single bytes of a shorter row.  Memory
+// bounds it: 8191 rows of 2048 bf16 to eight places each 50 us (6.0 TB/s); 4096 rows of 2047 to four places 17.4 us by
+// elements of 2 bytes, 14.5 so.
 template <typename V>
-__global__ __launch_bounds__(256) void gather_kernel(const OrderParams o, const uint8_t *x, int64_t x_stride, int row_units, const float *scale,
+__global__ __launch_bounds__(256) void gather_kernel(const OrderParams o, const uint8_t *x, int64_t x_stride, int row_bytes, const float *scale,
                                                      uint8_t *xs, float *xs_scale) {
   const int lane = threadIdx.x & 63;
   const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -193,20 +195,19 @@ __global__ __launch_bounds__(256) void gather_kernel(const OrderParams o, const 
   int row[MOE_MAX_TOPK];
 #pragma unroll
   for (int k = 0; k < MOE_MAX_TOPK; ++k) row[k] = places.row(k);
-  const V *in = reinterpret_cast<const V *>(x + t * x_stride);
-  V *out = reinterpret_cast<V *>(xs);
-  constexpr int U = 4;  // units in flight per lane
-  for (int c = lane; c < row_units; c += 64 * U) {
+  const uint8_t *in = x + t * x_stride;
+  constexpr int U = 4, B = sizeof(V);  // units in flight per lane; bytes of one
+  for (int c = lane * B; c < row_bytes; c += 64 * B * U) {
     V v[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) v[u] = in[min(c + u * 64, row_units - 1)];
+    for (int u = 0; u < U; ++u) v[u] = *reinterpret_cast<const V *>(in + min(c + u * 64 * B, row_bytes - B));
 #pragma unroll
     for (int k = 0; k < MOE_MAX_TOPK; ++k) {
       if (row[k] < 0) continue;
-      V *to = out + (int64_t)row[k] * row_units + c;
+      uint8_t *to = xs + (int64_t)row[k] * row_bytes;
 #pragma unroll
       for (int u = 0; u < U; ++u)
-        if (c + u * 64 < row_units) to[u * 64] = v[u];
+        if (c + u * 64 * B < row_bytes) *reinterpret_cast<V *>(to + min(c + u * 64 * B, row_bytes - B)) = v[u];
     }
   }
   if (scale && lane < o.top_k) {
@@ -215,7 +216,7 @@ __global__ __launch_bounds__(256) void gather_kernel(const OrderParams o, const 
   // rows of nobody: as many as there are places without a row, one token's wavefront after the other
   const int64_t n = (int64_t)o.n_tokens * o.top_k;
   for (int64_t r = rows_used(o) + t; r < n; r += o.n_tokens) {
-    for (int c = lane; c < row_units; c += 64) out[r * row_units + c] = V{};
+    for (int c = lane * B; c < row_bytes; c += 64 * B) *reinterpret_cast<V *>(xs + r * row_bytes + min(c, row_bytes - B)) = V{};
     if (scale && lane == 0) xs_scale[r] = 0.f;
   }
 }
@@ -224,7 +225,7 @@ __global__ __launch_bounds__(256) void gather_kernel(const OrderParams o, const 
 // y = base + sum over k of weight * row, in the order of k.  KC: top_k rounded up to a power of two.  Places without a row read
 // one that is there (or nothing at all if there is none) and are left out by a selection, not by a weight of 0.  A wavefront takes
 // a token, CH units of a row at a time, so that it reads a row's bytes one after the other (8191 x 8 rows of 2048 bf16 onto fp32:
-// 117 us by single units, 110 so, 92 with loads that leave the caches alone: 4.4 TB/s).
+// 117 us by single units, 110 so, 92 with loads that leave the caches alone: 4.4 TB/s).  Memory bounds it.
 template <int YS, int Y, int VEC, int KC, int CH>
 __global__ __launch_bounds__(256) void combine_kernel(const OrderParams o, const void *ys, const float *weight, const void *base, void *y) {
   const int lane = threadIdx.x & 63;
@@ -242,13 +243,14 @@ __global__ __launch_bounds__(256) void combine_kernel(const OrderParams o, const
     if (row[k] >= 0) some = row[k];
   }
   for (int c = lane * VEC; c < d; c += 64 * VEC * CH) {
-    int at[CH];
+    // (units behind the last one load it again)
+    RowUnit unit[CH];
 #pragma unroll
-    for (int u = 0; u < CH; ++u) at[u] = min(c + u * 64 * VEC, d - VEC);
+    for (int u = 0; u < CH; ++u) unit[u] = row_unit<VEC>(c + u * 64 * VEC, d);
     float acc[CH][VEC], b[CH][VEC];
     if (base)
 #pragma unroll
-      for (int u = 0; u < CH; ++u) load_row<Y>(base, t * d + at[u], b[u]);
+      for (int u = 0; u < CH; ++u) load_row<Y>(base, t * d + unit[u].at, b[u]);
 #pragma unroll
     for (int u = 0; u < CH; ++u)
 #pragma unroll
@@ -260,7 +262,7 @@ __global__ __launch_bounds__(256) void combine_kernel(const OrderParams o, const
 #pragma unroll
         for (int u = 0; u < CH; ++u) {
           float v[VEC];
-          load_row<YS, VEC, true>(ys, from + at[u], v);
+          load_row<YS, VEC, true>(ys, from + unit[u].at, v);
 #pragma unroll
           for (int i = 0; i < VEC; ++i) acc[u][i] = row[k] >= 0 ? __builtin_fmaf(w[k], v[i], acc[u][i]) : acc[u][i];
         }
@@ -272,12 +274,13 @@ __global__ __launch_bounds__(256) void combine_kernel(const OrderParams o, const
       if (base)
 #pragma unroll
         for (int i = 0; i < VEC; ++i) acc[u][i] += b[u][i];
-      store_row<Y>(y, t * d + at[u], acc[u]);
+      store_unit<Y>(y, t * d, unit[u], acc[u]);
     }
   }
 }
 
-// dys[row] = weight * dy[token], dweight = <dy[token], ys[row]>
+// dys[row] = weight * dy[token], dweight = <dy[token], ys[row]>.  A wavefront takes a token, so that its row of dy is read once and
+// the dot products stay in registers.  Memory bounds it: 4096 x 4 rows of 2048 bf16, 151 MB in 29 us (5.2 TB/s).
 template <int DY, int YS, int VEC>
 __global__ __launch_bounds__(256) void combine_backward_kernel(const OrderParams o, const void *dy, const void *ys, const float *weight, void *dys,
                                                                float *dweight) {
@@ -295,21 +298,22 @@ __global__ __launch_bounds__(256) void combine_backward_kernel(const OrderParams
     dot[k] = 0.f;
   }
   for (int c = lane * VEC; c < d; c += 64 * VEC) {
+    const RowUnit u = row_unit<VEC>(c, d);
     float g[VEC];
-    load_row<DY>(dy, t * d + c, g);
+    load_row<DY>(dy, t * d + u.at, g);
 #pragma unroll
     for (int k = 0; k < MOE_MAX_TOPK; ++k) {
       if (row[k] < 0) continue;
-      const int64_t at = (int64_t)row[k] * d + c;
+      const int64_t at = (int64_t)row[k] * d;
       float v[VEC];
       if (dweight) {
-        load_row<YS, VEC, true>(ys, at, v);
+        load_row<YS, VEC, true>(ys, at + u.at, v);
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) dot[k] = __builtin_fmaf(g[i], v[i], dot[k]);
+        for (int i = 0; i < VEC; ++i) dot[k] = i >= u.skip ? __builtin_fmaf(g[i], v[i], dot[k]) : dot[k];
       }
 #pragma unroll
       for (int i = 0; i < VEC; ++i) v[i] = w[k] * g[i];
-      store_row<YS>(dys, at, v);
+      store_unit<YS>(dys, at, u, v);
     }
   }
   if (dweight) {
@@ -325,11 +329,9 @@ __global__ __launch_bounds__(256) void combine_backward_kernel(const OrderParams
     float zero[VEC];
 #pragma unroll
     for (int i = 0; i < VEC; ++i) zero[i] = 0.f;
-    for (int c = lane * VEC; c < d; c += 64 * VEC) store_row<YS>(dys, r * d + c, zero);
+    for (int c = lane * VEC; c < d; c += 64 * VEC) store_row<YS>(dys, r * d + row_unit<VEC>(c, d).at, zero);
   }
 }
-
-bool aligned(const void *p, int by) { return reinterpret_cast<uintptr_t>(p) % by == 0; }
 
 template <int N>
 struct Const {
@@ -371,20 +373,19 @@ hipError_t launch_gather_rows(const OrderParams &o, const void *x, int fmt, int6
   const dim3 grid((uint32_t)((o.n_tokens + 3) / 4)), block(256);
   const auto go = [&](auto v) {
     using V = decltype(v);
-    hipLaunchKernelGGL((gather_kernel<V>), grid, block, 0, s, o, static_cast<const uint8_t *>(x), stride, (int)(row / sizeof(V)), scale,
+    hipLaunchKernelGGL((gather_kernel<V>), grid, block, 0, s, o, static_cast<const uint8_t *>(x), stride, (int)row, scale,
                        static_cast<uint8_t *>(xs), xs_scale);
   };
-  const auto fits = [&](int by) { return row % by == 0 && stride % by == 0 && aligned(x, by) && aligned(xs, by); };
-  if (fits(16)) go(rows_u32x4{});
-  else if (fits(4)) go(uint32_t{});
-  else if (fits(2)) go(uint16_t{});
+  if (row >= 16) go(rows_u32x4_codes{});
   else go(uint8_t{});
   return hipGetLastError();
 }
 
 hipError_t launch_combine_rows(const OrderParams &o, const void *ys, int ys_fmt, const float *weight, const void *base, void *y, int y_fmt,
                                hipStream_t s) {
-  const bool wide = o.hidden % 8 == 0 && aligned(ys, 16) && aligned(y, 16) && (!base || aligned(base, 16));
+  // Units of 8 columns wherever a row begins, the last one over the one before it; rows of fewer by single columns.  4096 x 4 rows of
+  // 2047 bf16: 16 us, by single columns 64.
+  const bool wide = o.hidden >= 8;
   const dim3 grid((uint32_t)((o.n_tokens + 3) / 4)), block(256);
   const auto go = [&](auto YS, auto Y) {
     const auto with = [&](auto VEC, auto KC) {
@@ -392,6 +393,7 @@ hipError_t launch_combine_rows(const OrderParams &o, const void *ys, int ys_fmt,
         hipLaunchKernelGGL((combine_kernel<decltype(YS)::value, decltype(Y)::value, decltype(VEC)::value, decltype(KC)::value, decltype(CH)::value>),
                            grid, block, 0, s, o, ys, weight, base, y);
       };
+      // (4096 x 4 rows: of 2048 columns 13 us by four units, 17 by one; of 512 columns 4.4 by one, 6.4 by four)
       if (o.hidden <= 64 * decltype(VEC)::value * 2) go_on(Const<1>{});
       else go_on(Const<4>{});
     };
@@ -415,7 +417,7 @@ hipError_t launch_combine_rows(const OrderParams &o, const void *ys, int ys_fmt,
 
 hipError_t launch_combine_rows_backward(const OrderParams &o, const void *dy, int dy_fmt, const void *ys, int ys_fmt, const float *weight,
                                         void *dys, float *dweight, hipStream_t s) {
-  const bool wide = o.hidden % 8 == 0 && aligned(dy, 16) && (!ys || aligned(ys, 16)) && aligned(dys, 16);
+  const bool wide = o.hidden >= 8;  // (see above; 4096 x 4 rows of 2047 bf16: 31 us, by single columns 97)
   const dim3 grid((uint32_t)((o.n_tokens + 3) / 4)), block(256);
   const auto go = [&](auto DY, auto YS) {
     const auto with = [&](auto VEC) {
