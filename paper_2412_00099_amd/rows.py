@@ -37,6 +37,7 @@ class KeptExperts(NamedTuple):
 
 
 _FLOATS = {torch.float32: B.MOE_R_FP32, torch.bfloat16: B.MOE_R_BF16}
+# (sizes one by one: as a tuple they take a fifth longer)
 _empty, _empty_like = torch.empty, torch.empty_like
 # (the numbers themselves: making Stream and device objects of them takes longer than some of the kernels)
 _current_device, _stream_of = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
@@ -103,8 +104,8 @@ def norm_rows(h, y=None, gain=None, *, eps=1e-6, out=torch.bfloat16) -> NormedRo
     at = _on(h, y, gain)
     if at != _current_device():
         return _elsewhere(at, norm_rows, h, y, gain, eps=eps, out=out)
-    h_out = h if y is None else _empty_like(h) if h_stride == d else h.new_empty((n, d))
-    x = _empty((n, d), dtype=out, device=h.device)
+    h_out = h if y is None else _empty_like(h) if h_stride == d else h.new_empty(n, d)
+    x = _empty(n, d, dtype=out, device=h.device)
     rstd = _empty(n, dtype=torch.float32, device=h.device)
     scale = _empty_like(rstd) if out is torch.int8 else None
     B.moe_norm_rows(h.data_ptr(), h_fmt, h_stride, _ptr(y), y_fmt, y_stride, _ptr(gain), eps, n, d,
@@ -169,7 +170,7 @@ def gather_rows(x, order, scale=None):
     at = _on(x, scale, order.row_of, order.offsets)
     if at != _current_device():
         return _elsewhere(at, gather_rows, x, order, scale)
-    xs = x.new_empty((t * k, d))
+    xs = x.new_empty(t * k, d)
     xs_scale = scale.new_empty(t * k) if scale is not None else None
     B.moe_gather_rows(x.data_ptr(), fmt, stride, _ptr(scale), order.row_of.data_ptr(), order.offsets.data_ptr(), t, k, e, d,
                       xs.data_ptr(), _ptr(xs_scale), _stream_of(at))
@@ -189,9 +190,9 @@ def combine_rows(ys, order, weight=None, base=None, out=None):
     if base is not None:
         y = _empty_like(base)
     elif out is None or out is ys.dtype:
-        y = ys.new_empty((t, d))
+        y = ys.new_empty(t, d)
     else:
-        y = _empty((t, d), dtype=out, device=ys.device)
+        y = _empty(t, d, dtype=out, device=ys.device)
     B.moe_combine_rows(ys.data_ptr(), ys_fmt, order.row_of.data_ptr(), _ptr(weight), _ptr(base), t, k, d, y.data_ptr(),
                        _fmt(y, _FLOATS), _stream_of(at))
     return y
@@ -235,9 +236,9 @@ def experts_rows(weight_fmt, blobs, inter, xs, offsets, *, scale=None, keep=Fals
     if at != _current_device():
         return _elsewhere(at, experts_rows, weight_fmt, blobs, inter, xs, offsets, scale=scale, keep=keep)
     dev, pitch = xs.device, (inter + 63) // 64 * 64
-    h = _empty((n, pitch), dtype=torch.bfloat16, device=dev)
-    gu = _empty((n, 2, pitch), dtype=torch.float32, device=dev) if keep else None
-    ys = _empty((n, d), dtype=torch.bfloat16, device=dev)
+    h = _empty(n, pitch, dtype=torch.bfloat16, device=dev)
+    gu = _empty(n, 2, pitch, dtype=torch.float32, device=dev) if keep else None
+    ys = _empty(n, d, dtype=torch.bfloat16, device=dev)
     B.moe_experts_rows(wfmt, d, inter, e, blobs.data_ptr(), stride, xs.data_ptr(), _ptr(scale), offsets.data_ptr(), n,
                        h.data_ptr(), _ptr(gu), ys.data_ptr(), _stream_of(at))
     return (ys, KeptExperts(h, gu)) if keep else ys
@@ -253,7 +254,7 @@ def experts_rows_backward(weight_fmt, blobs, inter, xs, offsets, kept, dys, *, r
     at = _on(xs, blobs, offsets, dys, kept.h, kept.gu)
     if at != _current_device():
         return _elsewhere(at, experts_rows_backward, weight_fmt, blobs, inter, xs, offsets, kept, dys, rows=rows, weights=weights)
-    dgu = _empty((n, 2, pitch), dtype=torch.bfloat16, device=xs.device)
+    dgu = _empty(n, 2, pitch, dtype=torch.bfloat16, device=xs.device)
     dxs = _empty_like(xs) if rows else None
     dblobs = _empty_like(blobs) if weights else None
     B.moe_experts_rows_backward(wfmt, d, inter, e, blobs.data_ptr(), stride, xs.data_ptr(), offsets.data_ptr(), n, kept.h.data_ptr(),
