@@ -16,8 +16,9 @@
 // holds every code exactly.
 //
 // A workgroup of eight wavefronts has a compute unit to itself and walks over tiles of up to 256 x 256, a wavefront 128 x 64 of
-// it; where experts have few rows two workgroups share a compute unit and tiles are 64 x 128.  The summed index goes through LDS in stages of 64 (8-bit: 128) values, whole 128-byte lines, filled by loads that bypass
-// the registers: two stages of the rows' side, which other workgroups of the XCD read too, and three of the weights' side, which
+// it; where experts have fewer rows two workgroups share a compute unit and tiles are 128 x 128 or 64 x 128 (launch_product).  The
+// summed index goes through LDS in stages of 64 (8-bit: 128) values, whole 128-byte lines, filled by loads that bypass the
+// registers: two stages of the rows' side, which other workgroups of the XCD read too, and three of the weights' side, which
 // comes from memory.  A stage is two steps of the matrix cores; the fragments of the next step are read while they work on this
 // one's, and there is one barrier a stage.  Both rings run on from tile to tile.
 //
@@ -819,30 +820,40 @@ __global__ __launch_bounds__(kBlock, MB == 8 ? 2 : 4) void product_kernel(const 
   f.run();
 }
 
-// Tiles of 256 x 256 where they are as many as the compute units, which then have one workgroup each, and an expert has more than 96
-// rows on average; otherwise tiles of 64 rows and 128 columns, and two workgroups a compute unit.  Measured with 60 experts of
-// 2048 x 1408 and four a token, kUp + kColumns in us, small tiles against large ones: 16 tokens 122 and 161, 512 tokens 223 and
-// 253 (8 bits: 147 and 180), 1024 tokens (68 rows an expert) 273 and 318 (182 and 207), 1280 tokens 280 and 316, 2048 tokens (137
-// rows) 348 and 338 (235 and 242), 4096 tokens 578 and 458 (398 and 323).  Where large tiles are too few: 8 experts of 1024 x 704
-// and two a token, 512 tokens 26 and 55, 2048 tokens 46 and 59.
+// Which tiles, by the rows an expert has on average (the host knows no more).  Large: 256 x 256, one workgroup a compute unit.  Middle:
+// 128 x 128, two workgroups, so that one computes while the other waits for weights or stores.  Small: 64 x 128, two workgroups,
+// less work for rows that are not there.  Measured with 60 uneven experts of 2048 x 1408 and four a token, small | middle | large, us:
+//   tokens (rows an expert)     512 (34)          1024 (68)         2048 (137)        4096 (273)        8192 (546)
+//   kUp                         139 | 139 | 138   170 | 173 | 181   214 | 191 | 183   324 | 261 | 229   - | 478 | 381
+//   kColumns                    80 | 83 | 114     96 | 90 | 113     123 | 112 | 127   204 | 158 | 169   - | 300 | 272
+//   kUp, 8 bits                 76 | 82 | 78      87 | 87 | 87      113 | 104 | 105   169 | 138 | 131   - | 245 | 221
+//   kColumns, 8 bits            63 | 69 | 94      75 | 78 | 100     91 | 101 | 117    157 | 137 | 163   - | 271 | 282
+//   kDgu                                                                              215 | 188 | 189
+// Where tiles are too few for the compute units, smaller ones: 8 experts of 1024 x 704 and two a token, 512 tokens 23 | 26 | 34,
+// 2048 tokens 40 | 39 | 42.
 //
-// Columns of bytes: small tiles have 256 of them where tiles of 128 would be three or more for a compute unit.  In us against 128:
-// 16 tokens 38 and 45, 64 tokens 41 and 51, 512 tokens 62 and 68; where there are fewer tiles, 2 tokens 24 and 19, 8 experts and
-// 2048 tokens 26 and 23.
+// Columns of bytes: 256 of them a tile, but with small tiles only where tiles of 128 would be three or more for a compute unit.  In
+// us against 128: 16 tokens 38 and 45, 64 tokens 41 and 51, 512 tokens 62 and 68; where there are fewer tiles, 2 tokens 24 and 19, 8
+// experts and 2048 tokens 26 and 23.  Middle tiles, 4096 tokens: 136 and 144.
 template <int FORM, bool INT8>
 hipError_t launch_product(const ProductArgs &g, int n_cus, hipStream_t s) {
   const int grid = n_cus / 8 * 8;  // (the XCDs are eight)
   if constexpr (FORM != kWeights) {
-    // at most, from what the host knows
+    // upper bounds, from what the host knows
     const int64_t n_rows = g.p.n_rows, n_experts = g.p.n_experts, with_rows = n_rows < n_experts ? n_rows : n_experts;
     const int pitch = expert_rows_pitch(g.p.inter), wide = FORM == kUp ? 2 * pitch : FORM == kDgu ? pitch : g.p.hidden;
     const auto tiles = [&](int rows, int cols) { return (n_rows / rows + with_rows) * ((wide + cols - 1) / cols); };
-    if (tiles(256, 256) < grid || n_rows <= 96 * n_experts) {
-      constexpr bool BYTES = FORM == kColumns && INT8;
+    constexpr bool BYTES = FORM == kColumns && INT8;
+    constexpr int SMALL = BYTES ? 160 : 64, MIDDLE = BYTES ? 768 : FORM == kColumns ? 400 : 144;
+    if (n_rows <= SMALL * n_experts || tiles(128, 128) < grid) {
       if (BYTES && tiles(64, 128) >= 3 * grid)
         hipLaunchKernelGGL((product_kernel<FORM, INT8, BYTES ? 4 : 2, 2>), dim3(2 * grid), dim3(kBlock), 0, s, g);
       else
         hipLaunchKernelGGL((product_kernel<FORM, INT8, 2, 2>), dim3(2 * grid), dim3(kBlock), 0, s, g);
+      return hipGetLastError();
+    }
+    if (n_rows <= MIDDLE * n_experts || tiles(256, 256) < grid) {
+      hipLaunchKernelGGL((product_kernel<FORM, INT8, BYTES ? 4 : 2, 4>), dim3(2 * grid), dim3(kBlock), 0, s, g);
       return hipGetLastError();
     }
   }
