@@ -1,4 +1,5 @@
-"""Compile the HIP sources into paper_2412_00099_amd/libmoe_cache.so (gfx950 only, in-tree)."""
+"""Compile the HIP sources into paper_2412_00099_amd/libmoe_cache.so (gfx950 only, in-tree), and the tensors' part of the row
+operators (host code only) into _rows.so beside it."""
 from __future__ import annotations
 
 import os
@@ -9,6 +10,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libmoe_cache.so")
+TENSORS_OUT = os.path.join(HERE, "_rows.so")
 OBJ_DIR = os.path.join(HERE, "_build")
 
 COMMON = [
@@ -43,6 +45,25 @@ SOURCES = {
 }
 
 
+def _tensors_command(obj: str) -> list[str]:
+    """csrc/rows_torch.cpp to an object file"""
+    import importlib.util
+    import sysconfig
+
+    torch = os.path.dirname(importlib.util.find_spec("torch").origin)
+    return [os.environ.get("CXX", "g++"), "-c", os.path.join(CSRC, "rows_torch.cpp"), "-o", obj, "-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden",
+            "-Wall", "-DUSE_ROCM=1", "-D__HIP_PLATFORM_AMD__=1", "-I" + os.path.join(ROOT, "include"), "-isystem", os.path.join(torch, "include"),
+            "-isystem", "/opt/rocm/include", "-I" + sysconfig.get_paths()["include"]]
+
+
+def _tensors_link(obj: str) -> list[str]:
+    import importlib.util
+
+    libs = os.path.join(os.path.dirname(importlib.util.find_spec("torch").origin), "lib")
+    return [os.environ.get("CXX", "g++"), "-shared", "-o", TENSORS_OUT, obj, "-L" + HERE, "-l:libmoe_cache.so", "-L" + libs, "-ltorch_python", "-ltorch",
+            "-ltorch_cpu", "-lc10", "-lc10_hip", "-Wl,-rpath,$ORIGIN", "-Wl,-rpath," + libs]
+
+
 def build(verbose: bool = True) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     os.makedirs(OBJ_DIR, exist_ok=True)
@@ -55,6 +76,11 @@ def build(verbose: bool = True) -> str:
             print("[build]", " ".join(cmd), flush=True)
         procs.append((src, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
         objs.append(obj)
+    tensors_obj = os.path.join(OBJ_DIR, "rows_torch.cpp.o")
+    cmd = _tensors_command(tensors_obj)
+    if verbose:
+        print("[build]", " ".join(cmd), flush=True)
+    procs.append(("rows_torch.cpp", subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
     failed = False
     for src, p in procs:
         out, _ = p.communicate()
@@ -65,8 +91,12 @@ def build(verbose: bool = True) -> str:
             print(f"[build] {src} failed", file=sys.stderr)
             failed = True
     if failed:
-        raise RuntimeError("hipcc failed")
+        raise RuntimeError("a compiler failed")
     cmd = [hipcc, "-shared", "-fPIC", "--offload-arch=gfx950", "-o", OUT] + objs
+    if verbose:
+        print("[build]", " ".join(cmd), flush=True)
+    subprocess.check_call(cmd)
+    cmd = _tensors_link(tensors_obj)
     if verbose:
         print("[build]", " ".join(cmd), flush=True)
     subprocess.check_call(cmd)

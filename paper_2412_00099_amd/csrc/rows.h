@@ -94,6 +94,19 @@ typedef uint32_t rows_u32x4_bf16 __attribute__((ext_vector_type(4), aligned(2)))
 typedef uint32_t rows_u32x4_codes __attribute__((ext_vector_type(4), aligned(1)));
 typedef uint32_t rows_u32x2_codes __attribute__((ext_vector_type(2), aligned(1)));
 
+// ONCE: read by nobody else in the launch, so it need not push anything out of the caches
+template <bool ONCE>
+__device__ __forceinline__ rows_u32x4 load16(const float *p) {
+  const rows_u32x4_f32 *q = reinterpret_cast<const rows_u32x4_f32 *>(p);
+  if constexpr (ONCE) return __builtin_nontemporal_load(q);
+  else return *q;
+}
+template <bool ONCE>
+__device__ __forceinline__ rows_u32x4 load16(const uint16_t *p) {
+  const rows_u32x4_bf16 *q = reinterpret_cast<const rows_u32x4_bf16 *>(p);
+  if constexpr (ONCE) return __builtin_nontemporal_load(q);
+  else return *q;
+}
 template <bool ONCE, typename T>
 __device__ __forceinline__ T load_one(const T *p) {
   if constexpr (ONCE) return __builtin_nontemporal_load(p);
@@ -111,8 +124,7 @@ __device__ __forceinline__ RowUnit row_unit(int c, int d) {
   u.skip = c - u.at;
   return u;
 }
-// VEC elements of type FMT (VEC 8: 16-byte accesses; 1: one element).  ONCE: read by nobody else in the launch, so it need not
-// push anything out of the caches
+// VEC elements of type FMT (VEC 8: 16-byte accesses; 1: one element).
 template <int FMT, int VEC, bool ONCE = false>
 __device__ __forceinline__ void load_row(const void *p, int64_t at, float (&v)[VEC]) {
   if constexpr (VEC == 1) {
@@ -121,15 +133,14 @@ __device__ __forceinline__ void load_row(const void *p, int64_t at, float (&v)[V
     else
       v[0] = __uint_as_float((uint32_t)load_one<ONCE>(static_cast<const uint16_t *>(p) + at) << 16);
   } else if constexpr (FMT == MOE_R_FP32) {
-    const rows_u32x4_f32 *q = reinterpret_cast<const rows_u32x4_f32 *>(static_cast<const float *>(p) + at);
-    const rows_u32x4_f32 a = load_one<ONCE>(q), b = load_one<ONCE>(q + 1);
+    const rows_u32x4 a = load16<ONCE>(static_cast<const float *>(p) + at), b = load16<ONCE>(static_cast<const float *>(p) + at + 4);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       v[i] = __uint_as_float(a[i]);
       v[4 + i] = __uint_as_float(b[i]);
     }
   } else {
-    const rows_u32x4_bf16 a = load_one<ONCE>(reinterpret_cast<const rows_u32x4_bf16 *>(static_cast<const uint16_t *>(p) + at));
+    const rows_u32x4 a = load16<ONCE>(static_cast<const uint16_t *>(p) + at);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       v[2 * i] = bf16_lo(a[i]);
