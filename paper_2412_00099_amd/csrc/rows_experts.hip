@@ -808,7 +808,7 @@ struct Product {
 };
 
 template <int FORM, bool INT8, int NJ, int MB>
-__global__ __launch_bounds__(kBlock, MB == 8 ? 2 : 4) void product_kernel(const ProductArgs g) {
+__global__ __launch_bounds__(kBlock, MB == 8 ? 2 : FORM == kColumns && INT8 && MB == 2 ? 8 : 4) void product_kernel(const ProductArgs g) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds[Product<FORM, INT8, NJ, MB>::LDS_BYTES];
   if constexpr (FORM == kColumns) {  // rows of nobody
     const ExpertRowsParams &p = g.p;
@@ -827,14 +827,14 @@ __global__ __launch_bounds__(kBlock, MB == 8 ? 2 : 4) void product_kernel(const 
 //   kUp                         139 | 139 | 138   170 | 173 | 181   214 | 191 | 183   324 | 261 | 229   - | 478 | 381
 //   kColumns                    80 | 83 | 114     96 | 90 | 113     123 | 112 | 127   204 | 158 | 169   - | 300 | 272
 //   kUp, 8 bits                 76 | 82 | 78      87 | 87 | 87      113 | 104 | 105   169 | 138 | 131   - | 245 | 221
-//   kColumns, 8 bits            63 | 69 | 94      75 | 78 | 100     91 | 101 | 117    157 | 137 | 163   - | 271 | 282
+//   kColumns, 8 bits            60 | 69 | 94      65 | 78 | 100     100 | 101 | 117   157 | 137 | 163   - | 271 | 282
 //   kDgu                                                                              215 | 188 | 189
 // Where tiles are too few for the compute units, smaller ones: 8 experts of 1024 x 704 and two a token, 512 tokens 23 | 26 | 34,
 // 2048 tokens 40 | 39 | 42.
 //
-// Columns of bytes: 256 of them a tile, but with small tiles only where tiles of 128 would be three or more for a compute unit.  In
-// us against 128: 16 tokens 38 and 45, 64 tokens 41 and 51, 512 tokens 62 and 68; where there are fewer tiles, 2 tokens 24 and 19, 8
-// experts and 2048 tokens 26 and 23.  Middle tiles, 4096 tokens: 136 and 144.
+// Columns of bytes take half the LDS: four workgroups a compute unit with small tiles (two, or two of 64 x 256 | four: 16 tokens 45, 36 |
+// 33, 512 tokens 68, 61 | 60, 1024 tokens -, 74 | 65, 8 experts of 4096 x 4096 and 512 tokens -, 100 | 85; but 256 tokens 55, 43 | 48),
+// 256 columns a middle tile (4096 tokens 136, with 128 columns 144).
 template <int FORM, bool INT8>
 hipError_t launch_product(const ProductArgs &g, int n_cus, hipStream_t s) {
   const int grid = n_cus / 8 * 8;  // (the XCDs are eight)
@@ -844,12 +844,9 @@ hipError_t launch_product(const ProductArgs &g, int n_cus, hipStream_t s) {
     const int pitch = expert_rows_pitch(g.p.inter), wide = FORM == kUp ? 2 * pitch : FORM == kDgu ? pitch : g.p.hidden;
     const auto tiles = [&](int rows, int cols) { return (n_rows / rows + with_rows) * ((wide + cols - 1) / cols); };
     constexpr bool BYTES = FORM == kColumns && INT8;
-    constexpr int SMALL = BYTES ? 160 : 64, MIDDLE = BYTES ? 768 : FORM == kColumns ? 400 : 144;
+    constexpr int SMALL = BYTES ? 136 : 64, MIDDLE = BYTES ? 768 : FORM == kColumns ? 400 : 144;
     if (n_rows <= SMALL * n_experts || tiles(128, 128) < grid) {
-      if (BYTES && tiles(64, 128) >= 3 * grid)
-        hipLaunchKernelGGL((product_kernel<FORM, INT8, BYTES ? 4 : 2, 2>), dim3(2 * grid), dim3(kBlock), 0, s, g);
-      else
-        hipLaunchKernelGGL((product_kernel<FORM, INT8, 2, 2>), dim3(2 * grid), dim3(kBlock), 0, s, g);
+      hipLaunchKernelGGL((product_kernel<FORM, INT8, 2, 2>), dim3((BYTES ? 4 : 2) * grid), dim3(kBlock), 0, s, g);
       return hipGetLastError();
     }
     if (n_rows <= MIDDLE * n_experts || tiles(256, 256) < grid) {
