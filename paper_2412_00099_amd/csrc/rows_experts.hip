@@ -38,7 +38,6 @@ typedef __amdgpu_buffer_rsrc_t Buffer;
 #define LDS_PTR(T, p) ((__attribute__((address_space(3))) T *)(p))
 
 constexpr int kWavesWg = 8, kBlock = kWavesWg * 64;
-constexpr int kRowStages = 2, kWeightStages = 3;
 
 enum { kUp = 0, kDgu = 1, kColumns = 2, kWeights = 3 };
 
@@ -335,14 +334,15 @@ __device__ __forceinline__ float sigmoid(float g) { return __builtin_amdgcn_rcpf
 
 // ---- one tile ---------------------------------------------------------------------------------------------
 // NJ: fragments of 16 weight rows or columns a wavefront has.  MB: 32-row blocks of a tile at most.
-template <int FORM, bool INT8, int NJ, int MB>
+// RS, WS: stages of the rows' ring and of the weights'.
+template <int FORM, bool INT8, int NJ, int MB, int RS, int WS>
 struct Product {
   static constexpr int EL = INT8 ? 1 : 2;
   static constexpr int ROWS = MB * 32, COLS = NJ * 64, OF_WAVE = NJ * 16;  // of a tile; of a wavefront
   static constexpr int RECS = COLS / 2;                                   // kUp: records of a tile, each has two products
   static constexpr bool NARROW = FORM == kColumns && INT8;       // the weights' stage is of bytes: half as long
-  static constexpr uint32_t ROW_STAGE = ROWS * 128, WEIGHT_STAGE = COLS * (NARROW ? 64 : 128), WEIGHT_BASE = kRowStages * ROW_STAGE;
-  static constexpr uint32_t LDS_BYTES = WEIGHT_BASE + kWeightStages * WEIGHT_STAGE;
+  static constexpr uint32_t ROW_STAGE = ROWS * 128, WEIGHT_STAGE = COLS * (NARROW ? 64 : 128), WEIGHT_BASE = RS * ROW_STAGE;
+  static constexpr uint32_t LDS_BYTES = WEIGHT_BASE + WS * WEIGHT_STAGE;
   static constexpr int A_LOADS = MB / 2, B_LOADS = NARROW ? NJ / 2 : NJ;  // of a wavefront for a stage
   static constexpr bool FOURS = FORM == kDgu || (FORM == kUp && NJ == 4);  // side by side: fragments of 4 rows of each 8
   static constexpr int T_BYTES = NARROW ? COLS : COLS * 2, T_LANES = T_BYTES / 16, T_ROWS = 64 / T_LANES;  // transposed: a row, its lanes in a load, rows of a load
@@ -354,7 +354,7 @@ struct Product {
   uint32_t row_bytes;
   int n_cols, m_both, m_tiles;  // tiles over the columns; kWeights: over 2 * pitch rows of gate and up gradients, then pitch of down
   // Of the workgroup's tiles: lane i has tile listed + i.  (Requests are at most as many tiles ahead as there are stages.)
-  static constexpr int LIST = 64 - 2 * kWeightStages;
+  static constexpr int LIST = 64 - 2 * WS;
   TileList deal;
   Tile list;
   int listed;
@@ -532,7 +532,7 @@ struct Product {
 #pragma unroll
     for (int i = 0; i < B_LOADS; ++i) request_weights(i);
   }
-  static __device__ __forceinline__ uint32_t next_row_stage(uint32_t at) { return ROW_STAGE - at; }
+  static __device__ __forceinline__ uint32_t next_row_stage(uint32_t at) { return RS == 2 ? ROW_STAGE - at : at == WEIGHT_BASE - ROW_STAGE ? 0 : at + ROW_STAGE; }
   static __device__ __forceinline__ uint32_t next_weight_stage(uint32_t at) { return at == LDS_BYTES - WEIGHT_STAGE ? WEIGHT_BASE : at + WEIGHT_STAGE; }
 
   // Where the lane's fragments lie in a stage: of the weights for each j, of the rows for block 0; of the stage's first step.
@@ -588,12 +588,12 @@ struct Product {
     i32x4 x[MB], w0[NJ], w1[NJ];
     uint32_t w_at[NJ], x_at, rows_stage = 0, weights_stage = WEIGHT_BASE;  // the stages whose fragments are read
     fragment_offsets(w_at, x_at);
-    request_rows();
-    request_weights();
-    request_rows();
-    request_weights();
-    request_weights();
-    landed_but<A_LOADS + 2 * B_LOADS>();
+#pragma unroll
+    for (int i = 0; i < WS; ++i) {
+      if (i < RS) request_rows();
+      request_weights();
+    }
+    landed_but<(RS - 1) * A_LOADS + (WS - 1) * B_LOADS>();
 #pragma unroll
     for (int j = 0; j < NJ; ++j) w0[j] = read_w(w_at[j], weights_stage, false);
 #pragma unroll
@@ -638,11 +638,12 @@ struct Product {
       };
       for (int left = stages_of(t); left > 0; --left) {
         step(w0, w1, true);
-        // Everybody has read all of this stage: its places are free.  The next one has landed when no more than the weights of the
-        // one behind it are outstanding, and the stores of the tile before, which came behind those.
-        if (stores >= 24) landed_but<B_LOADS + 24>();
-        else if (stores >= 12) landed_but<B_LOADS + 12>();
-        else landed_but<B_LOADS>();
+        // Everybody has read all of this stage: its places are free.  The next one has landed when no more is outstanding than what
+        // was requested behind it, and the stores of the tile before, which came behind that.
+        constexpr int BEHIND = (WS > RS ? B_LOADS : 0) + (RS - 2) * (A_LOADS + B_LOADS);
+        if (stores >= 24) landed_but<BEHIND + 24>();
+        else if (stores >= 12) landed_but<BEHIND + 12>();
+        else landed_but<BEHIND>();
         stores = 0;
         if constexpr (FORM == kWeights) {
           request_rows();
@@ -807,16 +808,16 @@ struct Product {
   }
 };
 
-template <int FORM, bool INT8, int NJ, int MB>
-__global__ __launch_bounds__(kBlock, MB == 8 ? 2 : FORM == kColumns && INT8 && MB == 2 ? 8 : 4) void product_kernel(const ProductArgs g) {
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[Product<FORM, INT8, NJ, MB>::LDS_BYTES];
+template <int FORM, bool INT8, int NJ, int MB, int RS = 2, int WS = 3>
+__global__ __launch_bounds__(kBlock, MB == 8 || RS > 2 ? 2 : FORM == kColumns && INT8 && MB == 2 ? 8 : 4) void product_kernel(const ProductArgs g) {
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[Product<FORM, INT8, NJ, MB, RS, WS>::LDS_BYTES];
   if constexpr (FORM == kColumns) {  // rows of nobody
     const ExpertRowsParams &p = g.p;
     const int used = uniform(min(max(p.offsets[p.n_experts], 0), p.n_rows));
     for (int64_t r = used + blockIdx.x; r < p.n_rows; r += gridDim.x)
       for (int c = threadIdx.x * 8; c < p.hidden; c += kBlock * 8) *reinterpret_cast<rows_u32x4 *>(g.out + r * p.hidden + c) = rows_u32x4{};
   }
-  Product<FORM, INT8, NJ, MB> f(g, lds);
+  Product<FORM, INT8, NJ, MB, RS, WS> f(g, lds);
   f.run();
 }
 
@@ -832,6 +833,10 @@ __global__ __launch_bounds__(kBlock, MB == 8 ? 2 : FORM == kColumns && INT8 && M
 // Where tiles are too few for the compute units, smaller ones: 8 experts of 1024 x 704 and two a token, 512 tokens 23 | 26 | 34,
 // 2048 tokens 40 | 39 | 42.
 //
+// One small tile a compute unit at most, gate and up in bf16: nobody else keeps memory busy, so the rings have all of the LDS (60
+// experts of 2048 x 1408 and four a token, 1 token 12.7 us, otherwise 15.8; 2 tokens 17.5 and 20; rows of 4096, 8 experts of 512: 20 and
+// 26).  8-bit rows have half the stages (11 and 11), the records' stages do not wait for the ring (18 and 18): not there.
+//
 // Columns of bytes take half the LDS: four workgroups a compute unit with small tiles (two, or two of 64 x 256 | four: 16 tokens 45, 36 |
 // 33, 512 tokens 68, 61 | 60, 1024 tokens -, 74 | 65, 8 experts of 4096 x 4096 and 512 tokens -, 100 | 85; but 256 tokens 55, 43 | 48),
 // 256 columns a middle tile (4096 tokens 136, with 128 columns 144).
@@ -846,7 +851,11 @@ hipError_t launch_product(const ProductArgs &g, int n_cus, hipStream_t s) {
     constexpr bool BYTES = FORM == kColumns && INT8;
     constexpr int SMALL = BYTES ? 136 : 64, MIDDLE = BYTES ? 768 : FORM == kColumns ? 400 : 144;
     if (n_rows <= SMALL * n_experts || tiles(128, 128) < grid) {
-      hipLaunchKernelGGL((product_kernel<FORM, INT8, 2, 2>), dim3((BYTES ? 4 : 2) * grid), dim3(kBlock), 0, s, g);
+      constexpr bool DEEP = FORM == kUp && !INT8;
+      if (DEEP && tiles(64, 128) <= grid)
+        hipLaunchKernelGGL((product_kernel<FORM, INT8, 2, 2, DEEP ? 6 : 2, DEEP ? 6 : 3>), dim3(grid), dim3(kBlock), 0, s, g);
+      else
+        hipLaunchKernelGGL((product_kernel<FORM, INT8, 2, 2>), dim3((BYTES ? 4 : 2) * grid), dim3(kBlock), 0, s, g);
       return hipGetLastError();
     }
     if (n_rows <= MIDDLE * n_experts || tiles(256, 256) < grid) {
