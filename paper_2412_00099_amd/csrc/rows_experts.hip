@@ -59,9 +59,21 @@ __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirs
 __device__ __forceinline__ Buffer buffer_of(const void *base, uint32_t bytes) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(base), 0, (int)bytes, 0x00020000);
 }
-// 16 bytes per lane straight into LDS, lane after lane from `lds` (the same in every lane)
-__device__ __forceinline__ void to_lds(Buffer b, uint32_t off, uint32_t at, uint8_t *lds) {
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(b, LDS_PTR(void, lds), 16, off, at, 0, 0);
+// the same for to_lds, as the instruction takes it
+__device__ __forceinline__ i32x4 words_of(const void *base, uint32_t bytes) {
+  const uint64_t at = reinterpret_cast<uint64_t>(base);
+  return i32x4{(int)(uint32_t)at, (int)(uint32_t)(at >> 32 & 0xffff), (int)bytes, 0x00020000};
+}
+// 16 bytes per lane straight into LDS, lane after lane from `lds` (the same in every lane).  Written out, without results in
+// registers: the compiler, which would see that LDS is written, waits for all of them ahead of every transposed read of LDS
+// (16384 rows, 60 experts of 2048 x 1408: down 156, gradients of the rows 288, of the weights 600 us that way, 143, 270 and 526 so).  landed_but waits for them instead.
+__device__ __forceinline__ void to_lds(i32x4 b, uint32_t off, uint32_t at, uint8_t *lds) {
+  const uint32_t to = (uint32_t)reinterpret_cast<uintptr_t>(LDS_PTR(void, lds));
+  asm volatile(
+      "s_mov_b32 m0, %0\n\t"
+      "s_nop 3\n\t"  // (five states between a write of a scalar register by the vector unit and its use)
+      "buffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(to), "v"(off), "s"(b), "s"(at)
+      : "memory");  // (and m0, which is reserved: the compiler sets it ahead of each use of its own, of which there are none here)
 }
 // all but the last N loads of each wavefront of the workgroup have landed, and the reads of LDS that they have issued are done
 template <int N>
@@ -361,7 +373,7 @@ struct Product {
   // What is requested next, of the rows and of the weights: the tile, how many of its stages are left, the place in the ring and
   // where the operand is; the lane's place in loads 0 and 1 (2 and 3 are a_more, b_more behind; side by side see b_xor)
   static constexpr bool SIDE = FORM == kUp || FORM == kDgu;
-  Buffer a, b;
+  i32x4 a, b;  // resources
   int a_tile, b_tile, a_left, b_left;
   uint32_t a_put, b_put, a_at, b_at, a_more, b_more;
   uint32_t a_off[2], b_off[SIDE ? 1 : 2];
@@ -426,7 +438,7 @@ struct Product {
       }
     } else {
       const uint32_t a_bytes = FORM == kColumns ? (uint32_t)g.a_pitch * 2 : row_bytes;
-      a = buffer_of(g.a + (int64_t)t.row0 * a_bytes, any ? t.rows * a_bytes : 0);
+      a = words_of(g.a + (int64_t)t.row0 * a_bytes, any ? t.rows * a_bytes : 0);
       a_more = 16 * a_bytes;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
@@ -453,7 +465,7 @@ struct Product {
       }
     } else {
       const uint32_t rec_bytes = 3 * row_bytes;
-      b = buffer_of(g.p.blobs + (int64_t)max(t.expert, 0) * g.p.blob_stride, any ? (uint32_t)g.p.inter * rec_bytes : 0);
+      b = words_of(g.p.blobs + (int64_t)max(t.expert, 0) * g.p.blob_stride, any ? (uint32_t)g.p.inter * rec_bytes : 0);
       section_left = pitch / 64;
       if constexpr (SIDE) {
         // kUp: of a wavefront's rows of the image the first half are gate rows, the others the same records' up rows.  (A record
@@ -483,7 +495,7 @@ struct Product {
     uint8_t *at = lds + a_put + wave * (A_LOADS * 1024);
     if constexpr (FORM == kWeights) {
       const int n = max(min(64, a_rows_left), 0);
-      a = buffer_of(a_base, n > 0 ? n * a_row - a_skip : 0);
+      a = words_of(a_base, n > 0 ? n * a_row - a_skip : 0);
     }
     to_lds(a, a_off[i & 1], a_at + (i >> 1) * a_more, at + i * 1024);
     if (i + 1 < A_LOADS) return;
@@ -503,7 +515,7 @@ struct Product {
     uint8_t *at = lds + b_put + wave * (B_LOADS * 1024);
     if constexpr (FORM == kWeights) {
       const int n = max(min(64, b_rows_left), 0);
-      b = buffer_of(b_base, n > 0 ? n * row_bytes - b_skip : 0);
+      b = words_of(b_base, n > 0 ? n * row_bytes - b_skip : 0);
     }
     if constexpr (SIDE) to_lds(b, b_off[0] ^ (i * (FOURS ? 32 : 64)), b_at + i * b_more, at + i * 1024);
     else to_lds(b, b_off[i & 1], b_at + (i >> 1) * b_more, at + i * 1024);
