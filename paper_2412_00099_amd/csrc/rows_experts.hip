@@ -123,7 +123,7 @@ __device__ __forceinline__ int64_t of_lane(int64_t v, int lane) {
 // What an expert's tiles are.  Its rows are cut into the fewest parts of at most MOST, all but the last of the same size,
 // which is whole blocks: they are computed whole.  cost: of a
 // tile, in rows; that the weights have to come in costs about as much as 128 rows do.  kWeights: the rows in
-// whole stages and 64 for the stores (16384 rows in 60 uneven experts: 590 us, with 212 for them 624, with unrounded rows and 384 634).
+// whole stages and 128 for the stores (16384 rows in 60 uneven experts: 541 us, with 64 for them 569, with 16 559).
 struct ExpertTiles {
   int parts, each, n, cost;
 };
@@ -133,7 +133,7 @@ __device__ __forceinline__ ExpertTiles expert_tiles(int count, int n_cols, int m
   t.parts = (count + MOST - 1) / MOST;
   t.each = t.parts > 0 ? ((count + t.parts - 1) / t.parts + 31) / 32 * 32 : 0;
   t.n = FORM == kWeights ? m_tiles * n_cols : t.parts * n_cols;
-  t.cost = FORM == kWeights ? (count + 63) / 64 * 64 + 64 : t.each + 128;
+  t.cost = FORM == kWeights ? (count + 63) / 64 * 64 + 128 : t.each + 128;
   return t;
 }
 // Tiles in the order expert, column, row, so that the workgroups that share weights are neighbours.  The list is cut into eight
@@ -632,15 +632,14 @@ struct Product {
             for (int j = 0; j < NJ; ++j) acc[m][j] = mma(now[j], x[m], acc[m][j]);
             x[m] = read_x(x_at, rows_stage, second, m);
           }
-          // (load by load in between: all at once they would hold up the matrix cores; kWeights, whose tiles are short, is slower
-          // that way)
-          if (!second && FORM != kWeights) {
+          // (load by load in between: all at once they would hold up the matrix cores)
+          if (!second) {
             if (m < A_LOADS) request_rows(m);
             else if (m < A_LOADS + B_LOADS) request_weights(m - A_LOADS);
           }
           __builtin_amdgcn_sched_barrier(0);
         }
-        if (!second && FORM != kWeights) {
+        if (!second) {
 #pragma unroll
           for (int m = MB; m < A_LOADS + B_LOADS; ++m) {
             if (m < A_LOADS) request_rows(m);
@@ -657,10 +656,6 @@ struct Product {
         else if (stores >= 12) landed_but<BEHIND + 12>();
         else landed_but<BEHIND>();
         stores = 0;
-        if constexpr (FORM == kWeights) {
-          request_rows();
-          request_weights();
-        }
         rows_stage = next_row_stage(rows_stage);
         weights_stage = next_weight_stage(weights_stage);
         step(w1, w0, false);
@@ -836,18 +831,18 @@ __global__ __launch_bounds__(kBlock, MB == 8 || RS > 2 ? 2 : FORM == kColumns &&
 // Which tiles, by the rows an expert has on average (the host knows no more).  Large: 256 x 256, one workgroup a compute unit.  Middle:
 // 128 x 128, two workgroups, so that one computes while the other waits for weights or stores.  Small: 64 x 128, two workgroups,
 // less work for rows that are not there.  Measured with 60 uneven experts of 2048 x 1408 and four a token, small | middle | large, us:
-//   tokens (rows an expert)     512 (34)          1024 (68)         2048 (137)        4096 (273)        8192 (546)
-//   kUp                         139 | 139 | 138   170 | 173 | 181   214 | 191 | 183   324 | 261 | 229   - | 478 | 381
-//   kColumns                    80 | 83 | 114     96 | 90 | 113     123 | 112 | 127   204 | 158 | 169   - | 300 | 272
-//   kUp, 8 bits                 76 | 82 | 78      87 | 87 | 87      113 | 104 | 105   169 | 138 | 131   - | 245 | 221
-//   kColumns, 8 bits            60 | 69 | 94      65 | 78 | 100     100 | 101 | 117   157 | 137 | 163   - | 271 | 282
-//   kDgu                                                                              215 | 188 | 189
-// Where tiles are too few for the compute units, smaller ones: 8 experts of 1024 x 704 and two a token, 512 tokens 23 | 26 | 34,
-// 2048 tokens 40 | 39 | 42.
+//   tokens (rows an expert)   512 (34)        768 (51)          1024 (68)         1536 (102)        2048 (137)        4096 (273)
+//   kUp                       163 | 160 | 166 152 | 145 | 158   171 | 170 | 184   190 | 176 | 168   215 | 197 | 196   329 | 256 | 222
+//   kColumns                  77 | 80 | 84    88 | 85 | 84      88 | 90 | 86      103 | 99 | 93     111 | 108 | 99    174 | 141 | 135
+//   kUp, 8 bits               76 | 83 | 77    -                 88 | 91 | 87      102 | 97 | 95     114 | 105 | 103   173 | 139 | 128
+//   kColumns, 8 bits          55 | 60 | 73    -                 63 | 71 | 81      80 | 74 | 90      90 | 94 | 98      156 | 134 | 143
+//   kDgu                                                                                                              225 | 193 | 198
+// and with 8192 tokens kColumns, 8 bits, 322 | 258 | 229.  Where tiles are too few for the compute units, smaller ones: 8 experts of
+// 1024 x 704 and two a token, 2048 tokens 36 | 37 | 39; 16 of 2048 x 512 and two, 600 tokens 31 | 35 | 44.
 //
-// One small tile a compute unit at most, gate and up in bf16: nobody else keeps memory busy, so the rings have all of the LDS (60
-// experts of 2048 x 1408 and four a token, 1 token 12.7 us, otherwise 15.8; 2 tokens 17.5 and 20; rows of 4096, 8 experts of 512: 20 and
-// 26).  8-bit rows have half the stages (11 and 11), the records' stages do not wait for the ring (18 and 18): not there.
+// One small tile a compute unit at most, in bf16: nobody else keeps memory busy, so the rings have all of the LDS (kUp, 60 experts of
+// 2048 x 1408 and four a token, 1 token 12.7 us, otherwise 15.8; 2 tokens 17.5 and 20; kColumns, 1 token 11.2 and 12.1).  8-bit rows
+// have half the stages (11 and 11): not there.
 //
 // Columns of bytes take half the LDS: four workgroups a compute unit with small tiles (two, or two of 64 x 256 | four: 16 tokens 45, 36 |
 // 33, 512 tokens 68, 61 | 60, 1024 tokens -, 74 | 65, 8 experts of 4096 x 4096 and 512 tokens -, 100 | 85; but 256 tokens 55, 43 | 48),
@@ -861,9 +856,9 @@ hipError_t launch_product(const ProductArgs &g, int n_cus, hipStream_t s) {
     const int pitch = expert_rows_pitch(g.p.inter), wide = FORM == kUp ? 2 * pitch : FORM == kDgu ? pitch : g.p.hidden;
     const auto tiles = [&](int rows, int cols) { return (n_rows / rows + with_rows) * ((wide + cols - 1) / cols); };
     constexpr bool BYTES = FORM == kColumns && INT8;
-    constexpr int SMALL = BYTES ? 136 : 64, MIDDLE = BYTES ? 768 : FORM == kColumns ? 400 : 144;
+    constexpr int SMALL = BYTES ? 88 : 48, MIDDLE = BYTES ? 320 : FORM == kColumns ? SMALL : 84;
     if (n_rows <= SMALL * n_experts || tiles(128, 128) < grid) {
-      constexpr bool DEEP = FORM == kUp && !INT8;
+      constexpr bool DEEP = FORM != kDgu && !INT8;
       if (DEEP && tiles(64, 128) <= grid)
         hipLaunchKernelGGL((product_kernel<FORM, INT8, 2, 2, DEEP ? 6 : 2, DEEP ? 6 : 3>), dim3(grid), dim3(kBlock), 0, s, g);
       else
