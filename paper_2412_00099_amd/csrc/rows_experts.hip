@@ -120,10 +120,10 @@ __device__ __forceinline__ int64_t of_lane(int64_t v, int lane) {
   return (int64_t)((uint64_t)(uint32_t)of_lane((int)(v >> 32), lane) << 32 | (uint32_t)of_lane((int)v, lane));
 }
 
-// What an expert's tiles are.  Its rows are cut into the fewest parts of at most MOST, all but the last of the same size,
-// which is whole blocks: they are computed whole.  cost: of a
-// tile, in rows; that the weights have to come in costs about as much as 128 rows do.  kWeights: the rows in
-// whole stages and 128 for the stores (16384 rows in 60 uneven experts: 541 us, with 64 for them 569, with 16 559).
+// What an expert's tiles are.  Its rows are cut into the fewest parts of at most MOST, all but the last of the same size, which is
+// whole blocks: they are computed whole.  cost: of a tile, in rows; that the weights have to come in costs about as much as 128 rows
+// do.  kWeights: the rows in whole stages and 128 for the stores (16384 rows in 60 uneven experts: 541 us, with 64 for them 569,
+// with 16 559).
 struct ExpertTiles {
   int parts, each, n, cost;
 };
