@@ -22,6 +22,11 @@
 // comes from memory.  A stage is two steps of the matrix cores; the fragments of the next step are read while they work on this
 // one's, and there is one barrier a stage.  Both rings run on from tile to tile.
 //
+// Measured: 8192 rows on 8 experts of 4096 x 14336 in 8 bits, kUp 818 us (2.35 POP/s), kColumns 975 (0.99 PFLOP/s), bound by the matrix
+// cores; 16384 uneven rows on 60 experts of 2048 x 1408, kUp with its sums kept 257 us, kColumns 127 (down) and 235 (gradients of the
+// rows, 0.8 PFLOP/s), kDgu 187, kWeights 487, bound by workgroups that end early and, where much is stored, by stores; 8 rows on
+// 8 of them, 17 + 12 us, bound by what a compute unit keeps in flight (138 MB, 4.8 TB/s).
+//
 // Which expert and which of its rows a tile has is worked out from `offsets` on the device.  All loads go through buffer
 // resources that end where the expert's rows or records end: what lies beyond arrives as zeros.
 #include "rows.h"
