@@ -23,8 +23,8 @@
 // one's, and there is one barrier a stage.  Both rings run on from tile to tile.
 //
 // Measured: 8192 rows on 8 experts of 4096 x 14336 in 8 bits, kUp 818 us (2.35 POP/s), kColumns 975 (0.99 PFLOP/s), bound by the matrix
-// cores; 16384 uneven rows on 60 experts of 2048 x 1408, kUp with its sums kept 257 us, kColumns 127 (down) and 235 (gradients of the
-// rows, 0.8 PFLOP/s), kDgu 187, kWeights 487, bound by workgroups that end early and, where much is stored, by stores; 8 rows on
+// cores; 16384 uneven rows on 60 experts of 2048 x 1408, kUp with its sums kept 251 us, kColumns 126 (down) and 233 (gradients of the
+// rows, 0.8 PFLOP/s), kDgu 183, kWeights 445, bound by workgroups that end early and, where much is stored, by stores; 8 rows on
 // 8 of them, 17 + 12 us, bound by what a compute unit keeps in flight (138 MB, 4.8 TB/s).
 //
 // Which expert and which of its rows a tile has is worked out from `offsets` on the device.  All loads go through buffer
@@ -93,7 +93,8 @@ __device__ __forceinline__ f32x4 mma(i32x4 a, i32x4 b, f32x4 c) {
 __device__ __forceinline__ i32x4 mma(i32x4 a, i32x4 b, i32x4 c) { return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0); }
 
 // ---- tiles ------------------------------------------------------------------------------------------------
-// kWeights: row0, rows are the expert's, col = tile of the gradient's rows * n_cols + tile of its columns
+// kWeights: row0, rows are the expert's, col = tile of the gradient's columns * m_tiles + tile of its rows (the other way round 502 us
+// for 482)
 struct Tile {
   int expert;  // -1: no tile
   int row0, rows, col;
@@ -413,7 +414,7 @@ struct Product {
   }
   // kWeights: the tile's rows of the gradient: first of the 3 * pitch, how many
   __device__ __forceinline__ int gradient_row(const Tile &t) const {
-    const int m = t.col / n_cols;
+    const int m = t.col % m_tiles;
     return m < m_both ? m * 256 : 2 * pitch + (m - m_both) * 256;
   }
   __device__ __forceinline__ int gradient_rows(int first) const { return min(256, (first < 2 * pitch ? 2 : 3) * pitch - first); }
@@ -460,7 +461,7 @@ struct Product {
       const bool down = gradient_row(t) >= 2 * pitch;
       b_at = 0;
       b_rows_left = any ? t.rows : 0;
-      b_skip = t.col % n_cols * COLS * 2;
+      b_skip = t.col / m_tiles * COLS * 2;
       b_base = (down ? g.b2 : g.b) + (int64_t)t.row0 * row_bytes + b_skip;
       b_more = 4 * row_bytes;
 #pragma unroll
@@ -805,7 +806,7 @@ struct Product {
       }
     } else {
       const Buffer out = buffer_of(g.dblobs + t.expert * p.blob_stride, (uint32_t)tail);
-      const int m_rows = gradient_rows(m0), col0 = t.col % n_cols * COLS;
+      const int m_rows = gradient_rows(m0), col0 = t.col / m_tiles * COLS;
 #pragma unroll
       for (int m = 0; m < MB; ++m) {
         if (m > 0 && m >= blocks) break;
