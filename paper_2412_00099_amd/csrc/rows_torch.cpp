@@ -236,6 +236,9 @@ struct Shape {
 Shape shape_of(int fmt, const Tensor &blobs, int inter, const Tensor &xs, const Tensor &offsets) {
   if (offsets.dim() != 1 || offsets.size(0) < 2 || blobs.dim() < 1 || !blobs.is_contiguous() || blobs.size(0) != offsets.size(0) - 1)
     wrong("blobs has to be contiguous, one blob for each expert of offsets");
+  const at::ScalarType type = blobs.scalar_type();
+  if (type != at::kByte && type != at::kChar && !(type == at::kBFloat16 && fmt == MOE_W_BF16))
+    wrong(std::string("blobs: packed experts are bytes") + (fmt == MOE_W_BF16 ? " or bfloat16, not " : ", not ") + c10::toString(type));
   const int32_t e = size32(blobs.size(0));
   dense(offsets, {(int64_t)e + 1}, at::kInt, "offsets");
   if (xs.dim() != 2) wrong("xs has to be a matrix");

@@ -86,8 +86,8 @@ def _weight_fmt(weight_fmt):
 
 
 def experts_rows(weight_fmt, blobs, inter, xs, offsets, *, scale=None, keep=False):
-    """The SwiGLU experts on sorted rows.  blobs [n_experts, ...]: packed experts ('bf16' or 'int8'); offsets: a TokenOrder's.
-    keep: returns (ys, KeptExperts) for the backward, else ys."""
+    """The SwiGLU experts on sorted rows.  blobs [n_experts, ...]: packed experts ('bf16' or 'int8'), as bytes or bfloat16;
+    offsets: a TokenOrder's.  keep: returns (ys, KeptExperts) for the backward, else ys."""
     ys, h, gu = _rows.experts_rows(_weight_fmt(weight_fmt), blobs, inter, xs, offsets, scale, keep)
     return (ys, KeptExperts(h, gu)) if keep else ys
 
