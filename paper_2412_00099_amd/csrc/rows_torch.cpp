@@ -1,7 +1,8 @@
-// The row operators for tensors, the part that every call goes through: checks of shapes, types and places, the outputs from
+// The row operators for tensors, the part that every call goes through: checks of shapes, types, places and history, the outputs from
 // PyTorch's allocator, the current stream, the call of the C entry point.  In Python this took 10.5 us a call where the kernel takes 3 (a
 // norm of 37 rows), here 5.5.
 #include <ATen/ATen.h>
+#include <c10/core/GradMode.h>
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/utils/pybind.h>
@@ -71,6 +72,15 @@ float *to_floats(const Maybe &t) { return static_cast<float *>(to(t)); }
 int32_t *to_ints(const Tensor &t) { return static_cast<int32_t *>(t.mutable_data_ptr()); }
 Tensor fresh(const Tensor &like, at::IntArrayRef shape, at::ScalarType type) { return at::empty(shape, like.options().dtype(type)); }
 
+bool differentiable(const Tensor &t) { return t.requires_grad(); }
+bool differentiable(const Maybe &t) { return t && t->requires_grad(); }
+// The results have no history for automatic differentiation: a caller who would lose a gradient that way is told.
+template <typename... T>
+void no_history(const T &...t) {
+  if (c10::GradMode::is_enabled() && (differentiable(t) || ...))
+    wrong("an input requires a gradient, which this call does not record: call it under torch.no_grad(), or in a torch.autograd.Function with the backward calls");
+}
+
 // The GPU that all tensors are on, current for the call, and its current stream
 class Place {
  public:
@@ -101,6 +111,7 @@ class Place {
 };
 
 std::tuple<Tensor, Tensor, Maybe, Tensor> norm_rows(const Tensor &h, const Maybe &y, const Maybe &gain, double eps, int x_fmt) {
+  no_history(h, y, gain);
   const int h_fmt = format(h, "h");
   const Rows r = rows_of(h, "h");
   int y_fmt = h_fmt;
@@ -126,6 +137,7 @@ std::tuple<Tensor, Tensor, Maybe, Tensor> norm_rows(const Tensor &h, const Maybe
 }
 
 std::tuple<Tensor, Maybe> norm_rows_backward(const Tensor &h, const Maybe &gain, const Tensor &rstd, const Tensor &dx, const Maybe &dh) {
+  no_history(h, gain, rstd, dx, dh);
   const int h_fmt = format(h, "h"), x_fmt = format(dx, "dx");
   const Rows r = rows_of(h, "h");
   dense(h, {r.n, r.d}, {}, "h");
@@ -174,6 +186,7 @@ Order order_of(const Tensor &offsets, const Tensor &row_of) {
 }
 
 std::tuple<Tensor, Maybe> gather_rows(const Tensor &x, const Tensor &offsets, const Tensor &row_of, const Maybe &scale) {
+  no_history(x, scale);
   const Order o = order_of(offsets, row_of);
   const int fmt = format(x, "x", true);
   const Rows r = rows_of(x, "x");
@@ -193,6 +206,7 @@ std::tuple<Tensor, Maybe> gather_rows(const Tensor &x, const Tensor &offsets, co
 
 // y_fmt: of the result; -1: that of base, or of ys
 Tensor combine_rows(const Tensor &ys, const Tensor &offsets, const Tensor &row_of, const Maybe &weight, const Maybe &base, int y_fmt) {
+  no_history(ys, weight, base);
   const Order o = order_of(offsets, row_of);
   const int ys_fmt = format(ys, "ys"), base_fmt = base ? format(*base, "base") : ys_fmt;
   const int64_t n = (int64_t)o.t * o.k;
@@ -211,6 +225,7 @@ Tensor combine_rows(const Tensor &ys, const Tensor &offsets, const Tensor &row_o
 }
 
 std::tuple<Tensor, Maybe> combine_rows_backward(const Tensor &dy, const Tensor &ys, const Tensor &offsets, const Tensor &row_of, const Maybe &weight) {
+  no_history(dy, ys, weight);
   const Order o = order_of(offsets, row_of);
   const int dy_fmt = format(dy, "dy"), ys_fmt = format(ys, "ys");
   const int64_t n = (int64_t)o.t * o.k;
@@ -250,6 +265,7 @@ Shape shape_of(int fmt, const Tensor &blobs, int inter, const Tensor &xs, const 
 
 std::tuple<Tensor, Maybe, Maybe> experts_rows(int fmt, const Tensor &blobs, int inter, const Tensor &xs, const Tensor &offsets, const Maybe &scale,
                                               bool keep) {
+  no_history(blobs, xs, scale);
   const Shape s = shape_of(fmt, blobs, inter, xs, offsets);
   dense(scale, {s.n}, at::kFloat, "scale");
   const Place on(xs);
@@ -265,6 +281,7 @@ std::tuple<Tensor, Maybe, Maybe> experts_rows(int fmt, const Tensor &blobs, int 
 
 std::tuple<Maybe, Maybe> experts_rows_backward(int fmt, const Tensor &blobs, int inter, const Tensor &xs, const Tensor &offsets, const Tensor &h,
                                                const Tensor &gu, const Tensor &dys, bool rows, bool weights) {
+  no_history(blobs, xs, h, gu, dys);
   const Shape s = shape_of(fmt, blobs, inter, xs, offsets);
   dense(dys, {s.n, s.d}, at::kBFloat16, "dys");
   dense(h, {s.n, s.pitch}, at::kBFloat16, "kept.h");
