@@ -46,6 +46,10 @@ extern "C" {
 
 #define MOE_MAX_EXPERTS 64
 #define MOE_MAX_TOPK 8
+/* the operators on many rows: experts and width at most; rows, and tokens times top_k, fewer than */
+#define MOE_ROWS_MAX_EXPERTS 512
+#define MOE_ROWS_MAX_HIDDEN 8192
+#define MOE_ROWS_LIMIT (1 << 26)
 
 typedef struct moe_cache moe_cache_t; /* opaque, owned by the library */
 
@@ -325,8 +329,9 @@ int moe_cache_profile(moe_cache_t *ctx, int32_t enable, int32_t reset, double *a
  * The calls below need no context, allocate nothing and wait for nothing: they check their arguments (MOE_EINVAL), enqueue
  * their kernels on `stream` (whose device must be current) and return; all pointers are device memory.  They may be captured
  * into a graph.  Rows are dense (row i at i * hidden elements) where no stride is given; strides count elements.
- * hidden <= 8192, n_rows and n_tokens * top_k < 2^26, experts <= 512, top_k <= 8.  Elements are aligned to their type (the
- * experts' rows to 16 bytes).  n_rows or n_tokens 0 is no error.
+ * hidden <= MOE_ROWS_MAX_HIDDEN, n_rows and n_tokens * top_k < MOE_ROWS_LIMIT, experts <= MOE_ROWS_MAX_EXPERTS, top_k <=
+ * MOE_MAX_TOPK: other sizes are refused before a pointer is looked at.  Elements are aligned to their type (the experts' rows to 16
+ * bytes).  n_rows or n_tokens 0 is no error.
  * Sums and statistics are held in 32 bits; results are the same bit for bit from call to call.
  *
  * moe_norm_rows: h_out = h + y (rounded to h_fmt), x = h_out * rstd * gain, rstd = 1 / sqrt(mean(h_out^2) + eps).

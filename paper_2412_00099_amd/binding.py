@@ -14,6 +14,7 @@ lib = C.CDLL(LIB_PATH)
 
 MOE_MAX_EXPERTS = 64
 MOE_MAX_TOPK = 8
+MOE_ROWS_MAX_EXPERTS, MOE_ROWS_MAX_HIDDEN, MOE_ROWS_LIMIT = 512, 8192, 1 << 26
 MOE_OK, MOE_EINVAL, MOE_ENOMEM, MOE_EHIP, MOE_ESTATE = 0, -1, -2, -3, -4
 MOE_W_FP32, MOE_W_BF16, MOE_W_INT8_PC, MOE_W_INT4_G128 = 0, 1, 2, 3
 MOE_A_FP32, MOE_A_BF16 = 0, 1

@@ -5,8 +5,8 @@
 
 namespace moe {
 
-constexpr int kRowMaxExperts = 512;  // experts of a sort or of a launch over sorted rows
-constexpr int kRowMaxHidden = 8192;  // width of a row
+constexpr int kRowMaxExperts = MOE_ROWS_MAX_EXPERTS;  // of a sort or of a launch over sorted rows
+constexpr int kRowMaxHidden = MOE_ROWS_MAX_HIDDEN;    // width of a row
 
 // bytes of one element of a row (moe_row_fmt), 0: unknown
 __host__ __device__ constexpr int row_elem(int fmt) {

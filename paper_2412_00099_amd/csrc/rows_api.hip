@@ -7,7 +7,7 @@ using namespace moe;
 
 namespace {
 
-constexpr int64_t kMaxRows = 1 << 26;
+constexpr int64_t kMaxRows = MOE_ROWS_LIMIT;
 
 bool float_rows(int32_t f) { return f == MOE_R_FP32 || f == MOE_R_BF16; }
 bool off(const void *p, int by) { return reinterpret_cast<uintptr_t>(p) % by != 0; }

@@ -70,7 +70,12 @@ const int32_t *ints(const Tensor &t) { return static_cast<const int32_t *>(t.con
 void *to(const Maybe &t) { return t ? t->mutable_data_ptr() : nullptr; }
 float *to_floats(const Maybe &t) { return static_cast<float *>(to(t)); }
 int32_t *to_ints(const Tensor &t) { return static_cast<int32_t *>(t.mutable_data_ptr()); }
-Tensor fresh(const Tensor &like, at::IntArrayRef shape, at::ScalarType type) { return at::empty(shape, like.options().dtype(type)); }
+// within: what the library takes.  It refuses other sizes before it looks at a pointer, and nothing is allocated for them.
+Tensor fresh(const Tensor &like, at::IntArrayRef shape, at::ScalarType type, bool within) {
+  static constexpr int64_t nothing[] = {0};
+  return at::empty(within ? shape : at::IntArrayRef(nothing), like.options().dtype(type));
+}
+bool within(int64_t rows, int64_t hidden) { return rows < MOE_ROWS_LIMIT && hidden <= MOE_ROWS_MAX_HIDDEN; }
 
 bool differentiable(const Tensor &t) { return t.requires_grad(); }
 bool differentiable(const Maybe &t) { return t && t->requires_grad(); }
@@ -125,11 +130,12 @@ std::tuple<Tensor, Tensor, Maybe, Tensor> norm_rows(const Tensor &h, const Maybe
   dense(gain, {r.d}, at::kFloat, "gain");
   const Place on(h);
   on.has(y, gain);
-  const Tensor h_out = y ? fresh(h, {r.n, r.d}, h.scalar_type()) : h;
-  const Tensor x = fresh(h, {r.n, r.d}, x_fmt == MOE_R_FP32 ? at::kFloat : x_fmt == MOE_R_BF16 ? at::kBFloat16 : at::kChar);
-  const Tensor rstd = fresh(h, {r.n}, at::kFloat);
+  const bool ok = within(r.n, r.d);
+  const Tensor h_out = y ? fresh(h, {r.n, r.d}, h.scalar_type(), ok) : h;
+  const Tensor x = fresh(h, {r.n, r.d}, x_fmt == MOE_R_FP32 ? at::kFloat : x_fmt == MOE_R_BF16 ? at::kBFloat16 : at::kChar, ok);
+  const Tensor rstd = fresh(h, {r.n}, at::kFloat, ok);
   Maybe scale;
-  if (x_fmt == MOE_R_INT8) scale = fresh(h, {r.n}, at::kFloat);
+  if (x_fmt == MOE_R_INT8) scale = fresh(h, {r.n}, at::kFloat, ok);
   check(moe_norm_rows(h.const_data_ptr(), h_fmt, r.stride, at_(y), y_fmt, y_stride, floats(gain), (float)eps, r.n, r.d,
                       y ? h_out.mutable_data_ptr() : nullptr, x.mutable_data_ptr(), x_fmt, to_floats(scale), to_floats(rstd), on.stream()),
         "moe_norm_rows");
@@ -147,16 +153,22 @@ std::tuple<Tensor, Maybe> norm_rows_backward(const Tensor &h, const Maybe &gain,
   dense(rstd, {r.n}, at::kFloat, "rstd");
   const Place on(h);
   on.has(gain, rstd, dx, dh);
-  const Tensor out = fresh(h, {r.n, r.d}, h.scalar_type());
+  const bool ok = within(r.n, r.d);
+  const Tensor out = fresh(h, {r.n, r.d}, h.scalar_type(), ok);
   Maybe dgain, work;
   const size_t need = gain ? moe_norm_rows_backward_bytes(r.n, r.d) : 0;
-  if (gain) dgain = fresh(h, {r.d}, at::kFloat);
-  if (need) work = fresh(h, {(int64_t)need}, at::kByte);
+  if (gain) dgain = fresh(h, {r.d}, at::kFloat, ok);
+  if (need) work = fresh(h, {(int64_t)need}, at::kByte, ok);
   check(moe_norm_rows_backward(h.const_data_ptr(), h_fmt, floats(gain), floats(rstd), dx.const_data_ptr(), x_fmt, at_(dh), r.n, r.d,
                                out.mutable_data_ptr(), to_floats(dgain), to(work), need, on.stream()),
         "moe_norm_rows_backward");
   return {out, dgain};
 }
+
+struct Order {
+  int32_t t, k, e;
+  bool within(int64_t hidden) const { return k <= MOE_MAX_TOPK && e <= MOE_ROWS_MAX_EXPERTS && ::within((int64_t)t * k, hidden); }
+};
 
 std::tuple<Tensor, Tensor, Tensor> sort_tokens(const Tensor &ids, int n_experts) {
   if (ids.dim() != 2) wrong("ids has to be [tokens, top_k]");
@@ -164,19 +176,17 @@ std::tuple<Tensor, Tensor, Tensor> sort_tokens(const Tensor &ids, int n_experts)
   dense(ids, {t, k}, at::kInt, "ids");
   if (n_experts < 1) wrong("n_experts has to be 1 or more");
   const Place on(ids);
-  const Tensor offsets = fresh(ids, {(int64_t)n_experts + 1}, at::kInt), row_of = fresh(ids, {t, k}, at::kInt),
-               entry_of = fresh(ids, {(int64_t)t * k}, at::kInt);
+  const bool ok = Order{t, k, n_experts}.within(1);
+  const Tensor offsets = fresh(ids, {(int64_t)n_experts + 1}, at::kInt, ok), row_of = fresh(ids, {t, k}, at::kInt, ok),
+               entry_of = fresh(ids, {(int64_t)t * k}, at::kInt, ok);
   Maybe work;
   const size_t need = moe_sort_tokens_bytes(t, k, n_experts);
-  if (need) work = fresh(ids, {(int64_t)need}, at::kByte);
+  if (need) work = fresh(ids, {(int64_t)need}, at::kByte, ok);
   check(moe_sort_tokens(ints(ids), t, k, n_experts, to_ints(offsets), to_ints(row_of), to_ints(entry_of), to(work), need, on.stream()),
         "moe_sort_tokens");
   return {offsets, row_of, entry_of};
 }
 
-struct Order {
-  int32_t t, k, e;
-};
 Order order_of(const Tensor &offsets, const Tensor &row_of) {
   if (row_of.dim() != 2 || offsets.dim() != 1) wrong("row_of has to be [tokens, top_k], offsets [n_experts + 1]");
   const Order o{size32(row_of.size(0)), size32(row_of.size(1)), size32(offsets.size(0) - 1)};
@@ -195,9 +205,10 @@ std::tuple<Tensor, Maybe> gather_rows(const Tensor &x, const Tensor &offsets, co
   const Place on(x);
   on.has(scale, row_of, offsets);
   const int64_t n = (int64_t)o.t * o.k;
-  const Tensor xs = fresh(x, {n, r.d}, x.scalar_type());
+  const bool ok = o.within(r.d);
+  const Tensor xs = fresh(x, {n, r.d}, x.scalar_type(), ok);
   Maybe xs_scale;
-  if (scale) xs_scale = fresh(x, {n}, at::kFloat);
+  if (scale) xs_scale = fresh(x, {n}, at::kFloat, ok);
   check(moe_gather_rows(x.const_data_ptr(), fmt, r.stride, floats(scale), ints(row_of), ints(offsets), o.t, o.k, o.e, r.d, xs.mutable_data_ptr(),
                         to_floats(xs_scale), on.stream()),
         "moe_gather_rows");
@@ -218,7 +229,7 @@ Tensor combine_rows(const Tensor &ys, const Tensor &offsets, const Tensor &row_o
   dense(base, {o.t, d}, type, "base");
   const Place on(ys);
   on.has(weight, base, row_of);
-  const Tensor y = fresh(ys, {o.t, d}, type);
+  const Tensor y = fresh(ys, {o.t, d}, type, Order{o.t, o.k, 1}.within(d));
   check(moe_combine_rows(ys.const_data_ptr(), ys_fmt, ints(row_of), floats(weight), at_(base), o.t, o.k, d, y.mutable_data_ptr(), y_fmt, on.stream()),
         "moe_combine_rows");
   return y;
@@ -235,9 +246,10 @@ std::tuple<Tensor, Maybe> combine_rows_backward(const Tensor &dy, const Tensor &
   dense(weight, {o.t, o.k}, at::kFloat, "weight");
   const Place on(dy);
   on.has(ys, weight, row_of, offsets);
-  const Tensor dys = fresh(ys, {n, d}, ys.scalar_type());
+  const bool ok = o.within(d);
+  const Tensor dys = fresh(ys, {n, d}, ys.scalar_type(), ok);
   Maybe dweight;
-  if (weight) dweight = fresh(ys, {o.t, o.k}, at::kFloat);
+  if (weight) dweight = fresh(ys, {o.t, o.k}, at::kFloat, ok);
   check(moe_combine_rows_backward(dy.const_data_ptr(), dy_fmt, ys.const_data_ptr(), ys_fmt, ints(row_of), ints(offsets), floats(weight), o.t, o.k, o.e,
                                   d, dys.mutable_data_ptr(), to_floats(dweight), on.stream()),
         "moe_combine_rows_backward");
@@ -246,7 +258,9 @@ std::tuple<Tensor, Maybe> combine_rows_backward(const Tensor &dy, const Tensor &
 
 struct Shape {
   int32_t e, n, d, pitch;
-  int64_t blob;  // bytes
+  int64_t blob;  // bytes, at least `bytes` if ok
+  int64_t bytes;
+  bool ok;       // see fresh
 };
 Shape shape_of(int fmt, const Tensor &blobs, int inter, const Tensor &xs, const Tensor &offsets) {
   if (offsets.dim() != 1 || offsets.size(0) < 2 || blobs.dim() < 1 || !blobs.is_contiguous() || blobs.size(0) != offsets.size(0) - 1)
@@ -258,7 +272,9 @@ Shape shape_of(int fmt, const Tensor &blobs, int inter, const Tensor &xs, const 
   dense(offsets, {(int64_t)e + 1}, at::kInt, "offsets");
   if (xs.dim() != 2) wrong("xs has to be a matrix");
   if (inter < 0 || inter > INT_MAX - 64) wrong("bad inter");
-  const Shape s{e, size32(xs.size(0)), size32(xs.size(1)), (inter + 63) / 64 * 64, (int64_t)blobs.nbytes() / e};
+  Shape s{e, size32(xs.size(0)), size32(xs.size(1)), (inter + 63) / 64 * 64, (int64_t)blobs.nbytes() / e, 0, false};
+  s.bytes = (int64_t)moe_blob_bytes(fmt, s.d, inter);
+  s.ok = s.bytes > 0 && s.bytes <= s.blob && e <= MOE_ROWS_MAX_EXPERTS && within(s.n, s.d);
   dense(xs, {s.n, s.d}, fmt == MOE_W_INT8_PC ? at::kChar : at::kBFloat16, "xs");
   return s;
 }
@@ -270,9 +286,9 @@ std::tuple<Tensor, Maybe, Maybe> experts_rows(int fmt, const Tensor &blobs, int 
   dense(scale, {s.n}, at::kFloat, "scale");
   const Place on(xs);
   on.has(blobs, offsets, scale);
-  const Tensor h = fresh(xs, {s.n, s.pitch}, at::kBFloat16), ys = fresh(xs, {s.n, s.d}, at::kBFloat16);
+  const Tensor h = fresh(xs, {s.n, s.pitch}, at::kBFloat16, s.ok), ys = fresh(xs, {s.n, s.d}, at::kBFloat16, s.ok);
   Maybe gu;
-  if (keep) gu = fresh(xs, {s.n, 2, s.pitch}, at::kFloat);
+  if (keep) gu = fresh(xs, {s.n, 2, s.pitch}, at::kFloat, s.ok);
   check(moe_experts_rows(fmt, s.d, inter, s.e, blobs.const_data_ptr(), s.blob, xs.const_data_ptr(), floats(scale), ints(offsets), s.n,
                          h.mutable_data_ptr(), to_floats(gu), ys.mutable_data_ptr(), on.stream()),
         "moe_experts_rows");
@@ -288,10 +304,10 @@ std::tuple<Maybe, Maybe> experts_rows_backward(int fmt, const Tensor &blobs, int
   dense(gu, {s.n, 2, s.pitch}, at::kFloat, "kept.gu");
   const Place on(xs);
   on.has(blobs, offsets, dys, h, gu);
-  const Tensor dgu = fresh(xs, {s.n, 2, s.pitch}, at::kBFloat16);
+  const Tensor dgu = fresh(xs, {s.n, 2, s.pitch}, at::kBFloat16, s.ok);
   Maybe dxs, dblobs;
-  if (rows) dxs = fresh(xs, {s.n, s.d}, xs.scalar_type());
-  if (weights) dblobs = fresh(blobs, blobs.sizes(), blobs.scalar_type());
+  if (rows) dxs = fresh(xs, {s.n, s.d}, xs.scalar_type(), s.ok);
+  if (weights) dblobs = fresh(blobs, blobs.sizes(), blobs.scalar_type(), s.ok);
   check(moe_experts_rows_backward(fmt, s.d, inter, s.e, blobs.const_data_ptr(), s.blob, xs.const_data_ptr(), ints(offsets), s.n, h.const_data_ptr(),
                                   floats(gu), dys.const_data_ptr(), dgu.mutable_data_ptr(), to(dxs), to(dblobs), on.stream()),
         "moe_experts_rows_backward");
