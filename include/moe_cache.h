@@ -390,8 +390,8 @@ int moe_combine_rows_backward(const void *dy_dev, int32_t dy_fmt, const void *ys
  * them.  gu_dev: fp32 [n_rows, 2, pitch]: g and u, for the backward, or NULL.  Both 16-byte aligned; the caller keeps them for the
  * backward or throws them away.
  * moe_experts_rows_backward (MOE_W_BF16): from dys the gradients of xs and, in the layout of the blobs, of the weights (zeros
- * for an expert without rows).  h_dev, gu_dev: as the forward left them; dgu_dev: workspace, bf16 [n_rows, 2, pitch], 16-byte
- * aligned.  dxs_dev or dblobs_dev NULL: not wanted.  Rows of nobody: dxs is zero. */
+ * for an expert without rows; what lies between blobs is left as it is).  h_dev, gu_dev: as the forward left them; dgu_dev:
+ * workspace, bf16 [n_rows, 2, pitch], 16-byte aligned.  dxs_dev or dblobs_dev NULL: not wanted.  Rows of nobody: dxs is zero. */
 int moe_experts_rows(int32_t weight_fmt, int32_t hidden, int32_t inter, int32_t n_experts, const void *blobs_dev, int64_t blob_stride,
                      const void *xs_dev, const float *scale_dev, const int32_t *offsets_dev, int32_t n_rows, void *h_dev, float *gu_dev,
                      void *ys_dev, void *stream);

@@ -311,6 +311,8 @@ std::tuple<Maybe, Maybe> experts_rows_backward(int fmt, const Tensor &blobs, int
   check(moe_experts_rows_backward(fmt, s.d, inter, s.e, blobs.const_data_ptr(), s.blob, xs.const_data_ptr(), ints(offsets), s.n, h.const_data_ptr(),
                                   floats(gu), dys.const_data_ptr(), dgu.mutable_data_ptr(), to(dxs), to(dblobs), on.stream()),
         "moe_experts_rows_backward");
+  // what lies between blobs has no gradient, and the library leaves it alone
+  if (weights && s.blob > s.bytes) dblobs->view({s.e, -1}).view(at::kByte).slice(1, s.bytes).zero_();
   return {dxs, dblobs};
 }
 

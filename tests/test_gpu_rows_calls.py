@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from test_gpu_rows import BF16, DEV
+from test_gpu_rows import BF16, DEV, gen, make_blobs, normal, offsets_of
 
 pytestmark = pytest.mark.gpu
 
@@ -25,3 +25,24 @@ def test_sizes_are_refused_before_memory_is_taken(lib, what):
     with pytest.raises(lib.MoEError):
         call()
     assert torch.cuda.max_memory_allocated() - before < 1 << 16
+
+
+@pytest.mark.parametrize("dtype", [torch.uint8, BF16])
+def test_what_lies_between_blobs_has_no_gradient(lib, dtype):
+    """Blobs may lie further apart than they are long; what the caching allocator hands out for the gradients is not zero."""
+    g = gen(1)
+    hidden, inter, counts = 1024, 200, [5, 0, 40]
+    packed, _ = make_blobs(lib, g, "bf16", 3, hidden, inter)
+    n = packed.shape[1]
+    blobs = torch.full((3, n + 512), 7, dtype=torch.uint8, device=DEV)
+    blobs[:, :n] = packed
+    xs, dys = normal(g, 45, hidden, dtype=BF16), normal(g, 45, hidden, dtype=BF16)
+    ys, kept = lib.experts_rows("bf16", blobs, inter, xs, offsets_of(counts), keep=True)
+    _, want = lib.experts_rows_backward("bf16", packed, inter, xs, offsets_of(counts), kept, dys, rows=False)
+    full = [torch.full_like(blobs, 0xff) for _ in range(3)]
+    torch.cuda.synchronize()
+    del full
+    _, got = lib.experts_rows_backward("bf16", blobs.view(dtype), inter, xs, offsets_of(counts), kept, dys, rows=False)
+    assert got.dtype == dtype
+    got = got.view(torch.uint8)
+    assert torch.equal(got[:, :n], want) and not got[:, n:].any()
