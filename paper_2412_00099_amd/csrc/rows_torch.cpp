@@ -142,17 +142,18 @@ std::tuple<Tensor, Tensor, Maybe, Tensor> norm_rows(const Tensor &h, const Maybe
   return {h_out, x, scale, rstd};
 }
 
-std::tuple<Tensor, Maybe> norm_rows_backward(const Tensor &h, const Maybe &gain, const Tensor &rstd, const Tensor &dx, const Maybe &dh) {
-  no_history(h, gain, rstd, dx, dh);
-  const int h_fmt = format(h, "h"), x_fmt = format(dx, "dx");
-  const Rows r = rows_of(h, "h");
-  dense(h, {r.n, r.d}, {}, "h");
+std::tuple<Tensor, Maybe> norm_rows_backward(const Tensor &rows, const Maybe &gain, const Tensor &rstd, const Tensor &dx, const Maybe &dh) {
+  no_history(rows, gain, rstd, dx, dh);
+  const int h_fmt = format(rows, "h"), x_fmt = format(dx, "dx");
+  const Rows r = rows_of(rows, "h");
   dense(dx, {r.n, r.d}, {}, "dx");
-  dense(dh, {r.n, r.d}, h.scalar_type(), "dh");
+  dense(dh, {r.n, r.d}, rows.scalar_type(), "dh");
   dense(gain, {r.d}, at::kFloat, "gain");
   dense(rstd, {r.n}, at::kFloat, "rstd");
-  const Place on(h);
+  const Place on(rows);
   on.has(gain, rstd, dx, dh);
+  // (without y norm_rows hands back the rows that it was given, which may lie apart; the library takes dense ones)
+  const Tensor h = rows.contiguous();
   const bool ok = within(r.n, r.d);
   const Tensor out = fresh(h, {r.n, r.d}, h.scalar_type(), ok);
   Maybe dgain, work;

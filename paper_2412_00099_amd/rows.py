@@ -24,7 +24,7 @@ _ROW_FMT = {torch.float32: B.MOE_R_FP32, torch.bfloat16: B.MOE_R_BF16, torch.int
 
 
 class NormedRows(NamedTuple):
-    h: torch.Tensor             # the residual stream after the addition
+    h: torch.Tensor             # the residual stream after the addition; without y the tensor that was given, not a copy
     x: torch.Tensor             # its norm, or 8-bit codes
     scale: torch.Tensor | None  # of 8-bit codes: one per row
     rstd: torch.Tensor          # 1 / sqrt(mean h^2 + eps) of each row, for the backward
@@ -57,7 +57,7 @@ def norm_rows(h, y=None, gain=None, *, eps=1e-6, out=torch.bfloat16) -> NormedRo
 
 def norm_rows_backward(h, gain, rstd, dx, dh=None):
     """(gradient of the rows that were added, gradient of gain or None without one).  h, rstd: norm_rows' results; dx: gradient of
-    x; dh: gradient of the sum itself."""
+    x; dh: gradient of the sum itself.  (Without y, h is the caller's own tensor and has to hold the same values still.)"""
     return _rows.norm_rows_backward(h, gain, rstd, dx, dh)
 
 

@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from test_gpu_rows import BF16, DEV, gen, make_blobs, normal, offsets_of
+from test_gpu_rows import BF16, DEV, F32, gen, make_blobs, normal, offsets_of
 
 pytestmark = pytest.mark.gpu
 
@@ -46,3 +46,16 @@ def test_what_lies_between_blobs_has_no_gradient(lib, dtype):
     assert got.dtype == dtype
     got = got.view(torch.uint8)
     assert torch.equal(got[:, :n], want) and not got[:, n:].any()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_gradient_of_rows_that_lie_apart(lib, dtype):
+    """norm_rows takes rows with a stride, and without y hands them back: its backward takes what it returns."""
+    g = gen(2)
+    h, gain, dx = normal(g, 70, 900, dtype=dtype)[:, 3:703], 1 + normal(g, 700, std=0.2), normal(g, 70, 700, dtype=BF16)
+    n = lib.norm_rows(h, gain=gain)
+    assert torch.equal(n.h, h)
+    got, want = (lib.norm_rows_backward(t, gain, n.rstd, dx) for t in (n.h, h.contiguous()))
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    with pytest.raises(ValueError):
+        lib.norm_rows_backward(h.t().contiguous().t(), gain, n.rstd, dx)
