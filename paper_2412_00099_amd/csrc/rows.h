@@ -2,6 +2,7 @@
 #pragma once
 
 #include "common.h"
+#include "row_grid.h"
 
 namespace moe {
 
@@ -77,6 +78,8 @@ hipError_t launch_experts_dw(const ExpertRowsParams &p, const uint16_t *xs, cons
 #if defined(__HIPCC__)
 // for lambdas that are called in several places: as calls they would keep their captures in memory
 #define MOE_ROWS_INLINE __attribute__((always_inline))
+// the workgroup's place in a grid of row_grid
+__device__ __forceinline__ int64_t row_group() { return blockIdx.y * kRowGridX + blockIdx.x; }
 typedef uint32_t rows_u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t rows_u32x2 __attribute__((ext_vector_type(2)));
 

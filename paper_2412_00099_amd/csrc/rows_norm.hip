@@ -29,11 +29,9 @@ __global__ __launch_bounds__(1024) void norm_rows_kernel(const NormRowsParams p,
   __shared__ uint32_t part_top[kMaxWaves];
   // a row belongs to a wavefront or to the whole workgroup
   const int lane = threadIdx.x & 63, wave = waves == 1 ? 0 : threadIdx.x >> 6;
-  int64_t row = blockIdx.x;
-  if (waves == 1) {
-    row = row * (blockDim.x >> 6) + (threadIdx.x >> 6);
-    if (row >= p.n_rows) return;  // (no barrier in this form)
-  }
+  int64_t row = row_group();
+  if (waves == 1) row = row * (blockDim.x >> 6) + (threadIdx.x >> 6);
+  if (row >= p.n_rows) return;  // (ahead of the barrier only with all of the row's wavefronts)
   const int t = wave * 64 + lane, step = waves * 64 * VEC, d = p.hidden;
   float h[NV][VEC], y[NV][VEC];
 #pragma unroll
@@ -299,7 +297,8 @@ hipError_t launch_norm_rows(const NormRowsParams &p, int n_cus, hipStream_t s) {
   while (p.n_rows < 4 * n_cus && waves < kMaxWaves && waves * 64 * vec < d) waves *= 2;
   const int nv = (d + waves * 64 * vec - 1) / (waves * 64 * vec);
   const int rows_per_wg = waves == 1 ? 4 : 1;
-  const dim3 grid((uint32_t)((p.n_rows + rows_per_wg - 1) / rows_per_wg)), block(waves == 1 ? 256 : waves * 64);
+  const RowGrid g = row_grid(((int64_t)p.n_rows + rows_per_wg - 1) / rows_per_wg);
+  const dim3 grid(g.x, g.y), block(waves == 1 ? 256 : waves * 64);
   const auto go = [&](auto H, auto Y, auto X) {
     const auto with = [&](auto VEC, auto NV) {
       hipLaunchKernelGGL((norm_rows_kernel<decltype(H)::value, decltype(Y)::value, decltype(X)::value, decltype(VEC)::value, decltype(NV)::value>),

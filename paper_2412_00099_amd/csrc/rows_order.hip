@@ -189,7 +189,7 @@ template <typename V>
 __global__ __launch_bounds__(256) void gather_kernel(const OrderParams o, const uint8_t *x, int64_t x_stride, int row_bytes, const float *scale,
                                                      uint8_t *xs, float *xs_scale) {
   const int lane = threadIdx.x & 63;
-  const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int64_t t = row_group() * 4 + (threadIdx.x >> 6);
   if (t >= o.n_tokens) return;
   const Places places(o, t, nullptr, lane);
   int row[MOE_MAX_TOPK];
@@ -229,7 +229,7 @@ __global__ __launch_bounds__(256) void gather_kernel(const OrderParams o, const 
 template <int YS, int Y, int VEC, int KC, int CH>
 __global__ __launch_bounds__(256) void combine_kernel(const OrderParams o, const void *ys, const float *weight, const void *base, void *y) {
   const int lane = threadIdx.x & 63;
-  const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int64_t t = row_group() * 4 + (threadIdx.x >> 6);
   if (t >= o.n_tokens) return;
   const int d = o.hidden;
   const Places places(o, t, weight, lane);
@@ -285,7 +285,7 @@ template <int DY, int YS, int VEC>
 __global__ __launch_bounds__(256) void combine_backward_kernel(const OrderParams o, const void *dy, const void *ys, const float *weight, void *dys,
                                                                float *dweight) {
   const int lane = threadIdx.x & 63;
-  const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int64_t t = row_group() * 4 + (threadIdx.x >> 6);
   if (t >= o.n_tokens) return;
   const int d = o.hidden;
   const Places places(o, t, weight, lane);
@@ -370,7 +370,8 @@ hipError_t launch_sort_tokens(const int32_t *ids, int64_t n, int n_experts, int3
 hipError_t launch_gather_rows(const OrderParams &o, const void *x, int fmt, int64_t x_stride, const float *scale, void *xs, float *xs_scale,
                               hipStream_t s) {
   const int64_t row = (int64_t)o.hidden * row_elem(fmt), stride = x_stride * row_elem(fmt);
-  const dim3 grid((uint32_t)((o.n_tokens + 3) / 4)), block(256);
+  const RowGrid g = row_grid(((int64_t)o.n_tokens + 3) / 4);
+  const dim3 grid(g.x, g.y), block(256);
   const auto go = [&](auto v) {
     using V = decltype(v);
     hipLaunchKernelGGL((gather_kernel<V>), grid, block, 0, s, o, static_cast<const uint8_t *>(x), stride, (int)row, scale,
@@ -386,7 +387,8 @@ hipError_t launch_combine_rows(const OrderParams &o, const void *ys, int ys_fmt,
   // Units of 8 columns wherever a row begins, the last one over the one before it; rows of fewer by single columns.  4096 x 4 rows of
   // 2047 bf16: 16 us, by single columns 64.
   const bool wide = o.hidden >= 8;
-  const dim3 grid((uint32_t)((o.n_tokens + 3) / 4)), block(256);
+  const RowGrid g = row_grid(((int64_t)o.n_tokens + 3) / 4);
+  const dim3 grid(g.x, g.y), block(256);
   const auto go = [&](auto YS, auto Y) {
     const auto with = [&](auto VEC, auto KC) {
       const auto go_on = [&](auto CH) {
@@ -418,7 +420,8 @@ hipError_t launch_combine_rows(const OrderParams &o, const void *ys, int ys_fmt,
 hipError_t launch_combine_rows_backward(const OrderParams &o, const void *dy, int dy_fmt, const void *ys, int ys_fmt, const float *weight,
                                         void *dys, float *dweight, hipStream_t s) {
   const bool wide = o.hidden >= 8;  // (see above; 4096 x 4 rows of 2047 bf16: 31 us, by single columns 97)
-  const dim3 grid((uint32_t)((o.n_tokens + 3) / 4)), block(256);
+  const RowGrid g = row_grid(((int64_t)o.n_tokens + 3) / 4);
+  const dim3 grid(g.x, g.y), block(256);
   const auto go = [&](auto DY, auto YS) {
     const auto with = [&](auto VEC) {
       hipLaunchKernelGGL((combine_backward_kernel<decltype(DY)::value, decltype(YS)::value, decltype(VEC)::value>), grid, block, 0, s, o, dy, ys,
