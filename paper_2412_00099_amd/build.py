@@ -45,61 +45,69 @@ SOURCES = {
 }
 
 
+def _torch() -> str:
+    import importlib.util
+
+    spec = importlib.util.find_spec("torch")
+    if spec is None:
+        raise RuntimeError("PyTorch is not installed")
+    return os.path.dirname(spec.origin)
+
+
 def _tensors_command(obj: str) -> list[str]:
     """csrc/rows_torch.cpp to an object file"""
-    import importlib.util
     import sysconfig
 
-    torch = os.path.dirname(importlib.util.find_spec("torch").origin)
     return [os.environ.get("CXX", "g++"), "-c", os.path.join(CSRC, "rows_torch.cpp"), "-o", obj, "-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden",
-            "-Wall", "-DUSE_ROCM=1", "-D__HIP_PLATFORM_AMD__=1", "-I" + os.path.join(ROOT, "include"), "-isystem", os.path.join(torch, "include"),
+            "-Wall", "-DUSE_ROCM=1", "-D__HIP_PLATFORM_AMD__=1", "-I" + os.path.join(ROOT, "include"), "-isystem", os.path.join(_torch(), "include"),
             "-isystem", "/opt/rocm/include", "-I" + sysconfig.get_paths()["include"]]
 
 
 def _tensors_link(obj: str) -> list[str]:
-    import importlib.util
+    libs = os.path.join(_torch(), "lib")
+    return [os.environ.get("CXX", "g++"), "-shared", "-o", TENSORS_OUT, obj, "-L" + os.path.dirname(OUT), "-l:libmoe_cache.so", "-L" + libs,
+            "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_hip", "-Wl,-rpath,$ORIGIN", "-Wl,-rpath," + libs]
 
-    libs = os.path.join(os.path.dirname(importlib.util.find_spec("torch").origin), "lib")
-    return [os.environ.get("CXX", "g++"), "-shared", "-o", TENSORS_OUT, obj, "-L" + HERE, "-l:libmoe_cache.so", "-L" + libs, "-ltorch_python", "-ltorch",
-            "-ltorch_cpu", "-lc10", "-lc10_hip", "-Wl,-rpath,$ORIGIN", "-Wl,-rpath," + libs]
+
+def _start(cmd: list[str], verbose: bool) -> subprocess.Popen:
+    if verbose:
+        print("[build]", " ".join(cmd), flush=True)
+    return subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+
+
+def _done(what: str, p: subprocess.Popen, verbose: bool) -> bool:
+    out, _ = p.communicate()
+    out = "\n".join(l for l in out.splitlines() if "packed-fp32-ops" not in l and l.strip())
+    if out and verbose:
+        print(out)
+    if p.returncode != 0:
+        print(f"[build] {what} failed", file=sys.stderr)
+    return p.returncode == 0
 
 
 def build(verbose: bool = True) -> str:
+    """The library, and then the tensors' part of the row operators, which also needs a host compiler and PyTorch's headers: without
+    them the library is there all the same, and the error says what is not."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     os.makedirs(OBJ_DIR, exist_ok=True)
-    objs = []
-    procs = []
-    for src, extra in SOURCES.items():
-        obj = os.path.join(OBJ_DIR, src + ".o")
-        cmd = [hipcc, "-c", os.path.join(CSRC, src), "-o", obj] + COMMON + extra
-        if verbose:
-            print("[build]", " ".join(cmd), flush=True)
-        procs.append((src, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
-        objs.append(obj)
-    tensors_obj = os.path.join(OBJ_DIR, "rows_torch.cpp.o")
-    cmd = _tensors_command(tensors_obj)
-    if verbose:
-        print("[build]", " ".join(cmd), flush=True)
-    procs.append(("rows_torch.cpp", subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
-    failed = False
-    for src, p in procs:
-        out, _ = p.communicate()
-        out = "\n".join(l for l in out.splitlines() if "packed-fp32-ops" not in l and l.strip())
-        if out and verbose:
-            print(out)
-        if p.returncode != 0:
-            print(f"[build] {src} failed", file=sys.stderr)
-            failed = True
-    if failed:
-        raise RuntimeError("a compiler failed")
+    objs = [os.path.join(OBJ_DIR, src + ".o") for src in SOURCES]
+    procs = [(src, _start([hipcc, "-c", os.path.join(CSRC, src), "-o", obj] + COMMON + extra, verbose))
+             for (src, extra), obj in zip(SOURCES.items(), objs)]
+    tensors_obj, tensors, missing = os.path.join(OBJ_DIR, "rows_torch.cpp.o"), None, "a compiler failed"
+    try:
+        tensors = _start(_tensors_command(tensors_obj), verbose)
+    except (OSError, RuntimeError) as e:
+        missing = str(e)
+    compiled = [_done(src, p, verbose) for src, p in procs]
+    tensors_compiled = tensors is not None and _done("rows_torch.cpp", tensors, verbose)
+    if not all(compiled):
+        raise RuntimeError("hipcc failed")
     cmd = [hipcc, "-shared", "-fPIC", "--offload-arch=gfx950", "-o", OUT] + objs
     if verbose:
         print("[build]", " ".join(cmd), flush=True)
     subprocess.check_call(cmd)
-    cmd = _tensors_link(tensors_obj)
-    if verbose:
-        print("[build]", " ".join(cmd), flush=True)
-    subprocess.check_call(cmd)
+    if not tensors_compiled or not _done("_rows.so", _start(_tensors_link(tensors_obj), verbose), verbose):
+        raise RuntimeError(f"{OUT} is built, the row operators for tensors are not: {missing}")
     return OUT
 
 

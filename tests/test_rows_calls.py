@@ -1,6 +1,14 @@
-"""How the operators on many rows are called, as far as that shows without a GPU: what their tensors' part refuses."""
+"""How the operators on many rows are called, as far as that shows without a GPU: what their tensors' part refuses, and what works
+where it has not been built."""
+import importlib.util
+import os
+import subprocess
+import sys
+
 import pytest
 import torch
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
 @pytest.fixture(scope="module")
@@ -46,3 +54,49 @@ def test_gradients_are_not_lost_in_silence(moe, call):
         call(moe, o)
     with torch.no_grad(), pytest.raises(ValueError, match="GPU"):  # (as far as the next check)
         call(moe, o)
+
+
+WITHOUT = """
+import sys
+
+class Missing:
+    def find_spec(self, name, path=None, target=None):
+        if name == "paper_2412_00099_amd._rows":
+            raise ImportError("no such library")
+
+sys.meta_path.insert(0, Missing())
+import paper_2412_00099_amd as moe
+assert moe.moe_blob_bytes(moe.MOE_W_BF16, 512, 8) and moe.MoEDecoder and moe.ExpertStore
+for name in ("norm_rows", "experts_rows", "TokenOrder"):
+    try:
+        getattr(moe, name)
+    except ImportError as e:
+        assert "build.py" in str(e)
+    else:
+        raise SystemExit(name)
+try:
+    moe.something_else
+except AttributeError:
+    print("fine")
+"""
+
+
+def test_decode_needs_no_tensors_part():
+    run = subprocess.run([sys.executable, "-c", WITHOUT], cwd=ROOT, capture_output=True, text=True, timeout=120)
+    assert run.returncode == 0 and run.stdout.split() == ["fine"], run.stderr[-2000:]
+
+
+def test_the_library_is_built_without_a_host_compiler(tmp_path, monkeypatch):
+    spec = importlib.util.spec_from_file_location("build_of_a_test", os.path.join(ROOT, "paper_2412_00099_amd", "build.py"))
+    build = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(build)
+    if not os.path.exists(os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")):
+        pytest.skip("no hipcc")
+    monkeypatch.setattr(build, "SOURCES", {"trace_sim.hip": []})
+    monkeypatch.setattr(build, "OUT", str(tmp_path / "libmoe_cache.so"))
+    monkeypatch.setattr(build, "TENSORS_OUT", str(tmp_path / "_rows.so"))
+    monkeypatch.setattr(build, "OBJ_DIR", str(tmp_path))
+    monkeypatch.setenv("CXX", str(tmp_path / "no-such-compiler"))
+    with pytest.raises(RuntimeError, match="row operators"):
+        build.build(verbose=False)
+    assert os.path.exists(tmp_path / "libmoe_cache.so") and not os.path.exists(tmp_path / "_rows.so")
