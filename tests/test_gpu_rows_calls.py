@@ -1,10 +1,16 @@
-"""How the operators on many rows are called, at sizes and layouts that the numerical tests do not have."""
+"""How the operators on many rows are called: through tensors and through the C entry points, at sizes and layouts that the
+numerical tests do not have."""
+import os
+import subprocess
+import sys
+
 import pytest
 import torch
 
-from test_gpu_rows import BF16, DEV, F32, gen, make_blobs, normal, offsets_of
+from test_gpu_rows import BF16, DEV, F32, I8, gen, ids_of, make_blobs, make_rows, normal, offsets_of
 
 pytestmark = pytest.mark.gpu
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
 @pytest.mark.parametrize("what", ["experts", "most experts", "top_k", "hidden", "inter"])
@@ -59,3 +65,85 @@ def test_gradient_of_rows_that_lie_apart(lib, dtype):
     assert all(torch.equal(a, b) for a, b in zip(got, want))
     with pytest.raises(ValueError):
         lib.norm_rows_backward(h.t().contiguous().t(), gain, n.rstd, dx)
+
+
+FIRST = """
+import torch
+import paper_2412_00099_amd as moe
+
+g = torch.Generator(device="cuda")
+g.manual_seed(0)
+T, K, E, d, I = 40, 2, 5, 1024, 24
+h, gain, dx = (torch.randn(*s, generator=g, device="cuda") for s in ((T, d), (d,), (T, d)))
+ids = torch.randint(-1, E, (T, K), generator=g, device="cuda", dtype=torch.int32)
+weight = torch.rand(T, K, generator=g, device="cuda")
+blobs = (torch.randn(E, I, 3, d, generator=g, device="cuda") * 0.03).bfloat16()
+torch.cuda.synchronize()
+
+def layer():
+    n = moe.norm_rows(h, None, gain)
+    o = moe.sort_tokens(ids, E)
+    xs, _ = moe.gather_rows(n.x, o)
+    ys, kept = moe.experts_rows("bf16", blobs, I, xs, o.offsets, keep=True)
+    y = moe.combine_rows(ys, o, weight)
+    dys, dweight = moe.combine_rows_backward(y, ys, o, weight)
+    dxs, dblobs = moe.experts_rows_backward("bf16", blobs, I, xs, o.offsets, kept, dys)
+    return n.x, y, dweight, dxs, dblobs, *moe.norm_rows_backward(h, gain, n.rstd, dx)
+
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    out = layer()
+for _ in range(3):
+    h.mul_(1.5).add_(0.1)
+    want = layer()
+    torch.cuda.synchronize()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(out, want))
+print("same")
+"""
+
+
+def test_the_first_calls_of_a_process_can_be_captured():
+    run = subprocess.run([sys.executable, "-c", FIRST], cwd=ROOT, capture_output=True, text=True, timeout=100)
+    assert run.returncode == 0 and run.stdout.split()[-1] == "same", run.stderr[-2000:]
+
+
+def test_c_entry_points_with_pointers(lib):
+    """The same results, bit for bit, as through tensors."""
+    g = gen(4)
+    T, K, E, d, I = 2100, 2, 5, 512, 40
+    stream = torch.cuda.current_stream().cuda_stream
+    new = lambda *shape, dtype=BF16: torch.empty(*shape, dtype=dtype, device=DEV)  # noqa: E731
+    ids, weight = ids_of(g, T, K, E, 0.1), torch.rand(T, K, generator=g, device=DEV)
+    want = lib.sort_tokens(ids, E)
+    offsets, row_of, entry_of = (torch.empty_like(t) for t in want)
+    need = lib.moe_sort_tokens_bytes(T, K, E)
+    work = new(need, dtype=torch.uint8)
+    lib.moe_sort_tokens(ids.data_ptr(), T, K, E, offsets.data_ptr(), row_of.data_ptr(), entry_of.data_ptr(), work.data_ptr(), need, stream)
+    assert need > 0 and all(torch.equal(a, b) for a, b in zip((offsets, row_of, entry_of), want))
+
+    x, scale = torch.randint(-127, 128, (T, d), generator=g, device=DEV, dtype=torch.int32).to(I8), torch.rand(T, generator=g, device=DEV)
+    xs, ss = new(T * K, d, dtype=I8), new(T * K, dtype=F32)
+    lib.moe_gather_rows(x.data_ptr(), lib.MOE_R_INT8, d, scale.data_ptr(), row_of.data_ptr(), offsets.data_ptr(), T, K, E, d, xs.data_ptr(),
+                        ss.data_ptr(), stream)
+    assert all(torch.equal(a, b) for a, b in zip((xs, ss), lib.gather_rows(x, want, scale)))
+
+    blobs, _ = make_blobs(lib, g, "bf16", E, d, I)
+    rows, dys = make_rows(g, "bf16", T * K, d)[0], normal(g, T * K, d, dtype=BF16)
+    h, gu, ys = new(T * K, 64), new(T * K, 2, 64, dtype=F32), new(T * K, d)
+    n = blobs.shape[1]
+    lib.moe_experts_rows(lib.MOE_W_BF16, d, I, E, blobs.data_ptr(), n, rows.data_ptr(), None, offsets.data_ptr(), T * K, h.data_ptr(), gu.data_ptr(),
+                         ys.data_ptr(), stream)
+    want_ys, kept = lib.experts_rows("bf16", blobs, I, rows, want.offsets, keep=True)
+    used = int(offsets[-1])
+    assert torch.equal(ys, want_ys) and torch.equal(h[:used], kept.h[:used]) and torch.equal(gu[:used], kept.gu[:used])
+    dgu, dxs, dblobs = new(T * K, 2, 64), new(T * K, d), torch.empty_like(blobs)
+    lib.moe_experts_rows_backward(lib.MOE_W_BF16, d, I, E, blobs.data_ptr(), n, rows.data_ptr(), offsets.data_ptr(), T * K, h.data_ptr(),
+                                  gu.data_ptr(), dys.data_ptr(), dgu.data_ptr(), dxs.data_ptr(), dblobs.data_ptr(), stream)
+    assert all(torch.equal(a, b) for a, b in zip((dxs, dblobs), lib.experts_rows_backward("bf16", blobs, I, rows, want.offsets, kept, dys)))
+
+    dy, back, dweight = normal(g, T, d), new(T * K, d), new(T, K, dtype=F32)
+    lib.moe_combine_rows_backward(dy.data_ptr(), lib.MOE_R_FP32, ys.data_ptr(), lib.MOE_R_BF16, row_of.data_ptr(), offsets.data_ptr(),
+                                  weight.data_ptr(), T, K, E, d, back.data_ptr(), dweight.data_ptr(), stream)
+    assert all(torch.equal(a, b) for a, b in zip((back, dweight), lib.combine_rows_backward(dy, ys, want, weight)))
