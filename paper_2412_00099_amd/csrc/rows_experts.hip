@@ -289,7 +289,8 @@ __device__ __forceinline__ i32x4 widen(i32x2 q) {
 }
 
 // Results go through buffer resources too: rows that the tile does not have lie behind their end and are dropped, so that no
-// lane branches (a branch that differs between lanes would take the loops around it out of scalar control).
+// lane branches (a branch that differs between lanes would take the loops around it out of scalar control).  Bytes within a blob, its
+// gradient and a tile's kept sums pass 2^31: they are counted in unsigned 32 bits, elements in signed ones.
 constexpr uint32_t kNowhere = 0xf8000000u;
 template <int N>
 __device__ __forceinline__ void store_bf16(Buffer p, uint32_t off, const float (&v)[N]) {
@@ -692,7 +693,7 @@ struct Product {
       constexpr int N = NJ * 2;  // records of a lane
       const int rec = t.col * RECS + wn * (OF_WAVE / 2) + q * N;
       const Buffer h = buffer_of(g.out + (int64_t)t.row0 * pitch, t.rows * pitch * 2);
-      const Buffer both = buffer_of(g.gu_out + (int64_t)t.row0 * 2 * pitch, g.gu_out ? t.rows * 2 * pitch * 4 : 0);
+      const Buffer both = buffer_of(g.gu_out + (int64_t)t.row0 * 2 * pitch, g.gu_out ? (uint32_t)t.rows * 2 * pitch * 4 : 0);
       float sg[N], su[N];
       if constexpr (INT8) {
         const Buffer scales = buffer_of(blob + tail, p.inter * 4);
@@ -729,7 +730,7 @@ struct Product {
         store_bf16(h, rec < pitch ? (r * pitch + rec) * 2 : kNowhere, v);
         if (g.gu_out) {
           if constexpr (N == 8) {
-            const uint32_t at = rec < pitch ? ((m * 32 + wm * 16 + (lane & 7)) * 2 * pitch + rec + (lane & 8) / 2) * 4 : kNowhere;
+            const uint32_t at = rec < pitch ? ((m * 32 + wm * 16 + (lane & 7)) * 2 * pitch + rec + (lane & 8) / 2) * 4u : kNowhere;
             store_lines(both, at, 64 * pitch, four_f32(gate), four_f32(gate + 4));
             store_lines(both, at + pitch * 4, 64 * pitch, four_f32(up), four_f32(up + 4));
           } else {
@@ -740,7 +741,7 @@ struct Product {
         }
       }
     } else if constexpr (FORM == kDgu) {
-      const Buffer in = buffer_of(g.gu_in + (int64_t)t.row0 * 2 * pitch, t.rows * 2 * pitch * 4),
+      const Buffer in = buffer_of(g.gu_in + (int64_t)t.row0 * 2 * pitch, (uint32_t)t.rows * 2 * pitch * 4),
                    out = buffer_of(g.out + (int64_t)t.row0 * 2 * pitch, t.rows * 2 * pitch * 2);
 #pragma unroll
       for (int m = 0; m < MB; ++m) {
@@ -812,7 +813,7 @@ struct Product {
         if (m > 0 && m >= blocks) break;
         const int r = m * 32 + wm * 16 + (lane & 7), at = m0 + r, which = at >= 2 * pitch ? 2 : at >= pitch ? 1 : 0, rec = at - which * pitch;
         // (a record that is not there lies behind the end)
-        const uint32_t to = r < m_rows ? ((rec * 3 + which) * p.hidden + col0 + wn * 64 + (lane & 8) * 4 + q * 8) * 2 : kNowhere;
+        const uint32_t to = r < m_rows ? ((rec * 3 + which) * p.hidden + col0 + wn * 64 + (lane & 8) * 4 + q * 8) * 2u : kNowhere;
         const rows_u32x4 v0 = eight_bf16([&](int i) MOE_ROWS_INLINE { return acc[m][i >> 2][i & 3]; }),
                    v1 = eight_bf16([&](int i) MOE_ROWS_INLINE { return acc[m][2 + (i >> 2)][i & 3]; });
         store_lines(out, to, 8 * 3 * p.hidden * 2, v0, v1);

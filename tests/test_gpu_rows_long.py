@@ -1,8 +1,9 @@
-"""The operators on many rows at the ends of what they take."""
+"""The operators on many rows at the ends of what they take: the most rows, and blobs whose offsets pass 31 bits."""
 import pytest
 import torch
 
-from test_gpu_rows import DEV, F32, U32, gen, normal, within
+from test_gpu_rows import BF16, DEV, F32, U16, U32, gen, normal, offsets_of, within
+from test_gpu_rows_gradients import gradients
 
 pytestmark = pytest.mark.gpu
 MOST = (1 << 26) - 1
@@ -40,3 +41,31 @@ def test_order_of_the_most_places(lib):
     assert not dys[n:].any()
     square = torch.where(there, x.double().square(), 0.0)
     within(dweight, square, 2 * U32 * square, "dweight")
+
+
+def test_an_expert_of_four_gigabytes(lib):
+    """One large tile of rows: offsets into the blob, its gradient and the kept sums pass 2^31 bytes."""
+    hidden, inter, rows = 512, 1310719, 250
+    g = gen(3)
+    w = torch.empty(1, inter, 3, hidden, device=DEV, dtype=BF16)
+    w.normal_(0.0, 0.05, generator=g)
+    assert w.nbytes == lib.moe_blob_bytes(lib.MOE_W_BF16, hidden, inter) and w.nbytes > 0xefff0000
+    xs, dys = normal(g, rows + 2, hidden, dtype=BF16), normal(g, rows + 2, hidden, dtype=BF16, std=0.01)
+    ys, kept = lib.experts_rows("bf16", w, inter, xs, offsets_of([rows]), keep=True)
+    dxs, dw = lib.experts_rows_backward("bf16", w, inter, xs, offsets_of([rows]), kept, dys)
+    assert not ys[rows:].any() and not dxs[rows:].any()
+    x, dy = xs[:rows].double(), dys[:rows].double()
+    y, dx = torch.zeros_like(x), torch.zeros_like(x)
+    for at in range(0, inter, 1 << 16):
+        wg, wu, wd = w[0, at:at + (1 << 16)].double().unbind(1)
+        a, b = x @ wg.t(), x @ wu.t()
+        y += (torch.nn.functional.silu(a) * b) @ wd
+        (one, _), *weights = gradients(x, wg, wu, wd.t(), dy)
+        dx += one
+        for i, (ref, bound) in enumerate(weights):
+            within(dw[0, at:at + (1 << 16), i], ref, bound, f"records from {at} on, {i}")
+    # (sums over 1.3 million records: as vectors, each row's and each column's; one rounding of the products or gradients that are
+    # summed and one of the result, twice over)
+    for got, ref in ((ys[:rows], y), (dxs[:rows], dx)):
+        for dim in (0, 1):
+            assert bool(((got.double() - ref).norm(dim=dim) <= 4 * U16 * ref.norm(dim=dim)).all())
