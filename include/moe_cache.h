@@ -380,8 +380,9 @@ int moe_combine_rows_backward(const void *dy_dev, int32_t dy_fmt, const void *ys
                               int32_t n_experts, int32_t hidden, void *dys_dev, float *dweight_dev, void *stream);
 
 /* The SwiGLU experts on sorted rows (Eq. 1 without the weighted sum): ys[r] = E_e(xs[r]) for offsets[e] <= r < offsets[e + 1],
- * zeros for the rows of nobody.  blobs_dev: packed experts (moe_pack_expert), expert e at e * blob_stride bytes, 16-byte aligned;
- * e.g. a slot pool that holds all experts.  hidden and inter as moe_blob_bytes takes them, one blob smaller than 4 GB.
+ * zeros for the rows of nobody (those ahead of offsets[0], too: a part of the offsets with its blobs is a part of the experts).
+ * blobs_dev: packed experts (moe_pack_expert), expert e at e * blob_stride bytes, 16-byte aligned.  hidden and inter as moe_blob_bytes
+ * takes them, one blob smaller than 0xf0000000 bytes.
  *   MOE_W_BF16     xs_dev bf16, scale_dev NULL
  *   MOE_W_INT8_PC  xs_dev 8-bit codes with a scale for each row (moe_norm_rows, moe_gather_rows).  The sums of the first product
  *                  are whole numbers and exact; h is bf16.

@@ -825,11 +825,13 @@ struct Product {
 template <int FORM, bool INT8, int NJ, int MB, int RS = 2, int WS = 3>
 __global__ __launch_bounds__(kBlock, MB == 8 || RS > 2 ? 2 : FORM == kColumns && INT8 && MB == 2 ? 8 : 4) void product_kernel(const ProductArgs g) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds[Product<FORM, INT8, NJ, MB, RS, WS>::LDS_BYTES];
-  if constexpr (FORM == kColumns) {  // rows of nobody
+  if constexpr (FORM == kColumns) {  // rows of nobody: ahead of the first expert (some of the experts on all of the rows), behind the last
     const ExpertRowsParams &p = g.p;
-    const int used = uniform(min(max(p.offsets[p.n_experts], 0), p.n_rows));
-    for (int64_t r = used + blockIdx.x; r < p.n_rows; r += gridDim.x)
-      for (int c = threadIdx.x * 8; c < p.hidden; c += kBlock * 8) *reinterpret_cast<rows_u32x4 *>(g.out + r * p.hidden + c) = rows_u32x4{};
+    const int first = uniform(first_row(p, 0)), end = max(uniform(min(p.offsets[p.n_experts], p.n_rows)), first);
+    for (int r = blockIdx.x; r < p.n_rows - (end - first); r += gridDim.x) {
+      uint16_t *row = g.out + (int64_t)(r < first ? r : r + (end - first)) * p.hidden;
+      for (int c = threadIdx.x * 8; c < p.hidden; c += kBlock * 8) *reinterpret_cast<rows_u32x4 *>(row + c) = rows_u32x4{};
+    }
   }
   Product<FORM, INT8, NJ, MB, RS, WS> f(g, lds);
   f.run();

@@ -67,6 +67,37 @@ def test_gradient_of_rows_that_lie_apart(lib, dtype):
         lib.norm_rows_backward(h.t().contiguous().t(), gain, n.rstd, dx)
 
 
+@pytest.mark.parametrize("fmt", ["bf16", "int8"])
+@pytest.mark.parametrize("first,last", [(0, 3), (2, 5), (1, 2), (3, 4)])
+def test_some_of_the_experts_on_all_of_the_rows(lib, fmt, first, last):
+    """A part of the offsets with the same part of the blobs: rows ahead of its first expert are rows of nobody, too."""
+    g = gen(3)
+    hidden, inter, counts = 1024, 72, [40, 3, 100, 0, 65]
+    blobs, _ = make_blobs(lib, g, fmt, 5, hidden, inter)
+    xs, scale, _ = make_rows(g, fmt, 210, hidden)
+    off = offsets_of(counts)
+    at, end = int(off[first]), int(off[last])
+
+    def poison():  # what the caching allocator hands out for the results is not zero
+        full = [torch.full((210, hidden), float("nan"), dtype=BF16, device=DEV) for _ in range(4)]
+        torch.cuda.synchronize()
+        del full
+
+    want = lib.experts_rows(fmt, blobs, inter, xs, off, scale=scale)
+    poison()
+    got = lib.experts_rows(fmt, blobs[first:last], inter, xs, off[first:last + 1], scale=scale)
+    assert torch.equal(got[at:end], want[at:end]) and not got[:at].any() and not got[end:].any()
+    if fmt == "bf16":
+        dys = normal(g, 210, hidden, dtype=BF16)
+        _, kept = lib.experts_rows(fmt, blobs, inter, xs, off, keep=True)
+        dxs, dblobs = lib.experts_rows_backward(fmt, blobs, inter, xs, off, kept, dys)
+        _, kept = lib.experts_rows(fmt, blobs[first:last], inter, xs, off[first:last + 1], keep=True)
+        poison()
+        some, some_blobs = lib.experts_rows_backward(fmt, blobs[first:last], inter, xs, off[first:last + 1], kept, dys)
+        assert torch.equal(some[at:end], dxs[at:end]) and not some[:at].any() and not some[end:].any()
+        assert torch.equal(some_blobs, dblobs[first:last])
+
+
 FIRST = """
 import torch
 import paper_2412_00099_amd as moe
