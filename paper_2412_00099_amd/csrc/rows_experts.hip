@@ -10,8 +10,11 @@
 //   kColumns    the summed index are the records (H with down, dG and dU with gate and up): the weights' side is transposed on
 //               its way out of LDS
 //   kWeights    the summed index are the rows: both sides are transposed
-// H and the gradients of G and U pass through memory rounded to bf16, as the rows do; G and U themselves are kept for the
-// backward in 32 bits (rounded to bf16 they were the largest part of the gradients' error).  With 8-bit weights the rows of the
+// H and the gradients of G and U pass through memory rounded to bf16, as the rows do: the matrix cores take bf16, and H in
+// two or (as the prompt path through the cache has it) three parts of bf16 would double or triple the products over the records and
+// the bytes of H.  It makes an error of 0.0023 of the results' size where 32-bit H leaves 0.0017, the rounding of the results
+// themselves (8 to 16384 rows).  G and U are kept for the backward in 32 bits (rounded to bf16 they were the largest part of the
+// gradients' error).  With 8-bit weights the rows of the
 // first product are 8-bit codes too (whole-number sums, exact), H stays bf16 and the weights of down are widened to bf16, which
 // holds every code exactly.
 //
@@ -22,10 +25,10 @@
 // comes from memory.  A stage is two steps of the matrix cores; the fragments of the next step are read while they work on this
 // one's, and there is one barrier a stage.  Both rings run on from tile to tile.
 //
-// Measured: 8192 rows on 8 experts of 4096 x 14336 in 8 bits, kUp 818 us (2.35 POP/s), kColumns 975 (0.99 PFLOP/s), bound by the matrix
-// cores; 16384 uneven rows on 60 experts of 2048 x 1408, kUp with its sums kept 251 us, kColumns 126 (down) and 233 (gradients of the
-// rows, 0.8 PFLOP/s), kDgu 183, kWeights 445, bound by workgroups that end early and, where much is stored, by stores; 8 rows on
-// 8 of them, 17 + 12 us, bound by what a compute unit keeps in flight (138 MB, 4.8 TB/s).
+// Measured: 8192 rows on 8 experts of 4096 x 14336 in 8 bits, kUp 832 us (2.31 POP/s), kColumns 991 (0.97 PFLOP/s), bound by the matrix
+// cores; 16384 uneven rows on 60 experts of 2048 x 1408, kUp with its sums kept 254 us, kColumns 137 (down) and 249 (gradients of the
+// rows, 0.74 PFLOP/s), kDgu 187, kWeights 458, bound by workgroups that end early and, where much is stored, by stores; 8 rows on
+// 8 of them, 17 + 12 us, 138 MB at 4.8 TB/s, bound by the 176 and 128 tiles that 256 compute units have there.
 //
 // Which expert and which of its rows a tile has is worked out from `offsets` on the device.  All loads go through buffer
 // resources that end where the expert's rows or records end: what lies beyond arrives as zeros.
@@ -846,7 +849,8 @@ __global__ __launch_bounds__(kBlock, MB == 8 || RS > 2 ? 2 : FORM == kColumns &&
 //   kUp, 8 bits               76 | 83 | 77    -                 88 | 91 | 87      102 | 97 | 95     114 | 105 | 103   173 | 139 | 128
 //   kColumns, 8 bits          55 | 60 | 73    -                 63 | 71 | 81      80 | 74 | 90      90 | 94 | 98      156 | 134 | 143
 //   kDgu                                                                                                              225 | 193 | 198
-// and with 8192 tokens kColumns, 8 bits, 322 | 258 | 229.  Where tiles are too few for the compute units, smaller ones: 8 experts of
+// and with 8192 tokens kColumns, 8 bits, 322 | 258 | 229.  (kUp in 8 bits and kDgu have the limits of kUp in bf16; in the table another
+// form is ahead by up to 4 % for them there.)  Where tiles are too few for the compute units, smaller ones: 8 experts of
 // 1024 x 704 and two a token, 2048 tokens 36 | 37 | 39; 16 of 2048 x 512 and two, 600 tokens 31 | 35 | 44.
 //
 // One small tile a compute unit at most, in bf16: nobody else keeps memory busy, so the rings have all of the LDS (kUp, 60 experts of

@@ -5,8 +5,8 @@
 //   same however the sum of squares is split over lanes, and both reductions of a row run together.
 //   backward, n = h' r: dh = dh' + r (dx gain - n mean(dx gain n)), dgain = sum over the rows of dx n
 // Bound by memory: every row is read once into registers and written once.  All sums are in 32 bits.
-// Measured: 16384 rows of 4096, fp32 + bf16 -> fp32 and 8 bits, 738 MB in 144 us (5.1 TB/s); 4096 rows of 2048, fp32 + bf16 -> fp32
-// and bf16, 101 MB in 19 us (5.3 TB/s); its gradient, with the gain's, 22 + 4 us; one row 2.4 us.
+// Measured: 16384 rows of 4096, fp32 + bf16 -> fp32 and 8 bits, 738 MB in 149 us (5.0 TB/s); 4096 rows of 2048, fp32 + bf16 -> fp32
+// and bf16, 101 MB in 20 us (5.0 TB/s); its gradient, with the gain's, 23 + 5 us; one row 3.0 us.
 #include <algorithm>
 
 #include "rows.h"

@@ -1,7 +1,7 @@
 // Tokens sorted by the expert that takes them, their rows brought into that order and the results brought back.
 //
 // A place is a token's k-th choice, place = token * top_k + k.  The sort is a stable counting sort: an expert's rows come in
-// the order of the tokens, so the result does not depend on timing (no atomics).  Places without an expert (an id outside
+// the order of the tokens, so the result does not depend on timing (the only atomics add whole numbers up).  Places without an expert (an id outside
 // 0..n_experts-1) have no row; as many rows at the end of the order belong to nobody and are filled with zeros.
 #include "rows.h"
 
@@ -10,7 +10,9 @@ namespace {
 
 constexpr int kSortWaves = 16, kSortThreads = kSortWaves * 64;
 constexpr int kSortBlocks = 256;      // workgroups of the two-launch form at most
-constexpr int kSortSingle = 4096;     // places that one workgroup sorts by itself (2044 take 4.8 us, in two launches 6.6; 4000 7.1 and 6.8; 8000 11.8 and 8.1; 16384 25 and 9)
+// Places that one workgroup sorts by itself (2044 take 4.8 us, in two launches 6.6; 4000 7.1 and 6.8; 8000 11.8 and 8.1; 16384 25 and
+// 9).  More are counted by a launch of their own first, since no workgroup knows another's counts within one.
+constexpr int kSortSingle = 4096;
 constexpr int kSortChunk = 1024;      // places a workgroup takes at least in the two-launch form: one for each thread
 
 // Lanes of the wavefront that hold the same key as this one.  BITS: bits of a key.

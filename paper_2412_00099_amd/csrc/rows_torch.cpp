@@ -1,6 +1,6 @@
 // The row operators for tensors, the part that every call goes through: checks of shapes, types, places and history, the outputs from
 // PyTorch's allocator, the current stream, the call of the C entry point.  In Python this took 10.5 us a call where the kernel takes 3 (a
-// norm of 37 rows), here 5.5.
+// norm of 37 rows), here 5.9.
 #include <ATen/ATen.h>
 #include <c10/core/GradMode.h>
 #include <c10/hip/HIPFunctions.h>
