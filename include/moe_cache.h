@@ -50,6 +50,10 @@ extern "C" {
 #define MOE_ROWS_MAX_EXPERTS 512
 #define MOE_ROWS_MAX_HIDDEN 8192
 #define MOE_ROWS_LIMIT (1 << 26)
+/* attention: the width of a head, heads and sequences at most */
+#define MOE_ATTEND_MAX_DIM 128
+#define MOE_ATTEND_MAX_HEADS 256
+#define MOE_ATTEND_MAX_SEQS 16384
 
 typedef struct moe_cache moe_cache_t; /* opaque, owned by the library */
 
@@ -399,6 +403,73 @@ int moe_experts_rows(int32_t weight_fmt, int32_t hidden, int32_t inter, int32_t 
 int moe_experts_rows_backward(int32_t weight_fmt, int32_t hidden, int32_t inter, int32_t n_experts, const void *blobs_dev,
                               int64_t blob_stride, const void *xs_dev, const int32_t *offsets_dev, int32_t n_rows, const void *h_dev,
                               const float *gu_dev, const void *dys_dev, void *dgu_dev, void *dxs_dev, void *dblobs_dev, void *stream);
+
+/* ---- Attention beside the experts: of the rows of a prompt or a training batch, and of new tokens over a cache of pages ----
+ *
+ * As the calls above: no context, nothing allocated, nothing waited for, sizes refused before a pointer is looked at, graphs
+ * possible, the same results from call to call.  Rows are bf16; a row of q has n_heads heads of head_dim values, one of k and v has
+ * n_kv_heads; query head h reads head h / (n_heads / n_kv_heads).  head_dim is a multiple of 8 up to MOE_ATTEND_MAX_DIM, n_heads a multiple of
+ * n_kv_heads up to MOE_ATTEND_MAX_HEADS, n_seqs <= MOE_ATTEND_MAX_SEQS.  Strides count elements, from token to token and from head to
+ * head; the values of a head are dense.  Pointers and strides of bf16 rows that are read are multiples of 16 bytes.
+ *   A query at position p sees key j if j <= p and (window 0, or j > p - window, or j < sinks).
+ *   z_j = softmax_scale <q, k_j>, y = sum_j exp(z_j - lse) v_j, lse = log sum_j exp(z_j), over the keys that it sees; y is 0 (lse
+ *   -infinity) if there are none.  Sums are held in 32 bits; keys and values that nobody sees may hold anything.
+ *
+ * A cache has n_pages pages of `page` tokens (a power of two, 16 to 1024), page_stride elements from page to page:
+ *   k_pages, v_pages [n_pages][n_kv_heads][page][head_dim]; page * n_pages < 2^31
+ *   MOE_R_BF16  k_scale, v_scale NULL
+ *   MOE_R_INT8  codes c that stand for c * scale; k_scale, v_scale fp32 [n_pages][n_kv_heads][page], dense
+ * both 16-byte aligned, as are their pages.  table_dev [n_seqs, table_pages]: token t of sequence i is in page table[i, t / page]; ids outside
+ * 0..n_pages-1 (-1) are no page, and what would be there is seen by nobody.
+ *
+ * moe_plan_pages: pages and places for the tokens that the sequences bring.  Sequence i has have[i] tokens in the cache and brings more[i]
+ *   (negative: 0).  Entries ceil(have / page) .. ceil((have + more) / page) - 1 of its row of the table, as far as the row goes, are
+ *   taken from free_dev [n_free] in the order of the sequences, from element *used_dev on (used_dev NULL: 0); behind the end of free_dev
+ *   they become -1.  All other entries are read or left alone.
+ *     offsets_dev [n_seqs + 1]     the tokens of sequence i are rows offsets[i] .. offsets[i + 1] - 1
+ *     slots_dev, positions_dev [n_tokens]  of each row: page * `page` + place in it, -1 if there is no page; position in the sequence.
+ *                                  Rows behind the last sequence: -1 and -1
+ *     lengths_dev [n_seqs]         have + more
+ *     used_out_dev [1]             *used_dev + the entries that were to be taken; more than n_free: there were too few pages
+ *   Numbers that pass 2^31 - 1 stay there.  No result may overlap what is read, nor two rows of the table each other.
+ * moe_store_pages: rows of k and v (fmt fp32 or bf16) to their slots; a slot outside 0..n_pages*page-1 takes nothing.  Slots have to
+ *   differ.  cache_fmt bf16: rounded.  int8: with top the largest |v| of a token's head, code = round(127 v / top) (to even, as if
+ *   computed exactly), scale = top / 127; top < 1e-30: codes and scale 0; with an infinity or NaN: codes 0, scale NaN.
+ * moe_attend_pages: one new token per sequence, the last of its lengths_dev[i] tokens.  Length 0 (or less): y is 0.  Every sequence is
+ *   split over the GPU by what the lengths say; the workspace holds the parts' sums: moe_attend_pages_bytes(n_seqs, n_heads,
+ *   n_kv_heads, head_dim) bytes, 16-byte aligned, of this call alone until it is done.
+ * moe_attend_rows: packed sequences.  Sequence i has the rows offsets[i] .. offsets[i + 1] - 1 of q and y, and k_offsets[i] ..
+ *   k_offsets[i + 1] - 1 of k and v (k_offsets_dev NULL: the same); its queries are its last rows, so that query r of nq is at position
+ *   nk - nq + r (one ahead of the first key sees nothing).  y_dev dense [n_rows, n_heads, head_dim]; lse_dev fp32 [n_heads, n_rows], for
+ *   the backward, or NULL.  Rows of no sequence: y is 0.
+ * moe_attend_rows_backward: from dy the gradients of q, k and v, dense, bf16 (rows of no sequence: 0).  y, lse: as the forward left
+ *   them.  P = exp(z - lse), dv = sum P dy, dz = P (<dy, v> - <dy, y>), dq = softmax_scale sum dz k, dk = softmax_scale sum dz q, sums
+ *   over the heads of a group and over all queries in a fixed order.  P and dz are rounded to bf16 for the matrix cores.  y and dy
+ *   dense.  Workspace: moe_attend_rows_backward_bytes(n_rows, n_heads) bytes, 16-byte aligned. */
+int moe_plan_pages(const int32_t *have_dev, const int32_t *more_dev, int32_t n_seqs, int32_t page, const int32_t *free_dev, int32_t n_free,
+                   const int32_t *used_dev, int32_t *table_dev, int32_t table_pages, int32_t *offsets_dev, int32_t *slots_dev,
+                   int32_t *positions_dev, int32_t n_tokens, int32_t *lengths_dev, int32_t *used_out_dev, void *stream);
+int moe_store_pages(const void *k_dev, const void *v_dev, int32_t fmt, int64_t k_stride, int64_t k_head_stride, int64_t v_stride,
+                    int64_t v_head_stride, const int32_t *slots_dev, int32_t n_rows, int32_t n_kv_heads, int32_t head_dim, void *k_pages_dev,
+                    void *v_pages_dev, int32_t cache_fmt, int64_t page_stride, int32_t n_pages, int32_t page, float *k_scale_dev,
+                    float *v_scale_dev, void *stream);
+size_t moe_attend_pages_bytes(int32_t n_seqs, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim);
+int moe_attend_pages(const void *q_dev, int64_t q_stride, int64_t q_head_stride, const void *k_pages_dev, const void *v_pages_dev,
+                     int32_t cache_fmt, int64_t page_stride, int32_t n_pages, int32_t page, const float *k_scale_dev,
+                     const float *v_scale_dev, const int32_t *table_dev, int32_t table_pages, const int32_t *lengths_dev, int32_t n_seqs,
+                     int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, float softmax_scale, int32_t window, int32_t sinks, void *y_dev,
+                     void *workspace_dev, size_t workspace_bytes, void *stream);
+int moe_attend_rows(const void *q_dev, int64_t q_stride, int64_t q_head_stride, const void *k_dev, int64_t k_stride, int64_t k_head_stride,
+                    const void *v_dev, int64_t v_stride, int64_t v_head_stride, const int32_t *offsets_dev, const int32_t *k_offsets_dev,
+                    int32_t n_seqs, int32_t n_rows, int32_t n_k_rows, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                    float softmax_scale, int32_t window, int32_t sinks, void *y_dev, float *lse_dev, void *stream);
+size_t moe_attend_rows_backward_bytes(int32_t n_rows, int32_t n_heads);
+int moe_attend_rows_backward(const void *q_dev, int64_t q_stride, int64_t q_head_stride, const void *k_dev, int64_t k_stride,
+                             int64_t k_head_stride, const void *v_dev, int64_t v_stride, int64_t v_head_stride, const int32_t *offsets_dev,
+                             const int32_t *k_offsets_dev, int32_t n_seqs, int32_t n_rows, int32_t n_k_rows, int32_t n_heads,
+                             int32_t n_kv_heads, int32_t head_dim, float softmax_scale, int32_t window, int32_t sinks, const void *y_dev,
+                             const float *lse_dev, const void *dy_dev, void *dq_dev, void *dk_dev, void *dv_dev, void *workspace_dev,
+                             size_t workspace_bytes, void *stream);
 
 const char *moe_last_error(void);
 

@@ -177,6 +177,22 @@ lib.moe_experts_rows.restype = C.c_int
 lib.moe_experts_rows.argtypes = [_i32, _i32, _i32, _i32, _vp, _i64, _vp, _vp, _vp, _i32, _vp, _vp, _vp, _vp]
 lib.moe_experts_rows_backward.restype = C.c_int
 lib.moe_experts_rows_backward.argtypes = [_i32, _i32, _i32, _i32, _vp, _i64, _vp, _vp, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp]
+lib.moe_plan_pages.restype = C.c_int
+lib.moe_plan_pages.argtypes = [_vp, _vp, _i32, _i32, _vp, _i32, _vp, _vp, _i32, _vp, _vp, _vp, _i32, _vp, _vp, _vp]
+lib.moe_store_pages.restype = C.c_int
+lib.moe_store_pages.argtypes = [_vp, _vp, _i32, _i64, _i64, _i64, _i64, _vp, _i32, _i32, _i32, _vp, _vp, _i32, _i64, _i32, _i32, _vp, _vp, _vp]
+lib.moe_attend_pages_bytes.restype = C.c_size_t
+lib.moe_attend_pages_bytes.argtypes = [_i32, _i32, _i32, _i32]
+lib.moe_attend_pages.restype = C.c_int
+lib.moe_attend_pages.argtypes = [_vp, _i64, _i64, _vp, _vp, _i32, _i64, _i32, _i32, _vp, _vp, _vp, _i32, _vp, _i32, _i32, _i32, _i32, C.c_float,
+                                 _i32, _i32, _vp, _vp, C.c_size_t, _vp]
+_attend_rows = [_vp, _i64, _i64, _vp, _i64, _i64, _vp, _i64, _i64, _vp, _vp, _i32, _i32, _i32, _i32, _i32, _i32, C.c_float, _i32, _i32]
+lib.moe_attend_rows.restype = C.c_int
+lib.moe_attend_rows.argtypes = _attend_rows + [_vp, _vp, _vp]
+lib.moe_attend_rows_backward_bytes.restype = C.c_size_t
+lib.moe_attend_rows_backward_bytes.argtypes = [_i32, _i32]
+lib.moe_attend_rows_backward.restype = C.c_int
+lib.moe_attend_rows_backward.argtypes = _attend_rows + [_vp, _vp, _vp, _vp, _vp, _vp, _vp, C.c_size_t, _vp]
 lib.moe_last_error.restype = C.c_char_p
 lib.moe_last_error.argtypes = []
 
@@ -187,6 +203,8 @@ EXPORTS = [
     "moe_cache_set_baseline", "moe_cache_reset", "moe_residual_rmsnorm", "moe_cache_profile", "moe_last_error",
     "moe_norm_rows", "moe_norm_rows_backward_bytes", "moe_norm_rows_backward", "moe_sort_tokens_bytes", "moe_sort_tokens",
     "moe_gather_rows", "moe_combine_rows", "moe_combine_rows_backward", "moe_experts_rows", "moe_experts_rows_backward",
+    "moe_plan_pages", "moe_store_pages", "moe_attend_pages_bytes", "moe_attend_pages", "moe_attend_rows",
+    "moe_attend_rows_backward_bytes", "moe_attend_rows_backward",
 ]
 
 
@@ -415,3 +433,50 @@ def moe_experts_rows_backward(weight_fmt, hidden, inter, n_experts, blobs_dev, b
     _check(lib.moe_experts_rows_backward(weight_fmt, hidden, inter, n_experts, blobs_dev, blob_stride, xs_dev, offsets_dev, n_rows,
                                          h_dev, gu_dev, dys_dev, dgu_dev, dxs_dev, dblobs_dev, stream),
            "moe_experts_rows_backward")
+
+
+def moe_plan_pages(have_dev, more_dev, n_seqs, page, free_dev, n_free, used_dev, table_dev, table_pages, offsets_dev, slots_dev,
+                   positions_dev, n_tokens, lengths_dev, used_out_dev, stream) -> None:
+    _check(lib.moe_plan_pages(have_dev, more_dev, n_seqs, page, free_dev, n_free, used_dev, table_dev, table_pages, offsets_dev,
+                              slots_dev, positions_dev, n_tokens, lengths_dev, used_out_dev, stream), "moe_plan_pages")
+
+
+def moe_store_pages(k_dev, v_dev, fmt, k_stride, k_head_stride, v_stride, v_head_stride, slots_dev, n_rows, n_kv_heads, head_dim,
+                    k_pages_dev, v_pages_dev, cache_fmt, page_stride, n_pages, page, k_scale_dev, v_scale_dev, stream) -> None:
+    _check(lib.moe_store_pages(k_dev, v_dev, fmt, k_stride, k_head_stride, v_stride, v_head_stride, slots_dev, n_rows, n_kv_heads,
+                               head_dim, k_pages_dev, v_pages_dev, cache_fmt, page_stride, n_pages, page, k_scale_dev, v_scale_dev,
+                               stream), "moe_store_pages")
+
+
+def moe_attend_pages_bytes(n_seqs: int, n_heads: int, n_kv_heads: int, head_dim: int) -> int:
+    return int(lib.moe_attend_pages_bytes(n_seqs, n_heads, n_kv_heads, head_dim))
+
+
+def moe_attend_pages(q_dev, q_stride, q_head_stride, k_pages_dev, v_pages_dev, cache_fmt, page_stride, n_pages, page, k_scale_dev,
+                     v_scale_dev, table_dev, table_pages, lengths_dev, n_seqs, n_heads, n_kv_heads, head_dim, softmax_scale, window,
+                     sinks, y_dev, workspace_dev, workspace_bytes, stream) -> None:
+    _check(lib.moe_attend_pages(q_dev, q_stride, q_head_stride, k_pages_dev, v_pages_dev, cache_fmt, page_stride, n_pages, page,
+                                k_scale_dev, v_scale_dev, table_dev, table_pages, lengths_dev, n_seqs, n_heads, n_kv_heads, head_dim,
+                                softmax_scale, window, sinks, y_dev, workspace_dev, workspace_bytes, stream), "moe_attend_pages")
+
+
+def moe_attend_rows(q_dev, q_stride, q_head_stride, k_dev, k_stride, k_head_stride, v_dev, v_stride, v_head_stride, offsets_dev,
+                    k_offsets_dev, n_seqs, n_rows, n_k_rows, n_heads, n_kv_heads, head_dim, softmax_scale, window, sinks, y_dev,
+                    lse_dev, stream) -> None:
+    _check(lib.moe_attend_rows(q_dev, q_stride, q_head_stride, k_dev, k_stride, k_head_stride, v_dev, v_stride, v_head_stride,
+                               offsets_dev, k_offsets_dev, n_seqs, n_rows, n_k_rows, n_heads, n_kv_heads, head_dim, softmax_scale,
+                               window, sinks, y_dev, lse_dev, stream), "moe_attend_rows")
+
+
+def moe_attend_rows_backward_bytes(n_rows: int, n_heads: int) -> int:
+    return int(lib.moe_attend_rows_backward_bytes(n_rows, n_heads))
+
+
+def moe_attend_rows_backward(q_dev, q_stride, q_head_stride, k_dev, k_stride, k_head_stride, v_dev, v_stride, v_head_stride,
+                             offsets_dev, k_offsets_dev, n_seqs, n_rows, n_k_rows, n_heads, n_kv_heads, head_dim, softmax_scale,
+                             window, sinks, y_dev, lse_dev, dy_dev, dq_dev, dk_dev, dv_dev, workspace_dev, workspace_bytes,
+                             stream) -> None:
+    _check(lib.moe_attend_rows_backward(q_dev, q_stride, q_head_stride, k_dev, k_stride, k_head_stride, v_dev, v_stride,
+                                        v_head_stride, offsets_dev, k_offsets_dev, n_seqs, n_rows, n_k_rows, n_heads, n_kv_heads,
+                                        head_dim, softmax_scale, window, sinks, y_dev, lse_dev, dy_dev, dq_dev, dk_dev, dv_dev,
+                                        workspace_dev, workspace_bytes, stream), "moe_attend_rows_backward")

@@ -1,5 +1,5 @@
 """Compile the HIP sources into paper_2412_00099_amd/libmoe_cache.so (gfx950 only, in-tree), and the tensors' part of the row
-operators (host code only) into _rows.so beside it."""
+operators and of attention (host code only) into _rows.so beside it."""
 from __future__ import annotations
 
 import os
@@ -42,6 +42,10 @@ SOURCES = {
     "rows_order.hip": [],
     "rows_experts.hip": [],
     "rows_api.hip": [],
+    "pages.hip": ["-ffp-contract=off"],  # (8-bit codes, as above)
+    "attend_pages.hip": [],
+    "attend_rows.hip": [],
+    "attend_api.hip": [],
 }
 
 
@@ -54,18 +58,21 @@ def _torch() -> str:
     return os.path.dirname(spec.origin)
 
 
-def _tensors_command(obj: str) -> list[str]:
-    """csrc/rows_torch.cpp to an object file"""
+TENSORS_SOURCES = ("rows_torch.cpp", "attend_torch.cpp")
+
+
+def _tensors_command(src: str, obj: str) -> list[str]:
+    """one of TENSORS_SOURCES to an object file"""
     import sysconfig
 
-    return [os.environ.get("CXX", "g++"), "-c", os.path.join(CSRC, "rows_torch.cpp"), "-o", obj, "-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden",
+    return [os.environ.get("CXX", "g++"), "-c", os.path.join(CSRC, src), "-o", obj, "-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden",
             "-Wall", "-DUSE_ROCM=1", "-D__HIP_PLATFORM_AMD__=1", "-I" + os.path.join(ROOT, "include"), "-isystem", os.path.join(_torch(), "include"),
             "-isystem", "/opt/rocm/include", "-I" + sysconfig.get_paths()["include"]]
 
 
-def _tensors_link(obj: str) -> list[str]:
+def _tensors_link(objs: list[str]) -> list[str]:
     libs = os.path.join(_torch(), "lib")
-    return [os.environ.get("CXX", "g++"), "-shared", "-o", TENSORS_OUT, obj, "-L" + os.path.dirname(OUT), "-l:libmoe_cache.so", "-L" + libs,
+    return [os.environ.get("CXX", "g++"), "-shared", "-o", TENSORS_OUT, *objs, "-L" + os.path.dirname(OUT), "-l:libmoe_cache.so", "-L" + libs,
             "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_hip", "-Wl,-rpath,$ORIGIN", "-Wl,-rpath," + libs]
 
 
@@ -93,20 +100,22 @@ def build(verbose: bool = True) -> str:
     objs = [os.path.join(OBJ_DIR, src + ".o") for src in SOURCES]
     procs = [(src, _start([hipcc, "-c", os.path.join(CSRC, src), "-o", obj] + COMMON + extra, verbose))
              for (src, extra), obj in zip(SOURCES.items(), objs)]
-    tensors_obj, tensors, missing = os.path.join(OBJ_DIR, "rows_torch.cpp.o"), None, "a compiler failed"
+    tensors_objs, tensors, missing = [os.path.join(OBJ_DIR, src + ".o") for src in TENSORS_SOURCES], [], "a compiler failed"
     try:
-        tensors = _start(_tensors_command(tensors_obj), verbose)
+        for src, obj in zip(TENSORS_SOURCES, tensors_objs):
+            tensors.append(_start(_tensors_command(src, obj), verbose))
     except (OSError, RuntimeError) as e:
         missing = str(e)
     compiled = [_done(src, p, verbose) for src, p in procs]
-    tensors_compiled = tensors is not None and _done("rows_torch.cpp", tensors, verbose)
+    tensors_done = [_done(src, p, verbose) for src, p in zip(TENSORS_SOURCES, tensors)]
+    tensors_compiled = len(tensors_done) == len(TENSORS_SOURCES) and all(tensors_done)
     if not all(compiled):
         raise RuntimeError("hipcc failed")
     cmd = [hipcc, "-shared", "-fPIC", "--offload-arch=gfx950", "-o", OUT] + objs
     if verbose:
         print("[build]", " ".join(cmd), flush=True)
     subprocess.check_call(cmd)
-    if not tensors_compiled or not _done("_rows.so", _start(_tensors_link(tensors_obj), verbose), verbose):
+    if not tensors_compiled or not _done("_rows.so", _start(_tensors_link(tensors_objs), verbose), verbose):
         raise RuntimeError(f"{OUT} is built, the row operators for tensors are not: {missing}")
     return OUT
 

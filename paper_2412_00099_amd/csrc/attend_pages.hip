@@ -1,0 +1,446 @@
+// Attention of one new token per sequence over a cache of pages.
+//
+//   z_j = scale <q, k_j> over the keys that are seen, y = sum_j exp(z_j - m) v_j / sum_j exp(z_j - m), m the largest so far
+//
+// Bound by memory: every key and value that is seen is read once.  The heads that share a key are up to 16 columns of a product:
+// S^T = K Q^T (rows: keys), O^T = V^T P^T (rows: dims), so that a lane keeps one head throughout, its maximum and its share of the sum
+// in registers, and P^T goes from the first product into the second without changing lanes: which keys stand for which summed index
+// of the second product is free, as long as V^T is read in the same order.  P is split into two parts of bf16 (what is left of a
+// value is 2^-17 of it): the second product costs nothing here.  8-bit codes are widened to bf16, which holds them exactly; their
+// scales go to the scores and to P.
+//
+// The work of all sequences is a line of tiles of 32 keys (sequence, group of heads, tile), cut into equal shares, one for each
+// wavefront of the launch, whatever the lengths are.  A wavefront keeps a ring of stages of its own in LDS, a stage the keys and
+// values of a tile, filled by loads that bypass the registers, and runs from one sequence into the next; no wavefront waits
+// for another.  What it has of a (sequence, group) that it does not have whole goes to the workspace: sums, maximum, sum of
+// exponentials; a second launch joins these.
+#include <algorithm>
+
+#include "attend.h"
+#include "rows.h"
+#include "tiles.h"
+
+namespace moe {
+namespace {
+
+constexpr int kTile = 32;        // keys
+constexpr int kWaves = 4;        // of a workgroup: one for each SIMD
+constexpr int kGroups = 256;     // workgroups: one for each compute unit
+constexpr int kWorkers = kGroups * kWaves;
+constexpr int kCols = 16;        // heads of a product
+
+// The workspace: the share of a worker, in tiles; per sequence the place of its first tile on the line; then, for each worker, what
+// it has of the (sequence, group) that began ahead of it and of the one that goes on behind it: [heads][dim] and [heads][2]
+struct Parts {
+  int64_t *share, *start;
+  float *sums, *stats;
+  int rows;  // heads of a group at most
+};
+__host__ __device__ inline int group_rows(int heads, int kv_heads) { return heads / kv_heads < kCols ? heads / kv_heads : kCols; }
+__host__ __device__ inline int64_t parts_head(int n_seqs) { return ((int64_t)n_seqs + 2) / 2 * 16; }
+__device__ __forceinline__ Parts parts_of(const AttendPagesParams &p) {
+  Parts r;
+  r.rows = group_rows(p.heads, p.c.kv_heads);
+  r.share = reinterpret_cast<int64_t *>(p.parts);
+  r.start = r.share + 1;
+  r.sums = reinterpret_cast<float *>(reinterpret_cast<uint8_t *>(p.parts) + parts_head(p.n_seqs));
+  r.stats = r.sums + (int64_t)2 * kWorkers * r.rows * p.c.dim;
+  return r;
+}
+
+typedef const __attribute__((address_space(4))) int32_t *Constant;  // read with scalar loads
+__device__ __forceinline__ Constant constant(const int32_t *p) { return (Constant)(uintptr_t)p; }
+
+// What is seen of a sequence: keys below `end` from `lo` on, and those below `sinks`
+struct Seen {
+  int end, lo, sink_tiles, first, tiles;  // tile t < sink_tiles is tile t of the cache, the others follow from `first` on
+};
+__device__ __forceinline__ Seen seen_of(const AttendPagesParams &p, int length) {
+  Seen s;
+  length = max(length, 0);
+  s.end = (int)min(min((int64_t)length, (int64_t)p.table_pages << p.c.page_bits), (int64_t)INT32_MAX - 2 * kTile);
+  s.lo = p.window > 0 ? max(length - p.window, 0) : 0;
+  s.first = s.lo / kTile;
+  const int last = (int)(((int64_t)s.end + kTile - 1) / kTile);
+  s.sink_tiles = min(min((int)(((int64_t)min(p.sinks, s.lo) + kTile - 1) / kTile), s.first), last);
+  s.tiles = s.sink_tiles + max(last - s.first, 0);
+  return s;
+}
+
+template <int CACHE, int DT>
+struct Attend {
+  static constexpr bool INT8 = CACHE == MOE_R_INT8;
+  static constexpr int EL = INT8 ? 1 : 2;
+  static constexpr int ROW = DT * EL, CHUNKS = ROW / 16;              // of a key in LDS
+  static constexpr int ROWS_LOAD = 64 / CHUNKS, LOADS = kTile / ROWS_LOAD;  // keys of a load, loads of a tile
+  static constexpr int MATRIX = kTile * ROW, STAGE = 2 * MATRIX, RING = 32768 / STAGE;
+  static constexpr int SCALES = INT8 ? 256 : 0;
+  static constexpr int WAVE_LDS = RING * (STAGE + SCALES);
+  static constexpr int AHEAD = (INT8 ? 1 : 0);                        // loads of a stage's scales
+  static constexpr int KS = DT / 32, DS = DT / 16;                    // steps over the dims, blocks of them
+
+  const AttendPagesParams p;
+  uint8_t *lds;
+  int lane, l, q, n_groups, per_kv;
+
+  // chunk c of key r lies at c ^ f(r): reads of 16 keys at four chunks, and transposed ones, spread over all banks
+  static __device__ __forceinline__ int swap(int r) { return CHUNKS == 16 ? r & 15 : CHUNKS == 8 ? (r >> 1) & 7 : (r >> 2) & 3; }
+
+  struct Spot {
+    int seq, group, tile;
+    Seen s;
+  };
+  __device__ __forceinline__ void open(Spot &a) const {
+    a.s = seen_of(p, constant(p.lengths)[a.seq]);
+  }
+  __device__ __forceinline__ void step(Spot &a) const {
+    if (++a.tile < a.s.tiles) return;
+    a.tile = 0;
+    if (++a.group < n_groups) return;
+    a.group = 0;
+    do {
+      if (++a.seq >= p.n_seqs) return;
+      open(a);
+    } while (a.s.tiles == 0);
+  }
+  __device__ __forceinline__ int tile_at(const Spot &a) const {
+    return uniform((a.tile < a.s.sink_tiles ? a.tile : a.s.first + a.tile - a.s.sink_tiles) * kTile);
+  }
+  // the page of 16 keys, -1: none
+  __device__ __forceinline__ int page_at(const Spot &a, int pos) const {
+    if (pos >= a.s.end) return -1;
+    const int id = constant(p.table)[(int64_t)a.seq * p.table_pages + (pos >> p.c.page_bits)];
+    return id < p.c.n_pages ? id : -1;
+  }
+
+  // Requests the keys and values of a tile; returns which of its halves there are.
+  template <bool VALUES>
+  __device__ __forceinline__ void request(const Spot &a, bool there, const int (&page)[2], int stage) const {
+    uint8_t *at = lds + stage * STAGE + (VALUES ? MATRIX : 0);
+    const int pos0 = tile_at(a), kv = a.group / per_kv, bytes = p.c.dim * EL;
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const int half = i * ROWS_LOAD / 16, r = i * ROWS_LOAD + lane / CHUNKS, pos = pos0 + r;
+      const int c = ((lane % CHUNKS) ^ swap(r)) * 16;
+      const int first = (pos0 + half * 16) & ((1 << p.c.page_bits) - 1);
+      const bool ok = there && page[half] >= 0;
+      const int64_t from = ok ? page[half] * p.c.page_stride + (((int64_t)kv << p.c.page_bits) + first) * p.c.dim : 0;
+      const int rows = ok ? min(a.s.end - (pos0 + half * 16), 16) : 0;
+      const bool mine = c < bytes && (pos >= a.s.lo || pos < p.sinks);
+      to_lds(words_of(static_cast<const uint8_t *>(VALUES ? p.c.v : p.c.k) + from * EL, rows * bytes),
+             mine ? (uint32_t)((r - half * 16) * bytes + c) : 0xf8000000u, 0, at + i * 1024);
+    }
+    if constexpr (INT8 && !VALUES) {
+      // lanes 0 .. 31: scales of the keys, the others: of the values.  (Where there are none: any; they are not used.)
+      const int r = lane & 31, id = page[r / 16], pos = pos0 + r;
+      const bool ok = there && id >= 0 && pos < a.s.end;
+      const int64_t from = ok ? (((int64_t)id * p.c.kv_heads + kv) << p.c.page_bits) + (pos & ((1 << p.c.page_bits) - 1)) : 0;
+      scale_to_lds((lane < 32 ? p.c.k_scale : p.c.v_scale) + from, lds + RING * STAGE + stage * SCALES);
+    }
+  }
+  static __device__ __forceinline__ void scale_to_lds(const float *from, uint8_t *to) {
+    const uint32_t at = uniform((uint32_t)reinterpret_cast<uintptr_t>(LDS_PTR(void, to)));
+    asm volatile(
+        "s_mov_b32 m0, %0\n\t"
+        "s_nop 3\n\t"
+        "global_load_lds_dword %1, off" ::"s"(at), "v"(from)
+        : "memory");
+  }
+  template <int N>
+  static __device__ __forceinline__ void landed() {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
+  }
+  static __device__ __forceinline__ i32x4 widen(i32x2 c) {  // 8 codes as bf16 (exact: the lower halves of the floats are zero)
+    i32x4 v;
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      const int u = c[w];
+      const float f0 = (float)(int8_t)u, f1 = (float)(int8_t)(u >> 8), f2 = (float)(int8_t)(u >> 16), f3 = (float)(u >> 24);
+      v[2 * w] = (int)__builtin_amdgcn_perm(__float_as_uint(f1), __float_as_uint(f0), 0x07060302);
+      v[2 * w + 1] = (int)__builtin_amdgcn_perm(__float_as_uint(f3), __float_as_uint(f2), 0x07060302);
+    }
+    return v;
+  }
+
+  __device__ __forceinline__ void run(int worker, uint8_t *mine) {
+    lds = mine;
+    lane = threadIdx.x & 63;
+    l = lane & 15;
+    q = lane >> 4;
+    const int per = p.heads / p.c.kv_heads;
+    per_kv = (per + kCols - 1) / kCols;
+    n_groups = p.c.kv_heads * per_kv;
+    // the line, and this worker's share of it
+    int64_t all = 0;
+    for (int s0 = 0; s0 < p.n_seqs; s0 += 64) all += s0 + lane < p.n_seqs ? seen_of(p, p.lengths[s0 + lane]).tiles : 0;
+    all = of_lane(sum_upto(all), 63) * n_groups;
+    const int64_t share = max((all + kWorkers - 1) / kWorkers, (int64_t)1), begin = worker * share;
+    const Parts parts = parts_of(p);
+    if (worker == 0 && lane == 0) *parts.share = share;
+    if (begin >= all) return;
+    int left = (int)min(share, all - begin);
+    Spot now{0, 0, 0, {}};
+    int64_t before = 0;
+    for (int s0 = 0; s0 < p.n_seqs; s0 += 64) {
+      const int tiles = s0 + lane < p.n_seqs ? seen_of(p, p.lengths[s0 + lane]).tiles : 0;
+      const int64_t past = before + sum_upto((int64_t)tiles) * n_groups;
+      const uint64_t behind = __ballot(past > begin);
+      if (behind != 0) {
+        const int at = __builtin_ctzll(behind), n = of_lane(tiles, at);
+        const int64_t in = begin - (of_lane(past, at) - (int64_t)n * n_groups);
+        now.seq = uniform(s0 + at);
+        now.group = uniform((int)(in / n));
+        now.tile = uniform((int)(in % n));
+        break;
+      }
+      before = of_lane(past, 63);
+    }
+    open(now);
+    int64_t line = begin;
+    Spot then = now;
+    int then_left = left;
+    uint32_t halves = 0;  // two bits a stage: which halves of the tiles that are under way there are
+    int pages[2];
+    // a stage's requests: keys (and scales), values
+    const auto look = [&] {
+      const int pos = tile_at(then);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) pages[h] = then_left > 0 ? page_at(then, pos + 16 * h) : -1;
+      halves = halves << 2 | (pages[0] >= 0 ? 1 : 0) | (pages[1] >= 0 ? 2 : 0);
+    };
+    const auto next = [&] {
+      if (then_left > 0 && --then_left > 0) step(then);
+    };
+    for (int i = 0; i < RING; ++i) {
+      look();
+      request<false>(then, then_left > 0, pages, i);
+      request<true>(then, then_left > 0, pages, i);
+      next();
+    }
+    // all requests behind those that are waited for
+    constexpr int BEHIND = (2 * RING - 1) * LOADS + (RING - 1) * AHEAD, BEHIND_V = (2 * RING - 1) * LOADS + RING * AHEAD;
+    f32x4 o[DS];
+    i32x4 qf[KS];
+    float top = -INFINITY, sum = 0.f;
+    const float scale = p.scale * 1.4426950408889634f;  // exponentials to the base 2
+    int head0 = 0, heads = 0, stage = 0;
+    bool fresh = true, from_start = false;
+    for (; left > 0; --left, ++line) {
+      if (fresh) {
+        const int kv = now.group / per_kv, part = now.group % per_kv;
+        head0 = kv * per + part * kCols;
+        heads = min(per - part * kCols, kCols);
+        from_start = now.tile == 0;
+        if (from_start && now.group == 0 && lane == 0) parts.start[now.seq] = line;
+        const uint16_t *qp = static_cast<const uint16_t *>(p.q.at) + now.seq * p.q.token + (head0 + min(l, heads - 1)) * p.q.head;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+          const int d = INT8 ? ((s >> 1) * 4 + q) * 16 + (s & 1) * 8 : (s * 4 + q) * 8;
+          qf[s] = i32x4{0, 0, 0, 0};
+          if (l < heads && d < p.c.dim) qf[s] = *reinterpret_cast<const i32x4 *>(qp + d);
+        }
+#pragma unroll
+        for (int d = 0; d < DS; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+        top = -INFINITY;
+        sum = 0.f;
+        fresh = false;
+      }
+      const uint8_t *kt = lds + stage * STAGE, *vt = kt + MATRIX;
+      const float *scales = reinterpret_cast<const float *>(lds + RING * STAGE + stage * SCALES);
+      landed<BEHIND>();
+      f32x4 z[2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        z[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+        const int r = t * 16 + l;
+        if constexpr (INT8) {
+#pragma unroll
+          for (int s = 0; s < KS / 2; ++s) {
+            const i32x4 codes = *reinterpret_cast<const i32x4 *>(kt + r * ROW + (((s * 4 + q) ^ swap(r)) * 16));
+            z[t] = mma(widen(i32x2{codes[0], codes[1]}), qf[2 * s], z[t]);
+            z[t] = mma(widen(i32x2{codes[2], codes[3]}), qf[2 * s + 1], z[t]);
+          }
+        } else {
+#pragma unroll
+          for (int s = 0; s < KS; ++s) z[t] = mma(*reinterpret_cast<const i32x4 *>(kt + r * ROW + (((s * 4 + q) ^ swap(r)) * 16)), qf[s], z[t]);
+        }
+      }
+      f32x4 ks[2], vs[2];
+      if constexpr (INT8) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          ks[t] = *reinterpret_cast<const f32x4 *>(scales + t * 16 + q * 4);
+          vs[t] = *reinterpret_cast<const f32x4 *>(scales + 32 + t * 16 + q * 4);
+        }
+      }
+      const uint32_t there = halves >> (2 * (RING - 1)) & 3;
+      const int pos0 = tile_at(now);
+      float w[8], most = top;
+      bool see[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int pos = pos0 + (i / 4) * 16 + q * 4 + i % 4;
+        see[i] = (there >> (i / 4) & 1) && pos < now.s.end && (pos >= now.s.lo || pos < p.sinks);
+        w[i] = z[i / 4][i % 4] * scale;
+        if constexpr (INT8) w[i] *= ks[i / 4][i % 4];
+        w[i] = see[i] ? w[i] : -INFINITY;
+        most = fmaxf(most, w[i]);
+      }
+      most = fmaxf(most, __shfl_xor(most, 16));
+      most = fmaxf(most, __shfl_xor(most, 32));
+      const float base = most == -INFINITY ? 0.f : most, shrink = __builtin_amdgcn_exp2f(top - base);
+      top = most;
+      sum *= shrink;
+      i32x4 hi, lo;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        w[i] = __builtin_amdgcn_exp2f(w[i] - base);
+        sum += w[i];
+        if constexpr (INT8) w[i] = see[i] ? w[i] * vs[i / 4][i % 4] : 0.f;
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        hi[i] = (int)pack_bf16(w[2 * i], w[2 * i + 1]);
+        lo[i] = (int)pack_bf16(w[2 * i] - bf16_lo(hi[i]), w[2 * i + 1] - bf16_hi(hi[i]));
+      }
+#pragma unroll
+      for (int d = 0; d < DS; ++d) o[d] *= shrink;
+      // (the keys have been read: the products above have waited for them)
+      look();
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      request<false>(then, then_left > 0, pages, stage);
+      landed<BEHIND_V>();
+#pragma unroll
+      for (int d = 0; d < DS; ++d) {
+        i32x4 v;
+        if constexpr (INT8) {
+          const int r8 = l >> 1, r = (r8 < 4 ? r8 : r8 + 12) + q * 4;
+          v = widen(__builtin_amdgcn_ds_read_tr8_b64_v2i32(LDS_PTR(i32x2, vt + r * ROW + ((d ^ swap(r)) * 16) + (l & 1) * 8)));
+        } else {
+          const int r = q * 4 + (l >> 2), c = d * 2 + ((l & 3) >> 1), in = (l & 1) * 8;
+          const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, vt + r * ROW + ((c ^ swap(r)) * 16) + in));
+          const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, vt + (r + 16) * ROW + ((c ^ swap(r + 16)) * 16) + in));
+          v = __builtin_bit_cast(i32x4, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+        }
+        o[d] = mma(v, hi, o[d]);
+        o[d] = mma(v, lo, o[d]);
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      request<true>(then, then_left > 0, pages, stage);
+      next();
+      stage = stage + 1 == RING ? 0 : stage + 1;
+      const bool ends = now.tile + 1 == now.s.tiles;
+      if (ends || left == 1) {
+        sum += __shfl_xor(sum, 16);
+        sum += __shfl_xor(sum, 32);
+        if (from_start && ends) {
+          const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
+          uint16_t *y = p.y + ((int64_t)now.seq * p.heads + head0 + l) * p.c.dim;
+#pragma unroll
+          for (int d = 0; d < DS; ++d) {
+            const int c = d * 16 + q * 4;
+            if (l < heads && c < p.c.dim)
+              *reinterpret_cast<rows_u32x2 *>(y + c) = rows_u32x2{pack_bf16(o[d][0] * inv, o[d][1] * inv), pack_bf16(o[d][2] * inv, o[d][3] * inv)};
+          }
+        } else {
+          const int64_t row = ((int64_t)worker * 2 + (from_start ? 1 : 0)) * parts.rows + l;
+#pragma unroll
+          for (int d = 0; d < DS; ++d) {
+            const int c = d * 16 + q * 4;
+            if (l < heads && c < p.c.dim) *reinterpret_cast<f32x4 *>(parts.sums + row * p.c.dim + c) = o[d];
+          }
+          if (l < heads && q == 0) {
+            parts.stats[row * 2] = top;
+            parts.stats[row * 2 + 1] = sum;
+          }
+        }
+        fresh = true;
+      }
+      if (left > 1) step(now);
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (nothing is under way into LDS when the workgroup ends)
+  }
+};
+
+template <int CACHE, int DT>
+__global__ __launch_bounds__(kWaves * 64) void attend_pages_kernel(const AttendPagesParams p) {
+  __shared__ __align__(16) uint8_t lds[kWaves * Attend<CACHE, DT>::WAVE_LDS];
+  const int wave = uniform(threadIdx.x >> 6);
+  Attend<CACHE, DT> a{p};
+  a.run(uniform(blockIdx.x * kWaves) + wave, lds + wave * Attend<CACHE, DT>::WAVE_LDS);
+}
+
+// One workgroup for each (sequence, head): its parts, or zeros where nothing is seen
+constexpr int kJoinBlock = 256;
+__global__ __launch_bounds__(kJoinBlock) void join_pages_kernel(const AttendPagesParams p) {
+  __shared__ float part[kJoinBlock / 32][MOE_ATTEND_MAX_DIM + 1];
+  __shared__ float tops[kJoinBlock / 64];
+  const int seq = blockIdx.x / p.heads, head = blockIdx.x % p.heads, tid = threadIdx.x;
+  const Seen s = seen_of(p, p.lengths[seq]);
+  uint16_t *y = p.y + ((int64_t)seq * p.heads + head) * p.c.dim;
+  if (s.tiles == 0) {
+    for (int d = tid; d < p.c.dim; d += kJoinBlock) y[d] = 0;
+    return;
+  }
+  const Parts parts = parts_of(p);
+  const int per = p.heads / p.c.kv_heads, per_kv = (per + kCols - 1) / kCols, kv = head / per, in = head % per;
+  const int64_t share = *parts.share, from = parts.start[seq] + (int64_t)(kv * per_kv + in / kCols) * s.tiles;
+  const int first = (int)(from / share), last = (int)((from + s.tiles - 1) / share);
+  if (first == last) return;  // (one worker had all of it)
+  const auto row_of = [&](int w) { return ((int64_t)w * 2 + (w == first ? 1 : 0)) * parts.rows + in % kCols; };
+  float top = -INFINITY;
+  for (int w = first + tid; w <= last; w += kJoinBlock) top = fmaxf(top, parts.stats[row_of(w) * 2]);
+#pragma unroll
+  for (int m = 1; m < 64; m <<= 1) top = fmaxf(top, __shfl_xor(top, m));
+  if ((tid & 63) == 0) tops[tid >> 6] = top;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kJoinBlock / 64; ++i) top = fmaxf(top, tops[i]);
+  const float base = top == -INFINITY ? 0.f : top;
+  const int strip = tid / 32, d = tid % 32 * 4;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  float sum = 0.f;
+  for (int w = first + strip; w <= last; w += kJoinBlock / 32) {
+    const int64_t row = row_of(w);
+    const float weight = __builtin_amdgcn_exp2f(parts.stats[row * 2] - base);
+    sum += weight * parts.stats[row * 2 + 1];
+    if (d < p.c.dim) acc += weight * *reinterpret_cast<const f32x4 *>(parts.sums + row * p.c.dim + d);
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (d < p.c.dim) part[strip][d + i] = acc[i];
+  if (tid % 32 == 0) part[strip][MOE_ATTEND_MAX_DIM] = sum;
+  __syncthreads();
+  if (tid < p.c.dim) {
+    float v = 0.f, n = 0.f;
+#pragma unroll
+    for (int i = 0; i < kJoinBlock / 32; ++i) {
+      v += part[i][tid];
+      n += part[i][MOE_ATTEND_MAX_DIM];
+    }
+    y[tid] = (uint16_t)pack_bf16(n > 0.f || n != n ? v / n : 0.f, 0.f);
+  }
+}
+
+template <int CACHE, int DT>
+hipError_t attend_with(const AttendPagesParams &p, hipStream_t s) {
+  attend_pages_kernel<CACHE, DT><<<kGroups, kWaves * 64, 0, s>>>(p);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+size_t attend_pages_bytes(int n_seqs, int heads, int kv_heads, int dim) {
+  return parts_head(n_seqs) + (size_t)2 * kWorkers * group_rows(heads, kv_heads) * (dim + 2) * sizeof(float);
+}
+
+hipError_t launch_attend_pages(const AttendPagesParams &p, int cache_fmt, hipStream_t s) {
+  hipError_t e;
+  if (cache_fmt == MOE_R_INT8) e = p.c.dim <= 64 ? attend_with<MOE_R_INT8, 64>(p, s) : attend_with<MOE_R_INT8, 128>(p, s);
+  else e = p.c.dim <= 64 ? attend_with<MOE_R_BF16, 64>(p, s) : attend_with<MOE_R_BF16, 128>(p, s);
+  if (e != hipSuccess) return e;
+  join_pages_kernel<<<p.n_seqs * p.heads, kJoinBlock, 0, s>>>(p);
+  return hipGetLastError();
+}
+
+}  // namespace moe

@@ -1,0 +1,132 @@
+"""What attention and the cache's pages refuse: every check comes before the GPU is touched, so the pointers here are never read."""
+import pytest
+import torch
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_2412_00099_amd import binding
+
+    return binding
+
+
+P = 0x10000  # never dereferenced
+
+
+def refused(B, call, good, **bad):
+    args = dict(good, **bad)
+    code = call(*args.values())
+    assert code == B.MOE_EINVAL, (bad, code)
+    assert B.moe_last_error()
+
+
+PLAN = dict(have=P, more=P, n_seqs=3, page=16, free=P, n_free=8, used=None, table=P, table_pages=4, offsets=P, slots=P, positions=P, n_tokens=9,
+            lengths=2 * P, used_out=P, stream=None)
+
+
+@pytest.mark.parametrize("bad", [
+    dict(have=None), dict(more=None), dict(free=None), dict(table=None), dict(offsets=None), dict(slots=None), dict(positions=None), dict(lengths=None),
+    dict(used_out=None), dict(n_seqs=-1), dict(n_seqs=16385), dict(page=0), dict(page=8), dict(page=17), dict(page=2048), dict(page=-16), dict(n_free=-1),
+    dict(table_pages=-1), dict(n_tokens=-1), dict(n_tokens=1 << 26), dict(have=P + 2), dict(used=P + 1), dict(used=P), dict(lengths=P), dict(table=P + 1)])
+def test_plan(B, bad):
+    refused(B, B.lib.moe_plan_pages, PLAN, **bad)
+
+
+CACHE = dict(k_pages=P, v_pages=P, cache_fmt=1, page_stride=2 * 16 * 64, n_pages=9, page=16, k_scale=None, v_scale=None)
+BAD_CACHE = [dict(k_pages=None), dict(v_pages=None), dict(cache_fmt=0), dict(cache_fmt=3), dict(page_stride=2 * 16 * 64 - 8), dict(page_stride=2 * 16 * 64 + 4),
+             dict(page_stride=(1 << 40) + 16), dict(n_pages=-1), dict(n_pages=1 << 27), dict(page=24), dict(page=8), dict(page=2048), dict(k_scale=P),
+             dict(v_scale=P), dict(cache_fmt=2), dict(cache_fmt=2, k_scale=P), dict(cache_fmt=2, k_scale=P + 2, v_scale=P), dict(k_pages=P + 8),
+             dict(cache_fmt=2, k_scale=P, v_scale=P, page_stride=2 * 16 * 64 + 8)]
+STORE = dict(k=P, v=P, fmt=1, k_stride=128, k_head=64, v_stride=128, v_head=64, slots=P, n_rows=5, kv=2, dim=64,
+             **{k: CACHE[k] for k in ("k_pages", "v_pages", "cache_fmt", "page_stride", "n_pages", "page", "k_scale", "v_scale")}, stream=None)
+
+
+@pytest.mark.parametrize("bad", BAD_CACHE + [dict(k=None), dict(v=None), dict(slots=None), dict(fmt=2), dict(fmt=-1), dict(n_rows=-1), dict(n_rows=1 << 26), dict(kv=0),
+                                             dict(kv=257), dict(dim=0), dict(dim=60), dict(dim=136), dict(k=P + 1), dict(slots=P + 2), dict(k_stride=-1), dict(v_head=-8)])
+def test_store(B, bad):
+    refused(B, B.lib.moe_store_pages, STORE, **bad)
+
+
+SEEN = dict(softmax_scale=0.125, window=0, sinks=0)
+BAD_SEEN = [dict(softmax_scale=0.0), dict(softmax_scale=-1.0), dict(softmax_scale=float("nan")), dict(softmax_scale=float("inf")), dict(window=-1), dict(sinks=-1)]
+PAGES = dict(q=P, q_stride=256, q_head=64, **CACHE, table=P, table_pages=4, lengths=P, n_seqs=3, heads=4, kv=2, dim=64, **SEEN, y=P, work=P,
+             work_bytes=1 << 28, stream=None)
+
+
+@pytest.mark.parametrize("bad", BAD_CACHE + BAD_SEEN + [
+    dict(q=None), dict(table=None), dict(lengths=None), dict(y=None), dict(work=None), dict(work_bytes=100), dict(work=P + 8), dict(heads=5), dict(heads=0),
+    dict(heads=512), dict(kv=0), dict(kv=-2), dict(dim=4), dict(dim=256), dict(n_seqs=-1), dict(n_seqs=16385), dict(table_pages=-1), dict(q_stride=63),
+    dict(q_stride=260), dict(q_stride=1 << 24), dict(q_head=32), dict(q_head=68), dict(q=P + 8), dict(y=P + 2), dict(lengths=P + 1)])
+def test_pages(B, bad):
+    refused(B, B.lib.moe_attend_pages, PAGES, **bad)
+
+
+ROWS = dict(q=P, q_stride=256, q_head=64, k=P, k_stride=128, k_head=64, v=P, v_stride=128, v_head=64, offsets=P, k_offsets=P, n_seqs=3, n_rows=100,
+            n_k_rows=300, heads=4, kv=2, dim=64, **SEEN)
+BAD_ROWS = BAD_SEEN + [
+    dict(q=None), dict(k=None), dict(v=None), dict(offsets=None), dict(k_offsets=None), dict(n_seqs=-1), dict(n_seqs=16385), dict(n_rows=-1),
+    dict(n_rows=1 << 26), dict(n_k_rows=1 << 26), dict(heads=3), dict(dim=12), dict(dim=136), dict(q_stride=8), dict(k_stride=132), dict(v_head=4),
+    dict(v_stride=1 << 24), dict(q=P + 2), dict(v=P + 8), dict(offsets=P + 2)]
+
+
+@pytest.mark.parametrize("bad", BAD_ROWS + [dict(y=None), dict(y=P + 4), dict(lse=P + 2)])
+def test_rows(B, bad):
+    refused(B, B.lib.moe_attend_rows, dict(ROWS, y=P, lse=None, stream=None), **bad)
+
+
+@pytest.mark.parametrize("bad", BAD_ROWS + [dict(y=None), dict(lse=None), dict(dy=None), dict(dq=None), dict(dk=None), dict(dv=None), dict(dy=P + 8),
+                                            dict(work=None), dict(work=P + 4), dict(work_bytes=100 * 4 * 4 - 1)])
+def test_rows_backward(B, bad):
+    refused(B, B.lib.moe_attend_rows_backward, dict(ROWS, y=P, lse=P, dy=P, dq=P, dk=P, dv=P, work=P, work_bytes=100 * 4 * 4, stream=None), **bad)
+
+
+def test_workspaces(B):
+    assert B.moe_attend_rows_backward_bytes(100, 4) == 1600 and B.moe_attend_rows_backward_bytes(0, 4) == 0
+    assert B.moe_attend_pages_bytes(0, 4, 2, 64) == 0 and B.moe_attend_pages_bytes(3, 4, 2, 64) > 0
+    assert B.moe_attend_pages_bytes(3, 4, 0, 64) == 0 and B.moe_attend_pages_bytes(3, 2, 4, 64) == 0
+
+
+def test_nothing_to_do(B):
+    assert B.lib.moe_store_pages(*dict(STORE, n_rows=0, k=None, v=None, slots=None).values()) == B.MOE_OK
+    assert B.lib.moe_attend_pages(*dict(PAGES, n_seqs=0, q=None, y=None, work=None, work_bytes=0).values()) == B.MOE_OK
+    assert B.lib.moe_attend_rows(*dict(ROWS, n_rows=0, q=None, y=None, lse=None, stream=None).values()) == B.MOE_OK
+
+
+def test_tensors_on_the_cpu_and_of_other_shapes(B):
+    import paper_2412_00099_amd as moe
+
+    bf16, i32 = torch.bfloat16, torch.int32
+    q, k = torch.zeros(5, 4, 64, dtype=bf16), torch.zeros(5, 2, 64, dtype=bf16)
+    at = torch.zeros(2, dtype=i32)
+    pages, table, n = torch.zeros(3, 2, 16, 64, dtype=bf16), torch.zeros(5, 2, dtype=i32), torch.zeros(5, dtype=i32)
+    calls = [
+        lambda: moe.attend_rows(q, k, k, at),                                # on the CPU
+        lambda: moe.attend_rows(q.float(), k, k, at),
+        lambda: moe.attend_rows(q, k, k[:4], at),
+        lambda: moe.attend_rows(q, k[..., :32], k[..., :32], at),
+        lambda: moe.attend_rows(q[0], k, k, at),
+        lambda: moe.attend_rows(q, k, k, at.long()),
+        lambda: moe.attend_rows(q, k[:3], k[:3], at),
+        lambda: moe.attend_rows(q.transpose(1, 2), k, k, at),
+        lambda: moe.attend_rows(q, k, k, at, k_offsets=at[:1]),
+        lambda: moe.attend_rows_backward(q, k, k, at, q, torch.zeros(4, 4), q),
+        lambda: moe.attend_rows_backward(q, k, k, at, q.float(), torch.zeros(4, 5), q),
+        lambda: moe.attend_pages(q, pages, pages, table, n),
+        lambda: moe.attend_pages(q, pages, pages[:2], table, n),
+        lambda: moe.attend_pages(q, pages, pages.float(), table, n),
+        lambda: moe.attend_pages(q, pages.transpose(1, 2), pages.transpose(1, 2), table, n),
+        lambda: moe.attend_pages(q, pages, pages, table[:4], n),
+        lambda: moe.attend_pages(q, pages, pages, table, n, torch.zeros(3, 2, 8), torch.zeros(3, 2, 16)),
+        lambda: moe.store_pages(k, k, n, pages, pages),
+        lambda: moe.store_pages(k, k.float(), n, pages, pages),
+        lambda: moe.store_pages(q, q, n, pages, pages),
+        lambda: moe.store_pages(k, k, n[:4], pages, pages),
+        lambda: moe.plan_pages(n, n, table, n, 16, 5),
+        lambda: moe.plan_pages(n, n[:4], table, n, 16, 5),
+        lambda: moe.plan_pages(n, n, table[:, :1], n, 16, 5),
+        lambda: moe.plan_pages(n, n, table, n, 16, 5, used=n),
+    ]
+    for i, call in enumerate(calls):
+        with pytest.raises(ValueError):
+            call()
+            print(i)
