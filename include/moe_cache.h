@@ -440,12 +440,13 @@ int moe_experts_rows_backward(int32_t weight_fmt, int32_t hidden, int32_t inter,
  *   n_kv_heads, head_dim) bytes, 16-byte aligned, of this call alone until it is done.
  * moe_attend_rows: packed sequences.  Sequence i has the rows offsets[i] .. offsets[i + 1] - 1 of q and y, and k_offsets[i] ..
  *   k_offsets[i + 1] - 1 of k and v (k_offsets_dev NULL: the same); its queries are its last rows, so that query r of nq is at position
- *   nk - nq + r (one ahead of the first key sees nothing).  y_dev dense [n_rows, n_heads, head_dim]; lse_dev fp32 [n_heads, n_rows], for
- *   the backward, or NULL.  Rows of no sequence: y is 0.
- * moe_attend_rows_backward: from dy the gradients of q, k and v, dense, bf16 (rows of no sequence: 0).  y, lse: as the forward left
- *   them.  P = exp(z - lse), dv = sum P dy, dz = P (<dy, v> - <dy, y>), dq = softmax_scale sum dz k, dk = softmax_scale sum dz q, sums
+ *   nk - nq + r (one ahead of the first key sees nothing).  y_dev dense [n_rows, n_heads, head_dim].  For the backward, or NULL:
+ *   y_low_dev (as y_dev): bf16 of what the rounding of y leaves; lse_dev fp32 [n_heads, n_rows].  Rows of no sequence: y is 0, the
+ *   others are left alone.
+ * moe_attend_rows_backward: from dy the gradients of q, k and v, dense, bf16 (rows of no sequence: 0).  y, y_low, lse: as the forward left
+ *   them (y_low_dev NULL: y is taken as it is, which makes the error of dq and dk about a tenth larger).  P = exp(z - lse), dv = sum P dy, dz = P (<dy, v> - <dy, y>), dq = softmax_scale sum dz k, dk = softmax_scale sum dz q, sums
  *   over the heads of a group and over all queries in a fixed order.  P and dz are rounded to bf16 for the matrix cores.  y and dy
- *   dense.  Workspace: moe_attend_rows_backward_bytes(n_rows, n_heads) bytes, 16-byte aligned. */
+ *   dense.  The workspace: moe_attend_rows_backward_bytes bytes, 16-byte aligned, of this call alone until it is done. */
 int moe_plan_pages(const int32_t *have_dev, const int32_t *more_dev, int32_t n_seqs, int32_t page, const int32_t *free_dev, int32_t n_free,
                    const int32_t *used_dev, int32_t *table_dev, int32_t table_pages, int32_t *offsets_dev, int32_t *slots_dev,
                    int32_t *positions_dev, int32_t n_tokens, int32_t *lengths_dev, int32_t *used_out_dev, void *stream);
@@ -462,13 +463,13 @@ int moe_attend_pages(const void *q_dev, int64_t q_stride, int64_t q_head_stride,
 int moe_attend_rows(const void *q_dev, int64_t q_stride, int64_t q_head_stride, const void *k_dev, int64_t k_stride, int64_t k_head_stride,
                     const void *v_dev, int64_t v_stride, int64_t v_head_stride, const int32_t *offsets_dev, const int32_t *k_offsets_dev,
                     int32_t n_seqs, int32_t n_rows, int32_t n_k_rows, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
-                    float softmax_scale, int32_t window, int32_t sinks, void *y_dev, float *lse_dev, void *stream);
-size_t moe_attend_rows_backward_bytes(int32_t n_rows, int32_t n_heads);
+                    float softmax_scale, int32_t window, int32_t sinks, void *y_dev, void *y_low_dev, float *lse_dev, void *stream);
+size_t moe_attend_rows_backward_bytes(int32_t n_rows, int32_t n_k_rows, int32_t n_seqs, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim);
 int moe_attend_rows_backward(const void *q_dev, int64_t q_stride, int64_t q_head_stride, const void *k_dev, int64_t k_stride,
                              int64_t k_head_stride, const void *v_dev, int64_t v_stride, int64_t v_head_stride, const int32_t *offsets_dev,
                              const int32_t *k_offsets_dev, int32_t n_seqs, int32_t n_rows, int32_t n_k_rows, int32_t n_heads,
                              int32_t n_kv_heads, int32_t head_dim, float softmax_scale, int32_t window, int32_t sinks, const void *y_dev,
-                             const float *lse_dev, const void *dy_dev, void *dq_dev, void *dk_dev, void *dv_dev, void *workspace_dev,
+                             const void *y_low_dev, const float *lse_dev, const void *dy_dev, void *dq_dev, void *dk_dev, void *dv_dev, void *workspace_dev,
                              size_t workspace_bytes, void *stream);
 
 const char *moe_last_error(void);

@@ -13,7 +13,7 @@ try:
         norm_rows, norm_rows_backward, sort_tokens,
     )
     from .attention import (  # noqa: F401
-        PagePlan, attend_pages, attend_rows, attend_rows_backward, plan_pages, store_pages,
+        KeptAttention, PagePlan, attend_pages, attend_rows, attend_rows_backward, plan_pages, store_pages,
     )
 except ImportError as e:
     _rows_missing = str(e)
@@ -21,6 +21,6 @@ except ImportError as e:
     def __getattr__(name):
         if name in ("rows", "KeptExperts", "NormedRows", "TokenOrder", "combine_rows", "combine_rows_backward", "experts_rows",
                     "experts_rows_backward", "gather_rows", "norm_rows", "norm_rows_backward", "sort_tokens",
-                    "attention", "PagePlan", "attend_pages", "attend_rows", "attend_rows_backward", "plan_pages", "store_pages"):
+                    "attention", "KeptAttention", "PagePlan", "attend_pages", "attend_rows", "attend_rows_backward", "plan_pages", "store_pages"):
             raise ImportError(_rows_missing)
         raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

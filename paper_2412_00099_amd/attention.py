@@ -23,6 +23,13 @@ class PagePlan(NamedTuple):
     used: torch.Tensor       # [1]: how far the free pages are used up; more than there are: some tokens got no page
 
 
+class KeptAttention(NamedTuple):
+    """What the backward of attend_rows needs of the forward, beside y."""
+
+    lse: torch.Tensor         # [heads, rows]: log of the sums of exponentials
+    low: torch.Tensor | None  # [rows, heads, dim]: what the rounding of y leaves
+
+
 def plan_pages(have, more, table, free, page, n_tokens, *, used=None) -> PagePlan:
     """Pages for `more` new tokens of sequences that have `have` (int32 [sequences]), taken from `free` (int32, page ids) from
     element `used` (int32 [1], None: the first) on, and written into `table` (int32 [sequences, pages]) in place.  n_tokens: rows of
@@ -45,12 +52,12 @@ def attend_pages(q, k_pages, v_pages, table, lengths, k_scale=None, v_scale=None
 
 def attend_rows(q, k, v, offsets, *, k_offsets=None, scale=None, window=0, sinks=0, keep=False):
     """y [rows, heads, dim]: causal attention within each sequence, rows offsets[i] .. offsets[i + 1] - 1 of q over rows k_offsets[i] ..
-    k_offsets[i + 1] - 1 of k and v (None: the same rows); the queries are the last rows of their sequence.  keep: returns (y, lse
-    [heads, rows]) for the backward, else y."""
-    y, lse = _rows.attend_rows(q, k, v, offsets, k_offsets, scale, window, sinks, keep)
-    return (y, lse) if keep else y
+    k_offsets[i + 1] - 1 of k and v (None: the same rows); the queries are the last rows of their sequence.  keep: returns (y,
+    KeptAttention) for the backward, else y."""
+    y, lse, low = _rows.attend_rows(q, k, v, offsets, k_offsets, scale, window, sinks, keep)
+    return (y, KeptAttention(lse, low)) if keep else y
 
 
-def attend_rows_backward(q, k, v, offsets, y, lse, dy, *, k_offsets=None, scale=None, window=0, sinks=0):
-    """(gradient of q, of k, of v); y, lse: attend_rows' results with the same arguments; dy dense."""
-    return _rows.attend_rows_backward(q, k, v, offsets, y, lse, dy, k_offsets, scale, window, sinks)
+def attend_rows_backward(q, k, v, offsets, y, kept, dy, *, k_offsets=None, scale=None, window=0, sinks=0):
+    """(gradient of q, of k, of v); y, kept: attend_rows' results with the same arguments; dy dense."""
+    return _rows.attend_rows_backward(q, k, v, offsets, y, kept.lse, kept.low, dy, k_offsets, scale, window, sinks)

@@ -43,19 +43,30 @@ size_t attend_pages_bytes(int n_seqs, int heads, int kv_heads, int dim);
 hipError_t launch_attend_pages(const AttendPagesParams &p, int cache_fmt, hipStream_t s);
 
 // ---- attend_rows.hip ----
+// Some of the queries that see some keys: see attend_rows.hip
+struct KeyPiece {
+  int sequence, part, first, count;  // tiles `first` on of the list
+  int index, of, slot;               // which of how many pieces; where the sums of the list's first piece are (of > 1)
+};
 struct AttendRowsParams {
   HeadRows q, k, v;
   const int32_t *offsets, *k_offsets;
   int32_t n_seqs, n_rows, n_k_rows, heads, kv_heads, dim, window, sinks;
   float scale;
   uint16_t *y;
-  float *lse;  // [heads][n_rows], forward: may be NULL
+  uint16_t *low;  // y's rounding, or NULL
+  float *lse;     // [heads][n_rows], forward: may be NULL
   // backward
   const uint16_t *dy;
   uint16_t *dq, *dk, *dv;
   float *delta;  // [heads][n_rows]: <dy, y>
+  int32_t *n_pieces;
+  KeyPiece *pieces;
+  float *sums;  // [max_slots][kv_heads][128 keys][2][dim]: of pieces
+  int32_t max_pieces, max_slots;
 };
 hipError_t launch_attend_rows(const AttendRowsParams &p, hipStream_t s);
-hipError_t launch_attend_rows_backward(const AttendRowsParams &p, hipStream_t s);
+size_t attend_rows_backward_bytes(int n_rows, int n_k_rows, int n_seqs, int heads, int kv_heads, int dim);
+hipError_t launch_attend_rows_backward(const AttendRowsParams &p, uint8_t *workspace, hipStream_t s);
 
 }  // namespace moe

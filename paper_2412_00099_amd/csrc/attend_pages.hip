@@ -24,10 +24,11 @@ namespace moe {
 namespace {
 
 constexpr int kTile = 32;        // keys
-constexpr int kWaves = 4;        // of a workgroup: one for each SIMD
+constexpr int kWaves = 8;        // of a workgroup: two for each SIMD
 constexpr int kGroups = 256;     // workgroups: one for each compute unit
 constexpr int kWorkers = kGroups * kWaves;
 constexpr int kCols = 16;        // heads of a product
+constexpr uint32_t kNowhere = 0xf8000000u;
 
 // The workspace: the share of a worker, in tiles; per sequence the place of its first tile on the line; then, for each worker, what
 // it has of the (sequence, group) that began ahead of it and of the one that goes on behind it: [heads][dim] and [heads][2]
@@ -73,7 +74,7 @@ struct Attend {
   static constexpr int EL = INT8 ? 1 : 2;
   static constexpr int ROW = DT * EL, CHUNKS = ROW / 16;              // of a key in LDS
   static constexpr int ROWS_LOAD = 64 / CHUNKS, LOADS = kTile / ROWS_LOAD;  // keys of a load, loads of a tile
-  static constexpr int MATRIX = kTile * ROW, STAGE = 2 * MATRIX, RING = 32768 / STAGE;
+  static constexpr int MATRIX = kTile * ROW, STAGE = 2 * MATRIX, RING = 16384 / STAGE;
   static constexpr int SCALES = INT8 ? 256 : 0;
   static constexpr int WAVE_LDS = RING * (STAGE + SCALES);
   static constexpr int AHEAD = (INT8 ? 1 : 0);                        // loads of a stage's scales
@@ -110,31 +111,51 @@ struct Attend {
   __device__ __forceinline__ int page_at(const Spot &a, int pos) const {
     if (pos >= a.s.end) return -1;
     const int id = constant(p.table)[(int64_t)a.seq * p.table_pages + (pos >> p.c.page_bits)];
-    return id < p.c.n_pages ? id : -1;
+    return id < p.c.n_pages ? max(id, -1) : -1;
   }
 
-  // Requests the keys and values of a tile; returns which of its halves there are.
+  // A tile that is requested: where its halves of 16 keys begin in the cache (keys and values alike), how many bytes they have
+  struct Place {
+    int pos, kv;
+    bool all;  // every key that is there is seen
+    int id[2];
+    int64_t from[2];
+    uint32_t bytes[2];
+  };
+  // `there` false: nothing; its loads bring zeros
+  __device__ __forceinline__ Place place_of(const Spot &a, bool there) const {
+    Place r;
+    r.pos = there ? tile_at(a) : 0;
+    r.kv = a.group / per_kv;
+    r.all = r.pos >= a.s.lo;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int pos = r.pos + 16 * h, id = there ? page_at(a, pos) : -1;
+      r.id[h] = id;
+      r.from[h] = id < 0 ? 0 : id * p.c.page_stride + (((int64_t)r.kv << p.c.page_bits) + (pos & ((1 << p.c.page_bits) - 1))) * p.c.dim;
+      r.bytes[h] = id < 0 ? 0 : min(a.s.end - pos, 16) * p.c.dim * EL;
+    }
+    return r;
+  }
+  // Requests its keys or values.  Keys that are not seen arrive as zeros: they may hold anything.
   template <bool VALUES>
-  __device__ __forceinline__ void request(const Spot &a, bool there, const int (&page)[2], int stage) const {
-    uint8_t *at = lds + stage * STAGE + (VALUES ? MATRIX : 0);
-    const int pos0 = tile_at(a), kv = a.group / per_kv, bytes = p.c.dim * EL;
+  __device__ __forceinline__ void request(const Spot &a, const Place &at, int stage) const {
+    uint8_t *to = lds + stage * STAGE + (VALUES ? MATRIX : 0);
+    const uint8_t *base = static_cast<const uint8_t *>(VALUES ? p.c.v : p.c.k);
+    const int bytes = p.c.dim * EL;
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
-      const int half = i * ROWS_LOAD / 16, r = i * ROWS_LOAD + lane / CHUNKS, pos = pos0 + r;
-      const int c = ((lane % CHUNKS) ^ swap(r)) * 16;
-      const int first = (pos0 + half * 16) & ((1 << p.c.page_bits) - 1);
-      const bool ok = there && page[half] >= 0;
-      const int64_t from = ok ? page[half] * p.c.page_stride + (((int64_t)kv << p.c.page_bits) + first) * p.c.dim : 0;
-      const int rows = ok ? min(a.s.end - (pos0 + half * 16), 16) : 0;
-      const bool mine = c < bytes && (pos >= a.s.lo || pos < p.sinks);
-      to_lds(words_of(static_cast<const uint8_t *>(VALUES ? p.c.v : p.c.k) + from * EL, rows * bytes),
-             mine ? (uint32_t)((r - half * 16) * bytes + c) : 0xf8000000u, 0, at + i * 1024);
+      const int half = i * ROWS_LOAD / 16, r = i * ROWS_LOAD + lane / CHUNKS, c = ((lane % CHUNKS) ^ swap(r)) * 16;
+      uint32_t off = c < bytes ? (uint32_t)((r - half * 16) * bytes + c) : kNowhere;
+      if (!at.all && at.pos + r < a.s.lo && at.pos + r >= p.sinks) off = kNowhere;
+      to_lds(words_of(base + at.from[half] * EL, at.bytes[half]), off, 0, to + i * 1024);
     }
     if constexpr (INT8 && !VALUES) {
       // lanes 0 .. 31: scales of the keys, the others: of the values.  (Where there are none: any; they are not used.)
-      const int r = lane & 31, id = page[r / 16], pos = pos0 + r;
-      const bool ok = there && id >= 0 && pos < a.s.end;
-      const int64_t from = ok ? (((int64_t)id * p.c.kv_heads + kv) << p.c.page_bits) + (pos & ((1 << p.c.page_bits) - 1)) : 0;
+      const int r = lane & 31, pos = at.pos + r;
+      int64_t from = 0;
+      if ((r < 16 ? at.bytes[0] : at.bytes[1]) != 0 && pos < a.s.end)
+        from = (((int64_t)(r < 16 ? at.id[0] : at.id[1]) * p.c.kv_heads + at.kv) << p.c.page_bits) + (pos & ((1 << p.c.page_bits) - 1));
       scale_to_lds((lane < 32 ? p.c.k_scale : p.c.v_scale) + from, lds + RING * STAGE + stage * SCALES);
     }
   }
@@ -200,21 +221,19 @@ struct Attend {
     Spot then = now;
     int then_left = left;
     uint32_t halves = 0;  // two bits a stage: which halves of the tiles that are under way there are
-    int pages[2];
+    Place to_come;
     // a stage's requests: keys (and scales), values
-    const auto look = [&] {
-      const int pos = tile_at(then);
-#pragma unroll
-      for (int h = 0; h < 2; ++h) pages[h] = then_left > 0 ? page_at(then, pos + 16 * h) : -1;
-      halves = halves << 2 | (pages[0] >= 0 ? 1 : 0) | (pages[1] >= 0 ? 2 : 0);
+    const auto look = [&]() MOE_ROWS_INLINE {
+      to_come = place_of(then, then_left > 0);
+      halves = halves << 2 | (to_come.bytes[0] ? 1 : 0) | (to_come.bytes[1] ? 2 : 0);
     };
-    const auto next = [&] {
+    const auto next = [&]() MOE_ROWS_INLINE {
       if (then_left > 0 && --then_left > 0) step(then);
     };
     for (int i = 0; i < RING; ++i) {
       look();
-      request<false>(then, then_left > 0, pages, i);
-      request<true>(then, then_left > 0, pages, i);
+      request<false>(then, to_come, i);
+      request<true>(then, to_come, i);
       next();
     }
     // all requests behind those that are waited for
@@ -308,7 +327,7 @@ struct Attend {
       // (the keys have been read: the products above have waited for them)
       look();
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      request<false>(then, then_left > 0, pages, stage);
+      request<false>(then, to_come, stage);
       landed<BEHIND_V>();
 #pragma unroll
       for (int d = 0; d < DS; ++d) {
@@ -326,7 +345,7 @@ struct Attend {
         o[d] = mma(v, lo, o[d]);
       }
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      request<true>(then, then_left > 0, pages, stage);
+      request<true>(then, to_come, stage);
       next();
       stage = stage + 1 == RING ? 0 : stage + 1;
       const bool ends = now.tile + 1 == now.s.tiles;
@@ -363,7 +382,7 @@ struct Attend {
 };
 
 template <int CACHE, int DT>
-__global__ __launch_bounds__(kWaves * 64) void attend_pages_kernel(const AttendPagesParams p) {
+__global__ __launch_bounds__(kWaves * 64, 2) void attend_pages_kernel(const AttendPagesParams p) {
   __shared__ __align__(16) uint8_t lds[kWaves * Attend<CACHE, DT>::WAVE_LDS];
   const int wave = uniform(threadIdx.x >> 6);
   Attend<CACHE, DT> a{p};

@@ -11,12 +11,15 @@
 // The other side's rows go through LDS in tiles of 64, two at a time, one computed while the next one is loaded, for all four
 // wavefronts of a workgroup.
 //
-// P and dZ are rounded to bf16 for the matrix cores: in two parts each they would cost half as much again, and the error that they
-// make (2^-9 of single terms of a sum, at random) is below that of the rounding of the results.
+// P and dZ are rounded to bf16 for the matrix cores; in two parts each they would cost a third of the products more.  The error that
+// this makes is as large as that of the results' own rounding (together 0.0022 to 0.0025 of their size, 0.0017 for the results' alone).  delta is
+// the same for all keys of a query, and with Y as it is rounded it was the next largest part (0.0027): the forward keeps what the
+// rounding of Y leaves, in bf16.
 //
 // Which sequence and which of its rows a workgroup has is worked out from the offsets on the device.  Loads go through buffer
 // resources that end where the sequence ends: what lies beyond arrives as zeros.
 #include <algorithm>
+#include <type_traits>
 
 #include "attend.h"
 #include "rows.h"
@@ -30,7 +33,7 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 constexpr int kWaves = 4, kBlock = kWaves * 64;
 constexpr int kOwn = 32 * kWaves;  // rows of a workgroup
 constexpr int kTile = 64;          // rows of the other side in LDS
-constexpr uint32_t kNowhere = 0xf8000000u;
+constexpr uint32_t kNowhere = 0xc0000000u;  // behind every tile, and with what is added to it still within 32 bits
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 __device__ __forceinline__ f32x16 mma(i32x4 a, i32x4 b, f32x16 c) {
@@ -91,45 +94,59 @@ __device__ __forceinline__ void clear_rows(const int32_t *offsets, int n_seqs, i
   }
 }
 
-// Rows of DT values in LDS.  Chunk c of row r lies at c ^ f(r): both kinds of reads (16 rows at one chunk; 8 rows of four chunks,
+__device__ __forceinline__ uint32_t lds_at(const uint8_t *p) { return (uint32_t)reinterpret_cast<uintptr_t>(LDS_PTR(void, p)); }
+// Rows of up to KS * 16 values in LDS, 128 or 256 bytes each.  Chunk c of row r lies at c ^ f(r): both kinds of reads (16 rows at one chunk; 8 rows of four chunks,
 // transposed) spread over all banks
-template <int DT>
+template <int STEPS>
 struct Tiles {
-  static constexpr int ROW = DT * 2, CHUNKS = ROW / 16, ROWS_LOAD = 64 / CHUNKS;
+  static constexpr int KS = STEPS, DS = (KS + 1) / 2;  // steps of 16 over the dims, blocks of 32 of them
+  static constexpr int ROW = KS <= 4 ? 128 : 256, CHUNKS = ROW / 16, ROWS_LOAD = 64 / CHUNKS;
   static constexpr int BYTES = kTile * ROW, LOADS = BYTES / 1024 / kWaves;  // of a wavefront for a tile
-  static constexpr int KS = DT / 16, DS = DT / 32;                          // steps over the dims, blocks of them
   static __device__ __forceinline__ int swap(int r) { return CHUNKS == 16 ? ((r & 3) << 2) | ((r >> 2) & 3) : ((r & 2) << 1) | ((r >> 2) & 3); }
 
-  // where a wavefront's loads of a tile come from, per lane
+  // Where the lane's first load of a tile comes from: the row and the chunk in bytes.  Load i is ROWS_LOAD rows further on, its
+  // chunk exchanged with another number.
   struct Source {
-    uint32_t off[LOADS];
+    uint32_t row, chunk;
   };
-  static __device__ __forceinline__ Source source(int wave, int lane, int64_t token, int dim) {
-    Source s;
-#pragma unroll
-    for (int i = 0; i < LOADS; ++i) {
-      const int r = (wave * LOADS + i) * ROWS_LOAD + lane / CHUNKS, c = ((lane % CHUNKS) ^ swap(r)) * 16;
-      s.off[i] = c < dim * 2 ? (uint32_t)(r * (uint32_t)token * 2 + c) : kNowhere;
-    }
-    return s;
+  static __device__ __forceinline__ Source source(int wave, int lane, int64_t token) {
+    const int r = wave * LOADS * ROWS_LOAD + lane / CHUNKS;
+    return {(uint32_t)r * (uint32_t)token * 2, (uint32_t)((lane % CHUNKS) ^ swap(r)) * 16};
   }
   // the tile's rows from `from` on, `rows` of them (or fewer than none)
-  static __device__ __forceinline__ void request(const Source &s, const uint16_t *from, int rows, int64_t token, int dim, int wave, uint8_t *to) {
+  static __device__ __forceinline__ void request(Source s, const uint16_t *from, int rows, int64_t token, int dim, int wave, uint8_t *to) {
     const i32x4 b = words_of(from, rows > 0 ? (uint32_t)((min(rows, kTile) - 1) * (uint32_t)token * 2 + dim * 2) : 0u);
+    asm("" : "+v"(s.row), "+v"(s.chunk));  // (hidden, see Reader)
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i) to_lds(b, s.off[i], 0, to + (wave * LOADS + i) * 1024);
+    for (int i = 0; i < LOADS; ++i) {
+      const uint32_t c = s.chunk ^ (i * (ROW == 256 ? 16 : 32));
+      to_lds(b, c < (uint32_t)dim * 2 ? s.row + c : kNowhere, (uint32_t)i * ROWS_LOAD * (uint32_t)token * 2, to + (wave * LOADS + i) * 1024);
+    }
   }
-  // 32 rows from r0 on as rows of a product, step s over the dims
-  static __device__ __forceinline__ i32x4 rows(const uint8_t *t, int r0, int s, int lane) {
-    const int r = r0 + (lane & 31);
-    return *reinterpret_cast<const i32x4 *>(t + r * ROW + (((s * 2 + (lane >> 5)) ^ swap(r)) * 16));
+  // Where the lane reads in a tile: of 32 rows at one chunk (step s over the dims: at ^ s * 32), transposed of 4 rows of four
+  // chunks (block d of the dims: at ^ d * 64; the rows 8 further on: at ^ 32).  What is read follows from these with one operation.
+  // hide: from the compiler, which would hold all of them in registers where there are none left.
+  struct Reader {
+    uint32_t rows, columns;
+    __device__ __forceinline__ Reader(uint32_t tile, const Reader &lane, bool hide) : rows(tile + lane.rows), columns(tile + lane.columns) {
+      if (hide) asm("" : "+v"(rows), "+v"(columns));
+    }
+    __device__ __forceinline__ Reader(int lane) {
+      rows = (lane & 31) * ROW + (((lane >> 5) ^ swap(lane & 31)) * 16);
+      const int r = 4 * (lane >> 5) + ((lane & 15) >> 2), c = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
+      columns = r * ROW + ((c ^ swap(r)) * 16) + (lane & 1) * 8;
+    }
+  };
+  // rows r0 .. r0 + 31 as rows of a product, step s over the dims; `in` bytes behind the tile
+  static __device__ __forceinline__ i32x4 rows(const Reader &a, uint32_t in, int r0, int s) {
+    return *(LDS_PTR(i32x4, (uintptr_t)((a.rows ^ (s * 32)) + in + r0 * ROW)));
   }
   // dims d * 32 .. as rows of a product, summed over the 16 rows from r0 on
-  static __device__ __forceinline__ i32x4 columns(const uint8_t *t, int r0, int d, int lane) {
-    const int r = r0 + 4 * (lane >> 5) + ((lane & 15) >> 2), c = d * 4 + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1), in = (lane & 1) * 8;
-    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, t + r * ROW + ((c ^ swap(r)) * 16) + in));
-    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, t + (r + 8) * ROW + ((c ^ swap(r + 8)) * 16) + in));
-    return __builtin_bit_cast(i32x4, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+  static __device__ __forceinline__ i32x4 columns(const Reader &a, uint32_t in, int r0, int d) {
+    const uint32_t at = a.columns ^ (d * 64);
+    const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, (uintptr_t)(at + in + r0 * ROW)));
+    const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, (uintptr_t)((at ^ 32) + in + (r0 + 8) * ROW)));
+    return __builtin_bit_cast(i32x4, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
   }
   // a wavefront's own rows as columns of a product: lane's row is `at` (there: it exists)
   static __device__ __forceinline__ void own(const uint16_t *at, bool there, int dim, int lane, i32x4 (&f)[KS]) {
@@ -140,15 +157,18 @@ struct Tiles {
       if (there && d < dim) f[s] = *reinterpret_cast<const i32x4 *>(at + d);
     }
   }
-  // the lane's column of a result, times v
-  static __device__ __forceinline__ void store(uint16_t *at, bool there, int dim, int lane, const f32x16 (&o)[DS], float v) {
+  // the lane's column of a result, times v; low: and what its rounding leaves, unless nullptr
+  static __device__ __forceinline__ void store(uint16_t *at, uint16_t *low, bool there, int dim, int lane, const f32x16 (&o)[DS], float v) {
 #pragma unroll
     for (int d = 0; d < DS; ++d)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int c = d * 32 + i * 8 + (lane >> 5) * 4;
-        if (there && c < dim)
-          *reinterpret_cast<rows_u32x2 *>(at + c) = rows_u32x2{pack_bf16(o[d][4 * i] * v, o[d][4 * i + 1] * v), pack_bf16(o[d][4 * i + 2] * v, o[d][4 * i + 3] * v)};
+        if (!there || c >= dim) continue;
+        const float a = o[d][4 * i] * v, b = o[d][4 * i + 1] * v, e = o[d][4 * i + 2] * v, f = o[d][4 * i + 3] * v;
+        const rows_u32x2 r = {pack_bf16(a, b), pack_bf16(e, f)};
+        *reinterpret_cast<rows_u32x2 *>(at + c) = r;
+        if (low) *reinterpret_cast<rows_u32x2 *>(low + c) = rows_u32x2{pack_bf16(a - bf16_lo(r[0]), b - bf16_hi(r[0])), pack_bf16(e - bf16_lo(r[1]), f - bf16_hi(r[1]))};
       }
   }
 };
@@ -165,9 +185,9 @@ struct Item {
 };
 // Workgroups go to the XCDs in turn, and each XCD has an L2 of its own: where eight divides the heads of k, an XCD has all
 // workgroups of some of them.
-__device__ __forceinline__ Item item_of(int heads, int kv_heads) {
+__device__ __forceinline__ Item item_of(int heads, int kv_heads, int lead = 0) {
   Item r;
-  const uint32_t b = (uint32_t)row_group();
+  const uint32_t b = (uint32_t)row_group() - lead;
   if (kv_heads % 8 == 0) {
     const uint32_t each = heads / 8, at = b >> 3;
     r.head = (b & 7) * each + at % each;
@@ -178,8 +198,8 @@ __device__ __forceinline__ Item item_of(int heads, int kv_heads) {
   }
   return r;
 }
-dim3 grid_of(int parts, int heads) {
-  const RowGrid g = row_grid((int64_t)parts * heads);
+dim3 grid_of(int64_t parts, int heads, int lead = 0) {
+  const RowGrid g = row_grid(parts * heads + lead);
   return dim3(g.x, g.y);
 }
 
@@ -208,10 +228,10 @@ __device__ __forceinline__ bool sees(const AttendRowsParams &p, int pos, int key
   return key <= pos && (p.window == 0 || pos - p.window < key || key < p.sinks);
 }
 
-template <int DT>
+template <int KS>
 __global__ __launch_bounds__(kBlock, 2) void attend_rows_kernel(const AttendRowsParams p, const int parts) {
-  using T = Tiles<DT>;
-  __shared__ __align__(16) uint8_t lds[4 * T::BYTES];
+  using T = Tiles<KS>;
+  __shared__ __align__(256) uint8_t lds[4 * T::BYTES];
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
   const Item item = item_of(p.heads, p.kv_heads);
   if (item.part >= parts) return;
@@ -227,7 +247,7 @@ __global__ __launch_bounds__(kBlock, 2) void attend_rows_kernel(const AttendRows
   const KeyTiles tiles = key_tiles(p, s, r0, r1);
   const uint16_t *k = static_cast<const uint16_t *>(p.k.at) + s.k0 * p.k.token + kv * p.k.head;
   const uint16_t *v = static_cast<const uint16_t *>(p.v.at) + s.k0 * p.v.token + kv * p.v.head;
-  const typename T::Source ks = T::source(wave, lane, p.k.token, p.dim), vs = T::source(wave, lane, p.v.token, p.dim);
+  const typename T::Source ks = T::source(wave, lane, p.k.token), vs = T::source(wave, lane, p.v.token);
   const auto request = [&](int t) MOE_ROWS_INLINE {
     const int key = tiles.at(t), rows = s.nk - key;
     uint8_t *to = lds + (t & 1) * 2 * T::BYTES;
@@ -241,27 +261,27 @@ __global__ __launch_bounds__(kBlock, 2) void attend_rows_kernel(const AttendRows
   for (int d = 0; d < T::DS; ++d) o[d] = zero16();
   float top = -INFINITY, sum = 0.f;
   const float scale = p.scale * kLog2e;
+  const typename T::Reader reader(lane);
   if (tiles.n > 0) request(0);
   for (int t = 0; t < tiles.n; ++t) {
     landed_but<0>();
     if (t + 1 < tiles.n) request(t + 1);
-    const uint8_t *kt = lds + (t & 1) * 2 * T::BYTES, *vt = kt + T::BYTES;
     const int key = tiles.at(t);
     if (mine > r1 || see_none(p, p0, p1, key, key + kTile - 1)) continue;
+    const typename T::Reader at(lds_at(lds) + (t & 1) * 2 * T::BYTES, reader, false);
     f32x16 z[2];
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
       z[m] = zero16();
 #pragma unroll
-      for (int i = 0; i < T::KS; ++i) z[m] = mma(T::rows(kt, m * 32, i, lane), q[i], z[m]);
+      for (int i = 0; i < T::KS; ++i) z[m] = mma(T::rows(at, 0, m * 32, i), q[i], z[m]);
     }
     if (!see_all(p, p0, p1, key, key + kTile - 1)) {
 #pragma unroll
       for (int m = 0; m < 2; ++m)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          const int at = key + m * 32 + i / 4 * 8 + (lane >> 5) * 4 + i % 4;
-          z[m][i] = sees(p, pos, at) ? z[m][i] : -INFINITY;
+          z[m][i] = sees(p, pos, key + m * 32 + i / 4 * 8 + (lane >> 5) * 4 + i % 4) ? z[m][i] : -INFINITY;
         }
     }
     float most = -INFINITY;
@@ -290,21 +310,107 @@ __global__ __launch_bounds__(kBlock, 2) void attend_rows_kernel(const AttendRows
     for (int i = 0; i < 4; ++i) {
       const i32x4 f = summed(z[i >> 1], i & 1);
 #pragma unroll
-      for (int d = 0; d < T::DS; ++d) o[d] = mma(T::columns(vt, i * 16, d, lane), f, o[d]);
+      for (int d = 0; d < T::DS; ++d) o[d] = mma(T::columns(at, T::BYTES, i * 16, d), f, o[d]);
     }
   }
   sum += __shfl_xor(sum, 32);
   const bool there = row < s.nq;
-  T::store(p.y + ((int64_t)(s.q0 + row) * p.heads + item.head) * p.dim, there, p.dim, lane, o, sum > 0.f || sum != sum ? 1.f / sum : 0.f);
+  const int64_t dense = ((int64_t)(s.q0 + row) * p.heads + item.head) * p.dim;
+  T::store(p.y + dense, p.low ? p.low + dense : nullptr, there, p.dim, lane, o, sum > 0.f || sum != sum ? 1.f / sum : 0.f);
   if (p.lse && there && lane < 32) p.lse[(int64_t)item.head * p.n_rows + s.q0 + row] = top * kLn2 + __logf(sum);
 }
 
-template <int DT>
+// ---- the gradients of k and v: how their work is cut ------------------------------------------------------------
+// The queries that see any of kOwn keys, tile by tile, and that for each head of the group, are a list.  Lists are long and few
+// where few heads of k serve many of q, or where first keys stay visible: a list of more than half as many tiles again as a
+// workgroup's equal share is cut into pieces of about a share, whose sums, in 32 bits, are added up in order by a launch of its own.
+// (A piece costs as much as some eight tiles: 128 rows of sums to memory and back.)
+constexpr int kShares = 512;   // workgroups that the GPU holds at once
+constexpr int kLeast = 16;     // tiles of a share at least
+constexpr int kLead = 8;       // workgroups ahead of those with rows in the launch that plans: one plans, and each XCD has one
+struct List {
+  int first, end, tiles;  // query rows of the sequence, from a tile's first row on; tiles of one head
+};
+__device__ __forceinline__ List list_of(const AttendRowsParams &p, const Sequence &s, int part) {
+  const int k0 = part * kOwn, k1 = min(k0 + kOwn, s.nk) - 1;
+  List l;
+  l.first = max(k0 - s.ahead, 0) / kTile * kTile;
+  l.end = p.window > 0 && k0 >= p.sinks ? (int)min((int64_t)s.nq, (int64_t)k1 + p.window - s.ahead) : s.nq;
+  l.tiles = max((l.end - l.first + kTile - 1) / kTile, 0);
+  return l;
+}
+// of the threads of the workgroup up to this one, and of all
+template <typename V>
+__device__ __forceinline__ V block_upto(V v, V *waves, V &all) {
+  const V upto = sum_upto(v);
+  if ((threadIdx.x & 63) == 63) waves[threadIdx.x >> 6] = upto;
+  __syncthreads();
+  V before = 0;
+  all = 0;
+  for (int w = 0; w < kWaves; ++w) {
+    before += w < (int)(threadIdx.x >> 6) ? waves[w] : 0;
+    all += waves[w];
+  }
+  __syncthreads();
+  return before + upto;
+}
+// The pieces, in the order of the sequences and their keys.
+__device__ __forceinline__ void plan_pieces(const AttendRowsParams &p, uint8_t *lds) {
+  int64_t *waves = reinterpret_cast<int64_t *>(lds);
+  int64_t *past = waves + kWaves;  // parts of the chunk's sequences up to and with each
+  const int per = p.heads / p.kv_heads, tid = threadIdx.x;
+  int64_t total = 0, share = 0, pieces = 0, slots = 0, all;
+  for (int pass = 0; pass < 2; ++pass) {
+    for (int s0 = 0; s0 < p.n_seqs; s0 += kBlock) {
+      const int64_t n = s0 + tid < p.n_seqs ? (sequence_of(p, s0 + tid).nk + kOwn - 1) / kOwn : 0;
+      int64_t parts;
+      past[tid] = block_upto(n, waves, parts);
+      __syncthreads();
+      for (int64_t u0 = 0; u0 < parts; u0 += kBlock) {
+        const int64_t u = u0 + tid;
+        int at = 0, part = 0, tiles = 0;
+        if (u < parts) {
+#pragma unroll
+          for (int o = kBlock / 2; o > 0; o >>= 1) at += past[at + o - 1] <= u ? o : 0;
+          part = (int)(u - (at > 0 ? past[at - 1] : 0));
+          tiles = list_of(p, sequence_of(p, s0 + at), part).tiles * per;
+        }
+        if (pass == 0) {
+          total += tiles;
+          continue;
+        }
+        int n = u < parts ? 1 : 0;
+        if (2 * (int64_t)tiles > 3 * share) n = (int)((tiles + share - 1) / share);
+        const int64_t slot = slots + block_upto((int64_t)(n > 1 ? n : 0), waves, all) - n;
+        slots += all;
+        if (n > 1 && slot + n > p.max_slots) n = 1;  // (only where sequences overlap)
+        const int64_t piece = pieces + block_upto((int64_t)n, waves, all) - n;
+        pieces += all;
+        for (int i = 0; i < n; ++i) {
+          const int from = (int)((int64_t)tiles * i / n), to = (int)((int64_t)tiles * (i + 1) / n);
+          if (piece + i < p.max_pieces) p.pieces[piece + i] = KeyPiece{s0 + at, part, from, to - from, i, n, (int)slot};
+        }
+      }
+      __syncthreads();
+    }
+    if (pass == 0) {
+      block_upto(total, waves, all);
+      share = max((all * p.kv_heads + kShares - 1) / kShares, (int64_t)kLeast);
+    }
+  }
+  if (tid == 0) *p.n_pieces = (int)min(pieces, (int64_t)p.max_pieces);
+}
+
+template <int KS>
 __global__ __launch_bounds__(kBlock, 2) void attend_rows_dq_kernel(const AttendRowsParams p, const int parts) {
-  using T = Tiles<DT>;
-  __shared__ __align__(16) uint8_t lds[4 * T::BYTES];
+  using T = Tiles<KS>;
+  __shared__ __align__(256) uint8_t lds[4 * T::BYTES];
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
-  const Item item = item_of(p.heads, p.kv_heads);
+  if (row_group() < kLead) {
+    if (row_group() == 0) plan_pieces(p, lds);
+    return;
+  }
+  const Item item = item_of(p.heads, p.kv_heads, kLead);
   if (item.part >= parts) return;
   const Part part = part_of<false>(p, item.part);
   if (part.sequence < 0) {
@@ -318,7 +424,7 @@ __global__ __launch_bounds__(kBlock, 2) void attend_rows_dq_kernel(const AttendR
   const KeyTiles tiles = key_tiles(p, s, r0, r1);
   const uint16_t *k = static_cast<const uint16_t *>(p.k.at) + s.k0 * p.k.token + kv * p.k.head;
   const uint16_t *v = static_cast<const uint16_t *>(p.v.at) + s.k0 * p.v.token + kv * p.v.head;
-  const typename T::Source ks = T::source(wave, lane, p.k.token, p.dim), vs = T::source(wave, lane, p.v.token, p.dim);
+  const typename T::Source ks = T::source(wave, lane, p.k.token), vs = T::source(wave, lane, p.v.token);
   const auto request = [&](int t) MOE_ROWS_INLINE {
     const int key = tiles.at(t), rows = s.nk - key;
     uint8_t *to = lds + (t & 1) * 2 * T::BYTES;
@@ -337,6 +443,13 @@ __global__ __launch_bounds__(kBlock, 2) void attend_rows_dq_kernel(const AttendR
     for (int i = 0; i < T::KS; ++i)
 #pragma unroll
       for (int w = 0; w < 4; ++w) delta += bf16_lo(y[i][w]) * bf16_lo(dy[i][w]) + bf16_hi(y[i][w]) * bf16_hi(dy[i][w]);
+    if (p.low) {
+      T::own(p.low + dense, there, p.dim, lane, y);
+#pragma unroll
+      for (int i = 0; i < T::KS; ++i)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) delta += bf16_lo(y[i][w]) * bf16_lo(dy[i][w]) + bf16_hi(y[i][w]) * bf16_hi(dy[i][w]);
+    }
     delta += __shfl_xor(delta, 32);
   }
   T::own(static_cast<const uint16_t *>(p.q.at) + at_row * p.q.token + item.head * p.q.head, there, p.dim, lane, q);
@@ -345,22 +458,23 @@ __global__ __launch_bounds__(kBlock, 2) void attend_rows_dq_kernel(const AttendR
   f32x16 o[T::DS];
 #pragma unroll
   for (int d = 0; d < T::DS; ++d) o[d] = zero16();
+  const typename T::Reader reader(lane);
   if (tiles.n > 0) request(0);
   for (int t = 0; t < tiles.n; ++t) {
     landed_but<0>();
     if (t + 1 < tiles.n) request(t + 1);
-    const uint8_t *kt = lds + (t & 1) * 2 * T::BYTES, *vt = kt + T::BYTES;
     const int key = tiles.at(t);
     if (mine > r1) continue;
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
       const int key0 = key + m * 32;
       if (see_none(p, p0, p1, key0, key0 + 31)) continue;
+      const typename T::Reader at(lds_at(lds) + (t & 1) * 2 * T::BYTES + m * 32 * T::ROW, reader, false);
       f32x16 z = zero16(), dp = zero16();
 #pragma unroll
-      for (int i = 0; i < T::KS; ++i) z = mma(T::rows(kt, m * 32, i, lane), q[i], z);
+      for (int i = 0; i < T::KS; ++i) z = mma(T::rows(at, 0, 0, i), q[i], z);
 #pragma unroll
-      for (int i = 0; i < T::KS; ++i) dp = mma(T::rows(vt, m * 32, i, lane), dy[i], dp);
+      for (int i = 0; i < T::KS; ++i) dp = mma(T::rows(at, T::BYTES, 0, i), dy[i], dp);
 #pragma unroll
       for (int i = 0; i < 16; ++i) z[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i], scale, -lse)) * (dp[i] - delta);
       if (!see_all(p, p0, p1, key0, key0 + 31)) {
@@ -371,39 +485,43 @@ __global__ __launch_bounds__(kBlock, 2) void attend_rows_dq_kernel(const AttendR
       for (int i = 0; i < 2; ++i) {
         const i32x4 f = summed(z, i);
 #pragma unroll
-        for (int d = 0; d < T::DS; ++d) o[d] = mma(T::columns(kt, m * 32 + i * 16, d, lane), f, o[d]);
+        for (int d = 0; d < T::DS; ++d) o[d] = mma(T::columns(at, 0, i * 16, d), f, o[d]);
       }
     }
   }
-  T::store(p.dq + dense, there, p.dim, lane, o, p.scale);
+  T::store(p.dq + dense, nullptr, there, p.dim, lane, o, p.scale);
 }
 
-template <int DT>
-__global__ __launch_bounds__(kBlock, 1) void attend_rows_dkv_kernel(const AttendRowsParams p, const int parts) {
-  using T = Tiles<DT>;
-  __shared__ __align__(16) uint8_t lds[4 * T::BYTES + 4 * kTile * 4];
+template <int KS>
+__global__ __launch_bounds__(kBlock, 2) void attend_rows_dkv_kernel(const AttendRowsParams p, const int parts) {
+  using T = Tiles<KS>;
+  __shared__ __align__(256) uint8_t lds[4 * T::BYTES + 4 * kTile * 4];
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
   const Item item = item_of(p.kv_heads, p.kv_heads);
   if (item.part >= parts) return;
-  const Part part = part_of<true>(p, item.part);
-  const int kv = item.head, per = p.heads / p.kv_heads;
-  if (part.sequence < 0) {
-    const int step = parts - (item.part - part.over);
-    clear_rows(p.k_offsets, p.n_seqs, p.n_k_rows, p.dk, kv, p.kv_heads, p.dim, part.over, step);
-    clear_rows(p.k_offsets, p.n_seqs, p.n_k_rows, p.dv, kv, p.kv_heads, p.dim, part.over, step);
+  const int kv = item.head, per = p.heads / p.kv_heads, n_pieces = *p.n_pieces;
+  if (item.part >= n_pieces) {
+    clear_rows(p.k_offsets, p.n_seqs, p.n_k_rows, p.dk, kv, p.kv_heads, p.dim, item.part - n_pieces, parts - n_pieces);
+    clear_rows(p.k_offsets, p.n_seqs, p.n_k_rows, p.dv, kv, p.kv_heads, p.dim, item.part - n_pieces, parts - n_pieces);
     return;
   }
-  const Sequence s = sequence_of(p, part.sequence);
-  const int k0 = part.part * kOwn, k1 = min(k0 + kOwn, s.nk) - 1, mine = k0 + wave * 32, key = mine + (lane & 31);
+  const KeyPiece piece = p.pieces[item.part];
+  const Sequence s = sequence_of(p, piece.sequence);
+  const int k0 = piece.part * kOwn, k1 = min(k0 + kOwn, s.nk) - 1, mine = k0 + wave * 32, key = mine + (lane & 31);
   const bool there = key < s.nk;
-  // the queries that see any of the workgroup's keys
-  const int first = max(k0 - s.ahead, 0) / kTile * kTile;
-  const int end = p.window > 0 && k0 >= p.sinks ? (int)min((int64_t)s.nq, (int64_t)k1 + p.window - s.ahead) : s.nq;
-  const int tiles = max((end - first + kTile - 1) / kTile, 0), all = tiles * per;
-  const typename T::Source qs = T::source(wave, lane, p.q.token, p.dim), ds = T::source(wave, lane, (int64_t)p.heads * p.dim, p.dim);
+  const List list = list_of(p, s, piece.part);
+  const int first = list.first, end = list.end, all = piece.count;
+  const typename T::Source qs = T::source(wave, lane, p.q.token), ds = T::source(wave, lane, (int64_t)p.heads * p.dim);
   uint8_t *stats = lds + 4 * T::BYTES;
+  // the heads one after the other, their tiles in turn
+  int next_head = kv * per + (all > 0 ? piece.first / list.tiles : 0), next_row = first + (all > 0 ? piece.first % list.tiles * kTile : 0);
   const auto request = [&](int t) MOE_ROWS_INLINE {
-    const int head = kv * per + t / tiles, row = first + t % tiles * kTile, rows = s.nq - row;
+    const int head = next_head, row = next_row, rows = s.nq - row;
+    next_row += kTile;
+    if (next_row >= end) {
+      next_row = first;
+      ++next_head;
+    }
     uint8_t *to = lds + (t & 1) * 2 * T::BYTES;
     T::request(qs, static_cast<const uint16_t *>(p.q.at) + (int64_t)(s.q0 + row) * p.q.token + head * p.q.head, rows, p.q.token, p.dim, wave, to);
     T::request(ds, p.dy + ((int64_t)(s.q0 + row) * p.heads + head) * p.dim, rows, (int64_t)p.heads * p.dim, p.dim, wave, to + T::BYTES);
@@ -418,23 +536,24 @@ __global__ __launch_bounds__(kBlock, 1) void attend_rows_dkv_kernel(const Attend
 #pragma unroll
   for (int d = 0; d < T::DS; ++d) dk[d] = dv[d] = zero16();
   const float scale = p.scale * kLog2e;
+  const typename T::Reader reader(lane);
+  int row = next_row;
   if (all > 0) request(0);
-  for (int t = 0; t < all; ++t) {
+  for (int t = 0; t < all; ++t, row = row + kTile < end ? row + kTile : first) {
     landed_but<0>();
     if (t + 1 < all) request(t + 1);
-    const uint8_t *qt = lds + (t & 1) * 2 * T::BYTES, *dt = qt + T::BYTES;
     const float *lse = reinterpret_cast<const float *>(stats + (t & 1) * 2 * kTile * 4), *delta = lse + kTile;
-    const int row = first + t % tiles * kTile;
     if (mine > k1) continue;
-#pragma unroll
+#pragma unroll 1
     for (int m = 0; m < 2; ++m) {
       const int row0 = row + m * 32, p0 = row0 + s.ahead, p1 = min(row0 + 31, s.nq - 1) + s.ahead;
       if (row0 >= s.nq || see_none(p, p0, p1, mine, mine + 31)) continue;
+      const typename T::Reader at(lds_at(lds) + (t & 1) * 2 * T::BYTES + m * 32 * T::ROW, reader, true);
       f32x16 z = zero16(), dp = zero16();
 #pragma unroll
-      for (int i = 0; i < T::KS; ++i) z = mma(T::rows(qt, m * 32, i, lane), k[i], z);
+      for (int i = 0; i < T::KS; ++i) z = mma(T::rows(at, 0, 0, i), k[i], z);
 #pragma unroll
-      for (int i = 0; i < T::KS; ++i) dp = mma(T::rows(dt, m * 32, i, lane), v[i], dp);
+      for (int i = 0; i < T::KS; ++i) dp = mma(T::rows(at, T::BYTES, 0, i), v[i], dp);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const f32x4 l4 = *reinterpret_cast<const f32x4 *>(lse + m * 32 + i * 8 + (lane >> 5) * 4);
@@ -456,38 +575,111 @@ __global__ __launch_bounds__(kBlock, 1) void attend_rows_dkv_kernel(const Attend
         const i32x4 f = summed(z, i), g = summed(dp, i);
 #pragma unroll
         for (int d = 0; d < T::DS; ++d) {
-          dv[d] = mma(T::columns(dt, m * 32 + i * 16, d, lane), f, dv[d]);
-          dk[d] = mma(T::columns(qt, m * 32 + i * 16, d, lane), g, dk[d]);
+          dv[d] = mma(T::columns(at, T::BYTES, i * 16, d), f, dv[d]);
+          dk[d] = mma(T::columns(at, 0, i * 16, d), g, dk[d]);
         }
       }
     }
   }
+  if (piece.of > 1) {
+    float *sums = p.sums + (((int64_t)(piece.slot + piece.index) * p.kv_heads + kv) * kOwn + key - k0) * 2 * p.dim;
+#pragma unroll
+    for (int d = 0; d < T::DS; ++d)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int c = d * 32 + i * 8 + (lane >> 5) * 4;
+        if (!there || c >= p.dim) continue;
+        *reinterpret_cast<f32x4 *>(sums + c) = f32x4{dk[d][4 * i], dk[d][4 * i + 1], dk[d][4 * i + 2], dk[d][4 * i + 3]};
+        *reinterpret_cast<f32x4 *>(sums + p.dim + c) = f32x4{dv[d][4 * i], dv[d][4 * i + 1], dv[d][4 * i + 2], dv[d][4 * i + 3]};
+      }
+    return;
+  }
   const int64_t to = (at_key * p.kv_heads + kv) * p.dim;
-  T::store(p.dk + to, there, p.dim, lane, dk, p.scale);
-  T::store(p.dv + to, there, p.dim, lane, dv, 1.f);
+  T::store(p.dk + to, nullptr, there, p.dim, lane, dk, p.scale);
+  T::store(p.dv + to, nullptr, there, p.dim, lane, dv, 1.f);
+}
+
+// The sums of the pieces of a list, in order; a workgroup has kJoinRows of its keys
+constexpr int kJoinRows = 16;
+__global__ __launch_bounds__(kBlock) void join_pieces_kernel(const AttendRowsParams p) {
+  const uint32_t b = (uint32_t)row_group();
+  const int strip = b % (kOwn / kJoinRows), kv = b / (kOwn / kJoinRows) % p.kv_heads, at = b / (kOwn / kJoinRows) / p.kv_heads;
+  if (at >= *p.n_pieces) return;
+  const KeyPiece piece = p.pieces[at];
+  if (piece.of < 2 || piece.index > 0) return;
+  const Sequence s = sequence_of(p, piece.sequence);
+  const int row0 = strip * kJoinRows, rows = min(kJoinRows, s.nk - piece.part * kOwn - row0), quads = p.dim / 4;
+  for (int u = threadIdx.x; u < rows * 2 * quads; u += kBlock) {
+    const int r = row0 + u / (2 * quads), c = u % (2 * quads);
+    const float *from = p.sums + (((int64_t)piece.slot * p.kv_heads + kv) * kOwn + r) * 2 * p.dim + c * 4;
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < piece.of; ++i) v += *reinterpret_cast<const f32x4 *>(from + (int64_t)i * p.kv_heads * kOwn * 2 * p.dim);
+    if (c < quads) v *= p.scale;
+    const int64_t to = ((int64_t)(s.k0 + piece.part * kOwn + r) * p.kv_heads + kv) * p.dim + c % quads * 4;
+    *reinterpret_cast<rows_u32x2 *>((c < quads ? p.dk : p.dv) + to) = rows_u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+  }
 }
 
 // parts of kOwn rows that the sequences have at most, and one at least that is none's: it clears the rows of no sequence
 int parts_of(int n_rows, int n_seqs) { return n_rows / kOwn + n_seqs + 1; }
 
+// f(steps over the dims): as many as there are, or the next more that there is a kernel for
+template <typename F>
+void with_steps(int dim, F f) {
+  if (dim <= 64) f(std::integral_constant<int, 4>());
+  else if (dim <= 80) f(std::integral_constant<int, 5>());
+  else if (dim <= 96) f(std::integral_constant<int, 6>());
+  else f(std::integral_constant<int, 8>());
+}
+
 }  // namespace
 
 hipError_t launch_attend_rows(const AttendRowsParams &p, hipStream_t s) {
   const int parts = parts_of(p.n_rows, p.n_seqs);
-  const dim3 grid = grid_of(parts, p.heads);
-  if (p.dim <= 64) attend_rows_kernel<64><<<grid, kBlock, 0, s>>>(p, parts);
-  else attend_rows_kernel<128><<<grid, kBlock, 0, s>>>(p, parts);
+  with_steps(p.dim, [&](auto ks) { attend_rows_kernel<decltype(ks)::value><<<grid_of(parts, p.heads), kBlock, 0, s>>>(p, parts); });
   return hipGetLastError();
 }
 
-hipError_t launch_attend_rows_backward(const AttendRowsParams &p, hipStream_t s) {
-  const int parts = parts_of(p.n_rows, p.n_seqs), k_parts = parts_of(p.n_k_rows, p.n_seqs);
-  if (p.dim <= 64) attend_rows_dq_kernel<64><<<grid_of(parts, p.heads), kBlock, 0, s>>>(p, parts);
-  else attend_rows_dq_kernel<128><<<grid_of(parts, p.heads), kBlock, 0, s>>>(p, parts);
+// The workspace: delta, the pieces, their sums.  A list of n tiles is cut if n > 1.5 shares, into n / share + 1 pieces at most, so that
+// there are 5 / 3 pieces of lists that are cut for each of all lists' shares, at most kShares.
+struct BackwardSpace {
+  int64_t pieces, sums, bytes;  // where they begin
+  int max_pieces, max_slots;
+};
+static BackwardSpace backward_space(int n_rows, int n_k_rows, int n_seqs, int heads, int kv_heads, int dim) {
+  BackwardSpace w;
+  const int parts = parts_of(n_k_rows, n_seqs);
+  const int64_t list = (int64_t)(heads / kv_heads) * ((n_rows + kTile - 1) / kTile);  // tiles, at most
+  const int64_t shares = std::min<int64_t>(kShares, list * (parts - 1) * kv_heads / kLeast + 1);
+  w.max_slots = 2 * list > 3 * kLeast ? (int)(5 * shares / (3 * kv_heads) + 1) : 0;
+  w.max_pieces = parts + (w.max_slots > 0 ? kShares / kv_heads + 1 : 0);
+  const auto up = [](int64_t v) { return (v + 255) / 256 * 256; };
+  w.pieces = up((int64_t)n_rows * heads * 4);
+  w.sums = up(w.pieces + 16 + (int64_t)w.max_pieces * sizeof(KeyPiece));
+  w.bytes = w.sums + (int64_t)w.max_slots * kv_heads * kOwn * 2 * dim * 4;
+  return w;
+}
+size_t attend_rows_backward_bytes(int n_rows, int n_k_rows, int n_seqs, int heads, int kv_heads, int dim) {
+  return backward_space(n_rows, n_k_rows, n_seqs, heads, kv_heads, dim).bytes;
+}
+
+hipError_t launch_attend_rows_backward(const AttendRowsParams &given, uint8_t *workspace, hipStream_t s) {
+  AttendRowsParams p = given;
+  const BackwardSpace w = backward_space(p.n_rows, p.n_k_rows, p.n_seqs, p.heads, p.kv_heads, p.dim);
+  p.delta = reinterpret_cast<float *>(workspace);
+  p.n_pieces = reinterpret_cast<int32_t *>(workspace + w.pieces);
+  p.pieces = reinterpret_cast<KeyPiece *>(workspace + w.pieces + 16);
+  p.sums = reinterpret_cast<float *>(workspace + w.sums);
+  p.max_pieces = w.max_pieces;
+  p.max_slots = w.max_slots;
+  const int parts = parts_of(p.n_rows, p.n_seqs), k_parts = w.max_pieces + 1;
+  with_steps(p.dim, [&](auto ks) { attend_rows_dq_kernel<decltype(ks)::value><<<grid_of(parts, p.heads, kLead), kBlock, 0, s>>>(p, parts); });
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if (p.dim <= 64) attend_rows_dkv_kernel<64><<<grid_of(k_parts, p.kv_heads), kBlock, 0, s>>>(p, k_parts);
-  else attend_rows_dkv_kernel<128><<<grid_of(k_parts, p.kv_heads), kBlock, 0, s>>>(p, k_parts);
+  with_steps(p.dim, [&](auto ks) { attend_rows_dkv_kernel<decltype(ks)::value><<<grid_of(k_parts, p.kv_heads), kBlock, 0, s>>>(p, k_parts); });
+  e = hipGetLastError();
+  if (e != hipSuccess || w.max_slots == 0) return e;
+  join_pieces_kernel<<<grid_of((int64_t)w.max_pieces * (kOwn / kJoinRows), p.kv_heads), kBlock, 0, s>>>(p);
   return hipGetLastError();
 }
 

@@ -145,40 +145,44 @@ Packed packed_of(const Tensor &q, const Tensor &k, const Tensor &v, const Tensor
   return r;
 }
 
-std::tuple<Tensor, Maybe> attend_rows(const Tensor &q, const Tensor &k, const Tensor &v, const Tensor &offsets, const Maybe &k_offsets,
+std::tuple<Tensor, Maybe, Maybe> attend_rows(const Tensor &q, const Tensor &k, const Tensor &v, const Tensor &offsets, const Maybe &k_offsets,
                                       std::optional<double> scale, int64_t window, int64_t sinks, bool keep) {
   no_history(q, k, v);
   const Packed r = packed_of(q, k, v, offsets, k_offsets);
   const Place on(q);
   on.has(k, v, offsets, k_offsets);
   const Tensor y = fresh(q, {r.q.n, r.q.h, r.q.d}, at::kBFloat16, r.ok);
-  Maybe lse;
-  if (keep) lse = fresh(q, {r.q.h, r.q.n}, at::kFloat, r.ok);
+  Maybe lse, low;
+  if (keep) {
+    lse = fresh(q, {r.q.h, r.q.n}, at::kFloat, r.ok);
+    low = fresh(q, {r.q.n, r.q.h, r.q.d}, at::kBFloat16, r.ok);
+  }
   check(moe_attend_rows(q.const_data_ptr(), r.q.token, r.q.head, k.const_data_ptr(), r.k.token, r.k.head, v.const_data_ptr(), r.v.token, r.v.head,
                         ints(offsets), r.k_offsets, r.n, r.q.n, r.k.n, r.q.h, r.k.h, r.q.d, scale_of(scale, r.q.d), size_or_all(window),
-                        size_or_all(sinks), y.mutable_data_ptr(), to_floats(lse), on.stream()),
+                        size_or_all(sinks), y.mutable_data_ptr(), to(low), to_floats(lse), on.stream()),
         "moe_attend_rows");
-  return {y, lse};
+  return {y, lse, low};
 }
 
 std::tuple<Tensor, Tensor, Tensor> attend_rows_backward(const Tensor &q, const Tensor &k, const Tensor &v, const Tensor &offsets, const Tensor &y,
-                                                        const Tensor &lse, const Tensor &dy, const Maybe &k_offsets, std::optional<double> scale,
+                                                        const Tensor &lse, const Maybe &low, const Tensor &dy, const Maybe &k_offsets, std::optional<double> scale,
                                                         int64_t window, int64_t sinks) {
-  no_history(q, k, v, y, lse, dy);
+  no_history(q, k, v, y, lse, low, dy);
   const Packed r = packed_of(q, k, v, offsets, k_offsets);
   dense(y, {r.q.n, r.q.h, r.q.d}, at::kBFloat16, "y");
+  dense(low, {r.q.n, r.q.h, r.q.d}, at::kBFloat16, "kept.low");
   dense(dy, {r.q.n, r.q.h, r.q.d}, at::kBFloat16, "dy");
-  dense(lse, {r.q.h, r.q.n}, at::kFloat, "lse");
+  dense(lse, {r.q.h, r.q.n}, at::kFloat, "kept.lse");
   const Place on(q);
-  on.has(k, v, offsets, k_offsets, y, lse, dy);
+  on.has(k, v, offsets, k_offsets, y, lse, low, dy);
   const Tensor dq = fresh(q, {r.q.n, r.q.h, r.q.d}, at::kBFloat16, r.ok), dk = fresh(k, {r.k.n, r.k.h, r.k.d}, at::kBFloat16, r.ok),
                dv = fresh(v, {r.k.n, r.k.h, r.k.d}, at::kBFloat16, r.ok);
   Maybe work;
-  const size_t need = moe_attend_rows_backward_bytes(r.q.n, r.q.h);
+  const size_t need = moe_attend_rows_backward_bytes(r.q.n, r.k.n, r.n, r.q.h, r.k.h, r.q.d);
   if (need) work = fresh(q, {(int64_t)need}, at::kByte, r.ok);
   check(moe_attend_rows_backward(q.const_data_ptr(), r.q.token, r.q.head, k.const_data_ptr(), r.k.token, r.k.head, v.const_data_ptr(), r.v.token,
                                  r.v.head, ints(offsets), r.k_offsets, r.n, r.q.n, r.k.n, r.q.h, r.k.h, r.q.d, scale_of(scale, r.q.d),
-                                 size_or_all(window), size_or_all(sinks), y.const_data_ptr(), floats(lse), dy.const_data_ptr(), dq.mutable_data_ptr(),
+                                 size_or_all(window), size_or_all(sinks), y.const_data_ptr(), at_(low), floats(lse), dy.const_data_ptr(), dq.mutable_data_ptr(),
                                  dk.mutable_data_ptr(), dv.mutable_data_ptr(), to(work), need, on.stream()),
         "moe_attend_rows_backward");
   return {dq, dk, dv};

@@ -69,19 +69,22 @@ BAD_ROWS = BAD_SEEN + [
     dict(v_stride=1 << 24), dict(q=P + 2), dict(v=P + 8), dict(offsets=P + 2)]
 
 
-@pytest.mark.parametrize("bad", BAD_ROWS + [dict(y=None), dict(y=P + 4), dict(lse=P + 2)])
+@pytest.mark.parametrize("bad", BAD_ROWS + [dict(y=None), dict(y=P + 4), dict(low=P + 8), dict(lse=P + 2)])
 def test_rows(B, bad):
-    refused(B, B.lib.moe_attend_rows, dict(ROWS, y=P, lse=None, stream=None), **bad)
+    refused(B, B.lib.moe_attend_rows, dict(ROWS, y=P, low=None, lse=None, stream=None), **bad)
 
 
-@pytest.mark.parametrize("bad", BAD_ROWS + [dict(y=None), dict(lse=None), dict(dy=None), dict(dq=None), dict(dk=None), dict(dv=None), dict(dy=P + 8),
-                                            dict(work=None), dict(work=P + 4), dict(work_bytes=100 * 4 * 4 - 1)])
+@pytest.mark.parametrize("bad", BAD_ROWS + [dict(y=None), dict(lse=None), dict(dy=None), dict(dq=None), dict(dk=None), dict(dv=None), dict(dy=P + 8), dict(low=P + 2),
+                                            dict(work=None), dict(work=P + 4), dict(work_bytes=100 * 4 * 4)])
 def test_rows_backward(B, bad):
-    refused(B, B.lib.moe_attend_rows_backward, dict(ROWS, y=P, lse=P, dy=P, dq=P, dk=P, dv=P, work=P, work_bytes=100 * 4 * 4, stream=None), **bad)
+    refused(B, B.lib.moe_attend_rows_backward, dict(ROWS, y=P, low=None, lse=P, dy=P, dq=P, dk=P, dv=P, work=P, work_bytes=1 << 30, stream=None), **bad)
 
 
 def test_workspaces(B):
-    assert B.moe_attend_rows_backward_bytes(100, 4) == 1600 and B.moe_attend_rows_backward_bytes(0, 4) == 0
+    size = B.moe_attend_rows_backward_bytes
+    assert size(100, 300, 3, 4, 2, 64) >= 1600 and size(0, 0, 0, 4, 2, 64) > 0
+    assert all(size(*bad) == 0 for bad in [(-1, 3, 1, 4, 2, 64), (3, 1 << 26, 1, 4, 2, 64), (3, 3, -1, 4, 2, 64), (3, 3, 1, 4, 0, 64), (3, 3, 1, 2, 4, 64), (3, 3, 1, 4, 2, 200)])
+    assert size(20001, 20001, 9, 16, 2, 80) < 128 << 20  # (pieces' sums do not grow with the rows)
     assert B.moe_attend_pages_bytes(0, 4, 2, 64) == 0 and B.moe_attend_pages_bytes(3, 4, 2, 64) > 0
     assert B.moe_attend_pages_bytes(3, 4, 0, 64) == 0 and B.moe_attend_pages_bytes(3, 2, 4, 64) == 0
 
@@ -89,7 +92,7 @@ def test_workspaces(B):
 def test_nothing_to_do(B):
     assert B.lib.moe_store_pages(*dict(STORE, n_rows=0, k=None, v=None, slots=None).values()) == B.MOE_OK
     assert B.lib.moe_attend_pages(*dict(PAGES, n_seqs=0, q=None, y=None, work=None, work_bytes=0).values()) == B.MOE_OK
-    assert B.lib.moe_attend_rows(*dict(ROWS, n_rows=0, q=None, y=None, lse=None, stream=None).values()) == B.MOE_OK
+    assert B.lib.moe_attend_rows(*dict(ROWS, n_rows=0, q=None, y=None, low=None, lse=None, stream=None).values()) == B.MOE_OK
 
 
 def test_tensors_on_the_cpu_and_of_other_shapes(B):
@@ -109,8 +112,8 @@ def test_tensors_on_the_cpu_and_of_other_shapes(B):
         lambda: moe.attend_rows(q, k[:3], k[:3], at),
         lambda: moe.attend_rows(q.transpose(1, 2), k, k, at),
         lambda: moe.attend_rows(q, k, k, at, k_offsets=at[:1]),
-        lambda: moe.attend_rows_backward(q, k, k, at, q, torch.zeros(4, 4), q),
-        lambda: moe.attend_rows_backward(q, k, k, at, q.float(), torch.zeros(4, 5), q),
+        lambda: moe.attend_rows_backward(q, k, k, at, q, moe.KeptAttention(torch.zeros(4, 4), None), q),
+        lambda: moe.attend_rows_backward(q, k, k, at, q.float(), moe.KeptAttention(torch.zeros(4, 5), q), q),
         lambda: moe.attend_pages(q, pages, pages, table, n),
         lambda: moe.attend_pages(q, pages, pages[:2], table, n),
         lambda: moe.attend_pages(q, pages, pages.float(), table, n),

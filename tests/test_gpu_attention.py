@@ -127,6 +127,10 @@ ROWS = [
     ([50, 130, 0, 9], [20, 7, 40, 0], 4, 2, 128, 0, 0),  # queries ahead of the first key, keys without queries, no keys
     ([50, 300], [20, 100], 2, 1, 64, 16, 2),
     ([3] * 70 + [200], None, 2, 1, 32, 0, 0),            # more sequences than lanes
+    ([2] * 300 + [900, 5, 130], None, 16, 1, 64, 0, 0),  # ... and than threads
+    ([2500, 700], None, 16, 1, 128, 0, 0),               # few heads of k: their queries are cut into pieces
+    ([2500, 0, 701], None, 12, 2, 80, 200, 5),
+    ([100, 1500], [2000, 1500], 8, 1, 96, 0, 0),
 ]
 
 
@@ -146,15 +150,18 @@ def test_rows(lib, case):
     q, k, v, dy, keys = rows_case(case)
     kw = dict(k_offsets=ints(starts(keys)) if given else None, window=window, sinks=sinks)
     offsets = ints(starts(each))
-    y, lse = lib.attend_rows(q, k, v, offsets, keep=True, **kw)
+    y, kept = lib.attend_rows(q, k, v, offsets, keep=True, **kw)
     want = reference(q, k, v, each, keys, window, sinks, dim ** -0.5, dy)
     close(y, *want["y"], "y")
-    grads = lib.attend_rows_backward(q, k, v, offsets, y, lse, dy, **kw)
+    grads = lib.attend_rows_backward(q, k, v, offsets, y, kept, dy, **kw)
     for n, got in zip(("dq", "dk", "dv"), grads):
         close(got, *want[n], n)
     assert torch.equal(lib.attend_rows(q, k, v, offsets, **kw), y)
-    for a, b in zip(grads, lib.attend_rows_backward(q, k, v, offsets, y, lse, dy, **kw)):
+    for a, b in zip(grads, lib.attend_rows_backward(q, k, v, offsets, y, kept, dy, **kw)):
         assert torch.equal(a, b)
+    # without what the rounding of y leaves: within the same bounds
+    for n, got in zip(("dq", "dk", "dv"), lib.attend_rows_backward(q, k, v, offsets, y, kept._replace(low=None), dy, **kw)):
+        close(got, *want[n], n)
 
 
 # ---- plan --------------------------------------------------------------------------------------------------
