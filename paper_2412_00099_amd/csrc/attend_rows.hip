@@ -56,28 +56,37 @@ __device__ __forceinline__ Sequence sequence_of(const AttendRowsParams &p, int s
   r.ahead = r.nk - r.nq;
   return r;
 }
-// Part `want` of the sequences' rows in parts of kOwn, a sequence's last part first (it has the most keys); no such part: sequence
-// -1, and by how much it was missed
+// Part `want` of the sequences' rows in parts of kOwn, later parts of the sequences first: they have more keys, and a workgroup with
+// much to do must not be the last to begin.  No such part: sequence -1, and by how much it was missed.
 struct Part {
   int sequence, part, over;
 };
-template <bool KEYS>
+__device__ __forceinline__ int parts_in(const AttendRowsParams &p, int s) {
+  if (s >= p.n_seqs) return 0;
+  const int from = min(max(p.offsets[s], 0), p.n_rows);
+  return (max(min(p.offsets[s + 1], p.n_rows) - from, 0) + kOwn - 1) / kOwn;
+}
 __device__ __forceinline__ Part part_of(const AttendRowsParams &p, int want) {
-  const int32_t *offsets = KEYS ? p.k_offsets : p.offsets;
-  const int most = KEYS ? p.n_k_rows : p.n_rows, lane = threadIdx.x & 63;
+  const int lane = threadIdx.x & 63;
+  if (p.n_seqs <= 64) {
+    const int n = parts_in(p, lane);
+    const auto from_on = [&](int part) { return of_lane(sum_upto(max(n - part, 0)), 63); };  // parts `part` .. of all sequences
+    const int all = from_on(0);
+    if (want >= all) return {-1, 0, want - all};
+    int at = 0, step = 1;  // the last part with `want` or fewer ahead of it and its like
+    while (from_on(step) > want) step *= 2;
+    for (; step > 0; step /= 2) at += from_on(at + step) > want ? step : 0;
+    const int ahead = from_on(at + 1), upto = sum_upto(n > at ? 1 : 0);
+    return {uniform(__builtin_ctzll(__ballot(upto > want - ahead))), uniform(at), 0};
+  }
+  // (more sequences: one after the other, since 64 at a time are looked at once)
   int64_t before = 0;
   for (int s0 = 0; s0 < p.n_seqs; s0 += 64) {
-    const int s = s0 + lane;
-    int n = 0;
-    if (s < p.n_seqs) {
-      const int from = min(max(offsets[s], 0), most);
-      n = (max(min(offsets[s + 1], most) - from, 0) + kOwn - 1) / kOwn;
-    }
-    const int64_t past = before + sum_upto((int64_t)n);
+    const int64_t past = before + sum_upto((int64_t)parts_in(p, s0 + lane));
     const uint64_t behind = __ballot(past > want);
     if (behind != 0) {
-      const int at = __builtin_ctzll(behind), in = (int)(of_lane(past, at) - want);
-      return {uniform(s0 + at), KEYS ? uniform(of_lane(n, at) - in) : uniform(in - 1), 0};
+      const int at = __builtin_ctzll(behind);
+      return {uniform(s0 + at), uniform((int)(of_lane(past, at) - want) - 1), 0};
     }
     before = of_lane(past, 63);
   }
@@ -172,6 +181,12 @@ struct Tiles {
       }
   }
 };
+__device__ __forceinline__ float largest(const f32x16 &z) {
+  float m = z[0];
+#pragma unroll
+  for (int i = 1; i < 16; ++i) m = fmaxf(m, z[i]);
+  return m;
+}
 // rows 16 t .. of a result as the summed side of the next product
 __device__ __forceinline__ i32x4 summed(const f32x16 &p, int t) {
   i32x4 f;
@@ -228,14 +243,18 @@ __device__ __forceinline__ bool sees(const AttendRowsParams &p, int pos, int key
   return key <= pos && (p.window == 0 || pos - p.window < key || key < p.sinks);
 }
 
+// Tiles that all of a workgroup's queries see go in two steps per 32 keys, in which matrix instructions and others do not wait for
+// each other: the scores of the next 32 keys while the exponentials of these are taken, and the product with the values while the
+// largest of the next scores is found.  The other tiles (the diagonal, a window's edge, first keys) are computed one by one and masked.
+// Tiles are requested two ahead; there is one barrier for each, in its middle or at its end, and values have three places in LDS.
 template <int KS>
 __global__ __launch_bounds__(kBlock, 2) void attend_rows_kernel(const AttendRowsParams p, const int parts) {
   using T = Tiles<KS>;
-  __shared__ __align__(256) uint8_t lds[4 * T::BYTES];
+  __shared__ __align__(256) uint8_t lds[5 * T::BYTES];
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
   const Item item = item_of(p.heads, p.kv_heads);
   if (item.part >= parts) return;
-  const Part part = part_of<false>(p, item.part);
+  const Part part = part_of(p, item.part);
   if (part.sequence < 0) {
     clear_rows(p.offsets, p.n_seqs, p.n_rows, p.y, item.head, p.heads, p.dim, part.over, parts - (item.part - part.over));
     return;
@@ -248,76 +267,143 @@ __global__ __launch_bounds__(kBlock, 2) void attend_rows_kernel(const AttendRows
   const uint16_t *k = static_cast<const uint16_t *>(p.k.at) + s.k0 * p.k.token + kv * p.k.head;
   const uint16_t *v = static_cast<const uint16_t *>(p.v.at) + s.k0 * p.v.token + kv * p.v.head;
   const typename T::Source ks = T::source(wave, lane, p.k.token), vs = T::source(wave, lane, p.v.token);
+  const uint32_t lds0 = lds_at(lds);
+  uint32_t v_put = 2 * T::BYTES, v_at = lds0 + 2 * T::BYTES;
   const auto request = [&](int t) MOE_ROWS_INLINE {
     const int key = tiles.at(t), rows = s.nk - key;
-    uint8_t *to = lds + (t & 1) * 2 * T::BYTES;
-    T::request(ks, k + key * p.k.token, rows, p.k.token, p.dim, wave, to);
-    T::request(vs, v + key * p.v.token, rows, p.v.token, p.dim, wave, to + T::BYTES);
+    T::request(ks, k + key * p.k.token, rows, p.k.token, p.dim, wave, lds + (t & 1) * T::BYTES);
+    T::request(vs, v + key * p.v.token, rows, p.v.token, p.dim, wave, lds + v_put);
+    v_put = v_put == 4 * T::BYTES ? 2 * T::BYTES : v_put + T::BYTES;
   };
   i32x4 q[T::KS];
-  T::own(static_cast<const uint16_t *>(p.q.at) + (s.q0 + min(row, s.nq - 1)) * p.q.token + item.head * p.q.head, row < s.nq, p.dim, lane, q);
   f32x16 o[T::DS];
+  float top = -INFINITY, most = -INFINITY, sum = 0.f;
+  T::own(static_cast<const uint16_t *>(p.q.at) + (s.q0 + min(row, s.nq - 1)) * p.q.token + item.head * p.q.head, row < s.nq, p.dim, lane, q);
 #pragma unroll
   for (int d = 0; d < T::DS; ++d) o[d] = zero16();
-  float top = -INFINITY, sum = 0.f;
   const float scale = p.scale * kLog2e;
   const typename T::Reader reader(lane);
-  if (tiles.n > 0) request(0);
-  for (int t = 0; t < tiles.n; ++t) {
-    landed_but<0>();
-    if (t + 1 < tiles.n) request(t + 1);
-    const int key = tiles.at(t);
-    if (mine > r1 || see_none(p, p0, p1, key, key + kTile - 1)) continue;
-    const typename T::Reader at(lds_at(lds) + (t & 1) * 2 * T::BYTES, reader, false);
-    f32x16 z[2];
-#pragma unroll
-    for (int m = 0; m < 2; ++m) {
-      z[m] = zero16();
-#pragma unroll
-      for (int i = 0; i < T::KS; ++i) z[m] = mma(T::rows(at, 0, m * 32, i), q[i], z[m]);
+  const auto next_tile = [&](int t) MOE_ROWS_INLINE {
+    if (t + 1 < tiles.n) {
+      landed_but<0>();
+      if (t + 2 < tiles.n) request(t + 2);
     }
-    if (!see_all(p, p0, p1, key, key + kTile - 1)) {
-#pragma unroll
-      for (int m = 0; m < 2; ++m)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          z[m][i] = sees(p, pos, key + m * 32 + i / 4 * 8 + (lane >> 5) * 4 + i % 4) ? z[m][i] : -INFINITY;
-        }
-    }
-    float most = -INFINITY;
-#pragma unroll
-    for (int m = 0; m < 2; ++m)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) most = fmaxf(most, z[m][i]);
-    most = fmaxf(most, __shfl_xor(most, 32)) * scale;
-    // The base of the exponentials follows the largest score when that is 2^8 ahead: until then nothing is multiplied
-    if (__any(most > top + 8.f)) {
-      const float to = fmaxf(top, most), shrink = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(top - to);
+  };
+  const auto next_values = [&] { v_at = v_at == lds0 + 4 * T::BYTES ? lds0 + 2 * T::BYTES : v_at + T::BYTES; };
+  // The base of the exponentials follows the largest score (of the query's two lanes; most: of the lane's own) when that is 2^8
+  // ahead: until then nothing is multiplied and no lane asks the other one
+  const auto rebase = [&]() MOE_ROWS_INLINE {
+    if (__any(most * scale > top + 8.f)) {
+      const float to = fmaxf(top, fmaxf(most, __shfl_xor(most, 32)) * scale), shrink = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(top - to);
       top = to;
       sum *= shrink;
 #pragma unroll
       for (int d = 0; d < T::DS; ++d) o[d] *= shrink;
     }
+  };
+
+  // 32 keys of a tile by themselves
+  const auto alone = [&](int key, uint32_t k_at, uint32_t values_at) MOE_ROWS_INLINE {
+    if (mine > r1 || see_none(p, p0, p1, key, key + 31)) return;
+    const typename T::Reader keys(k_at, reader, false), values(values_at, reader, false);
+    f32x16 z = zero16();
+#pragma unroll
+    for (int i = 0; i < T::KS; ++i) z = mma(T::rows(keys, 0, 0, i), q[i], z);
+    if (!see_all(p, p0, p1, key, key + 31)) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) z[i] = sees(p, pos, key + i / 4 * 8 + (lane >> 5) * 4 + i % 4) ? z[i] : -INFINITY;
+    }
+    most = largest(z);
+    rebase();
     const float base = top == -INFINITY ? 0.f : top;
 #pragma unroll
-    for (int m = 0; m < 2; ++m)
+    for (int i = 0; i < 16; ++i) {
+      z[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i], scale, -base));
+      sum += z[i];
+    }
+    const i32x4 f[2] = {summed(z, 0), summed(z, 1)};
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        z[m][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[m][i], scale, -base));
-        sum += z[m][i];
+    for (int i = 0; i < 2 * T::DS; ++i) o[i % T::DS] = mma(T::columns(values, 0, i / T::DS * 16, i % T::DS), f[i / T::DS], o[i % T::DS]);
+  };
+  const auto tile_alone = [&](int t) MOE_ROWS_INLINE {
+#pragma unroll 1
+    for (int m = 0; m < 2; ++m) alone(tiles.at(t) + 32 * m, lds0 + (t & 1) * T::BYTES + 32 * m * T::ROW, v_at + 32 * m * T::ROW);
+    next_tile(t);
+    next_values();
+  };
+
+  // z: the scores of 32 keys, `most` the largest; their values are at `values_at`.  next: those of the 32 keys at `k_at`.
+  const auto step = [&](f32x16 &z, f32x16 &next, uint32_t k_at, uint32_t values_at) MOE_ROWS_INLINE {
+    const typename T::Reader keys(k_at, reader, false), values(values_at, reader, false);
+    rebase();
+    constexpr int EACH = (16 + T::KS - 1) / T::KS, PVS = 2 * T::DS, AHEAD = 3;
+    i32x4 a[AHEAD + 1], c[AHEAD + 1];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) a[i] = T::rows(keys, 0, 0, i);
+    next = zero16();
+#pragma unroll
+    for (int i = 0; i < T::KS; ++i) {
+      __builtin_amdgcn_sched_barrier(0);
+      if (i + AHEAD < T::KS) a[(i + AHEAD) % (AHEAD + 1)] = T::rows(keys, 0, 0, i + AHEAD);
+      else c[i + AHEAD - T::KS] = T::columns(values, 0, (i + AHEAD - T::KS) / T::DS * 16, (i + AHEAD - T::KS) % T::DS);
+      next = mma(a[i % (AHEAD + 1)], q[i], next);
+#pragma unroll
+      for (int e = i * EACH; e < (i + 1) * EACH && e < 16; ++e) {
+        z[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[e], scale, -top));
+        sum += z[e];
       }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    const i32x4 f[2] = {summed(z, 0), summed(z, 1)};
+    most = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const i32x4 f = summed(z[i >> 1], i & 1);
+    for (int i = 0; i < PVS; ++i) {
+      __builtin_amdgcn_sched_barrier(0);
+      if (i + AHEAD < PVS) c[(i + AHEAD) % (AHEAD + 1)] = T::columns(values, 0, (i + AHEAD) / T::DS * 16, (i + AHEAD) % T::DS);
+      o[i % T::DS] = mma(c[i % (AHEAD + 1)], f[i / T::DS], o[i % T::DS]);
+      if (i >= PVS - 4) {
 #pragma unroll
-      for (int d = 0; d < T::DS; ++d) o[d] = mma(T::columns(at, T::BYTES, i * 16, d), f, o[d]);
+        for (int e = (i - PVS + 4) * 4; e < (i - PVS + 5) * 4; ++e) most = fmaxf(most, next[e]);
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+
+  if (tiles.n > 0) {
+    request(0);
+    if (tiles.n > 1) {
+      request(1);
+      landed_but<2 * T::LOADS>();
+    } else {
+      landed_but<0>();
+    }
+    // tiles from..to - 1 are seen by all
+    const int w0 = r0 + s.ahead, w1 = r1 + s.ahead;
+    const int to = min(max(tiles.sink_tiles + (w0 + 1) / kTile - tiles.first, 0), tiles.n);
+    const int from = p.window > 0 ? min(tiles.sink_tiles + max((max(w1 - p.window + 1, 0) + kTile - 1) / kTile - tiles.first, 0), to) : 0;
+    int t = 0;
+#pragma unroll 1
+    for (int round = 0; round < 2; ++round) {
+      for (const int end = round == 0 && from < to ? from : tiles.n; t < end; ++t) tile_alone(t);
+      if (t + 1 >= to) continue;
+      f32x16 za = zero16(), zb;
+      const typename T::Reader keys(lds0 + (t & 1) * T::BYTES, reader, false);
+#pragma unroll
+      for (int i = 0; i < T::KS; ++i) za = mma(T::rows(keys, 0, 0, i), q[i], za);
+      most = largest(za);
+      for (; t + 1 < to; ++t) {
+        step(za, zb, lds0 + (t & 1) * T::BYTES + 32 * T::ROW, v_at);
+        next_tile(t);
+        step(zb, za, lds0 + (~t & 1) * T::BYTES, v_at + 32 * T::ROW);
+        next_values();
+      }
     }
   }
-  sum += __shfl_xor(sum, 32);
   const bool there = row < s.nq;
+  const float total = sum + __shfl_xor(sum, 32);
   const int64_t dense = ((int64_t)(s.q0 + row) * p.heads + item.head) * p.dim;
-  T::store(p.y + dense, p.low ? p.low + dense : nullptr, there, p.dim, lane, o, sum > 0.f || sum != sum ? 1.f / sum : 0.f);
-  if (p.lse && there && lane < 32) p.lse[(int64_t)item.head * p.n_rows + s.q0 + row] = top * kLn2 + __logf(sum);
+  T::store(p.y + dense, p.low ? p.low + dense : nullptr, there, p.dim, lane, o, total > 0.f || total != total ? 1.f / total : 0.f);
+  if (p.lse && there && lane < 32) p.lse[(int64_t)item.head * p.n_rows + s.q0 + row] = top * kLn2 + __logf(total);
 }
 
 // ---- the gradients of k and v: how their work is cut ------------------------------------------------------------
@@ -354,13 +440,18 @@ __device__ __forceinline__ V block_upto(V v, V *waves, V &all) {
   __syncthreads();
   return before + upto;
 }
-// The pieces, in the order of the sequences and their keys.
+// The pieces, long ones first (in kSizes classes).  Three passes over the parts of the keys: their tiles, how many pieces of each size,
+// where each goes.
+constexpr int kSizes = 64;
 __device__ __forceinline__ void plan_pieces(const AttendRowsParams &p, uint8_t *lds) {
   int64_t *waves = reinterpret_cast<int64_t *>(lds);
-  int64_t *past = waves + kWaves;  // parts of the chunk's sequences up to and with each
+  int64_t *past = waves + kWaves;                              // parts of the chunk's sequences up to and with each
+  int *sizes = reinterpret_cast<int *>(past + kBlock);         // pieces of a size, then where the next one of it goes
   const int per = p.heads / p.kv_heads, tid = threadIdx.x;
-  int64_t total = 0, share = 0, pieces = 0, slots = 0, all;
-  for (int pass = 0; pass < 2; ++pass) {
+  int64_t total = 0, share = 0, all;
+  if (tid < kSizes) sizes[tid] = 0;
+  for (int pass = 0; pass < 3; ++pass) {
+    int64_t slots = 0;
     for (int s0 = 0; s0 < p.n_seqs; s0 += kBlock) {
       const int64_t n = s0 + tid < p.n_seqs ? (sequence_of(p, s0 + tid).nk + kOwn - 1) / kOwn : 0;
       int64_t parts;
@@ -384,8 +475,10 @@ __device__ __forceinline__ void plan_pieces(const AttendRowsParams &p, uint8_t *
         const int64_t slot = slots + block_upto((int64_t)(n > 1 ? n : 0), waves, all) - n;
         slots += all;
         if (n > 1 && slot + n > p.max_slots) n = 1;  // (only where sequences overlap)
-        const int64_t piece = pieces + block_upto((int64_t)n, waves, all) - n;
-        pieces += all;
+        if (n == 0) continue;
+        const int size = kSizes - 1 - (int)min((int64_t)tiles / n * kSizes / (3 * share / 2 + 1), (int64_t)kSizes - 1);
+        const int piece = atomicAdd(&sizes[size], n);  // (the order of equals changes no result)
+        if (pass == 1) continue;
         for (int i = 0; i < n; ++i) {
           const int from = (int)((int64_t)tiles * i / n), to = (int)((int64_t)tiles * (i + 1) / n);
           if (piece + i < p.max_pieces) p.pieces[piece + i] = KeyPiece{s0 + at, part, from, to - from, i, n, (int)slot};
@@ -396,9 +489,13 @@ __device__ __forceinline__ void plan_pieces(const AttendRowsParams &p, uint8_t *
     if (pass == 0) {
       block_upto(total, waves, all);
       share = max((all * p.kv_heads + kShares - 1) / kShares, (int64_t)kLeast);
+    } else if (pass == 1 && tid < 64) {
+      const int n = sizes[tid], upto = sum_upto(n);
+      sizes[tid] = upto - n;
+      if (tid == kSizes - 1) *p.n_pieces = min(upto, p.max_pieces);
     }
+    __syncthreads();
   }
-  if (tid == 0) *p.n_pieces = (int)min(pieces, (int64_t)p.max_pieces);
 }
 
 template <int KS>
@@ -412,7 +509,7 @@ __global__ __launch_bounds__(kBlock, 2) void attend_rows_dq_kernel(const AttendR
   }
   const Item item = item_of(p.heads, p.kv_heads, kLead);
   if (item.part >= parts) return;
-  const Part part = part_of<false>(p, item.part);
+  const Part part = part_of(p, item.part);
   if (part.sequence < 0) {
     clear_rows(p.offsets, p.n_seqs, p.n_rows, p.dq, item.head, p.heads, p.dim, part.over, parts - (item.part - part.over));
     return;
