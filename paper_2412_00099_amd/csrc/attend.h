@@ -15,7 +15,7 @@ struct HeadRows {
 struct PlanPagesParams {
   const int32_t *have, *more, *free, *used;  // used may be NULL
   int32_t *table, *offsets, *slots, *positions, *lengths, *used_out;
-  int32_t n_seqs, page, n_free, table_pages, n_tokens;
+  int32_t n_seqs, page_bits, n_free, table_pages, n_tokens;
 };
 hipError_t launch_plan_pages(const PlanPagesParams &p, hipStream_t s);
 
@@ -59,7 +59,7 @@ struct AttendRowsParams {
   // backward
   const uint16_t *dy;
   uint16_t *dq, *dk, *dv;
-  float *delta;  // [heads][n_rows]: <dy, y>
+  float *stats;  // [2][heads][n_rows]: -lse to the base 2, -<dy, y>
   int32_t *n_pieces;
   KeyPiece *pieces;
   float *sums;  // [max_slots][kv_heads][128 keys][2][dim]: of pieces

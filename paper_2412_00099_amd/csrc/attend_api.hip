@@ -126,7 +126,7 @@ int moe_plan_pages(const int32_t *have, const int32_t *more, int32_t n_seqs, int
       off(lengths, 4) || off(used_out, 4))
     return fail(MOE_EINVAL, "a pointer is not aligned to its type");
   if (used_out == used || (n_seqs > 0 && (lengths == have || lengths == more))) return fail(MOE_EINVAL, "a result overlaps what is read");
-  const PlanPagesParams p{have, more, free_pages, used, table, offsets, slots, positions, lengths, used_out, n_seqs, page, n_free, table_pages, n_tokens};
+  const PlanPagesParams p{have, more, free_pages, used, table, offsets, slots, positions, lengths, used_out, n_seqs, page_bits(page), n_free, table_pages, n_tokens};
   HIP_TRY(launch_plan_pages(p, static_cast<hipStream_t>(stream)));
   return MOE_OK;
 }

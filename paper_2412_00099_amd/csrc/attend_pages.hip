@@ -28,6 +28,7 @@ constexpr int kWaves = 8;        // of a workgroup: two for each SIMD
 constexpr int kGroups = 256;     // workgroups: one for each compute unit
 constexpr int kWorkers = kGroups * kWaves;
 constexpr int kCols = 16;        // heads of a product
+constexpr int kWholeTiles = 64;  // up to so many a workgroup may take a (sequence, group) by itself
 constexpr uint32_t kNowhere = 0xf8000000u;
 
 // The workspace: the share of a worker, in tiles; per sequence the place of its first tile on the line; then, for each worker, what
@@ -68,7 +69,7 @@ __device__ __forceinline__ Seen seen_of(const AttendPagesParams &p, int length) 
   return s;
 }
 
-template <int CACHE, int DT>
+template <int CACHE, int DT, bool WHOLE>
 struct Attend {
   static constexpr bool INT8 = CACHE == MOE_R_INT8;
   static constexpr int EL = INT8 ? 1 : 2;
@@ -95,6 +96,10 @@ struct Attend {
     a.s = seen_of(p, constant(p.lengths)[a.seq]);
   }
   __device__ __forceinline__ void step(Spot &a) const {
+    if constexpr (WHOLE) {
+      a.tile += kWaves;
+      return;
+    }
     if (++a.tile < a.s.tiles) return;
     a.tile = 0;
     if (++a.group < n_groups) return;
@@ -191,32 +196,43 @@ struct Attend {
     const int per = p.heads / p.c.kv_heads;
     per_kv = (per + kCols - 1) / kCols;
     n_groups = p.c.kv_heads * per_kv;
-    // the line, and this worker's share of it
-    int64_t all = 0;
-    for (int s0 = 0; s0 < p.n_seqs; s0 += 64) all += s0 + lane < p.n_seqs ? seen_of(p, p.lengths[s0 + lane]).tiles : 0;
-    all = of_lane(sum_upto(all), 63) * n_groups;
-    const int64_t share = max((all + kWorkers - 1) / kWorkers, (int64_t)1), begin = worker * share;
-    const Parts parts = parts_of(p);
-    if (worker == 0 && lane == 0) *parts.share = share;
-    if (begin >= all) return;
-    int left = (int)min(share, all - begin);
     Spot now{0, 0, 0, {}};
-    int64_t before = 0;
-    for (int s0 = 0; s0 < p.n_seqs; s0 += 64) {
-      const int tiles = s0 + lane < p.n_seqs ? seen_of(p, p.lengths[s0 + lane]).tiles : 0;
-      const int64_t past = before + sum_upto((int64_t)tiles) * n_groups;
-      const uint64_t behind = __ballot(past > begin);
-      if (behind != 0) {
-        const int at = __builtin_ctzll(behind), n = of_lane(tiles, at);
-        const int64_t in = begin - (of_lane(past, at) - (int64_t)n * n_groups);
-        now.seq = uniform(s0 + at);
-        now.group = uniform((int)(in / n));
-        now.tile = uniform((int)(in % n));
-        break;
+    int left;
+    int64_t begin = 0;
+    const Parts parts = parts_of(p);
+    if constexpr (WHOLE) {
+      now.seq = uniform(blockIdx.x / n_groups);
+      now.group = uniform(blockIdx.x % n_groups);
+      now.tile = worker % kWaves;
+      open(now);
+      left = (max(now.s.tiles - now.tile, 0) + kWaves - 1) / kWaves;
+    } else {
+      // the line, and this worker's share of it
+      int64_t all = 0;
+      for (int s0 = 0; s0 < p.n_seqs; s0 += 64) all += s0 + lane < p.n_seqs ? seen_of(p, p.lengths[s0 + lane]).tiles : 0;
+      all = of_lane(sum_upto(all), 63) * n_groups;
+      const int64_t share = max((all + kWorkers - 1) / kWorkers, (int64_t)1);
+      begin = worker * share;
+      if (worker == 0 && lane == 0) *parts.share = share;
+      if (begin >= all) return;
+      left = (int)min(share, all - begin);
+      int64_t before = 0;
+      for (int s0 = 0; s0 < p.n_seqs; s0 += 64) {
+        const int tiles = s0 + lane < p.n_seqs ? seen_of(p, p.lengths[s0 + lane]).tiles : 0;
+        const int64_t past = before + sum_upto((int64_t)tiles) * n_groups;
+        const uint64_t behind = __ballot(past > begin);
+        if (behind != 0) {
+          const int at = __builtin_ctzll(behind), n = of_lane(tiles, at);
+          const int64_t in = begin - (of_lane(past, at) - (int64_t)n * n_groups);
+          now.seq = uniform(s0 + at);
+          now.group = uniform((int)(in / n));
+          now.tile = uniform((int)(in % n));
+          break;
+        }
+        before = of_lane(past, 63);
       }
-      before = of_lane(past, 63);
+      open(now);
     }
-    open(now);
     int64_t line = begin;
     Spot then = now;
     int then_left = left;
@@ -250,7 +266,7 @@ struct Attend {
         head0 = kv * per + part * kCols;
         heads = min(per - part * kCols, kCols);
         from_start = now.tile == 0;
-        if (from_start && now.group == 0 && lane == 0) parts.start[now.seq] = line;
+        if (!WHOLE && from_start && now.group == 0 && lane == 0) parts.start[now.seq] = line;
         const uint16_t *qp = static_cast<const uint16_t *>(p.q.at) + now.seq * p.q.token + (head0 + min(l, heads - 1)) * p.q.head;
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
@@ -349,7 +365,7 @@ struct Attend {
       next();
       stage = stage + 1 == RING ? 0 : stage + 1;
       const bool ends = now.tile + 1 == now.s.tiles;
-      if (ends || left == 1) {
+      if (!WHOLE && (ends || left == 1)) {
         sum += __shfl_xor(sum, 16);
         sum += __shfl_xor(sum, 32);
         if (from_start && ends) {
@@ -378,22 +394,63 @@ struct Attend {
       if (left > 1) step(now);
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (nothing is under way into LDS when the workgroup ends)
+    if constexpr (WHOLE) join(now, fresh, o, top, sum);
+  }
+
+  // WHOLE: what the workgroup's wavefronts have of the heads, through LDS.  none: this one has seen no tile.
+  __device__ __forceinline__ void join(const Spot &now, bool none, const f32x4 (&o)[DS], float top, float sum) {
+    uint8_t *all = lds - (threadIdx.x >> 6) * WAVE_LDS;
+    float *sums = reinterpret_cast<float *>(all), *stats = sums + kWaves * kCols * DT;  // [wave][head][dim], [wave][head][2]
+    const int wave = threadIdx.x >> 6, heads_of_kv = p.heads / p.c.kv_heads;
+    __syncthreads();
+    if (none) {
+      top = -INFINITY;
+      sum = 0.f;
+    }
+    sum += __shfl_xor(sum, 16);
+    sum += __shfl_xor(sum, 32);
+    const int row = wave * kCols + l;
+#pragma unroll
+    for (int d = 0; d < DS; ++d) *reinterpret_cast<f32x4 *>(sums + row * DT + d * 16 + q * 4) = none ? f32x4{0.f, 0.f, 0.f, 0.f} : o[d];
+    if (q == 0) {
+      stats[row * 2] = top;
+      stats[row * 2 + 1] = sum;
+    }
+    __syncthreads();
+    const int h = threadIdx.x / 32, c = threadIdx.x % 32 * 4, head0 = now.group / per_kv * heads_of_kv + now.group % per_kv * kCols;
+    if (h >= min(heads_of_kv - now.group % per_kv * kCols, kCols) || c >= p.c.dim) return;
+    float most = -INFINITY, total = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) most = fmaxf(most, stats[(w * kCols + h) * 2]);
+    const float base = most == -INFINITY ? 0.f : most;
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float weight = __builtin_amdgcn_exp2f(stats[(w * kCols + h) * 2] - base);
+      total += weight * stats[(w * kCols + h) * 2 + 1];
+      v += weight * *reinterpret_cast<const f32x4 *>(sums + (w * kCols + h) * DT + c);
+    }
+    v *= total > 0.f || total != total ? 1.f / total : 0.f;
+    *reinterpret_cast<rows_u32x2 *>(p.y + ((int64_t)now.seq * p.heads + head0 + h) * p.c.dim + c) = rows_u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
   }
 };
 
-template <int CACHE, int DT>
+template <int CACHE, int DT, bool WHOLE>
 __global__ __launch_bounds__(kWaves * 64, 2) void attend_pages_kernel(const AttendPagesParams p) {
-  __shared__ __align__(16) uint8_t lds[kWaves * Attend<CACHE, DT>::WAVE_LDS];
+  using A = Attend<CACHE, DT, WHOLE>;
+  static_assert(kWaves * kCols * (DT + 2) * 4 <= kWaves * A::WAVE_LDS, "the join's sums go where the rings were");
+  __shared__ __align__(16) uint8_t lds[kWaves * A::WAVE_LDS];
   const int wave = uniform(threadIdx.x >> 6);
-  Attend<CACHE, DT> a{p};
-  a.run(uniform(blockIdx.x * kWaves) + wave, lds + wave * Attend<CACHE, DT>::WAVE_LDS);
+  A a{p};
+  a.run(uniform(blockIdx.x * kWaves) + wave, lds + wave * A::WAVE_LDS);
 }
 
 // One workgroup for each (sequence, head): its parts, or zeros where nothing is seen
 constexpr int kJoinBlock = 256;
 __global__ __launch_bounds__(kJoinBlock) void join_pages_kernel(const AttendPagesParams p) {
-  __shared__ float part[kJoinBlock / 32][MOE_ATTEND_MAX_DIM + 1];
-  __shared__ float tops[kJoinBlock / 64];
+  constexpr int STRIPS = kJoinBlock / 32;
+  __shared__ float weights[kWorkers], part[STRIPS][MOE_ATTEND_MAX_DIM];
+  __shared__ float tops[kJoinBlock / 64], totals[kJoinBlock / 64];
   const int seq = blockIdx.x / p.heads, head = blockIdx.x % p.heads, tid = threadIdx.x;
   const Seen s = seen_of(p, p.lengths[seq]);
   uint16_t *y = p.y + ((int64_t)seq * p.heads + head) * p.c.dim;
@@ -404,11 +461,11 @@ __global__ __launch_bounds__(kJoinBlock) void join_pages_kernel(const AttendPage
   const Parts parts = parts_of(p);
   const int per = p.heads / p.c.kv_heads, per_kv = (per + kCols - 1) / kCols, kv = head / per, in = head % per;
   const int64_t share = *parts.share, from = parts.start[seq] + (int64_t)(kv * per_kv + in / kCols) * s.tiles;
-  const int first = (int)(from / share), last = (int)((from + s.tiles - 1) / share);
-  if (first == last) return;  // (one worker had all of it)
-  const auto row_of = [&](int w) { return ((int64_t)w * 2 + (w == first ? 1 : 0)) * parts.rows + in % kCols; };
-  float top = -INFINITY;
-  for (int w = first + tid; w <= last; w += kJoinBlock) top = fmaxf(top, parts.stats[row_of(w) * 2]);
+  const int first = (int)(from / share), n = (int)((from + s.tiles - 1) / share) - first + 1;
+  if (n == 1) return;  // (one worker had all of it)
+  const auto row_of = [&](int i) { return ((int64_t)(first + i) * 2 + (i == 0 ? 1 : 0)) * parts.rows + in % kCols; };
+  float top = -INFINITY, total = 0.f;
+  for (int i = tid; i < n; i += kJoinBlock) top = fmaxf(top, weights[i] = parts.stats[row_of(i) * 2]);
 #pragma unroll
   for (int m = 1; m < 64; m <<= 1) top = fmaxf(top, __shfl_xor(top, m));
   if ((tid & 63) == 0) tops[tid >> 6] = top;
@@ -416,34 +473,53 @@ __global__ __launch_bounds__(kJoinBlock) void join_pages_kernel(const AttendPage
 #pragma unroll
   for (int i = 0; i < kJoinBlock / 64; ++i) top = fmaxf(top, tops[i]);
   const float base = top == -INFINITY ? 0.f : top;
-  const int strip = tid / 32, d = tid % 32 * 4;
-  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  float sum = 0.f;
-  for (int w = first + strip; w <= last; w += kJoinBlock / 32) {
-    const int64_t row = row_of(w);
-    const float weight = __builtin_amdgcn_exp2f(parts.stats[row * 2] - base);
-    sum += weight * parts.stats[row * 2 + 1];
-    if (d < p.c.dim) acc += weight * *reinterpret_cast<const f32x4 *>(parts.sums + row * p.c.dim + d);
+  for (int i = tid; i < n; i += kJoinBlock) {
+    weights[i] = __builtin_amdgcn_exp2f(weights[i] - base);
+    total += weights[i] * parts.stats[row_of(i) * 2 + 1];
   }
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (d < p.c.dim) part[strip][d + i] = acc[i];
-  if (tid % 32 == 0) part[strip][MOE_ATTEND_MAX_DIM] = sum;
+  for (int m = 1; m < 64; m <<= 1) total += __shfl_xor(total, m);
+  if ((tid & 63) == 0) totals[tid >> 6] = total;
+  __syncthreads();
+  const int strip = tid / 32, d = tid % 32 * 4;
+  if (d < p.c.dim) {
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    int i = strip;
+    for (; i + 7 * STRIPS < n; i += 8 * STRIPS) {
+      f32x4 v[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = *reinterpret_cast<const f32x4 *>(parts.sums + row_of(i + k * STRIPS) * p.c.dim + d);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) acc += weights[i + k * STRIPS] * v[k];
+    }
+    for (; i < n; i += STRIPS) acc += weights[i] * *reinterpret_cast<const f32x4 *>(parts.sums + row_of(i) * p.c.dim + d);
+    *reinterpret_cast<f32x4 *>(&part[strip][d]) = acc;
+  }
   __syncthreads();
   if (tid < p.c.dim) {
-    float v = 0.f, n = 0.f;
+    float v = 0.f;
+    total = 0.f;
 #pragma unroll
-    for (int i = 0; i < kJoinBlock / 32; ++i) {
-      v += part[i][tid];
-      n += part[i][MOE_ATTEND_MAX_DIM];
-    }
-    y[tid] = (uint16_t)pack_bf16(n > 0.f || n != n ? v / n : 0.f, 0.f);
+    for (int i = 0; i < STRIPS; ++i) v += part[i][tid];
+#pragma unroll
+    for (int i = 0; i < kJoinBlock / 64; ++i) total += totals[i];
+    y[tid] = (uint16_t)pack_bf16(total > 0.f || total != total ? v / total : 0.f, 0.f);
   }
 }
 
 template <int CACHE, int DT>
 hipError_t attend_with(const AttendPagesParams &p, hipStream_t s) {
-  attend_pages_kernel<CACHE, DT><<<kGroups, kWaves * 64, 0, s>>>(p);
+  const int per = p.heads / p.c.kv_heads, groups = p.n_seqs * p.c.kv_heads * ((per + kCols - 1) / kCols);
+  const int64_t width = (int64_t)p.table_pages << p.c.page_bits;  // no sequence has more
+  const int64_t most = p.window > 0 ? std::min<int64_t>(width, (int64_t)p.window + p.sinks + 2 * kTile) : width;
+  if (most <= kWholeTiles * kTile && groups <= kGroups) {
+    attend_pages_kernel<CACHE, DT, true><<<groups, kWaves * 64, 0, s>>>(p);
+    return hipGetLastError();
+  }
+  attend_pages_kernel<CACHE, DT, false><<<kGroups, kWaves * 64, 0, s>>>(p);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  join_pages_kernel<<<p.n_seqs * p.heads, kJoinBlock, 0, s>>>(p);
   return hipGetLastError();
 }
 
@@ -454,12 +530,8 @@ size_t attend_pages_bytes(int n_seqs, int heads, int kv_heads, int dim) {
 }
 
 hipError_t launch_attend_pages(const AttendPagesParams &p, int cache_fmt, hipStream_t s) {
-  hipError_t e;
-  if (cache_fmt == MOE_R_INT8) e = p.c.dim <= 64 ? attend_with<MOE_R_INT8, 64>(p, s) : attend_with<MOE_R_INT8, 128>(p, s);
-  else e = p.c.dim <= 64 ? attend_with<MOE_R_BF16, 64>(p, s) : attend_with<MOE_R_BF16, 128>(p, s);
-  if (e != hipSuccess) return e;
-  join_pages_kernel<<<p.n_seqs * p.heads, kJoinBlock, 0, s>>>(p);
-  return hipGetLastError();
+  if (cache_fmt == MOE_R_INT8) return p.c.dim <= 64 ? attend_with<MOE_R_INT8, 64>(p, s) : attend_with<MOE_R_INT8, 128>(p, s);
+  return p.c.dim <= 64 ? attend_with<MOE_R_BF16, 64>(p, s) : attend_with<MOE_R_BF16, 128>(p, s);
 }
 
 }  // namespace moe

@@ -551,7 +551,13 @@ __global__ __launch_bounds__(kBlock, 2) void attend_rows_dq_kernel(const AttendR
   }
   T::own(static_cast<const uint16_t *>(p.q.at) + at_row * p.q.token + item.head * p.q.head, there, p.dim, lane, q);
   const float lse = p.lse[(int64_t)item.head * p.n_rows + at_row] * kLog2e, scale = p.scale * kLog2e;
-  if (there && lane < 32) p.delta[(int64_t)item.head * p.n_rows + at_row] = delta;
+  if (there && lane < 32) {
+    p.stats[(int64_t)item.head * p.n_rows + at_row] = -lse;
+    p.stats[(int64_t)(p.heads + item.head) * p.n_rows + at_row] = -delta;
+  }
+  f32x16 less_delta;  // what dP begins with
+#pragma unroll
+  for (int i = 0; i < 16; ++i) less_delta[i] = -delta;
   f32x16 o[T::DS];
 #pragma unroll
   for (int d = 0; d < T::DS; ++d) o[d] = zero16();
@@ -567,13 +573,14 @@ __global__ __launch_bounds__(kBlock, 2) void attend_rows_dq_kernel(const AttendR
       const int key0 = key + m * 32;
       if (see_none(p, p0, p1, key0, key0 + 31)) continue;
       const typename T::Reader at(lds_at(lds) + (t & 1) * 2 * T::BYTES + m * 32 * T::ROW, reader, false);
-      f32x16 z = zero16(), dp = zero16();
+      f32x16 z = zero16(), dp = less_delta;
 #pragma unroll
-      for (int i = 0; i < T::KS; ++i) z = mma(T::rows(at, 0, 0, i), q[i], z);
+      for (int i = 0; i < T::KS; ++i) {
+        z = mma(T::rows(at, 0, 0, i), q[i], z);
+        dp = mma(T::rows(at, T::BYTES, 0, i), dy[i], dp);
+      }
 #pragma unroll
-      for (int i = 0; i < T::KS; ++i) dp = mma(T::rows(at, T::BYTES, 0, i), dy[i], dp);
-#pragma unroll
-      for (int i = 0; i < 16; ++i) z[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i], scale, -lse)) * (dp[i] - delta);
+      for (int i = 0; i < 16; ++i) z[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i], scale, -lse)) * dp[i];
       if (!see_all(p, p0, p1, key0, key0 + 31)) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) z[i] = sees(p, pos, key0 + i / 4 * 8 + (lane >> 5) * 4 + i % 4) ? z[i] : 0.f;
@@ -623,7 +630,7 @@ __global__ __launch_bounds__(kBlock, 2) void attend_rows_dkv_kernel(const Attend
     T::request(qs, static_cast<const uint16_t *>(p.q.at) + (int64_t)(s.q0 + row) * p.q.token + head * p.q.head, rows, p.q.token, p.dim, wave, to);
     T::request(ds, p.dy + ((int64_t)(s.q0 + row) * p.heads + head) * p.dim, rows, (int64_t)p.heads * p.dim, p.dim, wave, to + T::BYTES);
     const int64_t at = (int64_t)head * p.n_rows + s.q0 + row;
-    if (wave < 2) word_to_lds(words_of((wave == 0 ? p.lse : p.delta) + at, (uint32_t)min(rows, kTile) * 4), lane * 4, stats + ((t & 1) * 2 + wave) * kTile * 4);
+    if (wave < 2) word_to_lds(words_of(p.stats + (wave == 0 ? at : at + (int64_t)p.heads * p.n_rows), (uint32_t)min(rows, kTile) * 4), lane * 4, stats + ((t & 1) * 2 + wave) * kTile * 4);
   };
   i32x4 k[T::KS], v[T::KS];
   const int64_t at_key = s.k0 + min(key, s.nk - 1);
@@ -639,27 +646,30 @@ __global__ __launch_bounds__(kBlock, 2) void attend_rows_dkv_kernel(const Attend
   for (int t = 0; t < all; ++t, row = row + kTile < end ? row + kTile : first) {
     landed_but<0>();
     if (t + 1 < all) request(t + 1);
-    const float *lse = reinterpret_cast<const float *>(stats + (t & 1) * 2 * kTile * 4), *delta = lse + kTile;
+    const float *less_lse = reinterpret_cast<const float *>(stats + (t & 1) * 2 * kTile * 4), *less_delta = less_lse + kTile;
     if (mine > k1) continue;
 #pragma unroll 1
     for (int m = 0; m < 2; ++m) {
       const int row0 = row + m * 32, p0 = row0 + s.ahead, p1 = min(row0 + 31, s.nq - 1) + s.ahead;
       if (row0 >= s.nq || see_none(p, p0, p1, mine, mine + 31)) continue;
       const typename T::Reader at(lds_at(lds) + (t & 1) * 2 * T::BYTES + m * 32 * T::ROW, reader, true);
-      f32x16 z = zero16(), dp = zero16();
-#pragma unroll
-      for (int i = 0; i < T::KS; ++i) z = mma(T::rows(at, 0, 0, i), k[i], z);
-#pragma unroll
-      for (int i = 0; i < T::KS; ++i) dp = mma(T::rows(at, T::BYTES, 0, i), v[i], dp);
+      f32x16 z = zero16(), dp;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const f32x4 l4 = *reinterpret_cast<const f32x4 *>(lse + m * 32 + i * 8 + (lane >> 5) * 4);
-        const f32x4 d4 = *reinterpret_cast<const f32x4 *>(delta + m * 32 + i * 8 + (lane >> 5) * 4);
+        const f32x4 d4 = *reinterpret_cast<const f32x4 *>(less_delta + m * 32 + i * 8 + (lane >> 5) * 4);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          z[4 * i + j] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[4 * i + j], scale, -l4[j] * kLog2e));
-          dp[4 * i + j] -= d4[j];
-        }
+        for (int j = 0; j < 4; ++j) dp[4 * i + j] = d4[j];
+      }
+#pragma unroll
+      for (int i = 0; i < T::KS; ++i) {
+        z = mma(T::rows(at, 0, 0, i), k[i], z);
+        dp = mma(T::rows(at, T::BYTES, 0, i), v[i], dp);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const f32x4 l4 = *reinterpret_cast<const f32x4 *>(less_lse + m * 32 + i * 8 + (lane >> 5) * 4);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) z[4 * i + j] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[4 * i + j], scale, l4[j]));
       }
       if (!see_all(p, p0, p1, mine, mine + 31)) {
 #pragma unroll
@@ -737,7 +747,7 @@ hipError_t launch_attend_rows(const AttendRowsParams &p, hipStream_t s) {
   return hipGetLastError();
 }
 
-// The workspace: delta, the pieces, their sums.  A list of n tiles is cut if n > 1.5 shares, into n / share + 1 pieces at most, so that
+// The workspace: what the gradients of k and v need of each query, the pieces, their sums.  A list of n tiles is cut if n > 1.5 shares, into n / share + 1 pieces at most, so that
 // there are 5 / 3 pieces of lists that are cut for each of all lists' shares, at most kShares.
 struct BackwardSpace {
   int64_t pieces, sums, bytes;  // where they begin
@@ -751,7 +761,7 @@ static BackwardSpace backward_space(int n_rows, int n_k_rows, int n_seqs, int he
   w.max_slots = 2 * list > 3 * kLeast ? (int)(5 * shares / (3 * kv_heads) + 1) : 0;
   w.max_pieces = parts + (w.max_slots > 0 ? kShares / kv_heads + 1 : 0);
   const auto up = [](int64_t v) { return (v + 255) / 256 * 256; };
-  w.pieces = up((int64_t)n_rows * heads * 4);
+  w.pieces = up((int64_t)n_rows * heads * 8);
   w.sums = up(w.pieces + 16 + (int64_t)w.max_pieces * sizeof(KeyPiece));
   w.bytes = w.sums + (int64_t)w.max_slots * kv_heads * kOwn * 2 * dim * 4;
   return w;
@@ -763,7 +773,7 @@ size_t attend_rows_backward_bytes(int n_rows, int n_k_rows, int n_seqs, int head
 hipError_t launch_attend_rows_backward(const AttendRowsParams &given, uint8_t *workspace, hipStream_t s) {
   AttendRowsParams p = given;
   const BackwardSpace w = backward_space(p.n_rows, p.n_k_rows, p.n_seqs, p.heads, p.kv_heads, p.dim);
-  p.delta = reinterpret_cast<float *>(workspace);
+  p.stats = reinterpret_cast<float *>(workspace);
   p.n_pieces = reinterpret_cast<int32_t *>(workspace + w.pieces);
   p.pieces = reinterpret_cast<KeyPiece *>(workspace + w.pieces + 16);
   p.sums = reinterpret_cast<float *>(workspace + w.sums);

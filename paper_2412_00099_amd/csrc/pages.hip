@@ -26,7 +26,7 @@ __global__ __launch_bounds__(kPlanBlock) void plan_pages_kernel(const PlanPagesP
   const int64_t step = (int64_t)gridDim.x * kPlanBlock, mine = (int64_t)blockIdx.x * kPlanBlock + tid;
   const int64_t used = p.used ? *p.used : 0;
   int64_t all_tokens = 0, all_taken = 0;
-  const auto pages_of = [&](int64_t n) { return min((n + p.page - 1) / p.page, (int64_t)p.table_pages); };
+  const auto pages_of = [&](int64_t n) { return min((n + (1 << p.page_bits) - 1) >> p.page_bits, (int64_t)p.table_pages); };
   const auto free_page = [&](int64_t i) { return i >= 0 && i < p.n_free ? p.free[i] : -1; };
   for (int s0 = 0; s0 < p.n_seqs; s0 += kChunk) {
     int64_t have[kEach], more[kEach], take[kEach], upto_tokens = 0, upto_taken = 0;
@@ -83,11 +83,11 @@ __global__ __launch_bounds__(kPlanBlock) void plan_pages_kernel(const PlanPagesP
     const int64_t end = min(tokens[kChunk], (int64_t)p.n_tokens);
     for (int64_t v = first(tokens[0]); v < end; v += step) {
       const int c = of(tokens, v), s = s0 + c;
-      const int64_t had = max(p.have[s], 0), pos = had + (v - tokens[c]), old = pages_of(had), at = pos / p.page;
+      const int64_t had = max(p.have[s], 0), pos = had + (v - tokens[c]), old = pages_of(had), at = pos >> p.page_bits;
       int64_t slot = -1;
       if (at < p.table_pages) {
         const int64_t page = at < old ? p.table[(int64_t)s * p.table_pages + at] : free_page(used + taken[c] + (at - old));
-        slot = page < 0 ? -1 : page * p.page + pos % p.page;
+        slot = page < 0 ? -1 : page << p.page_bits | (pos & ((1 << p.page_bits) - 1));
       }
       p.slots[v] = slot > INT32_MAX ? -1 : (int)slot;
       p.positions[v] = to32(pos);
