@@ -11,10 +11,11 @@
 // The other side's rows go through LDS in tiles of 64, two at a time, one computed while the next one is loaded, for all four
 // wavefronts of a workgroup.
 //
-// P and dZ are rounded to bf16 for the matrix cores; in two parts each they would cost a third of the products more.  The error that
-// this makes is as large as that of the results' own rounding (together 0.0022 to 0.0025 of their size, 0.0017 for the results' alone).  delta is
-// the same for all keys of a query, and with Y as it is rounded it was the next largest part (0.0027): the forward keeps what the
-// rounding of Y leaves, in bf16.
+// P and dZ are rounded to bf16 for the matrix cores.  The error that this makes is as large as that of the results' own rounding
+// (gradients 0.0024 of their size together, 0.0017 for the results' alone); dZ in two parts would cost a third (dQ) and a quarter
+// (dK) of the products more, and is taken in two parts only where queries do not see all keys of a tile: all of a short sequence.  delta
+// is the same for all keys of a query, and with Y as it is rounded it would be the next largest part of the error (0.0027): the
+// forward keeps what the rounding of Y leaves, in bf16.
 //
 // Which sequence and which of its rows a workgroup has is worked out from the offsets on the device.  Loads go through buffer
 // resources that end where the sequence ends: what lies beyond arrives as zeros.
@@ -195,6 +196,28 @@ __device__ __forceinline__ i32x4 summed(const f32x16 &p, int t) {
   return f;
 }
 
+// what the rounding of rows 16 t .. of it leaves
+__device__ __forceinline__ i32x4 left_over(const f32x16 &p, int t) {
+  i32x4 f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float a = p[8 * t + 2 * i], b = p[8 * t + 2 * i + 1];
+    const uint32_t r = pack_bf16(a, b);
+    f[i] = (int)pack_bf16(a - bf16_lo(r), b - bf16_hi(r));
+  }
+  return f;
+}
+// sum + the values of f, as they are rounded
+__device__ __forceinline__ float add_up(float sum, const i32x4 &f) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int two = f[i];  // (a bit cast of f[i] itself takes element 0 of f, whatever i is)
+    sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, two), __builtin_bit_cast(bf16x2, 0x3f803f80), sum, false);
+  }
+  return sum;
+}
+
 struct Item {
   int part, head;  // behind the last one: no part
 };
@@ -247,7 +270,9 @@ __device__ __forceinline__ bool sees(const AttendRowsParams &p, int pos, int key
 // each other: the scores of the next 32 keys while the exponentials of these are taken, and the product with the values while the
 // largest of the next scores is found.  The other tiles (the diagonal, a window's edge, first keys) are computed one by one and masked.
 // Tiles are requested two ahead; there is one barrier for each, in its middle or at its end, and values have three places in LDS.
-template <int KS>
+// Y is divided by the sum of the exponentials as they are rounded, so that the rounding of one that outweighs the others cancels (the
+// error of Y 0.0022 of its size otherwise); KEEP: lse is of the sum in 32 bits, since the backward takes the exponentials anew.
+template <int KS, bool KEEP>
 __global__ __launch_bounds__(kBlock, 2) void attend_rows_kernel(const AttendRowsParams p, const int parts) {
   using T = Tiles<KS>;
   __shared__ __align__(256) uint8_t lds[5 * T::BYTES];
@@ -277,7 +302,7 @@ __global__ __launch_bounds__(kBlock, 2) void attend_rows_kernel(const AttendRows
   };
   i32x4 q[T::KS];
   f32x16 o[T::DS];
-  float top = -INFINITY, most = -INFINITY, sum = 0.f;
+  float top = -INFINITY, most = -INFINITY, sum = 0.f, rounded = 0.f;
   T::own(static_cast<const uint16_t *>(p.q.at) + (s.q0 + min(row, s.nq - 1)) * p.q.token + item.head * p.q.head, row < s.nq, p.dim, lane, q);
 #pragma unroll
   for (int d = 0; d < T::DS; ++d) o[d] = zero16();
@@ -290,13 +315,15 @@ __global__ __launch_bounds__(kBlock, 2) void attend_rows_kernel(const AttendRows
     }
   };
   const auto next_values = [&] { v_at = v_at == lds0 + 4 * T::BYTES ? lds0 + 2 * T::BYTES : v_at + T::BYTES; };
-  // The base of the exponentials follows the largest score (of the query's two lanes; most: of the lane's own) when that is 2^8
-  // ahead: until then nothing is multiplied and no lane asks the other one
-  const auto rebase = [&]() MOE_ROWS_INLINE {
-    if (__any(most * scale > top + 8.f)) {
+  // The base of the exponentials follows the largest score (of the query's two lanes; most: of the lane's own) when that is `slack`
+  // ahead (to the base 2): until then nothing is multiplied and no lane asks the other one.  No slack: the largest exponential is 1,
+  // which has no rounding, and that counts for queries that see few keys.
+  const auto rebase = [&](float slack) MOE_ROWS_INLINE {
+    if (__any(most * scale > top + slack)) {
       const float to = fmaxf(top, fmaxf(most, __shfl_xor(most, 32)) * scale), shrink = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(top - to);
       top = to;
-      sum *= shrink;
+      if (KEEP) sum *= shrink;
+      rounded *= shrink;
 #pragma unroll
       for (int d = 0; d < T::DS; ++d) o[d] *= shrink;
     }
@@ -314,14 +341,15 @@ __global__ __launch_bounds__(kBlock, 2) void attend_rows_kernel(const AttendRows
       for (int i = 0; i < 16; ++i) z[i] = sees(p, pos, key + i / 4 * 8 + (lane >> 5) * 4 + i % 4) ? z[i] : -INFINITY;
     }
     most = largest(z);
-    rebase();
+    rebase(0.f);
     const float base = top == -INFINITY ? 0.f : top;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       z[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i], scale, -base));
-      sum += z[i];
+      if (KEEP) sum += z[i];
     }
     const i32x4 f[2] = {summed(z, 0), summed(z, 1)};
+    rounded = add_up(add_up(rounded, f[0]), f[1]);
 #pragma unroll
     for (int i = 0; i < 2 * T::DS; ++i) o[i % T::DS] = mma(T::columns(values, 0, i / T::DS * 16, i % T::DS), f[i / T::DS], o[i % T::DS]);
   };
@@ -335,7 +363,7 @@ __global__ __launch_bounds__(kBlock, 2) void attend_rows_kernel(const AttendRows
   // z: the scores of 32 keys, `most` the largest; their values are at `values_at`.  next: those of the 32 keys at `k_at`.
   const auto step = [&](f32x16 &z, f32x16 &next, uint32_t k_at, uint32_t values_at) MOE_ROWS_INLINE {
     const typename T::Reader keys(k_at, reader, false), values(values_at, reader, false);
-    rebase();
+    rebase(8.f);
     constexpr int EACH = (16 + T::KS - 1) / T::KS, PVS = 2 * T::DS, AHEAD = 3;
     i32x4 a[AHEAD + 1], c[AHEAD + 1];
 #pragma unroll
@@ -350,7 +378,7 @@ __global__ __launch_bounds__(kBlock, 2) void attend_rows_kernel(const AttendRows
 #pragma unroll
       for (int e = i * EACH; e < (i + 1) * EACH && e < 16; ++e) {
         z[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[e], scale, -top));
-        sum += z[e];
+        if (KEEP) sum += z[e];
       }
     }
     __builtin_amdgcn_sched_barrier(0);
@@ -361,6 +389,7 @@ __global__ __launch_bounds__(kBlock, 2) void attend_rows_kernel(const AttendRows
       __builtin_amdgcn_sched_barrier(0);
       if (i + AHEAD < PVS) c[(i + AHEAD) % (AHEAD + 1)] = T::columns(values, 0, (i + AHEAD) / T::DS * 16, (i + AHEAD) % T::DS);
       o[i % T::DS] = mma(c[i % (AHEAD + 1)], f[i / T::DS], o[i % T::DS]);
+      if (i < 2) rounded = add_up(rounded, f[i]);
       if (i >= PVS - 4) {
 #pragma unroll
         for (int e = (i - PVS + 4) * 4; e < (i - PVS + 5) * 4; ++e) most = fmaxf(most, next[e]);
@@ -400,10 +429,11 @@ __global__ __launch_bounds__(kBlock, 2) void attend_rows_kernel(const AttendRows
     }
   }
   const bool there = row < s.nq;
-  const float total = sum + __shfl_xor(sum, 32);
+  const float total = rounded + __shfl_xor(rounded, 32);
   const int64_t dense = ((int64_t)(s.q0 + row) * p.heads + item.head) * p.dim;
   T::store(p.y + dense, p.low ? p.low + dense : nullptr, there, p.dim, lane, o, total > 0.f || total != total ? 1.f / total : 0.f);
-  if (p.lse && there && lane < 32) p.lse[(int64_t)item.head * p.n_rows + s.q0 + row] = top * kLn2 + __logf(total);
+  if (KEEP) sum += __shfl_xor(sum, 32);
+  if (KEEP && there && lane < 32) p.lse[(int64_t)item.head * p.n_rows + s.q0 + row] = top * kLn2 + __logf(sum);
 }
 
 // ---- the gradients of k and v: how their work is cut ------------------------------------------------------------
@@ -581,15 +611,24 @@ __global__ __launch_bounds__(kBlock, 2) void attend_rows_dq_kernel(const AttendR
       }
 #pragma unroll
       for (int i = 0; i < 16; ++i) z[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i], scale, -lse)) * dp[i];
-      if (!see_all(p, p0, p1, key0, key0 + 31)) {
+      bool again = !see_all(p, p0, p1, key0, key0 + 31);
+      i32x4 low[2];
+      if (again) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) z[i] = sees(p, pos, key0 + i / 4 * 8 + (lane >> 5) * 4 + i % 4) ? z[i] : 0.f;
+        low[0] = left_over(z, 0);
+        low[1] = left_over(z, 1);
       }
+      i32x4 f[2] = {summed(z, 0), summed(z, 1)};
+#pragma unroll 1
+      for (;; again = false) {  // (one product in the code: two keep the sums in twice the registers)
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const i32x4 f = summed(z, i);
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int d = 0; d < T::DS; ++d) o[d] = mma(T::columns(at, 0, i * 16, d), f, o[d]);
+          for (int d = 0; d < T::DS; ++d) o[d] = mma(T::columns(at, 0, i * 16, d), f[i], o[d]);
+        if (!again) break;
+        f[0] = low[0];
+        f[1] = low[1];
       }
     }
   }
@@ -671,20 +710,32 @@ __global__ __launch_bounds__(kBlock, 2) void attend_rows_dkv_kernel(const Attend
 #pragma unroll
         for (int j = 0; j < 4; ++j) z[4 * i + j] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[4 * i + j], scale, l4[j]));
       }
-      if (!see_all(p, p0, p1, mine, mine + 31)) {
+      bool again = !see_all(p, p0, p1, mine, mine + 31);
+      if (again) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) z[i] = sees(p, p0 + i / 4 * 8 + (lane >> 5) * 4 + i % 4, key) ? z[i] : 0.f;
       }
 #pragma unroll
       for (int i = 0; i < 16; ++i) dp[i] *= z[i];
+      const i32x4 f[2] = {summed(z, 0), summed(z, 1)};
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const i32x4 f = summed(z, i), g = summed(dp, i);
+      for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int d = 0; d < T::DS; ++d) {
-          dv[d] = mma(T::columns(at, T::BYTES, i * 16, d), f, dv[d]);
-          dk[d] = mma(T::columns(at, 0, i * 16, d), g, dk[d]);
-        }
+        for (int d = 0; d < T::DS; ++d) dv[d] = mma(T::columns(at, T::BYTES, i * 16, d), f[i], dv[d]);
+      i32x4 g[2] = {summed(dp, 0), summed(dp, 1)}, low[2];
+      if (again) {
+        low[0] = left_over(dp, 0);
+        low[1] = left_over(dp, 1);
+      }
+#pragma unroll 1
+      for (;; again = false) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int d = 0; d < T::DS; ++d) dk[d] = mma(T::columns(at, 0, i * 16, d), g[i], dk[d]);
+        if (!again) break;
+        g[0] = low[0];
+        g[1] = low[1];
       }
     }
   }
@@ -743,7 +794,11 @@ void with_steps(int dim, F f) {
 
 hipError_t launch_attend_rows(const AttendRowsParams &p, hipStream_t s) {
   const int parts = parts_of(p.n_rows, p.n_seqs);
-  with_steps(p.dim, [&](auto ks) { attend_rows_kernel<decltype(ks)::value><<<grid_of(parts, p.heads), kBlock, 0, s>>>(p, parts); });
+  with_steps(p.dim, [&](auto ks) {
+    constexpr int KS = decltype(ks)::value;
+    if (p.lse) attend_rows_kernel<KS, true><<<grid_of(parts, p.heads), kBlock, 0, s>>>(p, parts);
+    else attend_rows_kernel<KS, false><<<grid_of(parts, p.heads), kBlock, 0, s>>>(p, parts);
+  });
   return hipGetLastError();
 }
 
