@@ -413,7 +413,8 @@ int moe_experts_rows_backward(int32_t weight_fmt, int32_t hidden, int32_t inter,
  * head; the values of a head are dense.  Pointers and strides of bf16 rows that are read are multiples of 16 bytes.
  *   A query at position p sees key j if j <= p and (window 0, or j > p - window, or j < sinks).
  *   z_j = softmax_scale <q, k_j>, y = sum_j exp(z_j - lse) v_j, lse = log sum_j exp(z_j), over the keys that it sees; y is 0 (lse
- *   -infinity) if there are none.  Sums are held in 32 bits; keys and values that nobody sees may hold anything.
+ *   -infinity) if there are none.  Sums are held in 32 bits.  What a query does not see
+ *   may hold anything.
  *
  * A cache has n_pages pages of `page` tokens (a power of two, 16 to 1024), page_stride elements from page to page:
  *   k_pages, v_pages [n_pages][n_kv_heads][page][head_dim]; page * n_pages < 2^31
@@ -445,7 +446,8 @@ int moe_experts_rows_backward(int32_t weight_fmt, int32_t hidden, int32_t inter,
  *   others are left alone.
  * moe_attend_rows_backward: from dy the gradients of q, k and v, dense, bf16 (rows of no sequence: 0).  y, y_low, lse: as the forward left
  *   them (y_low_dev NULL: y is taken as it is, which makes the error of dq and dk about a tenth larger).  P = exp(z - lse), dv = sum P dy, dz = P (<dy, v> - <dy, y>), dq = softmax_scale sum dz k, dk = softmax_scale sum dz q, sums
- *   over the heads of a group and over all queries in a fixed order.  P and dz are rounded to bf16 for the matrix cores.  y and dy
+ *   over the heads of a group and over all queries in a fixed order.  P and dz are rounded to bf16 for the matrix cores.  Infinities and
+ *   NaN in a sequence may make NaN of any of its gradients (of no other sequence's).  y and dy
  *   dense.  The workspace: moe_attend_rows_backward_bytes bytes, 16-byte aligned, of this call alone until it is done. */
 int moe_plan_pages(const int32_t *have_dev, const int32_t *more_dev, int32_t n_seqs, int32_t page, const int32_t *free_dev, int32_t n_free,
                    const int32_t *used_dev, int32_t *table_dev, int32_t table_pages, int32_t *offsets_dev, int32_t *slots_dev,

@@ -207,6 +207,67 @@ __device__ __forceinline__ i32x4 left_over(const f32x16 &p, int t) {
   }
   return f;
 }
+// Where some queries do not see a key, its exponential is 0, but a product with an infinity or NaN would not be: the forward looks for
+// such values wherever something is masked, and adds them apart.  (The backward does not: its kernels have no registers left for it.)
+enum { kPlusInf = 0, kMinusInf = 1, kNotANumber = 2 };
+template <typename F>
+__device__ __forceinline__ i32x4 each_bf16(const i32x4 &c, F f) {  // f of each value's bits
+  i32x4 r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t two = c[i];
+    r[i] = (int)(f(two & 0xffffu) | f(two >> 16) << 16);
+  }
+  return r;
+}
+__device__ __forceinline__ i32x4 finite_of(const i32x4 &c) {
+  return each_bf16(c, [](uint32_t v) { return (v & 0x7f80u) == 0x7f80u ? 0u : v; });
+}
+__device__ __forceinline__ i32x4 ones_where(const i32x4 &c, int kind) {
+  return each_bf16(c, [kind](uint32_t v) {
+    const bool is = kind == kPlusInf ? v == 0x7f80u : kind == kMinusInf ? v == 0xff80u : (v & 0x7fffu) > 0x7f80u;
+    return is ? 0x3f80u : 0u;
+  });
+}
+// whether any of 32 rows of a tile holds an infinity or NaN
+template <typename T>
+__device__ __forceinline__ bool odd_rows(const typename T::Reader &at, uint32_t in) {
+  typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+  u16x2 most = {0, 0};
+#pragma unroll
+  for (int s = 0; s < T::KS; ++s) {
+    const i32x4 x = T::rows(at, in, 0, s);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t two = x[i] & 0x7fff7fff;
+      most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, two));
+    }
+  }
+  return __any(max(most[0], most[1]) >= 0x7f80);
+}
+// rows 16 t .. of what `seen` has a bit for, as 1 and 0
+__device__ __forceinline__ i32x4 ones_of(uint32_t seen, int t) {
+  i32x4 f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) f[i] = (int)((seen >> (8 * t + 2 * i) & 1) * 0x3f80u | (seen >> (8 * t + 2 * i + 1) & 1) * 0x3f800000u);
+  return f;
+}
+// o + the product of 32 rows' columns with f, in which a row that holds an infinity or NaN counts where `seen` has a bit (register i of
+// the lane: bit i).
+template <typename T>
+__device__ __forceinline__ void add_apart(const typename T::Reader &at, uint32_t in, const i32x4 (&f)[2], uint32_t seen, f32x16 (&o)[T::DS]) {
+#pragma unroll
+  for (int d = 0; d < T::DS; ++d) {
+    o[d] += mma(finite_of(T::columns(at, in, 16, d)), f[1], mma(finite_of(T::columns(at, in, 0, d)), f[0], zero16()));
+#pragma unroll 1
+    for (int kind = 0; kind < 3; ++kind) {
+      const f32x16 n = mma(ones_where(T::columns(at, in, 16, d), kind), ones_of(seen, 1), mma(ones_where(T::columns(at, in, 0, d), kind), ones_of(seen, 0), zero16()));
+      const float value = kind == kNotANumber ? NAN : kind == kPlusInf ? INFINITY : -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[d][i] += n[i] > 0.f ? value : 0.f;
+    }
+  }
+}
 // sum + the values of f, as they are rounded
 __device__ __forceinline__ float add_up(float sum, const i32x4 &f) {
   typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -336,9 +397,16 @@ __global__ __launch_bounds__(kBlock, 2) void attend_rows_kernel(const AttendRows
     f32x16 z = zero16();
 #pragma unroll
     for (int i = 0; i < T::KS; ++i) z = mma(T::rows(keys, 0, 0, i), q[i], z);
+    bool odd = false;
+    uint32_t seen = 0;
     if (!see_all(p, p0, p1, key, key + 31)) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) z[i] = sees(p, pos, key + i / 4 * 8 + (lane >> 5) * 4 + i % 4) ? z[i] : -INFINITY;
+      for (int i = 0; i < 16; ++i) {
+        const bool is = sees(p, pos, key + i / 4 * 8 + (lane >> 5) * 4 + i % 4);
+        seen |= is ? 1u << i : 0u;
+        z[i] = is ? z[i] : -INFINITY;
+      }
+      odd = odd_rows<T>(values, 0);
     }
     most = largest(z);
     rebase(0.f);
@@ -350,6 +418,10 @@ __global__ __launch_bounds__(kBlock, 2) void attend_rows_kernel(const AttendRows
     }
     const i32x4 f[2] = {summed(z, 0), summed(z, 1)};
     rounded = add_up(add_up(rounded, f[0]), f[1]);
+    if (odd) {
+      add_apart<T>(values, 0, f, seen, o);
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < 2 * T::DS; ++i) o[i % T::DS] = mma(T::columns(values, 0, i / T::DS * 16, i % T::DS), f[i / T::DS], o[i % T::DS]);
   };
