@@ -164,6 +164,127 @@ def test_rows(lib, case):
         close(got, *want[n], n)
 
 
+@pytest.mark.parametrize("window,sinks,dim", [(0, 0, 128), (0, 0, 64), (60, 0, 80), (60, 40, 128)])
+@pytest.mark.parametrize("what", [math.nan, math.inf, -math.inf])
+def test_rows_that_are_not_seen_may_hold_anything(lib, window, sinks, dim, what):
+    """Behind the last sequence, in another sequence, ahead of a window, and of the same sequence but later on."""
+    g = gen(dim + window)
+    each, H, KV = [300, 90], 4, 2
+    q = normal(g, 400, H, dim, std=2.0, dtype=BF16)
+    k, v = normal(g, 400, KV, dim, dtype=BF16), normal(g, 400, KV, dim, dtype=BF16)
+    want = reference(q[:390], k[:390], v[:390], each, each, window, sinks, dim ** -0.5)["y"]
+    q[390:], k[390:], v[390:] = what, what, what
+    at = 133
+    v[at, 0, 5] = what   # of one key: dim 5 of heads 0 and 1
+    v[at + 1, 1] = what  # of the next one: all of heads 2 and 3
+    k[at + 37, 1, 0] = math.nan
+    y = lib.attend_rows(q, k, v, ints(starts(each)), window=window, sinks=sinks)
+    assert not y[390:].any()
+    clean = torch.ones(390, H, dim, dtype=torch.bool, device=DEV)
+    ok = visible(300, 300, window, sinks)
+    clean[:300][ok[:, at], 0:2, 5] = False
+    clean[:300, 2:][ok[:, at + 1] | ok[:, at + 37]] = False
+    over = (y[:390].double() - want[0]).abs() - want[1] * (1 + 2 * U)
+    assert float(torch.where(clean, over, -1.0).max()) <= 0  # (a comparison with NaN would be false)
+    got = y[:300].float()
+    assert bool(torch.isfinite(got[clean[:300]]).all())
+    one = got[ok[:, at]][:, 0:2, 5]
+    assert bool((one.isnan() if what != what else one == what).all())
+    # (rows that see the NaN key are NaN, the others have the values' infinities)
+    two = got[ok[:, at + 1] & ~ok[:, at + 37]][:, 2:]
+    assert bool((two.isnan() if what != what else two == what).all())
+    assert bool(got[ok[:, at + 37]][:, 2:].isnan().all())
+
+
+def test_gradients_of_other_sequences(lib):
+    """An infinity or NaN stays in its sequence's gradients."""
+    g = gen(7)
+    each = [100, 70, 130]
+    offsets = ints(starts(each))
+    q, k, v, dy = (normal(g, 310, h, 96, dtype=BF16) for h in (4, 2, 2, 4))
+    want = reference(q[:300], k[:300], v[:300], each, each, 0, 0, 96 ** -0.5, dy[:300])
+    for t in (q, k, v, dy):
+        t[100:170] = math.nan
+        t[300:] = math.inf
+    y, kept = lib.attend_rows(q, k, v, offsets, keep=True)
+    for n, got in zip(("y", "dq", "dk", "dv"), (y, *lib.attend_rows_backward(q, k, v, offsets, y, kept, dy))):
+        assert not got[300:].any() and bool(got[100:170].isnan().all())
+        rows = torch.tensor([i for i in range(300) if not 100 <= i < 170], device=DEV)
+        close(got[rows], want[n][0][rows], want[n][1][rows], n)
+
+
+def test_offsets_that_do_not_fit(lib):
+    """Rows ahead of the first sequence and behind the last; offsets beyond the rows or out of order read nothing out of range."""
+    g = gen(3)
+    q, k, v, dy = (normal(g, 200, h, 64, dtype=BF16) for h in (2, 1, 1, 2))
+    want = reference(q[20:150], k[20:150], v[20:150], [60, 70], [60, 70], 0, 0, 0.125, dy[20:150])
+    offsets = ints([20, 80, 150])
+    y, kept = lib.attend_rows(q, k, v, offsets, keep=True)
+    for n, got in zip(("y", "dq", "dk", "dv"), (y, *lib.attend_rows_backward(q, k, v, offsets, y, kept, dy))):
+        assert not got[:20].any() and not got[150:].any()
+        close(got[20:150], *want[n], n)
+    y = lib.attend_rows(q, k, v, ints([20, 80, 1 << 30]))  # (the last sequence has the rows that there are)
+    want = reference(q[20:], k[20:], v[20:], [60, 120], [60, 120], 0, 0, 0.125)
+    close(y[20:], *want["y"], "y")
+    for bad in ([150, 20, -5], [-(1 << 31), (1 << 31) - 1, 0]):
+        y, kept = lib.attend_rows(q, k, v, ints(bad), keep=True)
+        lib.attend_rows_backward(q, k, v, ints(bad), torch.zeros_like(y), lib.KeptAttention(torch.zeros_like(kept.lse), None), dy)
+        torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("layout", ["heads first", "one projection", "wide", "one head"])
+def test_layouts(lib, layout):
+    g = gen(11)
+    T, H, KV, D = 230, 4, 2, 64
+    if layout == "heads first":
+        q, k, v = (normal(g, h, T, D, dtype=BF16).transpose(0, 1) for h in (H, KV, KV))
+    elif layout == "one projection":
+        x = normal(g, T, (H + 2 * KV) * D, dtype=BF16)
+        q, k, v = x[:, :H * D].view(T, H, D), x[:, H * D:(H + KV) * D].view(T, KV, D), x[:, (H + KV) * D:].view(T, KV, D)
+    elif layout == "wide":
+        q, k, v = (normal(g, T, h, 3, D + 8, dtype=BF16)[:, :, 1, :D] for h in (H, KV, KV))
+    else:
+        H = KV = 1
+        q, k, v = (normal(g, T, 1, D, dtype=BF16) for _ in range(3))
+    dy = normal(g, T, H, D, dtype=BF16)
+    offsets, kw = ints([0, 100, T]), dict(window=50, sinks=2, scale=0.2)
+    y, kept = lib.attend_rows(q, k, v, offsets, keep=True, **kw)
+    want = reference(q, k, v, [100, T - 100], [100, T - 100], 50, 2, 0.2, dy)
+    for n, got in zip(("y", "dq", "dk", "dv"), (y, *lib.attend_rows_backward(q, k, v, offsets, y, kept, dy, **kw))):
+        close(got, *want[n], n)
+
+
+def test_gradients_against_differences(lib):
+    """The loss <y, w> along a direction of each input: the gradient's product with it against a central difference of the same
+    calls.  q, k, v are whole multiples of 2^-6 up to 2 and steps of 2^-4 keep them bf16.  Third derivatives are below 4 along these
+    directions in 64 bits (a step of h gives h^2 / 6 of them), and y's roundings of U each are independent in thousands of terms."""
+    g = gen(13)
+    T, H, KV, D = 96, 2, 1, 32
+    q, k, v = ((normal(g, T, h, D) * 16).round().clamp(-64, 64) / 64 for h in (H, KV, KV))
+    w = normal(g, T, H, D, dtype=BF16)
+    offsets = ints([0, 40, T])
+
+    def loss(q, k, v):
+        return float((lib.attend_rows(q.to(BF16), k.to(BF16), v.to(BF16), offsets, window=30, sinks=2).double() * w.double()).sum())
+
+    def exact(q, k, v):
+        return float((reference(q, k, v, [40, T - 40], [40, T - 40], 30, 2, D ** -0.5)["y"][0] * w.double()).sum())
+
+    b = [t.to(BF16) for t in (q, k, v)]
+    y, kept = lib.attend_rows(*b, offsets, window=30, sinks=2, keep=True)
+    grads = lib.attend_rows_backward(*b, offsets, y, kept, w, window=30, sinks=2)
+    h = 2.0 ** -4
+    noise = 4 * U * float((y.double() * w.double()).square().sum()) ** 0.5 / h  # (four times the spread of two sums of roundings)
+    for i, grad in enumerate(grads):
+        step = torch.randint(-1, 2, b[i].shape, generator=g, device=DEV).float()
+        plus, minus = [list((q, k, v)) for _ in range(2)]
+        plus[i], minus[i] = plus[i] + h * step, minus[i] - h * step
+        along = float((grad.double() * step.double()).sum())
+        curved = abs((exact(*plus) - exact(*minus)) / (2 * h) - float((reference(*b, [40, T - 40], [40, T - 40], 30, 2, D ** -0.5, w)[("dq", "dk", "dv")[i]][0] * step.double()).sum()))
+        size = 4 * U * float((grad.double() * step.double()).square().sum()) ** 0.5
+        assert abs((loss(*plus) - loss(*minus)) / (2 * h) - along) <= noise + size + curved, i
+
+
 # ---- plan --------------------------------------------------------------------------------------------------
 def plan_by_hand(have, more, table, free, used, page, n_tokens):
     table, width = [list(r) for r in table], len(table[0]) if table else 0
@@ -387,3 +508,205 @@ def test_pages_that_are_not_there(lib):
     want = paged_reference(q[:1], [[k[-30:], v[-30:]]], 0, 0, 0.125)
     close(y[:1], *want, "window")
     assert not y[1:].any()
+
+
+# ---- how the calls are made --------------------------------------------------------------------------------
+def serve_setup(lib, cache=BF16, seed=17, **kw):
+    """Three requests: their prompts by attend_rows, stored; then tokens one by one."""
+    g = gen(seed)
+    H, KV, D, page, prompts, steps = 4, 2, 64, 16, [37, 1, 90], 20
+    n = [p + steps for p in prompts]
+    q = [normal(g, m, H, D, std=2.0, dtype=BF16) for m in n]
+    k, v = ([normal(g, m, KV, D, dtype=BF16) for m in n] for _ in range(2))
+    pages = [torch.full((40, KV, page, D), math.nan, device=DEV).to(BF16) if cache == BF16 else torch.full((40, KV, page, D), 3, dtype=I8, device=DEV) for _ in range(2)]
+    scales = [torch.full((40, KV, page), math.nan, device=DEV) for _ in range(2)] if cache == I8 else [None, None]
+    return dict(H=H, KV=KV, D=D, page=page, prompts=prompts, steps=steps, q=q, k=k, v=v, pages=pages, scales=scales, table=torch.full((3, 8), -1, dtype=I32, device=DEV),
+                free=torch.randperm(40, generator=g, device=DEV).int())
+
+
+def step_rows(s, key, t):
+    return torch.stack([x[p + t] for x, p in zip(s[key], s["prompts"])])
+
+
+@pytest.mark.parametrize("cache", [BF16, I8])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (24, 3)])
+def test_prompts_then_tokens(lib, cache, window, sinks):
+    """plan, store and both attentions together: tokens one by one give what the whole sequence gives at once."""
+    s = serve_setup(lib, cache)
+    want = []
+    for q, k, v in zip(s["q"], s["k"], s["v"]):
+        want.append(reference(q, k, v, [q.shape[0]], [q.shape[0]], window, sinks, s["D"] ** -0.5)["y"])
+    cat = lambda key: torch.cat([x[:p] for x, p in zip(s[key], s["prompts"])])  # noqa: E731
+    plan = lib.plan_pages(ints([0, 0, 0]), ints(s["prompts"]), s["table"], s["free"], s["page"], sum(s["prompts"]) + 3)
+    pad = torch.nn.functional.pad
+    rows = [pad(cat(key), (0, 0, 0, 0, 0, 3)) for key in ("q", "k", "v")]
+    y = lib.attend_rows(*rows, plan.offsets, window=window, sinks=sinks)
+    assert not y[-3:].any()
+    for i, p in enumerate(s["prompts"]):
+        a = int(plan.offsets[i])
+        close(y[a:a + p], want[i][0][:p], want[i][1][:p], "prompt")
+    lib.store_pages(rows[1], rows[2], plan.slots, *s["pages"], *s["scales"])
+    ones = ints([1, 1, 1])
+    for t in range(s["steps"]):
+        plan = lib.plan_pages(plan.lengths, ones, s["table"], s["free"], s["page"], 3, used=plan.used)
+        lib.store_pages(step_rows(s, "k", t), step_rows(s, "v", t), plan.slots, *s["pages"], *s["scales"])
+        y = lib.attend_pages(step_rows(s, "q", t), *s["pages"], s["table"], plan.lengths, *s["scales"], window=window, sinks=sinks)
+        for i, p in enumerate(s["prompts"]):
+            if cache == BF16:
+                close(y[i], want[i][0][p + t], want[i][1][p + t], "token")
+            else:  # a code is off by half a step of 1/127 of the largest of 64 normal values (2.5) at most, at random in each key and value
+                assert float((y[i].double() - want[i][0][p + t]).norm() / want[i][0][p + t].norm()) <= 0.05
+    assert plan.lengths.tolist() == [p + s["steps"] for p in s["prompts"]]
+    assert int(plan.used) == sum(up(p + s["steps"], s["page"]) for p in s["prompts"])
+
+
+def test_a_captured_step_is_replayed(lib):
+    """One decoding step as a graph: plan, store, attend; lengths and used go round in the graph's own tensors."""
+    s = serve_setup(lib)
+    pad_rows = [torch.cat([x[:p] for x, p in zip(s[key], s["prompts"])]) for key in ("k", "v")]
+    first = lib.plan_pages(ints([0, 0, 0]), ints(s["prompts"]), s["table"], s["free"], s["page"], sum(s["prompts"]))
+    lib.store_pages(*pad_rows, first.slots, *s["pages"])
+    have, used, ones = first.lengths.clone(), first.used.clone(), ints([1, 1, 1])
+    q, k, v = (step_rows(s, key, 0).clone() for key in ("q", "k", "v"))
+
+    def step():
+        plan = lib.plan_pages(have, ones, s["table"], s["free"], s["page"], 3, used=used)
+        lib.store_pages(k, v, plan.slots, *s["pages"])
+        y = lib.attend_pages(q, *s["pages"], s["table"], plan.lengths)
+        have.copy_(plan.lengths)
+        used.copy_(plan.used)
+        return y
+
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        out = step()
+    other = torch.randn(1 << 20, device=DEV)
+    for t in range(s["steps"]):
+        for to, key in ((q, "q"), (k, "k"), (v, "v")):
+            to.copy_(step_rows(s, key, t))
+        graph.replay()
+        other = other * 1.5 - other.mean()  # (the program's own work in between)
+        if t % 3 == 0:
+            torch.cuda.synchronize()
+        for i, p in enumerate(s["prompts"]):
+            n = p + t + 1
+            want = reference(s["q"][i][:n], s["k"][i][:n], s["v"][i][:n], [n], [n], 0, 0, s["D"] ** -0.5)["y"]
+            close(out[i], want[0][-1], want[1][-1], (t, i))
+
+
+def test_captured_gradients_beside_eager_ones(lib):
+    """attend_rows and its backward in a graph, replayed on other inputs, with eager calls of the same kind in between."""
+    g = gen(23)
+    offsets = ints([0, 300, 1300])
+    ts = [normal(g, 1300, h, 64, dtype=BF16) for h in (16, 1, 1, 16)]
+
+    def both(q, k, v, dy):
+        y, kept = lib.attend_rows(q, k, v, offsets, keep=True)
+        return (y, *lib.attend_rows_backward(q, k, v, offsets, y, kept, dy))
+
+    both(*ts)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        out = both(*ts)
+    for seed in range(4):
+        new = [normal(gen(100 + seed), *t.shape, dtype=BF16) for t in ts]
+        for t, n in zip(ts, new):
+            t.copy_(n)
+        graph.replay()
+        eager = both(*new)
+        torch.cuda.synchronize()
+        for a, b in zip(out, eager):
+            assert torch.equal(a, b)
+
+
+def test_streams_and_calls_at_once(lib):
+    """The calls go to the current stream; two at once have workspaces of their own."""
+    g = gen(29)
+    values, pages, _, table = paged(g, [3000, 40, 900], 2, 128, 16, BF16)
+    q = normal(g, 3, 8, 128, dtype=BF16)
+    want = paged_reference(q, values, 0, 0, 128 ** -0.5)
+    lengths = ints([3000, 40, 900])
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    out = []
+    for _ in range(4):
+        for s in streams:
+            with torch.cuda.stream(s):
+                out.append(lib.attend_pages(q, *pages, table, lengths))
+    torch.cuda.synchronize()
+    close(out[0], *want, "y")
+    assert all(torch.equal(out[0], y) for y in out)
+
+
+def test_offsets_in_a_large_cache(lib):
+    """Pages beyond 2^32 bytes of the cache."""
+    KV, page, D = 8, 64, 128
+    n = (1 << 32) // (KV * page * D * 2) + 40
+    pages = [torch.empty(n, KV, page, D, dtype=BF16, device=DEV) for _ in range(2)]
+    g = gen(31)
+    ids = torch.tensor([n - 1, 3, n - 7, (1 << 32) // (KV * page * D * 2)], dtype=I32, device=DEV)
+    k, v = (normal(g, 250, KV, D, dtype=BF16) for _ in range(2))
+    pos = torch.arange(250, device=DEV)
+    lib.store_pages(k, v, (ids[pos // page] * page + pos % page).int(), *pages)
+    for x, p in zip((k, v), pages):
+        assert torch.equal(p[ids.long()].transpose(1, 2).reshape(-1, KV, D)[:250], x)
+    q = normal(g, 1, 16, D, std=2.0, dtype=BF16)
+    y = lib.attend_pages(q, *pages, ids[None].contiguous(), ints([250]))
+    close(y, *paged_reference(q, [[k.double(), v.double()]], 0, 0, D ** -0.5), "y")
+
+
+def test_nothing_to_do(lib):
+    empty = torch.empty(0, 4, 64, dtype=BF16, device=DEV)
+    y, kept = lib.attend_rows(empty, empty[:, :2], empty[:, :2], ints([0]), keep=True)
+    assert y.shape == empty.shape and kept.lse.shape == (4, 0)
+    k = torch.randn(10, 2, 64, device=DEV).to(BF16)
+    y, kept = lib.attend_rows(empty, k, k, ints([0, 0]), k_offsets=ints([0, 10]), keep=True)
+    dq, dk, dv = lib.attend_rows_backward(empty, k, k, ints([0, 0]), y, kept, empty, k_offsets=ints([0, 10]))
+    assert dq.shape == empty.shape and not dk.any() and not dv.any()
+    q = torch.randn(10, 4, 64, device=DEV).to(BF16)
+    none = torch.empty(0, 2, 64, dtype=BF16, device=DEV)
+    y = lib.attend_rows(q, none, none, ints([0, 10]), k_offsets=ints([0, 0]))
+    assert not y.any()
+    y = lib.attend_rows(q, k, k, ints([0]))  # (no sequence)
+    assert not y.any()
+    pages = torch.empty(0, 2, 16, 64, dtype=BF16, device=DEV)
+    y = lib.attend_pages(q, pages, pages, torch.zeros(10, 3, dtype=I32, device=DEV), ints([5] * 10))
+    assert not y.any()
+    lib.store_pages(k, k, ints([0] * 10), pages, pages)
+    assert lib.attend_pages(empty, pages, pages, torch.zeros(0, 3, dtype=I32, device=DEV), ints([])).shape == empty.shape
+
+
+def test_gradients_are_not_lost_silently(lib):
+    q = torch.randn(10, 2, 64, device=DEV).to(BF16).requires_grad_()
+    with pytest.raises(ValueError, match="gradient"):
+        lib.attend_rows(q, q, q, ints([0, 10]))
+    with torch.no_grad():
+        lib.attend_rows(q, q, q, ints([0, 10]))
+
+
+def test_sizes_are_refused_before_memory_is_taken(lib):
+    q = torch.zeros(1024, 1, 512, dtype=BF16, device=DEV).expand(1024, 600, 512)
+    torch.cuda.synchronize()
+    torch.cuda.reset_peak_memory_stats()
+    before = torch.cuda.memory_allocated()
+    with pytest.raises((lib.MoEError, ValueError)):
+        lib.attend_rows(q, q, q, ints([0, 1024]), keep=True)
+    with pytest.raises((lib.MoEError, ValueError)):
+        lib.plan_pages(ints([1]), ints([1]), ints([[0]]), ints([1]), 16, 1 << 30)
+    assert torch.cuda.max_memory_allocated() - before < 1 << 16
+
+
+def test_calls_through_the_c_entry_points(lib):
+    """Without tensors' part: pointers, another stream, a cache written in place."""
+    g = gen(37)
+    q, k, v = normal(g, 70, 2, 64, dtype=BF16), normal(g, 70, 2, 64, dtype=BF16), normal(g, 70, 2, 64, dtype=BF16)
+    offsets, y = ints([0, 70]), torch.full((70, 2, 64), 9.0, device=DEV).to(BF16)
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    P = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+    lib.moe_attend_rows(P(q), 128, 64, P(k), 128, 64, P(v), 128, 64, P(offsets), None, 1, 70, 70, 2, 2, 64, 0.125, 0, 0, P(y), None, None, stream.cuda_stream)
+    stream.synchronize()
+    close(y, *reference(q, k, v, [70], [70], 0, 0, 0.125)["y"], "y")
+    assert torch.equal(y, lib.attend_rows(q, k, v, offsets))
