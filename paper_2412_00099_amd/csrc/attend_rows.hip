@@ -61,37 +61,35 @@ __device__ __forceinline__ Sequence sequence_of(const AttendRowsParams &p, int s
 // much to do must not be the last to begin.  No such part: sequence -1, and by how much it was missed.
 struct Part {
   int sequence, part, over;
+  Sequence s;
 };
-__device__ __forceinline__ int parts_in(const AttendRowsParams &p, int s) {
-  if (s >= p.n_seqs) return 0;
-  const int from = min(max(p.offsets[s], 0), p.n_rows);
-  return (max(min(p.offsets[s + 1], p.n_rows) - from, 0) + kOwn - 1) / kOwn;
-}
 __device__ __forceinline__ Part part_of(const AttendRowsParams &p, int want) {
   const int lane = threadIdx.x & 63;
   if (p.n_seqs <= 64) {
-    const int n = parts_in(p, lane);
+    const Sequence mine = lane < p.n_seqs ? sequence_of(p, lane) : Sequence{0, 0, 0, 0, 0};
+    const int n = (mine.nq + kOwn - 1) / kOwn;
     const auto from_on = [&](int part) { return of_lane(sum_upto(max(n - part, 0)), 63); };  // parts `part` .. of all sequences
     const int all = from_on(0);
-    if (want >= all) return {-1, 0, want - all};
+    if (want >= all) return {-1, 0, want - all, {}};
     int at = 0, step = 1;  // the last part with `want` or fewer ahead of it and its like
     while (from_on(step) > want) step *= 2;
     for (; step > 0; step /= 2) at += from_on(at + step) > want ? step : 0;
     const int ahead = from_on(at + 1), upto = sum_upto(n > at ? 1 : 0);
-    return {uniform(__builtin_ctzll(__ballot(upto > want - ahead))), uniform(at), 0};
+    const int l = uniform(__builtin_ctzll(__ballot(upto > want - ahead)));
+    return {l, uniform(at), 0, {of_lane(mine.q0, l), of_lane(mine.nq, l), of_lane(mine.k0, l), of_lane(mine.nk, l), of_lane(mine.ahead, l)}};
   }
   // (more sequences: one after the other, since 64 at a time are looked at once)
   int64_t before = 0;
   for (int s0 = 0; s0 < p.n_seqs; s0 += 64) {
-    const int64_t past = before + sum_upto((int64_t)parts_in(p, s0 + lane));
+    const int64_t past = before + sum_upto((int64_t)(s0 + lane < p.n_seqs ? (sequence_of(p, s0 + lane).nq + kOwn - 1) / kOwn : 0));
     const uint64_t behind = __ballot(past > want);
     if (behind != 0) {
       const int at = __builtin_ctzll(behind);
-      return {uniform(s0 + at), uniform((int)(of_lane(past, at) - want) - 1), 0};
+      return {uniform(s0 + at), uniform((int)(of_lane(past, at) - want) - 1), 0, sequence_of(p, uniform(s0 + at))};
     }
     before = of_lane(past, 63);
   }
-  return {-1, 0, uniform((int)(want - before))};
+  return {-1, 0, uniform((int)(want - before)), {}};
 }
 // zeros for the rows of no sequence, shared by `step` workgroups
 __device__ __forceinline__ void clear_rows(const int32_t *offsets, int n_seqs, int n_rows, uint16_t *to, int head, int heads, int dim, int at, int step) {
@@ -169,16 +167,25 @@ struct Tiles {
   }
   // the lane's column of a result, times v; low: and what its rounding leaves, unless nullptr
   static __device__ __forceinline__ void store(uint16_t *at, uint16_t *low, bool there, int dim, int lane, const f32x16 (&o)[DS], float v) {
+    // Of 16 dims a lane has four, then four 8 further on; its other half has those in between.  They exchange four: 16 bytes each.
+    const auto put = [&](uint16_t *to, int d, int i, const uint32_t (&w)[4]) MOE_ROWS_INLINE {
+      const auto a = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false), b = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
+      const int c = d * 32 + i * 16 + (lane >> 5) * 8;
+      if (there && c < dim) *reinterpret_cast<rows_u32x4 *>(to + c) = rows_u32x4{a[0], b[0], a[1], b[1]};
+    };
 #pragma unroll
     for (int d = 0; d < DS; ++d)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int c = d * 32 + i * 8 + (lane >> 5) * 4;
-        if (!there || c >= dim) continue;
-        const float a = o[d][4 * i] * v, b = o[d][4 * i + 1] * v, e = o[d][4 * i + 2] * v, f = o[d][4 * i + 3] * v;
-        const rows_u32x2 r = {pack_bf16(a, b), pack_bf16(e, f)};
-        *reinterpret_cast<rows_u32x2 *>(at + c) = r;
-        if (low) *reinterpret_cast<rows_u32x2 *>(low + c) = rows_u32x2{pack_bf16(a - bf16_lo(r[0]), b - bf16_hi(r[0])), pack_bf16(e - bf16_lo(r[1]), f - bf16_hi(r[1]))};
+      for (int i = 0; i < 2; ++i) {
+        uint32_t w[4], l[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float x = o[d][8 * i + 2 * k] * v, y = o[d][8 * i + 2 * k + 1] * v;
+          w[k] = pack_bf16(x, y);
+          l[k] = pack_bf16(x - bf16_lo(w[k]), y - bf16_hi(w[k]));
+        }
+        put(at, d, i, w);
+        if (low) put(low, d, i, l);
       }
   }
 };
@@ -345,7 +352,7 @@ __global__ __launch_bounds__(kBlock, 2) void attend_rows_kernel(const AttendRows
     clear_rows(p.offsets, p.n_seqs, p.n_rows, p.y, item.head, p.heads, p.dim, part.over, parts - (item.part - part.over));
     return;
   }
-  const Sequence s = sequence_of(p, part.sequence);
+  const Sequence s = part.s;
   const int r0 = part.part * kOwn, r1 = min(r0 + kOwn, s.nq) - 1, mine = r0 + wave * 32, row = mine + (lane & 31);
   const int p0 = mine + s.ahead, p1 = min(mine + 31, r1) + s.ahead, pos = row + s.ahead;
   const int kv = item.head / (p.heads / p.kv_heads);
@@ -482,17 +489,18 @@ __global__ __launch_bounds__(kBlock, 2) void attend_rows_kernel(const AttendRows
     const int w0 = r0 + s.ahead, w1 = r1 + s.ahead;
     const int to = min(max(tiles.sink_tiles + (w0 + 1) / kTile - tiles.first, 0), tiles.n);
     const int from = p.window > 0 ? min(tiles.sink_tiles + max((max(w1 - p.window + 1, 0) + kTile - 1) / kTile - tiles.first, 0), to) : 0;
+    const int fast = min(to, tiles.n - 1);  // (the last one looks ahead in vain, unless there is nothing behind it)
     int t = 0;
 #pragma unroll 1
     for (int round = 0; round < 2; ++round) {
-      for (const int end = round == 0 && from < to ? from : tiles.n; t < end; ++t) tile_alone(t);
-      if (t + 1 >= to) continue;
+      for (const int end = round == 0 && from < fast ? from : tiles.n; t < end; ++t) tile_alone(t);
+      if (t >= fast) continue;
       f32x16 za = zero16(), zb;
       const typename T::Reader keys(lds0 + (t & 1) * T::BYTES, reader, false);
 #pragma unroll
       for (int i = 0; i < T::KS; ++i) za = mma(T::rows(keys, 0, 0, i), q[i], za);
       most = largest(za);
-      for (; t + 1 < to; ++t) {
+      for (; t < fast; ++t) {
         step(za, zb, lds0 + (t & 1) * T::BYTES + 32 * T::ROW, v_at);
         next_tile(t);
         step(zb, za, lds0 + (~t & 1) * T::BYTES, v_at + 32 * T::ROW);
@@ -616,7 +624,7 @@ __global__ __launch_bounds__(kBlock, 2) void attend_rows_dq_kernel(const AttendR
     clear_rows(p.offsets, p.n_seqs, p.n_rows, p.dq, item.head, p.heads, p.dim, part.over, parts - (item.part - part.over));
     return;
   }
-  const Sequence s = sequence_of(p, part.sequence);
+  const Sequence s = part.s;
   const int r0 = part.part * kOwn, r1 = min(r0 + kOwn, s.nq) - 1, mine = r0 + wave * 32, row = mine + (lane & 31);
   const int p0 = mine + s.ahead, p1 = min(mine + 31, r1) + s.ahead, pos = row + s.ahead;
   const int kv = item.head / (p.heads / p.kv_heads);
