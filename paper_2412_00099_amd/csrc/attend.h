@@ -63,7 +63,7 @@ struct AttendRowsParams {
   int32_t *n_pieces;
   KeyPiece *pieces;
   float *sums;  // [max_slots][kv_heads][128 keys][2][dim]: of pieces
-  int32_t max_pieces, max_slots;
+  int32_t max_pieces, max_slots, shares;
 };
 hipError_t launch_attend_rows(const AttendRowsParams &p, hipStream_t s);
 size_t attend_rows_backward_bytes(int n_rows, int n_k_rows, int n_seqs, int heads, int kv_heads, int dim);

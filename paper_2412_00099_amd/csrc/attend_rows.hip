@@ -290,7 +290,8 @@ struct Item {
   int part, head;  // behind the last one: no part
 };
 // Workgroups go to the XCDs in turn, and each XCD has an L2 of its own: where eight divides the heads of k, an XCD has all
-// workgroups of some of them.
+// workgroups of some of them.  (One of these heads after the other, so that fewer are in the L2 at a time, makes the workgroups end less
+// evenly: 8192 tokens, 16 heads of 128, with gradients 395 us, that way 415.)
 __device__ __forceinline__ Item item_of(int heads, int kv_heads, int lead = 0) {
   Item r;
   const uint32_t b = (uint32_t)row_group() - lead;
@@ -520,8 +521,10 @@ __global__ __launch_bounds__(kBlock, 2) void attend_rows_kernel(const AttendRows
 // The queries that see any of kOwn keys, tile by tile, and that for each head of the group, are a list.  Lists are long and few
 // where few heads of k serve many of q, or where first keys stay visible: a list of more than half as many tiles again as a
 // workgroup's equal share is cut into pieces of about a share, whose sums, in 32 bits, are added up in order by a launch of its own.
-// (A piece costs as much as some eight tiles: 128 rows of sums to memory and back.)
-constexpr int kShares = 512;   // workgroups that the GPU holds at once
+// (A piece costs as much as some eight tiles: 128 rows of sums to memory and back.)  There are 512 shares of wide heads, as many as the
+// GPU holds workgroups at once, and more of narrow heads, whose sums are smaller (16384 tokens, 4 heads of 64 for 16, with all else: 512
+// shares 538, 768 499, 1024 481 us; 8192 tokens, 16 heads of 128: 401, 404, 441; 20001 tokens, 2 heads of 80 for 16, window: 669, 663, 659).
+inline int shares_of(int dim) { return std::min(std::max(65536 / dim, 512), 1024); }
 constexpr int kLeast = 16;     // tiles of a share at least
 constexpr int kLead = 8;       // workgroups ahead of those with rows in the launch that plans: one plans, and each XCD has one
 struct List {
@@ -598,7 +601,7 @@ __device__ __forceinline__ void plan_pieces(const AttendRowsParams &p, uint8_t *
     }
     if (pass == 0) {
       block_upto(total, waves, all);
-      share = max((all * p.kv_heads + kShares - 1) / kShares, (int64_t)kLeast);
+      share = max((all * p.kv_heads + p.shares - 1) / p.shares, (int64_t)kLeast);
     } else if (pass == 1 && tid < 64) {
       const int n = sizes[tid], upto = sum_upto(n);
       sizes[tid] = upto - n;
@@ -606,6 +609,45 @@ __device__ __forceinline__ void plan_pieces(const AttendRowsParams &p, uint8_t *
     }
     __syncthreads();
   }
+}
+
+// Products of the backward.  What they read of LDS is requested AHEAD steps before its use, in this order; left to
+// itself the compiler reads right ahead of each use and waits (gradients of k and v, dims of 80: 300 us, so 262; with dims of 128 they have
+// no registers left for it: 165, with what then goes to memory 318).
+// z + 32 rows with x, dp + the 32 rows of the tile behind it with y
+template <typename T, int AHEAD>
+__device__ __forceinline__ void two_products(const typename T::Reader &at, const i32x4 (&x)[T::KS], const i32x4 (&y)[T::KS], f32x16 &z, f32x16 &dp) {
+  i32x4 a[AHEAD + 1], b[AHEAD + 1];
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) {
+    a[i] = T::rows(at, 0, 0, i);
+    b[i] = T::rows(at, T::BYTES, 0, i);
+  }
+#pragma unroll
+  for (int i = 0; i < T::KS; ++i) {
+    __builtin_amdgcn_sched_barrier(0);
+    if (i + AHEAD < T::KS) {
+      a[(i + AHEAD) % (AHEAD + 1)] = T::rows(at, 0, 0, i + AHEAD);
+      b[(i + AHEAD) % (AHEAD + 1)] = T::rows(at, T::BYTES, 0, i + AHEAD);
+    }
+    z = mma(a[i % (AHEAD + 1)], x[i], z);
+    dp = mma(b[i % (AHEAD + 1)], y[i], dp);
+  }
+  __builtin_amdgcn_sched_barrier(0);
+}
+// o + 32 rows' columns with f
+template <typename T, int AHEAD>
+__device__ __forceinline__ void add_columns(const typename T::Reader &at, uint32_t in, const i32x4 (&f)[2], f32x16 (&o)[T::DS]) {
+  i32x4 c[AHEAD + 1];
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) c[i] = T::columns(at, in, i / T::DS * 16, i % T::DS);
+#pragma unroll
+  for (int i = 0; i < 2 * T::DS; ++i) {
+    __builtin_amdgcn_sched_barrier(0);
+    if (i + AHEAD < 2 * T::DS) c[(i + AHEAD) % (AHEAD + 1)] = T::columns(at, in, (i + AHEAD) / T::DS * 16, (i + AHEAD) % T::DS);
+    o[i % T::DS] = mma(c[i % (AHEAD + 1)], f[i / T::DS], o[i % T::DS]);
+  }
+  __builtin_amdgcn_sched_barrier(0);
 }
 
 template <int KS>
@@ -684,11 +726,7 @@ __global__ __launch_bounds__(kBlock, 2) void attend_rows_dq_kernel(const AttendR
       if (see_none(p, p0, p1, key0, key0 + 31)) continue;
       const typename T::Reader at(lds_at(lds) + (t & 1) * 2 * T::BYTES + m * 32 * T::ROW, reader, false);
       f32x16 z = zero16(), dp = less_delta;
-#pragma unroll
-      for (int i = 0; i < T::KS; ++i) {
-        z = mma(T::rows(at, 0, 0, i), q[i], z);
-        dp = mma(T::rows(at, T::BYTES, 0, i), dy[i], dp);
-      }
+      two_products<T, 2>(at, q, dy, z, dp);
 #pragma unroll
       for (int i = 0; i < 16; ++i) z[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i], scale, -lse)) * dp[i];
       bool again = !see_all(p, p0, p1, key0, key0 + 31);
@@ -702,10 +740,7 @@ __global__ __launch_bounds__(kBlock, 2) void attend_rows_dq_kernel(const AttendR
       i32x4 f[2] = {summed(z, 0), summed(z, 1)};
 #pragma unroll 1
       for (;; again = false) {  // (one product in the code: two keep the sums in twice the registers)
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-          for (int d = 0; d < T::DS; ++d) o[d] = mma(T::columns(at, 0, i * 16, d), f[i], o[d]);
+        add_columns<T, 3>(at, 0, f, o);
         if (!again) break;
         f[0] = low[0];
         f[1] = low[1];
@@ -779,10 +814,14 @@ __global__ __launch_bounds__(kBlock, 2) void attend_rows_dkv_kernel(const Attend
 #pragma unroll
         for (int j = 0; j < 4; ++j) dp[4 * i + j] = d4[j];
       }
+      if constexpr (KS < 8) {
+        two_products<T, 2>(at, k, v, z, dp);
+      } else {
 #pragma unroll
-      for (int i = 0; i < T::KS; ++i) {
-        z = mma(T::rows(at, 0, 0, i), k[i], z);
-        dp = mma(T::rows(at, T::BYTES, 0, i), v[i], dp);
+        for (int i = 0; i < T::KS; ++i) {
+          z = mma(T::rows(at, 0, 0, i), k[i], z);
+          dp = mma(T::rows(at, T::BYTES, 0, i), v[i], dp);
+        }
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -798,10 +837,14 @@ __global__ __launch_bounds__(kBlock, 2) void attend_rows_dkv_kernel(const Attend
 #pragma unroll
       for (int i = 0; i < 16; ++i) dp[i] *= z[i];
       const i32x4 f[2] = {summed(z, 0), summed(z, 1)};
+      if constexpr (KS < 8) {
+        add_columns<T, 3>(at, T::BYTES, f, dv);
+      } else {
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int d = 0; d < T::DS; ++d) dv[d] = mma(T::columns(at, T::BYTES, i * 16, d), f[i], dv[d]);
+          for (int d = 0; d < T::DS; ++d) dv[d] = mma(T::columns(at, T::BYTES, i * 16, d), f[i], dv[d]);
+      }
       i32x4 g[2] = {summed(dp, 0), summed(dp, 1)}, low[2];
       if (again) {
         low[0] = left_over(dp, 0);
@@ -809,10 +852,14 @@ __global__ __launch_bounds__(kBlock, 2) void attend_rows_dkv_kernel(const Attend
       }
 #pragma unroll 1
       for (;; again = false) {
+        if constexpr (KS < 8) {
+          add_columns<T, 3>(at, 0, g, dk);
+        } else {
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+          for (int i = 0; i < 2; ++i)
 #pragma unroll
-          for (int d = 0; d < T::DS; ++d) dk[d] = mma(T::columns(at, 0, i * 16, d), g[i], dk[d]);
+            for (int d = 0; d < T::DS; ++d) dk[d] = mma(T::columns(at, 0, i * 16, d), g[i], dk[d]);
+        }
         if (!again) break;
         g[0] = low[0];
         g[1] = low[1];
@@ -883,7 +930,7 @@ hipError_t launch_attend_rows(const AttendRowsParams &p, hipStream_t s) {
 }
 
 // The workspace: what the gradients of k and v need of each query, the pieces, their sums.  A list of n tiles is cut if n > 1.5 shares, into n / share + 1 pieces at most, so that
-// there are 5 / 3 pieces of lists that are cut for each of all lists' shares, at most kShares.
+// there are 5 / 3 pieces of lists that are cut for each of all lists' shares.
 struct BackwardSpace {
   int64_t pieces, sums, bytes;  // where they begin
   int max_pieces, max_slots;
@@ -892,9 +939,9 @@ static BackwardSpace backward_space(int n_rows, int n_k_rows, int n_seqs, int he
   BackwardSpace w;
   const int parts = parts_of(n_k_rows, n_seqs);
   const int64_t list = (int64_t)(heads / kv_heads) * ((n_rows + kTile - 1) / kTile);  // tiles, at most
-  const int64_t shares = std::min<int64_t>(kShares, list * (parts - 1) * kv_heads / kLeast + 1);
+  const int64_t shares = std::min<int64_t>(shares_of(dim), list * (parts - 1) * kv_heads / kLeast + 1);
   w.max_slots = 2 * list > 3 * kLeast ? (int)(5 * shares / (3 * kv_heads) + 1) : 0;
-  w.max_pieces = parts + (w.max_slots > 0 ? kShares / kv_heads + 1 : 0);
+  w.max_pieces = parts + (w.max_slots > 0 ? shares_of(dim) / kv_heads + 1 : 0);
   const auto up = [](int64_t v) { return (v + 255) / 256 * 256; };
   w.pieces = up((int64_t)n_rows * heads * 8);
   w.sums = up(w.pieces + 16 + (int64_t)w.max_pieces * sizeof(KeyPiece));
@@ -913,6 +960,7 @@ hipError_t launch_attend_rows_backward(const AttendRowsParams &given, uint8_t *w
   p.pieces = reinterpret_cast<KeyPiece *>(workspace + w.pieces + 16);
   p.sums = reinterpret_cast<float *>(workspace + w.sums);
   p.max_pieces = w.max_pieces;
+  p.shares = shares_of(p.dim);
   p.max_slots = w.max_slots;
   const int parts = parts_of(p.n_rows, p.n_seqs), k_parts = w.max_pieces + 1;
   with_steps(p.dim, [&](auto ks) { attend_rows_dq_kernel<decltype(ks)::value><<<grid_of(parts, p.heads, kLead), kBlock, 0, s>>>(p, parts); });
