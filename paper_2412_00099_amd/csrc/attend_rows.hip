@@ -57,17 +57,18 @@ __device__ __forceinline__ Sequence sequence_of(const AttendRowsParams &p, int s
   r.ahead = r.nk - r.nq;
   return r;
 }
-// Part `want` of the sequences' rows in parts of kOwn, later parts of the sequences first: they have more keys, and a workgroup with
+// Part `want` of the sequences' rows in parts of OWN, later parts of the sequences first: they have more keys, and a workgroup with
 // much to do must not be the last to begin.  No such part: sequence -1, and by how much it was missed.
 struct Part {
   int sequence, part, over;
   Sequence s;
 };
+template <int OWN = kOwn>
 __device__ __forceinline__ Part part_of(const AttendRowsParams &p, int want) {
   const int lane = threadIdx.x & 63;
   if (p.n_seqs <= 64) {
     const Sequence mine = lane < p.n_seqs ? sequence_of(p, lane) : Sequence{0, 0, 0, 0, 0};
-    const int n = (mine.nq + kOwn - 1) / kOwn;
+    const int n = (mine.nq + OWN - 1) / OWN;
     const auto from_on = [&](int part) { return of_lane(sum_upto(max(n - part, 0)), 63); };  // parts `part` .. of all sequences
     const int all = from_on(0);
     if (want >= all) return {-1, 0, want - all, {}};
@@ -81,7 +82,7 @@ __device__ __forceinline__ Part part_of(const AttendRowsParams &p, int want) {
   // (more sequences: one after the other, since 64 at a time are looked at once)
   int64_t before = 0;
   for (int s0 = 0; s0 < p.n_seqs; s0 += 64) {
-    const int64_t past = before + sum_upto((int64_t)(s0 + lane < p.n_seqs ? (sequence_of(p, s0 + lane).nq + kOwn - 1) / kOwn : 0));
+    const int64_t past = before + sum_upto((int64_t)(s0 + lane < p.n_seqs ? (sequence_of(p, s0 + lane).nq + OWN - 1) / OWN : 0));
     const uint64_t behind = __ballot(past > want);
     if (behind != 0) {
       const int at = __builtin_ctzll(behind);
@@ -129,6 +130,16 @@ struct Tiles {
     for (int i = 0; i < LOADS; ++i) {
       const uint32_t c = s.chunk ^ (i * (ROW == 256 ? 16 : 32));
       to_lds(b, c < (uint32_t)dim * 2 ? s.row + c : kNowhere, (uint32_t)i * ROWS_LOAD * (uint32_t)token * 2, to + (wave * LOADS + i) * 1024);
+    }
+  }
+  // 32 rows by one wavefront alone; s: source of wavefront 0
+  static constexpr int LOADS32 = 32 / ROWS_LOAD;
+  static __device__ __forceinline__ void request32(const Source &s, const uint16_t *from, int rows, int64_t token, int dim, uint8_t *to) {
+    const i32x4 b = words_of(from, rows > 0 ? (uint32_t)((min(rows, 32) - 1) * (uint32_t)token * 2 + dim * 2) : 0u);
+#pragma unroll
+    for (int i = 0; i < LOADS32; ++i) {
+      const uint32_t c = s.chunk ^ (ROW == 256 ? (i & 3) * 16 : (i & 1) * 32);
+      to_lds(b, c < (uint32_t)dim * 2 ? s.row + c : kNowhere, (uint32_t)i * ROWS_LOAD * (uint32_t)token * 2, to + i * 1024);
     }
   }
   // Where the lane reads in a tile: of 32 rows at one chunk (step s over the dims: at ^ s * 32), transposed of 4 rows of four
@@ -335,59 +346,27 @@ __device__ __forceinline__ bool sees(const AttendRowsParams &p, int pos, int key
   return key <= pos && (p.window == 0 || pos - p.window < key || key < p.sinks);
 }
 
-// Tiles that all of a workgroup's queries see go in two steps per 32 keys, in which matrix instructions and others do not wait for
-// each other: the scores of the next 32 keys while the exponentials of these are taken, and the product with the values while the
-// largest of the next scores is found.  The other tiles (the diagonal, a window's edge, first keys) are computed one by one and masked.
-// Tiles are requested two ahead; there is one barrier for each, in its middle or at its end, and values have three places in LDS.
-// Y is divided by the sum of the exponentials as they are rounded, so that the rounding of one that outweighs the others cancels (the
-// error of Y 0.0022 of its size otherwise); KEEP: lse is of the sum in 32 bits, since the backward takes the exponentials anew.
+// What a wavefront has of its 32 queries.  Y is divided by the sum of the exponentials as they are rounded, so that the rounding of
+// one that outweighs the others cancels (the error of Y 0.0022 of its size otherwise); KEEP: lse is of the sum in 32 bits, since the
+// backward takes the exponentials anew.
 template <int KS, bool KEEP>
-__global__ __launch_bounds__(kBlock, 2) void attend_rows_kernel(const AttendRowsParams p, const int parts) {
+struct Queries {
   using T = Tiles<KS>;
-  __shared__ __align__(256) uint8_t lds[5 * T::BYTES];
-  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
-  const Item item = item_of(p.heads, p.kv_heads);
-  if (item.part >= parts) return;
-  const Part part = part_of(p, item.part);
-  if (part.sequence < 0) {
-    clear_rows(p.offsets, p.n_seqs, p.n_rows, p.y, item.head, p.heads, p.dim, part.over, parts - (item.part - part.over));
-    return;
-  }
-  const Sequence s = part.s;
-  const int r0 = part.part * kOwn, r1 = min(r0 + kOwn, s.nq) - 1, mine = r0 + wave * 32, row = mine + (lane & 31);
-  const int p0 = mine + s.ahead, p1 = min(mine + 31, r1) + s.ahead, pos = row + s.ahead;
-  const int kv = item.head / (p.heads / p.kv_heads);
-  const KeyTiles tiles = key_tiles(p, s, r0, r1);
-  const uint16_t *k = static_cast<const uint16_t *>(p.k.at) + s.k0 * p.k.token + kv * p.k.head;
-  const uint16_t *v = static_cast<const uint16_t *>(p.v.at) + s.k0 * p.v.token + kv * p.v.head;
-  const typename T::Source ks = T::source(wave, lane, p.k.token), vs = T::source(wave, lane, p.v.token);
-  const uint32_t lds0 = lds_at(lds);
-  uint32_t v_put = 2 * T::BYTES, v_at = lds0 + 2 * T::BYTES;
-  const auto request = [&](int t) MOE_ROWS_INLINE {
-    const int key = tiles.at(t), rows = s.nk - key;
-    T::request(ks, k + key * p.k.token, rows, p.k.token, p.dim, wave, lds + (t & 1) * T::BYTES);
-    T::request(vs, v + key * p.v.token, rows, p.v.token, p.dim, wave, lds + v_put);
-    v_put = v_put == 4 * T::BYTES ? 2 * T::BYTES : v_put + T::BYTES;
-  };
   i32x4 q[T::KS];
   f32x16 o[T::DS];
-  float top = -INFINITY, most = -INFINITY, sum = 0.f, rounded = 0.f;
-  T::own(static_cast<const uint16_t *>(p.q.at) + (s.q0 + min(row, s.nq - 1)) * p.q.token + item.head * p.q.head, row < s.nq, p.dim, lane, q);
+  float top, most, sum, rounded, scale;  // most: the largest score that is new, of the lane's own keys; the others to the base 2
+
+  __device__ __forceinline__ void begin(float s) {
 #pragma unroll
-  for (int d = 0; d < T::DS; ++d) o[d] = zero16();
-  const float scale = p.scale * kLog2e;
-  const typename T::Reader reader(lane);
-  const auto next_tile = [&](int t) MOE_ROWS_INLINE {
-    if (t + 1 < tiles.n) {
-      landed_but<0>();
-      if (t + 2 < tiles.n) request(t + 2);
-    }
-  };
-  const auto next_values = [&] { v_at = v_at == lds0 + 4 * T::BYTES ? lds0 + 2 * T::BYTES : v_at + T::BYTES; };
-  // The base of the exponentials follows the largest score (of the query's two lanes; most: of the lane's own) when that is `slack`
-  // ahead (to the base 2): until then nothing is multiplied and no lane asks the other one.  No slack: the largest exponential is 1,
-  // which has no rounding, and that counts for queries that see few keys.
-  const auto rebase = [&](float slack) MOE_ROWS_INLINE {
+    for (int d = 0; d < T::DS; ++d) o[d] = zero16();
+    top = most = -INFINITY;
+    sum = rounded = 0.f;
+    scale = s;
+  }
+  // The base of the exponentials follows the largest score (of the query's two lanes) when that is `slack` ahead (to the base 2): until
+  // then nothing is multiplied and no lane asks the other one.  No slack: the largest exponential is 1, which has no rounding, and
+  // that counts for queries that see few keys.
+  __device__ __forceinline__ void rebase(float slack) {
     if (__any(most * scale > top + slack)) {
       const float to = fmaxf(top, fmaxf(most, __shfl_xor(most, 32)) * scale), shrink = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(top - to);
       top = to;
@@ -396,12 +375,9 @@ __global__ __launch_bounds__(kBlock, 2) void attend_rows_kernel(const AttendRows
 #pragma unroll
       for (int d = 0; d < T::DS; ++d) o[d] *= shrink;
     }
-  };
-
-  // 32 keys of a tile by themselves
-  const auto alone = [&](int key, uint32_t k_at, uint32_t values_at) MOE_ROWS_INLINE {
-    if (mine > r1 || see_none(p, p0, p1, key, key + 31)) return;
-    const typename T::Reader keys(k_at, reader, false), values(values_at, reader, false);
+  }
+  // 32 keys from `key` on by themselves; the queries are at positions p0 .. p1, the lane's at pos
+  __device__ __forceinline__ void add(const AttendRowsParams &p, const typename T::Reader &keys, const typename T::Reader &values, int p0, int p1, int pos, int key, int lane) {
     f32x16 z = zero16();
 #pragma unroll
     for (int i = 0; i < T::KS; ++i) z = mma(T::rows(keys, 0, 0, i), q[i], z);
@@ -432,17 +408,9 @@ __global__ __launch_bounds__(kBlock, 2) void attend_rows_kernel(const AttendRows
     }
 #pragma unroll
     for (int i = 0; i < 2 * T::DS; ++i) o[i % T::DS] = mma(T::columns(values, 0, i / T::DS * 16, i % T::DS), f[i / T::DS], o[i % T::DS]);
-  };
-  const auto tile_alone = [&](int t) MOE_ROWS_INLINE {
-#pragma unroll 1
-    for (int m = 0; m < 2; ++m) alone(tiles.at(t) + 32 * m, lds0 + (t & 1) * T::BYTES + 32 * m * T::ROW, v_at + 32 * m * T::ROW);
-    next_tile(t);
-    next_values();
-  };
-
-  // z: the scores of 32 keys, `most` the largest; their values are at `values_at`.  next: those of the 32 keys at `k_at`.
-  const auto step = [&](f32x16 &z, f32x16 &next, uint32_t k_at, uint32_t values_at) MOE_ROWS_INLINE {
-    const typename T::Reader keys(k_at, reader, false), values(values_at, reader, false);
+  }
+  // z: the scores of 32 keys that all see, `most` the largest.  next: those of the 32 keys at `keys`.
+  __device__ __forceinline__ void step(f32x16 &z, f32x16 &next, const typename T::Reader &keys, const typename T::Reader &values) {
     rebase(8.f);
     constexpr int EACH = (16 + T::KS - 1) / T::KS, PVS = 2 * T::DS, AHEAD = 3;
     i32x4 a[AHEAD + 1], c[AHEAD + 1];
@@ -476,6 +444,62 @@ __global__ __launch_bounds__(kBlock, 2) void attend_rows_kernel(const AttendRows
       }
     }
     __builtin_amdgcn_sched_barrier(0);
+  }
+};
+
+// Tiles that all of a workgroup's queries see go in two steps per 32 keys, in which matrix instructions and others do not wait for
+// each other: the scores of the next 32 keys while the exponentials of these are taken, and the product with the values while the
+// largest of the next scores is found.  The other tiles (the diagonal, a window's edge, first keys) are computed one by one and masked.
+// Tiles are requested two ahead; there is one barrier for each, in its middle or at its end, and values have three places in LDS.
+template <int KS, bool KEEP>
+__global__ __launch_bounds__(kBlock, 2) void attend_rows_kernel(const AttendRowsParams p, const int parts) {
+  using T = Tiles<KS>;
+  __shared__ __align__(256) uint8_t lds[5 * T::BYTES];
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+  const Item item = item_of(p.heads, p.kv_heads);
+  if (item.part >= parts) return;
+  const Part part = part_of(p, item.part);
+  if (part.sequence < 0) {
+    clear_rows(p.offsets, p.n_seqs, p.n_rows, p.y, item.head, p.heads, p.dim, part.over, parts - (item.part - part.over));
+    return;
+  }
+  const Sequence s = part.s;
+  const int r0 = part.part * kOwn, r1 = min(r0 + kOwn, s.nq) - 1, mine = r0 + wave * 32, row = mine + (lane & 31);
+  const int p0 = mine + s.ahead, p1 = min(mine + 31, r1) + s.ahead, pos = row + s.ahead;
+  const int kv = item.head / (p.heads / p.kv_heads);
+  const KeyTiles tiles = key_tiles(p, s, r0, r1);
+  const uint16_t *k = static_cast<const uint16_t *>(p.k.at) + s.k0 * p.k.token + kv * p.k.head;
+  const uint16_t *v = static_cast<const uint16_t *>(p.v.at) + s.k0 * p.v.token + kv * p.v.head;
+  const typename T::Source ks = T::source(wave, lane, p.k.token), vs = T::source(wave, lane, p.v.token);
+  const uint32_t lds0 = lds_at(lds);
+  uint32_t v_put = 2 * T::BYTES, v_at = lds0 + 2 * T::BYTES;
+  const auto request = [&](int t) MOE_ROWS_INLINE {
+    const int key = tiles.at(t), rows = s.nk - key;
+    T::request(ks, k + key * p.k.token, rows, p.k.token, p.dim, wave, lds + (t & 1) * T::BYTES);
+    T::request(vs, v + key * p.v.token, rows, p.v.token, p.dim, wave, lds + v_put);
+    v_put = v_put == 4 * T::BYTES ? 2 * T::BYTES : v_put + T::BYTES;
+  };
+  Queries<KS, KEEP> w;
+  T::own(static_cast<const uint16_t *>(p.q.at) + (s.q0 + min(row, s.nq - 1)) * p.q.token + item.head * p.q.head, row < s.nq, p.dim, lane, w.q);
+  w.begin(p.scale * kLog2e);
+  const typename T::Reader reader(lane);
+  const auto at = [&](uint32_t tile) MOE_ROWS_INLINE { return typename T::Reader(tile, reader, false); };
+  const auto next_tile = [&](int t) MOE_ROWS_INLINE {
+    if (t + 1 < tiles.n) {
+      landed_but<0>();
+      if (t + 2 < tiles.n) request(t + 2);
+    }
+  };
+  const auto next_values = [&] { v_at = v_at == lds0 + 4 * T::BYTES ? lds0 + 2 * T::BYTES : v_at + T::BYTES; };
+  const auto tile_alone = [&](int t) MOE_ROWS_INLINE {
+#pragma unroll 1
+    for (int m = 0; m < 2; ++m) {
+      const int key = tiles.at(t) + 32 * m;
+      if (mine > r1 || see_none(p, p0, p1, key, key + 31)) continue;
+      w.add(p, at(lds0 + (t & 1) * T::BYTES + 32 * m * T::ROW), at(v_at + 32 * m * T::ROW), p0, p1, pos, key, lane);
+    }
+    next_tile(t);
+    next_values();
   };
 
   if (tiles.n > 0) {
@@ -497,24 +521,126 @@ __global__ __launch_bounds__(kBlock, 2) void attend_rows_kernel(const AttendRows
       for (const int end = round == 0 && from < fast ? from : tiles.n; t < end; ++t) tile_alone(t);
       if (t >= fast) continue;
       f32x16 za = zero16(), zb;
-      const typename T::Reader keys(lds0 + (t & 1) * T::BYTES, reader, false);
+      const typename T::Reader keys = at(lds0 + (t & 1) * T::BYTES);
 #pragma unroll
-      for (int i = 0; i < T::KS; ++i) za = mma(T::rows(keys, 0, 0, i), q[i], za);
-      most = largest(za);
+      for (int i = 0; i < T::KS; ++i) za = mma(T::rows(keys, 0, 0, i), w.q[i], za);
+      w.most = largest(za);
       for (; t < fast; ++t) {
-        step(za, zb, lds0 + (t & 1) * T::BYTES + 32 * T::ROW, v_at);
+        w.step(za, zb, at(lds0 + (t & 1) * T::BYTES + 32 * T::ROW), at(v_at));
         next_tile(t);
-        step(zb, za, lds0 + (~t & 1) * T::BYTES, v_at + 32 * T::ROW);
+        w.step(zb, za, at(lds0 + (~t & 1) * T::BYTES), at(v_at + 32 * T::ROW));
         next_values();
       }
     }
   }
   const bool there = row < s.nq;
-  const float total = rounded + __shfl_xor(rounded, 32);
+  const float total = w.rounded + __shfl_xor(w.rounded, 32);
   const int64_t dense = ((int64_t)(s.q0 + row) * p.heads + item.head) * p.dim;
-  T::store(p.y + dense, p.low ? p.low + dense : nullptr, there, p.dim, lane, o, total > 0.f || total != total ? 1.f / total : 0.f);
-  if (KEEP) sum += __shfl_xor(sum, 32);
-  if (KEEP && there && lane < 32) p.lse[(int64_t)item.head * p.n_rows + s.q0 + row] = top * kLn2 + __logf(sum);
+  T::store(p.y + dense, p.low ? p.low + dense : nullptr, there, p.dim, lane, w.o, total > 0.f || total != total ? 1.f / total : 0.f);
+  if (KEEP) w.sum += __shfl_xor(w.sum, 32);
+  if (KEEP && there && lane < 32) p.lse[(int64_t)item.head * p.n_rows + s.q0 + row] = w.top * kLn2 + __logf(w.sum);
+}
+
+// Few queries: a workgroup has 32, and each of its wavefronts a quarter of the keys, 32 at a time in turn, in a ring of its own; what
+// they have is joined through LDS.
+template <int KS, bool KEEP>
+__global__ __launch_bounds__(kBlock, 1) void attend_few_rows_kernel(const AttendRowsParams p, const int parts) {
+  using T = Tiles<KS>;
+  constexpr int HALF = 32 * T::ROW, PITCH = T::ROW / 2 + 4;  // bytes of 32 rows; floats of a query's sums
+  static_assert(kWaves * 32 * (PITCH + 4) * 4 <= kWaves * 4 * HALF, "the sums go where the rings were");
+  __shared__ __align__(256) uint8_t lds[kWaves * 4 * HALF];
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+  const Item item = item_of(p.heads, p.kv_heads);
+  if (item.part >= parts) return;
+  const Part part = part_of<32>(p, item.part);
+  if (part.sequence < 0) {
+    clear_rows(p.offsets, p.n_seqs, p.n_rows, p.y, item.head, p.heads, p.dim, part.over, parts - (item.part - part.over));
+    return;
+  }
+  const Sequence s = part.s;
+  const int r0 = part.part * 32, r1 = min(r0 + 32, s.nq) - 1, row = r0 + (lane & 31), p0 = r0 + s.ahead, p1 = r1 + s.ahead, pos = row + s.ahead;
+  const int kv = item.head / (p.heads / p.kv_heads);
+  const KeyTiles tiles = key_tiles(p, s, r0, r1);
+  const uint16_t *k = static_cast<const uint16_t *>(p.k.at) + s.k0 * p.k.token + kv * p.k.head;
+  const uint16_t *v = static_cast<const uint16_t *>(p.v.at) + s.k0 * p.v.token + kv * p.v.head;
+  const typename T::Source ks = T::source(0, lane, p.k.token), vs = T::source(0, lane, p.v.token);
+  uint8_t *mine = lds + wave * 4 * HALF;
+  const auto key_of = [&](int u) { return tiles.at(u >> 1) + (u & 1) * 32; };
+  const auto request = [&](int u, int place) MOE_ROWS_INLINE {  // (behind the last one: nothing, which arrives as zeros)
+    const int key = u < 2 * tiles.n ? key_of(u) : 0, rows = u < 2 * tiles.n ? s.nk - key : 0;
+    T::request32(ks, k + key * p.k.token, rows, p.k.token, p.dim, mine + place * 2 * HALF);
+    T::request32(vs, v + key * p.v.token, rows, p.v.token, p.dim, mine + place * 2 * HALF + HALF);
+  };
+  Queries<KS, KEEP> w;
+  T::own(static_cast<const uint16_t *>(p.q.at) + (s.q0 + min(row, s.nq - 1)) * p.q.token + item.head * p.q.head, row < s.nq, p.dim, lane, w.q);
+  w.begin(p.scale * kLog2e);
+  const typename T::Reader reader(lane);
+  request(wave, 0);
+  request(wave + kWaves, 1);
+  int place = 0;
+  for (int u = wave; u < 2 * tiles.n; u += kWaves, place ^= 1) {
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * T::LOADS32) : "memory");
+    const int key = key_of(u);
+    if (!see_none(p, p0, p1, key, key + 31)) {
+      const uint32_t at = lds_at(mine) + place * 2 * HALF;
+      w.add(p, typename T::Reader(at, reader, false), typename T::Reader(at + HALF, reader, false), p0, p1, pos, key, lane);
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    request(u + 2 * kWaves, place);
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  w.rounded += __shfl_xor(w.rounded, 32);
+  if (KEEP) w.sum += __shfl_xor(w.sum, 32);
+  float *sums = reinterpret_cast<float *>(lds), *stats = sums + kWaves * 32 * PITCH;  // [wave][query][dim], [wave][query][3]
+#pragma unroll
+  for (int d = 0; d < T::DS; ++d)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int c = d * 32 + i * 8 + (lane >> 5) * 4;
+      *reinterpret_cast<f32x4 *>(sums + (wave * 32 + (lane & 31)) * PITCH + c) = f32x4{w.o[d][4 * i], w.o[d][4 * i + 1], w.o[d][4 * i + 2], w.o[d][4 * i + 3]};
+    }
+  if (lane < 32) {
+    float *at = stats + (wave * 32 + lane) * 3;
+    at[0] = w.top;
+    at[1] = w.rounded;
+    at[2] = w.sum;
+  }
+  __syncthreads();
+  // eight threads a query
+  const int r = threadIdx.x >> 3, place8 = threadIdx.x & 7;
+  if (r0 + r >= s.nq) return;
+  float top = -INFINITY, total = 0.f, sum = 0.f, weight[kWaves];
+#pragma unroll
+  for (int i = 0; i < kWaves; ++i) top = fmaxf(top, stats[(i * 32 + r) * 3]);
+  const float base = top == -INFINITY ? 0.f : top;
+#pragma unroll
+  for (int i = 0; i < kWaves; ++i) {
+    weight[i] = __builtin_amdgcn_exp2f(stats[(i * 32 + r) * 3] - base);
+    total += weight[i] * stats[(i * 32 + r) * 3 + 1];
+    sum += weight[i] * stats[(i * 32 + r) * 3 + 2];
+  }
+  const float inv = total > 0.f || total != total ? 1.f / total : 0.f;
+  const int64_t dense = ((int64_t)(s.q0 + r0 + r) * p.heads + item.head) * p.dim;
+  for (int c = place8 * 8; c < p.dim; c += 64) {
+    rows_u32x4 hi, lo;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < kWaves; ++i) x += weight[i] * *reinterpret_cast<const f32x4 *>(sums + (i * 32 + r) * PITCH + c + 4 * h);
+      x *= inv;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint32_t two = pack_bf16(x[2 * i], x[2 * i + 1]);
+        hi[2 * h + i] = two;
+        lo[2 * h + i] = pack_bf16(x[2 * i] - bf16_lo(two), x[2 * i + 1] - bf16_hi(two));
+      }
+    }
+    *reinterpret_cast<rows_u32x4 *>(p.y + dense + c) = hi;
+    if (p.low) *reinterpret_cast<rows_u32x4 *>(p.low + dense + c) = lo;
+  }
+  if (KEEP && place8 == 0) p.lse[(int64_t)item.head * p.n_rows + s.q0 + r0 + r] = top * kLn2 + __logf(sum);
 }
 
 // ---- the gradients of k and v: how their work is cut ------------------------------------------------------------
@@ -905,8 +1031,8 @@ __global__ __launch_bounds__(kBlock) void join_pieces_kernel(const AttendRowsPar
   }
 }
 
-// parts of kOwn rows that the sequences have at most, and one at least that is none's: it clears the rows of no sequence
-int parts_of(int n_rows, int n_seqs) { return n_rows / kOwn + n_seqs + 1; }
+// parts of `own` rows that the sequences have at most, and one at least that is none's: it clears the rows of no sequence
+int parts_of(int n_rows, int n_seqs, int own = kOwn) { return n_rows / own + n_seqs + 1; }
 
 // f(steps over the dims): as many as there are, or the next more that there is a kernel for
 template <typename F>
@@ -919,10 +1045,17 @@ void with_steps(int dim, F f) {
 
 }  // namespace
 
+constexpr int kFew = 128;  // workgroups of kOwn queries up to which a wavefront takes a quarter of the keys instead
 hipError_t launch_attend_rows(const AttendRowsParams &p, hipStream_t s) {
   const int parts = parts_of(p.n_rows, p.n_seqs);
   with_steps(p.dim, [&](auto ks) {
     constexpr int KS = decltype(ks)::value;
+    if ((int64_t)parts * p.heads <= kFew) {
+      const int few = parts_of(p.n_rows, p.n_seqs, 32);
+      if (p.lse) attend_few_rows_kernel<KS, true><<<grid_of(few, p.heads), kBlock, 0, s>>>(p, few);
+      else attend_few_rows_kernel<KS, false><<<grid_of(few, p.heads), kBlock, 0, s>>>(p, few);
+      return;
+    }
     if (p.lse) attend_rows_kernel<KS, true><<<grid_of(parts, p.heads), kBlock, 0, s>>>(p, parts);
     else attend_rows_kernel<KS, false><<<grid_of(parts, p.heads), kBlock, 0, s>>>(p, parts);
   });

@@ -144,7 +144,15 @@ def rows_case(case, extra=0):
     return q, both[:, 0], both[:, 1], dy, keys
 
 
-@pytest.mark.parametrize("case", ROWS, ids=str)
+def many_heads(case):
+    """The case with as many heads, in groups of the same size, as it takes for more than 128 workgroups of 128 queries: up to there
+    the forward divides the keys among the wavefronts of a workgroup instead."""
+    each, keys, heads, kv, dim, window, sinks = case
+    times = up(129, (sum(each) // 128 + len(each) + 1) * heads)
+    return each, keys, heads * times, kv * times, dim, window, sinks
+
+
+@pytest.mark.parametrize("case", [f(c) for f in (lambda c: c, many_heads) for c in ROWS], ids=lambda c: str(c)[:90])
 def test_rows(lib, case):
     each, given, heads, kv, dim, window, sinks = case
     q, k, v, dy, keys = rows_case(case)
@@ -166,10 +174,11 @@ def test_rows(lib, case):
 
 @pytest.mark.parametrize("window,sinks,dim", [(0, 0, 128), (0, 0, 64), (60, 0, 80), (60, 40, 128)])
 @pytest.mark.parametrize("what", [math.nan, math.inf, -math.inf])
-def test_rows_that_are_not_seen_may_hold_anything(lib, window, sinks, dim, what):
+@pytest.mark.parametrize("times", [1, 6])
+def test_rows_that_are_not_seen_may_hold_anything(lib, window, sinks, dim, what, times):
     """Behind the last sequence, in another sequence, ahead of a window, and of the same sequence but later on."""
     g = gen(dim + window)
-    each, H, KV = [300, 90], 4, 2
+    each, H, KV = [300, 90], 4 * times, 2 * times
     q = normal(g, 400, H, dim, std=2.0, dtype=BF16)
     k, v = normal(g, 400, KV, dim, dtype=BF16), normal(g, 400, KV, dim, dtype=BF16)
     want = reference(q[:390], k[:390], v[:390], each, each, window, sinks, dim ** -0.5)["y"]
@@ -183,7 +192,7 @@ def test_rows_that_are_not_seen_may_hold_anything(lib, window, sinks, dim, what)
     clean = torch.ones(390, H, dim, dtype=torch.bool, device=DEV)
     ok = visible(300, 300, window, sinks)
     clean[:300][ok[:, at], 0:2, 5] = False
-    clean[:300, 2:][ok[:, at + 1] | ok[:, at + 37]] = False
+    clean[:300, 2:4][ok[:, at + 1] | ok[:, at + 37]] = False
     over = (y[:390].double() - want[0]).abs() - want[1] * (1 + 2 * U)
     assert float(torch.where(clean, over, -1.0).max()) <= 0  # (a comparison with NaN would be false)
     got = y[:300].float()
@@ -191,9 +200,9 @@ def test_rows_that_are_not_seen_may_hold_anything(lib, window, sinks, dim, what)
     one = got[ok[:, at]][:, 0:2, 5]
     assert bool((one.isnan() if what != what else one == what).all())
     # (rows that see the NaN key are NaN, the others have the values' infinities)
-    two = got[ok[:, at + 1] & ~ok[:, at + 37]][:, 2:]
+    two = got[ok[:, at + 1] & ~ok[:, at + 37]][:, 2:4]
     assert bool((two.isnan() if what != what else two == what).all())
-    assert bool(got[ok[:, at + 37]][:, 2:].isnan().all())
+    assert bool(got[ok[:, at + 37]][:, 2:4].isnan().all())
 
 
 def test_gradients_of_other_sequences(lib):
