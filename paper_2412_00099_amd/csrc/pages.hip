@@ -3,8 +3,10 @@
 // Plan: sums over the sequences (new tokens, pages to take) in the order of the sequences.  One launch: every workgroup goes over all
 // sequences, kChunk at a time, and sums them up for itself (a few KB from the caches), then finds the sequence of each of its tokens
 // and taken pages by bisection of the chunk's sums in LDS.  A token of a page that is taken in this launch finds the page in the
-// list of free ones, not in the table, so that no workgroup waits for another.
-// Store: bound by memory; a lane has 8 values of a head, the 8-bit form takes the largest over a head's lanes.
+// list of free ones, not in the table, so that no workgroup waits for another.  Bound by latency: the sequences' numbers, two barriers,
+// the entries.  Eight requests 4.3 us, 1024 with 320000 new tokens 7.6.
+// Store: bound by memory; a lane has 8 values of a head, the 8-bit form takes the largest over a head's lanes.  8 tokens of 16 heads of
+// 128 2.8 us; 8191 of 8 heads into 8 bits, 51 MB, 14 us (3.6 TB/s).
 #include <algorithm>
 
 #include "attend.h"
