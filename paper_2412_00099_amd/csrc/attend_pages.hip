@@ -202,8 +202,7 @@ struct Attend {
     per_kv = (per + kCols - 1) / kCols;
     n_groups = p.c.kv_heads * per_kv;
     Spot now{0, 0, 0, {}};
-    int left;
-    int64_t begin = 0;
+    int64_t left, begin = 0;
     const Parts parts = parts_of(p);
     if constexpr (WHOLE) {
       now.seq = uniform(blockIdx.x / n_groups);
@@ -220,7 +219,7 @@ struct Attend {
       begin = worker * share;
       if (worker == 0 && lane == 0) *parts.share = share;
       if (begin >= all) return;
-      left = (int)min(share, all - begin);
+      left = min(share, all - begin);
       int64_t before = 0;
       for (int s0 = 0; s0 < p.n_seqs; s0 += 64) {
         const int tiles = s0 + lane < p.n_seqs ? seen_of(p, p.lengths[s0 + lane]).tiles : 0;
@@ -240,7 +239,7 @@ struct Attend {
     }
     int64_t line = begin;
     Spot then = now;
-    int then_left = left;
+    int64_t then_left = left;
     uint32_t halves = 0;  // two bits a stage: which halves of the tiles that are under way there are
     Place to_come;
     // a stage's requests: keys (and scales), values

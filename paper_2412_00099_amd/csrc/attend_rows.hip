@@ -64,7 +64,7 @@ __device__ __forceinline__ Sequence sequence_of(const AttendRowsParams &p, int s
   return r;
 }
 // Part `want` of the sequences' rows in parts of OWN, later parts of the sequences first: they have more keys, and a workgroup with
-// much to do must not be the last to begin.  No such part: sequence -1, and by how much it was missed.
+// much to do must not be the last to begin.  No such part: sequence -1, and how far behind the last one it is (-1: it is not).
 struct Part {
   int sequence, part, over;
   Sequence s;
@@ -85,18 +85,25 @@ __device__ __forceinline__ Part part_of(const AttendRowsParams &p, int want) {
     const int l = uniform(__builtin_ctzll(__ballot(upto > want - ahead)));
     return {l, uniform(at), 0, {of_lane(mine.q0, l), of_lane(mine.nq, l), of_lane(mine.k0, l), of_lane(mine.nk, l), of_lane(mine.ahead, l)}};
   }
-  // (more sequences: one after the other, since 64 at a time are looked at once)
-  int64_t before = 0;
-  for (int s0 = 0; s0 < p.n_seqs; s0 += 64) {
-    const int64_t past = before + sum_upto((int64_t)(s0 + lane < p.n_seqs ? (sequence_of(p, s0 + lane).nq + OWN - 1) / OWN : 0));
-    const uint64_t behind = __ballot(past > want);
-    if (behind != 0) {
-      const int at = __builtin_ctzll(behind);
-      return {uniform(s0 + at), uniform((int)(of_lane(past, at) - want) - 1), 0, sequence_of(p, uniform(s0 + at))};
-    }
-    before = of_lane(past, 63);
+  // More sequences: nobody adds up what is ahead of each.  Sequence s has the numbers from offsets[s] / OWN + s on, of which it needs no
+  // more than there are up to the next sequence's first; the others stay idle.  The sequence is found 64 at a time.  (1000 sequences of
+  // 10000 rows in all, 16 heads of 128 over 8: 168 us, 244 with the sequences' parts added up 64
+  // at a time; with the gradients 581, 736.)
+  const auto first_of = [&](int s) { return min(max(p.offsets[s], 0), p.n_rows) / OWN + s; };
+  int from = 0, to = p.n_seqs;  // the last one whose numbers begin at `want` or ahead of it is among these
+  while (from < to) {
+    const int step = (to - from + 63) / 64, s = from + (lane + 1) * step;
+    const int n = __popcll(__ballot(s <= to && first_of(min(s, to)) <= want));
+    from += n * step;
+    to = min(from + step - 1, to);
   }
-  return {-1, 0, uniform((int)(want - before)), {}};
+  from = uniform(from);
+  const int over = uniform(want - first_of(from));
+  if (from == p.n_seqs) return {-1, 0, over, {}};
+  const Sequence s = sequence_of(p, from);
+  const int n = (s.nq + OWN - 1) / OWN;
+  if (over < 0 || over >= n) return {-1, 0, -1, {}};
+  return {from, n - 1 - over, 0, s};
 }
 // zeros for the rows of no sequence, shared by `step` workgroups
 __device__ __forceinline__ void clear_rows(const int32_t *offsets, int n_seqs, int n_rows, uint16_t *to, int head, int heads, int dim, int at, int step) {
@@ -466,7 +473,8 @@ __global__ __launch_bounds__(kBlock, 2) void attend_rows_kernel(const AttendRows
   if (item.part >= parts) return;
   const Part part = part_of(p, item.part);
   if (part.sequence < 0) {
-    clear_rows(p.offsets, p.n_seqs, p.n_rows, p.y, item.head, p.heads, p.dim, part.over, parts - (item.part - part.over));
+    if (part.over >= 0)
+      clear_rows(p.offsets, p.n_seqs, p.n_rows, p.y, item.head, p.heads, p.dim, part.over, parts - (item.part - part.over));
     return;
   }
   const Sequence s = part.s;
@@ -560,7 +568,8 @@ __global__ __launch_bounds__(kBlock, 1) void attend_few_rows_kernel(const Attend
   if (item.part >= parts) return;
   const Part part = part_of<32>(p, item.part);
   if (part.sequence < 0) {
-    clear_rows(p.offsets, p.n_seqs, p.n_rows, p.y, item.head, p.heads, p.dim, part.over, parts - (item.part - part.over));
+    if (part.over >= 0)
+      clear_rows(p.offsets, p.n_seqs, p.n_rows, p.y, item.head, p.heads, p.dim, part.over, parts - (item.part - part.over));
     return;
   }
   const Sequence s = part.s;
@@ -795,7 +804,8 @@ __global__ __launch_bounds__(kBlock, 2) void attend_rows_dq_kernel(const AttendR
   if (item.part >= parts) return;
   const Part part = part_of(p, item.part);
   if (part.sequence < 0) {
-    clear_rows(p.offsets, p.n_seqs, p.n_rows, p.dq, item.head, p.heads, p.dim, part.over, parts - (item.part - part.over));
+    if (part.over >= 0)
+      clear_rows(p.offsets, p.n_seqs, p.n_rows, p.dq, item.head, p.heads, p.dim, part.over, parts - (item.part - part.over));
     return;
   }
   const Sequence s = part.s;
