@@ -161,12 +161,12 @@ struct Attend {
       to_lds(words_of(base + at.from[half] * EL, at.bytes[half]), off, 0, to + i * 1024);
     }
     if constexpr (INT8 && !VALUES) {
-      // lanes 0 .. 31: scales of the keys, the others: of the values.  (Where there are none: any; they are not used.)
+      // lanes 0 .. 31: scales of the keys, the others: of the values.  (Where there are none: any word; it is not used.)
       const int r = lane & 31, pos = at.pos + r;
-      int64_t from = 0;
+      const float *from = reinterpret_cast<const float *>(p.lengths);
       if ((r < 16 ? at.bytes[0] : at.bytes[1]) != 0 && pos < a.s.end)
-        from = (((int64_t)(r < 16 ? at.id[0] : at.id[1]) * p.c.kv_heads + at.kv) << p.c.page_bits) + (pos & ((1 << p.c.page_bits) - 1));
-      scale_to_lds((lane < 32 ? p.c.k_scale : p.c.v_scale) + from, lds + RING * STAGE + stage * SCALES);
+        from = (lane < 32 ? p.c.k_scale : p.c.v_scale) + (((int64_t)(r < 16 ? at.id[0] : at.id[1]) * p.c.kv_heads + at.kv) << p.c.page_bits) + (pos & ((1 << p.c.page_bits) - 1));
+      scale_to_lds(from, lds + RING * STAGE + stage * SCALES);
     }
   }
   static __device__ __forceinline__ void scale_to_lds(const float *from, uint8_t *to) {

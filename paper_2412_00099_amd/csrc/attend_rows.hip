@@ -705,11 +705,13 @@ __device__ __forceinline__ void plan_pieces(const AttendRowsParams &p, uint8_t *
   int64_t total = 0, share = 0, all;
   if (tid < kSizes) sizes[tid] = 0;
   for (int pass = 0; pass < 3; ++pass) {
-    int64_t slots = 0;
+    int64_t slots = 0, left = p.max_pieces;
     for (int s0 = 0; s0 < p.n_seqs; s0 += kBlock) {
       const int64_t n = s0 + tid < p.n_seqs ? (sequence_of(p, s0 + tid).nk + kOwn - 1) / kOwn : 0;
       int64_t parts;
       past[tid] = block_upto(n, waves, parts);
+      parts = min(parts, left);  // (all of them, unless sequences overlap)
+      left -= parts;
       __syncthreads();
       for (int64_t u0 = 0; u0 < parts; u0 += kBlock) {
         const int64_t u = u0 + tid;

@@ -1,6 +1,8 @@
 // Attention and the cache's pages for tensors: as the row operators are (rows_torch.cpp).
 #include "tensors.h"
 
+#include <c10/core/InferenceMode.h>
+
 #include <cmath>
 #include <tuple>
 
@@ -16,7 +18,7 @@ Heads heads_of(const Tensor &t, const char *name) {
   Heads r{size32(t.size(0)), size32(t.size(1)), size32(t.size(2)), 0, 0};
   // (what there is only one of has no stride)
   r.head = r.h > 1 ? t.stride(1) : r.d;
-  r.token = r.n > 1 ? t.stride(0) : std::max(r.h * r.head, (int64_t)r.d);
+  r.token = r.n > 1 ? t.stride(0) : r.d;
   return r;
 }
 void bf16(const Tensor &t, const char *name) {
@@ -50,6 +52,13 @@ Pages pages_of(const Tensor &k, const Tensor &v, const Maybe &k_scale, const May
   return r;
 }
 
+// (PyTorch refuses to count their changes, but only once they are made)
+void writable(const Tensor &t, const char *name) {
+  if (t.is_inference() && !c10::InferenceMode::is_enabled()) wrong(std::string(name) + " is of inference mode: it is written to in that mode only");
+}
+void writable(const Maybe &t, const char *name) {
+  if (t) writable(*t, name);
+}
 void written(const Tensor &t) { t.unsafeGetTensorImpl()->bump_version(); }
 void written(const Maybe &t) {
   if (t) written(*t);
@@ -64,6 +73,7 @@ std::tuple<Tensor, Tensor, Tensor, Tensor, Tensor> plan_pages(const Tensor &have
   dense(table, {n, width}, at::kInt, "table");
   dense(free, {n_free}, at::kInt, "free");
   dense(used, {1}, at::kInt, "used");
+  writable(table, "table");
   const int32_t t = size_or_all(n_tokens);
   const Place on(have);
   on.has(more, table, free, used);
@@ -86,6 +96,10 @@ void store_pages(const Tensor &k, const Tensor &v, const Tensor &slots, const Te
   if (v.scalar_type() != k.scalar_type() || v.sizes() != k.sizes()) wrong("v has to have the shape and type of k");
   if (c.h != hk.h || c.d != hk.d) wrong("k has other heads than k_pages");
   dense(slots, {hk.n}, at::kInt, "slots");
+  writable(k_pages, "k_pages");
+  writable(v_pages, "v_pages");
+  writable(k_scale, "k_scale");
+  writable(v_scale, "v_scale");
   const Place on(k);
   on.has(v, slots, k_pages, v_pages, k_scale, v_scale);
   check(moe_store_pages(k.const_data_ptr(), v.const_data_ptr(), fmt, hk.token, hk.head, hv.token, hv.head, ints(slots), hk.n, hk.h, hk.d,

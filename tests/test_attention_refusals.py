@@ -133,3 +133,15 @@ def test_tensors_on_the_cpu_and_of_other_shapes(B):
         with pytest.raises(ValueError):
             call()
             print(i)
+
+
+def test_caches_of_inference_mode_are_not_written_outside_it(B):
+    import paper_2412_00099_amd as moe
+
+    k, n = torch.zeros(5, 2, 64, dtype=torch.bfloat16), torch.zeros(5, dtype=torch.int32)
+    with torch.inference_mode():
+        pages, table = torch.zeros(3, 2, 16, 64, dtype=torch.bfloat16), torch.zeros(5, 2, dtype=torch.int32)
+    with pytest.raises(ValueError, match="inference"):
+        moe.store_pages(k, k, n, pages, pages)
+    with pytest.raises(ValueError, match="inference"):
+        moe.plan_pages(n, n, table, n, 16, 5)

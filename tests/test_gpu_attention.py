@@ -237,7 +237,7 @@ def test_offsets_that_do_not_fit(lib):
     y = lib.attend_rows(q, k, v, ints([20, 80, 1 << 30]))  # (the last sequence has the rows that there are)
     want = reference(q[20:], k[20:], v[20:], [60, 120], [60, 120], 0, 0, 0.125)
     close(y[20:], *want["y"], "y")
-    for bad in ([150, 20, -5], [-(1 << 31), (1 << 31) - 1, 0]):
+    for bad in ([150, 20, -5], [-(1 << 31), (1 << 31) - 1, 0], [0, 200] * 400, [(7919 * i) % 300 - 50 for i in range(500)]):
         y, kept = lib.attend_rows(q, k, v, ints(bad), keep=True)
         lib.attend_rows_backward(q, k, v, ints(bad), torch.zeros_like(y), lib.KeptAttention(torch.zeros_like(kept.lse), None), dy)
         torch.cuda.synchronize()
@@ -263,6 +263,40 @@ def test_layouts(lib, layout):
     want = reference(q, k, v, [100, T - 100], [100, T - 100], 50, 2, 0.2, dy)
     for n, got in zip(("y", "dq", "dk", "dv"), (y, *lib.attend_rows_backward(q, k, v, offsets, y, kept, dy, **kw))):
         close(got, *want[n], n)
+
+
+def test_one_row_between_heads_that_lie_far_apart(lib):
+    """Of one row there is no stride that could be too large."""
+    g = gen(12)
+    q, k, v = (normal(g, 4, 1 << 16, 64, dtype=BF16)[:, 70:71].transpose(0, 1) for _ in range(3))
+    for x in (q, k, v):
+        assert x.shape == (1, 4, 64) and x.stride(1) == 1 << 22
+    y, kept = lib.attend_rows(q, k, v, ints([0, 1]), keep=True)
+    dy = normal(g, 1, 4, 64, dtype=BF16)
+    dq, dk, dv = lib.attend_rows_backward(q, k, v, ints([0, 1]), y, kept, dy)
+    assert torch.equal(y, v) and torch.equal(dv, dy)
+    pages = torch.zeros(1, 4, 16, 64, dtype=BF16, device=DEV)
+    lib.store_pages(k, v, ints([3]), pages, pages.clone())
+    assert torch.equal(pages[0, :, 3], k[0])
+    assert torch.equal(lib.attend_pages(q, pages, pages, ints([[0]]), ints([4]), window=1)[0], k[0])
+
+
+def test_caches_of_inference_mode(lib):
+    """They are written to in that mode, and refused outside it ahead of the launch."""
+    g = gen(14)
+    k, slots = normal(g, 2, 1, 64, dtype=BF16), ints([1, 5])
+    with torch.inference_mode():
+        pages = [torch.zeros(1, 1, 16, 64, dtype=BF16, device=DEV) for _ in range(2)]
+        table = ints([[-1]])
+        lib.store_pages(k, k, slots, *pages)
+        lib.plan_pages(ints([0]), ints([1]), table, ints([7]), 16, 1)
+    assert torch.equal(pages[0][0, 0, 5], k[1, 0]) and table.item() == 7
+    before = [p.clone() for p in pages]
+    for call in (lambda: lib.store_pages(k + 1, k, slots, *pages), lambda: lib.plan_pages(ints([0]), ints([1]), table, ints([8]), 16, 1)):
+        with pytest.raises(ValueError, match="inference"):
+            call()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(before, pages)) and table.item() == 7
 
 
 def test_gradients_against_differences(lib):
