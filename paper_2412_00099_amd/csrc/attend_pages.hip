@@ -449,65 +449,118 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_pages_kernel(const Atte
   a.run(uniform(blockIdx.x * kWaves) + wave, lds + wave * A::WAVE_LDS);
 }
 
-// One workgroup for each (sequence, head): its parts, or zeros where nothing is seen
-constexpr int kJoinBlock = 256;
-__global__ __launch_bounds__(kJoinBlock) void join_pages_kernel(const AttendPagesParams p) {
+// The parts of each (sequence, head), or zeros where nothing is seen.  A workgroup has `each` heads of a (sequence, group): one where
+// few workgroups are to do; kJoinHeads where there are so many that their starts count, most of them for nothing, since the worker that
+// had all of a group wrote it.  Few parts are a wavefront's work, many the workgroup's, head by head.  (All in all, 412 sequences of up to 5
+// tokens, 48 heads: 21 us, with a workgroup for each head 35; 512 of up to 1000, 16 heads: 113, 120.  20 of up to 16000, 32 heads, have
+// long lists of parts: one head each 109, four 114.)
+constexpr int kJoinBlock = 256, kJoinWaves = kJoinBlock / 64, kJoinHeads = 4, kFewParts = 16;
+constexpr int kJoinMost = 1024;  // workgroups of one head each, at most
+__global__ __launch_bounds__(kJoinBlock, 4) void join_pages_kernel(const AttendPagesParams p, const int each) {
   constexpr int STRIPS = kJoinBlock / 32;
   __shared__ float weights[kWorkers], part[STRIPS][MOE_ATTEND_MAX_DIM];
-  __shared__ float tops[kJoinBlock / 64], totals[kJoinBlock / 64];
-  const int seq = blockIdx.x / p.heads, head = blockIdx.x % p.heads, tid = threadIdx.x;
+  __shared__ float tops[kJoinWaves], totals[kJoinWaves];
+  const Parts parts = parts_of(p);
+  const int tid = threadIdx.x, per = p.heads / p.c.kv_heads, per_kv = (per + kCols - 1) / kCols, n_groups = p.c.kv_heads * per_kv;
+  const int shares = (parts.rows + each - 1) / each, item = blockIdx.x / shares, seq = item / n_groups, group = item % n_groups;
+  const int in0 = group % per_kv * kCols + blockIdx.x % shares * each, in1 = min(min(in0 + each, per), (group % per_kv + 1) * kCols);
+  const int64_t share = *parts.share, start = parts.start[seq];
   const Seen s = seen_of(p, p.lengths[seq]);
-  uint16_t *y = p.y + ((int64_t)seq * p.heads + head) * p.c.dim;
+  uint16_t *y = p.y + ((int64_t)seq * p.heads + group / per_kv * per) * p.c.dim;
   if (s.tiles == 0) {
-    for (int d = tid; d < p.c.dim; d += kJoinBlock) y[d] = 0;
+    for (int d = in0 * p.c.dim + tid; d < in1 * p.c.dim; d += kJoinBlock) y[d] = 0;
     return;
   }
-  const Parts parts = parts_of(p);
-  const int per = p.heads / p.c.kv_heads, per_kv = (per + kCols - 1) / kCols, kv = head / per, in = head % per;
-  const int64_t share = *parts.share, from = parts.start[seq] + (int64_t)(kv * per_kv + in / kCols) * s.tiles;
+  const int64_t from = start + (int64_t)group * s.tiles;
   const int first = (int)(from / share), n = (int)((from + s.tiles - 1) / share) - first + 1;
   if (n == 1) return;  // (one worker had all of it)
-  const auto row_of = [&](int i) { return ((int64_t)(first + i) * 2 + (i == 0 ? 1 : 0)) * parts.rows + in % kCols; };
-  float top = -INFINITY, total = 0.f;
-  for (int i = tid; i < n; i += kJoinBlock) top = fmaxf(top, weights[i] = parts.stats[row_of(i) * 2]);
+  const auto row_of = [&](int i, int in) { return (uint32_t)((first + i) * 2 + (i == 0 ? 1 : 0)) * parts.rows + in % kCols; };
+  if (each > 1 && n <= kFewParts) {
+    const int in = in0 + (tid >> 6), lane = tid & 63, half = lane >> 5, d = lane % 32 * 4;
+    if (in >= in1) return;
+    f32x4 v[kFewParts / 2];
 #pragma unroll
-  for (int m = 1; m < 64; m <<= 1) top = fmaxf(top, __shfl_xor(top, m));
-  if ((tid & 63) == 0) tops[tid >> 6] = top;
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < kJoinBlock / 64; ++i) top = fmaxf(top, tops[i]);
-  const float base = top == -INFINITY ? 0.f : top;
-  for (int i = tid; i < n; i += kJoinBlock) {
-    weights[i] = __builtin_amdgcn_exp2f(weights[i] - base);
-    total += weights[i] * parts.stats[row_of(i) * 2 + 1];
-  }
-#pragma unroll
-  for (int m = 1; m < 64; m <<= 1) total += __shfl_xor(total, m);
-  if ((tid & 63) == 0) totals[tid >> 6] = total;
-  __syncthreads();
-  const int strip = tid / 32, d = tid % 32 * 4;
-  if (d < p.c.dim) {
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    int i = strip;
-    for (; i + 7 * STRIPS < n; i += 8 * STRIPS) {
-      f32x4 v[8];
-#pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] = *reinterpret_cast<const f32x4 *>(parts.sums + row_of(i + k * STRIPS) * p.c.dim + d);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) acc += weights[i + k * STRIPS] * v[k];
+    for (int k = 0; k < kFewParts / 2; ++k) {
+      const int i = 2 * k + half;
+      v[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (i < n && d < p.c.dim) v[k] = *reinterpret_cast<const f32x4 *>(parts.sums + row_of(i, in) * p.c.dim + d);
     }
-    for (; i < n; i += STRIPS) acc += weights[i] * *reinterpret_cast<const f32x4 *>(parts.sums + row_of(i) * p.c.dim + d);
-    *reinterpret_cast<f32x4 *>(&part[strip][d]) = acc;
+    float top = -INFINITY, total = 0.f;
+    if (lane < n) {
+      top = parts.stats[row_of(lane, in) * 2];
+      total = parts.stats[row_of(lane, in) * 2 + 1];
+    }
+    float most = top;
+#pragma unroll
+    for (int m = 1; m < kFewParts; m <<= 1) most = fmaxf(most, __shfl_xor(most, m));
+    most = __shfl(most, 0);
+    const float weight = __builtin_amdgcn_exp2f(top - (most == -INFINITY ? 0.f : most));
+    total *= weight;
+#pragma unroll
+    for (int m = 1; m < kFewParts; m <<= 1) total += __shfl_xor(total, m);
+    total = __shfl(total, 0);
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < kFewParts / 2; ++k) acc += __shfl(weight, 2 * k + half) * v[k];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      acc[i] += __shfl_xor(acc[i], 32);
+      acc[i] = total > 0.f || total != total ? acc[i] / total : 0.f;
+    }
+    if (half == 0 && d < p.c.dim) *reinterpret_cast<rows_u32x2 *>(y + in * p.c.dim + d) = rows_u32x2{pack_bf16(acc[0], acc[1]), pack_bf16(acc[2], acc[3])};
+    return;
   }
-  __syncthreads();
-  if (tid < p.c.dim) {
-    float v = 0.f;
-    total = 0.f;
+  for (int in = in0; in < in1; ++in) {
+    const int strip = tid / 32, d = tid % 32 * 4;
+    // (the first sums come while the weights are worked out)
+    f32x4 v[8];
+    const auto load = [&](int i0) MOE_ROWS_INLINE {
 #pragma unroll
-    for (int i = 0; i < STRIPS; ++i) v += part[i][tid];
+      for (int k = 0; k < 8; ++k) {
+        const int i = i0 + strip + k * STRIPS;
+        v[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (i < n && d < p.c.dim) v[k] = *reinterpret_cast<const f32x4 *>(parts.sums + row_of(i, in) * p.c.dim + d);
+      }
+    };
+    load(0);
+    float top = -INFINITY, total = 0.f;
+    for (int i = tid; i < n; i += kJoinBlock) top = fmaxf(top, weights[i] = parts.stats[row_of(i, in) * 2]);
 #pragma unroll
-    for (int i = 0; i < kJoinBlock / 64; ++i) total += totals[i];
-    y[tid] = (uint16_t)pack_bf16(total > 0.f || total != total ? v / total : 0.f, 0.f);
+    for (int m = 1; m < 64; m <<= 1) top = fmaxf(top, __shfl_xor(top, m));
+    if ((tid & 63) == 0) tops[tid >> 6] = top;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kJoinWaves; ++i) top = fmaxf(top, tops[i]);
+    const float base = top == -INFINITY ? 0.f : top;
+    for (int i = tid; i < n; i += kJoinBlock) {
+      weights[i] = __builtin_amdgcn_exp2f(weights[i] - base);
+      total += weights[i] * parts.stats[row_of(i, in) * 2 + 1];
+    }
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) total += __shfl_xor(total, m);
+    if ((tid & 63) == 0) totals[tid >> 6] = total;
+    __syncthreads();
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    for (int i0 = 0; i0 < n; i0 += 8 * STRIPS) {
+      if (i0 > 0) load(i0);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int i = i0 + strip + k * STRIPS;
+        if (i < n) acc += weights[i] * v[k];
+      }
+    }
+    if (d < p.c.dim) *reinterpret_cast<f32x4 *>(&part[strip][d]) = acc;
+    __syncthreads();
+    if (tid < p.c.dim) {
+      float sum = 0.f;
+      total = 0.f;
+#pragma unroll
+      for (int i = 0; i < STRIPS; ++i) sum += part[i][tid];
+#pragma unroll
+      for (int i = 0; i < kJoinWaves; ++i) total += totals[i];
+      y[in * p.c.dim + tid] = (uint16_t)pack_bf16(total > 0.f || total != total ? sum / total : 0.f, 0.f);
+    }
+    __syncthreads();
   }
 }
 
@@ -523,7 +576,8 @@ hipError_t attend_with(const AttendPagesParams &p, hipStream_t s) {
   attend_pages_kernel<CACHE, DT, false><<<kGroups, kWaves * 64, 0, s>>>(p);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  join_pages_kernel<<<p.n_seqs * p.heads, kJoinBlock, 0, s>>>(p);
+  const int rows = group_rows(p.heads, p.c.kv_heads), each = groups * rows <= kJoinMost ? 1 : kJoinHeads;
+  join_pages_kernel<<<groups * ((rows + each - 1) / each), kJoinBlock, 0, s>>>(p, each);
   return hipGetLastError();
 }
 

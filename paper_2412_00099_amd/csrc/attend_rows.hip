@@ -662,11 +662,13 @@ __global__ __launch_bounds__(kBlock, 1) void attend_few_rows_kernel(const Attend
 // The queries that see any of kOwn keys, tile by tile, and that for each head of the group, are a list.  Lists are long and few
 // where few heads of k serve many of q, or where first keys stay visible: a list of more than half as many tiles again as a
 // workgroup's equal share is cut into pieces of about a share, whose sums, in 32 bits, are added up in order by a launch of its own.
-// (A piece costs as much as some eight tiles: 128 rows of sums to memory and back.)  There are 512 shares of wide heads, as many as the
+// (A piece costs as much as some eight tiles, 128 rows of sums to memory and back, but where few lists leave compute units idle, a
+// list's tiles one after the other take longer: 1193 tokens, 4 heads of 112 for 1, with all else: shares of 16 tiles at least 115 us, 8 77, 4 61,
+// 2 63; 2005 tokens, 16 heads of 64: 54, 54, 50, 52.)  There are 512 shares of wide heads, as many as the
 // GPU holds workgroups at once, and more of narrow heads, whose sums are smaller (16384 tokens, 4 heads of 64 for 16, with all else: 512
 // shares 538, 768 499, 1024 481 us; 8192 tokens, 16 heads of 128: 401, 404, 441; 20001 tokens, 2 heads of 80 for 16, window: 669, 663, 659).
 inline int shares_of(int dim) { return std::min(std::max(65536 / dim, 512), 1024); }
-constexpr int kLeast = 16;     // tiles of a share at least
+constexpr int kLeast = 4;     // tiles of a share at least
 constexpr int kLead = 8;       // workgroups ahead of those with rows in the launch that plans: one plans, and each XCD has one
 struct List {
   int first, end, tiles;  // query rows of the sequence, from a tile's first row on; tiles of one head
