@@ -443,7 +443,8 @@ int moe_experts_rows_backward(int32_t weight_fmt, int32_t hidden, int32_t inter,
  *   k_offsets[i + 1] - 1 of k and v (k_offsets_dev NULL: the same); its queries are its last rows, so that query r of nq is at position
  *   nk - nq + r (one ahead of the first key sees nothing).  y_dev dense [n_rows, n_heads, head_dim].  For the backward, or NULL:
  *   y_low_dev (as y_dev): bf16 of what the rounding of y leaves; lse_dev fp32 [n_heads, n_rows].  Rows of no sequence: y is 0, the
- *   others are left alone.
+ *   others are left alone.  Few queries of many keys are split over the GPU: the workspace holds what the shares have,
+ *   moe_attend_rows_bytes bytes, 16-byte aligned, of this call alone until it is done (0: none is needed, it may be NULL).
  * moe_attend_rows_backward: from dy the gradients of q, k and v, dense, bf16 (rows of no sequence: 0).  y, y_low, lse: as the forward left
  *   them (y_low_dev NULL: y is taken as it is, which makes the error of dq and dk about a tenth larger).  P = exp(z - lse), dv = sum P dy, dz = P (<dy, v> - <dy, y>), dq = softmax_scale sum dz k, dk = softmax_scale sum dz q, sums
  *   over the heads of a group and over all queries in a fixed order.  P and dz are rounded to bf16 for the matrix cores.  Infinities and
@@ -462,10 +463,12 @@ int moe_attend_pages(const void *q_dev, int64_t q_stride, int64_t q_head_stride,
                      const float *v_scale_dev, const int32_t *table_dev, int32_t table_pages, const int32_t *lengths_dev, int32_t n_seqs,
                      int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, float softmax_scale, int32_t window, int32_t sinks, void *y_dev,
                      void *workspace_dev, size_t workspace_bytes, void *stream);
+size_t moe_attend_rows_bytes(int32_t n_rows, int32_t n_k_rows, int32_t n_seqs, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim);
 int moe_attend_rows(const void *q_dev, int64_t q_stride, int64_t q_head_stride, const void *k_dev, int64_t k_stride, int64_t k_head_stride,
                     const void *v_dev, int64_t v_stride, int64_t v_head_stride, const int32_t *offsets_dev, const int32_t *k_offsets_dev,
                     int32_t n_seqs, int32_t n_rows, int32_t n_k_rows, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
-                    float softmax_scale, int32_t window, int32_t sinks, void *y_dev, void *y_low_dev, float *lse_dev, void *stream);
+                    float softmax_scale, int32_t window, int32_t sinks, void *y_dev, void *y_low_dev, float *lse_dev, void *workspace_dev,
+                    size_t workspace_bytes, void *stream);
 size_t moe_attend_rows_backward_bytes(int32_t n_rows, int32_t n_k_rows, int32_t n_seqs, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim);
 int moe_attend_rows_backward(const void *q_dev, int64_t q_stride, int64_t q_head_stride, const void *k_dev, int64_t k_stride,
                              int64_t k_head_stride, const void *v_dev, int64_t v_stride, int64_t v_head_stride, const int32_t *offsets_dev,

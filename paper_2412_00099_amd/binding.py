@@ -188,7 +188,9 @@ lib.moe_attend_pages.argtypes = [_vp, _i64, _i64, _vp, _vp, _i32, _i64, _i32, _i
                                  _i32, _i32, _vp, _vp, C.c_size_t, _vp]
 _attend_rows = [_vp, _i64, _i64, _vp, _i64, _i64, _vp, _i64, _i64, _vp, _vp, _i32, _i32, _i32, _i32, _i32, _i32, C.c_float, _i32, _i32]
 lib.moe_attend_rows.restype = C.c_int
-lib.moe_attend_rows.argtypes = _attend_rows + [_vp, _vp, _vp, _vp]
+lib.moe_attend_rows.argtypes = _attend_rows + [_vp, _vp, _vp, _vp, C.c_size_t, _vp]
+lib.moe_attend_rows_bytes.restype = C.c_size_t
+lib.moe_attend_rows_bytes.argtypes = [_i32] * 6
 lib.moe_attend_rows_backward_bytes.restype = C.c_size_t
 lib.moe_attend_rows_backward_bytes.argtypes = [_i32] * 6
 lib.moe_attend_rows_backward.restype = C.c_int
@@ -203,7 +205,7 @@ EXPORTS = [
     "moe_cache_set_baseline", "moe_cache_reset", "moe_residual_rmsnorm", "moe_cache_profile", "moe_last_error",
     "moe_norm_rows", "moe_norm_rows_backward_bytes", "moe_norm_rows_backward", "moe_sort_tokens_bytes", "moe_sort_tokens",
     "moe_gather_rows", "moe_combine_rows", "moe_combine_rows_backward", "moe_experts_rows", "moe_experts_rows_backward",
-    "moe_plan_pages", "moe_store_pages", "moe_attend_pages_bytes", "moe_attend_pages", "moe_attend_rows",
+    "moe_plan_pages", "moe_store_pages", "moe_attend_pages_bytes", "moe_attend_pages", "moe_attend_rows_bytes", "moe_attend_rows",
     "moe_attend_rows_backward_bytes", "moe_attend_rows_backward",
 ]
 
@@ -460,12 +462,16 @@ def moe_attend_pages(q_dev, q_stride, q_head_stride, k_pages_dev, v_pages_dev, c
                                 softmax_scale, window, sinks, y_dev, workspace_dev, workspace_bytes, stream), "moe_attend_pages")
 
 
+def moe_attend_rows_bytes(n_rows: int, n_k_rows: int, n_seqs: int, n_heads: int, n_kv_heads: int, head_dim: int) -> int:
+    return int(lib.moe_attend_rows_bytes(n_rows, n_k_rows, n_seqs, n_heads, n_kv_heads, head_dim))
+
+
 def moe_attend_rows(q_dev, q_stride, q_head_stride, k_dev, k_stride, k_head_stride, v_dev, v_stride, v_head_stride, offsets_dev,
                     k_offsets_dev, n_seqs, n_rows, n_k_rows, n_heads, n_kv_heads, head_dim, softmax_scale, window, sinks, y_dev,
-                    y_low_dev, lse_dev, stream) -> None:
+                    y_low_dev, lse_dev, workspace_dev, workspace_bytes, stream) -> None:
     _check(lib.moe_attend_rows(q_dev, q_stride, q_head_stride, k_dev, k_stride, k_head_stride, v_dev, v_stride, v_head_stride,
                                offsets_dev, k_offsets_dev, n_seqs, n_rows, n_k_rows, n_heads, n_kv_heads, head_dim, softmax_scale,
-                               window, sinks, y_dev, y_low_dev, lse_dev, stream), "moe_attend_rows")
+                               window, sinks, y_dev, y_low_dev, lse_dev, workspace_dev, workspace_bytes, stream), "moe_attend_rows")
 
 
 def moe_attend_rows_backward_bytes(n_rows: int, n_k_rows: int, n_seqs: int, n_heads: int, n_kv_heads: int, head_dim: int) -> int:

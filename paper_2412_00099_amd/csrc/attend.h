@@ -56,6 +56,7 @@ struct AttendRowsParams {
   uint16_t *y;
   uint16_t *low;  // y's rounding, or NULL
   float *lse;     // [heads][n_rows], forward: may be NULL
+  int32_t splits; // of the keys, forward: 1, or stats [parts][splits][heads][128 queries][4] and sums [...][128][dim] are used
   // backward
   const uint16_t *dy;
   uint16_t *dq, *dk, *dv;
@@ -65,7 +66,8 @@ struct AttendRowsParams {
   float *sums;  // [max_slots][kv_heads][128 keys][2][dim]: of pieces
   int32_t max_pieces, max_slots, shares;
 };
-hipError_t launch_attend_rows(const AttendRowsParams &p, hipStream_t s);
+size_t attend_rows_bytes(int n_rows, int n_k_rows, int n_seqs, int heads, int dim);
+hipError_t launch_attend_rows(const AttendRowsParams &p, uint8_t *workspace, hipStream_t s);
 size_t attend_rows_backward_bytes(int n_rows, int n_k_rows, int n_seqs, int heads, int kv_heads, int dim);
 hipError_t launch_attend_rows_backward(const AttendRowsParams &p, uint8_t *workspace, hipStream_t s);
 

@@ -186,21 +186,31 @@ int moe_attend_pages(const void *q, int64_t q_stride, int64_t q_head_stride, con
   return MOE_OK;
 }
 
+size_t moe_attend_rows_bytes(int32_t n_rows, int32_t n_k_rows, int32_t n_seqs, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim) {
+  if (n_rows < 0 || n_rows >= kMaxRows || n_k_rows < 0 || n_k_rows >= kMaxRows || n_seqs < 0 || n_seqs > MOE_ATTEND_MAX_SEQS || n_kv_heads < 1 ||
+      n_heads < n_kv_heads || n_heads > MOE_ATTEND_MAX_HEADS || head_dim < 8 || head_dim > MOE_ATTEND_MAX_DIM)
+    return 0;
+  return attend_rows_bytes(n_rows, n_k_rows, n_seqs, n_heads, head_dim);
+}
+
 int moe_attend_rows(const void *q, int64_t q_stride, int64_t q_head_stride, const void *k, int64_t k_stride, int64_t k_head_stride, const void *v,
                     int64_t v_stride, int64_t v_head_stride, const int32_t *offsets, const int32_t *k_offsets, int32_t n_seqs, int32_t n_rows,
                     int32_t n_k_rows, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, float softmax_scale, int32_t window, int32_t sinks,
-                    void *y, void *y_low, float *lse, void *stream) {
+                    void *y, void *y_low, float *lse, void *workspace, size_t workspace_bytes, void *stream) {
   if (const int bad = check_attend_rows(q, q_stride, q_head_stride, k, k_stride, k_head_stride, v, v_stride, v_head_stride, offsets, k_offsets,
                                         n_seqs, n_rows, n_k_rows, n_heads, n_kv_heads, head_dim, softmax_scale, window, sinks))
     return bad;
   if (n_rows == 0) return MOE_OK;
   if (!y || off(y, 16) || off(y_low, 16) || off(lse, 4)) return fail(MOE_EINVAL, "y_dev is NULL, or a pointer is not aligned");
+  const size_t need = moe_attend_rows_bytes(n_rows, n_k_rows, n_seqs, n_heads, n_kv_heads, head_dim);
+  if (need > 0 && (!workspace || off(workspace, 16) || workspace_bytes < need))
+    return fail(MOE_EINVAL, "a workspace of %zu bytes, 16-byte aligned, is needed", need);
   AttendRowsParams p = rows_params(q, q_stride, q_head_stride, k, k_stride, k_head_stride, v, v_stride, v_head_stride, offsets, k_offsets, n_seqs,
                                    n_rows, n_k_rows, n_heads, n_kv_heads, head_dim, softmax_scale, window, sinks);
   p.y = static_cast<uint16_t *>(y);
   p.low = static_cast<uint16_t *>(y_low);
   p.lse = lse;
-  HIP_TRY(launch_attend_rows(p, static_cast<hipStream_t>(stream)));
+  HIP_TRY(launch_attend_rows(p, static_cast<uint8_t *>(workspace), static_cast<hipStream_t>(stream)));
   return MOE_OK;
 }
 

@@ -337,7 +337,8 @@ dim3 grid_of(int64_t parts, int heads, int lead = 0) {
 // the tiles of keys that the queries r0 .. r1 of a sequence see, in turn
 struct KeyTiles {
   int sink_tiles, first, n;
-  __device__ __forceinline__ int at(int t) const { return (t < sink_tiles ? t : first + t - sink_tiles) * kTile; }
+  int begin;  // a share's first one
+  __device__ __forceinline__ int at(int t) const { return (t + begin < sink_tiles ? t + begin : first + t + begin - sink_tiles) * kTile; }
 };
 __device__ __forceinline__ KeyTiles key_tiles(const AttendRowsParams &p, const Sequence &s, int r0, int r1) {
   KeyTiles k;
@@ -346,6 +347,7 @@ __device__ __forceinline__ KeyTiles key_tiles(const AttendRowsParams &p, const S
   k.first = lo / kTile;
   k.sink_tiles = min((min(p.sinks, lo) + kTile - 1) / kTile, k.first);
   k.n = k.sink_tiles + max(last - k.first, 0);
+  k.begin = 0;
   return k;
 }
 // of queries at positions p0 .. p1 and keys k0 .. k1: whether all see all, whether none sees any
@@ -464,16 +466,22 @@ struct Queries {
 // each other: the scores of the next 32 keys while the exponentials of these are taken, and the product with the values while the
 // largest of the next scores is found.  The other tiles (the diagonal, a window's edge, first keys) are computed one by one and masked.
 // Tiles are requested two ahead; there is one barrier for each, in its middle or at its end, and values have three places in LDS.
-template <int KS, bool KEEP>
+// SPLIT: few queries, many keys.  The tiles are cut into p.splits shares, each a workgroup's, and what it has goes to the workspace.
+// (32 heads of 128, 8 of k: 100 queries behind 8000 tokens 36 us, with 32 queries a workgroup and no shares 72; 512 behind 8000: 63, 88, where the
+// products alone take 46; four times 4 behind up to 9000: 60, 150.  8 heads, 2000 tokens: 33, 46.  Below some 1500 keys it
+// does not pay: 8 heads, 1000 tokens 24.5, 20.6; 300 queries with a window of 1000: 20.8, 15.2.)
+template <int KS, bool KEEP, bool SPLIT>
 __global__ __launch_bounds__(kBlock, 2) void attend_rows_kernel(const AttendRowsParams p, const int parts) {
   using T = Tiles<KS>;
   __shared__ __align__(256) uint8_t lds[5 * T::BYTES];
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
-  const Item item = item_of(p.heads, p.kv_heads);
+  Item item = item_of(p.heads, p.kv_heads);
+  const int place = item.part, share = SPLIT ? uniform(place % p.splits) : 0;
+  if (SPLIT) item.part = uniform(place / p.splits);
   if (item.part >= parts) return;
   const Part part = part_of(p, item.part);
   if (part.sequence < 0) {
-    if (part.over >= 0)
+    if (part.over >= 0 && share == 0)
       clear_rows(p.offsets, p.n_seqs, p.n_rows, p.y, item.head, p.heads, p.dim, part.over, parts - (item.part - part.over));
     return;
   }
@@ -481,7 +489,12 @@ __global__ __launch_bounds__(kBlock, 2) void attend_rows_kernel(const AttendRows
   const int r0 = part.part * kOwn, r1 = min(r0 + kOwn, s.nq) - 1, mine = r0 + wave * 32, row = mine + (lane & 31);
   const int p0 = mine + s.ahead, p1 = min(mine + 31, r1) + s.ahead, pos = row + s.ahead;
   const int kv = item.head / (p.heads / p.kv_heads);
-  const KeyTiles tiles = key_tiles(p, s, r0, r1);
+  KeyTiles tiles = key_tiles(p, s, r0, r1);
+  if (SPLIT) {
+    const int all = tiles.n;
+    tiles.begin = uniform((int)((int64_t)all * share / p.splits));
+    tiles.n = uniform((int)((int64_t)all * (share + 1) / p.splits)) - tiles.begin;
+  }
   const uint16_t *k = static_cast<const uint16_t *>(p.k.at) + s.k0 * p.k.token + kv * p.k.head;
   const uint16_t *v = static_cast<const uint16_t *>(p.v.at) + s.k0 * p.v.token + kv * p.v.head;
   const typename T::Source ks = T::source(wave, lane, p.k.token), vs = T::source(wave, lane, p.v.token);
@@ -526,8 +539,8 @@ __global__ __launch_bounds__(kBlock, 2) void attend_rows_kernel(const AttendRows
     }
     // tiles from..to - 1 are seen by all
     const int w0 = r0 + s.ahead, w1 = r1 + s.ahead;
-    const int to = min(max(tiles.sink_tiles + (w0 + 1) / kTile - tiles.first, 0), tiles.n);
-    const int from = p.window > 0 ? min(tiles.sink_tiles + max((max(w1 - p.window + 1, 0) + kTile - 1) / kTile - tiles.first, 0), to) : 0;
+    const int to = min(max(tiles.sink_tiles + (w0 + 1) / kTile - tiles.first - tiles.begin, 0), tiles.n);
+    const int from = p.window > 0 ? min(max(tiles.sink_tiles + max((max(w1 - p.window + 1, 0) + kTile - 1) / kTile - tiles.first, 0) - tiles.begin, 0), to) : 0;
     const int fast = min(to, tiles.n - 1);  // (the last one looks ahead in vain, unless there is nothing behind it)
     int t = 0;
 #pragma unroll 1
@@ -549,10 +562,80 @@ __global__ __launch_bounds__(kBlock, 2) void attend_rows_kernel(const AttendRows
   }
   const bool there = row < s.nq;
   const float total = w.rounded + __shfl_xor(w.rounded, 32);
+  if (SPLIT) {
+    w.sum += __shfl_xor(w.sum, 32);
+    const int64_t at = ((int64_t)place * p.heads + item.head) * kOwn + wave * 32 + (lane & 31);
+#pragma unroll
+    for (int d = 0; d < T::DS; ++d)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int c = d * 32 + i * 8 + (lane >> 5) * 4;
+        if (there && c < p.dim) *reinterpret_cast<f32x4 *>(p.sums + at * p.dim + c) = f32x4{w.o[d][4 * i], w.o[d][4 * i + 1], w.o[d][4 * i + 2], w.o[d][4 * i + 3]};
+      }
+    if (there && lane < 32) *reinterpret_cast<f32x4 *>(p.stats + at * 4) = f32x4{w.top, total, w.sum, 0.f};
+    return;
+  }
   const int64_t dense = ((int64_t)(s.q0 + row) * p.heads + item.head) * p.dim;
   T::store(p.y + dense, p.low ? p.low + dense : nullptr, there, p.dim, lane, w.o, total > 0.f || total != total ? 1.f / total : 0.f);
   if (KEEP) w.sum += __shfl_xor(w.sum, 32);
   if (KEEP && there && lane < 32) p.lse[(int64_t)item.head * p.n_rows + s.q0 + row] = w.top * kLn2 + __logf(w.sum);
+}
+
+// What the shares of the keys have; a workgroup has kJoinRows of the queries of a part, a thread eight dims of one of them.
+constexpr int kJoinRows = 16;
+__global__ __launch_bounds__(kBlock) void join_rows_kernel(const AttendRowsParams p, const int parts) {
+  const int b = blockIdx.x, row0 = b % (kOwn / kJoinRows) * kJoinRows, head = b / (kOwn / kJoinRows) % p.heads, at = b / (kOwn / kJoinRows) / p.heads;
+  const Part part = part_of(p, at);
+  if (at >= parts || part.sequence < 0) return;
+  const int first = part.part * kOwn + row0, rows = min(kJoinRows, part.s.nq - first), chunks = p.dim / 8;
+  for (int u = threadIdx.x; u < rows * chunks; u += kBlock) {
+    const int r = u / chunks, c = u % chunks * 8;
+    const int64_t from = ((int64_t)at * p.splits * p.heads + head) * kOwn + row0 + r, step = (int64_t)p.heads * kOwn;
+    float top = -INFINITY, total = 0.f, sum = 0.f;
+    f32x4 x[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+    constexpr int AT_ONCE = 4;  // shares whose loads are under way together
+    for (int i0 = 0; i0 < p.splits; i0 += AT_ONCE) {
+      f32x4 of[AT_ONCE], y[AT_ONCE][2];
+#pragma unroll
+      for (int i = 0; i < AT_ONCE; ++i) {
+        const int64_t share = from + min(i0 + i, p.splits - 1) * step;
+        of[i] = *reinterpret_cast<const f32x4 *>(p.stats + share * 4);
+        if (i0 + i >= p.splits) of[i] = f32x4{-INFINITY, 0.f, 0.f, 0.f};
+        y[i][0] = *reinterpret_cast<const f32x4 *>(p.sums + share * p.dim + c);
+        y[i][1] = *reinterpret_cast<const f32x4 *>(p.sums + share * p.dim + c + 4);
+      }
+      float to = top;
+#pragma unroll
+      for (int i = 0; i < AT_ONCE; ++i) to = fmaxf(to, of[i][0]);
+      const float base = to == -INFINITY ? 0.f : to, shrink = __builtin_amdgcn_exp2f(top - base);
+      top = to;
+      total *= shrink;
+      sum *= shrink;
+      x[0] *= shrink;
+      x[1] *= shrink;
+#pragma unroll
+      for (int i = 0; i < AT_ONCE; ++i) {
+        if (of[i][0] == -INFINITY) continue;  // (nothing of it is seen)
+        const float weight = __builtin_amdgcn_exp2f(of[i][0] - base);
+        total += weight * of[i][1];
+        sum += weight * of[i][2];
+        x[0] += weight * y[i][0];
+        x[1] += weight * y[i][1];
+      }
+    }
+    const float inv = total > 0.f || total != total ? 1.f / total : 0.f;
+    const int64_t dense = ((int64_t)(part.s.q0 + first + r) * p.heads + head) * p.dim + c;
+    rows_u32x4 hi, lo;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float v0 = x[i / 2][i % 2 * 2] * inv, v1 = x[i / 2][i % 2 * 2 + 1] * inv;
+      hi[i] = pack_bf16(v0, v1);
+      lo[i] = pack_bf16(v0 - bf16_lo(hi[i]), v1 - bf16_hi(hi[i]));
+    }
+    *reinterpret_cast<rows_u32x4 *>(p.y + dense) = hi;
+    if (p.low) *reinterpret_cast<rows_u32x4 *>(p.low + dense) = lo;
+    if (p.lse && c == 0) p.lse[(int64_t)head * p.n_rows + part.s.q0 + first + r] = top * kLn2 + __logf(sum);
+  }
 }
 
 // Few queries: a workgroup has 32, and each of its wavefronts a quarter of the keys, 32 at a time in turn, in a ring of its own; what
@@ -1031,7 +1114,6 @@ __global__ __launch_bounds__(kBlock, 2) void attend_rows_dkv_kernel(const Attend
 }
 
 // The sums of the pieces of a list, in order; a workgroup has kJoinRows of its keys
-constexpr int kJoinRows = 16;
 __global__ __launch_bounds__(kBlock) void join_pieces_kernel(const AttendRowsParams p) {
   const uint32_t b = (uint32_t)row_group();
   const int strip = b % (kOwn / kJoinRows), kv = b / (kOwn / kJoinRows) % p.kv_heads, at = b / (kOwn / kJoinRows) / p.kv_heads;
@@ -1065,9 +1147,45 @@ void with_steps(int dim, F f) {
 
 }  // namespace
 
-constexpr int kFew = 128;  // workgroups of kOwn queries up to which a wavefront takes a quarter of the keys instead
-hipError_t launch_attend_rows(const AttendRowsParams &p, hipStream_t s) {
+constexpr int kFew = 128;        // workgroups of kOwn queries up to which a wavefront takes a quarter of the keys instead
+constexpr int kShareKeys = 256, kManyKeys = 1500;  // of a sequence: for a share of them at least; for there to be any
+constexpr int kMostShares = 512; // workgroups of shares, as many as the GPU holds at once
+struct ForwardSpace {
+  int splits;
+  int64_t sums, bytes;  // where they begin
+};
+// seen: keys of a query at most
+static ForwardSpace forward_space(int n_rows, int n_k_rows, int n_seqs, int heads, int dim, int64_t seen) {
+  ForwardSpace w{1, 0, 0};
+  if (n_seqs > 0) seen = std::min<int64_t>(n_k_rows / n_seqs, seen);
+  if (n_seqs == 0 || n_rows == 0 || seen < kManyKeys) return w;
+  const int64_t parts = parts_of(n_rows, n_seqs), real = std::max<int64_t>(parts - 1, 1) * heads;
+  w.splits = (int)std::max<int64_t>(std::min(kMostShares / real, seen / kShareKeys), 1);
+  if (w.splits == 1) return w;
+  const int64_t rows = parts * w.splits * heads * kOwn;
+  w.sums = rows * 16;
+  w.bytes = w.sums + rows * dim * 4;
+  return w;
+}
+size_t attend_rows_bytes(int n_rows, int n_k_rows, int n_seqs, int heads, int dim) { return forward_space(n_rows, n_k_rows, n_seqs, heads, dim, n_k_rows).bytes; }
+
+hipError_t launch_attend_rows(const AttendRowsParams &given, uint8_t *workspace, hipStream_t s) {
+  AttendRowsParams p = given;
   const int parts = parts_of(p.n_rows, p.n_seqs);
+  const int64_t seen = p.window > 0 ? (int64_t)p.window + p.sinks + kOwn : p.n_k_rows;
+  const ForwardSpace w = forward_space(p.n_rows, p.n_k_rows, p.n_seqs, p.heads, p.dim, seen);
+  if (w.splits > 1) {
+    p.splits = w.splits;
+    p.stats = reinterpret_cast<float *>(workspace);
+    p.sums = reinterpret_cast<float *>(workspace + w.sums);
+    with_steps(p.dim, [&](auto ks) {
+      attend_rows_kernel<decltype(ks)::value, true, true><<<grid_of((int64_t)parts * w.splits, p.heads), kBlock, 0, s>>>(p, parts);
+    });
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    join_rows_kernel<<<(parts - 1) * p.heads * (kOwn / kJoinRows), kBlock, 0, s>>>(p, parts - 1);
+    return hipGetLastError();
+  }
   with_steps(p.dim, [&](auto ks) {
     constexpr int KS = decltype(ks)::value;
     if ((int64_t)parts * p.heads <= kFew) {
@@ -1076,8 +1194,8 @@ hipError_t launch_attend_rows(const AttendRowsParams &p, hipStream_t s) {
       else attend_few_rows_kernel<KS, false><<<grid_of(few, p.heads), kBlock, 0, s>>>(p, few);
       return;
     }
-    if (p.lse) attend_rows_kernel<KS, true><<<grid_of(parts, p.heads), kBlock, 0, s>>>(p, parts);
-    else attend_rows_kernel<KS, false><<<grid_of(parts, p.heads), kBlock, 0, s>>>(p, parts);
+    if (p.lse) attend_rows_kernel<KS, true, false><<<grid_of(parts, p.heads), kBlock, 0, s>>>(p, parts);
+    else attend_rows_kernel<KS, false, false><<<grid_of(parts, p.heads), kBlock, 0, s>>>(p, parts);
   });
   return hipGetLastError();
 }

@@ -171,9 +171,12 @@ std::tuple<Tensor, Maybe, Maybe> attend_rows(const Tensor &q, const Tensor &k, c
     lse = fresh(q, {r.q.h, r.q.n}, at::kFloat, r.ok);
     low = fresh(q, {r.q.n, r.q.h, r.q.d}, at::kBFloat16, r.ok);
   }
+  Maybe work;
+  const size_t need = moe_attend_rows_bytes(r.q.n, r.k.n, r.n, r.q.h, r.k.h, r.q.d);
+  if (need) work = fresh(q, {(int64_t)need}, at::kByte, r.ok);
   check(moe_attend_rows(q.const_data_ptr(), r.q.token, r.q.head, k.const_data_ptr(), r.k.token, r.k.head, v.const_data_ptr(), r.v.token, r.v.head,
                         ints(offsets), r.k_offsets, r.n, r.q.n, r.k.n, r.q.h, r.k.h, r.q.d, scale_of(scale, r.q.d), size_or_all(window),
-                        size_or_all(sinks), y.mutable_data_ptr(), to(low), to_floats(lse), on.stream()),
+                        size_or_all(sinks), y.mutable_data_ptr(), to(low), to_floats(lse), to(work), need, on.stream()),
         "moe_attend_rows");
   return {y, lse, low};
 }

@@ -71,7 +71,13 @@ BAD_ROWS = BAD_SEEN + [
 
 @pytest.mark.parametrize("bad", BAD_ROWS + [dict(y=None), dict(y=P + 4), dict(low=P + 8), dict(lse=P + 2)])
 def test_rows(B, bad):
-    refused(B, B.lib.moe_attend_rows, dict(ROWS, y=P, low=None, lse=None, stream=None), **bad)
+    refused(B, B.lib.moe_attend_rows, dict(ROWS, y=P, low=None, lse=None, work=P, work_bytes=1 << 28, stream=None), **bad)
+
+
+@pytest.mark.parametrize("bad", [dict(work=None), dict(work=P + 8), dict(work_bytes=1 << 10)])
+def test_rows_of_many_keys(B, bad):
+    good = dict(ROWS, n_k_rows=9000, y=P, low=None, lse=None, work=P, work_bytes=B.moe_attend_rows_bytes(100, 9000, 3, 4, 2, 64), stream=None)
+    refused(B, B.lib.moe_attend_rows, good, **bad)
 
 
 @pytest.mark.parametrize("bad", BAD_ROWS + [dict(y=None), dict(lse=None), dict(dy=None), dict(dq=None), dict(dk=None), dict(dv=None), dict(dy=P + 8), dict(low=P + 2),
@@ -85,6 +91,10 @@ def test_workspaces(B):
     assert size(100, 300, 3, 4, 2, 64) >= 1600 and size(0, 0, 0, 4, 2, 64) > 0
     assert all(size(*bad) == 0 for bad in [(-1, 3, 1, 4, 2, 64), (3, 1 << 26, 1, 4, 2, 64), (3, 3, -1, 4, 2, 64), (3, 3, 1, 4, 0, 64), (3, 3, 1, 2, 4, 64), (3, 3, 1, 4, 2, 200)])
     assert size(20001, 20001, 9, 16, 2, 80) < 128 << 20  # (pieces' sums do not grow with the rows)
+    size = B.moe_attend_rows_bytes
+    assert size(100, 8100, 1, 32, 8, 128) > 0 and size(8192, 8192, 1, 32, 8, 128) == 0 and size(100, 100, 1, 32, 8, 128) == 0
+    assert all(size(*bad) == 0 for bad in [(-1, 8100, 1, 4, 2, 64), (3, 1 << 26, 1, 4, 2, 64), (3, 8100, -1, 4, 2, 64), (3, 8100, 0, 4, 2, 64), (0, 8100, 1, 4, 2, 64), (3, 8100, 1, 4, 0, 64)])
+    assert max(size(n, 1 << 25, 1, h, 1, 128) for n in (1, 100, 128, 1000, 5000, 32000) for h in (1, 3, 32, 200)) < 80 << 20  # (shares do not grow with the keys)
     assert B.moe_attend_pages_bytes(0, 4, 2, 64) == 0 and B.moe_attend_pages_bytes(3, 4, 2, 64) > 0
     assert B.moe_attend_pages_bytes(3, 4, 0, 64) == 0 and B.moe_attend_pages_bytes(3, 2, 4, 64) == 0
 
@@ -92,7 +102,7 @@ def test_workspaces(B):
 def test_nothing_to_do(B):
     assert B.lib.moe_store_pages(*dict(STORE, n_rows=0, k=None, v=None, slots=None).values()) == B.MOE_OK
     assert B.lib.moe_attend_pages(*dict(PAGES, n_seqs=0, q=None, y=None, work=None, work_bytes=0).values()) == B.MOE_OK
-    assert B.lib.moe_attend_rows(*dict(ROWS, n_rows=0, q=None, y=None, low=None, lse=None, stream=None).values()) == B.MOE_OK
+    assert B.lib.moe_attend_rows(*dict(ROWS, n_rows=0, q=None, y=None, low=None, lse=None, work=None, work_bytes=0, stream=None).values()) == B.MOE_OK
 
 
 def test_tensors_on_the_cpu_and_of_other_shapes(B):
