@@ -134,10 +134,10 @@ ROWS = [
     ([2500, 0, 701], None, 12, 2, 80, 200, 5),
     ([100, 1500], [2000, 1500], 8, 1, 96, 0, 0),
     ([100], [4000], 4, 2, 128, 0, 0),                    # few queries of many keys: the keys are cut into shares
-    ([1, 0, 40, 3], [1500, 700, 1900, 0], 2, 1, 72, 0, 0),
-    ([130, 6], [2900, 1300], 2, 2, 64, 700, 5),
-    ([130], [3001], 6, 1, 96, 1000, 130),
-    ([1400], None, 1, 1, 80, 0, 0),
+    ([1, 0, 40, 3], [4500, 700, 1900, 0], 2, 1, 72, 0, 0),
+    ([130, 6], [2900, 1300], 2, 2, 64, 1600, 5),
+    ([130], [3001], 6, 1, 96, 1400, 130),
+    ([1800], None, 1, 1, 80, 0, 0),
     ([1] + [0] * 70 + [90], [1000] * 71 + [40000], 1, 1, 16, 0, 0),
 ]
 
@@ -217,15 +217,15 @@ def test_rows_that_are_not_seen_may_hold_anything(lib, window, sinks, dim, what,
 def test_shares_of_keys_that_are_not_seen(lib, what):
     """As above where the keys are cut into shares; rows of no sequence are zeros, and so is what sees no key."""
     g = gen(21)
-    H, KV, dim, each, keys = 2, 1, 64, [40, 7], [1200, 2]
+    H, KV, dim, each, keys = 2, 1, 64, [40, 7], [4000, 2]
     q = normal(g, 60, H, dim, std=2.0, dtype=BF16)
-    k, v = normal(g, 1210, KV, dim, dtype=BF16), normal(g, 1210, KV, dim, dtype=BF16)
-    want = reference(q[:47], k[:1202], v[:1202], each, keys, 0, 0, dim ** -0.5)
-    k[1202:], v[1202:] = what, what
-    v[1180, 0, 5] = what
+    k, v = normal(g, 4010, KV, dim, dtype=BF16), normal(g, 4010, KV, dim, dtype=BF16)
+    want = reference(q[:47], k[:4002], v[:4002], each, keys, 0, 0, dim ** -0.5)
+    k[4002:], v[4002:] = what, what
+    v[3980, 0, 5] = what
     k_offsets = ints(starts(keys))
     y, kept = lib.attend_rows(q, k, v, ints(starts(each)), k_offsets=k_offsets, keep=True)
-    assert lib.moe_attend_rows_bytes(60, 1210, 2, H, KV, dim) > 0
+    assert lib.moe_attend_rows_bytes(60, 4010, 2, H, KV, dim) > 0
     assert not y[47:].any() and not y[40:45].any() and bool((kept.lse[:, 40:45] == -math.inf).all())
     sees = torch.arange(40, device=DEV) >= 20
     one = y[:40][sees][:, :, 5].float()
