@@ -56,7 +56,7 @@ struct AttendRowsParams {
   uint16_t *y;
   uint16_t *low;  // y's rounding, or NULL
   float *lse;     // [heads][n_rows], forward: may be NULL
-  int32_t splits; // of the keys, forward: 1, or stats [parts][splits][heads][128 queries][4] and sums [...][128][dim] are used
+  int32_t splits; // shares of the keys of 128 queries; more than one, forward: stats [parts][splits][heads][128 queries][4], sums [...][128][dim]
   // backward
   const uint16_t *dy;
   uint16_t *dq, *dk, *dv;
@@ -64,6 +64,7 @@ struct AttendRowsParams {
   int32_t *n_pieces;
   KeyPiece *pieces;
   float *sums;  // [max_slots][kv_heads][128 keys][2][dim]: of pieces
+  float *q_sums;  // [parts][splits][heads][128 queries][dim]: of shares
   int32_t max_pieces, max_slots, shares;
 };
 size_t attend_rows_bytes(int n_rows, int n_k_rows, int n_seqs, int heads, int dim);

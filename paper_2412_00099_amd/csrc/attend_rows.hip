@@ -212,6 +212,16 @@ struct Tiles {
         if (low) put(low, d, i, l);
       }
   }
+  // ... in 32 bits
+  static __device__ __forceinline__ void store_sums(float *at, bool there, int dim, int lane, const f32x16 (&o)[DS]) {
+#pragma unroll
+    for (int d = 0; d < DS; ++d)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int c = d * 32 + i * 8 + (lane >> 5) * 4;
+        if (there && c < dim) *reinterpret_cast<f32x4 *>(at + c) = f32x4{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]};
+      }
+  }
 };
 __device__ __forceinline__ float largest(const f32x16 &z) {
   float m = z[0];
@@ -339,6 +349,11 @@ struct KeyTiles {
   int sink_tiles, first, n;
   int begin;  // a share's first one
   __device__ __forceinline__ int at(int t) const { return (t + begin < sink_tiles ? t + begin : first + t + begin - sink_tiles) * kTile; }
+  __device__ __forceinline__ void cut(int share, int of) {
+    const int all = n;
+    begin = uniform((int)((int64_t)all * share / of));
+    n = uniform((int)((int64_t)all * (share + 1) / of)) - begin;
+  }
 };
 __device__ __forceinline__ KeyTiles key_tiles(const AttendRowsParams &p, const Sequence &s, int r0, int r1) {
   KeyTiles k;
@@ -490,11 +505,7 @@ __global__ __launch_bounds__(kBlock, 2) void attend_rows_kernel(const AttendRows
   const int p0 = mine + s.ahead, p1 = min(mine + 31, r1) + s.ahead, pos = row + s.ahead;
   const int kv = item.head / (p.heads / p.kv_heads);
   KeyTiles tiles = key_tiles(p, s, r0, r1);
-  if (SPLIT) {
-    const int all = tiles.n;
-    tiles.begin = uniform((int)((int64_t)all * share / p.splits));
-    tiles.n = uniform((int)((int64_t)all * (share + 1) / p.splits)) - tiles.begin;
-  }
+  if (SPLIT) tiles.cut(share, p.splits);
   const uint16_t *k = static_cast<const uint16_t *>(p.k.at) + s.k0 * p.k.token + kv * p.k.head;
   const uint16_t *v = static_cast<const uint16_t *>(p.v.at) + s.k0 * p.v.token + kv * p.v.head;
   const typename T::Source ks = T::source(wave, lane, p.k.token), vs = T::source(wave, lane, p.v.token);
@@ -565,13 +576,7 @@ __global__ __launch_bounds__(kBlock, 2) void attend_rows_kernel(const AttendRows
   if (SPLIT) {
     w.sum += __shfl_xor(w.sum, 32);
     const int64_t at = ((int64_t)place * p.heads + item.head) * kOwn + wave * 32 + (lane & 31);
-#pragma unroll
-    for (int d = 0; d < T::DS; ++d)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int c = d * 32 + i * 8 + (lane >> 5) * 4;
-        if (there && c < p.dim) *reinterpret_cast<f32x4 *>(p.sums + at * p.dim + c) = f32x4{w.o[d][4 * i], w.o[d][4 * i + 1], w.o[d][4 * i + 2], w.o[d][4 * i + 3]};
-      }
+    T::store_sums(p.sums + at * p.dim, there, p.dim, lane, w.o);
     if (there && lane < 32) *reinterpret_cast<f32x4 *>(p.stats + at * 4) = f32x4{w.top, total, w.sum, 0.f};
     return;
   }
@@ -878,7 +883,9 @@ __device__ __forceinline__ void add_columns(const typename T::Reader &at, uint32
   __builtin_amdgcn_sched_barrier(0);
 }
 
-template <int KS>
+// SPLIT: few queries, many keys, as in the forward; the sums of a share's keys go to the workspace.  (With all else: 2000 tokens, 8 heads of 128
+// for 2, 133 us, without shares 161; 1000 of 8 heads 80, 94; 400 54, 59; 3529 behind up to 12135, 2 heads: 244, 466.)
+template <int KS, bool SPLIT>
 __global__ __launch_bounds__(kBlock, 2) void attend_rows_dq_kernel(const AttendRowsParams p, const int parts) {
   using T = Tiles<KS>;
   __shared__ __align__(256) uint8_t lds[4 * T::BYTES];
@@ -887,11 +894,13 @@ __global__ __launch_bounds__(kBlock, 2) void attend_rows_dq_kernel(const AttendR
     if (row_group() == 0) plan_pieces(p, lds);
     return;
   }
-  const Item item = item_of(p.heads, p.kv_heads, kLead);
+  Item item = item_of(p.heads, p.kv_heads, kLead);
+  const int place = item.part, share = SPLIT ? uniform(place % p.splits) : 0;
+  if (SPLIT) item.part = uniform(place / p.splits);
   if (item.part >= parts) return;
   const Part part = part_of(p, item.part);
   if (part.sequence < 0) {
-    if (part.over >= 0)
+    if (part.over >= 0 && share == 0)
       clear_rows(p.offsets, p.n_seqs, p.n_rows, p.dq, item.head, p.heads, p.dim, part.over, parts - (item.part - part.over));
     return;
   }
@@ -899,7 +908,8 @@ __global__ __launch_bounds__(kBlock, 2) void attend_rows_dq_kernel(const AttendR
   const int r0 = part.part * kOwn, r1 = min(r0 + kOwn, s.nq) - 1, mine = r0 + wave * 32, row = mine + (lane & 31);
   const int p0 = mine + s.ahead, p1 = min(mine + 31, r1) + s.ahead, pos = row + s.ahead;
   const int kv = item.head / (p.heads / p.kv_heads);
-  const KeyTiles tiles = key_tiles(p, s, r0, r1);
+  KeyTiles tiles = key_tiles(p, s, r0, r1);
+  if (SPLIT) tiles.cut(share, p.splits);
   const uint16_t *k = static_cast<const uint16_t *>(p.k.at) + s.k0 * p.k.token + kv * p.k.head;
   const uint16_t *v = static_cast<const uint16_t *>(p.v.at) + s.k0 * p.v.token + kv * p.v.head;
   const typename T::Source ks = T::source(wave, lane, p.k.token), vs = T::source(wave, lane, p.v.token);
@@ -932,7 +942,7 @@ __global__ __launch_bounds__(kBlock, 2) void attend_rows_dq_kernel(const AttendR
   }
   T::own(static_cast<const uint16_t *>(p.q.at) + at_row * p.q.token + item.head * p.q.head, there, p.dim, lane, q);
   const float lse = p.lse[(int64_t)item.head * p.n_rows + at_row] * kLog2e, scale = p.scale * kLog2e;
-  if (there && lane < 32) {
+  if (there && lane < 32 && share == 0) {
     p.stats[(int64_t)item.head * p.n_rows + at_row] = -lse;
     p.stats[(int64_t)(p.heads + item.head) * p.n_rows + at_row] = -delta;
   }
@@ -975,6 +985,10 @@ __global__ __launch_bounds__(kBlock, 2) void attend_rows_dq_kernel(const AttendR
         f[1] = low[1];
       }
     }
+  }
+  if (SPLIT) {
+    T::store_sums(p.q_sums + (((int64_t)place * p.heads + item.head) * kOwn + wave * 32 + (lane & 31)) * p.dim, there, p.dim, lane, o);
+    return;
   }
   T::store(p.dq + dense, nullptr, there, p.dim, lane, o, p.scale);
 }
@@ -1097,15 +1111,8 @@ __global__ __launch_bounds__(kBlock, 2) void attend_rows_dkv_kernel(const Attend
   }
   if (piece.of > 1) {
     float *sums = p.sums + (((int64_t)(piece.slot + piece.index) * p.kv_heads + kv) * kOwn + key - k0) * 2 * p.dim;
-#pragma unroll
-    for (int d = 0; d < T::DS; ++d)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int c = d * 32 + i * 8 + (lane >> 5) * 4;
-        if (!there || c >= p.dim) continue;
-        *reinterpret_cast<f32x4 *>(sums + c) = f32x4{dk[d][4 * i], dk[d][4 * i + 1], dk[d][4 * i + 2], dk[d][4 * i + 3]};
-        *reinterpret_cast<f32x4 *>(sums + p.dim + c) = f32x4{dv[d][4 * i], dv[d][4 * i + 1], dv[d][4 * i + 2], dv[d][4 * i + 3]};
-      }
+    T::store_sums(sums, there, p.dim, lane, dk);
+    T::store_sums(sums + p.dim, there, p.dim, lane, dv);
     return;
   }
   const int64_t to = (at_key * p.kv_heads + kv) * p.dim;
@@ -1113,9 +1120,27 @@ __global__ __launch_bounds__(kBlock, 2) void attend_rows_dkv_kernel(const Attend
   T::store(p.dv + to, nullptr, there, p.dim, lane, dv, 1.f);
 }
 
-// The sums of the pieces of a list, in order; a workgroup has kJoinRows of its keys
-__global__ __launch_bounds__(kBlock) void join_pieces_kernel(const AttendRowsParams p) {
-  const uint32_t b = (uint32_t)row_group();
+// The sums of the pieces of a list, in order; a workgroup has kJoinRows of its keys.  The first `ahead` workgroups: the shares of the
+// gradients of q, kJoinRows queries each.
+__global__ __launch_bounds__(kBlock) void join_pieces_kernel(const AttendRowsParams p, const int ahead) {
+  uint32_t b = (uint32_t)row_group();
+  if ((int)b < ahead) {
+    const int strip = b % (kOwn / kJoinRows), head = b / (kOwn / kJoinRows) % p.heads, at = b / (kOwn / kJoinRows) / p.heads;
+    const Part part = part_of(p, at);
+    if (part.sequence < 0) return;
+    const int first = part.part * kOwn + strip * kJoinRows, rows = min(kJoinRows, part.s.nq - first), quads = p.dim / 4;
+    const int64_t step = (int64_t)p.heads * kOwn * p.dim;
+    for (int u = threadIdx.x; u < rows * quads; u += kBlock) {
+      const int r = u / quads, c = u % quads * 4;
+      const float *from = p.q_sums + (((int64_t)at * p.splits * p.heads + head) * kOwn + strip * kJoinRows + r) * p.dim + c;
+      f32x4 v = {0.f, 0.f, 0.f, 0.f};
+      for (int i = 0; i < p.splits; ++i) v += *reinterpret_cast<const f32x4 *>(from + i * step);
+      v *= p.scale;
+      *reinterpret_cast<rows_u32x2 *>(p.dq + ((int64_t)(part.s.q0 + first + r) * p.heads + head) * p.dim + c) = rows_u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+    }
+    return;
+  }
+  b -= ahead;
   const int strip = b % (kOwn / kJoinRows), kv = b / (kOwn / kJoinRows) % p.kv_heads, at = b / (kOwn / kJoinRows) / p.kv_heads;
   if (at >= *p.n_pieces) return;
   const KeyPiece piece = p.pieces[at];
@@ -1136,6 +1161,19 @@ __global__ __launch_bounds__(kBlock) void join_pieces_kernel(const AttendRowsPar
 // parts of `own` rows that the sequences have at most, and one at least that is none's: it clears the rows of no sequence
 int parts_of(int n_rows, int n_seqs, int own = kOwn) { return n_rows / own + n_seqs + 1; }
 
+// keys of a query, at most
+int64_t seen_of(const AttendRowsParams &p) { return p.window > 0 ? (int64_t)p.window + p.sinks + kOwn : p.n_k_rows; }
+// Into how many shares the keys of kOwn queries are cut: 1 unless a sequence has `many` keys that are seen, and then so many that there
+// are as many workgroups as the GPU holds at once, with `least` keys each or more.
+constexpr int kMostShares = 512;
+int shares_of_keys(int n_rows, int n_k_rows, int n_seqs, int heads, int64_t seen, int least, int many) {
+  if (n_seqs == 0 || n_rows == 0) return 1;
+  seen = std::min<int64_t>(n_k_rows / n_seqs, seen);
+  if (seen < many) return 1;
+  const int64_t real = std::max<int64_t>(parts_of(n_rows, n_seqs) - 1, 1) * heads;
+  return (int)std::max<int64_t>(std::min(kMostShares / real, seen / least), 1);
+}
+
 // f(steps over the dims): as many as there are, or the next more that there is a kernel for
 template <typename F>
 void with_steps(int dim, F f) {
@@ -1148,21 +1186,15 @@ void with_steps(int dim, F f) {
 }  // namespace
 
 constexpr int kFew = 128;        // workgroups of kOwn queries up to which a wavefront takes a quarter of the keys instead
-constexpr int kShareKeys = 256, kManyKeys = 1500;  // of a sequence: for a share of them at least; for there to be any
-constexpr int kMostShares = 512; // workgroups of shares, as many as the GPU holds at once
 struct ForwardSpace {
   int splits;
   int64_t sums, bytes;  // where they begin
 };
-// seen: keys of a query at most
+constexpr int kShareKeys = 256, kManyKeys = 1500;  // of a sequence: for a share of them at least; for there to be any
 static ForwardSpace forward_space(int n_rows, int n_k_rows, int n_seqs, int heads, int dim, int64_t seen) {
-  ForwardSpace w{1, 0, 0};
-  if (n_seqs > 0) seen = std::min<int64_t>(n_k_rows / n_seqs, seen);
-  if (n_seqs == 0 || n_rows == 0 || seen < kManyKeys) return w;
-  const int64_t parts = parts_of(n_rows, n_seqs), real = std::max<int64_t>(parts - 1, 1) * heads;
-  w.splits = (int)std::max<int64_t>(std::min(kMostShares / real, seen / kShareKeys), 1);
+  ForwardSpace w{shares_of_keys(n_rows, n_k_rows, n_seqs, heads, seen, kShareKeys, kManyKeys), 0, 0};
   if (w.splits == 1) return w;
-  const int64_t rows = parts * w.splits * heads * kOwn;
+  const int64_t rows = (int64_t)parts_of(n_rows, n_seqs) * w.splits * heads * kOwn;
   w.sums = rows * 16;
   w.bytes = w.sums + rows * dim * 4;
   return w;
@@ -1172,8 +1204,7 @@ size_t attend_rows_bytes(int n_rows, int n_k_rows, int n_seqs, int heads, int di
 hipError_t launch_attend_rows(const AttendRowsParams &given, uint8_t *workspace, hipStream_t s) {
   AttendRowsParams p = given;
   const int parts = parts_of(p.n_rows, p.n_seqs);
-  const int64_t seen = p.window > 0 ? (int64_t)p.window + p.sinks + kOwn : p.n_k_rows;
-  const ForwardSpace w = forward_space(p.n_rows, p.n_k_rows, p.n_seqs, p.heads, p.dim, seen);
+  const ForwardSpace w = forward_space(p.n_rows, p.n_k_rows, p.n_seqs, p.heads, p.dim, seen_of(p));
   if (w.splits > 1) {
     p.splits = w.splits;
     p.stats = reinterpret_cast<float *>(workspace);
@@ -1203,10 +1234,11 @@ hipError_t launch_attend_rows(const AttendRowsParams &given, uint8_t *workspace,
 // The workspace: what the gradients of k and v need of each query, the pieces, their sums.  A list of n tiles is cut if n > 1.5 shares, into n / share + 1 pieces at most, so that
 // there are 5 / 3 pieces of lists that are cut for each of all lists' shares.
 struct BackwardSpace {
-  int64_t pieces, sums, bytes;  // where they begin
-  int max_pieces, max_slots;
+  int64_t pieces, sums, q_sums, bytes;  // where they begin
+  int max_pieces, max_slots, splits;
 };
-static BackwardSpace backward_space(int n_rows, int n_k_rows, int n_seqs, int heads, int kv_heads, int dim) {
+constexpr int kShareKeysDq = 128, kManyKeysDq = 256;
+static BackwardSpace backward_space(int n_rows, int n_k_rows, int n_seqs, int heads, int kv_heads, int dim, int64_t seen) {
   BackwardSpace w;
   const int parts = parts_of(n_k_rows, n_seqs);
   const int64_t list = (int64_t)(heads / kv_heads) * ((n_rows + kTile - 1) / kTile);  // tiles, at most
@@ -1216,31 +1248,40 @@ static BackwardSpace backward_space(int n_rows, int n_k_rows, int n_seqs, int he
   const auto up = [](int64_t v) { return (v + 255) / 256 * 256; };
   w.pieces = up((int64_t)n_rows * heads * 8);
   w.sums = up(w.pieces + 16 + (int64_t)w.max_pieces * sizeof(KeyPiece));
-  w.bytes = w.sums + (int64_t)w.max_slots * kv_heads * kOwn * 2 * dim * 4;
+  w.q_sums = w.sums + (int64_t)w.max_slots * kv_heads * kOwn * 2 * dim * 4;
+  w.splits = shares_of_keys(n_rows, n_k_rows, n_seqs, heads, seen, kShareKeysDq, kManyKeysDq);
+  w.bytes = w.q_sums + (w.splits > 1 ? (int64_t)parts_of(n_rows, n_seqs) * w.splits * heads * kOwn * dim * 4 : 0);
   return w;
 }
 size_t attend_rows_backward_bytes(int n_rows, int n_k_rows, int n_seqs, int heads, int kv_heads, int dim) {
-  return backward_space(n_rows, n_k_rows, n_seqs, heads, kv_heads, dim).bytes;
+  return backward_space(n_rows, n_k_rows, n_seqs, heads, kv_heads, dim, n_k_rows).bytes;
 }
 
 hipError_t launch_attend_rows_backward(const AttendRowsParams &given, uint8_t *workspace, hipStream_t s) {
   AttendRowsParams p = given;
-  const BackwardSpace w = backward_space(p.n_rows, p.n_k_rows, p.n_seqs, p.heads, p.kv_heads, p.dim);
+  const BackwardSpace w = backward_space(p.n_rows, p.n_k_rows, p.n_seqs, p.heads, p.kv_heads, p.dim, seen_of(p));
   p.stats = reinterpret_cast<float *>(workspace);
   p.n_pieces = reinterpret_cast<int32_t *>(workspace + w.pieces);
   p.pieces = reinterpret_cast<KeyPiece *>(workspace + w.pieces + 16);
   p.sums = reinterpret_cast<float *>(workspace + w.sums);
+  p.q_sums = reinterpret_cast<float *>(workspace + w.q_sums);
+  p.splits = w.splits;
   p.max_pieces = w.max_pieces;
   p.shares = shares_of(p.dim);
   p.max_slots = w.max_slots;
   const int parts = parts_of(p.n_rows, p.n_seqs), k_parts = w.max_pieces + 1;
-  with_steps(p.dim, [&](auto ks) { attend_rows_dq_kernel<decltype(ks)::value><<<grid_of(parts, p.heads, kLead), kBlock, 0, s>>>(p, parts); });
+  with_steps(p.dim, [&](auto ks) {
+    constexpr int KS = decltype(ks)::value;
+    if (w.splits > 1) attend_rows_dq_kernel<KS, true><<<grid_of((int64_t)parts * w.splits, p.heads, kLead), kBlock, 0, s>>>(p, parts);
+    else attend_rows_dq_kernel<KS, false><<<grid_of(parts, p.heads, kLead), kBlock, 0, s>>>(p, parts);
+  });
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   with_steps(p.dim, [&](auto ks) { attend_rows_dkv_kernel<decltype(ks)::value><<<grid_of(k_parts, p.kv_heads), kBlock, 0, s>>>(p, k_parts); });
   e = hipGetLastError();
-  if (e != hipSuccess || w.max_slots == 0) return e;
-  join_pieces_kernel<<<grid_of((int64_t)w.max_pieces * (kOwn / kJoinRows), p.kv_heads), kBlock, 0, s>>>(p);
+  if (e != hipSuccess || (w.max_slots == 0 && w.splits == 1)) return e;
+  const int ahead = w.splits > 1 ? (parts - 1) * p.heads * (kOwn / kJoinRows) : 0, behind = w.max_slots > 0 ? w.max_pieces * (kOwn / kJoinRows) : 0;
+  join_pieces_kernel<<<grid_of(behind, p.kv_heads, ahead), kBlock, 0, s>>>(p, ahead);
   return hipGetLastError();
 }
 
