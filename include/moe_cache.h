@@ -446,10 +446,10 @@ int moe_experts_rows_backward(int32_t weight_fmt, int32_t hidden, int32_t inter,
  *   others are left alone.  Few queries of many keys are split over the GPU: the workspace holds what the shares have,
  *   moe_attend_rows_bytes bytes, 16-byte aligned, of this call alone until it is done (0: none is needed, it may be NULL).
  * moe_attend_rows_backward: from dy the gradients of q, k and v, dense, bf16 (rows of no sequence: 0).  y, y_low, lse: as the forward left
- *   them (y_low_dev NULL: y is taken as it is, which makes the error of dq and dk about a tenth larger).  P = exp(z - lse), dv = sum P dy, dz = P (<dy, v> - <dy, y>), dq = softmax_scale sum dz k, dk = softmax_scale sum dz q, sums
- *   over the heads of a group and over all queries in a fixed order.  P and dz are rounded to bf16 for the matrix cores.  Infinities and
- *   NaN in a sequence may make NaN of any of its gradients (of no other sequence's).  y and dy
- *   dense.  The workspace: moe_attend_rows_backward_bytes bytes, 16-byte aligned, of this call alone until it is done. */
+ *   them (y_low_dev NULL: y is taken as it is rounded, and dq and dk are less exact).  P = exp(z - lse), dv = sum P dy, dz = P (<dy, v>
+ *   - <dy, y>), dq = softmax_scale sum dz k, dk = softmax_scale sum dz q, sums over the heads of a group and over all queries in a fixed
+ *   order.  For the matrix cores P and dz are rounded to bf16, dz for dq to two of them.  Infinities and NaN in a sequence may make NaN
+ *   of any of its gradients (of no other sequence's).  y and dy dense.  The workspace: moe_attend_rows_backward_bytes bytes, 16-byte aligned, of this call alone until it is done. */
 int moe_plan_pages(const int32_t *have_dev, const int32_t *more_dev, int32_t n_seqs, int32_t page, const int32_t *free_dev, int32_t n_free,
                    const int32_t *used_dev, int32_t *table_dev, int32_t table_pages, int32_t *offsets_dev, int32_t *slots_dev,
                    int32_t *positions_dev, int32_t n_tokens, int32_t *lengths_dev, int32_t *used_out_dev, void *stream);

@@ -12,17 +12,19 @@
 // wavefronts of a workgroup.
 //
 // P and dZ are rounded to bf16 for the matrix cores.  The error that this makes is as large as that of the results' own rounding
-// (gradients 0.0024 of their size together, 0.0017 for the results' alone); dZ in two parts would cost a third (dQ) and a quarter
-// (dK) of the products more, and is taken in two parts only where queries do not see all keys of a tile: all of a short sequence.  delta
-// is the same for all keys of a query, and with Y as it is rounded it would be the next largest part of the error (0.0027): the
-// forward keeps what the rounding of Y leaves, in bf16.
+// (dK and dV 0.0023 of their size together, 0.0017 for the results' alone).  For dQ dZ is taken in two parts: the errors of one part
+// are added up with keys that have much in common, their share of the query's direction, while the dZ themselves cancel (0.0024 to 0.0027;
+// two parts are a third of the products more, 386 to 403 us of 8192 tokens, all in all).  For dK, where they would not fit into the registers,
+// only where queries do not see all keys of a tile: all of a short sequence.  delta is the same for all keys of
+// a query, and with Y as it is rounded it would be the next largest part of the error: the forward keeps what the rounding of Y leaves,
+// in bf16.
 //
 // Which sequence and which of its rows a workgroup has is worked out from the offsets on the device.  Loads go through buffer
 // resources that end where the sequence ends: what lies beyond arrives as zeros.
 //
-// Measured: 16384 tokens, 32 heads of 128, 8 of k: 2190 us (1.00 PFLOP/s).  With gradients, 8192 tokens in five sequences, 16 heads of 128:
-// 104 + 130 + 175 + 5 us (0.63, 0.75, 0.75 PFLOP/s of the products that each makes); 20001 tokens in nine, 16 heads of 80, 2 of k, window 1000
-// and three first keys: 180 + 205 + 250 + 15.  16384 tokens: the matrix cores work 42 % of the time and the vector units as much again,
+// Measured: 16384 tokens, 32 heads of 128, 8 of k: 2080 us (1.06 PFLOP/s).  With gradients, 8192 tokens in five sequences, 16 heads of 128:
+// 104 + 145 + 175 + 5 us (0.63, 0.90, 0.75 PFLOP/s of the products that each makes); 20001 tokens in nine, 16 heads of 80, 2 of k, window 1000
+// and three first keys: 180 + 225 + 250 + 16.  16384 tokens: the matrix cores work 42 % of the time and the vector units as much again,
 // with two wavefronts a SIMD (what the registers allow).  Tried for the forward, of 2115 us: the same without the two steps 2120; matrix
 // instructions at a higher wave priority the same; 64 queries a wavefront and one of them a SIMD, half the reads of LDS, 2490.
 #include <algorithm>
@@ -883,6 +885,22 @@ __device__ __forceinline__ void add_columns(const typename T::Reader &at, uint32
   __builtin_amdgcn_sched_barrier(0);
 }
 
+// ... and with g
+template <typename T, int AHEAD>
+__device__ __forceinline__ void add_columns_twice(const typename T::Reader &at, uint32_t in, const i32x4 (&f)[2], const i32x4 (&g)[2], f32x16 (&o)[T::DS]) {
+  i32x4 c[AHEAD + 1];
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) c[i] = T::columns(at, in, i / T::DS * 16, i % T::DS);
+#pragma unroll
+  for (int i = 0; i < 2 * T::DS; ++i) {
+    __builtin_amdgcn_sched_barrier(0);
+    if (i + AHEAD < 2 * T::DS) c[(i + AHEAD) % (AHEAD + 1)] = T::columns(at, in, (i + AHEAD) / T::DS * 16, (i + AHEAD) % T::DS);
+    o[i % T::DS] = mma(c[i % (AHEAD + 1)], f[i / T::DS], o[i % T::DS]);
+    o[i % T::DS] = mma(c[i % (AHEAD + 1)], g[i / T::DS], o[i % T::DS]);
+  }
+  __builtin_amdgcn_sched_barrier(0);
+}
+
 // SPLIT: few queries, many keys, as in the forward; the sums of a share's keys go to the workspace.  (With all else: 2000 tokens, 8 heads of 128
 // for 2, 133 us, without shares 161; 1000 of 8 heads 80, 94; 400 54, 59; 3529 behind up to 12135, 2 heads: 244, 466.)
 template <int KS, bool SPLIT>
@@ -968,22 +986,12 @@ __global__ __launch_bounds__(kBlock, 2) void attend_rows_dq_kernel(const AttendR
       two_products<T, 2>(at, q, dy, z, dp);
 #pragma unroll
       for (int i = 0; i < 16; ++i) z[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i], scale, -lse)) * dp[i];
-      bool again = !see_all(p, p0, p1, key0, key0 + 31);
-      i32x4 low[2];
-      if (again) {
+      if (!see_all(p, p0, p1, key0, key0 + 31)) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) z[i] = sees(p, pos, key0 + i / 4 * 8 + (lane >> 5) * 4 + i % 4) ? z[i] : 0.f;
-        low[0] = left_over(z, 0);
-        low[1] = left_over(z, 1);
       }
-      i32x4 f[2] = {summed(z, 0), summed(z, 1)};
-#pragma unroll 1
-      for (;; again = false) {  // (one product in the code: two keep the sums in twice the registers)
-        add_columns<T, 3>(at, 0, f, o);
-        if (!again) break;
-        f[0] = low[0];
-        f[1] = low[1];
-      }
+      const i32x4 f[2] = {summed(z, 0), summed(z, 1)}, low[2] = {left_over(z, 0), left_over(z, 1)};
+      add_columns_twice<T, 3>(at, 0, f, low, o);
     }
   }
   if (SPLIT) {
