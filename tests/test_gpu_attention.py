@@ -129,6 +129,7 @@ ROWS = [
     ([3] * 70 + [200], None, 2, 1, 32, 0, 0),            # more sequences than lanes
     ([2] * 300 + [900, 5, 130], None, 16, 1, 64, 0, 0),  # ... and than threads
     ([i % 4 for i in range(3000)] + [400], None, 2, 1, 64, 0, 0),
+    ([2] * 80 + [0, 70, 1], None, 1, 1, 64, 0, 0),
     ([0] * 70 + [130, 0, 257] + [0] * 5000, None, 2, 2, 72, 40, 2),
     ([2500, 700], None, 16, 1, 128, 0, 0),               # few heads of k: their queries are cut into pieces
     ([2500, 0, 701], None, 12, 2, 80, 200, 5),
@@ -670,15 +671,16 @@ def test_a_captured_step_is_replayed(lib):
             close(out[i], want[0][-1], want[1][-1], (t, i))
 
 
-def test_captured_gradients_beside_eager_ones(lib):
+@pytest.mark.parametrize("each,keys,heads", [([300, 1000], [300, 1000], 16), ([30, 100], [1700, 2000], 2)])
+def test_captured_gradients_beside_eager_ones(lib, each, keys, heads):
     """attend_rows and its backward in a graph, replayed on other inputs, with eager calls of the same kind in between."""
     g = gen(23)
-    offsets = ints([0, 300, 1300])
-    ts = [normal(g, 1300, h, 64, dtype=BF16) for h in (16, 1, 1, 16)]
+    offsets, k_offsets = ints(starts(each)), ints(starts(keys))
+    ts = [normal(g, n, h, 64, dtype=BF16) for n, h in ((sum(each), heads), (sum(keys), 1), (sum(keys), 1), (sum(each), heads))]
 
     def both(q, k, v, dy):
-        y, kept = lib.attend_rows(q, k, v, offsets, keep=True)
-        return (y, *lib.attend_rows_backward(q, k, v, offsets, y, kept, dy))
+        y, kept = lib.attend_rows(q, k, v, offsets, k_offsets=k_offsets, keep=True)
+        return (y, *lib.attend_rows_backward(q, k, v, offsets, y, kept, dy, k_offsets=k_offsets))
 
     both(*ts)
     graph = torch.cuda.CUDAGraph()
