@@ -31,6 +31,7 @@
 #include <type_traits>
 
 #include "attend.h"
+#include "row_range.h"
 #include "rows.h"
 #include "tiles.h"
 
@@ -57,13 +58,8 @@ struct Sequence {
   int q0, nq, k0, nk, ahead;
 };
 __device__ __forceinline__ Sequence sequence_of(const AttendRowsParams &p, int s) {
-  Sequence r;
-  r.q0 = min(max(p.offsets[s], 0), p.n_rows);
-  r.nq = max(min(p.offsets[s + 1], p.n_rows) - r.q0, 0);
-  r.k0 = min(max(p.k_offsets[s], 0), p.n_k_rows);
-  r.nk = max(min(p.k_offsets[s + 1], p.n_k_rows) - r.k0, 0);
-  r.ahead = r.nk - r.nq;
-  return r;
+  const RowRange q = row_range(p.offsets[s], p.offsets[s + 1], p.n_rows), k = row_range(p.k_offsets[s], p.k_offsets[s + 1], p.n_k_rows);
+  return {q.first, q.count, k.first, k.count, k.count - q.count};
 }
 // Part `want` of the sequences' rows in parts of OWN, later parts of the sequences first: they have more keys, and a workgroup with
 // much to do must not be the last to begin.  No such part: sequence -1, and how far behind the last one it is (-1: it is not).
@@ -91,7 +87,7 @@ __device__ __forceinline__ Part part_of(const AttendRowsParams &p, int want) {
   // more than there are up to the next sequence's first; the others stay idle.  The sequence is found 64 at a time.  (1000 sequences of
   // 10000 rows in all, 16 heads of 128 over 8: 168 us, 244 with the sequences' parts added up 64
   // at a time; with the gradients 581, 736.)
-  const auto first_of = [&](int s) { return min(max(p.offsets[s], 0), p.n_rows) / OWN + s; };
+  const auto first_of = [&](int s) { return row_within(p.offsets[s], p.n_rows) / OWN + s; };
   int from = 0, to = p.n_seqs;  // the last one whose numbers begin at `want` or ahead of it is among these
   while (from < to) {
     const int step = (to - from + 63) / 64, s = from + (lane + 1) * step;
@@ -109,7 +105,7 @@ __device__ __forceinline__ Part part_of(const AttendRowsParams &p, int want) {
 }
 // zeros for the rows of no sequence, shared by `step` workgroups
 __device__ __forceinline__ void clear_rows(const int32_t *offsets, int n_seqs, int n_rows, uint16_t *to, int head, int heads, int dim, int at, int step) {
-  const int first = min(max(offsets[0], 0), n_rows), last = min(max(offsets[n_seqs], first), n_rows);
+  const int first = row_within(offsets[0], n_rows), last = max(row_within(offsets[n_seqs], n_rows), first);
   const int64_t units = (int64_t)(first + n_rows - last) * (dim / 8);
   for (int64_t u = (int64_t)at * kBlock + threadIdx.x; u < units; u += (int64_t)step * kBlock) {
     int64_t r = u / (dim / 8);

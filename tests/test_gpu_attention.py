@@ -273,6 +273,29 @@ def test_offsets_that_do_not_fit(lib):
         torch.cuda.synchronize()
 
 
+def test_ends_of_sequences_far_below_zero(lib):
+    """An end so far ahead of its start that their difference passes 32 bits is of a sequence without rows: nothing out of range is read,
+    and its neighbours have their rows."""
+    least = -(1 << 31)
+    g = gen(4)
+    q, k, v, dy = (normal(g, 200, h, 64, dtype=BF16) for h in (2, 1, 1, 2))
+    for bad in ([150, least, 20], [200, least + 1, -5], [1, least] + [0] * 200, [199, least] * 100, [least, least, 150]):
+        for of in (dict(), dict(k_offsets=ints([0] + [200] * (len(bad) - 1)))):
+            y, kept = lib.attend_rows(q, k, v, ints(bad), keep=True, **of)
+            lib.attend_rows_backward(q, k, v, ints(bad), torch.zeros_like(y), lib.KeptAttention(torch.zeros_like(kept.lse), None), dy, **of)
+            torch.cuda.synchronize()
+    # keys that end far below zero: their queries see none, the next sequence has its own
+    want = reference(q[60:], k[:140], v[:140], [140], [140], 0, 0, 0.125, dy[60:])
+    kw = dict(k_offsets=ints([150, least, 140]))
+    offsets = ints([0, 60, 200])
+    y, kept = lib.attend_rows(q, k, v, offsets, keep=True, **kw)
+    assert not y[:60].any()
+    close(y[60:], *want["y"], "y")
+    dq = lib.attend_rows_backward(q, k, v, offsets, y, kept, dy, **kw)[0]
+    assert not dq[:60].any()
+    close(dq[60:], *want["dq"], "dq")
+
+
 @pytest.mark.parametrize("layout", ["heads first", "one projection", "wide", "one head"])
 def test_layouts(lib, layout):
     g = gen(11)
