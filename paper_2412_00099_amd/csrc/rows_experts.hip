@@ -32,6 +32,7 @@
 //
 // Which expert and which of its rows a tile has is worked out from `offsets` on the device.  All loads go through buffer
 // resources that end where the expert's rows or records end: what lies beyond arrives as zeros.
+#include "row_range.h"
 #include "rows.h"
 #include "tiles.h"
 
@@ -63,8 +64,8 @@ struct Tile {
   int expert;  // -1: no tile
   int row0, rows, col;
 };
-__device__ __forceinline__ int first_row(const ExpertRowsParams &p, int e) { return min(max(p.offsets[e], 0), p.n_rows); }
-__device__ __forceinline__ int row_count(const ExpertRowsParams &p, int e) { return max(min(p.offsets[e + 1], p.n_rows) - first_row(p, e), 0); }
+__device__ __forceinline__ int first_row(const ExpertRowsParams &p, int e) { return row_within(p.offsets[e], p.n_rows); }
+__device__ __forceinline__ int row_count(const ExpertRowsParams &p, int e) { return row_range(p.offsets[e], p.offsets[e + 1], p.n_rows).count; }
 
 // What an expert's tiles are.  Its rows are cut into the fewest parts of at most MOST, all but the last of the same size, which is
 // whole blocks: they are computed whole.  cost: of a tile, in rows; that the weights have to come in costs about as much as 128 rows
