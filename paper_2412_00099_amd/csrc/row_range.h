@@ -7,14 +7,17 @@
 namespace moe {
 
 // of rows 0 .. rows - 1
-constexpr int32_t row_within(int32_t at, int32_t rows) { return at < 0 ? 0 : at < rows ? at : rows; }
+constexpr int32_t row_within(int32_t at, int32_t rows) {
+  const int32_t below = at < rows ? at : rows;
+  return below < 0 ? 0 : below;
+}
 struct RowRange {
   int32_t first, count;
 };
 // Both ends are brought into the range ahead of the difference, which then cannot pass 32 bits.  An end ahead of the first row: none.
 constexpr RowRange row_range(int32_t from, int32_t to, int32_t rows) {
-  const int32_t first = row_within(from, rows), end = row_within(to, rows);
-  return {first, end > first ? end - first : 0};
+  const int32_t first = row_within(from, rows), count = row_within(to, rows) - first;
+  return {first, count < 0 ? 0 : count};
 }
 
 }  // namespace moe
