@@ -440,6 +440,7 @@ struct Queries {
   // z: the scores of 32 keys that all see, `most` the largest.  next: those of the 32 keys at `keys`.
   __device__ __forceinline__ void step(f32x16 &z, f32x16 &next, const typename T::Reader &keys, const typename T::Reader &values) {
     rebase(8.f);
+    const float base = top == -INFINITY ? 0.f : top;  // (all scores so far -infinity: their exponentials are 0)
     constexpr int EACH = (16 + T::KS - 1) / T::KS, PVS = 2 * T::DS, AHEAD = 3;
     i32x4 a[AHEAD + 1], c[AHEAD + 1];
 #pragma unroll
@@ -453,7 +454,7 @@ struct Queries {
       next = mma(a[i % (AHEAD + 1)], q[i], next);
 #pragma unroll
       for (int e = i * EACH; e < (i + 1) * EACH && e < 16; ++e) {
-        z[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[e], scale, -top));
+        z[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[e], scale, -base));
         if (KEEP) sum += z[e];
       }
     }

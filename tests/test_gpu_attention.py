@@ -237,6 +237,30 @@ def test_shares_of_keys_that_are_not_seen(lib, what):
     assert float(torch.where(clean, over, -1.0).max()) <= 0
 
 
+@pytest.mark.parametrize("dim", [64, 80, 128])
+@pytest.mark.parametrize("each,keys,heads", [
+    ([400], None, 2), ([400], None, 48),  # the keys divided among wavefronts; whole tiles by a workgroup
+    ([70], [4000], 2)])                   # shares of the keys
+@pytest.mark.parametrize("first,n", [(0, 32), (0, 64), (0, 130), (37, 64), (128, 64), (0, 300)])
+def test_scores_of_minus_infinity(lib, dim, each, keys, heads, first, n):
+    """Keys that score -infinity with every query weigh nothing, also where a query sees a whole tile of them ahead of any other."""
+    g = gen(dim + n)
+    nk = sum(keys or each)
+    q = normal(g, sum(each), heads, dim, std=2.0, dtype=BF16)
+    k, v = (normal(g, nk, 1, dim, dtype=BF16) for _ in range(2))
+    q[:, :, 3] = 1.0
+    ok = visible(sum(each), nk, 0, 0)
+    ok[:, first:first + n] = False
+    kept = k.clone()
+    k[first:first + n, :, 3] = -math.inf
+    y, keep = lib.attend_rows(q, k, v, ints(starts(each)), k_offsets=ints(starts(keys or each)), keep=True)
+    some = ok.any(1)
+    for h in range(0, heads, max(1, heads // 3)):
+        want, bound = one_head(q[:, h].double(), kept[:, 0].double(), v[:, 0].double(), ok, dim ** -0.5)["y"]
+        close(y[some, h], want[some], bound[some], (h, "y"))
+    assert bool(torch.isfinite(keep.lse[:, some]).all())
+
+
 def test_gradients_of_other_sequences(lib):
     """An infinity or NaN stays in its sequence's gradients."""
     g = gen(7)
