@@ -619,7 +619,8 @@ __global__ __launch_bounds__(kBlock) void join_rows_kernel(const AttendRowsParam
       x[1] *= shrink;
 #pragma unroll
       for (int i = 0; i < AT_ONCE; ++i) {
-        if (of[i][0] == -INFINITY) continue;  // (nothing of it is seen)
+        // (Nothing of it is seen, or all scores are -infinity.  If they are NaN the largest is -infinity, too, but the sum is NaN.)
+        if (of[i][0] == -INFINITY && of[i][1] == 0.f) continue;
         const float weight = __builtin_amdgcn_exp2f(of[i][0] - base);
         total += weight * of[i][1];
         sum += weight * of[i][2];

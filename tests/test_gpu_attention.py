@@ -237,6 +237,50 @@ def test_shares_of_keys_that_are_not_seen(lib, what):
     assert float(torch.where(clean, over, -1.0).max()) <= 0
 
 
+def test_shares_of_keys_with_nan(lib):
+    """A NaN that a query has or sees is in its y and lse, whichever share of the keys it is in, as it is without shares; the other
+    queries and heads have their values."""
+    g = gen(22)
+    H, KV, dim, nq, nk = 4, 2, 64, 100, 3900
+    q = normal(g, nq, H, dim, std=2.0, dtype=BF16)
+    k, v = normal(g, nk, KV, dim, dtype=BF16), normal(g, nk, KV, dim, dtype=BF16)
+    assert lib.moe_attend_rows_bytes(nq, nk, 1, H, KV, dim) > 0
+    offsets, k_offsets = ints([0, nq]), ints([0, nk])
+
+    def check(q, k, v, bad):
+        """bad [nq, H]: what has to be NaN"""
+        y, kept = lib.attend_rows(q, k, v, offsets, k_offsets=k_offsets, keep=True)
+        assert bool(y.isnan().all(2)[bad].all()) and bool(kept.lse.isnan().t()[bad].all())
+        over = (y.double() - want[0]).abs() - want[1] * (1 + 2 * U)
+        assert float(over[~bad].max()) <= 0 if bool((~bad).any()) else True
+        assert bool(torch.isfinite(kept.lse.t()[~bad]).all())
+        # without shares: the same sequence among empty ones, so that there are few keys for each
+        empty = [0] * 9
+        y, kept = lib.attend_rows(q, k, v, ints(empty + [0, nq]), k_offsets=ints(empty + [0, nk]), keep=True)
+        assert lib.moe_attend_rows_bytes(nq, nk, 10, H, KV, dim) == 0
+        assert bool(y.isnan().all(2)[bad].all()) and bool(kept.lse.isnan().t()[bad].all()) and bool(torch.isfinite(kept.lse.t()[~bad]).all())
+
+    want = reference(q, k, v, [nq], [nk], 0, 0, dim ** -0.5)["y"]
+    none = torch.zeros(nq, H, dtype=torch.bool, device=DEV)
+    check(q, k, v, none)
+    for rows, value in (((0,), math.nan), ((17, 63, 99), math.nan), (range(nq), math.nan)):  # in queries: in one value, in all of them
+        for dims in (slice(5, 6), slice(None)):
+            bad, x = none.clone(), q.clone()
+            for r in rows:
+                bad[r, 1] = True
+                x[r, 1, dims] = value
+            check(x, k, v, bad)
+    bad, x = none.clone(), k.clone()
+    bad[:, 2:], x[:, 1, 7] = True, math.nan  # in all keys of a head
+    check(q, x, v, bad)
+    for tile in range(0, nk // 64 - 6):  # in all keys of tiles, of every share's among them; all queries see them
+        for n in (1, 4, 5):
+            x = k.clone()
+            x[64 * tile:64 * (tile + n), 1, 7] = math.nan
+            y, kept = lib.attend_rows(q, x, v, offsets, k_offsets=k_offsets, keep=True)
+            assert bool(y[:, 2:].isnan().all()) and bool(kept.lse[2:].isnan().all()) and bool(torch.isfinite(y[:, :2]).all()), (tile, n)
+
+
 @pytest.mark.parametrize("dim", [64, 80, 128])
 @pytest.mark.parametrize("each,keys,heads", [
     ([400], None, 2), ([400], None, 48),  # the keys divided among wavefronts; whole tiles by a workgroup
