@@ -6,7 +6,7 @@
 // S^T = K Q^T (rows: keys), O^T = V^T P^T (rows: dims), so that a lane keeps one head throughout, its maximum and its share of the sum
 // in registers, and P^T goes from the first product into the second without changing lanes: which keys stand for which summed index
 // of the second product is free, as long as V^T is read in the same order.  P is split into two parts of bf16 (what is left of a
-// value is 2^-17 of it): the second product costs nothing here.  8-bit codes are widened to bf16, which holds them exactly; their
+// value is 2^-16 of it at most): the second product costs nothing here.  8-bit codes are widened to bf16, which holds them exactly; their
 // scales go to the scores and to P.
 //
 // The work of all sequences is a line of tiles of 32 keys (sequence, group of heads, tile), cut into equal shares, one for each
@@ -192,6 +192,14 @@ struct Attend {
     }
     return v;
   }
+  // Two exponentials in two parts each.  Values of bf16 may be infinite, and a part that is 0 or of the other sign would make NaN of
+  // them: the first part is cut off rather than rounded, and the second one is of 1 + 2^-22 of the exponential, so that it is above 0
+  // where the exponential is (above 2^-104, to be exact).  8-bit values are finite; there the first part is rounded, which leaves half as much.
+  static __device__ __forceinline__ i32x2 parts_of_p(float a, float b) {
+    constexpr float ABOVE = INT8 ? 1.f : 1.f + 0x1p-22f;
+    const uint32_t hi = INT8 ? pack_bf16(a, b) : __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302);
+    return i32x2{(int)hi, (int)pack_bf16(__builtin_fmaf(a, ABOVE, -bf16_lo(hi)), __builtin_fmaf(b, ABOVE, -bf16_hi(hi)))};
+  }
 
   __device__ __forceinline__ void run(int worker, uint8_t *mine) {
     lds = mine;
@@ -339,8 +347,9 @@ struct Attend {
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        hi[i] = (int)pack_bf16(w[2 * i], w[2 * i + 1]);
-        lo[i] = (int)pack_bf16(w[2 * i] - bf16_lo(hi[i]), w[2 * i + 1] - bf16_hi(hi[i]));
+        const i32x2 parts = parts_of_p(w[2 * i], w[2 * i + 1]);
+        hi[i] = parts[0];
+        lo[i] = parts[1];
       }
 #pragma unroll
       for (int d = 0; d < DS; ++d) o[d] *= shrink;

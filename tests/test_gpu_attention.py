@@ -652,6 +652,51 @@ def test_pages(lib, case, cache):
     assert torch.equal(got, again)
 
 
+@pytest.mark.parametrize("lengths,heads,kv,dim,page,window,sinks", [
+    ([1, 2, 40, 700], 4, 2, 128, 16, 0, 0),                   # a workgroup for each
+    ([5000, 1, 3, 900, 0, 64], 8, 2, 64, 32, 0, 0),           # in shares
+    ([5000, 1, 3, 900, 0, 64], 8, 2, 128, 16, 0, 0),
+    ([3000, 1, 500] * 40, 6, 2, 72, 16, 0, 0),                # ... joined by wavefronts
+    ([1500, 40, 700], 8, 2, 128, 16, 100, 4)])
+def test_infinities_in_pages(lib, lengths, heads, kv, dim, page, window, sinks):
+    """An infinity or NaN in a value that is seen is in y's dim of the heads that read it, as it is over rows; in a key, NaN."""
+    g = gen(dim + len(lengths))
+    values, pages, _, table = paged(g, lengths, kv, dim, page, BF16)
+    q = normal(g, len(lengths), heads, dim, std=2.0, dtype=BF16)
+    want, bound = paged_reference(q, values, window, sinks, dim ** -0.5)
+    expect = want.clone()
+    per = heads // kv
+
+    def put(cache, i, pos, head, d, value):
+        cache[int(table[i, pos // page]), head, pos % page, d] = value
+
+    for i, n in enumerate(lengths):
+        if n == 0:
+            continue
+        seen = visible(1, n, window, sinks)[0].nonzero()[:, 0].tolist()
+        for pos, d, value in ((n - 1, 0, math.inf), (seen[0], 1, -math.inf), (seen[len(seen) // 2], 2, math.nan), (n - 1, 3, math.inf), (seen[0], 3, math.inf),
+                              (seen[len(seen) // 3], 4, -math.inf)):
+            put(pages[1], i, pos, 0, d, value)
+            expect[i, :per, d] = value
+        if len(seen) > 1:  # both infinities in one dim
+            put(pages[1], i, seen[0], 0, 5, math.inf)
+            put(pages[1], i, n - 1, 0, 5, -math.inf)
+            expect[i, :per, 5] = math.nan
+        if len(seen) < n:  # not seen
+            hidden = sorted(set(range(n)) - set(seen))
+            put(pages[1], i, hidden[-1], 0, 6, math.inf)
+            put(pages[0], i, hidden[len(hidden) // 2], 0, 6, math.nan)
+        if i % 2:
+            put(pages[0], i, seen[len(seen) // 4], 1, 7, math.nan)
+            expect[i, per:2 * per] = math.nan
+    y = lib.attend_pages(q, *pages, table, ints(lengths), window=window, sinks=sinks).double()
+    assert torch.equal(y.isnan(), expect.isnan())
+    odd = expect.isinf()
+    assert torch.equal(y.isinf(), odd) and torch.equal(y[odd], expect[odd])
+    fine = torch.isfinite(expect)
+    close(y[fine], want[fine], bound[fine], "y")
+
+
 def test_pages_that_are_not_there(lib):
     """Pages of the table that are none hide their tokens; a length beyond the table sees what the table has; a window's earlier pages may have been given away."""
     g = gen(5)
