@@ -11,7 +11,7 @@ namespace {
 
 constexpr int64_t kMaxRows = MOE_ROWS_LIMIT;
 constexpr int64_t kMaxStride = 1 << 23;  // elements: a tile of rows stays within 32 bits
-constexpr int32_t kFar = 1 << 30;        // windows and sinks from here on are all the same
+constexpr int32_t kFar = 1 << 30;        // of fewer rows than kMaxRows: windows and sinks from here on are all the same
 
 bool off(const void *p, int by) { return reinterpret_cast<uintptr_t>(p) % by != 0; }
 
@@ -180,8 +180,8 @@ int moe_attend_pages(const void *q, int64_t q_stride, int64_t q_head_stride, con
   p.n_seqs = n_seqs;
   p.table_pages = table_pages;
   p.heads = n_heads;
-  p.window = std::min(window, kFar);
-  p.sinks = window > 0 ? std::min(sinks, kFar) : 0;
+  p.window = window;  // (a table may hold a page many times: 2^31 - 1 tokens are possible)
+  p.sinks = window > 0 ? sinks : 0;
   HIP_TRY(launch_attend_pages(p, cache_fmt, static_cast<hipStream_t>(stream)));
   return MOE_OK;
 }

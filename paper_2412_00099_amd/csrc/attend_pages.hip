@@ -65,7 +65,7 @@ struct Seen {
 __device__ __forceinline__ Seen seen_of(const AttendPagesParams &p, int length) {
   Seen s;
   length = max(length, 0);
-  s.end = (int)min(min((int64_t)length, (int64_t)p.table_pages << p.c.page_bits), (int64_t)INT32_MAX - 2 * kTile);
+  s.end = (int)min((int64_t)length, (int64_t)p.table_pages << p.c.page_bits);
   s.lo = p.window > 0 ? max(length - p.window, 0) : 0;
   s.first = s.lo / kTile;
   const int last = (int)(((int64_t)s.end + kTile - 1) / kTile);

@@ -722,6 +722,24 @@ def test_pages_that_are_not_there(lib):
     assert not y[1:].any()
 
 
+@pytest.mark.parametrize("cache", [BF16, I8])
+@pytest.mark.parametrize("window,sinks", [(0, 0), ((1 << 31) - 1, 0), ((1 << 30) + 5000, 0), ((1 << 30) + 5000, 700), (50, (1 << 30) + 100), (300, 5), (1 << 30, 1 << 30)])
+def test_as_many_tokens_as_lengths_count(lib, cache, window, sinks):
+    """2^31 - 1 of them, of which few pages are there: positions, windows and first keys that pass 2^30, and the last token of all."""
+    page, n, dim = 1024, (1 << 31) - 1, 64
+    entries = [0, 1, (1 << 20) - 5, 1 << 20, (1 << 21) - 2, (1 << 21) - 1]
+    g = gen(41)
+    values, pages, scales, few = paged(g, [len(entries) * page - 1], 1, dim, page, cache)
+    table = torch.full((1, 1 << 21), -1, dtype=I32, device=DEV)
+    table[0, entries] = few[0, :len(entries)]
+    q = normal(g, 1, 2, dim, std=2.0, dtype=BF16)
+    pos = (torch.tensor(entries, device=DEV)[:, None] * page + torch.arange(page, device=DEV)).reshape(-1)[:-1]
+    assert int(pos[-1]) == n - 1
+    seen = torch.ones_like(pos, dtype=torch.bool) if window == 0 else (pos > n - 1 - window) | (pos < sinks)
+    want = paged_reference(q, [[x[seen] for x in values[0]]], 0, 0, dim ** -0.5)
+    close(lib.attend_pages(q, *pages, table, ints([n]), *scales, window=window, sinks=sinks), *want, "y")
+
+
 # ---- how the calls are made --------------------------------------------------------------------------------
 def serve_setup(lib, cache=BF16, seed=17, **kw):
     """Three requests: their prompts by attend_rows, stored; then tokens one by one."""
