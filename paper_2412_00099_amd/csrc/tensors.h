@@ -3,6 +3,7 @@
 #pragma once
 
 #include <ATen/ATen.h>
+#include <c10/core/AutogradState.h>
 #include <c10/core/GradMode.h>
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
@@ -79,11 +80,16 @@ inline bool within(int64_t rows, int64_t hidden) { return rows < MOE_ROWS_LIMIT 
 
 inline bool differentiable(const Tensor &t) { return t.requires_grad(); }
 inline bool differentiable(const Maybe &t) { return t && t->requires_grad(); }
-// The results have no history for automatic differentiation: a caller who would lose a gradient that way is told.
+inline bool has_tangent(const Tensor &t) { return t._fw_grad(0).defined(); }  // (there is one level)
+inline bool has_tangent(const Maybe &t) { return t && has_tangent(*t); }
+// The results have no history for automatic differentiation: a caller who would lose a gradient that way, or a tangent of the
+// forward mode (which torch.no_grad() does not switch off), is told.
 template <typename... T>
 inline void no_history(const T &...t) {
   if (c10::GradMode::is_enabled() && (differentiable(t) || ...))
     wrong("an input requires a gradient, which this call does not record: call it under torch.no_grad(), or in a torch.autograd.Function with the backward calls");
+  if (c10::AutogradState::get_tls_state().get_fw_grad_mode() && (has_tangent(t) || ...))
+    wrong("an input has a tangent of forward-mode differentiation, which this call does not propagate: call it on the primal, or in a torch.autograd.Function with a jvp");
 }
 
 // The GPU that all tensors are on, current for the call, and its current stream
