@@ -155,3 +155,84 @@ def test_caches_of_inference_mode_are_not_written_outside_it(B):
         moe.store_pages(k, k, n, pages, pages)
     with pytest.raises(ValueError, match="inference"):
         moe.plan_pages(n, n, table, n, 16, 5)
+
+
+def test_each_wrong_shape_or_type_is_told_by_its_own_check(B):
+    """These checks come ahead of the one for a GPU, so that each call names what is wrong with it."""
+    import paper_2412_00099_amd as moe
+
+    bf16, i32, i8 = torch.bfloat16, torch.int32, torch.int8
+    q, k = torch.zeros(5, 4, 64, dtype=bf16), torch.zeros(5, 2, 64, dtype=bf16)
+    at, lse = torch.zeros(2, dtype=i32), torch.zeros(4, 5)
+    pages, table, n = torch.zeros(3, 2, 16, 64, dtype=bf16), torch.zeros(5, 2, dtype=i32), torch.zeros(5, dtype=i32)
+    codes, scale = torch.zeros(3, 2, 16, 64, dtype=i8), torch.zeros(3, 2, 16)
+    kept = moe.KeptAttention
+    apart = torch.zeros(6, 2, 16, 64, dtype=bf16)[::2]
+    calls = [
+        (lambda: moe.attend_rows(q, k, k, at), "on a GPU"),
+        (lambda: moe.attend_rows(q.float(), k, k, at), "q: Float is not bfloat16"),
+        (lambda: moe.attend_rows(q, k.half(), k, at), "k: Half is not bfloat16"),
+        (lambda: moe.attend_rows(q, k, k.to(i8), at), "v: Char is not bfloat16"),
+        (lambda: moe.attend_rows(q[0], k, k, at), r"q has to be \[tokens, heads, dim\]"),
+        (lambda: moe.attend_rows(q, k[:, :, ::2], k, at), r"k has to be \[tokens, heads, dim\] with dense heads"),
+        (lambda: moe.attend_rows(q.transpose(1, 2), k, k, at), r"q has to be \[tokens, heads, dim\] with dense heads"),
+        (lambda: moe.attend_rows(q, k, k[:4], at), "k and v have to have the same shape"),
+        (lambda: moe.attend_rows(q, k[:, :1], k, at), "k and v have to have the same shape"),
+        (lambda: moe.attend_rows(q, k[..., :32], k[..., :32], at), "and q their dim"),
+        (lambda: moe.attend_rows(q, k[:3], k[:3], at), "without k_offsets"),
+        (lambda: moe.attend_rows(q, k, k, at.long()), "offsets has to be contiguous"),
+        (lambda: moe.attend_rows(q, k, k, torch.zeros(4, dtype=i32)[::2]), "offsets has to be contiguous"),
+        (lambda: moe.attend_rows(q, k, k, torch.zeros(2, 2, dtype=i32)), "offsets has to be"),
+        (lambda: moe.attend_rows(q, k, k, at[:0]), "offsets has to be"),
+        (lambda: moe.attend_rows(q, k, k, at, k_offsets=at[:1]), "k_offsets has to be contiguous"),
+        (lambda: moe.attend_rows(q, k, k, at, k_offsets=at.float()), "k_offsets has to be contiguous"),
+        (lambda: moe.attend_rows_backward(q, k, k, at, q, kept(lse, q), q), "on a GPU"),
+        (lambda: moe.attend_rows_backward(q, k, k, at, q, kept(lse[:, :4], q), q), "kept.lse has to be contiguous"),
+        (lambda: moe.attend_rows_backward(q, k, k, at, q, kept(lse.double(), q), q), "kept.lse has to be contiguous"),
+        (lambda: moe.attend_rows_backward(q, k, k, at, q, kept(lse, q[:4]), q), "kept.low has to be contiguous"),
+        (lambda: moe.attend_rows_backward(q, k, k, at, q, kept(lse, q.float()), q), "kept.low has to be contiguous"),
+        (lambda: moe.attend_rows_backward(q, k, k, at, q.float(), kept(lse, q), q), "y has to be contiguous"),
+        (lambda: moe.attend_rows_backward(q, k, k, at, q[:, :2], kept(lse, q), q), "y has to be contiguous"),
+        (lambda: moe.attend_rows_backward(q, k, k, at, q, kept(lse, None), q.transpose(0, 1)), "dy has to be contiguous"),
+        (lambda: moe.attend_rows_backward(q, k, k, at, q, kept(lse, None), q[:4]), "dy has to be contiguous"),
+        (lambda: moe.attend_pages(q, pages, pages, table, n), "on a GPU"),
+        (lambda: moe.attend_pages(q, apart, apart, table, n), "on a GPU"),
+        (lambda: moe.attend_pages(q.float(), pages, pages, table, n), "q: Float is not bfloat16"),
+        (lambda: moe.attend_pages(q, pages, pages[:2], table, n), "k_pages and v_pages have to be"),
+        (lambda: moe.attend_pages(q, pages, codes, table, n), "of one type"),
+        (lambda: moe.attend_pages(q, pages[0], pages[0], table, n), "k_pages and v_pages have to be"),
+        (lambda: moe.attend_pages(q, pages.float(), pages.float(), table, n), "neither bfloat16 nor int8"),
+        (lambda: moe.attend_pages(q, pages.transpose(1, 2), pages.transpose(1, 2), table, n), "have to be dense"),
+        (lambda: moe.attend_pages(q, pages, apart, table, n), "equally far apart"),
+        (lambda: moe.attend_pages(q[..., :32], pages, pages, table, n), "q has another dim"),
+        (lambda: moe.attend_pages(q, pages, pages, table[0], n), r"table has to be \[sequences, pages\]"),
+        (lambda: moe.attend_pages(q, pages, pages, table[:4], n), "table has to be contiguous"),
+        (lambda: moe.attend_pages(q, pages, pages, table[:, :1], n), "table has to be contiguous"),
+        (lambda: moe.attend_pages(q, pages, pages, table.long(), n), "table has to be contiguous"),
+        (lambda: moe.attend_pages(q, pages, pages, table, n[:4]), "lengths has to be contiguous"),
+        (lambda: moe.attend_pages(q, pages, pages, table, n.long()), "lengths has to be contiguous"),
+        (lambda: moe.attend_pages(q, codes, codes, table, n, scale[..., :8], scale), "k_scale has to be contiguous"),
+        (lambda: moe.attend_pages(q, codes, codes, table, n, scale, scale[:2]), "v_scale has to be contiguous"),
+        (lambda: moe.attend_pages(q, codes, codes, table, n, scale, scale.double()), "v_scale has to be contiguous"),
+        (lambda: moe.store_pages(k, k, n, pages, pages), "on a GPU"),
+        (lambda: moe.store_pages(k.half(), k.half(), n, pages, pages), "k: Half is neither"),
+        (lambda: moe.store_pages(k, k.float(), n, pages, pages), "v has to have the shape and type of k"),
+        (lambda: moe.store_pages(k, k[:4], n, pages, pages), "v has to have the shape and type of k"),
+        (lambda: moe.store_pages(q, q, n, pages, pages), "other heads than k_pages"),
+        (lambda: moe.store_pages(k[..., :32], k[..., :32], n, pages, pages), "other heads than k_pages"),
+        (lambda: moe.store_pages(k, k, n[:4], pages, pages), "slots has to be contiguous"),
+        (lambda: moe.store_pages(k, k, n.long(), pages, pages), "slots has to be contiguous"),
+        (lambda: moe.store_pages(k, k, n, codes, codes, scale, scale[..., :8]), "v_scale has to be contiguous"),
+        (lambda: moe.plan_pages(n, n, table, n, 16, 5), "on a GPU"),
+        (lambda: moe.plan_pages(n, n[:4], table, n, 16, 5), "more has to be contiguous"),
+        (lambda: moe.plan_pages(n.long(), n, table, n, 16, 5), "have has to be contiguous"),
+        (lambda: moe.plan_pages(n, n, table[:4], n, 16, 5), "table has to be contiguous"),
+        (lambda: moe.plan_pages(n, n, table[:, :1], n, 16, 5), "table has to be contiguous"),
+        (lambda: moe.plan_pages(n, n, table[0], n, 16, 5), r"table \[sequences, pages\]"),
+        (lambda: moe.plan_pages(n, n, table, n.long(), 16, 5), "free has to be contiguous"),
+        (lambda: moe.plan_pages(n, n, table, n, 16, 5, used=n), "used has to be contiguous"),
+    ]
+    for i, (call, what) in enumerate(calls):
+        print(i, what)
+        with pytest.raises(ValueError, match=what):
+            call()
