@@ -871,6 +871,42 @@ def test_streams_and_calls_at_once(lib):
     assert all(torch.equal(out[0], y) for y in out)
 
 
+def test_calls_at_once_of_different_work(lib):
+    """Calls on three streams, each with lengths, queries and rows of its own and so with other shares, pieces and parts in its workspace:
+    over pages, over rows with their keys in shares, and gradients in pieces and shares."""
+    jobs = []
+    for i, (lengths, each, keys, each2) in enumerate((([3000, 40, 900], [60, 9], [2500, 1900], [700, 41]), ([17, 5000], [100], [4000], [900]),
+                                                      ([2100, 1, 1300, 60], [5, 33, 20], [1800, 2000, 1700], [300, 300, 333]))):
+        g = gen(60 + i)
+        values, pages, _, table = paged(g, lengths, 2, 128, 16, BF16)
+        q = normal(g, len(lengths), 8, 128, dtype=BF16)
+        qr, k, v = normal(g, sum(each), 2, 64, dtype=BF16), normal(g, sum(keys), 1, 64, dtype=BF16), normal(g, sum(keys), 1, 64, dtype=BF16)
+        q2, k2, v2, dy2 = (normal(g, sum(each2), h, 64, dtype=BF16) for h in (8, 1, 1, 8))
+        offsets, k_offsets, offsets2, n = ints(starts(each)), ints(starts(keys)), ints(starts(each2)), ints(lengths)
+        assert lib.moe_attend_rows_bytes(sum(each), sum(keys), len(each), 2, 1, 64) > 0
+        want = (paged_reference(q, values, 0, 0, 128 ** -0.5), reference(qr, k, v, each, keys, 0, 0, 0.125)["y"],
+                *(reference(q2, k2, v2, each2, each2, 0, 0, 0.125, dy2)[x] for x in ("y", "dq", "dk", "dv")))
+
+        def run(q=q, pages=pages, table=table, n=n, rows=(qr, k, v, offsets), k_offsets=k_offsets, rows2=(q2, k2, v2, offsets2), dy2=dy2):
+            y = lib.attend_pages(q, *pages, table, n)
+            y1 = lib.attend_rows(*rows, k_offsets=k_offsets)
+            y2, kept = lib.attend_rows(*rows2, keep=True)
+            return (y, y1, y2, *lib.attend_rows_backward(*rows2, y2, kept, dy2))
+
+        jobs.append((torch.cuda.Stream(), run, want, []))
+    torch.cuda.synchronize()
+    for _ in range(6):
+        for stream, run, _, out in jobs:
+            with torch.cuda.stream(stream):
+                out.append(run())
+    torch.cuda.synchronize()
+    for _, _, want, out in jobs:
+        for got, (ref, bound), what in zip(out[0], want, ("pages", "shares", "y", "dq", "dk", "dv")):
+            close(got, ref, bound, what)
+        for other in out[1:]:
+            assert all(torch.equal(a, b) for a, b in zip(out[0], other))
+
+
 def test_offsets_in_a_large_cache(lib):
     """Pages beyond 2^32 bytes of the cache."""
     KV, page, D = 8, 64, 128
