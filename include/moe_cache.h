@@ -413,8 +413,8 @@ int moe_experts_rows_backward(int32_t weight_fmt, int32_t hidden, int32_t inter,
  * head; the values of a head are dense.  Pointers and strides of bf16 rows that are read are multiples of 16 bytes.
  *   A query at position p sees key j if j <= p and (window 0, or j > p - window, or j < sinks).
  *   z_j = softmax_scale <q, k_j>, y = sum_j exp(z_j - lse) v_j, lse = log sum_j exp(z_j), over the keys that it sees; y is 0 (lse
- *   -infinity) if there are none.  Sums are held in 32 bits.  What a query does not see
- *   may hold anything.
+ *   -infinity) if there are none, or if all z_j are -infinity.  Sums are held in 32 bits.  What a query does not see may hold anything;
+ *   a z_j that is NaN makes its y and lse NaN, infinities and NaN in values that it sees go into y.
  *
  * A cache has n_pages pages of `page` tokens (a power of two, 16 to 1024), page_stride elements from page to page:
  *   k_pages, v_pages [n_pages][n_kv_heads][page][head_dim]; page * n_pages < 2^31

@@ -305,6 +305,25 @@ def test_scores_of_minus_infinity(lib, dim, each, keys, heads, first, n):
     assert bool(torch.isfinite(keep.lse[:, some]).all())
 
 
+@pytest.mark.parametrize("each,keys,heads", [([200], None, 2), ([200], None, 100), ([30], [3000], 2)])
+def test_all_scores_minus_infinity(lib, each, keys, heads):
+    """As if nothing were seen: zeros and lse -infinity, in every form, over pages, too."""
+    g = gen(24)
+    nq, nk, dim = sum(each), sum(keys or each), 64
+    q, k, v = normal(g, nq, heads, dim, dtype=BF16), normal(g, nk, 1, dim, dtype=BF16), normal(g, nk, 1, dim, dtype=BF16)
+    q[:, 0, 3] = 1.0
+    k[:, :, 3] = -math.inf
+    q[:, 1:, 3] = 2.0
+    y, kept = lib.attend_rows(q, k, v, ints(starts(each)), k_offsets=ints(starts(keys or each)), keep=True)
+    assert not y.any() and bool((kept.lse == -math.inf).all())
+    n = 2900 if keys else 200  # (in shares, and by one workgroup)
+    pages = [torch.zeros(up(nk, 16) * 16, 1, dim, dtype=BF16, device=DEV) for _ in range(2)]
+    pages[0][:nk], pages[1][:nk] = k, v
+    pages = [p.view(-1, 16, 1, dim).transpose(1, 2).contiguous() for p in pages]
+    table = torch.arange(pages[0].shape[0], dtype=I32, device=DEV)[None]
+    assert not lib.attend_pages(q[:1], *pages, table, ints([n])).any()
+
+
 def test_gradients_of_other_sequences(lib):
     """An infinity or NaN stays in its sequence's gradients."""
     g = gen(7)
