@@ -17,8 +17,9 @@
 // one of them whole instead, its wavefronts every eighth tile, and joins through LDS: one launch (777 tokens 10.9 us, in two 12.9).
 //
 // Two wavefronts a SIMD with half the ring each, rather than one: what a wavefront does with a tile takes longer than its bytes.
-// Four sequences of up to 131072 tokens, 8 heads of 128 for 32, 1.25 GB in 222 + 7 us (5.6 TB/s; with one wavefront 252); 64 of up to
-// 8192 in 8 bits, 484 MB in 103 + 5 (177); 96 with a window of 4096, 4 heads of 64 for 32, 358 MB in 65 + 5 (100).
+// Pass after pass, both launches: four sequences of up to 131072 tokens, 8 heads of 128 for 32, 1.25 GB in 227 us (5.5 TB/s; with one
+// wavefront 252); 64 of up to 8192 in 8 bits, 484 MB in 103 (4.7 TB/s; 177); 96 with a window of 4096, 4 heads of 64 for 32, 358 MB in 76
+// (4.7 TB/s; 100).  In a trace, each launch by itself: 224 + 7, 114 (100 at least) + 5 and 66 + 5.
 #include <algorithm>
 
 #include "attend.h"

@@ -22,9 +22,9 @@
 // Which sequence and which of its rows a workgroup has is worked out from the offsets on the device.  Loads go through buffer
 // resources that end where the sequence ends: what lies beyond arrives as zeros.
 //
-// Measured: 16384 tokens, 32 heads of 128, 8 of k: 2080 us (1.06 PFLOP/s).  With gradients, 8192 tokens in five sequences, 16 heads of 128:
-// 104 + 145 + 175 + 5 us (0.63, 0.90, 0.75 PFLOP/s of the products that each makes); 20001 tokens in nine, 16 heads of 80, 2 of k, window 1000
-// and three first keys: 180 + 225 + 250 + 16.  16384 tokens: the matrix cores work 42 % of the time and the vector units as much again,
+// Measured: 16384 tokens, 32 heads of 128, 8 of k: 2080 to 2200 us, from card to card (1.06 to 1.00 PFLOP/s).  With gradients, on the slower of
+// these, 8192 tokens in five sequences, 16 heads of 128: 107 + 149 + 181 + 6 us (0.61, 0.88, 0.73 PFLOP/s of the products that each makes);
+// 20001 tokens in nine, 16 heads of 80, 2 of k, window 1000 and three first keys: 191 + 240 + 264 + 16.  16384 tokens: the matrix cores work 42 % of the time and the vector units as much again,
 // with two wavefronts a SIMD (what the registers allow).  Tried for the forward, of 2115 us: the same without the two steps 2120; matrix
 // instructions at a higher wave priority the same; 64 queries a wavefront and one of them a SIMD, half the reads of LDS, 2490.
 #include <algorithm>

@@ -4,7 +4,7 @@ Everything runs on the current stream of the tensors' device and returns at once
 to be ready there first, and be kept, as with any operator of PyTorch.  Shapes, types and places are checked ahead of the library
 (ValueError, in csrc/rows_torch.cpp, where the outputs are made, too), the rest by the library (MoEError).  Automatic
 differentiation is the caller's (examples/moe_layer.py): the calls record nothing, and while gradients are being recorded they
-refuse inputs that require one (ValueError).
+refuse inputs that require one (ValueError); inputs with a tangent of the forward mode they refuse, too.
 """
 from __future__ import annotations
 
