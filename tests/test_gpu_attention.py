@@ -281,6 +281,31 @@ def test_shares_of_keys_with_nan(lib):
             assert bool(y[:, 2:].isnan().all()) and bool(kept.lse[2:].isnan().all()) and bool(torch.isfinite(y[:, :2]).all()), (tile, n)
 
 
+@pytest.mark.parametrize("heads", [2, 48])
+def test_nan_in_queries(lib, heads):
+    """In every form without shares, and over pages by one workgroup and in shares: NaN for these queries and heads, values for the others."""
+    g = gen(25)
+    n, dim = 400, 64
+    q, k, v = normal(g, n, heads, dim, std=2.0, dtype=BF16), normal(g, n, 1, dim, dtype=BF16), normal(g, n, 1, dim, dtype=BF16)
+    want, bound = reference(q, k, v, [n], [n], 0, 0, 0.125)["y"]
+    bad = torch.zeros(n, heads, dtype=torch.bool, device=DEV)
+    for r in (0, 31, 130, 399):
+        q[r, 1, r % dim] = math.nan
+        bad[r, 1] = True
+    y, kept = lib.attend_rows(q, k, v, ints([0, n]), keep=True)
+    assert torch.equal(y.isnan(), bad[..., None].expand_as(y)) and torch.equal(kept.lse.isnan().t(), bad)
+    close(y[~bad], want[~bad], bound[~bad], "y")
+    for lengths in ([300], [3000, 40]):
+        values, pages, _, table = paged(g, lengths, 1, dim, 16, BF16)
+        one = normal(g, len(lengths), heads, dim, dtype=BF16)
+        want, bound = paged_reference(one, values, 0, 0, 0.125)
+        one[0, 1, 5] = math.nan
+        y = lib.attend_pages(one, *pages, table, ints(lengths))
+        assert bool(y[0, 1].isnan().all()) and int(y.isnan().sum()) == dim
+        fine = torch.isfinite(y)
+        close(y[fine], want[fine], bound[fine], "pages")
+
+
 @pytest.mark.parametrize("dim", [64, 80, 128])
 @pytest.mark.parametrize("each,keys,heads", [
     ([400], None, 2), ([400], None, 48),  # the keys divided among wavefronts; whole tiles by a workgroup
