@@ -14,10 +14,10 @@ constexpr int32_t row_within(int32_t at, int32_t rows) {
 struct RowRange {
   int32_t first, count;
 };
-// Both ends are brought into the range ahead of the difference, which then cannot pass 32 bits.  An end ahead of the first row: none.
+// The end is brought behind the first row ahead of the difference, which then cannot pass 32 bits.  An end ahead of the first row: none.
 constexpr RowRange row_range(int32_t from, int32_t to, int32_t rows) {
-  const int32_t first = row_within(from, rows), count = row_within(to, rows) - first;
-  return {first, count < 0 ? 0 : count};
+  const int32_t first = row_within(from, rows), below = to < rows ? to : rows;
+  return {first, (below > first ? below : first) - first};
 }
 
 }  // namespace moe
